@@ -53,7 +53,7 @@ typedef enum {
 } qzo_status;
 
 enum { QZO_ARCH_LLAMA = 0, QZO_ARCH_OPT = 1 };
-enum { QZO_DTYPE_BF16 = 0, QZO_DTYPE_F32 = 1, QZO_DTYPE_U32 = 2, QZO_DTYPE_I32 = 3 };
+enum { QZO_DTYPE_BF16 = 0, QZO_DTYPE_F32 = 1, QZO_DTYPE_U32 = 2, QZO_DTYPE_I32 = 3, QZO_DTYPE_E4M3 = 4 };
 
 /* Human-readable text of a status code (static storage). */
 const char* qzo_strerror(int status);
@@ -162,6 +162,97 @@ int qzo_perturbed_gemm_noalloc(const void* d_x_bf16, const void* d_wq, const voi
  * d_scales bf16 [count], in place.  g must be finite, clip >= 0. */
 int qzo_update_scales_flat(void* d_scales_bf16, int64_t count, uint64_t seed, uint64_t index_base,
                            float lr, float g, float clip, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Serving operators: what a tuned model needs to answer.  (The paper tunes by forward passes and evaluates
+ * the tuned model on question-answering tasks, Sec. 4.1; how it is served is this library's own design.)
+ * All of them can be captured into a CUDA graph: they launch kernels and do nothing else.
+ * Words "row", "slot", "position": a row is one token of this step; its position is its place in its
+ * request, 0 for the first token; its slot is where its key and value live in the paged cache, block id *
+ * block_size + place in the block.  A row with a negative position or slot is padding.
+ * d_status (int on the device, may be NULL): bit 1 is set when an index out of range is met (see each call).
+ * ---------------------------------------------------------------------------------- */
+
+/* Matrix-vector products with int4 weights and group scales, for up to QZO_GEMV_MAX_ROWS rows (the linear of
+ * qzo_perturbed_gemm at sign 0 for a step of few tokens):
+ *   Y[t][n] = sum_k X[t][k] s[k/128][n] q[k][n] (+ bias[n]).
+ * The products X q of a group of 128 are summed in fp32 (each is exact), then scaled in fp32.  Y is rounded once.
+ * d_x bf16 [M][ldx], 16-byte aligned, ldx a multiple of 8 and >= K; d_wq kernel layout (qzo_repack_int4); d_scales bf16
+ * [ceil(K/128)][N]; d_bias float [N] or NULL; d_y bf16 [M][ldy], ldy >= N, must not overlap d_x.  K and N multiples of 8. */
+#define QZO_GEMV_MAX_ROWS 16
+int qzo_gemv_int4(const void* d_x_bf16, int ldx, const void* d_wq, const void* d_scales_bf16, const float* d_bias,
+                  void* d_y_bf16, int ldy, int M, int K, int N, void* stream);
+
+/* A paged key-value cache of one layer, described by the caller (host struct, read during the call): keys and
+ * values in blocks [n_blocks][n_kv_heads][block_size][head_dim], 16-byte aligned.  dtype QZO_DTYPE_BF16 (both
+ * scales 1) or QZO_DTYPE_E4M3: the stored code times the scale (> 0) is the value; codes saturate at +-448.
+ * block_size is a power of two from 16 to 256, head_dim 64 or 128, n_blocks * block_size < 2^31. */
+typedef struct {
+  void* k;
+  void* v;
+  int dtype;
+  int n_blocks, block_size, n_kv_heads, head_dim;
+  float k_scale, v_scale;
+} qzo_kv_cache;
+
+/* Table of the rotation: float [max_pos][head_dim/2][2] = {cos, sin}(pos * theta^(-2i/head_dim)), the angles
+ * formed in fp64 (the table the model builds for itself).  max_pos * head_dim <= 2^30, head_dim 64 or 128. */
+int qzo_rope_table(float* d_table, int max_pos, int head_dim, float theta, void* stream);
+
+/* One pass over the new rows' queries, keys and values in front of the attention:
+ *   q'[t][h] = rot(norm(q[t][h]) q_gain),  k'[t][h] = rot(norm(k[t][h]) k_gain),  v'[t][h] = v[t][h],
+ * norm(x) = x / sqrt(mean(x^2) + norm_eps) over the head (left out, with its gain, where that gain is NULL), rot the
+ * rotation of the pairs (i, i + head_dim/2) by the row's position (left out when d_table is NULL).  q' goes to
+ * d_q_out, k' and v' into the cache at the row's slot; each is rounded once, from fp32.
+ * d_q bf16 [T][ldq] with head h at h * head_dim, d_k and d_v alike with n_kv_heads heads; 8-byte aligned, strides
+ * multiples of 4; d_q_out bf16 [T][ldqo], may be d_q itself (same stride) but not overlap it otherwise; gains float
+ * [head_dim], d_table as qzo_rope_table writes it (16-byte aligned).  d_positions, d_slots int32 [T]; the slots of one call are distinct.
+ * A row with a negative slot is padding: nothing of it is read or written.  A slot beyond the cache or a position
+ * outside [0, max_pos) sets bit 1 of the status word: the first is not written, the second is turned by the nearest position. */
+int qzo_qk_norm_rope_cache(const void* d_q_bf16, int ldq, const void* d_k_bf16, int ldk, const void* d_v_bf16, int ldv,
+                           const float* d_q_gain, const float* d_k_gain, float norm_eps, const float* d_table,
+                           int max_pos, const int32_t* d_positions, const int32_t* d_slots, void* d_q_out_bf16,
+                           int ldqo, const qzo_kv_cache* cache, int T, int n_heads, int* d_status, void* stream);
+
+/* Workspace of qzo_paged_attention for R rows over tables of max_len = table_width * block_size tokens (0 if none: the
+ * partial results of rows whose cache is split over several CTAs otherwise). */
+int qzo_paged_attention_workspace_bytes(int R, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes);
+
+/* Attention of one new token per row over the paged cache:
+ *   out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,  j = 0 .. position[t] (the row's own key among them),
+ * with keys and values of head h / (n_heads / n_kv_heads) found through the block table: token j of request r lives in
+ * block d_block_table[r][j / block_size].  A row with a negative position gives zeros.
+ * Several rows may belong to one request (a prompt's rows, each of which sees the keys up to its own).
+ * d_q bf16 [R][ldq] and d_out bf16 [R][ldo], head h at h * head_dim, 16-byte aligned, strides multiples of 8, not
+ * overlapping; d_block_table int32 [n_seqs][table_width]; d_row_seq int32 [R] = the request of each row, NULL: row t is
+ * request t (R <= n_seqs); scale > 0 (1 / sqrt(head_dim) as a rule); n_heads a multiple of n_kv_heads.
+ * d_workspace: qzo_paged_attention_workspace_bytes, 256-aligned; calls that may run at the same time (two streams, two
+ * captured graphs) need one each.  Nothing in it outlives the call.
+ * A request outside [0, n_seqs), a position beyond the table or a block id outside the cache sets bit 1 of the status
+ * word; such a row sees nothing, only the table's tokens, or nothing of that block. */
+int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache, const int32_t* d_block_table,
+                        int n_seqs, int table_width, const int32_t* d_row_seq, const int32_t* d_positions, float scale,
+                        void* d_out_bf16, int ldo, int R, int n_heads, void* d_workspace, size_t workspace_bytes,
+                        int* d_status, void* stream);
+
+/* Block tables and slot maps of a step, built on the device from the requests' lengths.
+ * d_lens int32 [B]: tokens each request holds in the cache; d_new int32 [B]: tokens it adds in this step, 0 for none,
+ * negative when it is finished.  d_block_table int32 [B][table_width]: entry j of request r names the block of its tokens
+ * j * block_size ...; entries beyond its length mean nothing.  d_free int32 [free_capacity], d_free_count int32 [1]: the
+ * stack of free blocks, its top at [count - 1].  In the order of the requests,
+ *  - the blocks of finished requests are pushed on the stack (first entry first);
+ *  - then each growing request takes the blocks it lacks from the top, one after the other, into its table;
+ *  - rows are numbered request by request: d_row_seq, d_positions, d_slots int32 [max_rows], -1 behind the last row;
+ *  - d_lens_out int32 [B] = the new lengths (0 for finished requests), d_free_count_out int32 [1] = the new count.
+ * d_lens_out may be d_lens and d_free_count_out may be d_free_count; no other arguments overlap.
+ * When the step cannot be served (too few free blocks, a table too narrow, more rows than max_rows, a negative length, a
+ * stack beyond its capacity), nothing is changed: lengths and count are handed on as they are, every row is padding, and
+ * bit 2 of the status word is set.  B from 1 to QZO_MAX_REQUESTS, block_size as in qzo_kv_cache. */
+#define QZO_MAX_REQUESTS 4096
+int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int B, int32_t* d_block_table, int table_width,
+                     int block_size, int32_t* d_free, int free_capacity, const int32_t* d_free_count, int max_rows,
+                     int32_t* d_row_seq, int32_t* d_positions, int32_t* d_slots, int32_t* d_lens_out,
+                     int32_t* d_free_count_out, int* d_status, void* stream);
 
 /* ------------------------------------------------------------------------------------
  * Model-level entry points
@@ -285,6 +376,19 @@ int qzo_enable_joint_spsa(qzo_model* m, void* d_workspace, size_t workspace_byte
 int qzo_step_host(qzo_model* m, const int32_t* h_tokens, const int32_t* h_labels, int B, int S,
                   uint64_t seed, float eps, float lr, float clip, float* h_out);
 
+/* One step of answering with the tuned model: R rows (new tokens of any requests, prompts' tokens among them) go
+ * through the unperturbed model, their keys and values into the paged cache, and d_logits (float [R][vocab], 16-byte
+ * aligned) receives the logits of each row.  Every row attends to its request's cached tokens up to itself, so a prompt is
+ * a step of its own rows (the keys of all rows of a layer are written before its attention reads them).
+ * h_caches: HOST array of n_layers cache descriptions (n_kv_heads = n_heads of the model); d_tokens, d_row_seq,
+ * d_positions, d_slots int32 [R], as qzo_assign_slots writes the last three; R <= max_tokens; positions < max_seq.
+ * Rows of padding (negative position or slot) give logits that mean nothing and touch no cache.  An index out of range
+ * (token, position, slot, block) sets bit 1 of the model's status word (qzo_device_status).
+ * Up to QZO_GEMV_MAX_ROWS rows the linears run as qzo_gemv_int4, above as qzo_perturbed_gemm with sign 0.  Asynchronous on the model's stream. */
+int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
+               const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
+               int table_width, float* d_logits);
+
 /* The trainable state (the inputs of Algorithm 1: the quantisation scales Delta that the caller hands over
  * and gets back).  linear_id = layer * L + position, L = 7 (Llama: q,k,v,o,gate,up,down) or 6 (OPT:
  * q,k,v,o,fc1,fc2): copies that linear's bf16 [G][N] scales out of / into the model's flat buffer;
@@ -314,7 +418,8 @@ int qzo_debug_gemm_wait_expiry(const void* d_x_bf16, const void* d_wq, const voi
                                void* stream);
 
 /* Reads the device status word: bit 0 = a bounded device-side wait expired in some launch since init
- * (returns QZO_ERR_DEVICE_TIMEOUT), bit 1 = a token id outside [0, vocab) was seen (QZO_ERR_BAD_ARG);
+ * (returns QZO_ERR_DEVICE_TIMEOUT), bit 1 = a token id outside [0, vocab) was seen, or in qzo_decode another index
+ * out of range (QZO_ERR_BAD_ARG);
  * 0 = nothing to report.  Synchronises. */
 int qzo_device_status(qzo_model* m, int* h_status);
 /* Overwrites the status word from the host (0 clears it).  For tests of the error path of a step and

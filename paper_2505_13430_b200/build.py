@@ -6,8 +6,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqzo.so")
-SOURCES = ["prims.cu", "gemm_w4a16.cu", "layers.cu", "model.cu"]
-HEADERS = ["qzo_common.cuh", "philox.cuh", "launch.cuh", "layers.cuh", os.path.join("..", "..", "include", "qzo.h")]
+SOURCES = ["prims.cu", "gemm_w4a16.cu", "layers.cu", "model.cu", "gemv_w4.cu", "paged.cu", "slots.cu"]
+HEADERS = ["qzo_common.cuh", "philox.cuh", "launch.cuh", "layers.cuh", "mma.cuh", os.path.join("..", "..", "include", "qzo.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 

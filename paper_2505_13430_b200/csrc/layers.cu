@@ -50,15 +50,20 @@ __device__ __forceinline__ float block_max(float v, float* red) {
 // index pert.base + tok * d + j; rows from pert.pair_rows on (the second copy of a paired step) take -eps.
 struct EmbedPerturb { unsigned long long seed, base; float sign_eps; int pair_rows; };
 
+// positions (may be null): the row's position, of S learned ones, instead of t % S; a negative one marks a row of
+// padding, whose token is not looked at; one beyond S - 1 is reported like a bad token.
 __global__ void embedding_kernel(const int32_t* __restrict__ tokens, const __nv_bfloat16* __restrict__ embed,
-                                 const __nv_bfloat16* __restrict__ pos, int S, int d, int vocab,
-                                 __nv_bfloat16* __restrict__ x, int* __restrict__ status, EmbedPerturb pert) {
+                                 const __nv_bfloat16* __restrict__ pos, const int32_t* __restrict__ positions, int S, int d,
+                                 int vocab, __nv_bfloat16* __restrict__ x, int* __restrict__ status, EmbedPerturb pert) {
   const int t = blockIdx.x;
-  int tok = tokens[t];
+  int at = positions ? positions[t] : t % S;
+  int tok = at < 0 ? 0 : tokens[t];
+  if (at >= S && threadIdx.x == 0 && status != nullptr) atomicOr(status, kStatusBadToken);
+  at = min(max(at, 0), S - 1);
   if ((tok < 0 || tok >= vocab) && threadIdx.x == 0 && status != nullptr) atomicOr(status, kStatusBadToken);
   tok = min(max(tok, 0), vocab - 1);
   const uint2* e = reinterpret_cast<const uint2*>(embed + (size_t)tok * d);
-  const uint2* pp = pos ? reinterpret_cast<const uint2*>(pos + (size_t)(t % S) * d) : nullptr;
+  const uint2* pp = pos ? reinterpret_cast<const uint2*>(pos + (size_t)at * d) : nullptr;
   uint2* o = reinterpret_cast<uint2*>(x + (size_t)t * d);
   const float se = (pert.pair_rows > 0 && t >= pert.pair_rows) ? -pert.sign_eps : pert.sign_eps;
   for (int i = threadIdx.x; i < d / 4; i += blockDim.x) {       // four elements = one counter block (d % 8 == 0)
@@ -495,10 +500,10 @@ __global__ void set_step_params_kernel(StepParams* __restrict__ dst, StepParams 
 
 int launch_embedding(const int32_t* tokens, const __nv_bfloat16* embed, const __nv_bfloat16* pos, int T, int S, int d,
                      int vocab, __nv_bfloat16* x, int* status, uint64_t seed, uint64_t index_base, float sign_eps,
-                     int pair_rows, cudaStream_t st) {
+                     int pair_rows, cudaStream_t st, const int32_t* positions) {
   if ((d % 8) || (index_base % 4)) return QZO_ERR_BAD_ARG;
   const EmbedPerturb pert{seed, index_base, sign_eps, pair_rows};
-  QZO_LAUNCH(embedding_kernel, dim3(T), dim3(128), 0, st, tokens, embed, pos, S, d, vocab, x, status, pert);
+  QZO_LAUNCH(embedding_kernel, dim3(T), dim3(128), 0, st, tokens, embed, pos, positions, S, d, vocab, x, status, pert);
   return QZO_OK;
 }
 int launch_add_rmsnorm(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* w2, int pair_rows,

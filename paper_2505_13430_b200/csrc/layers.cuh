@@ -3,10 +3,11 @@
 #include "qzo_common.cuh"
 
 namespace qzo {
+// positions (may be null): each row's position instead of t % S, negative for padding
 // sign_eps != 0: rows are perturbed as E + sign_eps z(seed, index_base + tok d + j); rows from pair_rows on take -sign_eps
 int launch_embedding(const int32_t* tokens, const __nv_bfloat16* embed, const __nv_bfloat16* pos, int T, int S, int d,
                      int vocab, __nv_bfloat16* x, int* status, uint64_t seed, uint64_t index_base, float sign_eps,
-                     int pair_rows, cudaStream_t st);
+                     int pair_rows, cudaStream_t st, const int32_t* positions = nullptr);
 // x <- x + delta (skipped when delta is null), then y = norm(x); y may alias delta.  pair_rows > 0: rows from
 // pair_rows on use the gains (and biases) w2 (b2).
 int launch_add_rmsnorm(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* w2, int pair_rows,
@@ -57,4 +58,18 @@ int launch_perturbed_gemm_group(const __nv_bfloat16* d_x, int M, int K, const Ge
 void set_gemm_wait_debug(long long limit_cycles, int skip_group);
 int launch_bf16_gemm_f32out(const __nv_bfloat16* d_x, const __nv_bfloat16* d_w, float* d_out, int M, int K, int N,
                             int* d_status, cudaStream_t st);
+
+// gemv_w4.cu: the unperturbed linears for up to QZO_GEMV_MAX_ROWS rows; ldx a multiple of 8
+int launch_gemv_group(const __nv_bfloat16* d_x, int ldx, int M, int K, const GemmLinear* lins, int n_lin, cudaStream_t st);
+
+// paged.cu
+bool cache_ok(const qzo_kv_cache* c);
+int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat16* k, int ldk, const __nv_bfloat16* v, int ldv,
+                              const float* q_gain, const float* k_gain, float norm_eps, const float* table, int max_pos,
+                              const int32_t* positions, const int32_t* slots, __nv_bfloat16* q_out, int ldqo,
+                              const qzo_kv_cache& c, int T, int H, int* status, cudaStream_t st);
+size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len);
+int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
+                           const int32_t* row_seq, const int32_t* positions, float scale, __nv_bfloat16* out, int ldo, int R,
+                           int H, void* ws, size_t ws_bytes, int* status, cudaStream_t st);
 }  // namespace qzo

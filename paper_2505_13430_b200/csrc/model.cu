@@ -333,6 +333,64 @@ int forward_loss(qzo_model* m, const int32_t* d_tokens, const int32_t* d_labels,
   return QZO_OK;
 }
 
+// The unperturbed linears of a decode step: the matrix-vector kernel up to its row limit, the GEMM above.
+static int decode_linears(qzo_model* m, const Linear* const* Ls, __nv_bfloat16* const* outs, int n, int ldo,
+                          const __nv_bfloat16* in, int R) {
+  if (R > QZO_GEMV_MAX_ROWS) return linears(m, Ls, outs, n, ldo, in, R, 0, 0, 1.0f, 0);
+  GemmLinear g[kMaxGroupedLinears];
+  for (int j = 0; j < n; ++j)
+    g[j] = GemmLinear{Ls[j]->wq, m->scales + Ls[j]->idx_base, Ls[j]->bias, outs[j], ldo, Ls[j]->N, 0};
+  return launch_gemv_group(in, Ls[0]->K, R, Ls[0]->K, g, n, m->stream);
+}
+
+// One step of answering: R rows through the unperturbed model over the paged caches of its layers.
+int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, const int32_t* row_seq, const int32_t* positions,
+           const int32_t* slots, int R, const int32_t* table, int n_seqs, int width, float* d_logits) {
+  const qzo_model_desc& d = m->desc;
+  const int dm = d.d_model, H = d.n_heads, dh = dm / H, F = d.d_ffn;
+  const bool llama = d.arch == QZO_ARCH_LLAMA;
+  const float scale = 1.0f / sqrtf((float)dh);
+  cudaStream_t st = m->stream;
+  // the logits of the training forwards are not needed here: their buffer holds the attention's partial results
+  const size_t ws_bytes = (size_t)2 * m->max_tokens * d.vocab * sizeof(float);
+  m->last_T = 0;
+  QZO_TRY(launch_embedding(tokens, m->embed, llama ? nullptr : m->pos_embed, R, d.max_seq, dm, d.vocab, m->x, m->status, 0, 0,
+                           0.0f, 0, st, positions));
+  const __nv_bfloat16* pending = nullptr;
+  for (int li = 0; li < d.n_layers; ++li) {
+    const Layer& L = m->layers[li];
+    QZO_TRY(add_norm(m, m->x, pending, L.norm1_w, L.norm1_b, 0, 0, 0, R, m->xn));
+    const Linear* qkv_l[3] = {&L.lin[0], &L.lin[1], &L.lin[2]};
+    __nv_bfloat16* qkv_o[3] = {m->qkv, m->qkv + dm, m->qkv + 2 * dm};
+    QZO_TRY(decode_linears(m, qkv_l, qkv_o, 3, 3 * dm, m->xn, R));
+    QZO_TRY(launch_qk_norm_rope_cache(m->qkv, 3 * dm, m->qkv + dm, 3 * dm, m->qkv + 2 * dm, 3 * dm, nullptr, nullptr, 0.0f,
+                                      llama ? m->rope_cs : nullptr, d.max_seq, positions, slots, m->qkv, 3 * dm, caches[li], R, H,
+                                      m->status, st));
+    QZO_TRY(launch_paged_attention(m->qkv, 3 * dm, caches[li], table, n_seqs, width, row_seq, positions, scale, m->att, dm, R, H,
+                                   m->logits, ws_bytes, m->status, st));
+    const Linear* o_l[1] = {&L.lin[3]};
+    __nv_bfloat16* xn_o[1] = {m->xn};
+    QZO_TRY(decode_linears(m, o_l, xn_o, 1, dm, m->att, R));
+    QZO_TRY(add_norm(m, m->x, m->xn, L.norm2_w, L.norm2_b, 0, 0, 0, R, m->xn));
+    if (llama) {
+      const Linear* gu_l[2] = {&L.lin[4], &L.lin[5]};
+      __nv_bfloat16* gu_o[2] = {m->mlp_a, m->mlp_b};
+      QZO_TRY(decode_linears(m, gu_l, gu_o, 2, F, m->xn, R));
+      QZO_TRY(launch_silu_mul(m->mlp_a, m->mlp_b, m->mlp_a, (int64_t)R * F, st));
+    } else {
+      const Linear* fc1_l[1] = {&L.lin[4]};
+      __nv_bfloat16* fc1_o[1] = {m->mlp_a};
+      QZO_TRY(decode_linears(m, fc1_l, fc1_o, 1, F, m->xn, R));
+      QZO_TRY(launch_relu(m->mlp_a, (int64_t)R * F, st));
+    }
+    const Linear* down_l[1] = {&L.lin[llama ? 6 : 5]};
+    QZO_TRY(decode_linears(m, down_l, xn_o, 1, dm, m->mlp_a, R));
+    pending = m->xn;
+  }
+  QZO_TRY(add_norm(m, m->x, pending, m->final_norm_w, m->final_norm_b, 0, 0, 0, R, m->xn));
+  return launch_bf16_gemm_f32out(m->xn, m->lm_head, d_logits, R, dm, d.vocab, m->status, st);
+}
+
 int check_batch(const qzo_model* m, const void* tok, const void* lab, int B, int S) {
   if (!m || !tok || !lab || B <= 0 || S <= 0) return QZO_ERR_BAD_ARG;
   if (S > m->desc.max_seq) return QZO_ERR_BAD_ARG;
@@ -821,6 +879,21 @@ int qzo_forward_loss(qzo_model* m, const int32_t* d_tokens, const int32_t* d_lab
   QZO_TRY(check_batch(m, d_tokens, d_labels, B, S));
   if (!d_loss || sign < -1 || sign > 1 || !(eps > 0.0f)) return QZO_ERR_BAD_ARG;
   return forward_loss(m, d_tokens, d_labels, B, S, seed, sign, eps, d_loss, nullptr, false);
+}
+
+int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
+               const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
+               int table_width, float* d_logits) {
+  if (!m || !h_caches || !d_tokens || !d_row_seq || !d_positions || !d_slots || !d_block_table || !d_logits) return QZO_ERR_BAD_ARG;
+  if (R <= 0 || n_seqs <= 0 || table_width <= 0 || ((uintptr_t)d_logits & 15)) return QZO_ERR_BAD_ARG;
+  if (R > m->max_tokens) return QZO_ERR_WORKSPACE;
+  const qzo_model_desc& d = m->desc;
+  for (int li = 0; li < d.n_layers; ++li) {
+    const qzo_kv_cache& c = h_caches[li];
+    if (!cache_ok(&c) || c.n_kv_heads != d.n_heads || c.head_dim != d.d_model / d.n_heads) return QZO_ERR_BAD_ARG;
+    if ((int64_t)table_width * c.block_size > INT32_MAX) return QZO_ERR_BAD_ARG;
+  }
+  return decode(m, h_caches, d_tokens, d_row_seq, d_positions, d_slots, R, d_block_table, n_seqs, table_width, d_logits);
 }
 
 int qzo_update_scales(qzo_model* m, uint64_t seed, float lr, float g, float clip) {

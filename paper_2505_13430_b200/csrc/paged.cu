@@ -1,0 +1,619 @@
+// The paged key-value cache of the serving path: head norms, rotation and cache write in one pass over the new rows, and
+// the attention of one new token per row over the cache.
+#include "qzo_common.cuh"
+#include "launch.cuh"
+#include "layers.cuh"
+#include "mma.cuh"
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <math.h>
+
+#include <algorithm>
+
+namespace qzo {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// =========================================================================================
+// Head norms, rotation, cache write
+// =========================================================================================
+
+struct RopeCacheParams {
+  const __nv_bfloat16 *q, *k, *v;
+  int ldq, ldk, ldv;
+  const float *q_gain, *k_gain;
+  float norm_eps;
+  const float* table;
+  int max_pos;
+  const int32_t *positions, *slots;
+  __nv_bfloat16* q_out;
+  int ldqo;
+  void *ck, *cv;
+  float inv_k_scale, inv_v_scale;
+  int n_slots, log2_block, H, Hkv;
+  int64_t items;
+  int* status;
+};
+
+__device__ __forceinline__ void unpack4(uint2 r, float v[4]) {
+  const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&r.x));
+  const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&r.y));
+  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+}
+__device__ __forceinline__ uint2 pack4_bf16(const float v[4]) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+__device__ __forceinline__ uint32_t pack4_e4m3(const float v[4]) {
+  const __nv_fp8x2_storage_t a = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
+  const __nv_fp8x2_storage_t b = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
+  return (uint32_t)a | ((uint32_t)b << 16);
+}
+
+// DH / 8 lanes per head; a lane holds elements 4 l .. 4 l + 3 of the lower half and their partners of the upper half, so a
+// pair is turned inside a lane and the norm's sum takes log2(DH / 8) shuffles.
+template <int DH, bool F8>
+__global__ void __launch_bounds__(256)
+qk_norm_rope_cache_kernel(const RopeCacheParams p) {
+  constexpr int LPH = DH / 8;
+  const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int64_t item = idx / LPH;
+  const int l = (int)(idx % LPH);
+  const int heads = p.H + 2 * p.Hkv;
+  const bool live = item < p.items;
+  const int t = live ? (int)(item / heads) : 0, hh = live ? (int)(item % heads) : 0;
+  const int slot = live ? p.slots[t] : -1;
+  const bool is_q = hh < p.H, is_v = hh >= p.H + p.Hkv;
+  const int h = is_q ? hh : is_v ? hh - p.H - p.Hkv : hh - p.H;
+  float lo[4] = {}, hi[4] = {};
+  if (slot >= 0) {
+    const __nv_bfloat16* src = is_q ? p.q + (size_t)t * p.ldq : is_v ? p.v + (size_t)t * p.ldv : p.k + (size_t)t * p.ldk;
+    src += h * DH + 4 * l;
+    unpack4(*reinterpret_cast<const uint2*>(src), lo);
+    unpack4(*reinterpret_cast<const uint2*>(src + DH / 2), hi);
+  }
+  const float* gain = is_v ? nullptr : is_q ? p.q_gain : p.k_gain;
+  float ss = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) ss += lo[e] * lo[e] + hi[e] * hi[e];
+#pragma unroll
+  for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  if (slot < 0) return;
+  if (gain) {
+    const float r = rsqrtf(ss * (1.0f / DH) + p.norm_eps);
+    const float4 ga = *reinterpret_cast<const float4*>(gain + 4 * l), gb = *reinterpret_cast<const float4*>(gain + DH / 2 + 4 * l);
+    lo[0] *= r * ga.x; lo[1] *= r * ga.y; lo[2] *= r * ga.z; lo[3] *= r * ga.w;
+    hi[0] *= r * gb.x; hi[1] *= r * gb.y; hi[2] *= r * gb.z; hi[3] *= r * gb.w;
+  }
+  if (p.table && !is_v) {
+    const int given = p.positions[t];
+    const int pos = min(max(given, 0), p.max_pos - 1);
+    if (pos != given && l == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+    const float4* cs = reinterpret_cast<const float4*>(p.table + 2 * ((size_t)pos * (DH / 2) + 4 * l));
+    const float4 c01 = cs[0], c23 = cs[1];
+    const float c[4] = {c01.x, c01.z, c23.x, c23.z}, s[4] = {c01.y, c01.w, c23.y, c23.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float a = lo[e], b = hi[e];
+      lo[e] = a * c[e] - b * s[e];
+      hi[e] = b * c[e] + a * s[e];
+    }
+  }
+  if (is_q) {
+    __nv_bfloat16* dst = p.q_out + (size_t)t * p.ldqo + h * DH + 4 * l;
+    *reinterpret_cast<uint2*>(dst) = pack4_bf16(lo);
+    *reinterpret_cast<uint2*>(dst + DH / 2) = pack4_bf16(hi);
+    return;
+  }
+  if (slot >= p.n_slots) {
+    if (l == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+    return;
+  }
+  const size_t row = (((size_t)(slot >> p.log2_block) * p.Hkv + h) << p.log2_block) + (slot & ((1 << p.log2_block) - 1));
+  const size_t at = row * DH + 4 * l;
+  void* pages = is_v ? p.cv : p.ck;
+  if (F8) {
+    const float inv = is_v ? p.inv_v_scale : p.inv_k_scale;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { lo[e] *= inv; hi[e] *= inv; }
+    uint8_t* dst = (uint8_t*)pages + at;
+    *reinterpret_cast<uint32_t*>(dst) = pack4_e4m3(lo);
+    *reinterpret_cast<uint32_t*>(dst + DH / 2) = pack4_e4m3(hi);
+  } else {
+    __nv_bfloat16* dst = (__nv_bfloat16*)pages + at;
+    *reinterpret_cast<uint2*>(dst) = pack4_bf16(lo);
+    *reinterpret_cast<uint2*>(dst + DH / 2) = pack4_bf16(hi);
+  }
+}
+
+// =========================================================================================
+// Attention of one new token per row
+// =========================================================================================
+
+constexpr int kAttWarps = 4;
+constexpr int kTileKeys = 16;                          // keys a warp takes at a time: one matrix tile
+constexpr int kSplitKeys = kAttWarps * kTileKeys;      // a split is a multiple of what its warps take together
+
+struct PagedParams {
+  const __nv_bfloat16* q;
+  int ldq;
+  const void *ck, *cv;
+  const int32_t* table;
+  int n_seqs, width;
+  const int32_t *row_seq, *positions;
+  float scale_log2e, v_scale;                          // the keys' scale is in the first
+  __nv_bfloat16* out;
+  int ldo, R, H, Hkv, G, chunks, splits, n_blocks, log2_block;
+  float *part_o, *part_ml;                             // [R][H][splits][DH], [R][H][splits][2]
+  int* status;
+};
+
+// Keys of split s of a row that sees len keys: [s * per, min(len, (s + 1) * per)).
+__device__ __forceinline__ int split_keys(int len, int splits) {
+  return ((len + splits - 1) / splits + kSplitKeys - 1) / kSplitKeys * kSplitKeys;
+}
+// Number of keys a row sees, 0 for padding; seq receives its request.  One thread reports what is out of range.
+__device__ __forceinline__ int row_keys(const PagedParams& p, int row, int* seq, bool report) {
+  const int pos = p.positions[row];
+  if (pos < 0) return 0;
+  const int s = p.row_seq ? p.row_seq[row] : row;
+  *seq = s;
+  const int most = p.width << p.log2_block;
+  const bool bad_seq = s < 0 || s >= p.n_seqs;
+  if ((bad_seq || pos >= most) && report && p.status) atomicOr(p.status, kStatusBadToken);
+  return bad_seq ? 0 : min(pos, most - 1) + 1;
+}
+
+// A row none of whose keys has a score above -inf (no key at all, or only blocks that are out of range) gives zeros.
+__device__ __forceinline__ float inverse_sum(const PagedParams& p, float sum) { return sum == 0.0f ? 0.0f : p.v_scale / sum; }
+
+__device__ __forceinline__ uint32_t pair_lo(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x5410); }
+__device__ __forceinline__ uint32_t pair_hi(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xFFFFu), __NV_E4M3);
+  return (uint32_t)h.x | ((uint32_t)h.y << 16);
+}
+
+// What one lane holds of a key row: NW words of two elements each, the row's 16-byte chunks t, t + 4, ... in order.
+// Values: the same for the chunks that belong to lane g.  8-bit codes become fp16 pairs, which hold them exactly.
+template <int DH, bool F8>
+struct Layout {
+  static constexpr int kRowBytes = DH * (F8 ? 1 : 2);
+  static constexpr int kKeyLoads = kRowBytes / 64;                       // 16-byte loads a lane of four makes
+  static constexpr int kKeyWords = DH / 8;                               // element pairs of a lane: DH / 4 elements
+  static constexpr int kKeyStep = F8 ? 16 : 8;                           // elements of a load
+  static constexpr int kValWords = DH / 16;                              // element pairs of one of eight lanes
+};
+
+template <int DH, bool F8>
+__device__ __forceinline__ void load_key(const uint8_t* row, int t, uint4 raw[Layout<DH, F8>::kKeyLoads]) {
+#pragma unroll
+  for (int j = 0; j < Layout<DH, F8>::kKeyLoads; ++j) raw[j] = load_stream16(row + 16 * (t + 4 * j));
+}
+template <int DH, bool F8>
+__device__ __forceinline__ void key_words(const uint4 raw[Layout<DH, F8>::kKeyLoads], uint32_t w[Layout<DH, F8>::kKeyWords]) {
+#pragma unroll
+  for (int j = 0; j < Layout<DH, F8>::kKeyLoads; ++j) {
+    const uint32_t r[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (F8) {
+        w[8 * j + 2 * i] = e4m3x2_to_f16x2(r[i]);
+        w[8 * j + 2 * i + 1] = e4m3x2_to_f16x2(r[i] >> 16);
+      } else {
+        w[4 * j + i] = r[i];
+      }
+    }
+  }
+}
+// Value words of lane g: element e of the list is dimension val_dim(g, e)
+template <int DH, bool F8>
+__device__ __forceinline__ int val_dim(int g, int e) {
+  if (!F8 && DH == 128) return (e & 7) + 8 * g + (e >> 3) * 64;
+  return (DH / 8) * g + e;
+}
+template <int DH, bool F8>
+struct ValRaw { uint32_t w[DH * (F8 ? 1 : 2) / 32]; };
+
+template <int DH, bool F8>
+__device__ __forceinline__ void load_val(const uint8_t* row, int g, ValRaw<DH, F8>& raw) {
+  if (F8 && DH == 64) {
+    const uint2 v = load_stream8(row + 8 * g);
+    raw.w[0] = v.x; raw.w[1] = v.y;
+  } else {
+#pragma unroll
+    for (int j = 0; j < DH * (F8 ? 1 : 2) / 128; ++j) {
+      const uint4 v = load_stream16(row + 16 * (g + 8 * j));
+      raw.w[4 * j] = v.x; raw.w[4 * j + 1] = v.y; raw.w[4 * j + 2] = v.z; raw.w[4 * j + 3] = v.w;
+    }
+  }
+}
+template <int DH, bool F8>
+__device__ __forceinline__ uint32_t val_word(const ValRaw<DH, F8>& raw, int u) {
+  if (!F8) return raw.w[u];
+  return e4m3x2_to_f16x2(raw.w[u >> 1] >> (16 * (u & 1)));
+}
+template <bool F8>
+__device__ __forceinline__ void mma_step(float c[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (F8) mma16816_f16(c, a0, a1, a2, a3, b0, b1);
+  else mma16816_bf16(c, a0, a1, a2, a3, b0, b1);
+}
+
+// A CTA = one row, one key head, up to 8 NT of the query heads that share it, one split of its keys; its warps take the
+// split's tiles of 16 keys in turn, each with its own running maximum and sum, and are joined at the end.
+// A tile is two products: S^T = K Q^T (keys x heads) and O^T += V^T P^T (dimensions x heads), so up to eight heads
+// share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.
+template <int DH, int NT, bool F8>
+__global__ void __launch_bounds__(kAttWarps * 32)
+paged_attention_kernel(const PagedParams p) {
+  using Lay = Layout<DH, F8>;
+  __shared__ float sm_o[kAttWarps][8 * NT][DH + 4];
+  __shared__ float sm_m[kAttWarps][8 * NT], sm_l[kAttWarps][8 * NT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int per_row = p.Hkv * p.chunks;
+  const int row = blockIdx.x / per_row, hk = blockIdx.x % per_row / p.chunks, chunk = blockIdx.x % p.chunks;
+  const int head0 = hk * p.G + chunk * 8 * NT;                       // first query head of the CTA
+  const int n_heads = min(8 * NT, p.G - chunk * 8 * NT);
+  const int split = blockIdx.y;
+  int seq = 0;
+  const int len = row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
+  const int per = split_keys(len, p.splits);
+  const int k0 = split * per, k1 = min(len, k0 + per);
+  if (k0 >= k1) {
+    if (len == 0 && split == 0)
+      for (int i = threadIdx.x; i < n_heads * DH / 8; i += kAttWarps * 32)
+        *reinterpret_cast<uint4*>(p.out + (size_t)row * p.ldo + (size_t)head0 * DH + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
+    return;
+  }
+
+  // Query fragments, the same chunks of dimensions as a key's lane t.  For 8-bit keys they become fp16: scaled by a power
+  // of two that brings the head's largest element to [64, 128), which only elements 2^-30 below it can feel.
+  uint32_t qf[NT][Lay::kKeyWords];
+  float unscale[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const bool have = nt * 8 + g < n_heads;
+    const __nv_bfloat16* qr = p.q + (size_t)row * p.ldq + (size_t)(head0 + (have ? nt * 8 + g : 0)) * DH;
+#pragma unroll
+    for (int j = 0; j < Lay::kKeyLoads; ++j)
+#pragma unroll
+      for (int i = 0; i < Lay::kKeyStep / 8; ++i) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (have) v = *reinterpret_cast<const uint4*>(qr + Lay::kKeyStep * (t + 4 * j) + 8 * i);
+        uint32_t* w = qf[nt] + Lay::kKeyStep / 2 * j + 4 * i;
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+      }
+    unscale[nt][0] = unscale[nt][1] = 1.0f;
+    if (F8) {
+      float big = 0.0f;
+#pragma unroll
+      for (int i = 0; i < Lay::kKeyWords; ++i) {
+        const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[nt][i]));
+        big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+      }
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+      big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+      const int e = (big > 0.0f && big < INFINITY) ? ilogbf(big) - 6 : 0;
+#pragma unroll
+      for (int i = 0; i < Lay::kKeyWords; ++i) {
+        const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[nt][i]));
+        const __half2 h = __floats2half2_rn(ldexpf(f.x, -e), ldexpf(f.y, -e));
+        qf[nt][i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      const float un = ldexpf(1.0f, e);
+      unscale[nt][0] = __shfl_sync(0xffffffffu, un, 8 * t);
+      unscale[nt][1] = __shfl_sync(0xffffffffu, un, 8 * t + 4);
+    }
+  }
+
+  float o[NT][DH / 16][4];
+  float m[NT][2], l[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    m[nt][0] = m[nt][1] = -INFINITY;
+    l[nt][0] = l[nt][1] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < DH / 16; ++u) o[nt][u][0] = o[nt][u][1] = o[nt][u][2] = o[nt][u][3] = 0.0f;
+  }
+  const int32_t* pages = p.table + (size_t)seq * p.width;
+  const int in_block = (1 << p.log2_block) - 1;
+  for (int key0 = k0 + warp * kTileKeys; key0 < k1; key0 += kSplitKeys) {
+    const int page = pages[key0 >> p.log2_block];
+    int n_keys = min(kTileKeys, k1 - key0);
+    if (page < 0 || page >= p.n_blocks) {                            // uniform over the warp
+      if (lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+      n_keys = 0;
+    }
+    const size_t first = ((((size_t)max(page, 0) * p.Hkv + hk) << p.log2_block) + (key0 & in_block)) * Lay::kRowBytes;
+    const uint8_t* kp = (const uint8_t*)p.ck + first;
+    const uint8_t* vp = (const uint8_t*)p.cv + first;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    uint4 kraw[2][Lay::kKeyLoads];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (g + 8 * i < n_keys) load_key<DH, F8>(kp + (size_t)(g + 8 * i) * Lay::kRowBytes, t, kraw[i]);
+      else
+#pragma unroll
+        for (int j = 0; j < Lay::kKeyLoads; ++j) kraw[i][j] = zero;
+    }
+    ValRaw<DH, F8> vraw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = 2 * t + (i & 1) + 8 * (i >> 1);
+      vraw[i] = ValRaw<DH, F8>{};
+      if (key < n_keys) load_val<DH, F8>(vp + (size_t)key * Lay::kRowBytes, g, vraw[i]);
+    }
+    uint32_t ka[Lay::kKeyWords], kb[Lay::kKeyWords];
+    key_words<DH, F8>(kraw[0], ka);
+    key_words<DH, F8>(kraw[1], kb);
+    uint32_t pb[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float s[4] = {};
+#pragma unroll
+      for (int i = 0; i < Lay::kKeyWords; i += 2)
+        mma_step<F8>(s, ka[i], kb[i], ka[i + 1], kb[i + 1], qf[nt][i], qf[nt][i + 1]);
+      const float f0 = p.scale_log2e * unscale[nt][0], f1 = p.scale_log2e * unscale[nt][1];
+      const bool in0 = g < n_keys, in1 = g + 8 < n_keys;
+      s[0] = in0 ? s[0] * f0 : -INFINITY;
+      s[1] = in0 ? s[1] * f1 : -INFINITY;
+      s[2] = in1 ? s[2] * f0 : -INFINITY;
+      s[3] = in1 ? s[3] * f1 : -INFINITY;
+      float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) {
+        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
+        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
+      }
+      mx0 = fmaxf(mx0, m[nt][0]);
+      mx1 = fmaxf(mx1, m[nt][1]);
+      // a maximum of -inf (every score so far is -inf): nothing to rescale, and exp2(-inf - 0) = 0
+      const float ref0 = mx0 == -INFINITY ? 0.0f : mx0, ref1 = mx1 == -INFINITY ? 0.0f : mx1;
+      const float corr0 = exp2f(m[nt][0] - ref0), corr1 = exp2f(m[nt][1] - ref1);
+      m[nt][0] = mx0; m[nt][1] = mx1;
+      s[0] = exp2f(s[0] - ref0); s[2] = exp2f(s[2] - ref0);
+      s[1] = exp2f(s[1] - ref1); s[3] = exp2f(s[3] - ref1);
+      l[nt][0] = l[nt][0] * corr0 + (s[0] + s[2]);
+      l[nt][1] = l[nt][1] * corr1 + (s[1] + s[3]);
+#pragma unroll
+      for (int u = 0; u < DH / 16; ++u) { o[nt][u][0] *= corr0; o[nt][u][2] *= corr0; o[nt][u][1] *= corr1; o[nt][u][3] *= corr1; }
+      // the weights of a tile, rounded to the values' type (relative 2^-9 or 2^-11 each, on terms that are summed in fp32)
+      uint32_t pk[2];
+      if (F8) {
+        const __half2 a = __floats2half2_rn(s[0], s[1]), b = __floats2half2_rn(s[2], s[3]);
+        pk[0] = *reinterpret_cast<const uint32_t*>(&a); pk[1] = *reinterpret_cast<const uint32_t*>(&b);
+      } else {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(s[0], s[1]), b = __floats2bfloat162_rn(s[2], s[3]);
+        pk[0] = *reinterpret_cast<const uint32_t*>(&a); pk[1] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      pb[nt][0] = transpose8x8(pk[0]);
+      pb[nt][1] = transpose8x8(pk[1]);
+    }
+#pragma unroll
+    for (int u = 0; u < Lay::kValWords; ++u) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = val_word<DH, F8>(vraw[i], u);
+      const uint32_t a0 = pair_lo(w[0], w[1]), a1 = pair_hi(w[0], w[1]), a2 = pair_lo(w[2], w[3]), a3 = pair_hi(w[2], w[3]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) mma_step<F8>(o[nt][u], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+    }
+  }
+
+  // join the warps
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) {
+      l[nt][0] += __shfl_xor_sync(0xffffffffu, l[nt][0], d);
+      l[nt][1] += __shfl_xor_sync(0xffffffffu, l[nt][1], d);
+    }
+    const int h = nt * 8 + 2 * t;
+    if (g == 0) {
+      sm_m[warp][h] = m[nt][0]; sm_m[warp][h + 1] = m[nt][1];
+      sm_l[warp][h] = l[nt][0]; sm_l[warp][h + 1] = l[nt][1];
+    }
+#pragma unroll
+    for (int u = 0; u < DH / 16; ++u) {
+      const int d0 = val_dim<DH, F8>(g, 2 * u), d1 = val_dim<DH, F8>(g, 2 * u + 1);
+      sm_o[warp][h][d0] = o[nt][u][0];
+      sm_o[warp][h + 1][d0] = o[nt][u][1];
+      sm_o[warp][h][d1] = o[nt][u][2];
+      sm_o[warp][h + 1][d1] = o[nt][u][3];
+    }
+  }
+  __syncthreads();
+  const bool last = p.splits == 1;
+  for (int i = threadIdx.x; i < n_heads * DH; i += kAttWarps * 32) {
+    const int h = i / DH, d = i % DH;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kAttWarps; ++w) mx = fmaxf(mx, sm_m[w][h]);
+    const float ref = mx == -INFINITY ? 0.0f : mx;
+    float sum = 0.0f, val = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kAttWarps; ++w) {
+      const float c = exp2f(sm_m[w][h] - ref);
+      sum += c * sm_l[w][h];
+      val += c * sm_o[w][h][d];
+    }
+    if (last) {
+      p.out[(size_t)row * p.ldo + (size_t)(head0 + h) * DH + d] = __float2bfloat16_rn(val * inverse_sum(p, sum));
+    } else {
+      const size_t at = ((size_t)row * p.H + head0 + h) * p.splits + split;
+      p.part_o[at * DH + d] = val;
+      if (d == 0) { p.part_ml[2 * at] = mx; p.part_ml[2 * at + 1] = sum; }
+    }
+  }
+}
+
+// Joins the splits of a row's head: one warp per (row, head), the splits in their order.
+template <int DH>
+__global__ void __launch_bounds__(256)
+paged_join_kernel(const PagedParams p) {
+  const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (item >= (int64_t)p.R * p.H) return;
+  const int row = (int)(item / p.H), h = (int)(item % p.H);
+  int seq = 0;
+  const int len = row_keys(p, row, &seq, false);
+  if (len == 0) return;                                // the first split wrote the zeros
+  const int per = split_keys(len, p.splits), n = (len + per - 1) / per;
+  const float* ml = p.part_ml + 2 * item * p.splits;
+  float mx = -INFINITY;
+  for (int s = lane; s < n; s += 32) mx = fmaxf(mx, ml[2 * s]);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+  const float ref = mx == -INFINITY ? 0.0f : mx;
+  float sum = 0.0f, v[DH / 32] = {};
+  for (int s = 0; s < n; ++s) {
+    const float c = exp2f(ml[2 * s] - ref);
+    sum += c * ml[2 * s + 1];
+    const float* o = p.part_o + (item * p.splits + s) * DH + lane * (DH / 32);
+#pragma unroll
+    for (int e = 0; e < DH / 32; ++e) v[e] += c * o[e];
+  }
+  const float f = inverse_sum(p, sum);
+  __nv_bfloat16* dst = p.out + (size_t)row * p.ldo + (size_t)h * DH + lane * (DH / 32);
+#pragma unroll
+  for (int e = 0; e < DH / 32; e += 2) *reinterpret_cast<__nv_bfloat162*>(dst + e) = __floats2bfloat162_rn(v[e] * f, v[e + 1] * f);
+}
+
+int log2_of(int v) {
+  int n = 0;
+  while ((1 << n) < v) ++n;
+  return n;
+}
+
+// Splits of the keys: as many as give every SM a few CTAs, none of them shorter than 256 keys of the longest row.
+int attention_splits(int64_t R, int Hkv, int chunks, int64_t max_len) {
+  const int64_t ctas = R * Hkv * chunks;
+  const int64_t want = (148 * 4 + ctas - 1) / ctas;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(want, max_len / 256));
+}
+int head_chunks(int G) { return G <= 8 ? 1 : (G + 15) / 16; }
+
+template <int DH, bool F8>
+int run_attention(const PagedParams& p, cudaStream_t st) {
+  const dim3 grid((unsigned)((int64_t)p.R * p.Hkv * p.chunks), p.splits);
+  if (p.G <= 8) QZO_LAUNCH((paged_attention_kernel<DH, 1, F8>), grid, dim3(kAttWarps * 32), 0, st, p);
+  else QZO_LAUNCH((paged_attention_kernel<DH, 2, F8>), grid, dim3(kAttWarps * 32), 0, st, p);
+  if (p.splits > 1)
+    QZO_LAUNCH(paged_join_kernel<DH>, dim3((unsigned)ceil_div64((int64_t)p.R * p.H, 8)), dim3(256), 0, st, p);
+  return QZO_OK;
+}
+
+}  // namespace
+
+bool cache_ok(const qzo_kv_cache* c) {
+  if (!c || !c->k || !c->v || ((uintptr_t)c->k & 15) || ((uintptr_t)c->v & 15)) return false;
+  if (c->n_blocks <= 0 || c->n_kv_heads <= 0 || !block_size_ok(c->block_size)) return false;
+  if ((int64_t)c->n_blocks * c->block_size > INT32_MAX) return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->dtype == QZO_DTYPE_BF16) return c->k_scale == 1.0f && c->v_scale == 1.0f;
+  return c->dtype == QZO_DTYPE_E4M3 && c->k_scale > 0.0f && c->v_scale > 0.0f && isfinite(c->k_scale) && isfinite(c->v_scale);
+}
+
+int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat16* k, int ldk, const __nv_bfloat16* v, int ldv,
+                              const float* q_gain, const float* k_gain, float norm_eps, const float* table, int max_pos,
+                              const int32_t* positions, const int32_t* slots, __nv_bfloat16* q_out, int ldqo,
+                              const qzo_kv_cache& c, int T, int H, int* status, cudaStream_t st) {
+  RopeCacheParams p{q, k, v, ldq, ldk, ldv, q_gain, k_gain, norm_eps, table, max_pos, positions, slots, q_out, ldqo, c.k, c.v,
+                    1.0f / c.k_scale, 1.0f / c.v_scale, c.n_blocks * c.block_size, log2_of(c.block_size), H, c.n_kv_heads,
+                    (int64_t)T * (H + 2 * c.n_kv_heads), status};
+  const int64_t ctas = ceil_div64(p.items * (c.head_dim / 8), 256);
+  if (ctas > INT32_MAX) return QZO_ERR_BAD_ARG;
+  const dim3 grid((unsigned)ctas), block(256);
+  const bool f8 = c.dtype == QZO_DTYPE_E4M3;
+  if (c.head_dim == 128) {
+    if (f8) QZO_LAUNCH((qk_norm_rope_cache_kernel<128, true>), grid, block, 0, st, p);
+    else QZO_LAUNCH((qk_norm_rope_cache_kernel<128, false>), grid, block, 0, st, p);
+  } else {
+    if (f8) QZO_LAUNCH((qk_norm_rope_cache_kernel<64, true>), grid, block, 0, st, p);
+    else QZO_LAUNCH((qk_norm_rope_cache_kernel<64, false>), grid, block, 0, st, p);
+  }
+  return QZO_OK;
+}
+
+size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
+  const int splits = attention_splits(R, Hkv, head_chunks(H / Hkv), max_len);
+  return splits > 1 ? (size_t)R * H * splits * (dh + 2) * sizeof(float) : 0;
+}
+
+int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
+                           const int32_t* row_seq, const int32_t* positions, float scale, __nv_bfloat16* out, int ldo, int R,
+                           int H, void* ws, size_t ws_bytes, int* status, cudaStream_t st) {
+  const int G = H / c.n_kv_heads, chunks = head_chunks(G), max_len = width * c.block_size;
+  if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
+  const int splits = attention_splits(R, c.n_kv_heads, chunks, max_len);
+  const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len);
+  if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 255))) return QZO_ERR_WORKSPACE;
+  PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
+                R, H, c.n_kv_heads, G, chunks, splits, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
+  if (splits > 1) {
+    p.part_o = (float*)ws;
+    p.part_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
+  }
+  const bool f8 = c.dtype == QZO_DTYPE_E4M3;
+  if (c.head_dim == 128) return f8 ? run_attention<128, true>(p, st) : run_attention<128, false>(p, st);
+  return f8 ? run_attention<64, true>(p, st) : run_attention<64, false>(p, st);
+}
+
+}  // namespace qzo
+
+using namespace qzo;
+
+extern "C" {
+
+int qzo_rope_table(float* d_table, int max_pos, int head_dim, float theta, void* stream) {
+  if (!d_table || max_pos <= 0 || (head_dim != 64 && head_dim != 128) || !(theta > 0.0f) || !isfinite(theta)) return QZO_ERR_BAD_ARG;
+  if ((int64_t)max_pos * head_dim > (1 << 30) || ((uintptr_t)d_table & 15)) return QZO_ERR_BAD_ARG;
+  QZO_TRY(check_device());
+  return launch_rope_table(d_table, max_pos, head_dim, theta, (cudaStream_t)stream);
+}
+
+int qzo_qk_norm_rope_cache(const void* d_q_bf16, int ldq, const void* d_k_bf16, int ldk, const void* d_v_bf16, int ldv,
+                           const float* d_q_gain, const float* d_k_gain, float norm_eps, const float* d_table, int max_pos,
+                           const int32_t* d_positions, const int32_t* d_slots, void* d_q_out_bf16, int ldqo,
+                           const qzo_kv_cache* cache, int T, int n_heads, int* d_status, void* stream) {
+  if (!d_q_bf16 || !d_k_bf16 || !d_v_bf16 || !d_positions || !d_slots || !d_q_out_bf16) return QZO_ERR_BAD_ARG;
+  if (!cache_ok(cache) || T <= 0 || n_heads <= 0 || n_heads % cache->n_kv_heads) return QZO_ERR_BAD_ARG;
+  if ((d_q_gain || d_k_gain) && !(norm_eps > 0.0f)) return QZO_ERR_BAD_ARG;
+  if (d_table && max_pos <= 0) return QZO_ERR_BAD_ARG;
+  const int64_t wq = (int64_t)n_heads * cache->head_dim, wk = (int64_t)cache->n_kv_heads * cache->head_dim;
+  if (ldq < wq || ldqo < wq || ldk < wk || ldv < wk || (ldq % 4) || (ldk % 4) || (ldv % 4) || (ldqo % 4)) return QZO_ERR_BAD_ARG;
+  if (((uintptr_t)d_q_bf16 | (uintptr_t)d_k_bf16 | (uintptr_t)d_v_bf16 | (uintptr_t)d_q_out_bf16) & 7) return QZO_ERR_BAD_ARG;
+  if (((uintptr_t)d_q_gain | (uintptr_t)d_k_gain | (uintptr_t)d_table) & 15) return QZO_ERR_BAD_ARG;
+  if (d_q_out_bf16 == d_q_bf16 && ldq != ldqo) return QZO_ERR_BAD_ARG;
+  QZO_TRY(check_device());
+  return launch_qk_norm_rope_cache((const __nv_bfloat16*)d_q_bf16, ldq, (const __nv_bfloat16*)d_k_bf16, ldk,
+                                   (const __nv_bfloat16*)d_v_bf16, ldv, d_q_gain, d_k_gain, norm_eps, d_table, max_pos, d_positions,
+                                   d_slots, (__nv_bfloat16*)d_q_out_bf16, ldqo, *cache, T, n_heads, d_status, (cudaStream_t)stream);
+}
+
+int qzo_paged_attention_workspace_bytes(int R, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes) {
+  if (!bytes || R <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0) return QZO_ERR_BAD_ARG;
+  if (head_dim != 64 && head_dim != 128) return QZO_ERR_BAD_ARG;
+  *bytes = paged_attention_bytes(R, n_heads, n_kv_heads, head_dim, max_len);
+  return QZO_OK;
+}
+
+int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache, const int32_t* d_block_table, int n_seqs,
+                        int table_width, const int32_t* d_row_seq, const int32_t* d_positions, float scale, void* d_out_bf16,
+                        int ldo, int R, int n_heads, void* d_workspace, size_t workspace_bytes, int* d_status, void* stream) {
+  if (!d_q_bf16 || !d_block_table || !d_positions || !d_out_bf16) return QZO_ERR_BAD_ARG;
+  if (!cache_ok(cache) || R <= 0 || n_seqs <= 0 || table_width <= 0 || n_heads <= 0 || n_heads % cache->n_kv_heads) return QZO_ERR_BAD_ARG;
+  if (!d_row_seq && R > n_seqs) return QZO_ERR_BAD_ARG;
+  if ((int64_t)table_width * cache->block_size > INT32_MAX || !(scale > 0.0f) || !isfinite(scale)) return QZO_ERR_BAD_ARG;
+  const int64_t wq = (int64_t)n_heads * cache->head_dim;
+  if (ldq < wq || ldo < wq || (ldq % 8) || (ldo % 8)) return QZO_ERR_BAD_ARG;
+  if (((uintptr_t)d_q_bf16 & 15) || ((uintptr_t)d_out_bf16 & 15)) return QZO_ERR_BAD_ARG;
+  QZO_TRY(check_device());
+  return launch_paged_attention((const __nv_bfloat16*)d_q_bf16, ldq, *cache, d_block_table, n_seqs, table_width, d_row_seq, d_positions,
+                                scale, (__nv_bfloat16*)d_out_bf16, ldo, R, n_heads, d_workspace, workspace_bytes, d_status,
+                                (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -31,7 +31,8 @@ void set_last_cuda_error(cudaError_t e);
 
 // Bits of the device status word of a model (0 = nothing to report).
 constexpr int kStatusTimeout = 1;    // a bounded device-side wait expired in some launch
-constexpr int kStatusBadToken = 2;   // a token id outside [0, vocab) reached the embedding
+constexpr int kStatusBadToken = 2;   // a token id outside [0, vocab) reached the embedding, or a serving operator met another index out of range
+constexpr int kStatusNotServed = 4;  // qzo_assign_slots: a step that the free blocks, tables or rows could not hold
 
 // Per-step quantities of a recorded forward (a CUDA graph that is replayed): the GEMM kernels read them
 // from device memory, so that one recorded launch sequence serves every seed and every eps.
@@ -57,6 +58,9 @@ inline bool first_use_on_device(std::atomic<unsigned long long>& mask) {
 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Block sizes of a paged cache: powers of two from 16 (the keys of one matrix tile) to 256.
+inline bool block_size_ok(int b) { return b >= 16 && b <= 256 && (b & (b - 1)) == 0; }
 
 // Checks that the current device is a compute-capability 10.x part; there is no other backend.
 int check_device();

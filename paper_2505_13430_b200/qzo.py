@@ -29,6 +29,8 @@ EXPORTS = (
     "qzo_device_status", "qzo_launch_count", "qzo_profile_gemms", "qzo_profile_read",
     "qzo_step_begin", "qzo_step_finish", "qzo_get_scales", "qzo_set_scales", "qzo_debug_set_status", "qzo_use_recorded_steps", "qzo_recorded_step_count", "qzo_perturbed_gemm_codebook16_channelwise",
     "qzo_joint_workspace_bytes", "qzo_enable_joint_spsa", "qzo_perturbed_gemm_table16", "qzo_debug_gemm_wait_expiry",
+    "qzo_gemv_int4", "qzo_rope_table", "qzo_qk_norm_rope_cache", "qzo_paged_attention_workspace_bytes", "qzo_paged_attention",
+    "qzo_assign_slots", "qzo_decode",
 )
 
 
@@ -51,6 +53,12 @@ class ModelDesc(ctypes.Structure):
 class Tensor(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("dptr", ctypes.c_void_p), ("dtype", ctypes.c_int),
                 ("shape", ctypes.c_int64 * 2)]
+
+
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int), ("n_blocks", ctypes.c_int),
+                ("block_size", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
 
 
 def _load():
@@ -100,6 +108,13 @@ def _load():
         "qzo_debug_set_capture": (ci, [vp, ci]),
         "qzo_debug_layer_output": (ci, [vp, ci, ci, vp, sz]),
         "qzo_device_status": (ci, [vp, P(ci)]),
+        "qzo_gemv_int4": (ci, [vp, ci, vp, vp, vp, vp, ci, ci, ci, ci, vp]),
+        "qzo_rope_table": (ci, [vp, ci, ci, cf, vp]),
+        "qzo_qk_norm_rope_cache": (ci, [vp, ci, vp, ci, vp, ci, vp, vp, cf, vp, ci, vp, vp, vp, ci, P(KvCacheDesc), ci, ci, vp, vp]),
+        "qzo_paged_attention_workspace_bytes": (ci, [ci, ci, ci, ci, ci, P(sz)]),
+        "qzo_paged_attention": (ci, [vp, ci, P(KvCacheDesc), vp, ci, ci, vp, vp, cf, vp, ci, ci, ci, vp, sz, vp, vp]),
+        "qzo_assign_slots": (ci, [vp, vp, ci, vp, ci, ci, vp, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp]),
+        "qzo_decode": (ci, [vp, P(KvCacheDesc), vp, vp, vp, vp, ci, vp, ci, ci, vp]),
         "qzo_profile_gemms": (ci, [vp, ci]),
         "qzo_profile_read": (ci, [vp, P(i64), P(ctypes.c_double), P(ctypes.c_double)]),
     }
@@ -277,6 +292,155 @@ def qzo_update_scales_flat(scales, seed, index_base, lr, g, clip):
     return scales
 
 
+# ---- serving operators ----
+
+GEMV_MAX_ROWS = 16
+MAX_REQUESTS = 4096
+
+
+def _here(*tensors):
+    """Stream of the current device; every tensor has to live there, the launches go to that device."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None:
+            assert t.is_cuda and t.get_device() == dev, "expects a CUDA tensor of the current device"
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _heads(t, what):
+    """Row stride of a bf16 [T][heads][head_dim] tensor whose heads lie side by side (a view of a projection's rows)."""
+    assert t.dtype == torch.bfloat16 and t.dim() == 3, f"{what}: expects bf16 [T][heads][head_dim]"
+    assert t.stride(2) == 1 and (t.stride(1) == t.shape[2] or t.shape[1] == 1), f"{what}: the heads of a row lie side by side"
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _ints(n, *tensors):
+    for t in tensors:
+        assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= n, f"expects contiguous int32 of {n} entries"
+
+
+def qzo_gemv_int4(x, wq, scales, K, N, bias=None, y=None):
+    """y = x W for up to 16 rows: x bf16 [M][K] (any row stride that is a multiple of 8), wq from qzo_repack_int4, scales
+    bf16 [ceil(K/128)][N], bias float32 [N] or None -> bf16 [M][N]."""
+    M = x.shape[0]
+    assert x.dtype == torch.bfloat16 and x.dim() == 2 and x.shape[1] == K and x.stride(1) == 1, "x: expects bf16 [M][K]"
+    assert wq.dtype == torch.uint8 and wq.is_contiguous() and wq.numel() >= -(-N // 128) * -(-K // 64) * 4096, "wq: too short"
+    assert scales.dtype == torch.bfloat16 and scales.is_contiguous() and scales.numel() >= -(-K // 128) * N, "scales: bf16 [ceil(K/128)][N]"
+    assert bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() >= N), "bias: float32 [N]"
+    if y is None:
+        y = torch.empty((M, N), dtype=torch.bfloat16, device=x.device)
+    assert y.dtype == torch.bfloat16 and y.shape == (M, N) and y.stride(1) == 1, "y: expects bf16 [M][N]"
+    st = _here(x, wq, scales, bias, y)
+    _check(_lib.qzo_gemv_int4(x.data_ptr(), x.stride(0) if M > 1 else K, wq.data_ptr(), scales.data_ptr(), _at(bias), y.data_ptr(),
+                              y.stride(0) if M > 1 else N, M, K, N, st), "qzo_gemv_int4")
+    return y
+
+
+class KvCache:
+    """One layer's paged cache: k, v [n_blocks][n_kv_heads][block_size][head_dim], bf16 or float8_e4m3fn (value = code *
+    scale).  Keeps the tensors alive."""
+
+    def __init__(self, k, v, k_scale=1.0, v_scale=1.0):
+        assert k.shape == v.shape and k.dim() == 4 and k.dtype == v.dtype, "k, v: [n_blocks][n_kv_heads][block_size][head_dim]"
+        assert k.is_cuda and k.is_contiguous() and v.is_contiguous() and k.device == v.device, "expects contiguous CUDA tensors"
+        kind = {torch.bfloat16: 0, torch.float8_e4m3fn: 4}[k.dtype]
+        self.k, self.v, self.k_scale, self.v_scale = k, v, float(k_scale), float(v_scale)
+        self.n_blocks, self.n_kv_heads, self.block_size, self.head_dim = k.shape
+        self.desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), kind, self.n_blocks, self.block_size, self.n_kv_heads, self.head_dim,
+                                self.k_scale, self.v_scale)
+        self._ref = ctypes.byref(self.desc)
+
+
+def qzo_rope_table(max_pos, head_dim, theta=10000.0):
+    """float32 [max_pos][head_dim/2][2]: cosine and sine of pos * theta**(-2i/head_dim)."""
+    table = torch.empty((max_pos, head_dim // 2, 2), dtype=torch.float32, device="cuda")
+    _check(_lib.qzo_rope_table(table.data_ptr(), max_pos, head_dim, theta, _here(table)), "qzo_rope_table")
+    return table
+
+
+def qzo_qk_norm_rope_cache(q, k, v, positions, slots, cache, q_gain=None, k_gain=None, norm_eps=1e-6, table=None, q_out=None,
+                           status=None):
+    """Head norms (where a gain is given), rotation (where a table is given) and cache write of T new rows; returns q_out
+    bf16 [T][heads][head_dim].  q, k, v bf16 [T][heads][head_dim] views; positions, slots int32 [T], negative = padding."""
+    T, H, dh = q.shape
+    assert k.shape == v.shape == (T, cache.n_kv_heads, dh) and dh == cache.head_dim, "k, v: [T][n_kv_heads][head_dim] of the cache"
+    ldq, ldk, ldv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    if q_out is None:
+        q_out = torch.empty((T, H, dh), dtype=torch.bfloat16, device=q.device)
+    assert q_out.shape == q.shape
+    ldo = _heads(q_out, "q_out")
+    _ints(T, positions, slots)
+    for gain in (q_gain, k_gain):
+        assert gain is None or (gain.dtype == torch.float32 and gain.is_contiguous() and gain.numel() == dh), "gains: float32 [head_dim]"
+    max_pos = 0
+    if table is not None:
+        assert table.dtype == torch.float32 and table.is_contiguous() and table.shape[1:] == (dh // 2, 2), "table: [max_pos][head_dim/2][2]"
+        max_pos = table.shape[0]
+    st = _here(q, k, v, positions, slots, cache.k, q_gain, k_gain, table, q_out, status)
+    _check(_lib.qzo_qk_norm_rope_cache(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, _at(q_gain), _at(k_gain), norm_eps,
+                                       _at(table), max_pos, positions.data_ptr(), slots.data_ptr(), q_out.data_ptr(), ldo, cache._ref,
+                                       T, H, _at(status), st), "qzo_qk_norm_rope_cache")
+    return q_out
+
+
+def qzo_paged_attention_workspace_bytes(R, n_heads, n_kv_heads, head_dim, max_len):
+    out = ctypes.c_size_t(0)
+    _check(_lib.qzo_paged_attention_workspace_bytes(R, n_heads, n_kv_heads, head_dim, max_len, ctypes.byref(out)),
+           "qzo_paged_attention_workspace_bytes")
+    return out.value
+
+
+def qzo_paged_attention(q, cache, block_table, positions, row_seq=None, scale=None, out=None, workspace=None, status=None):
+    """Attention of one new token per row over the paged cache: q bf16 [R][heads][head_dim], block_table int32
+    [n_seqs][table_width], positions int32 [R] (negative = empty row, zeros), row_seq int32 [R] or None (row t is request t)
+    -> bf16 [R][heads][head_dim]."""
+    R, H, dh = q.shape
+    ldq = _heads(q, "q")
+    if out is None:
+        out = torch.empty((R, H, dh), dtype=torch.bfloat16, device=q.device)
+    assert out.shape == q.shape and dh == cache.head_dim
+    ldo = _heads(out, "out")
+    n_seqs, width = block_table.shape
+    _ints(n_seqs * width, block_table)
+    _ints(R, positions)
+    if row_seq is not None:
+        _ints(R, row_seq)
+    if workspace is None:
+        need = qzo_paged_attention_workspace_bytes(R, H, cache.n_kv_heads, dh, width * cache.block_size)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
+    st = _here(q, cache.k, block_table, positions, row_seq, out, workspace, status)
+    _check(_lib.qzo_paged_attention(q.data_ptr(), ldq, cache._ref, block_table.data_ptr(), n_seqs, width, _at(row_seq),
+                                    positions.data_ptr(), dh ** -0.5 if scale is None else scale, out.data_ptr(), ldo, R, H,
+                                    _at(workspace), 0 if workspace is None else workspace.numel(), _at(status), st),
+           "qzo_paged_attention")
+    return out
+
+
+def qzo_assign_slots(lens, new, block_table, free, free_count, block_size, max_rows, lens_out=None, free_count_out=None,
+                     row_seq=None, positions=None, slots=None, status=None):
+    """Blocks, rows and slots of a step (all int32): lens [B], new [B] (negative = finished), block_table [B][width], free =
+    stack of free blocks, free_count [1].  Lengths and count are updated in place unless lens_out / free_count_out are
+    given.  Returns (row_seq, positions, slots), each [max_rows], -1 behind the last row."""
+    B, width = block_table.shape
+    lens_out = lens if lens_out is None else lens_out
+    free_count_out = free_count if free_count_out is None else free_count_out
+    if row_seq is None and positions is None and slots is None:
+        row_seq, positions, slots = torch.empty((3, max_rows), dtype=torch.int32, device=lens.device)
+    _ints(B, lens, new, lens_out)
+    _ints(B * width, block_table)
+    _ints(1, free, free_count, free_count_out)
+    _ints(max_rows, row_seq, positions, slots)
+    st = _here(lens, new, block_table, free, free_count, lens_out, free_count_out, row_seq, positions, slots, status)
+    _check(_lib.qzo_assign_slots(lens.data_ptr(), new.data_ptr(), B, block_table.data_ptr(), width, block_size, free.data_ptr(),
+                                 free.numel(), free_count.data_ptr(), max_rows, row_seq.data_ptr(), positions.data_ptr(),
+                                 slots.data_ptr(), lens_out.data_ptr(), free_count_out.data_ptr(), _at(status), st), "qzo_assign_slots")
+    return row_seq, positions, slots
+
+
 def make_desc(cfg):
     return ModelDesc(ARCH[cfg["arch"]], cfg["n_layers"], cfg["d_model"], cfg["n_heads"], cfg["d_ffn"],
                      cfg["vocab"], cfg["max_seq"], 128, cfg["norm_eps"], cfg["rope_theta"])
@@ -352,6 +516,23 @@ class Model:
         _check(_lib.qzo_forward_loss(self.handle, _ptr(tokens), _ptr(labels), B, S, seed, sign, eps, _ptr(out)),
                "qzo_forward_loss")
         return out
+
+    def qzo_decode(self, caches, tokens, row_seq, positions, slots, block_table, logits=None):
+        """One answering step of R rows over the layers' caches (list of KvCache, one per layer); tokens, row_seq, positions,
+        slots int32 [R], block_table int32 [n_seqs][width] -> float32 logits [R][vocab]."""
+        R = tokens.numel()
+        assert len(caches) == self.cfg["n_layers"], "expects one cache per layer"
+        _ints(R, tokens, row_seq, positions, slots)
+        n_seqs, width = block_table.shape
+        _ints(n_seqs * width, block_table)
+        if logits is None:
+            logits = torch.empty((R, self.cfg["vocab"]), dtype=torch.float32, device="cuda")
+        assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.shape == (R, self.cfg["vocab"])
+        _here(tokens, row_seq, positions, slots, block_table, logits, *(c.k for c in caches))
+        descs = (KvCacheDesc * len(caches))(*(c.desc for c in caches))
+        _check(_lib.qzo_decode(self.handle, descs, tokens.data_ptr(), row_seq.data_ptr(), positions.data_ptr(), slots.data_ptr(), R,
+                               block_table.data_ptr(), n_seqs, width, logits.data_ptr()), "qzo_decode")
+        return logits
 
     def qzo_update_scales(self, seed, lr, g, clip):
         _check(_lib.qzo_update_scales(self.handle, seed, lr, g, clip), "qzo_update_scales")

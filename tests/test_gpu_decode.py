@@ -1,0 +1,130 @@
+"""The tuned model answering: qzo_assign_slots and qzo_decode, prompts and single tokens of several requests over the paged
+caches, against the oracle's whole forward on each request's tokens."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import model as omodel
+from paper_2505_13430_b200 import inputs
+from tests.helpers import build_oracle_model
+
+pytestmark = pytest.mark.gpu
+
+TOL = 2e-2       # max |a - b| / max |b| per row of logits, as for the logits of the training forwards
+
+
+def _logits(om, tokens):
+    cap = {}
+    tok = np.asarray(tokens)[None]
+    omodel.forward_loss(om, tok, np.full_like(tok, -100), 0, 0, 1e-3, capture=cap)
+    return cap["logits"]
+
+
+class Server:
+    def __init__(self, qzo, gm, cfg, B, block, n_blocks, dtype=torch.bfloat16):
+        H, dh = cfg["n_heads"], cfg["d_model"] // cfg["n_heads"]
+        self.qzo, self.gm, self.B, self.block = qzo, gm, B, block
+        scale = 1.0 if dtype == torch.bfloat16 else 2.0 ** -5
+        shape = (n_blocks, H, block, dh)
+        self.caches = [qzo.KvCache(*(torch.full(shape, float("nan"), device="cuda").to(dtype) for _ in range(2)), scale, scale)
+                       for _ in range(cfg["n_layers"])]
+        i32 = dict(dtype=torch.int32, device="cuda")
+        self.lens, self.count = torch.zeros(B, **i32), torch.tensor([n_blocks], **i32)
+        self.table = torch.full((B, -(-cfg["max_seq"] // block)), -1, **i32)
+        self.free = torch.randperm(n_blocks, generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()
+        self.text = [[] for _ in range(B)]
+
+    def step(self, new, rows):
+        """new: request -> its new tokens, None when it is finished.  Returns (request, position, logits) of the rows."""
+        add = torch.zeros(self.B, dtype=torch.int32)
+        flat = []
+        for r in range(self.B):
+            toks = new.get(r, [])
+            add[r] = -1 if toks is None else len(toks)
+            self.text[r] = [] if toks is None else self.text[r] + list(toks)
+            flat += [] if toks is None else list(toks)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        seq, pos, slots = self.qzo.qzo_assign_slots(self.lens, add.cuda(), self.table, self.free, self.count, self.block, rows, status=status)
+        assert int(status.item()) == 0
+        tokens = torch.full((rows,), -12345, dtype=torch.int32)       # what stands in padding rows is not looked at
+        tokens[:len(flat)] = torch.tensor(flat, dtype=torch.int32)
+        logits = self.gm.qzo_decode(self.caches, tokens.cuda(), seq, pos, slots, self.table)
+        assert self.gm.qzo_device_status() == 0
+        return [(int(r), int(p), l) for r, p, l in zip(seq[:len(flat)].tolist(), pos[:len(flat)].tolist(), logits.cpu().numpy())]
+
+
+@pytest.mark.parametrize("name,block,dtype,tol", [("tiny", 16, torch.bfloat16, TOL), ("tiny_opt", 32, torch.bfloat16, TOL),
+                                                  ("tiny_dh128", 16, torch.bfloat16, TOL)])
+def test_decode_follows_the_oracle(name, block, dtype, tol):
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg(name)
+    raw = inputs.raw_model_tensors(cfg, seed=1000)
+    gm = qzo.build_model_from_raw(raw, 256)
+    om = build_oracle_model(raw)
+    rng = np.random.default_rng(3)
+    srv = Server(qzo, gm, cfg, B=3, block=block, n_blocks=3 * -(-cfg["max_seq"] // block), dtype=dtype)
+    take = lambda n: rng.integers(0, cfg["vocab"], n).tolist()  # noqa: E731
+    steps = [({0: take(5)}, 8),                                  # one short prompt: the matrix-vector path
+             ({0: take(1), 1: take(40)}, 48),                    # a token beside a long prompt: the GEMM path
+             ({0: take(1), 1: take(1)}, 2),
+             ({0: take(1), 2: take(11)}, 16),
+             ({0: None, 1: take(3), 2: take(1)}, 4),             # a finished request gives its blocks back
+             ({0: take(19), 2: take(1)}, 20),
+             ({0: take(1), 1: take(1), 2: take(1)}, 16)]
+    for new, rows in steps:
+        for r, p, got in srv.step(new, rows):
+            want = _logits(om, srv.text[r][:p + 1])[-1]
+            assert np.abs(got - want).max() <= tol * np.abs(want).max(), (r, p)
+    gm.close()
+
+
+def test_decode_agrees_with_the_training_forward_and_leaves_it_alone():
+    # the same tokens through qzo_forward_loss and qzo_decode; a training step after decoding gives what it gives without
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg("tiny")
+    raw = inputs.raw_model_tensors(cfg, seed=1000)
+    tok, lab = inputs.tokens_and_labels(cfg, 2, 32, seed=9)
+    outs = []
+    for decode_between in (False, True):
+        gm = qzo.build_model_from_raw(raw, 256)
+        first = gm.qzo_step(tok.cuda(), lab.cuda(), 5, 1e-3, 1e-3, 100.0)
+        if decode_between:
+            srv = Server(qzo, gm, cfg, 2, 16, 16)
+            rows = srv.step({0: tok[0].tolist(), 1: tok[1].tolist()}, 64)
+            gm.qzo_forward_loss(tok.cuda(), lab.cuda(), 0, 0, 1e-3)
+            full = gm.qzo_debug_layer_output(0, 1, 64)
+            got = np.stack([l for _, _, l in rows])
+            want = full.cpu().numpy()
+            assert np.abs(got - want).max() <= 1e-2 * np.abs(want).max()
+        second = gm.qzo_step(tok.cuda(), lab.cuda(), 6, 1e-3, 1e-3, 100.0)
+        outs.append((first, second, gm.scales.clone()))
+        gm.close()
+    assert outs[0][:2] == outs[1][:2] and torch.equal(outs[0][2], outs[1][2])
+
+
+def test_decode_refusals_and_reports():
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg("tiny")
+    raw = inputs.raw_model_tensors(cfg, seed=1000)
+    gm = qzo.build_model_from_raw(raw, 64)
+    srv = Server(qzo, gm, cfg, 1, 16, 4)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    one = torch.zeros(1, **i32)
+    table = torch.zeros((1, 4), **i32)
+
+    def refused(status, caches=srv.caches, n=1, width=4):
+        z = torch.zeros(n, **i32)
+        with pytest.raises(qzo.QzoError) as e:
+            gm.qzo_decode(caches, z, z, z, z, torch.zeros((1, width), **i32))
+        assert e.value.status == status
+
+    refused(qzo.ERR_WORKSPACE, n=65)
+    wrong = [qzo.KvCache(torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16, device="cuda"))] * 2
+    refused(qzo.ERR_BAD_ARG, caches=wrong)
+    # indices out of range: reported through the status word
+    for tokens, pos, slot in ((cfg["vocab"], 0, 0), (0, cfg["max_seq"], 0), (0, 0, 64)):
+        gm.qzo_decode(srv.caches, one + tokens, one, one + pos, one + slot, table)
+        assert gm.qzo_device_status() == 2
+        gm.qzo_debug_set_status(0)
+    assert gm.qzo_device_status() == 0
+    gm.close()
