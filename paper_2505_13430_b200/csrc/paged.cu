@@ -132,9 +132,8 @@ qk_norm_rope_cache_kernel(const RopeCacheParams p) {
 // Attention of one new token per row
 // =========================================================================================
 
-constexpr int kAttWarps = 4;
 constexpr int kTileKeys = 16;                          // keys a warp takes at a time: one matrix tile
-constexpr int kSplitKeys = kAttWarps * kTileKeys;      // a split is a multiple of what its warps take together
+constexpr int kSplitKeys = 64;                         // a split is a multiple of this many keys
 
 struct PagedParams {
   const __nv_bfloat16* q;
@@ -171,9 +170,9 @@ __device__ __forceinline__ float inverse_sum(const PagedParams& p, float sum) { 
 
 __device__ __forceinline__ uint32_t pair_lo(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x5410); }
 __device__ __forceinline__ uint32_t pair_hi(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xFFFFu), __NV_E4M3);
-  return (uint32_t)h.x | ((uint32_t)h.y << 16);
+// four codes as two fp16 pairs (exact)
+__device__ __forceinline__ void e4m3x4_to_f16x2(uint32_t four, uint32_t& lo, uint32_t& hi) {
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(four));
 }
 
 // What one lane holds of a key row: NW words of two elements each, the row's 16-byte chunks t, t + 4, ... in order.
@@ -200,8 +199,7 @@ __device__ __forceinline__ void key_words(const uint4 raw[Layout<DH, F8>::kKeyLo
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (F8) {
-        w[8 * j + 2 * i] = e4m3x2_to_f16x2(r[i]);
-        w[8 * j + 2 * i + 1] = e4m3x2_to_f16x2(r[i] >> 16);
+        e4m3x4_to_f16x2(r[i], w[8 * j + 2 * i], w[8 * j + 2 * i + 1]);
       } else {
         w[4 * j + i] = r[i];
       }
@@ -230,11 +228,6 @@ __device__ __forceinline__ void load_val(const uint8_t* row, int g, ValRaw<DH, F
     }
   }
 }
-template <int DH, bool F8>
-__device__ __forceinline__ uint32_t val_word(const ValRaw<DH, F8>& raw, int u) {
-  if (!F8) return raw.w[u];
-  return e4m3x2_to_f16x2(raw.w[u >> 1] >> (16 * (u & 1)));
-}
 template <bool F8>
 __device__ __forceinline__ void mma_step(float c[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if (F8) mma16816_f16(c, a0, a1, a2, a3, b0, b1);
@@ -245,12 +238,13 @@ __device__ __forceinline__ void mma_step(float c[4], uint32_t a0, uint32_t a1, u
 // split's tiles of 16 keys in turn, each with its own running maximum and sum, and are joined at the end.
 // A tile is two products: S^T = K Q^T (keys x heads) and O^T += V^T P^T (dimensions x heads), so up to eight heads
 // share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.
-template <int DH, int NT, bool F8>
-__global__ void __launch_bounds__(kAttWarps * 32)
+template <int DH, int NT, bool F8, int W>
+__global__ void __launch_bounds__(W * 32, (DH == 64 ? 16 : NT == 1 ? 12 : 8) / W)
 paged_attention_kernel(const PagedParams p) {
   using Lay = Layout<DH, F8>;
-  __shared__ float sm_o[kAttWarps][8 * NT][DH + 4];
-  __shared__ float sm_m[kAttWarps][8 * NT], sm_l[kAttWarps][8 * NT];
+  extern __shared__ __align__(16) float att_smem[];
+  float (*sm_o)[8 * NT][DH + 4] = reinterpret_cast<float (*)[8 * NT][DH + 4]>(att_smem);
+  __shared__ float sm_m[W][8 * NT], sm_l[W][8 * NT];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int per_row = p.Hkv * p.chunks;
   const int row = blockIdx.x / per_row, hk = blockIdx.x % per_row / p.chunks, chunk = blockIdx.x % p.chunks;
@@ -263,7 +257,7 @@ paged_attention_kernel(const PagedParams p) {
   const int k0 = split * per, k1 = min(len, k0 + per);
   if (k0 >= k1) {
     if (len == 0 && split == 0)
-      for (int i = threadIdx.x; i < n_heads * DH / 8; i += kAttWarps * 32)
+      for (int i = threadIdx.x; i < n_heads * DH / 8; i += W * 32)
         *reinterpret_cast<uint4*>(p.out + (size_t)row * p.ldo + (size_t)head0 * DH + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
     return;
   }
@@ -319,42 +313,69 @@ paged_attention_kernel(const PagedParams p) {
   }
   const int32_t* pages = p.table + (size_t)seq * p.width;
   const int in_block = (1 << p.log2_block) - 1;
-  for (int key0 = k0 + warp * kTileKeys; key0 < k1; key0 += kSplitKeys) {
-    const int page = pages[key0 >> p.log2_block];
-    int n_keys = min(kTileKeys, k1 - key0);
+  // A tile's keys and values stay in registers from their loads to their use, and the next tile's are loaded as soon as
+  // the registers are free: its keys behind the scores, its values behind the second product.  The block id is known one
+  // tile ahead of that.
+  uint4 kraw[2][Lay::kKeyLoads];
+  ValRaw<DH, F8> vraw[4];
+  size_t at = 0;                       // byte offset of the tile that is loaded next, its number of keys, its block id
+  int n_next = 0, page = 0;
+  auto find = [&](int key0) {
+    n_next = min(kTileKeys, k1 - key0);
     if (page < 0 || page >= p.n_blocks) {                            // uniform over the warp
       if (lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
-      n_keys = 0;
+      n_next = 0;
     }
-    const size_t first = ((((size_t)max(page, 0) * p.Hkv + hk) << p.log2_block) + (key0 & in_block)) * Lay::kRowBytes;
-    const uint8_t* kp = (const uint8_t*)p.ck + first;
-    const uint8_t* vp = (const uint8_t*)p.cv + first;
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    uint4 kraw[2][Lay::kKeyLoads];
+    at = ((((size_t)max(page, 0) * p.Hkv + hk) << p.log2_block) + (key0 & in_block)) * Lay::kRowBytes;
+  };
+  auto load_keys = [&]() {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      if (g + 8 * i < n_keys) load_key<DH, F8>(kp + (size_t)(g + 8 * i) * Lay::kRowBytes, t, kraw[i]);
+      if (g + 8 * i < n_next) load_key<DH, F8>((const uint8_t*)p.ck + at + (g + 8 * i) * Lay::kRowBytes, t, kraw[i]);
       else
 #pragma unroll
-        for (int j = 0; j < Lay::kKeyLoads; ++j) kraw[i][j] = zero;
+        for (int j = 0; j < Lay::kKeyLoads; ++j) kraw[i][j] = make_uint4(0u, 0u, 0u, 0u);
     }
-    ValRaw<DH, F8> vraw[4];
+  };
+  auto load_vals = [&]() {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int key = 2 * t + (i & 1) + 8 * (i >> 1);
-      vraw[i] = ValRaw<DH, F8>{};
-      if (key < n_keys) load_val<DH, F8>(vp + (size_t)key * Lay::kRowBytes, g, vraw[i]);
+      if (key < n_next) load_val<DH, F8>((const uint8_t*)p.cv + at + key * Lay::kRowBytes, g, vraw[i]);
+      else vraw[i] = ValRaw<DH, F8>{};
     }
+  };
+  int key0 = k0 + warp * kTileKeys;
+  if (key0 < k1) {
+    page = pages[key0 >> p.log2_block];
+    find(key0);
+    load_keys();
+    load_vals();
+    if (key0 + W * kTileKeys < k1) page = pages[(key0 + W * kTileKeys) >> p.log2_block];
+  }
+  for (; key0 < k1; key0 += W * kTileKeys) {
+    const int n_keys = n_next;
+    const bool more = key0 + W * kTileKeys < k1;
     uint32_t ka[Lay::kKeyWords], kb[Lay::kKeyWords];
     key_words<DH, F8>(kraw[0], ka);
     key_words<DH, F8>(kraw[1], kb);
+    float sc[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < Lay::kKeyWords; i += 2)
+        mma_step<F8>(sc[nt], ka[i], kb[i], ka[i + 1], kb[i + 1], qf[nt][i], qf[nt][i + 1]);
+    }
+    if (more) {
+      find(key0 + W * kTileKeys);
+      load_keys();
+      if (key0 + 2 * W * kTileKeys < k1) page = pages[(key0 + 2 * W * kTileKeys) >> p.log2_block];
+    }
     uint32_t pb[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float s[4] = {};
-#pragma unroll
-      for (int i = 0; i < Lay::kKeyWords; i += 2)
-        mma_step<F8>(s, ka[i], kb[i], ka[i + 1], kb[i + 1], qf[nt][i], qf[nt][i + 1]);
+      float (&s)[4] = sc[nt];
       const float f0 = p.scale_log2e * unscale[nt][0], f1 = p.scale_log2e * unscale[nt][1];
       const bool in0 = g < n_keys, in1 = g + 8 < n_keys;
       s[0] = in0 ? s[0] * f0 : -INFINITY;
@@ -392,14 +413,24 @@ paged_attention_kernel(const PagedParams p) {
       pb[nt][1] = transpose8x8(pk[1]);
     }
 #pragma unroll
-    for (int u = 0; u < Lay::kValWords; ++u) {
-      uint32_t w[4];
+    for (int u = 0; u < Lay::kValWords; u += 2) {
+      uint32_t w0[4], w1[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = val_word<DH, F8>(vraw[i], u);
-      const uint32_t a0 = pair_lo(w[0], w[1]), a1 = pair_hi(w[0], w[1]), a2 = pair_lo(w[2], w[3]), a3 = pair_hi(w[2], w[3]);
+      for (int i = 0; i < 4; ++i) {
+        if (F8) {
+          e4m3x4_to_f16x2(vraw[i].w[u / 2], w0[i], w1[i]);
+        } else {
+          w0[i] = vraw[i].w[F8 ? 0 : u];
+          w1[i] = vraw[i].w[F8 ? 0 : u + 1];
+        }
+      }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_step<F8>(o[nt][u], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+      for (int nt = 0; nt < NT; ++nt) {
+        mma_step<F8>(o[nt][u], pair_lo(w0[0], w0[1]), pair_hi(w0[0], w0[1]), pair_lo(w0[2], w0[3]), pair_hi(w0[2], w0[3]), pb[nt][0], pb[nt][1]);
+        mma_step<F8>(o[nt][u + 1], pair_lo(w1[0], w1[1]), pair_hi(w1[0], w1[1]), pair_lo(w1[2], w1[3]), pair_hi(w1[2], w1[3]), pb[nt][0], pb[nt][1]);
+      }
     }
+    if (more) load_vals();
   }
 
   // join the warps
@@ -426,15 +457,15 @@ paged_attention_kernel(const PagedParams p) {
   }
   __syncthreads();
   const bool last = p.splits == 1;
-  for (int i = threadIdx.x; i < n_heads * DH; i += kAttWarps * 32) {
+  for (int i = threadIdx.x; i < n_heads * DH; i += W * 32) {
     const int h = i / DH, d = i % DH;
     float mx = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kAttWarps; ++w) mx = fmaxf(mx, sm_m[w][h]);
+    for (int w = 0; w < W; ++w) mx = fmaxf(mx, sm_m[w][h]);
     const float ref = mx == -INFINITY ? 0.0f : mx;
     float sum = 0.0f, val = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kAttWarps; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float c = exp2f(sm_m[w][h] - ref);
       sum += c * sm_l[w][h];
       val += c * sm_o[w][h][d];
@@ -449,36 +480,58 @@ paged_attention_kernel(const PagedParams p) {
   }
 }
 
-// Joins the splits of a row's head: one warp per (row, head), the splits in their order.
+// Joins the splits of a row's head: one CTA per (row, head), its DH / 4 columns of threads each taking four dimensions,
+// its 256 / (DH / 4) rows of threads every so many of the splits; the rows are then summed in their order.
+constexpr int kJoinThreads = 256;
 template <int DH>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kJoinThreads)
 paged_join_kernel(const PagedParams p) {
-  const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (item >= (int64_t)p.R * p.H) return;
+  constexpr int kCols = DH / 4, kRows = kJoinThreads / kCols;
+  extern __shared__ float weight[];                    // [splits]
+  __shared__ float4 part[kRows][kCols];
+  __shared__ float part_sum[kRows], part_max[kJoinThreads / 32];
+  const int64_t item = blockIdx.x;
   const int row = (int)(item / p.H), h = (int)(item % p.H);
   int seq = 0;
   const int len = row_keys(p, row, &seq, false);
   if (len == 0) return;                                // the first split wrote the zeros
   const int per = split_keys(len, p.splits), n = (len + per - 1) / per;
-  const float* ml = p.part_ml + 2 * item * p.splits;
+  const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + item * p.splits;
   float mx = -INFINITY;
-  for (int s = lane; s < n; s += 32) mx = fmaxf(mx, ml[2 * s]);
+  for (int s = threadIdx.x; s < n; s += kJoinThreads) mx = fmaxf(mx, ml[s].x);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-  const float ref = mx == -INFINITY ? 0.0f : mx;
-  float sum = 0.0f, v[DH / 32] = {};
-  for (int s = 0; s < n; ++s) {
-    const float c = exp2f(ml[2 * s] - ref);
-    sum += c * ml[2 * s + 1];
-    const float* o = p.part_o + (item * p.splits + s) * DH + lane * (DH / 32);
+  if ((threadIdx.x & 31) == 0) part_max[threadIdx.x >> 5] = mx;
+  __syncthreads();
 #pragma unroll
-    for (int e = 0; e < DH / 32; ++e) v[e] += c * o[e];
+  for (int w = 0; w < kJoinThreads / 32; ++w) mx = fmaxf(mx, part_max[w]);
+  const float ref = mx == -INFINITY ? 0.0f : mx;
+  for (int s = threadIdx.x; s < n; s += kJoinThreads) weight[s] = exp2f(ml[s].x - ref);
+  __syncthreads();
+  const int c = threadIdx.x % kCols, r = threadIdx.x / kCols;
+  const float4* o = reinterpret_cast<const float4*>(p.part_o) + item * p.splits * kCols + c;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  float sum = 0.0f;
+#pragma unroll 4
+  for (int s = r; s < n; s += kRows) {
+    const float w = weight[s];
+    const float4 x = o[(size_t)s * kCols];
+    v.x = fmaf(w, x.x, v.x); v.y = fmaf(w, x.y, v.y); v.z = fmaf(w, x.z, v.z); v.w = fmaf(w, x.w, v.w);
+    sum = fmaf(w, ml[s].y, sum);
+  }
+  part[r][c] = v;
+  if (c == 0) part_sum[r] = sum;
+  __syncthreads();
+  if (r > 0) return;
+#pragma unroll
+  for (int i = 1; i < kRows; ++i) {
+    const float4 x = part[i][c];
+    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+    sum += part_sum[i];
   }
   const float f = inverse_sum(p, sum);
-  __nv_bfloat16* dst = p.out + (size_t)row * p.ldo + (size_t)h * DH + lane * (DH / 32);
-#pragma unroll
-  for (int e = 0; e < DH / 32; e += 2) *reinterpret_cast<__nv_bfloat162*>(dst + e) = __floats2bfloat162_rn(v[e] * f, v[e + 1] * f);
+  const float out[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
+  *reinterpret_cast<uint2*>(p.out + (size_t)row * p.ldo + (size_t)h * DH + 4 * c) = pack4_bf16(out);
 }
 
 int log2_of(int v) {
@@ -495,13 +548,22 @@ int attention_splits(int64_t R, int Hkv, int chunks, int64_t max_len) {
 }
 int head_chunks(int G) { return G <= 8 ? 1 : (G + 15) / 16; }
 
+template <int DH, int NT, bool F8, int W>
+int run_attention_w(const PagedParams& p, cudaStream_t st) {
+  const dim3 grid((unsigned)((int64_t)p.R * p.Hkv * p.chunks), p.splits);
+  constexpr int smem = W * 8 * NT * (DH + 4) * (int)sizeof(float);
+  if (smem > 40 * 1024)
+    QZO_CUDA_TRY(cudaFuncSetAttribute(paged_attention_kernel<DH, NT, F8, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  QZO_LAUNCH((paged_attention_kernel<DH, NT, F8, W>), grid, dim3(W * 32), smem, st, p);
+  return QZO_OK;
+}
+
 template <int DH, bool F8>
 int run_attention(const PagedParams& p, cudaStream_t st) {
-  const dim3 grid((unsigned)((int64_t)p.R * p.Hkv * p.chunks), p.splits);
-  if (p.G <= 8) QZO_LAUNCH((paged_attention_kernel<DH, 1, F8>), grid, dim3(kAttWarps * 32), 0, st, p);
-  else QZO_LAUNCH((paged_attention_kernel<DH, 2, F8>), grid, dim3(kAttWarps * 32), 0, st, p);
+  if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 4>(p, st)));
+  else QZO_TRY((run_attention_w<DH, 2, F8, 4>(p, st)));
   if (p.splits > 1)
-    QZO_LAUNCH(paged_join_kernel<DH>, dim3((unsigned)ceil_div64((int64_t)p.R * p.H, 8)), dim3(256), 0, st, p);
+    QZO_LAUNCH(paged_join_kernel<DH>, dim3((unsigned)((int64_t)p.R * p.H)), dim3(kJoinThreads), p.splits * (int)sizeof(float), st, p);
   return QZO_OK;
 }
 
