@@ -144,14 +144,14 @@ struct PagedParams {
   const int32_t *row_seq, *positions;
   float scale_log2e, v_scale;                          // the keys' scale is in the first
   __nv_bfloat16* out;
-  int ldo, R, H, Hkv, G, chunks, splits, n_blocks, log2_block;
+  int ldo, R, H, Hkv, G, chunks, splits, min_keys, n_blocks, log2_block;
   float *part_o, *part_ml;                             // [R][H][splits][DH], [R][H][splits][2]
   int* status;
 };
 
-// Keys of split s of a row that sees len keys: [s * per, min(len, (s + 1) * per)).
-__device__ __forceinline__ int split_keys(int len, int splits) {
-  return ((len + splits - 1) / splits + kSplitKeys - 1) / kSplitKeys * kSplitKeys;
+// Keys of split s of a row that sees len keys: [s * per, min(len, (s + 1) * per)), per at least the launch's minimum.
+__device__ __forceinline__ int split_keys(const PagedParams& p, int len) {
+  return max(p.min_keys, ((len + p.splits - 1) / p.splits + kSplitKeys - 1) / kSplitKeys * kSplitKeys);
 }
 // Number of keys a row sees, 0 for padding; seq receives its request.  One thread reports what is out of range.
 __device__ __forceinline__ int row_keys(const PagedParams& p, int row, int* seq, bool report) {
@@ -168,8 +168,12 @@ __device__ __forceinline__ int row_keys(const PagedParams& p, int row, int* seq,
 // A row none of whose keys has a score above -inf (no key at all, or only blocks that are out of range) gives zeros.
 __device__ __forceinline__ float inverse_sum(const PagedParams& p, float sum) { return sum == 0.0f ? 0.0f : p.v_scale / sum; }
 
-__device__ __forceinline__ uint32_t pair_lo(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x5410); }
-__device__ __forceinline__ uint32_t pair_hi(uint32_t a, uint32_t b) { return __byte_perm(a, b, 0x7632); }
+// 2^x, relative error 2^-22, 0 for -inf
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // four codes as two fp16 pairs (exact)
 __device__ __forceinline__ void e4m3x4_to_f16x2(uint32_t four, uint32_t& lo, uint32_t& hi) {
   asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(four));
@@ -184,12 +188,13 @@ struct Layout {
   static constexpr int kKeyWords = DH / 8;                               // element pairs of a lane: DH / 4 elements
   static constexpr int kKeyStep = F8 ? 16 : 8;                           // elements of a load
   static constexpr int kValWords = DH / 16;                              // element pairs of one of eight lanes
+  static constexpr int kValBytes = kRowBytes == 64 ? 8 : 16;             // bytes of a load of one of eight lanes
 };
 
 template <int DH, bool F8>
-__device__ __forceinline__ void load_key(const uint8_t* row, int t, uint4 raw[Layout<DH, F8>::kKeyLoads]) {
+__device__ __forceinline__ void load_key(const uint8_t* chunk, uint4 raw[Layout<DH, F8>::kKeyLoads]) {
 #pragma unroll
-  for (int j = 0; j < Layout<DH, F8>::kKeyLoads; ++j) raw[j] = load_stream16(row + 16 * (t + 4 * j));
+  for (int j = 0; j < Layout<DH, F8>::kKeyLoads; ++j) raw[j] = load_stream16(chunk + 64 * j);
 }
 template <int DH, bool F8>
 __device__ __forceinline__ void key_words(const uint4 raw[Layout<DH, F8>::kKeyLoads], uint32_t w[Layout<DH, F8>::kKeyWords]) {
@@ -216,16 +221,32 @@ template <int DH, bool F8>
 struct ValRaw { uint32_t w[DH * (F8 ? 1 : 2) / 32]; };
 
 template <int DH, bool F8>
-__device__ __forceinline__ void load_val(const uint8_t* row, int g, ValRaw<DH, F8>& raw) {
-  if (F8 && DH == 64) {
-    const uint2 v = load_stream8(row + 8 * g);
+__device__ __forceinline__ void load_val(const uint8_t* chunk, ValRaw<DH, F8>& raw) {
+  if (Layout<DH, F8>::kValBytes == 8) {
+    const uint2 v = load_stream8(chunk);
     raw.w[0] = v.x; raw.w[1] = v.y;
   } else {
 #pragma unroll
-    for (int j = 0; j < DH * (F8 ? 1 : 2) / 128; ++j) {
-      const uint4 v = load_stream16(row + 16 * (g + 8 * j));
+    for (int j = 0; j < Layout<DH, F8>::kRowBytes / 128; ++j) {
+      const uint4 v = load_stream16(chunk + 128 * j);
       raw.w[4 * j] = v.x; raw.w[4 * j + 1] = v.y; raw.w[4 * j + 2] = v.z; raw.w[4 * j + 3] = v.w;
     }
+  }
+}
+// Words u, u + 1 of keys a and b (keys 2t, 2t + 1 of a half tile): the fragments of elements 2u .. 2u + 3, each the pair
+// (a, b) of one dimension.  8-bit codes are paired first and converted as pairs.
+template <int DH, bool F8>
+__device__ __forceinline__ void val_pairs(const ValRaw<DH, F8>& a, const ValRaw<DH, F8>& b, int u, uint32_t f[4]) {
+  if (F8) {
+    const uint32_t x = a.w[u / 2], y = b.w[u / 2];
+    e4m3x4_to_f16x2(__byte_perm(x, y, 0x5140), f[0], f[1]);
+    e4m3x4_to_f16x2(__byte_perm(x, y, 0x7362), f[2], f[3]);
+  } else {
+    const uint32_t x0 = a.w[u], x1 = a.w[F8 ? 0 : u + 1], y0 = b.w[u], y1 = b.w[F8 ? 0 : u + 1];
+    f[0] = __byte_perm(x0, y0, 0x5410);
+    f[1] = __byte_perm(x0, y0, 0x7632);
+    f[2] = __byte_perm(x1, y1, 0x5410);
+    f[3] = __byte_perm(x1, y1, 0x7632);
   }
 }
 template <bool F8>
@@ -233,6 +254,18 @@ __device__ __forceinline__ void mma_step(float c[4], uint32_t a0, uint32_t a1, u
   if (F8) mma16816_f16(c, a0, a1, a2, a3, b0, b1);
   else mma16816_bf16(c, a0, a1, a2, a3, b0, b1);
 }
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+  if (F16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// What scores are taken relative to: their maximum, or 0 where there is none (all -inf).
+__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 
 // A CTA = one row, one key head, up to 8 NT of the query heads that share it, one split of its keys; its warps take the
 // split's tiles of 16 keys in turn, each with its own running maximum and sum, and are joined at the end.
@@ -253,7 +286,7 @@ paged_attention_kernel(const PagedParams p) {
   const int split = blockIdx.y;
   int seq = 0;
   const int len = row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
-  const int per = split_keys(len, p.splits);
+  const int per = split_keys(p, len);
   const int k0 = split * per, k1 = min(len, k0 + per);
   if (k0 >= k1) {
     if (len == 0 && split == 0)
@@ -318,31 +351,44 @@ paged_attention_kernel(const PagedParams p) {
   // tile ahead of that.
   uint4 kraw[2][Lay::kKeyLoads];
   ValRaw<DH, F8> vraw[4];
+  const uint8_t* const k_lane = (const uint8_t*)p.ck + g * Lay::kRowBytes + 16 * t;
+  const uint8_t* const v_lane = (const uint8_t*)p.cv + 2 * t * Lay::kRowBytes + Lay::kValBytes * g;
   size_t at = 0;                       // byte offset of the tile that is loaded next, its number of keys, its block id
   int n_next = 0, page = 0;
   auto find = [&](int key0) {
     n_next = min(kTileKeys, k1 - key0);
-    if (page < 0 || page >= p.n_blocks) {                            // uniform over the warp
+    if ((unsigned)page >= (unsigned)p.n_blocks) {                    // uniform over the warp
       if (lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
-      n_next = 0;
+      n_next = page = 0;
     }
-    at = ((((size_t)max(page, 0) * p.Hkv + hk) << p.log2_block) + (key0 & in_block)) * Lay::kRowBytes;
+    at = ((((size_t)page * p.Hkv + hk) << p.log2_block) + (key0 & in_block)) * Lay::kRowBytes;
   };
   auto load_keys = [&]() {
+    const uint8_t* from = k_lane + at;
+    if (n_next == kTileKeys) {                                       // uniform: a whole tile needs no look at its rows
+      load_key<DH, F8>(from, kraw[0]);
+      load_key<DH, F8>(from + 8 * Lay::kRowBytes, kraw[1]);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      if (g + 8 * i < n_next) load_key<DH, F8>((const uint8_t*)p.ck + at + (g + 8 * i) * Lay::kRowBytes, t, kraw[i]);
-      else
 #pragma unroll
-        for (int j = 0; j < Lay::kKeyLoads; ++j) kraw[i][j] = make_uint4(0u, 0u, 0u, 0u);
+      for (int j = 0; j < Lay::kKeyLoads; ++j) kraw[i][j] = make_uint4(0u, 0u, 0u, 0u);
+      if (g + 8 * i < n_next) load_key<DH, F8>(from + 8 * i * Lay::kRowBytes, kraw[i]);
     }
   };
   auto load_vals = [&]() {
+    const uint8_t* from = v_lane + at;
+    if (n_next == kTileKeys) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_val<DH, F8>(from + ((i & 1) + 8 * (i >> 1)) * Lay::kRowBytes, vraw[i]);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int key = 2 * t + (i & 1) + 8 * (i >> 1);
-      if (key < n_next) load_val<DH, F8>((const uint8_t*)p.cv + at + key * Lay::kRowBytes, g, vraw[i]);
-      else vraw[i] = ValRaw<DH, F8>{};
+      const int key = (i & 1) + 8 * (i >> 1);
+      vraw[i] = ValRaw<DH, F8>{};
+      if (2 * t + key < n_next) load_val<DH, F8>(from + key * Lay::kRowBytes, vraw[i]);
     }
   };
   int key0 = k0 + warp * kTileKeys;
@@ -372,62 +418,63 @@ paged_attention_kernel(const PagedParams p) {
       load_keys();
       if (key0 + 2 * W * kTileKeys < k1) page = pages[(key0 + 2 * W * kTileKeys) >> p.log2_block];
     }
+    // The running maximum is only raised when a score passes it by 2^kSlack: until then the weights are at most
+    // 2^kSlack, which costs no precision, and a tile needs neither the maximum over its keys nor a rescaling.
+    constexpr float kSlack = 8.0f;
+    bool raise = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float (&s)[4] = sc[nt];
+      const float f0 = F8 ? p.scale_log2e * unscale[nt][0] : p.scale_log2e, f1 = F8 ? p.scale_log2e * unscale[nt][1] : p.scale_log2e;
+      s[0] *= f0; s[1] *= f1; s[2] *= f0; s[3] *= f1;
+      if (n_keys < kTileKeys) {
+        if (g >= n_keys) s[0] = s[1] = -INFINITY;
+        if (g + 8 >= n_keys) s[2] = s[3] = -INFINITY;
+      }
+      raise = raise || fmaxf(s[0], s[2]) > m[nt][0] + kSlack || fmaxf(s[1], s[3]) > m[nt][1] + kSlack;
+    }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float (&s)[4] = sc[nt];
+        float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+          mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
+          mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
+        }
+        mx0 = fmaxf(mx0, m[nt][0]);
+        mx1 = fmaxf(mx1, m[nt][1]);
+        // a maximum of -inf (every score so far is -inf): nothing to rescale, and 2^(-inf - 0) = 0
+        const float corr0 = fast_exp2(m[nt][0] - finite_max(mx0)), corr1 = fast_exp2(m[nt][1] - finite_max(mx1));
+        m[nt][0] = mx0; m[nt][1] = mx1;
+        l[nt][0] *= corr0; l[nt][1] *= corr1;
+#pragma unroll
+        for (int u = 0; u < DH / 16; ++u) { o[nt][u][0] *= corr0; o[nt][u][2] *= corr0; o[nt][u][1] *= corr1; o[nt][u][3] *= corr1; }
+      }
+    }
     uint32_t pb[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float (&s)[4] = sc[nt];
-      const float f0 = p.scale_log2e * unscale[nt][0], f1 = p.scale_log2e * unscale[nt][1];
-      const bool in0 = g < n_keys, in1 = g + 8 < n_keys;
-      s[0] = in0 ? s[0] * f0 : -INFINITY;
-      s[1] = in0 ? s[1] * f1 : -INFINITY;
-      s[2] = in1 ? s[2] * f0 : -INFINITY;
-      s[3] = in1 ? s[3] * f1 : -INFINITY;
-      float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
-#pragma unroll
-      for (int d = 4; d < 32; d <<= 1) {
-        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
-        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
-      }
-      mx0 = fmaxf(mx0, m[nt][0]);
-      mx1 = fmaxf(mx1, m[nt][1]);
-      // a maximum of -inf (every score so far is -inf): nothing to rescale, and exp2(-inf - 0) = 0
-      const float ref0 = mx0 == -INFINITY ? 0.0f : mx0, ref1 = mx1 == -INFINITY ? 0.0f : mx1;
-      const float corr0 = exp2f(m[nt][0] - ref0), corr1 = exp2f(m[nt][1] - ref1);
-      m[nt][0] = mx0; m[nt][1] = mx1;
-      s[0] = exp2f(s[0] - ref0); s[2] = exp2f(s[2] - ref0);
-      s[1] = exp2f(s[1] - ref1); s[3] = exp2f(s[3] - ref1);
-      l[nt][0] = l[nt][0] * corr0 + (s[0] + s[2]);
-      l[nt][1] = l[nt][1] * corr1 + (s[1] + s[3]);
-#pragma unroll
-      for (int u = 0; u < DH / 16; ++u) { o[nt][u][0] *= corr0; o[nt][u][2] *= corr0; o[nt][u][1] *= corr1; o[nt][u][3] *= corr1; }
-      // the weights of a tile, rounded to the values' type (relative 2^-9 or 2^-11 each, on terms that are summed in fp32)
-      uint32_t pk[2];
-      if (F8) {
-        const __half2 a = __floats2half2_rn(s[0], s[1]), b = __floats2half2_rn(s[2], s[3]);
-        pk[0] = *reinterpret_cast<const uint32_t*>(&a); pk[1] = *reinterpret_cast<const uint32_t*>(&b);
-      } else {
-        const __nv_bfloat162 a = __floats2bfloat162_rn(s[0], s[1]), b = __floats2bfloat162_rn(s[2], s[3]);
-        pk[0] = *reinterpret_cast<const uint32_t*>(&a); pk[1] = *reinterpret_cast<const uint32_t*>(&b);
-      }
-      pb[nt][0] = transpose8x8(pk[0]);
-      pb[nt][1] = transpose8x8(pk[1]);
+      const float ref0 = finite_max(m[nt][0]), ref1 = finite_max(m[nt][1]);
+      s[0] = fast_exp2(s[0] - ref0); s[2] = fast_exp2(s[2] - ref0);
+      s[1] = fast_exp2(s[1] - ref1); s[3] = fast_exp2(s[3] - ref1);
+      l[nt][0] += s[0] + s[2];
+      l[nt][1] += s[1] + s[3];
+      // the weights of a tile, rounded to the values' type (relative 2^-9 or 2^-12 each, on terms that are summed in fp32)
+      pb[nt][0] = transpose8x8(pack_pair<F8>(s[0], s[1]));
+      pb[nt][1] = transpose8x8(pack_pair<F8>(s[2], s[3]));
     }
 #pragma unroll
     for (int u = 0; u < Lay::kValWords; u += 2) {
-      uint32_t w0[4], w1[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (F8) {
-          e4m3x4_to_f16x2(vraw[i].w[u / 2], w0[i], w1[i]);
-        } else {
-          w0[i] = vraw[i].w[F8 ? 0 : u];
-          w1[i] = vraw[i].w[F8 ? 0 : u + 1];
-        }
-      }
+      uint32_t lo[4], hi[4];
+      val_pairs<DH, F8>(vraw[0], vraw[1], u, lo);
+      val_pairs<DH, F8>(vraw[2], vraw[3], u, hi);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        mma_step<F8>(o[nt][u], pair_lo(w0[0], w0[1]), pair_hi(w0[0], w0[1]), pair_lo(w0[2], w0[3]), pair_hi(w0[2], w0[3]), pb[nt][0], pb[nt][1]);
-        mma_step<F8>(o[nt][u + 1], pair_lo(w1[0], w1[1]), pair_hi(w1[0], w1[1]), pair_lo(w1[2], w1[3]), pair_hi(w1[2], w1[3]), pb[nt][0], pb[nt][1]);
+        mma_step<F8>(o[nt][u], lo[0], lo[1], hi[0], hi[1], pb[nt][0], pb[nt][1]);
+        mma_step<F8>(o[nt][u + 1], lo[2], lo[3], hi[2], hi[3], pb[nt][0], pb[nt][1]);
       }
     }
     if (more) load_vals();
@@ -462,11 +509,11 @@ paged_attention_kernel(const PagedParams p) {
     float mx = -INFINITY;
 #pragma unroll
     for (int w = 0; w < W; ++w) mx = fmaxf(mx, sm_m[w][h]);
-    const float ref = mx == -INFINITY ? 0.0f : mx;
+    const float ref = finite_max(mx);
     float sum = 0.0f, val = 0.0f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const float c = exp2f(sm_m[w][h] - ref);
+      const float c = fast_exp2(sm_m[w][h] - ref);
       sum += c * sm_l[w][h];
       val += c * sm_o[w][h][d];
     }
@@ -495,7 +542,7 @@ paged_join_kernel(const PagedParams p) {
   int seq = 0;
   const int len = row_keys(p, row, &seq, false);
   if (len == 0) return;                                // the first split wrote the zeros
-  const int per = split_keys(len, p.splits), n = (len + per - 1) / per;
+  const int per = split_keys(p, len), n = (len + per - 1) / per;
   const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + item * p.splits;
   float mx = -INFINITY;
   for (int s = threadIdx.x; s < n; s += kJoinThreads) mx = fmaxf(mx, ml[s].x);
@@ -505,8 +552,8 @@ paged_join_kernel(const PagedParams p) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kJoinThreads / 32; ++w) mx = fmaxf(mx, part_max[w]);
-  const float ref = mx == -INFINITY ? 0.0f : mx;
-  for (int s = threadIdx.x; s < n; s += kJoinThreads) weight[s] = exp2f(ml[s].x - ref);
+  const float ref = finite_max(mx);
+  for (int s = threadIdx.x; s < n; s += kJoinThreads) weight[s] = fast_exp2(ml[s].x - ref);
   __syncthreads();
   const int c = threadIdx.x % kCols, r = threadIdx.x / kCols;
   const float4* o = reinterpret_cast<const float4*>(p.part_o) + item * p.splits * kCols + c;
@@ -540,11 +587,13 @@ int log2_of(int v) {
   return n;
 }
 
-// Splits of the keys: as many as give every SM a few CTAs, none of them shorter than 256 keys of the longest row.
-int attention_splits(int64_t R, int Hkv, int chunks, int64_t max_len) {
-  const int64_t ctas = R * Hkv * chunks;
-  const int64_t want = (148 * 4 + ctas - 1) / ctas;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(want, max_len / 256));
+// Splits of the keys.  Few CTAs (rows x key heads): as many splits as fill the SMs once, but none shorter than 128 keys.
+// More of them: pieces of 512 keys, so that rows of different lengths share the SMs evenly, as long as the grid stays
+// within eight times what the SMs hold.
+int attention_splits(int64_t R, int Hkv, int chunks, int dh, int64_t max_len) {
+  const int64_t slots = 148 * (dh == 64 ? 4 : 3), ctas = R * Hkv * chunks;
+  const int64_t fill = std::min<int64_t>(slots / ctas, max_len / 128), even = R > 1 ? std::min<int64_t>(max_len / 512, 8 * slots / ctas) : 1;
+  return (int)std::max<int64_t>(1, std::max(fill, even));
 }
 int head_chunks(int G) { return G <= 8 ? 1 : (G + 15) / 16; }
 
@@ -600,7 +649,7 @@ int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat
 }
 
 size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
-  const int splits = attention_splits(R, Hkv, head_chunks(H / Hkv), max_len);
+  const int splits = attention_splits(R, Hkv, head_chunks(H / Hkv), dh, max_len);
   return splits > 1 ? (size_t)R * H * splits * (dh + 2) * sizeof(float) : 0;
 }
 
@@ -609,11 +658,12 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
                            int H, void* ws, size_t ws_bytes, int* status, cudaStream_t st) {
   const int G = H / c.n_kv_heads, chunks = head_chunks(G), max_len = width * c.block_size;
   if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
-  const int splits = attention_splits(R, c.n_kv_heads, chunks, max_len);
+  const int splits = attention_splits(R, c.n_kv_heads, chunks, c.head_dim, max_len);
+  const int min_keys = (int64_t)R * c.n_kv_heads * chunks * splits > 148 * 4 ? 512 : 128;
   const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len);
   if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 255))) return QZO_ERR_WORKSPACE;
   PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
-                R, H, c.n_kv_heads, G, chunks, splits, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
+                R, H, c.n_kv_heads, G, chunks, splits, min_keys, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
   if (splits > 1) {
     p.part_o = (float*)ws;
     p.part_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
