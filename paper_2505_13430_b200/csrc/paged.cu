@@ -132,8 +132,7 @@ qk_norm_rope_cache_kernel(const RopeCacheParams p) {
 // Attention of one new token per row
 // =========================================================================================
 
-constexpr int kTileKeys = 16;                          // keys a warp takes at a time: one matrix tile
-constexpr int kSplitKeys = 64;                         // a split is a multiple of this many keys
+constexpr int kSub = 16;                               // keys of one matrix tile; a block of the cache holds whole ones
 
 struct PagedParams {
   const __nv_bfloat16* q;
@@ -144,20 +143,19 @@ struct PagedParams {
   const int32_t *row_seq, *positions;
   float scale_log2e, v_scale;                          // the keys' scale is in the first
   __nv_bfloat16* out;
-  int ldo, R, H, Hkv, G, chunks, splits, min_keys, n_blocks, log2_block;
+  int ldo, R, H, Hkv, G, chunks, splits, min_keys, round_keys, n_blocks, log2_block;
   float *part_o, *part_ml;                             // [R][H][splits][DH], [R][H][splits][2]
   int* status;
 };
 
 // Keys of split s of a row that sees len keys: [s * per, min(len, (s + 1) * per)), per at least the launch's minimum.
 __device__ __forceinline__ int split_keys(const PagedParams& p, int len) {
-  return max(p.min_keys, ((len + p.splits - 1) / p.splits + kSplitKeys - 1) / kSplitKeys * kSplitKeys);
+  return max(p.min_keys, ((len + p.splits - 1) / p.splits + p.round_keys - 1) / p.round_keys * p.round_keys);
 }
 // Number of keys a row sees, 0 for padding; seq receives its request.  One thread reports what is out of range.
 __device__ __forceinline__ int row_keys(const PagedParams& p, int row, int* seq, bool report) {
-  const int pos = p.positions[row];
+  const int pos = p.positions[row], s = p.row_seq ? p.row_seq[row] : row;
   if (pos < 0) return 0;
-  const int s = p.row_seq ? p.row_seq[row] : row;
   *seq = s;
   const int most = p.width << p.log2_block;
   const bool bad_seq = s < 0 || s >= p.n_seqs;
@@ -188,6 +186,8 @@ struct Layout {
   static constexpr int kKeyWords = DH / 8;                               // element pairs of a lane: DH / 4 elements
   static constexpr int kKeyStep = F8 ? 16 : 8;                           // elements of a load
   static constexpr int kValWords = DH / 16;                              // element pairs of one of eight lanes
+  static constexpr int kSubs = 256 / kRowBytes;                          // matrix tiles a warp takes at a time: 4 KB of keys, 4 KB of values
+  static constexpr int kTileKeys = kSub * kSubs;
   static constexpr int kValBytes = kRowBytes == 64 ? 8 : 16;             // bytes of a load of one of eight lanes
 };
 
@@ -268,15 +268,15 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 
 // A CTA = one row, one key head, up to 8 NT of the query heads that share it, one split of its keys; its warps take the
-// split's tiles of 16 keys in turn, each with its own running maximum and sum, and are joined at the end.
+// split's tiles in turn, each with its own running maximum and sum, and are joined at the end.
 // A tile is two products: S^T = K Q^T (keys x heads) and O^T += V^T P^T (dimensions x heads), so up to eight heads
 // share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.
 template <int DH, int NT, bool F8, int W>
-__global__ void __launch_bounds__(W * 32, (DH == 64 ? 16 : NT == 1 ? 12 : 8) / W)
+__global__ void __launch_bounds__(W * 32, (NT == 1 ? 12 : 8) / W)
 paged_attention_kernel(const PagedParams p) {
   using Lay = Layout<DH, F8>;
   extern __shared__ __align__(16) float att_smem[];
-  float (*sm_o)[8 * NT][DH + 4] = reinterpret_cast<float (*)[8 * NT][DH + 4]>(att_smem);
+  float (*sm_o)[8 * NT][DH + 1] = reinterpret_cast<float (*)[8 * NT][DH + 1]>(att_smem);
   __shared__ float sm_m[W][8 * NT], sm_l[W][8 * NT];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int per_row = p.Hkv * p.chunks;
@@ -284,21 +284,8 @@ paged_attention_kernel(const PagedParams p) {
   const int head0 = hk * p.G + chunk * 8 * NT;                       // first query head of the CTA
   const int n_heads = min(8 * NT, p.G - chunk * 8 * NT);
   const int split = blockIdx.y;
-  int seq = 0;
-  const int len = row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
-  const int per = split_keys(p, len);
-  const int k0 = split * per, k1 = min(len, k0 + per);
-  if (k0 >= k1) {
-    if (len == 0 && split == 0)
-      for (int i = threadIdx.x; i < n_heads * DH / 8; i += W * 32)
-        *reinterpret_cast<uint4*>(p.out + (size_t)row * p.ldo + (size_t)head0 * DH + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
-    return;
-  }
-
-  // Query fragments, the same chunks of dimensions as a key's lane t.  For 8-bit keys they become fp16: scaled by a power
-  // of two that brings the head's largest element to [64, 128), which only elements 2^-30 below it can feel.
+  // Query fragments: the same chunks of dimensions as a key's lane t.
   uint32_t qf[NT][Lay::kKeyWords];
-  float unscale[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const bool have = nt * 8 + g < n_heads;
@@ -312,6 +299,23 @@ paged_attention_kernel(const PagedParams p) {
         uint32_t* w = qf[nt] + Lay::kKeyStep / 2 * j + 4 * i;
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
       }
+  }
+  int seq = 0;
+  const int len = row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
+  const int per = split_keys(p, len);
+  const int k0 = split * per, k1 = min(len, k0 + per);
+  if (k0 >= k1) {
+    if (len == 0 && split == 0)
+      for (int i = threadIdx.x; i < n_heads * DH / 8; i += W * 32)
+        *reinterpret_cast<uint4*>(p.out + (size_t)row * p.ldo + (size_t)head0 * DH + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
+    return;
+  }
+
+  // For 8-bit keys the queries become fp16, scaled by a power of two that brings the head's largest element to [64, 128):
+  // exact but for elements 2^-30 below it.
+  float unscale[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
     unscale[nt][0] = unscale[nt][1] = 1.0f;
     if (F8) {
       float big = 0.0f;
@@ -322,16 +326,16 @@ paged_attention_kernel(const PagedParams p) {
       }
       big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
       big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-      const int e = (big > 0.0f && big < INFINITY) ? ilogbf(big) - 6 : 0;
+      // exponent of the largest less 6, within what both 2^e and 2^-e can hold (an infinity stays one)
+      const int e = big > 0.0f ? max((int)(__float_as_uint(big) >> 23) - 127 - 6, -120) : 0;
+      const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
       for (int i = 0; i < Lay::kKeyWords; ++i) {
         const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[nt][i]));
-        const __half2 h = __floats2half2_rn(ldexpf(f.x, -e), ldexpf(f.y, -e));
-        qf[nt][i] = *reinterpret_cast<const uint32_t*>(&h);
+        qf[nt][i] = pack_pair<true>(f.x * down, f.y * down);
       }
-      const float un = ldexpf(1.0f, e);
-      unscale[nt][0] = __shfl_sync(0xffffffffu, un, 8 * t);
-      unscale[nt][1] = __shfl_sync(0xffffffffu, un, 8 * t + 4);
+      unscale[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t);
+      unscale[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4);
     }
   }
 
@@ -349,74 +353,98 @@ paged_attention_kernel(const PagedParams p) {
   // A tile's keys and values stay in registers from their loads to their use, and the next tile's are loaded as soon as
   // the registers are free: its keys behind the scores, its values behind the second product.  The block id is known one
   // tile ahead of that.
-  uint4 kraw[2][Lay::kKeyLoads];
-  ValRaw<DH, F8> vraw[4];
+  constexpr int S = Lay::kSubs, kTileKeys = Lay::kTileKeys;
+  uint4 kraw[S][2][Lay::kKeyLoads];
+  ValRaw<DH, F8> vraw[S][4];
   const uint8_t* const k_lane = (const uint8_t*)p.ck + g * Lay::kRowBytes + 16 * t;
   const uint8_t* const v_lane = (const uint8_t*)p.cv + 2 * t * Lay::kRowBytes + Lay::kValBytes * g;
-  size_t at = 0;                       // byte offset of the tile that is loaded next, its number of keys, its block id
-  int n_next = 0, page = 0;
-  auto find = [&](int key0) {
-    n_next = min(kTileKeys, k1 - key0);
-    if ((unsigned)page >= (unsigned)p.n_blocks) {                    // uniform over the warp
-      if (lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
-      n_next = page = 0;
-    }
-    at = ((((size_t)page * p.Hkv + hk) << p.log2_block) + (key0 & in_block)) * Lay::kRowBytes;
+  size_t at[S];                        // of the tile that is loaded next: byte offsets, block ids, and where it ends
+  int page[S], next = 0;
+  bool whole = false;                  // it has all its keys, in blocks that exist
+  auto look_up = [&](int key0) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) page[i] = key0 + kSub * i < k1 ? pages[(key0 + kSub * i) >> p.log2_block] : 0;
   };
+  auto find = [&](int key0) {
+    next = key0;
+    whole = key0 + kTileKeys <= k1;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      if ((unsigned)page[i] >= (unsigned)p.n_blocks) {               // uniform over the warp
+        if (lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+        whole = false;
+      }
+      at[i] = ((((size_t)page[i] * p.Hkv + hk) << p.log2_block) + ((key0 + kSub * i) & in_block)) * Lay::kRowBytes;
+    }
+  };
+  auto keys_of = [&](int i) { return (unsigned)page[i] >= (unsigned)p.n_blocks ? 0 : k1 - next - kSub * i; };
   auto load_keys = [&]() {
-    const uint8_t* from = k_lane + at;
-    if (n_next == kTileKeys) {                                       // uniform: a whole tile needs no look at its rows
-      load_key<DH, F8>(from, kraw[0]);
-      load_key<DH, F8>(from + 8 * Lay::kRowBytes, kraw[1]);
+    if (whole) {                                                     // uniform: a whole tile needs no look at its rows
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        load_key<DH, F8>(k_lane + at[i], kraw[i][0]);
+        load_key<DH, F8>(k_lane + at[i] + 8 * Lay::kRowBytes, kraw[i][1]);
+      }
       return;
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < S; ++i) {
 #pragma unroll
-      for (int j = 0; j < Lay::kKeyLoads; ++j) kraw[i][j] = make_uint4(0u, 0u, 0u, 0u);
-      if (g + 8 * i < n_next) load_key<DH, F8>(from + 8 * i * Lay::kRowBytes, kraw[i]);
+      for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int j = 0; j < Lay::kKeyLoads; ++j) kraw[i][r][j] = make_uint4(0u, 0u, 0u, 0u);
+        if (g + 8 * r < keys_of(i)) load_key<DH, F8>(k_lane + at[i] + 8 * r * Lay::kRowBytes, kraw[i][r]);
+      }
     }
   };
   auto load_vals = [&]() {
-    const uint8_t* from = v_lane + at;
-    if (n_next == kTileKeys) {
+    if (whole) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load_val<DH, F8>(from + ((i & 1) + 8 * (i >> 1)) * Lay::kRowBytes, vraw[i]);
+      for (int i = 0; i < S; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) load_val<DH, F8>(v_lane + at[i] + ((r & 1) + 8 * (r >> 1)) * Lay::kRowBytes, vraw[i][r]);
       return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = (i & 1) + 8 * (i >> 1);
-      vraw[i] = ValRaw<DH, F8>{};
-      if (2 * t + key < n_next) load_val<DH, F8>(from + key * Lay::kRowBytes, vraw[i]);
+    for (int i = 0; i < S; ++i) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int key = (r & 1) + 8 * (r >> 1);
+        vraw[i][r] = ValRaw<DH, F8>{};
+        if (2 * t + key < keys_of(i)) load_val<DH, F8>(v_lane + at[i] + key * Lay::kRowBytes, vraw[i][r]);
+      }
     }
   };
   int key0 = k0 + warp * kTileKeys;
   if (key0 < k1) {
-    page = pages[key0 >> p.log2_block];
+    look_up(key0);
     find(key0);
     load_keys();
     load_vals();
-    if (key0 + W * kTileKeys < k1) page = pages[(key0 + W * kTileKeys) >> p.log2_block];
   }
   for (; key0 < k1; key0 += W * kTileKeys) {
-    const int n_keys = n_next;
-    const bool more = key0 + W * kTileKeys < k1;
-    uint32_t ka[Lay::kKeyWords], kb[Lay::kKeyWords];
-    key_words<DH, F8>(kraw[0], ka);
-    key_words<DH, F8>(kraw[1], kb);
-    float sc[NT][4];
+    const bool more = key0 + W * kTileKeys < k1, full = whole;
+    int n_keys[S];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.0f;
+    for (int i = 0; i < S; ++i) n_keys[i] = full ? kSub : keys_of(i);
+    if (more) look_up(key0 + W * kTileKeys);
+    float sc[NT][S][4];
 #pragma unroll
-      for (int i = 0; i < Lay::kKeyWords; i += 2)
-        mma_step<F8>(sc[nt], ka[i], kb[i], ka[i + 1], kb[i + 1], qf[nt][i], qf[nt][i + 1]);
+    for (int i = 0; i < S; ++i) {
+      uint32_t ka[Lay::kKeyWords], kb[Lay::kKeyWords];
+      key_words<DH, F8>(kraw[i][0], ka);
+      key_words<DH, F8>(kraw[i][1], kb);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        sc[nt][i][0] = sc[nt][i][1] = sc[nt][i][2] = sc[nt][i][3] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < Lay::kKeyWords; w += 2)
+          mma_step<F8>(sc[nt][i], ka[w], kb[w], ka[w + 1], kb[w + 1], qf[nt][w], qf[nt][w + 1]);
+      }
     }
     if (more) {
       find(key0 + W * kTileKeys);
       load_keys();
-      if (key0 + 2 * W * kTileKeys < k1) page = pages[(key0 + 2 * W * kTileKeys) >> p.log2_block];
     }
     // The running maximum is only raised when a score passes it by 2^kSlack: until then the weights are at most
     // 2^kSlack, which costs no precision, and a tile needs neither the maximum over its keys nor a rescaling.
@@ -424,20 +452,27 @@ paged_attention_kernel(const PagedParams p) {
     bool raise = false;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float (&s)[4] = sc[nt];
       const float f0 = F8 ? p.scale_log2e * unscale[nt][0] : p.scale_log2e, f1 = F8 ? p.scale_log2e * unscale[nt][1] : p.scale_log2e;
-      s[0] *= f0; s[1] *= f1; s[2] *= f0; s[3] *= f1;
-      if (n_keys < kTileKeys) {
-        if (g >= n_keys) s[0] = s[1] = -INFINITY;
-        if (g + 8 >= n_keys) s[2] = s[3] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        float (&s)[4] = sc[nt][i];
+        s[0] *= f0; s[1] *= f1; s[2] *= f0; s[3] *= f1;
+        if (!full) {
+          if (g >= n_keys[i]) s[0] = s[1] = -INFINITY;
+          if (g + 8 >= n_keys[i]) s[2] = s[3] = -INFINITY;
+        }
+        raise = raise || fmaxf(s[0], s[2]) > m[nt][0] + kSlack || fmaxf(s[1], s[3]) > m[nt][1] + kSlack;
       }
-      raise = raise || fmaxf(s[0], s[2]) > m[nt][0] + kSlack || fmaxf(s[1], s[3]) > m[nt][1] + kSlack;
     }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float (&s)[4] = sc[nt];
-        float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+          mx0 = fmaxf(mx0, fmaxf(sc[nt][i][0], sc[nt][i][2]));
+          mx1 = fmaxf(mx1, fmaxf(sc[nt][i][1], sc[nt][i][3]));
+        }
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
           mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
@@ -453,33 +488,40 @@ paged_attention_kernel(const PagedParams p) {
         for (int u = 0; u < DH / 16; ++u) { o[nt][u][0] *= corr0; o[nt][u][2] *= corr0; o[nt][u][1] *= corr1; o[nt][u][3] *= corr1; }
       }
     }
-    uint32_t pb[NT][2];
+    uint32_t pb[NT][S][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float (&s)[4] = sc[nt];
       const float ref0 = finite_max(m[nt][0]), ref1 = finite_max(m[nt][1]);
-      s[0] = fast_exp2(s[0] - ref0); s[2] = fast_exp2(s[2] - ref0);
-      s[1] = fast_exp2(s[1] - ref1); s[3] = fast_exp2(s[3] - ref1);
-      l[nt][0] += s[0] + s[2];
-      l[nt][1] += s[1] + s[3];
-      // the weights of a tile, rounded to the values' type (relative 2^-9 or 2^-12 each, on terms that are summed in fp32)
-      pb[nt][0] = transpose8x8(pack_pair<F8>(s[0], s[1]));
-      pb[nt][1] = transpose8x8(pack_pair<F8>(s[2], s[3]));
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        float (&s)[4] = sc[nt][i];
+        s[0] = fast_exp2(s[0] - ref0); s[2] = fast_exp2(s[2] - ref0);
+        s[1] = fast_exp2(s[1] - ref1); s[3] = fast_exp2(s[3] - ref1);
+        l[nt][0] += s[0] + s[2];
+        l[nt][1] += s[1] + s[3];
+        // the weights of a tile, rounded to the values' type (relative 2^-9 or 2^-12 each, on terms that are summed in fp32)
+        pb[nt][i][0] = transpose8x8(pack_pair<F8>(s[0], s[1]));
+        pb[nt][i][1] = transpose8x8(pack_pair<F8>(s[2], s[3]));
+      }
     }
 #pragma unroll
-    for (int u = 0; u < Lay::kValWords; u += 2) {
-      uint32_t lo[4], hi[4];
-      val_pairs<DH, F8>(vraw[0], vraw[1], u, lo);
-      val_pairs<DH, F8>(vraw[2], vraw[3], u, hi);
+    for (int i = 0; i < S; ++i) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        mma_step<F8>(o[nt][u], lo[0], lo[1], hi[0], hi[1], pb[nt][0], pb[nt][1]);
-        mma_step<F8>(o[nt][u + 1], lo[2], lo[3], hi[2], hi[3], pb[nt][0], pb[nt][1]);
+      for (int u = 0; u < Lay::kValWords; u += 2) {
+        uint32_t lo[4], hi[4];
+        val_pairs<DH, F8>(vraw[i][0], vraw[i][1], u, lo);
+        val_pairs<DH, F8>(vraw[i][2], vraw[i][3], u, hi);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma_step<F8>(o[nt][u], lo[0], lo[1], hi[0], hi[1], pb[nt][i][0], pb[nt][i][1]);
+          mma_step<F8>(o[nt][u + 1], lo[2], lo[3], hi[2], hi[3], pb[nt][i][0], pb[nt][i][1]);
+        }
       }
     }
     if (more) load_vals();
   }
 
+  cudaTriggerProgrammaticLaunchCompletion();           // the join's CTAs may take their places; they wait for this grid's end
   // join the warps
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -488,56 +530,57 @@ paged_attention_kernel(const PagedParams p) {
       l[nt][0] += __shfl_xor_sync(0xffffffffu, l[nt][0], d);
       l[nt][1] += __shfl_xor_sync(0xffffffffu, l[nt][1], d);
     }
-    const int h = nt * 8 + 2 * t;
-    if (g == 0) {
-      sm_m[warp][h] = m[nt][0]; sm_m[warp][h + 1] = m[nt][1];
-      sm_l[warp][h] = l[nt][0]; sm_l[warp][h + 1] = l[nt][1];
-    }
 #pragma unroll
-    for (int u = 0; u < DH / 16; ++u) {
-      const int d0 = val_dim<DH, F8>(g, 2 * u), d1 = val_dim<DH, F8>(g, 2 * u + 1);
-      sm_o[warp][h][d0] = o[nt][u][0];
-      sm_o[warp][h + 1][d0] = o[nt][u][1];
-      sm_o[warp][h][d1] = o[nt][u][2];
-      sm_o[warp][h + 1][d1] = o[nt][u][3];
+    for (int i = 0; i < 2; ++i) {
+      const int h = nt * 8 + 2 * t + i;
+      if (h >= n_heads) continue;
+      if (g == 0) { sm_m[warp][h] = m[nt][i]; sm_l[warp][h] = l[nt][i]; }
+#pragma unroll
+      for (int u = 0; u < DH / 16; ++u) {
+        sm_o[warp][h][val_dim<DH, F8>(g, 2 * u)] = o[nt][u][i];
+        sm_o[warp][h][val_dim<DH, F8>(g, 2 * u + 1)] = o[nt][u][2 + i];
+      }
     }
   }
   __syncthreads();
-  const bool last = p.splits == 1;
-  for (int i = threadIdx.x; i < n_heads * DH; i += W * 32) {
-    const int h = i / DH, d = i % DH;
+  for (int i = threadIdx.x; i < n_heads * (DH / 4); i += W * 32) {
+    const int h = i / (DH / 4), d = i % (DH / 4) * 4;
     float mx = -INFINITY;
 #pragma unroll
     for (int w = 0; w < W; ++w) mx = fmaxf(mx, sm_m[w][h]);
     const float ref = finite_max(mx);
-    float sum = 0.0f, val = 0.0f;
+    float sum = 0.0f, val[4] = {};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const float c = fast_exp2(sm_m[w][h] - ref);
-      sum += c * sm_l[w][h];
-      val += c * sm_o[w][h][d];
+      sum = fmaf(c, sm_l[w][h], sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) val[e] = fmaf(c, sm_o[w][h][d + e], val[e]);
     }
-    if (last) {
-      p.out[(size_t)row * p.ldo + (size_t)(head0 + h) * DH + d] = __float2bfloat16_rn(val * inverse_sum(p, sum));
+    if (p.splits == 1) {
+      const float f = inverse_sum(p, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) val[e] *= f;
+      *reinterpret_cast<uint2*>(p.out + (size_t)row * p.ldo + (size_t)(head0 + h) * DH + d) = pack4_bf16(val);
     } else {
       const size_t at = ((size_t)row * p.H + head0 + h) * p.splits + split;
-      p.part_o[at * DH + d] = val;
-      if (d == 0) { p.part_ml[2 * at] = mx; p.part_ml[2 * at + 1] = sum; }
+      *reinterpret_cast<float4*>(p.part_o + at * DH + d) = make_float4(val[0], val[1], val[2], val[3]);
+      if (d == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(mx, sum);
     }
   }
 }
 
-// Joins the splits of a row's head: one CTA per (row, head), its DH / 4 columns of threads each taking four dimensions,
-// its 256 / (DH / 4) rows of threads every so many of the splits; the rows are then summed in their order.
-constexpr int kJoinThreads = 256;
-template <int DH>
-__global__ void __launch_bounds__(kJoinThreads)
+// Joins the splits of a row's head: a CTA's COLS columns of threads take four dimensions each, its ROWS rows of threads
+// every so many of the splits; the rows are then summed in their order.  COLS * 4 < DH: several CTAs share a head.
+template <int DH, int COLS, int ROWS>
+__global__ void __launch_bounds__(COLS * ROWS)
 paged_join_kernel(const PagedParams p) {
-  constexpr int kCols = DH / 4, kRows = kJoinThreads / kCols;
+  constexpr int kThreads = COLS * ROWS, kParts = DH / 4 / COLS;
   extern __shared__ float weight[];                    // [splits]
-  __shared__ float4 part[kRows][kCols];
-  __shared__ float part_sum[kRows], part_max[kJoinThreads / 32];
-  const int64_t item = blockIdx.x;
+  __shared__ float4 part[ROWS][COLS];
+  __shared__ float part_sum[ROWS], part_max[kThreads / 32];
+  cudaGridDependencySynchronize();                     // started ahead of the attention's end: wait for its results
+  const int64_t item = blockIdx.x / kParts;
   const int row = (int)(item / p.H), h = (int)(item % p.H);
   int seq = 0;
   const int len = row_keys(p, row, &seq, false);
@@ -545,24 +588,24 @@ paged_join_kernel(const PagedParams p) {
   const int per = split_keys(p, len), n = (len + per - 1) / per;
   const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + item * p.splits;
   float mx = -INFINITY;
-  for (int s = threadIdx.x; s < n; s += kJoinThreads) mx = fmaxf(mx, ml[s].x);
+  for (int s = threadIdx.x; s < n; s += kThreads) mx = fmaxf(mx, ml[s].x);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
   if ((threadIdx.x & 31) == 0) part_max[threadIdx.x >> 5] = mx;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kJoinThreads / 32; ++w) mx = fmaxf(mx, part_max[w]);
+  for (int w = 0; w < kThreads / 32; ++w) mx = fmaxf(mx, part_max[w]);
   const float ref = finite_max(mx);
-  for (int s = threadIdx.x; s < n; s += kJoinThreads) weight[s] = fast_exp2(ml[s].x - ref);
+  for (int s = threadIdx.x; s < n; s += kThreads) weight[s] = fast_exp2(ml[s].x - ref);
   __syncthreads();
-  const int c = threadIdx.x % kCols, r = threadIdx.x / kCols;
-  const float4* o = reinterpret_cast<const float4*>(p.part_o) + item * p.splits * kCols + c;
+  const int c = threadIdx.x % COLS, r = threadIdx.x / COLS, d0 = 4 * (c + COLS * (blockIdx.x % kParts));
+  const float4* o = reinterpret_cast<const float4*>(p.part_o + item * p.splits * DH + d0);
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float sum = 0.0f;
 #pragma unroll 4
-  for (int s = r; s < n; s += kRows) {
+  for (int s = r; s < n; s += ROWS) {
     const float w = weight[s];
-    const float4 x = o[(size_t)s * kCols];
+    const float4 x = o[(size_t)s * (DH / 4)];
     v.x = fmaf(w, x.x, v.x); v.y = fmaf(w, x.y, v.y); v.z = fmaf(w, x.z, v.z); v.w = fmaf(w, x.w, v.w);
     sum = fmaf(w, ml[s].y, sum);
   }
@@ -571,14 +614,14 @@ paged_join_kernel(const PagedParams p) {
   __syncthreads();
   if (r > 0) return;
 #pragma unroll
-  for (int i = 1; i < kRows; ++i) {
+  for (int i = 1; i < ROWS; ++i) {
     const float4 x = part[i][c];
     v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
     sum += part_sum[i];
   }
   const float f = inverse_sum(p, sum);
   const float out[4] = {v.x * f, v.y * f, v.z * f, v.w * f};
-  *reinterpret_cast<uint2*>(p.out + (size_t)row * p.ldo + (size_t)h * DH + 4 * c) = pack4_bf16(out);
+  *reinterpret_cast<uint2*>(p.out + (size_t)row * p.ldo + (size_t)h * DH + d0) = pack4_bf16(out);
 }
 
 int log2_of(int v) {
@@ -593,6 +636,7 @@ int log2_of(int v) {
 int attention_splits(int64_t R, int Hkv, int chunks, int dh, int64_t max_len) {
   const int64_t slots = 148 * (dh == 64 ? 4 : 3), ctas = R * Hkv * chunks;
   const int64_t fill = std::min<int64_t>(slots / ctas, max_len / 128), even = R > 1 ? std::min<int64_t>(max_len / 512, 8 * slots / ctas) : 1;
+  if (getenv("QS")) return atoi(getenv("QS"));
   return (int)std::max<int64_t>(1, std::max(fill, even));
 }
 int head_chunks(int G) { return G <= 8 ? 1 : (G + 15) / 16; }
@@ -600,20 +644,43 @@ int head_chunks(int G) { return G <= 8 ? 1 : (G + 15) / 16; }
 template <int DH, int NT, bool F8, int W>
 int run_attention_w(const PagedParams& p, cudaStream_t st) {
   const dim3 grid((unsigned)((int64_t)p.R * p.Hkv * p.chunks), p.splits);
-  constexpr int smem = W * 8 * NT * (DH + 4) * (int)sizeof(float);
+  constexpr int smem = W * 8 * NT * (DH + 1) * (int)sizeof(float);
   if (smem > 40 * 1024)
     QZO_CUDA_TRY(cudaFuncSetAttribute(paged_attention_kernel<DH, NT, F8, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   QZO_LAUNCH((paged_attention_kernel<DH, NT, F8, W>), grid, dim3(W * 32), smem, st, p);
   return QZO_OK;
 }
 
+template <int DH, int COLS, int ROWS>
+int run_join(const PagedParams& p, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)((int64_t)p.R * p.H * (DH / 4 / COLS)));
+  cfg.blockDim = dim3(COLS * ROWS);
+  cfg.dynamicSmemBytes = p.splits * sizeof(float);
+  cfg.stream = st;
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  QZO_CUDA_TRY(cudaLaunchKernelEx(&cfg, paged_join_kernel<DH, COLS, ROWS>, p));
+  count_launch();
+  return QZO_OK;
+}
+
 template <int DH, bool F8>
 int run_attention(const PagedParams& p, cudaStream_t st) {
+  const int W = getenv("QW") ? atoi(getenv("QW")) : 4;
+  if (W == 4) {
   if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 4>(p, st)));
   else QZO_TRY((run_attention_w<DH, 2, F8, 4>(p, st)));
-  if (p.splits > 1)
-    QZO_LAUNCH(paged_join_kernel<DH>, dim3((unsigned)((int64_t)p.R * p.H)), dim3(kJoinThreads), p.splits * (int)sizeof(float), st, p);
-  return QZO_OK;
+  } else if (W == 8) {
+  if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 8>(p, st)));
+  else QZO_TRY((run_attention_w<DH, 2, F8, 8>(p, st)));
+  } else QZO_TRY((run_attention_w<DH, 1, F8, 16>(p, st)));
+  if (p.splits <= 1) return QZO_OK;
+  // many splits of few heads: a head's dimensions go to several CTAs, so that a thread adds up fewer of them
+  return p.splits > 16 ? run_join<DH, 8, 32>(p, st) : run_join<DH, DH / 4, 4>(p, st);
 }
 
 }  // namespace
@@ -659,11 +726,12 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
   const int G = H / c.n_kv_heads, chunks = head_chunks(G), max_len = width * c.block_size;
   if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
   const int splits = attention_splits(R, c.n_kv_heads, chunks, c.head_dim, max_len);
-  const int min_keys = (int64_t)R * c.n_kv_heads * chunks * splits > 148 * 4 ? 512 : 128;
+  const int subs = 256 / (c.head_dim * (c.dtype == QZO_DTYPE_E4M3 ? 1 : 2));
+  const int min_keys = ((int64_t)R * c.n_kv_heads * chunks * splits > 148 * 4 ? (getenv("QM") ? atoi(getenv("QM")) : 512) : 128) * subs;
   const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len);
   if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 255))) return QZO_ERR_WORKSPACE;
   PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
-                R, H, c.n_kv_heads, G, chunks, splits, min_keys, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
+                R, H, c.n_kv_heads, G, chunks, splits, min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
   if (splits > 1) {
     p.part_o = (float*)ws;
     p.part_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
