@@ -69,7 +69,8 @@ int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat
                               const int32_t* positions, const int32_t* slots, __nv_bfloat16* q_out, int ldqo,
                               const qzo_kv_cache& c, int T, int H, int* status, cudaStream_t st);
 size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len);
+// fewer_splits: a workspace that is too small for the splits of paged_attention_bytes gets as many as it holds
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
                            const int32_t* row_seq, const int32_t* positions, float scale, __nv_bfloat16* out, int ldo, int R,
-                           int H, void* ws, size_t ws_bytes, int* status, cudaStream_t st);
+                           int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st);
 }  // namespace qzo

@@ -367,7 +367,7 @@ int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, cons
                                       llama ? m->rope_cs : nullptr, d.max_seq, positions, slots, m->qkv, 3 * dm, caches[li], R, H,
                                       m->status, st));
     QZO_TRY(launch_paged_attention(m->qkv, 3 * dm, caches[li], table, n_seqs, width, row_seq, positions, scale, m->att, dm, R, H,
-                                   m->logits, ws_bytes, m->status, st));
+                                   m->logits, ws_bytes, true, m->status, st));
     const Linear* o_l[1] = {&L.lin[3]};
     __nv_bfloat16* xn_o[1] = {m->xn};
     QZO_TRY(decode_linears(m, o_l, xn_o, 1, dm, m->att, R));

@@ -14,6 +14,7 @@
 namespace qzo {
 namespace {
 
+constexpr int kSMs = 148;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // =========================================================================================
@@ -630,14 +631,23 @@ int log2_of(int v) {
   return n;
 }
 
-// Splits of the keys.  Few CTAs (rows x key heads): as many splits as fill the SMs once, but none shorter than 128 keys.
-// More of them: pieces of 512 keys, so that rows of different lengths share the SMs evenly, as long as the grid stays
-// within eight times what the SMs hold.
-int attention_splits(int64_t R, int Hkv, int chunks, int dh, int64_t max_len) {
-  const int64_t slots = 148 * (dh == 64 ? 4 : 3), ctas = R * Hkv * chunks;
-  const int64_t fill = std::min<int64_t>(slots / ctas, max_len / 128), even = R > 1 ? std::min<int64_t>(max_len / 512, 8 * slots / ctas) : 1;
-  if (getenv("QS")) return atoi(getenv("QS"));
-  return (int)std::max<int64_t>(1, std::max(fill, even));
+// How a launch divides its work.  `subs`: matrix tiles that make up 4 KB of keys (1 for 128 dimensions of bf16).
+struct Plan { int splits, wide, min_keys; };
+
+Plan attention_plan(int64_t R, int Hkv, int chunks, int subs, int64_t max_len) {
+  const int64_t ctas = R * Hkv * chunks;                     // without splits
+  // At most one CTA per SM and a short cache: CTAs of eight warps and no split, which saves the join's launch.  Measured
+  // (32 heads of 128, bf16; us): 1 row of 250 keys 5.8 against 7.5, of 512 8.3 against 7.9; 4 rows of 512 9.7 against
+  // 11.5, of 1024 15.6 against 16.7.
+  if (ctas <= kSMs && max_len <= (ctas <= kSMs / 2 ? 448 : 1024) * subs) return {1, 1, 0};
+  // Few CTAs: as many splits as fill the SMs once, but none shorter than 128 keys (1 row of 4096 keys: 17.1 us with 13
+  // splits, 18.1 with 9, 20.9 with 18).  More rows: pieces of 512 keys, so that rows of different lengths share the SMs
+  // evenly, as long as the grid stays within eight times what the SMs hold (16 rows of 100 to 2048 keys: 50.1 us against
+  // 51.5 without; equal lengths do not need it: 8 rows of 2048 52 against 48; a long row among short ones does).
+  const int64_t slots = kSMs * 3;                            // resident CTAs of four warps
+  const int64_t fill = std::min<int64_t>(slots / ctas, max_len / (128 * subs));
+  const int64_t even = R > 1 ? std::min<int64_t>(max_len / (512 * subs), 8 * slots / ctas) : 1;
+  return {(int)std::max<int64_t>(1, std::max(fill, even)), 0, (even > fill ? 512 : 128) * subs};
 }
 int head_chunks(int G) { return G <= 8 ? 1 : (G + 15) / 16; }
 
@@ -669,15 +679,9 @@ int run_join(const PagedParams& p, cudaStream_t st) {
 }
 
 template <int DH, bool F8>
-int run_attention(const PagedParams& p, cudaStream_t st) {
-  const int W = getenv("QW") ? atoi(getenv("QW")) : 4;
-  if (W == 4) {
-  if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 4>(p, st)));
-  else QZO_TRY((run_attention_w<DH, 2, F8, 4>(p, st)));
-  } else if (W == 8) {
-  if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 8>(p, st)));
-  else QZO_TRY((run_attention_w<DH, 2, F8, 8>(p, st)));
-  } else QZO_TRY((run_attention_w<DH, 1, F8, 16>(p, st)));
+int run_attention(const PagedParams& p, bool wide, cudaStream_t st) {
+  if (p.G <= 8) QZO_TRY(wide ? (run_attention_w<DH, 1, F8, 8>(p, st)) : (run_attention_w<DH, 1, F8, 4>(p, st)));
+  else QZO_TRY(wide ? (run_attention_w<DH, 2, F8, 8>(p, st)) : (run_attention_w<DH, 2, F8, 4>(p, st)));
   if (p.splits <= 1) return QZO_OK;
   // many splits of few heads: a head's dimensions go to several CTAs, so that a thread adds up fewer of them
   return p.splits > 16 ? run_join<DH, 8, 32>(p, st) : run_join<DH, DH / 4, 4>(p, st);
@@ -715,30 +719,34 @@ int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat
   return QZO_OK;
 }
 
+// Workspace for either type of cache: 8-bit keys are split less.
 size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
-  const int splits = attention_splits(R, Hkv, head_chunks(H / Hkv), dh, max_len);
+  const int splits = attention_plan(R, Hkv, head_chunks(H / Hkv), 128 / dh, max_len).splits;
   return splits > 1 ? (size_t)R * H * splits * (dh + 2) * sizeof(float) : 0;
 }
 
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
                            const int32_t* row_seq, const int32_t* positions, float scale, __nv_bfloat16* out, int ldo, int R,
-                           int H, void* ws, size_t ws_bytes, int* status, cudaStream_t st) {
+                           int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st) {
   const int G = H / c.n_kv_heads, chunks = head_chunks(G), max_len = width * c.block_size;
   if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
-  const int splits = attention_splits(R, c.n_kv_heads, chunks, c.head_dim, max_len);
   const int subs = 256 / (c.head_dim * (c.dtype == QZO_DTYPE_E4M3 ? 1 : 2));
-  const int min_keys = ((int64_t)R * c.n_kv_heads * chunks * splits > 148 * 4 ? (getenv("QM") ? atoi(getenv("QM")) : 512) : 128) * subs;
-  const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len);
-  if (need > 0 && (!ws || ws_bytes < need || ((uintptr_t)ws & 255))) return QZO_ERR_WORKSPACE;
+  const Plan plan = attention_plan(R, c.n_kv_heads, chunks, subs, max_len);
+  int splits = plan.splits;
+  const size_t per_split = (size_t)R * H * (c.head_dim + 2) * sizeof(float);
+  if (fewer_splits)
+    splits = (int)std::max<size_t>(1, std::min<size_t>(splits, ws_bytes / per_split));
+  else if (const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
+    if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
   PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
-                R, H, c.n_kv_heads, G, chunks, splits, min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
+                R, H, c.n_kv_heads, G, chunks, splits, plan.min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
   if (splits > 1) {
     p.part_o = (float*)ws;
     p.part_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
   }
   const bool f8 = c.dtype == QZO_DTYPE_E4M3;
-  if (c.head_dim == 128) return f8 ? run_attention<128, true>(p, st) : run_attention<128, false>(p, st);
-  return f8 ? run_attention<64, true>(p, st) : run_attention<64, false>(p, st);
+  if (c.head_dim == 128) return f8 ? run_attention<128, true>(p, plan.wide, st) : run_attention<128, false>(p, plan.wide, st);
+  return f8 ? run_attention<64, true>(p, plan.wide, st) : run_attention<64, false>(p, plan.wide, st);
 }
 
 }  // namespace qzo
@@ -792,8 +800,8 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
   if (((uintptr_t)d_q_bf16 & 15) || ((uintptr_t)d_out_bf16 & 15)) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_device());
   return launch_paged_attention((const __nv_bfloat16*)d_q_bf16, ldq, *cache, d_block_table, n_seqs, table_width, d_row_seq, d_positions,
-                                scale, (__nv_bfloat16*)d_out_bf16, ldo, R, n_heads, d_workspace, workspace_bytes, d_status,
-                                (cudaStream_t)stream);
+                                scale, (__nv_bfloat16*)d_out_bf16, ldo, R, n_heads, d_workspace, workspace_bytes, false,
+                                d_status, (cudaStream_t)stream);
 }
 
 }  // extern "C"
