@@ -177,8 +177,8 @@ int qzo_update_scales_flat(void* d_scales_bf16, int64_t count, uint64_t seed, ui
  * qzo_perturbed_gemm at sign 0 for a step of few tokens):
  *   Y[t][n] = sum_k X[t][k] s[k/128][n] q[k][n] (+ bias[n]).
  * The products X q of a group of 128 are summed in fp32 (each is exact), then scaled in fp32.  Y is rounded once.
- * d_x bf16 [M][ldx], 16-byte aligned, ldx a multiple of 8 and >= K; d_wq kernel layout (qzo_repack_int4); d_scales bf16
- * [ceil(K/128)][N]; d_bias float [N] or NULL; d_y bf16 [M][ldy], ldy >= N, must not overlap d_x.  K and N multiples of 8. */
+ * d_x bf16 [M][ldx], 16-byte aligned, ldx a multiple of 8 and >= K; d_wq kernel layout (qzo_repack_int4), 32-byte aligned; d_scales bf16
+ * [ceil(K/128)][N], 4-byte aligned; d_bias float [N] or NULL; d_y bf16 [M][ldy], ldy >= N, must not overlap d_x.  K and N multiples of 8. */
 #define QZO_GEMV_MAX_ROWS 16
 int qzo_gemv_int4(const void* d_x_bf16, int ldx, const void* d_wq, const void* d_scales_bf16, const float* d_bias,
                   void* d_y_bf16, int ldy, int M, int K, int N, void* stream);
