@@ -216,9 +216,18 @@ int run_gemv(GemvParams& p, cudaStream_t st) {
   int cluster = 1;
   while (cluster < kMaxCluster && 2 * cluster * blocks <= kSMs && 2 * cluster * W <= p.G) cluster *= 2;
   p.cluster = cluster;
+  constexpr int kSums = W * 8 * NT * (16 * RT + 1) * (int)sizeof(float), kMostRing = W * S * (RT * 1056 + 256 * 8 * NT);
+  const int smem = std::max(W * S * (RT * 1056 + 256 * p.M), kSums);
+  static std::atomic<unsigned long long> allowed{0};
+  QZO_CUDA_TRY(allow_dynamic_smem(gemv_w4_kernel<NT, RT, S, W>, std::max(kMostRing, kSums), allowed));
+  if (cluster == 1) {
+    QZO_LAUNCH((gemv_w4_kernel<NT, RT, S, W>), dim3(blocks), dim3(W * 32), smem, st, p);
+    return QZO_OK;
+  }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(blocks * cluster);
   cfg.blockDim = dim3(W * 32);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -226,10 +235,6 @@ int run_gemv(GemvParams& p, cudaStream_t st) {
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  const int ring = W * S * (RT * 1056 + 256 * p.M), sums = W * 8 * NT * (16 * RT + 1) * (int)sizeof(float);
-  cfg.dynamicSmemBytes = std::max(ring, sums);
-  if (cfg.dynamicSmemBytes > 48 * 1024)
-    QZO_CUDA_TRY(cudaFuncSetAttribute(gemv_w4_kernel<NT, RT, S, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes));
   QZO_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemv_w4_kernel<NT, RT, S, W>, (const GemvParams)p));
   count_launch();
   return QZO_OK;

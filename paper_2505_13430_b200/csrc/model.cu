@@ -24,13 +24,18 @@ void add_launches(long long n) { g_launches.fetch_add(n, std::memory_order_relax
 long long launch_count() { return g_launches.load(); }
 
 int check_device() {
+  static std::atomic<unsigned long long> known{0};           // devices below 64 that were found to be 10.x
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) { set_last_cuda_error(e); return QZO_ERR_UNSUPPORTED_DEVICE; }
+  const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (known.load(std::memory_order_relaxed) & bit) return QZO_OK;
   int major = 0;
   e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
   if (e != cudaSuccess) { set_last_cuda_error(e); return QZO_ERR_UNSUPPORTED_DEVICE; }
-  return major == 10 ? QZO_OK : QZO_ERR_UNSUPPORTED_DEVICE;
+  if (major != 10) return QZO_ERR_UNSUPPORTED_DEVICE;
+  known.fetch_or(bit, std::memory_order_relaxed);
+  return QZO_OK;
 }
 
 struct LinearShape { const char* name; int K, N; };

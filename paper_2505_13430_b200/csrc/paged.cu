@@ -655,8 +655,10 @@ template <int DH, int NT, bool F8, int W>
 int run_attention_w(const PagedParams& p, cudaStream_t st) {
   const dim3 grid((unsigned)((int64_t)p.R * p.Hkv * p.chunks), p.splits);
   constexpr int smem = W * 8 * NT * (DH + 1) * (int)sizeof(float);
-  if (smem > 40 * 1024)
-    QZO_CUDA_TRY(cudaFuncSetAttribute(paged_attention_kernel<DH, NT, F8, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  if (smem > 40 * 1024) {
+    static std::atomic<unsigned long long> allowed{0};
+    QZO_CUDA_TRY(allow_dynamic_smem(paged_attention_kernel<DH, NT, F8, W>, smem, allowed));
+  }
   QZO_LAUNCH((paged_attention_kernel<DH, NT, F8, W>), grid, dim3(W * 32), smem, st, p);
   return QZO_OK;
 }

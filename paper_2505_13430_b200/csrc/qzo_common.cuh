@@ -56,6 +56,20 @@ inline bool first_use_on_device(std::atomic<unsigned long long>& mask) {
   return (mask.fetch_or(bit) & bit) == 0;
 }
 
+// Allows a kernel `bytes` of dynamic shared memory on the current device, once per device (`done`: one bit per device id
+// below 64, set after the call has succeeded, so that a second thread never launches ahead of it).
+template <typename Kernel>
+inline cudaError_t allow_dynamic_smem(Kernel* kernel, int bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

@@ -162,8 +162,10 @@ extern "C" int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int
   const SlotParams p{d_lens, d_new, B, d_block_table, table_width, log2_block, d_free, free_capacity, d_free_count, max_rows,
                      d_row_seq, d_positions, d_slots, d_lens_out, d_free_count_out, d_status};
   const int smem = 3 * B * (int)sizeof(int);
-  if (smem > 40 * 1024)   // beyond the default limit of 48 KB with the kernel's own arrays
-    QZO_CUDA_TRY(cudaFuncSetAttribute(assign_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  if (smem > 40 * 1024) {   // beyond the default limit of 48 KB with the kernel's own arrays
+    static std::atomic<unsigned long long> allowed{0};
+    QZO_CUDA_TRY(allow_dynamic_smem(assign_slots_kernel, 3 * QZO_MAX_REQUESTS * (int)sizeof(int), allowed));
+  }
   QZO_LAUNCH(assign_slots_kernel, dim3(1), dim3(kSlotThreads), smem, (cudaStream_t)stream, p);
   return QZO_OK;
 }

@@ -298,45 +298,53 @@ GEMV_MAX_ROWS = 16
 MAX_REQUESTS = 4096
 
 
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_raw_stream, _device_now = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _here(*tensors):
     """Stream of the current device; every tensor has to live there, the launches go to that device."""
-    dev = torch.cuda.current_device()
+    dev = _device_now()
     for t in tensors:
         if t is not None:
-            assert t.is_cuda and t.get_device() == dev, "expects a CUDA tensor of the current device"
-    return torch._C._cuda_getCurrentRawStream(dev)
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
+            assert t.get_device() == dev, "expects CUDA tensors of the current device"
+    return _raw_stream(dev)
 
 
 def _heads(t, what):
     """Row stride of a bf16 [T][heads][head_dim] tensor whose heads lie side by side (a view of a projection's rows)."""
-    assert t.dtype == torch.bfloat16 and t.dim() == 3, f"{what}: expects bf16 [T][heads][head_dim]"
-    assert t.stride(2) == 1 and (t.stride(1) == t.shape[2] or t.shape[1] == 1), f"{what}: the heads of a row lie side by side"
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    T, H, dh = t.shape
+    ld, lh, one = t.stride()
+    assert t.dtype is _BF16 and one == 1 and (lh == dh or H == 1), f"{what}: expects bf16 [T][heads][head_dim], a row's heads side by side"
+    return ld if T > 1 else H * dh
 
 
 def _ints(n, *tensors):
     for t in tensors:
-        assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= n, f"expects contiguous int32 of {n} entries"
+        assert t.dtype is _I32 and t.is_contiguous() and t.numel() >= n, f"expects contiguous int32 of {n} entries"
 
 
 def qzo_gemv_int4(x, wq, scales, K, N, bias=None, y=None):
     """y = x W for up to 16 rows: x bf16 [M][K] (any row stride that is a multiple of 8), wq from qzo_repack_int4, scales
     bf16 [ceil(K/128)][N], bias float32 [N] or None -> bf16 [M][N]."""
-    M = x.shape[0]
-    assert x.dtype == torch.bfloat16 and x.dim() == 2 and x.shape[1] == K and x.stride(1) == 1, "x: expects bf16 [M][K]"
-    assert wq.dtype == torch.uint8 and wq.is_contiguous() and wq.numel() >= -(-N // 128) * -(-K // 64) * 4096, "wq: too short"
-    assert scales.dtype == torch.bfloat16 and scales.is_contiguous() and scales.numel() >= -(-K // 128) * N, "scales: bf16 [ceil(K/128)][N]"
-    assert bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() >= N), "bias: float32 [N]"
+    M, k = x.shape
+    ldx, one = x.stride()
+    assert x.dtype is _BF16 and k == K and one == 1, "x: expects bf16 [M][K]"
+    assert wq.dtype is torch.uint8 and wq.is_contiguous() and wq.numel() >= -(-N // 128) * -(-K // 64) * 4096, "wq: too short"
+    assert scales.dtype is _BF16 and scales.is_contiguous() and scales.numel() >= -(-K // 128) * N, "scales: bf16 [ceil(K/128)][N]"
+    b = None
+    if bias is not None:
+        assert bias.dtype is _F32 and bias.is_contiguous() and bias.numel() >= N, "bias: float32 [N]"
+        b = bias.data_ptr()
     if y is None:
-        y = torch.empty((M, N), dtype=torch.bfloat16, device=x.device)
-    assert y.dtype == torch.bfloat16 and y.shape == (M, N) and y.stride(1) == 1, "y: expects bf16 [M][N]"
+        y, ldy = x.new_empty((M, N)), N
+    else:
+        assert y.dtype is _BF16 and y.shape == (M, N) and y.stride(1) == 1, "y: expects bf16 [M][N]"
+        ldy = y.stride(0) if M > 1 else N
     st = _here(x, wq, scales, bias, y)
-    _check(_lib.qzo_gemv_int4(x.data_ptr(), x.stride(0) if M > 1 else K, wq.data_ptr(), scales.data_ptr(), _at(bias), y.data_ptr(),
-                              y.stride(0) if M > 1 else N, M, K, N, st), "qzo_gemv_int4")
+    rc = _lib.qzo_gemv_int4(x.data_ptr(), ldx if M > 1 else K, wq.data_ptr(), scales.data_ptr(), b, y.data_ptr(), ldy, M, K, N, st)
+    if rc:
+        _check(rc, "qzo_gemv_int4")
     return y
 
 
@@ -362,6 +370,10 @@ def qzo_rope_table(max_pos, head_dim, theta=10000.0):
     return table
 
 
+def _maybe(t):
+    return None if t is None else t.data_ptr()
+
+
 def qzo_qk_norm_rope_cache(q, k, v, positions, slots, cache, q_gain=None, k_gain=None, norm_eps=1e-6, table=None, q_out=None,
                            status=None):
     """Head norms (where a gain is given), rotation (where a table is given) and cache write of T new rows; returns q_out
@@ -370,20 +382,23 @@ def qzo_qk_norm_rope_cache(q, k, v, positions, slots, cache, q_gain=None, k_gain
     assert k.shape == v.shape == (T, cache.n_kv_heads, dh) and dh == cache.head_dim, "k, v: [T][n_kv_heads][head_dim] of the cache"
     ldq, ldk, ldv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     if q_out is None:
-        q_out = torch.empty((T, H, dh), dtype=torch.bfloat16, device=q.device)
-    assert q_out.shape == q.shape
-    ldo = _heads(q_out, "q_out")
+        q_out, ldo = q.new_empty((T, H, dh)), H * dh
+    else:
+        assert q_out.shape == (T, H, dh), "q_out: as q"
+        ldo = _heads(q_out, "q_out")
     _ints(T, positions, slots)
     for gain in (q_gain, k_gain):
-        assert gain is None or (gain.dtype == torch.float32 and gain.is_contiguous() and gain.numel() == dh), "gains: float32 [head_dim]"
+        assert gain is None or (gain.dtype is _F32 and gain.is_contiguous() and gain.numel() == dh), "gains: float32 [head_dim]"
     max_pos = 0
     if table is not None:
-        assert table.dtype == torch.float32 and table.is_contiguous() and table.shape[1:] == (dh // 2, 2), "table: [max_pos][head_dim/2][2]"
-        max_pos = table.shape[0]
+        max_pos, half, two = table.shape
+        assert table.dtype is _F32 and table.is_contiguous() and half == dh // 2 and two == 2, "table: [max_pos][head_dim/2][2]"
     st = _here(q, k, v, positions, slots, cache.k, q_gain, k_gain, table, q_out, status)
-    _check(_lib.qzo_qk_norm_rope_cache(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, _at(q_gain), _at(k_gain), norm_eps,
-                                       _at(table), max_pos, positions.data_ptr(), slots.data_ptr(), q_out.data_ptr(), ldo, cache._ref,
-                                       T, H, _at(status), st), "qzo_qk_norm_rope_cache")
+    rc = _lib.qzo_qk_norm_rope_cache(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, _maybe(q_gain), _maybe(k_gain), norm_eps,
+                                     _maybe(table), max_pos, positions.data_ptr(), slots.data_ptr(), q_out.data_ptr(), ldo, cache._ref,
+                                     T, H, _maybe(status), st)
+    if rc:
+        _check(rc, "qzo_qk_norm_rope_cache")
     return q_out
 
 
@@ -401,9 +416,11 @@ def qzo_paged_attention(q, cache, block_table, positions, row_seq=None, scale=No
     R, H, dh = q.shape
     ldq = _heads(q, "q")
     if out is None:
-        out = torch.empty((R, H, dh), dtype=torch.bfloat16, device=q.device)
-    assert out.shape == q.shape and dh == cache.head_dim
-    ldo = _heads(out, "out")
+        out, ldo = q.new_empty((R, H, dh)), H * dh
+    else:
+        assert out.shape == (R, H, dh), "out: as q"
+        ldo = _heads(out, "out")
+    assert dh == cache.head_dim, "q: the cache's head_dim"
     n_seqs, width = block_table.shape
     _ints(n_seqs * width, block_table)
     _ints(R, positions)
@@ -412,11 +429,13 @@ def qzo_paged_attention(q, cache, block_table, positions, row_seq=None, scale=No
     if workspace is None:
         need = qzo_paged_attention_workspace_bytes(R, H, cache.n_kv_heads, dh, width * cache.block_size)
         workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
+    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     st = _here(q, cache.k, block_table, positions, row_seq, out, workspace, status)
-    _check(_lib.qzo_paged_attention(q.data_ptr(), ldq, cache._ref, block_table.data_ptr(), n_seqs, width, _at(row_seq),
-                                    positions.data_ptr(), dh ** -0.5 if scale is None else scale, out.data_ptr(), ldo, R, H,
-                                    _at(workspace), 0 if workspace is None else workspace.numel(), _at(status), st),
-           "qzo_paged_attention")
+    rc = _lib.qzo_paged_attention(q.data_ptr(), ldq, cache._ref, block_table.data_ptr(), n_seqs, width, _maybe(row_seq),
+                                  positions.data_ptr(), dh ** -0.5 if scale is None else scale, out.data_ptr(), ldo, R, H, ws, ws_bytes,
+                                  _maybe(status), st)
+    if rc:
+        _check(rc, "qzo_paged_attention")
     return out
 
 
@@ -426,18 +445,22 @@ def qzo_assign_slots(lens, new, block_table, free, free_count, block_size, max_r
     stack of free blocks, free_count [1].  Lengths and count are updated in place unless lens_out / free_count_out are
     given.  Returns (row_seq, positions, slots), each [max_rows], -1 behind the last row."""
     B, width = block_table.shape
-    lens_out = lens if lens_out is None else lens_out
-    free_count_out = free_count if free_count_out is None else free_count_out
+    if lens_out is None:
+        lens_out = lens
+    if free_count_out is None:
+        free_count_out = free_count
     if row_seq is None and positions is None and slots is None:
-        row_seq, positions, slots = torch.empty((3, max_rows), dtype=torch.int32, device=lens.device)
+        row_seq, positions, slots = lens.new_empty((3, max_rows)).unbind()
     _ints(B, lens, new, lens_out)
     _ints(B * width, block_table)
     _ints(1, free, free_count, free_count_out)
     _ints(max_rows, row_seq, positions, slots)
     st = _here(lens, new, block_table, free, free_count, lens_out, free_count_out, row_seq, positions, slots, status)
-    _check(_lib.qzo_assign_slots(lens.data_ptr(), new.data_ptr(), B, block_table.data_ptr(), width, block_size, free.data_ptr(),
-                                 free.numel(), free_count.data_ptr(), max_rows, row_seq.data_ptr(), positions.data_ptr(),
-                                 slots.data_ptr(), lens_out.data_ptr(), free_count_out.data_ptr(), _at(status), st), "qzo_assign_slots")
+    rc = _lib.qzo_assign_slots(lens.data_ptr(), new.data_ptr(), B, block_table.data_ptr(), width, block_size, free.data_ptr(),
+                               free.numel(), free_count.data_ptr(), max_rows, row_seq.data_ptr(), positions.data_ptr(),
+                               slots.data_ptr(), lens_out.data_ptr(), free_count_out.data_ptr(), _maybe(status), st)
+    if rc:
+        _check(rc, "qzo_assign_slots")
     return row_seq, positions, slots
 
 
