@@ -5,11 +5,17 @@
 #include "qzo_common.cuh"
 #include "launch.cuh"
 
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+namespace cg = cooperative_groups;
+
 namespace qzo {
 namespace {
 
 constexpr int kSlotThreads = 1024;
-constexpr int kSlotPerThread = QZO_MAX_REQUESTS / kSlotThreads;
+constexpr int kSlotCluster = 8;
 
 struct SlotParams {
   const int32_t *lens, *add;
@@ -41,36 +47,40 @@ __device__ __forceinline__ Sums shfl_up_sums(Sums v, int d) {
   return {__shfl_up_sync(0xffffffffu, v.rows, d), __shfl_up_sync(0xffffffffu, v.need, d), __shfl_up_sync(0xffffffffu, v.back, d)};
 }
 
+// A cluster of CTAs (one for short steps): every CTA forms the same prefix sums, the rows and blocks are shared out among all
+// of their threads.  What bounds it is latency: loads that wait for one another and searches in shared memory.
 __global__ void __launch_bounds__(kSlotThreads)
 assign_slots_kernel(const SlotParams p) {
-  extern __shared__ int starts[];                    // first row, first block taken, first block given back: [3][B]
+  extern __shared__ int starts[];          // of each request: first row, first block taken, first block given back, length
   int* const row_start = starts;
   int* const need_start = starts + p.B;
   int* const back_start = starts + 2 * p.B;
-  __shared__ Sums warp_sums[32];
+  int* const lens = starts + 3 * p.B;
+  __shared__ Sums warp_sums[kSlotThreads / 32];
   __shared__ int bad;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, threads = blockDim.x;
+  const int all = threads * (int)cluster.num_blocks(), me = (int)cluster.block_rank() * threads + tid;
   const int mask = (1 << p.log2_block) - 1;
   auto blocks = [&](long long len) { return (len + mask) >> p.log2_block; };
   if (tid == 0) bad = 0;
   __syncthreads();
 
   // each thread takes consecutive requests
-  const int per = (p.B + kSlotThreads - 1) / kSlotThreads;
-  Sums each[kSlotPerThread], mine{0, 0, 0};
+  const int per = (p.B + threads - 1) / threads;
+  Sums mine{0, 0, 0};
   bool wrong = false;
-#pragma unroll
-  for (int i = 0; i < kSlotPerThread; ++i) {
-    const int r = tid * per + i;
-    each[i] = Sums{0, 0, 0};
-    if (i < per && r < p.B) {
-      const long long len = p.lens[r], add = p.add[r];
-      if (len < 0 || blocks(len + (add > 0 ? add : 0)) > p.width) wrong = true;
-      else if (add < 0) each[i].back = blocks(len);
-      else each[i] = Sums{add, blocks(len + add) - blocks(len), 0};
-    }
-    mine = add_sums(mine, each[i]);
+  auto sums_of = [&](int r) {
+    const long long len = p.lens[r], add = p.add[r];
+    if (len < 0 || blocks(len + (add > 0 ? add : 0)) > p.width) { wrong = true; return Sums{0, 0, 0}; }
+    return add < 0 ? Sums{0, 0, blocks(len)} : Sums{add, blocks(len + add) - blocks(len), 0};
+  };
+  const int r0 = tid * per, r1 = min(p.B, r0 + per);
+  for (int r = r0; r < r1; ++r) {
+    mine = add_sums(mine, sums_of(r));
+    lens[r] = p.lens[r];
   }
+  const long long held = *p.free_count;
   Sums scan = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -81,29 +91,25 @@ assign_slots_kernel(const SlotParams p) {
   if (wrong) bad = 1;
   __syncthreads();
   Sums before{0, 0, 0}, total{0, 0, 0};
-  for (int w = 0; w < kSlotThreads / 32; ++w) {
+  for (int w = 0; w * 32 * per < p.B; ++w) {         // warps that have requests
     if (w == warp) before = total;
     total = add_sums(total, warp_sums[w]);
   }
-  const long long held = *p.free_count, top = held + total.back;
+  const long long top = held + total.back;
   const bool served = !bad && held >= 0 && top <= p.capacity && total.need <= top && total.rows <= p.max_rows;
-  if (!served) {
-    for (int t = tid; t < p.max_rows; t += kSlotThreads) { p.row_seq[t] = -1; p.positions[t] = -1; p.slots[t] = -1; }
-    for (int r = tid; r < p.B; r += kSlotThreads) p.lens_out[r] = p.lens[r];
-    if (tid == 0) {
+  if (!served) {                                     // the same in every CTA
+    for (int t = me; t < p.max_rows; t += all) { p.row_seq[t] = -1; p.positions[t] = -1; p.slots[t] = -1; }
+    for (int r = me; r < p.B; r += all) p.lens_out[r] = lens[r];
+    if (me == 0) {
       *p.free_count_out = (int32_t)held;
       if (p.status) atomicOr(p.status, kStatusNotServed);
     }
     return;
   }
   Sums at = add_sums(before, Sums{scan.rows - mine.rows, scan.need - mine.need, scan.back - mine.back});
-#pragma unroll
-  for (int i = 0; i < kSlotPerThread; ++i) {
-    const int r = tid * per + i;
-    if (i < per && r < p.B) {
-      row_start[r] = (int)at.rows; need_start[r] = (int)at.need; back_start[r] = (int)at.back;
-      at = add_sums(at, each[i]);
-    }
+  for (int r = r0; r < r1; ++r) {
+    row_start[r] = (int)at.rows; need_start[r] = (int)at.need; back_start[r] = (int)at.back;
+    at = add_sums(at, sums_of(r));
   }
   __syncthreads();
 
@@ -115,29 +121,30 @@ assign_slots_kernel(const SlotParams p) {
     const int s = (int)top - 1 - i;
     return s < held ? p.free_list[s] : given_back(s - (int)held);
   };
-  for (int t = tid; t < p.max_rows; t += kSlotThreads) {
-    int seq = -1, pos = -1, slot = -1;
-    if (t < total.rows) {
-      seq = upper_bound(row_start, p.B, t) - 1;
-      const int len = p.lens[seq];
-      pos = len + (t - row_start[seq]);
-      const int have = (int)blocks(len), b = pos >> p.log2_block;
+  int seq = 0;                                       // the request of the thread's last row: the next row's is no earlier one
+  for (int t = me; t < p.max_rows; t += all) {
+    int pos = -1, slot = -1;
+    const bool row = t < total.rows;
+    if (row) {
+      if (seq + 1 < p.B && t >= row_start[seq + 1]) seq += upper_bound(row_start + seq, p.B - seq, t) - 1;
+      pos = lens[seq] + (t - row_start[seq]);
+      const int have = (int)blocks(lens[seq]), b = pos >> p.log2_block;
       const int id = b < have ? p.table[(size_t)seq * p.width + b] : taken(need_start[seq] + b - have);
       slot = id < 0 ? -1 : (id << p.log2_block) | (pos & mask);
     }
-    p.row_seq[t] = seq; p.positions[t] = pos; p.slots[t] = slot;
+    p.row_seq[t] = row ? seq : -1; p.positions[t] = pos; p.slots[t] = slot;
   }
-  for (int i = tid; i < (int)total.need; i += kSlotThreads) {
+  for (int i = me; i < (int)total.need; i += all) {
     const int r = upper_bound(need_start, p.B, i) - 1;
-    p.table[(size_t)r * p.width + blocks(p.lens[r]) + (i - need_start[r])] = taken(i);
+    p.table[(size_t)r * p.width + blocks(lens[r]) + (i - need_start[r])] = taken(i);
   }
-  for (int i = tid; i < (int)total.back; i += kSlotThreads) p.free_list[held + i] = given_back(i);
-  __syncthreads();
-  for (int r = tid; r < p.B; r += kSlotThreads) {
+  for (int i = me; i < (int)total.back; i += all) p.free_list[held + i] = given_back(i);
+  cluster.sync();                                    // every CTA has read the lengths and the count
+  for (int r = me; r < p.B; r += all) {
     const int add = p.add[r];
-    p.lens_out[r] = add < 0 ? 0 : p.lens[r] + add;
+    p.lens_out[r] = add < 0 ? 0 : lens[r] + add;
   }
-  if (tid == 0) *p.free_count_out = (int32_t)(top - total.need);
+  if (me == 0) *p.free_count_out = (int32_t)(top - total.need);
 }
 
 }  // namespace
@@ -161,11 +168,28 @@ extern "C" int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int
   while ((1 << log2_block) < block_size) ++log2_block;
   const SlotParams p{d_lens, d_new, B, d_block_table, table_width, log2_block, d_free, free_capacity, d_free_count, max_rows,
                      d_row_seq, d_positions, d_slots, d_lens_out, d_free_count_out, d_status};
-  const int smem = 3 * B * (int)sizeof(int);
+  const int smem = 4 * B * (int)sizeof(int);
   if (smem > 40 * 1024) {   // beyond the default limit of 48 KB with the kernel's own arrays
     static std::atomic<unsigned long long> allowed{0};
-    QZO_CUDA_TRY(allow_dynamic_smem(assign_slots_kernel, 3 * QZO_MAX_REQUESTS * (int)sizeof(int), allowed));
+    QZO_CUDA_TRY(allow_dynamic_smem(assign_slots_kernel, 4 * QZO_MAX_REQUESTS * (int)sizeof(int), allowed));
   }
-  QZO_LAUNCH(assign_slots_kernel, dim3(1), dim3(kSlotThreads), smem, (cudaStream_t)stream, p);
+  const int threads = std::min(kSlotThreads, ceil_div(std::max(B, max_rows), 32) * 32);
+  if (max_rows <= 2 * kSlotThreads) {
+    QZO_LAUNCH(assign_slots_kernel, dim3(1), dim3(threads), smem, (cudaStream_t)stream, p);
+    return QZO_OK;
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(kSlotCluster);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = (cudaStream_t)stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = kSlotCluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  QZO_CUDA_TRY(cudaLaunchKernelEx(&cfg, assign_slots_kernel, p));
+  count_launch();
   return QZO_OK;
 }
