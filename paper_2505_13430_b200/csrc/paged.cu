@@ -33,8 +33,8 @@ struct RopeCacheParams {
   int ldqo;
   void *ck, *cv;
   float inv_k_scale, inv_v_scale;
-  int n_slots, log2_block, H, Hkv;
-  int64_t items;
+  int n_slots, log2_block, H, Hkv, T;
+  int rows, parts, part_groups;     // rows of a CTA, or CTAs of a row; groups of lanes of a row in a CTA
   int* status;
 };
 
@@ -47,85 +47,121 @@ __device__ __forceinline__ uint2 pack4_bf16(const float v[4]) {
   const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
   return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
-__device__ __forceinline__ uint32_t pack4_e4m3(const float v[4]) {
-  const __nv_fp8x2_storage_t a = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
-  const __nv_fp8x2_storage_t b = __nv_cvt_float2_to_fp8x2(make_float2(v[2], v[3]), __NV_SATFINITE, __NV_E4M3);
+__device__ __forceinline__ uint4 pack8_bf16(const float v[8]) {
+  const uint2 a = pack4_bf16(v), b = pack4_bf16(v + 4);
+  return make_uint4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ uint32_t pack4_e4m3(const float v[4], float inv) {
+  const __nv_fp8x2_storage_t a = __nv_cvt_float2_to_fp8x2(make_float2(v[0] * inv, v[1] * inv), __NV_SATFINITE, __NV_E4M3);
+  const __nv_fp8x2_storage_t b = __nv_cvt_float2_to_fp8x2(make_float2(v[2] * inv, v[3] * inv), __NV_SATFINITE, __NV_E4M3);
   return (uint32_t)a | ((uint32_t)b << 16);
 }
+__device__ __forceinline__ uint2 pack8_e4m3(const float v[8], float inv) { return make_uint2(pack4_e4m3(v, inv), pack4_e4m3(v + 4, inv)); }
 
-// DH / 8 lanes per head; a lane holds elements 4 l .. 4 l + 3 of the lower half and their partners of the upper half, so a
-// pair is turned inside a lane and the norm's sum takes log2(DH / 8) shuffles.
+// DH / 16 lanes per pair of neighbouring heads; a lane holds elements 8 l .. 8 l + 7 of a head's lower half and their
+// partners of the upper half (a 16-byte load each), so a pair of elements is turned inside a lane and the norm's sum takes
+// log2(DH / 16) shuffles.  Two heads to a lane: they share the angles, and twice the bytes are in flight.  A CTA holds whole
+// rows where they are short, part of a row's heads where they are long.  Bound by HBM for long batches.
+constexpr int kRopeThreads = 256, kLaneHeads = 2;
+
 template <int DH, bool F8>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kRopeThreads)
 qk_norm_rope_cache_kernel(const RopeCacheParams p) {
-  constexpr int LPH = DH / 8;
-  const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  const int64_t item = idx / LPH;
-  const int l = (int)(idx % LPH);
-  const int heads = p.H + 2 * p.Hkv;
-  const bool live = item < p.items;
-  const int t = live ? (int)(item / heads) : 0, hh = live ? (int)(item % heads) : 0;
-  const int slot = live ? p.slots[t] : -1;
-  const bool is_q = hh < p.H, is_v = hh >= p.H + p.Hkv;
-  const int h = is_q ? hh : is_v ? hh - p.H - p.Hkv : hh - p.H;
-  float lo[4] = {}, hi[4] = {};
-  if (slot >= 0) {
-    const __nv_bfloat16* src = is_q ? p.q + (size_t)t * p.ldq : is_v ? p.v + (size_t)t * p.ldv : p.k + (size_t)t * p.ldk;
-    src += h * DH + 4 * l;
-    unpack4(*reinterpret_cast<const uint2*>(src), lo);
-    unpack4(*reinterpret_cast<const uint2*>(src + DH / 2), hi);
+  constexpr int LPH = DH / 16;
+  const int l = threadIdx.x % LPH, group = threadIdx.x / LPH, heads = p.H + 2 * p.Hkv;
+  int t, first;                                        // this lane's row, and its first head among queries, keys and values
+  if (p.parts == 1) {
+    const int row = group / p.part_groups;
+    t = row < p.rows ? blockIdx.x * p.rows + row : p.T;
+    first = kLaneHeads * (group - row * p.part_groups);
+  } else {
+    t = group < p.part_groups ? blockIdx.x / p.parts : p.T;
+    first = kLaneHeads * (blockIdx.x % p.parts * p.part_groups + group);
   }
-  const float* gain = is_v ? nullptr : is_q ? p.q_gain : p.k_gain;
-  float ss = 0.0f;
+  // the row's elements are on their way before it is known whether it is padding (they are not used then)
+  int slot = -1, given = 0;
+  uint4 lo_raw[kLaneHeads] = {}, hi_raw[kLaneHeads] = {};
+  if (t < p.T) {
+    slot = p.slots[t];
+    given = p.positions[t];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) ss += lo[e] * lo[e] + hi[e] * hi[e];
-#pragma unroll
-  for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-  if (slot < 0) return;
-  if (gain) {
-    const float r = rsqrtf(ss * (1.0f / DH) + p.norm_eps);
-    const float4 ga = *reinterpret_cast<const float4*>(gain + 4 * l), gb = *reinterpret_cast<const float4*>(gain + DH / 2 + 4 * l);
-    lo[0] *= r * ga.x; lo[1] *= r * ga.y; lo[2] *= r * ga.z; lo[3] *= r * ga.w;
-    hi[0] *= r * gb.x; hi[1] *= r * gb.y; hi[2] *= r * gb.z; hi[3] *= r * gb.w;
-  }
-  if (p.table && !is_v) {
-    const int given = p.positions[t];
-    const int pos = min(max(given, 0), p.max_pos - 1);
-    if (pos != given && l == 0 && p.status) atomicOr(p.status, kStatusBadToken);
-    const float4* cs = reinterpret_cast<const float4*>(p.table + 2 * ((size_t)pos * (DH / 2) + 4 * l));
-    const float4 c01 = cs[0], c23 = cs[1];
-    const float c[4] = {c01.x, c01.z, c23.x, c23.z}, s[4] = {c01.y, c01.w, c23.y, c23.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float a = lo[e], b = hi[e];
-      lo[e] = a * c[e] - b * s[e];
-      hi[e] = b * c[e] + a * s[e];
+    for (int i = 0; i < kLaneHeads; ++i) {
+      const int hh = first + i;
+      if (hh >= heads) continue;
+      const __nv_bfloat16* src = hh < p.H ? p.q + (size_t)t * p.ldq + hh * DH
+                               : hh < p.H + p.Hkv ? p.k + (size_t)t * p.ldk + (hh - p.H) * DH
+                                                  : p.v + (size_t)t * p.ldv + (hh - p.H - p.Hkv) * DH;
+      lo_raw[i] = *reinterpret_cast<const uint4*>(src + 8 * l);
+      hi_raw[i] = *reinterpret_cast<const uint4*>(src + DH / 2 + 8 * l);
     }
   }
-  if (is_q) {
-    __nv_bfloat16* dst = p.q_out + (size_t)t * p.ldqo + h * DH + 4 * l;
-    *reinterpret_cast<uint2*>(dst) = pack4_bf16(lo);
-    *reinterpret_cast<uint2*>(dst + DH / 2) = pack4_bf16(hi);
-    return;
-  }
-  if (slot >= p.n_slots) {
-    if (l == 0 && p.status) atomicOr(p.status, kStatusBadToken);
-    return;
-  }
-  const size_t row = (((size_t)(slot >> p.log2_block) * p.Hkv + h) << p.log2_block) + (slot & ((1 << p.log2_block) - 1));
-  const size_t at = row * DH + 4 * l;
-  void* pages = is_v ? p.cv : p.ck;
-  if (F8) {
-    const float inv = is_v ? p.inv_v_scale : p.inv_k_scale;
+  const bool work = slot >= 0;                         // lanes of padding go along for the shuffles only
+  float4 cs[4];                                        // {cos, sin} of two pairs each
+  if (p.table && work && first < p.H + p.Hkv) {
+    const int pos = min(max(given, 0), p.max_pos - 1);
+    if (pos != given && l == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+    const float4* row = reinterpret_cast<const float4*>(p.table + 2 * ((size_t)pos * (DH / 2) + 8 * l));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { lo[e] *= inv; hi[e] *= inv; }
-    uint8_t* dst = (uint8_t*)pages + at;
-    *reinterpret_cast<uint32_t*>(dst) = pack4_e4m3(lo);
-    *reinterpret_cast<uint32_t*>(dst + DH / 2) = pack4_e4m3(hi);
-  } else {
-    __nv_bfloat16* dst = (__nv_bfloat16*)pages + at;
-    *reinterpret_cast<uint2*>(dst) = pack4_bf16(lo);
-    *reinterpret_cast<uint2*>(dst + DH / 2) = pack4_bf16(hi);
+    for (int e = 0; e < 4; ++e) cs[e] = row[e];
+  }
+  const bool writes = work && slot < p.n_slots;
+  if (work && !writes && l == 0 && first == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+  const size_t block_row = (size_t)((unsigned)slot >> p.log2_block) * p.Hkv, in_block = slot & ((1 << p.log2_block) - 1);
+
+#pragma unroll
+  for (int i = 0; i < kLaneHeads; ++i) {
+    const int hh = first + i;
+    const bool is_q = hh < p.H, is_v = hh >= p.H + p.Hkv;
+    float lo[8], hi[8];
+    unpack4(make_uint2(lo_raw[i].x, lo_raw[i].y), lo); unpack4(make_uint2(lo_raw[i].z, lo_raw[i].w), lo + 4);
+    unpack4(make_uint2(hi_raw[i].x, hi_raw[i].y), hi); unpack4(make_uint2(hi_raw[i].z, hi_raw[i].w), hi + 4);
+    if (p.q_gain || p.k_gain) {                        // uniform: the shuffles need every lane
+      const float* gain = is_v ? nullptr : is_q ? p.q_gain : p.k_gain;
+      float ss = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss += lo[e] * lo[e] + hi[e] * hi[e];
+#pragma unroll
+      for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      if (gain) {
+        const float r = rsqrtf(ss * (1.0f / DH) + p.norm_eps);
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const float4 ga = *reinterpret_cast<const float4*>(gain + 8 * l + e), gb = *reinterpret_cast<const float4*>(gain + DH / 2 + 8 * l + e);
+          lo[e] *= r * ga.x; lo[e + 1] *= r * ga.y; lo[e + 2] *= r * ga.z; lo[e + 3] *= r * ga.w;
+          hi[e] *= r * gb.x; hi[e + 1] *= r * gb.y; hi[e + 2] *= r * gb.z; hi[e + 3] *= r * gb.w;
+        }
+      }
+    }
+    if (!work || hh >= heads) continue;
+    if (p.table && !is_v) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x0 = lo[2 * e], y0 = hi[2 * e], x1 = lo[2 * e + 1], y1 = hi[2 * e + 1];
+        lo[2 * e] = x0 * cs[e].x - y0 * cs[e].y;
+        hi[2 * e] = y0 * cs[e].x + x0 * cs[e].y;
+        lo[2 * e + 1] = x1 * cs[e].z - y1 * cs[e].w;
+        hi[2 * e + 1] = y1 * cs[e].z + x1 * cs[e].w;
+      }
+    }
+    if (is_q) {
+      __nv_bfloat16* dst = p.q_out + (size_t)t * p.ldqo + hh * DH + 8 * l;
+      *reinterpret_cast<uint4*>(dst) = pack8_bf16(lo);
+      *reinterpret_cast<uint4*>(dst + DH / 2) = pack8_bf16(hi);
+      continue;
+    }
+    if (!writes) continue;
+    const int h = is_v ? hh - p.H - p.Hkv : hh - p.H;
+    const size_t at = (((block_row + h) << p.log2_block) + in_block) * DH + 8 * l;
+    if (F8) {
+      uint8_t* dst = (uint8_t*)(is_v ? p.cv : p.ck) + at;
+      const float inv = is_v ? p.inv_v_scale : p.inv_k_scale;
+      *reinterpret_cast<uint2*>(dst) = pack8_e4m3(lo, inv);
+      *reinterpret_cast<uint2*>(dst + DH / 2) = pack8_e4m3(hi, inv);
+    } else {
+      __nv_bfloat16* dst = (__nv_bfloat16*)(is_v ? p.cv : p.ck) + at;
+      *reinterpret_cast<uint4*>(dst) = pack8_bf16(lo);
+      *reinterpret_cast<uint4*>(dst + DH / 2) = pack8_bf16(hi);
+    }
   }
 }
 
@@ -706,10 +742,14 @@ int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat
                               const qzo_kv_cache& c, int T, int H, int* status, cudaStream_t st) {
   RopeCacheParams p{q, k, v, ldq, ldk, ldv, q_gain, k_gain, norm_eps, table, max_pos, positions, slots, q_out, ldqo, c.k, c.v,
                     1.0f / c.k_scale, 1.0f / c.v_scale, c.n_blocks * c.block_size, log2_of(c.block_size), H, c.n_kv_heads,
-                    (int64_t)T * (H + 2 * c.n_kv_heads), status};
-  const int64_t ctas = ceil_div64(p.items * (c.head_dim / 8), 256);
+                    T, 1, 1, 1, status};
+  const int lanes = c.head_dim / 16, groups = ceil_div(H + 2 * c.n_kv_heads, kLaneHeads);
+  p.rows = std::max(1, kRopeThreads / (groups * lanes));
+  p.parts = ceil_div(groups * lanes, kRopeThreads);
+  p.part_groups = ceil_div(groups, p.parts);
+  const int64_t ctas = p.parts == 1 ? ceil_div(T, p.rows) : (int64_t)T * p.parts;
   if (ctas > INT32_MAX) return QZO_ERR_BAD_ARG;
-  const dim3 grid((unsigned)ctas), block(256);
+  const dim3 grid((unsigned)ctas), block(ceil_div(p.rows * p.part_groups * lanes, 32) * 32);
   const bool f8 = c.dtype == QZO_DTYPE_E4M3;
   if (c.head_dim == 128) {
     if (f8) QZO_LAUNCH((qk_norm_rope_cache_kernel<128, true>), grid, block, 0, st, p);
@@ -773,8 +813,8 @@ int qzo_qk_norm_rope_cache(const void* d_q_bf16, int ldq, const void* d_k_bf16, 
   if ((d_q_gain || d_k_gain) && !(norm_eps > 0.0f)) return QZO_ERR_BAD_ARG;
   if (d_table && max_pos <= 0) return QZO_ERR_BAD_ARG;
   const int64_t wq = (int64_t)n_heads * cache->head_dim, wk = (int64_t)cache->n_kv_heads * cache->head_dim;
-  if (ldq < wq || ldqo < wq || ldk < wk || ldv < wk || (ldq % 4) || (ldk % 4) || (ldv % 4) || (ldqo % 4)) return QZO_ERR_BAD_ARG;
-  if (((uintptr_t)d_q_bf16 | (uintptr_t)d_k_bf16 | (uintptr_t)d_v_bf16 | (uintptr_t)d_q_out_bf16) & 7) return QZO_ERR_BAD_ARG;
+  if (ldq < wq || ldqo < wq || ldk < wk || ldv < wk || (ldq % 8) || (ldk % 8) || (ldv % 8) || (ldqo % 8)) return QZO_ERR_BAD_ARG;
+  if (((uintptr_t)d_q_bf16 | (uintptr_t)d_k_bf16 | (uintptr_t)d_v_bf16 | (uintptr_t)d_q_out_bf16) & 15) return QZO_ERR_BAD_ARG;
   if (((uintptr_t)d_q_gain | (uintptr_t)d_k_gain | (uintptr_t)d_table) & 15) return QZO_ERR_BAD_ARG;
   if (d_q_out_bf16 == d_q_bf16 && ldq != ldqo) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_device());
