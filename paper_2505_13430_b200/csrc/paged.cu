@@ -62,7 +62,7 @@ __device__ __forceinline__ uint2 pack8_e4m3(const float v[8], float inv) { retur
 // partners of the upper half (a 16-byte load each), so a pair of elements is turned inside a lane and the norm's sum takes
 // log2(DH / 16) shuffles.  Two heads to a lane: they share the angles, and twice the bytes are in flight.  A CTA holds whole
 // rows where they are short, part of a row's heads where they are long.  Bound by HBM for long batches.
-constexpr int kRopeThreads = 256, kLaneHeads = 2;
+constexpr int kRopeThreads = 128, kLaneHeads = 2;
 
 template <int DH, bool F8>
 __global__ void __launch_bounds__(kRopeThreads)
@@ -102,12 +102,28 @@ qk_norm_rope_cache_kernel(const RopeCacheParams p) {
     if (pos != given && l == 0 && p.status) atomicOr(p.status, kStatusBadToken);
     const float4* row = reinterpret_cast<const float4*>(p.table + 2 * ((size_t)pos * (DH / 2) + 8 * l));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) cs[e] = row[e];
+    for (int e = 0; e < 4; ++e) cs[e] = __ldg(row + e);
   }
   const bool writes = work && slot < p.n_slots;
   if (work && !writes && l == 0 && first == 0 && p.status) atomicOr(p.status, kStatusBadToken);
   const size_t block_row = (size_t)((unsigned)slot >> p.log2_block) * p.Hkv, in_block = slot & ((1 << p.log2_block) - 1);
 
+  float root[kLaneHeads];                              // 1 / rms of the heads
+  if (p.q_gain || p.k_gain) {                          // uniform: the shuffles need every lane
+#pragma unroll
+    for (int i = 0; i < kLaneHeads; ++i) {
+      const uint32_t w[8] = {lo_raw[i].x, lo_raw[i].y, lo_raw[i].z, lo_raw[i].w, hi_raw[i].x, hi_raw[i].y, hi_raw[i].z, hi_raw[i].w};
+      float ss = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[e]));
+        ss += f.x * f.x + f.y * f.y;
+      }
+#pragma unroll
+      for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      root[i] = rsqrtf(ss * (1.0f / DH) + p.norm_eps);
+    }
+  }
 #pragma unroll
   for (int i = 0; i < kLaneHeads; ++i) {
     const int hh = first + i;
@@ -115,21 +131,14 @@ qk_norm_rope_cache_kernel(const RopeCacheParams p) {
     float lo[8], hi[8];
     unpack4(make_uint2(lo_raw[i].x, lo_raw[i].y), lo); unpack4(make_uint2(lo_raw[i].z, lo_raw[i].w), lo + 4);
     unpack4(make_uint2(hi_raw[i].x, hi_raw[i].y), hi); unpack4(make_uint2(hi_raw[i].z, hi_raw[i].w), hi + 4);
-    if (p.q_gain || p.k_gain) {                        // uniform: the shuffles need every lane
-      const float* gain = is_v ? nullptr : is_q ? p.q_gain : p.k_gain;
-      float ss = 0.0f;
+    const float* gain = is_v ? nullptr : is_q ? p.q_gain : p.k_gain;
+    if (gain) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss += lo[e] * lo[e] + hi[e] * hi[e];
-#pragma unroll
-      for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      if (gain) {
-        const float r = rsqrtf(ss * (1.0f / DH) + p.norm_eps);
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-          const float4 ga = *reinterpret_cast<const float4*>(gain + 8 * l + e), gb = *reinterpret_cast<const float4*>(gain + DH / 2 + 8 * l + e);
-          lo[e] *= r * ga.x; lo[e + 1] *= r * ga.y; lo[e + 2] *= r * ga.z; lo[e + 3] *= r * ga.w;
-          hi[e] *= r * gb.x; hi[e + 1] *= r * gb.y; hi[e + 2] *= r * gb.z; hi[e + 3] *= r * gb.w;
-        }
+      for (int e = 0; e < 8; e += 4) {
+        const float4 ga = __ldg(reinterpret_cast<const float4*>(gain + 8 * l + e)), gb = __ldg(reinterpret_cast<const float4*>(gain + DH / 2 + 8 * l + e));
+        const float r = root[i];
+        lo[e] *= r * ga.x; lo[e + 1] *= r * ga.y; lo[e + 2] *= r * ga.z; lo[e + 3] *= r * ga.w;
+        hi[e] *= r * gb.x; hi[e + 1] *= r * gb.y; hi[e + 2] *= r * gb.z; hi[e + 3] *= r * gb.w;
       }
     }
     if (!work || hh >= heads) continue;
