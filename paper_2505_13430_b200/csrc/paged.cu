@@ -534,7 +534,10 @@ paged_attention_kernel(const PagedParams p) {
         for (int u = 0; u < DH / 16; ++u) { o[nt][u][0] *= corr0; o[nt][u][2] *= corr0; o[nt][u][1] *= corr1; o[nt][u][3] *= corr1; }
       }
     }
-    uint32_t pb[NT][S][2];
+    // The weights of a tile in the values' type.  fp16 holds them to 2^-12; bf16 only to 2^-9, as much as the output's own
+    // rounding adds, so there they are the sum of two bf16 (the second holds what the first rounds away, to 2^-17 in all).
+    constexpr int kParts = F8 ? 1 : 2;
+    uint32_t pb[kParts][NT][S][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float ref0 = finite_max(m[nt][0]), ref1 = finite_max(m[nt][1]);
@@ -545,9 +548,15 @@ paged_attention_kernel(const PagedParams p) {
         s[1] = fast_exp2(s[1] - ref1); s[3] = fast_exp2(s[3] - ref1);
         l[nt][0] += s[0] + s[2];
         l[nt][1] += s[1] + s[3];
-        // the weights of a tile, rounded to the values' type (relative 2^-9 or 2^-12 each, on terms that are summed in fp32)
-        pb[nt][i][0] = transpose8x8(pack_pair<F8>(s[0], s[1]));
-        pb[nt][i][1] = transpose8x8(pack_pair<F8>(s[2], s[3]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t first = pack_pair<F8>(s[2 * h], s[2 * h + 1]);
+          pb[0][nt][i][h] = transpose8x8(first);
+          if (!F8) {
+            const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&first));
+            pb[kParts - 1][nt][i][h] = transpose8x8(pack_pair<F8>(s[2 * h] - f.x, s[2 * h + 1] - f.y));
+          }
+        }
       }
     }
 #pragma unroll
@@ -558,10 +567,12 @@ paged_attention_kernel(const PagedParams p) {
         val_pairs<DH, F8>(vraw[i][0], vraw[i][1], u, lo);
         val_pairs<DH, F8>(vraw[i][2], vraw[i][3], u, hi);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          mma_step<F8>(o[nt][u], lo[0], lo[1], hi[0], hi[1], pb[nt][i][0], pb[nt][i][1]);
-          mma_step<F8>(o[nt][u + 1], lo[2], lo[3], hi[2], hi[3], pb[nt][i][0], pb[nt][i][1]);
-        }
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) {
+            mma_step<F8>(o[nt][u], lo[0], lo[1], hi[0], hi[1], pb[part][nt][i][0], pb[part][nt][i][1]);
+            mma_step<F8>(o[nt][u + 1], lo[2], lo[3], hi[2], hi[3], pb[part][nt][i][0], pb[part][nt][i][1]);
+          }
       }
     }
     if (more) load_vals();
