@@ -67,7 +67,7 @@ __device__ __forceinline__ uint32_t lds4(uint32_t at) {
 // different 16-byte banks.
 template <int NT, int RT, int S, int W>
 __global__ void __launch_bounds__(W * 32)
-gemv_w4_kernel(const GemvParams p) {
+gemv_w4_kernel(GemvParams p) {
   constexpr int kWeightBytes = RT * 1024, kScaleBytes = RT * 32;
   extern __shared__ __align__(128) uint8_t gemv_smem[];
   const int rank = blockIdx.x % p.cluster, block = blockIdx.x / p.cluster;
@@ -148,6 +148,8 @@ gemv_w4_kernel(const GemvParams p) {
       }
     }
   };
+  serving_begin();
+  serving_next();
   const int step = W * p.cluster, first = rank * W + warp;
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) {
@@ -220,24 +222,7 @@ int run_gemv(GemvParams& p, cudaStream_t st) {
   const int smem = std::max(W * S * (RT * 1056 + 256 * p.M), kSums);
   static std::atomic<unsigned long long> allowed{0};
   QZO_CUDA_TRY(allow_dynamic_smem(gemv_w4_kernel<NT, RT, S, W>, std::max(kMostRing, kSums), allowed));
-  if (cluster == 1) {
-    QZO_LAUNCH((gemv_w4_kernel<NT, RT, S, W>), dim3(blocks), dim3(W * 32), smem, st, p);
-    return QZO_OK;
-  }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(blocks * cluster);
-  cfg.blockDim = dim3(W * 32);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = cluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  QZO_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemv_w4_kernel<NT, RT, S, W>, (const GemvParams)p));
-  count_launch();
-  return QZO_OK;
+  return launch_serving<GemvParams>(gemv_w4_kernel<NT, RT, S, W>, dim3(blocks * cluster), dim3(W * 32), smem, cluster, st, p);
 }
 
 }  // namespace

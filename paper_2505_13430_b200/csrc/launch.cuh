@@ -18,6 +18,37 @@ void add_launches(long long n);   // kernels run by replaying a recorded step
     }                                                                       \
   } while (0)
 
+// Launch of a serving kernel: allowed to start while the kernel before it in the stream ends (a decode step is a chain of
+// launches of a few microseconds).  Such a kernel calls serving_begin() before it touches global memory, in every CTA.
+// cluster > 1: CTAs of a cluster.
+template <typename Params>
+int launch_serving(void (*kernel)(Params), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, const Params& params) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attrs[2]{};
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = (unsigned)cluster;
+  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+  cfg.attrs = attrs;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  QZO_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, params));
+  count_launch();
+  return QZO_OK;
+}
+
+#ifdef __CUDACC__
+// Waits for the end of the kernel before this one and sees its writes.  Every CTA calls it, those without work too: the end
+// of this kernel stands for the end of all before it.
+__device__ __forceinline__ void serving_begin() { cudaGridDependencySynchronize(); }
+// From here on the next kernel's CTAs may take their places (once every CTA has come here or ended).
+__device__ __forceinline__ void serving_next() { cudaTriggerProgrammaticLaunchCompletion(); }
+#endif
+
 // prims.cu
 int launch_philox_words(uint64_t seed, uint64_t block_base, int64_t n_blocks, uint32_t* d_words,
                         float* d_uniforms, cudaStream_t st);

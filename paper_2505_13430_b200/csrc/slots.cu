@@ -50,7 +50,7 @@ __device__ __forceinline__ Sums shfl_up_sums(Sums v, int d) {
 // A cluster of CTAs (one for short steps): every CTA forms the same prefix sums, the rows and blocks are shared out among all
 // of their threads.  What bounds it is latency: loads that wait for one another and searches in shared memory.
 __global__ void __launch_bounds__(kSlotThreads)
-assign_slots_kernel(const SlotParams p) {
+assign_slots_kernel(SlotParams p) {
   extern __shared__ int starts[];          // of each request: first row, first block taken, first block given back, length
   int* const row_start = starts;
   int* const need_start = starts + p.B;
@@ -65,6 +65,8 @@ assign_slots_kernel(const SlotParams p) {
   auto blocks = [&](long long len) { return (len + mask) >> p.log2_block; };
   if (tid == 0) bad = 0;
   __syncthreads();
+  serving_begin();
+  serving_next();
 
   // each thread takes consecutive requests
   const int per = (p.B + threads - 1) / threads;
@@ -174,22 +176,6 @@ extern "C" int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int
     QZO_CUDA_TRY(allow_dynamic_smem(assign_slots_kernel, 4 * QZO_MAX_REQUESTS * (int)sizeof(int), allowed));
   }
   const int threads = std::min(kSlotThreads, ceil_div(std::max(B, max_rows), 32) * 32);
-  if (max_rows <= 2 * kSlotThreads) {
-    QZO_LAUNCH(assign_slots_kernel, dim3(1), dim3(threads), smem, (cudaStream_t)stream, p);
-    return QZO_OK;
-  }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(kSlotCluster);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = (cudaStream_t)stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = kSlotCluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  QZO_CUDA_TRY(cudaLaunchKernelEx(&cfg, assign_slots_kernel, p));
-  count_launch();
-  return QZO_OK;
+  const int cluster = max_rows <= 2 * kSlotThreads ? 1 : kSlotCluster;
+  return launch_serving<SlotParams>(assign_slots_kernel, dim3(cluster), dim3(threads), smem, cluster, (cudaStream_t)stream, p);
 }
