@@ -177,8 +177,8 @@ int qzo_update_scales_flat(void* d_scales_bf16, int64_t count, uint64_t seed, ui
  * qzo_perturbed_gemm at sign 0 for a step of few tokens):
  *   Y[t][n] = sum_k X[t][k] s[k/128][n] q[k][n] (+ bias[n]).
  * The products X q of a group of 128 are summed in fp32 (each is exact), then scaled in fp32.  Y is rounded once.
- * d_x bf16 [M][ldx], 16-byte aligned, ldx a multiple of 8 and >= K; d_wq kernel layout (qzo_repack_int4), 32-byte aligned; d_scales bf16
- * [ceil(K/128)][N], 4-byte aligned; d_bias float [N] or NULL; d_y bf16 [M][ldy], ldy >= N, must not overlap d_x.  K and N multiples of 8. */
+ * d_x bf16 [M][ldx], 16-byte aligned, ldx a multiple of 8 and >= K; d_wq kernel layout (qzo_repack_int4); d_scales bf16
+ * [ceil(K/128)][N], both 16-byte aligned; d_bias float [N] or NULL; d_y bf16 [M][ldy], ldy >= N, must not overlap d_x.  K and N multiples of 8. */
 #define QZO_GEMV_MAX_ROWS 16
 int qzo_gemv_int4(const void* d_x_bf16, int ldx, const void* d_wq, const void* d_scales_bf16, const float* d_bias,
                   void* d_y_bf16, int ldy, int M, int K, int N, void* stream);
@@ -214,17 +214,18 @@ int qzo_qk_norm_rope_cache(const void* d_q_bf16, int ldq, const void* d_k_bf16, 
                            int max_pos, const int32_t* d_positions, const int32_t* d_slots, void* d_q_out_bf16,
                            int ldqo, const qzo_kv_cache* cache, int T, int n_heads, int* d_status, void* stream);
 
-/* Workspace of qzo_paged_attention for R rows over tables of max_len = table_width * block_size tokens (0 if none: the
+/* Workspace of qzo_paged_attention for R rows over tables of max_len = table_width * block_size <= 2^30 tokens (0 if none: the
  * partial results of rows whose cache is split over several CTAs otherwise). */
 int qzo_paged_attention_workspace_bytes(int R, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes);
 
 /* Attention of one new token per row over the paged cache:
  *   out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,  j = 0 .. position[t] (the row's own key among them),
  * with keys and values of head h / (n_heads / n_kv_heads) found through the block table: token j of request r lives in
- * block d_block_table[r][j / block_size].  A row with a negative position gives zeros.
+ * block d_block_table[r][j / block_size].  A row with a negative position gives zeros, and so does one none of whose keys
+ * scores above -inf.  Entries of the table behind a row's position, and the rest of its last block, are not looked at.
  * Several rows may belong to one request (a prompt's rows, each of which sees the keys up to its own).
  * d_q bf16 [R][ldq] and d_out bf16 [R][ldo], head h at h * head_dim, 16-byte aligned, strides multiples of 8, not
- * overlapping; d_block_table int32 [n_seqs][table_width]; d_row_seq int32 [R] = the request of each row, NULL: row t is
+ * overlapping; d_block_table int32 [n_seqs][table_width], at most 2^30 tokens wide; d_row_seq int32 [R] = the request of each row, NULL: row t is
  * request t (R <= n_seqs); scale > 0 (1 / sqrt(head_dim) as a rule); n_heads a multiple of n_kv_heads.
  * d_workspace: qzo_paged_attention_workspace_bytes, 256-aligned; calls that may run at the same time (two streams, two
  * captured graphs) need one each.  Nothing in it outlives the call.

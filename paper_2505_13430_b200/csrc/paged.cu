@@ -831,7 +831,7 @@ int qzo_qk_norm_rope_cache(const void* d_q_bf16, int ldq, const void* d_k_bf16, 
 }
 
 int qzo_paged_attention_workspace_bytes(int R, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes) {
-  if (!bytes || R <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0) return QZO_ERR_BAD_ARG;
+  if (!bytes || R <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || max_len > kMostKeys) return QZO_ERR_BAD_ARG;
   if (head_dim != 64 && head_dim != 128) return QZO_ERR_BAD_ARG;
   *bytes = paged_attention_bytes(R, n_heads, n_kv_heads, head_dim, max_len);
   return QZO_OK;
@@ -843,7 +843,7 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
   if (!d_q_bf16 || !d_block_table || !d_positions || !d_out_bf16) return QZO_ERR_BAD_ARG;
   if (!cache_ok(cache) || R <= 0 || n_seqs <= 0 || table_width <= 0 || n_heads <= 0 || n_heads % cache->n_kv_heads) return QZO_ERR_BAD_ARG;
   if (!d_row_seq && R > n_seqs) return QZO_ERR_BAD_ARG;
-  if ((int64_t)table_width * cache->block_size > INT32_MAX || !(scale > 0.0f) || !isfinite(scale)) return QZO_ERR_BAD_ARG;
+  if ((int64_t)table_width * cache->block_size > kMostKeys || !(scale > 0.0f) || !isfinite(scale)) return QZO_ERR_BAD_ARG;
   const int64_t wq = (int64_t)n_heads * cache->head_dim;
   if (ldq < wq || ldo < wq || (ldq % 8) || (ldo % 8)) return QZO_ERR_BAD_ARG;
   if (((uintptr_t)d_q_bf16 & 15) || ((uintptr_t)d_out_bf16 & 15)) return QZO_ERR_BAD_ARG;

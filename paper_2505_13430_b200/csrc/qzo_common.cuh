@@ -73,6 +73,7 @@ inline cudaError_t allow_dynamic_smem(Kernel* kernel, int bytes, std::atomic<uns
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+constexpr int kMostKeys = 1 << 30;   // tokens that a row of a block table may hold
 // Block sizes of a paged cache: powers of two from 16 (the keys of one matrix tile) to 256.
 inline bool block_size_ok(int b) { return b >= 16 && b <= 256 && (b & (b - 1)) == 0; }
 

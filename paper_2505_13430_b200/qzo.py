@@ -337,7 +337,7 @@ def qzo_gemv_int4(x, wq, scales, K, N, bias=None, y=None):
         assert bias.dtype is _F32 and bias.is_contiguous() and bias.numel() >= N, "bias: float32 [N]"
         b = bias.data_ptr()
     if y is None:
-        y, ldy = x.new_empty((M, N)), N
+        y, ldy = x.new_empty(M, N), N
     else:
         assert y.dtype is _BF16 and y.shape == (M, N) and y.stride(1) == 1, "y: expects bf16 [M][N]"
         ldy = y.stride(0) if M > 1 else N
@@ -382,7 +382,7 @@ def qzo_qk_norm_rope_cache(q, k, v, positions, slots, cache, q_gain=None, k_gain
     assert k.shape == v.shape == (T, cache.n_kv_heads, dh) and dh == cache.head_dim, "k, v: [T][n_kv_heads][head_dim] of the cache"
     ldq, ldk, ldv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     if q_out is None:
-        q_out, ldo = q.new_empty((T, H, dh)), H * dh
+        q_out, ldo = q.new_empty(T, H, dh), H * dh
     else:
         assert q_out.shape == (T, H, dh), "q_out: as q"
         ldo = _heads(q_out, "q_out")
@@ -416,7 +416,7 @@ def qzo_paged_attention(q, cache, block_table, positions, row_seq=None, scale=No
     R, H, dh = q.shape
     ldq = _heads(q, "q")
     if out is None:
-        out, ldo = q.new_empty((R, H, dh)), H * dh
+        out, ldo = q.new_empty(R, H, dh), H * dh
     else:
         assert out.shape == (R, H, dh), "out: as q"
         ldo = _heads(out, "out")
@@ -450,7 +450,7 @@ def qzo_assign_slots(lens, new, block_table, free, free_count, block_size, max_r
     if free_count_out is None:
         free_count_out = free_count
     if row_seq is None and positions is None and slots is None:
-        row_seq, positions, slots = lens.new_empty((3, max_rows)).unbind()
+        row_seq, positions, slots = lens.new_empty(3, max_rows).unbind()
     _ints(B, lens, new, lens_out)
     _ints(B * width, block_table)
     _ints(1, free, free_count, free_count_out)

@@ -99,7 +99,7 @@ def test_gemv_refusals():
     def call(x, ldx, w, s, b, y, ldy, M, K, N):
         return _lib()._lib.qzo_gemv_int4(x, ldx, w, s, b, y, ldy, M, K, N, None)
     good = dict(x=P, ldx=256, w=P, s=P, b=NONE, y=P, ldy=64, M=2, K=256, N=64)
-    _refused(call, good, [dict(x=NONE), dict(w=NONE), dict(s=NONE), dict(y=NONE), dict(x=ODD), dict(w=ODD), dict(b=ODD), dict(M=0), dict(M=17),
+    _refused(call, good, [dict(x=NONE), dict(w=NONE), dict(s=NONE), dict(y=NONE), dict(x=ODD), dict(w=ODD), dict(s=ODD), dict(b=ODD), dict(M=0), dict(M=17),
                           dict(K=0), dict(K=252), dict(N=0), dict(N=60), dict(ldx=248), dict(ldx=260), dict(ldy=56)])
 
 
@@ -130,13 +130,13 @@ def test_paged_attention_refusals():
     good = dict(q=P, ldq=256, cache=_cache(), tab=P, n=3, w=4, seq=NONE, pos=P, scale=0.125, out=ctypes.c_void_p(0x20000), ldo=256, R=3, H=4,
                 ws=NONE, b=0)
     bad = [dict(q=NONE), dict(tab=NONE), dict(pos=NONE), dict(out=NONE), dict(q=ODD), dict(out=ODD), dict(ldq=248), dict(ldq=260), dict(ldo=64),
-           dict(n=0), dict(w=0), dict(w=1 << 28), dict(R=0), dict(R=4), dict(H=3), dict(H=0), dict(scale=0.0), dict(scale=float("nan")),
+           dict(n=0), dict(w=0), dict(w=(1 << 26) + 1), dict(R=0), dict(R=4), dict(H=3), dict(H=0), dict(scale=0.0), dict(scale=float("nan")),
            dict(cache=None)]
     _refused(call, good, bad + [dict(cache=_cache(**c)) for c in BAD_CACHES])
     # workspace: asked for where a long cache is split
     need = qzo.qzo_paged_attention_workspace_bytes(1, 4, 2, 64, 1 << 16)
     assert need > 0 and qzo.qzo_paged_attention_workspace_bytes(3, 4, 2, 64, 64) == 0
-    for args in ((0, 4, 2, 64, 64), (1, 3, 2, 64, 64), (1, 4, 0, 64, 64), (1, 4, 2, 80, 64), (1, 4, 2, 64, 0)):
+    for args in ((0, 4, 2, 64, 64), (1, 3, 2, 64, 64), (1, 4, 0, 64, 64), (1, 4, 2, 80, 64), (1, 4, 2, 64, 0), (1, 4, 2, 64, (1 << 30) + 1)):
         with pytest.raises(qzo.QzoError):
             qzo.qzo_paged_attention_workspace_bytes(*args)
 
