@@ -78,6 +78,26 @@ def test_decode_follows_the_oracle(name, block, dtype, tol):
     gm.close()
 
 
+def test_long_context_in_a_small_workspace():
+    # a prompt of several steps; the workspace holds fewer splits of the cache than the attention would take
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg("tiny", max_seq=4096)
+    raw = inputs.raw_model_tensors(cfg, seed=1000)
+    gm = qzo.build_model_from_raw(raw, 64)
+    om = build_oracle_model(raw)
+    srv = Server(qzo, gm, cfg, B=2, block=16, n_blocks=300)
+    rng = np.random.default_rng(5)
+    for step in range(10):
+        rows = srv.step({1: rng.integers(0, cfg["vocab"], 64).tolist()}, 64)
+    rows += srv.step({0: [3, 4], 1: [5]}, 3)
+    want = _logits(om, srv.text[1])
+    assert len(srv.text[1]) == 641
+    for r, p, got in rows:
+        ref = want[p] if r == 1 else _logits(om, srv.text[0])[p]
+        assert np.abs(got - ref).max() <= TOL * np.abs(ref).max(), (r, p)
+    gm.close()
+
+
 def test_decode_agrees_with_the_training_forward_and_leaves_it_alone():
     # the same tokens through qzo_forward_loss and qzo_decode; a training step after decoding gives what it gives without
     from paper_2505_13430_b200 import qzo

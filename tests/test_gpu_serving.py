@@ -271,6 +271,19 @@ def test_paged_attention_matches_oracle(lib, positions, H, Hkv, dh, block, kind,
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))
 
 
+@pytest.mark.parametrize("dh,split", [(64, False), (128, True)])
+def test_many_rows_of_different_lengths(lib, dh, split):
+    # more rows than the SMs hold: pieces of equal length, rows that need one and rows that need several
+    rng = np.random.default_rng(2)
+    positions = [int(n) for n in rng.integers(-1, 1100, 150)]
+    positions[7] = 1099
+    q, ck, cv, ks, vs, table = _attend_case(positions, 4, 4, dh, 16, "bf16", 0, 21)
+    assert (lib.qzo_paged_attention_workspace_bytes(150, 4, 4, dh, table.shape[1] * 16) > 0) == split
+    out = lib.qzo_paged_attention(q.cuda(), lib.KvCache(ck, cv, ks, vs), torch.from_numpy(table).cuda(),
+                                  torch.tensor(positions, dtype=torch.int32, device="cuda"))
+    _attend_check(out, q, ck, cv, ks, vs, table, np.arange(150), positions, dh ** -0.5)
+
+
 @pytest.mark.parametrize("kind,H,Hkv", [("bf16", 4, 4), ("e4m3", 16, 2)])
 def test_peaked_scores_and_a_given_scale(lib, kind, H, Hkv):
     # large scores: the maximum moves from tile to tile and single keys carry a row
