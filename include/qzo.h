@@ -248,7 +248,7 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
  * d_lens_out may be d_lens and d_free_count_out may be d_free_count; no other arguments overlap.
  * When the step cannot be served (too few free blocks, a table too narrow, more rows than max_rows, a negative length, a
  * stack beyond its capacity), nothing is changed: lengths and count are handed on as they are, every row is padding, and
- * bit 2 of the status word is set.  B from 1 to QZO_MAX_REQUESTS, block_size as in qzo_kv_cache. */
+ * bit 2 of the status word is set.  B from 1 to QZO_MAX_REQUESTS, max_rows up to 2^30, block_size as in qzo_kv_cache. */
 #define QZO_MAX_REQUESTS 4096
 int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int B, int32_t* d_block_table, int table_width,
                      int block_size, int32_t* d_free, int free_capacity, const int32_t* d_free_count, int max_rows,

@@ -146,5 +146,5 @@ def test_assign_slots_refusals():
         return _lib()._lib.qzo_assign_slots(lens, new, B, tab, w, bs, free, cap, cnt, rows, a, b, c, lo, co, None, None)
     good = dict(lens=P, new=P, B=4, tab=P, w=4, bs=16, free=P, cap=16, cnt=P, rows=8, a=P, b=P, c=P, lo=P, co=P)
     bad = [{n: NONE} for n in ("lens", "new", "tab", "free", "cnt", "a", "b", "c", "lo", "co")]
-    bad += [dict(B=0), dict(B=4097), dict(w=0), dict(bs=8), dict(bs=24), dict(cap=0), dict(rows=0), dict(w=1 << 28), dict(cap=1 << 28)]
+    bad += [dict(B=0), dict(B=4097), dict(w=0), dict(bs=8), dict(bs=24), dict(cap=0), dict(rows=0), dict(rows=(1 << 30) + 1), dict(w=1 << 28), dict(cap=1 << 28)]
     _refused(call, good, bad)
