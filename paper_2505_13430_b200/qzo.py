@@ -449,16 +449,22 @@ def qzo_assign_slots(lens, new, block_table, free, free_count, block_size, max_r
         lens_out = lens
     if free_count_out is None:
         free_count_out = free_count
-    if row_seq is None and positions is None and slots is None:
-        row_seq, positions, slots = lens.new_empty(3, max_rows).unbind()
     _ints(B, lens, new, lens_out)
     _ints(B * width, block_table)
     _ints(1, free, free_count, free_count_out)
-    _ints(max_rows, row_seq, positions, slots)
-    st = _here(lens, new, block_table, free, free_count, lens_out, free_count_out, row_seq, positions, slots, status)
+    if row_seq is None and positions is None and slots is None:
+        maps = lens.new_empty(3, max_rows)
+        row_seq, positions, slots = maps.unbind()
+        st = _here(lens, new, block_table, free, free_count, lens_out, free_count_out, status)
+        at = maps.data_ptr()
+        rows_at = at, at + 4 * max_rows, at + 8 * max_rows
+    else:
+        _ints(max_rows, row_seq, positions, slots)
+        st = _here(lens, new, block_table, free, free_count, lens_out, free_count_out, row_seq, positions, slots, status)
+        rows_at = row_seq.data_ptr(), positions.data_ptr(), slots.data_ptr()
     rc = _lib.qzo_assign_slots(lens.data_ptr(), new.data_ptr(), B, block_table.data_ptr(), width, block_size, free.data_ptr(),
-                               free.numel(), free_count.data_ptr(), max_rows, row_seq.data_ptr(), positions.data_ptr(),
-                               slots.data_ptr(), lens_out.data_ptr(), free_count_out.data_ptr(), _maybe(status), st)
+                               free.numel(), free_count.data_ptr(), max_rows, *rows_at, lens_out.data_ptr(), free_count_out.data_ptr(),
+                               _maybe(status), st)
     if rc:
         _check(rc, "qzo_assign_slots")
     return row_seq, positions, slots
