@@ -298,51 +298,61 @@ GEMV_MAX_ROWS = 16
 MAX_REQUESTS = 4096
 
 
-_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
 _raw_stream, _device_now = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
+# A serving call takes a few microseconds on the device, so these wrappers look at every tensor once, in as few steps as
+# possible.  Every tensor has to live on the current device: the launches go to that device's current stream.
 
-def _here(*tensors):
-    """Stream of the current device; every tensor has to live there, the launches go to that device."""
-    dev = _device_now()
+
+def _ints(dev, n, *tensors):
     for t in tensors:
-        if t is not None:
-            assert t.get_device() == dev, "expects CUDA tensors of the current device"
-    return _raw_stream(dev)
+        assert t.dtype is _I32 and t.numel() >= n and t.is_contiguous() and t.get_device() == dev, \
+            f"expects contiguous int32 of {n} entries on the current device"
 
 
-def _heads(t, what):
+def _heads(dev, t, what):
     """Row stride of a bf16 [T][heads][head_dim] tensor whose heads lie side by side (a view of a projection's rows)."""
     T, H, dh = t.shape
     ld, lh, one = t.stride()
-    assert t.dtype is _BF16 and one == 1 and (lh == dh or H == 1), f"{what}: expects bf16 [T][heads][head_dim], a row's heads side by side"
+    assert t.dtype is _BF16 and one == 1 and (lh == dh or H == 1) and t.get_device() == dev, \
+        f"{what}: expects bf16 [T][heads][head_dim] on the current device, a row's heads side by side"
     return ld if T > 1 else H * dh
 
 
-def _ints(n, *tensors):
-    for t in tensors:
-        assert t.dtype is _I32 and t.is_contiguous() and t.numel() >= n, f"expects contiguous int32 of {n} entries"
+def _floats(dev, n, t, what):
+    """Address of a contiguous float32 tensor of at least n entries, None for None."""
+    if t is None:
+        return None
+    assert t.dtype is _F32 and t.numel() >= n and t.is_contiguous() and t.get_device() == dev, f"{what}: expects float32 [{n}] on the current device"
+    return t.data_ptr()
+
+
+def _status(dev, t):
+    if t is None:
+        return None
+    _ints(dev, 1, t)
+    return t.data_ptr()
 
 
 def qzo_gemv_int4(x, wq, scales, K, N, bias=None, y=None):
     """y = x W for up to 16 rows: x bf16 [M][K] (any row stride that is a multiple of 8), wq from qzo_repack_int4, scales
     bf16 [ceil(K/128)][N], bias float32 [N] or None -> bf16 [M][N]."""
+    dev = _device_now()
     M, k = x.shape
     ldx, one = x.stride()
-    assert x.dtype is _BF16 and k == K and one == 1, "x: expects bf16 [M][K]"
-    assert wq.dtype is torch.uint8 and wq.is_contiguous() and wq.numel() >= -(-N // 128) * -(-K // 64) * 4096, "wq: too short"
-    assert scales.dtype is _BF16 and scales.is_contiguous() and scales.numel() >= -(-K // 128) * N, "scales: bf16 [ceil(K/128)][N]"
-    b = None
-    if bias is not None:
-        assert bias.dtype is _F32 and bias.is_contiguous() and bias.numel() >= N, "bias: float32 [N]"
-        b = bias.data_ptr()
+    assert x.dtype is _BF16 and k == K and one == 1 and x.get_device() == dev, "x: expects bf16 [M][K] on the current device"
+    assert wq.dtype is _U8 and wq.numel() >= (N + 127) // 128 * ((K + 63) // 64) * 4096 and wq.is_contiguous() and wq.get_device() == dev, \
+        "wq: expects the uint8 of qzo_repack_int4 on the current device"
+    assert scales.dtype is _BF16 and scales.numel() >= (K + 127) // 128 * N and scales.is_contiguous() and scales.get_device() == dev, \
+        "scales: expects bf16 [ceil(K/128)][N] on the current device"
     if y is None:
         y, ldy = x.new_empty(M, N), N
     else:
-        assert y.dtype is _BF16 and y.shape == (M, N) and y.stride(1) == 1, "y: expects bf16 [M][N]"
+        assert y.dtype is _BF16 and y.shape == (M, N) and y.stride(1) == 1 and y.get_device() == dev, "y: expects bf16 [M][N] on the current device"
         ldy = y.stride(0) if M > 1 else N
-    st = _here(x, wq, scales, bias, y)
-    rc = _lib.qzo_gemv_int4(x.data_ptr(), ldx if M > 1 else K, wq.data_ptr(), scales.data_ptr(), b, y.data_ptr(), ldy, M, K, N, st)
+    rc = _lib.qzo_gemv_int4(x.data_ptr(), ldx if M > 1 else K, wq.data_ptr(), scales.data_ptr(),
+                            None if bias is None else _floats(dev, N, bias, "bias"), y.data_ptr(), ldy, M, K, N, _raw_stream(dev))
     if rc:
         _check(rc, "qzo_gemv_int4")
     return y
@@ -358,6 +368,7 @@ class KvCache:
         kind = {torch.bfloat16: 0, torch.float8_e4m3fn: 4}[k.dtype]
         self.k, self.v, self.k_scale, self.v_scale = k, v, float(k_scale), float(v_scale)
         self.n_blocks, self.n_kv_heads, self.block_size, self.head_dim = k.shape
+        self.device = k.get_device()
         self.desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), kind, self.n_blocks, self.block_size, self.n_kv_heads, self.head_dim,
                                 self.k_scale, self.v_scale)
         self._ref = ctypes.byref(self.desc)
@@ -366,37 +377,35 @@ class KvCache:
 def qzo_rope_table(max_pos, head_dim, theta=10000.0):
     """float32 [max_pos][head_dim/2][2]: cosine and sine of pos * theta**(-2i/head_dim)."""
     table = torch.empty((max_pos, head_dim // 2, 2), dtype=torch.float32, device="cuda")
-    _check(_lib.qzo_rope_table(table.data_ptr(), max_pos, head_dim, theta, _here(table)), "qzo_rope_table")
+    _check(_lib.qzo_rope_table(table.data_ptr(), max_pos, head_dim, theta, _raw_stream(table.get_device())), "qzo_rope_table")
     return table
-
-
-def _maybe(t):
-    return None if t is None else t.data_ptr()
 
 
 def qzo_qk_norm_rope_cache(q, k, v, positions, slots, cache, q_gain=None, k_gain=None, norm_eps=1e-6, table=None, q_out=None,
                            status=None):
     """Head norms (where a gain is given), rotation (where a table is given) and cache write of T new rows; returns q_out
     bf16 [T][heads][head_dim].  q, k, v bf16 [T][heads][head_dim] views; positions, slots int32 [T], negative = padding."""
+    dev = _device_now()
     T, H, dh = q.shape
-    assert k.shape == v.shape == (T, cache.n_kv_heads, dh) and dh == cache.head_dim, "k, v: [T][n_kv_heads][head_dim] of the cache"
-    ldq, ldk, ldv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    assert k.shape == v.shape == (T, cache.n_kv_heads, dh) and dh == cache.head_dim and cache.device == dev, \
+        "k, v: expects [T][n_kv_heads][head_dim] of the cache, which is on the current device"
+    ldq, ldk, ldv = _heads(dev, q, "q"), _heads(dev, k, "k"), _heads(dev, v, "v")
     if q_out is None:
         q_out, ldo = q.new_empty(T, H, dh), H * dh
     else:
         assert q_out.shape == (T, H, dh), "q_out: as q"
-        ldo = _heads(q_out, "q_out")
-    _ints(T, positions, slots)
-    for gain in (q_gain, k_gain):
-        assert gain is None or (gain.dtype is _F32 and gain.is_contiguous() and gain.numel() == dh), "gains: float32 [head_dim]"
+        ldo = _heads(dev, q_out, "q_out")
+    _ints(dev, T, positions, slots)
     max_pos = 0
     if table is not None:
         max_pos, half, two = table.shape
-        assert table.dtype is _F32 and table.is_contiguous() and half == dh // 2 and two == 2, "table: [max_pos][head_dim/2][2]"
-    st = _here(q, k, v, positions, slots, cache.k, q_gain, k_gain, table, q_out, status)
-    rc = _lib.qzo_qk_norm_rope_cache(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, _maybe(q_gain), _maybe(k_gain), norm_eps,
-                                     _maybe(table), max_pos, positions.data_ptr(), slots.data_ptr(), q_out.data_ptr(), ldo, cache._ref,
-                                     T, H, _maybe(status), st)
+        assert half == dh // 2 and two == 2, "table: [max_pos][head_dim/2][2]"
+    rc = _lib.qzo_qk_norm_rope_cache(q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                     None if q_gain is None else _floats(dev, dh, q_gain, "q_gain"),
+                                     None if k_gain is None else _floats(dev, dh, k_gain, "k_gain"), norm_eps,
+                                     None if table is None else _floats(dev, max_pos * dh, table, "table"), max_pos,
+                                     positions.data_ptr(), slots.data_ptr(), q_out.data_ptr(), ldo, cache._ref, T, H,
+                                     None if status is None else _status(dev, status), _raw_stream(dev))
     if rc:
         _check(rc, "qzo_qk_norm_rope_cache")
     return q_out
@@ -413,27 +422,32 @@ def qzo_paged_attention(q, cache, block_table, positions, row_seq=None, scale=No
     """Attention of one new token per row over the paged cache: q bf16 [R][heads][head_dim], block_table int32
     [n_seqs][table_width], positions int32 [R] (negative = empty row, zeros), row_seq int32 [R] or None (row t is request t)
     -> bf16 [R][heads][head_dim]."""
+    dev = _device_now()
     R, H, dh = q.shape
-    ldq = _heads(q, "q")
+    ldq = _heads(dev, q, "q")
+    assert dh == cache.head_dim and cache.device == dev, "q: expects the head_dim of the cache, which is on the current device"
     if out is None:
         out, ldo = q.new_empty(R, H, dh), H * dh
     else:
         assert out.shape == (R, H, dh), "out: as q"
-        ldo = _heads(out, "out")
-    assert dh == cache.head_dim, "q: the cache's head_dim"
+        ldo = _heads(dev, out, "out")
     n_seqs, width = block_table.shape
-    _ints(n_seqs * width, block_table)
-    _ints(R, positions)
+    _ints(dev, 0, block_table)
+    _ints(dev, R, positions)
+    seqs = None
     if row_seq is not None:
-        _ints(R, row_seq)
+        _ints(dev, R, row_seq)
+        seqs = row_seq.data_ptr()
     if workspace is None:
         need = qzo_paged_attention_workspace_bytes(R, H, cache.n_kv_heads, dh, width * cache.block_size)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
-    ws, ws_bytes = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    st = _here(q, cache.k, block_table, positions, row_seq, out, workspace, status)
-    rc = _lib.qzo_paged_attention(q.data_ptr(), ldq, cache._ref, block_table.data_ptr(), n_seqs, width, _maybe(row_seq),
-                                  positions.data_ptr(), dh ** -0.5 if scale is None else scale, out.data_ptr(), ldo, R, H, ws, ws_bytes,
-                                  _maybe(status), st)
+        workspace = q.new_empty(need, dtype=_U8) if need else None
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        assert workspace.is_contiguous() and (workspace.get_device() == dev or workspace.numel() == 0), "workspace: contiguous, on the current device"
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = _lib.qzo_paged_attention(q.data_ptr(), ldq, cache._ref, block_table.data_ptr(), n_seqs, width, seqs, positions.data_ptr(),
+                                  dh ** -0.5 if scale is None else scale, out.data_ptr(), ldo, R, H, ws, ws_bytes,
+                                  None if status is None else _status(dev, status), _raw_stream(dev))
     if rc:
         _check(rc, "qzo_paged_attention")
     return out
@@ -449,22 +463,20 @@ def qzo_assign_slots(lens, new, block_table, free, free_count, block_size, max_r
         lens_out = lens
     if free_count_out is None:
         free_count_out = free_count
-    _ints(B, lens, new, lens_out)
-    _ints(B * width, block_table)
-    _ints(1, free, free_count, free_count_out)
+    dev = _device_now()
+    _ints(dev, B, lens, new, lens_out)
+    _ints(dev, 1, block_table, free, free_count, free_count_out)
     if row_seq is None and positions is None and slots is None:
         maps = lens.new_empty(3, max_rows)
         row_seq, positions, slots = maps.unbind()
-        st = _here(lens, new, block_table, free, free_count, lens_out, free_count_out, status)
         at = maps.data_ptr()
         rows_at = at, at + 4 * max_rows, at + 8 * max_rows
     else:
-        _ints(max_rows, row_seq, positions, slots)
-        st = _here(lens, new, block_table, free, free_count, lens_out, free_count_out, row_seq, positions, slots, status)
+        _ints(dev, max_rows, row_seq, positions, slots)
         rows_at = row_seq.data_ptr(), positions.data_ptr(), slots.data_ptr()
     rc = _lib.qzo_assign_slots(lens.data_ptr(), new.data_ptr(), B, block_table.data_ptr(), width, block_size, free.data_ptr(),
                                free.numel(), free_count.data_ptr(), max_rows, *rows_at, lens_out.data_ptr(), free_count_out.data_ptr(),
-                               _maybe(status), st)
+                               None if status is None else _status(dev, status), _raw_stream(dev))
     if rc:
         _check(rc, "qzo_assign_slots")
     return row_seq, positions, slots
@@ -551,13 +563,14 @@ class Model:
         slots int32 [R], block_table int32 [n_seqs][width] -> float32 logits [R][vocab]."""
         R = tokens.numel()
         assert len(caches) == self.cfg["n_layers"], "expects one cache per layer"
-        _ints(R, tokens, row_seq, positions, slots)
+        dev = _device_now()
+        _ints(dev, R, tokens, row_seq, positions, slots)
         n_seqs, width = block_table.shape
-        _ints(n_seqs * width, block_table)
+        _ints(dev, 1, block_table)
         if logits is None:
             logits = torch.empty((R, self.cfg["vocab"]), dtype=torch.float32, device="cuda")
-        assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.shape == (R, self.cfg["vocab"])
-        _here(tokens, row_seq, positions, slots, block_table, logits, *(c.k for c in caches))
+        assert logits.shape == (R, self.cfg["vocab"]) and all(c.device == dev for c in caches), "logits: float32 [R][vocab]; caches on the current device"
+        _floats(dev, R, logits, "logits")
         descs = (KvCacheDesc * len(caches))(*(c.desc for c in caches))
         _check(_lib.qzo_decode(self.handle, descs, tokens.data_ptr(), row_seq.data_ptr(), positions.data_ptr(), slots.data_ptr(), R,
                                block_table.data_ptr(), n_seqs, width, logits.data_ptr()), "qzo_decode")
