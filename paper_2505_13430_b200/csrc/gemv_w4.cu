@@ -1,5 +1,13 @@
 // Matrix-vector products with int4 weights and group scales, for up to 16 rows of activations:
 //   Y[t][n] = sum_g s[g][n] (sum_{k in group g} X[t][k] q[k][n]) (+ bias[n]).
+// The weights are the bytes that count, and each is used for a few rows only; the contraction runs on warp-level matrix
+// instructions (m16n8k16: one for up to eight rows, two above), because the tensor-memory path of the GEMM costs more per
+// group in hand-offs than the weights take to read (the same linears at 16 rows: 10.8, 18.2, 18.0 and 24.0 us there, 5.9, 12.4,
+// 11.7 and 15.3 us here, for K x N = 4096 x 4096, 4096 x 11008, 11008 x 4096 and 5120 x 13824).
+// What bounds it: turning nibbles into bf16 takes three instructions per pair of weights (shift, mask-and-or, subtract), so
+// at one row the ALU pipe is 60 % busy at 3.5 TB/s (8192 x 18944, 22.7 us); the 7B-sized linears are bound by what a launch
+// costs before its first bytes arrive and after its last ones (1 x 4096 x 11008: 9.6 us, where a plain read of as many bytes
+// takes 6.2 us); at 16 rows the activations are twice the bytes of the weights in shared memory.
 #include "qzo_common.cuh"
 #include "launch.cuh"
 #include "layers.cuh"

@@ -61,7 +61,9 @@ __device__ __forceinline__ uint2 pack8_e4m3(const float v[8], float inv) { retur
 // DH / 16 lanes per pair of neighbouring heads; a lane holds elements 8 l .. 8 l + 7 of a head's lower half and their
 // partners of the upper half (a 16-byte load each), so a pair of elements is turned inside a lane and the norm's sum takes
 // log2(DH / 16) shuffles.  Two heads to a lane: they share the angles, and twice the bytes are in flight.  A CTA holds whole
-// rows where they are short, part of a row's heads where they are long.  Bound by HBM for long batches.
+// rows where they are short, part of a row's heads where they are long.
+// Measured: 4096 rows of 32 + 32 heads of 128, bf16: 36.7 us, 5.5 TB/s (HBM); 4099 rows of 32 + 8 heads with norms and e4m3 pages
+// 23.7 us, 4.0 TB/s (issue slots: 560 warp instructions per two heads); one row 1.9 us (a launch and two dependent loads).
 constexpr int kRopeThreads = 128, kLaneHeads = 2;
 
 template <int DH, bool F8>
@@ -318,7 +320,12 @@ __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0
 // A CTA = one row, one key head, up to 8 NT of the query heads that share it, one split of its keys; its warps take the
 // split's tiles in turn, each with its own running maximum and sum, and are joined at the end.
 // A tile is two products: S^T = K Q^T (keys x heads) and O^T += V^T P^T (dimensions x heads), so up to eight heads
-// share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.
+// share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.  Every fragment
+// is loaded from the pages straight into registers: the k order of the products is free, so a lane's 16 consecutive bytes
+// of a key feed four k positions, and values are paired across two keys by byte permutes.
+// Bound by HBM where CTAs run long (1 row of 131071 keys, 32 heads on 8: bf16 84.2 us, 6.4 TB/s; e4m3 46.7 us, 5.7 TB/s), by
+// what a CTA needs before its first keys and after its last where they run short (64 rows to 4096 in e4m3, CTAs of up to 1024
+// keys: 55.4 us, 4.6 TB/s).
 template <int DH, int NT, bool F8, int W>
 __global__ void __launch_bounds__(W * 32, (NT == 1 ? 12 : 8) / W)
 paged_attention_kernel(PagedParams p) {
