@@ -46,24 +46,6 @@ __device__ __forceinline__ uint32_t weight_pair(uint32_t w, int p) {
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// 16-byte asynchronous copy global -> shared
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void zero16(uint32_t dst) {
-  asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(dst), "r"(0u) : "memory");
-}
-__device__ __forceinline__ uint4 lds16(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
-  return v;
-}
-__device__ __forceinline__ uint32_t lds4(uint32_t at) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at));
-  return v;
-}
-
 // NT: tiles of eight activation rows; RT: tiles of sixteen output features of a warp; S: stages of its ring; W: warps of a CTA,
 // which share its output features and take the groups of K in turn.
 // The weights are the A operand.  A lane's share of a tile is features 2g and 2g + 1 and the 32 k of its quarter t of the
@@ -171,14 +153,14 @@ gemv_w4_kernel(GemvParams p) {
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) {
     if (first + s * step < p.G) fetch(first + s * step, ring + s * stage_bytes);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    copies_commit();
   }
   int use = 0, fill = S - 1;
   for (int grp = first; grp < p.G; grp += step) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
+    copies_wait<S - 2>();
     __syncwarp();                                      // this stage has landed, and every lane is done with the one before it
     if (grp + (S - 1) * step < p.G) fetch(grp + (S - 1) * step, ring + fill * stage_bytes);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    copies_commit();
     contract(ring + use * stage_bytes);
     use = use + 1 == S ? 0 : use + 1;
     fill = fill + 1 == S ? 0 : fill + 1;

@@ -182,6 +182,7 @@ qk_norm_rope_cache_kernel(RopeCacheParams p) {
 // Attention of one new token per row
 // =========================================================================================
 
+constexpr int kStageBytes = 8192;                      // of a warp's ring: 4 KB of keys and 4 KB of values
 constexpr int kSub = 16;                               // keys of one matrix tile; a block of the cache holds whole ones
 
 struct PagedParams {
@@ -241,11 +242,13 @@ struct Layout {
   static constexpr int kValBytes = kRowBytes == 64 ? 8 : 16;             // bytes of a load of one of eight lanes
 };
 
-template <int DH, bool F8>
-__device__ __forceinline__ void load_key(const uint8_t* chunk, uint4 raw[Layout<DH, F8>::kKeyLoads]) {
-#pragma unroll
-  for (int j = 0; j < Layout<DH, F8>::kKeyLoads; ++j) raw[j] = load_stream16(chunk + 64 * j);
-}
+// Where unit c (16 bytes) of a tile's row stands: c ^ swizzle(row), so that the eight lanes of a phase (two g, four t) that read
+// keys (rows g, units t) or values (rows 2t, units g) read eight different 16-byte banks.
+template <int UNITS>
+__device__ __forceinline__ int key_swizzle(int row) { return UNITS >= 8 ? 4 * (row & 1) : 0; }
+template <int UNITS>
+__device__ __forceinline__ int val_swizzle(int row) { return UNITS >= 8 ? 2 * ((row >> 1) & 3) : (row >> 1) & 3; }
+
 template <int DH, bool F8>
 __device__ __forceinline__ void key_words(const uint4 raw[Layout<DH, F8>::kKeyLoads], uint32_t w[Layout<DH, F8>::kKeyWords]) {
 #pragma unroll
@@ -270,15 +273,17 @@ __device__ __forceinline__ int val_dim(int g, int e) {
 template <int DH, bool F8>
 struct ValRaw { uint32_t w[DH * (F8 ? 1 : 2) / 32]; };
 
+// what lane g has of a value row, from the tile at `tile` in shared memory
 template <int DH, bool F8>
-__device__ __forceinline__ void load_val(const uint8_t* chunk, ValRaw<DH, F8>& raw) {
+__device__ __forceinline__ void read_val(uint32_t tile, int row, int g, ValRaw<DH, F8>& raw) {
+  constexpr int kUnits = Layout<DH, F8>::kRowBytes / 16;
   if (Layout<DH, F8>::kValBytes == 8) {
-    const uint2 v = load_stream8(chunk);
+    const uint2 v = lds8(tile + 16 * (row * kUnits + ((g >> 1) ^ val_swizzle<kUnits>(row))) + 8 * (g & 1));
     raw.w[0] = v.x; raw.w[1] = v.y;
   } else {
 #pragma unroll
     for (int j = 0; j < Layout<DH, F8>::kRowBytes / 128; ++j) {
-      const uint4 v = load_stream16(chunk + 128 * j);
+      const uint4 v = lds16(tile + 16 * (row * kUnits + ((g + 8 * j) ^ val_swizzle<kUnits>(row))));
       raw.w[4 * j] = v.x; raw.w[4 * j + 1] = v.y; raw.w[4 * j + 2] = v.z; raw.w[4 * j + 3] = v.w;
     }
   }
@@ -317,22 +322,31 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
 // What scores are taken relative to: their maximum, or 0 where there is none (all -inf).
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 
+// Stages of a ring and CTAs of four warps on an SM, for NT tiles of eight heads: three CTAs with two stages each where their
+// registers allow it, two with three stages otherwise (64 rows to 4096 in e4m3: 55.3 us against 58.3 with two CTAs; 16 rows of
+// 8192 keys, 24 heads on one: 13.9 us against 17.2 with three).
+__host__ __device__ constexpr int resident_ctas(int NT) { return NT == 1 ? 3 : 2; }
+__host__ __device__ constexpr int ring_stages(int NT) { return NT == 1 ? 2 : 3; }
+
 // A CTA = one row, one key head, up to 8 NT of the query heads that share it, one split of its keys; its warps take the
 // split's tiles in turn, each with its own running maximum and sum, and are joined at the end.
 // A tile is two products: S^T = K Q^T (keys x heads) and O^T += V^T P^T (dimensions x heads), so up to eight heads
-// share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.  Every fragment
-// is loaded from the pages straight into registers: the k order of the products is free, so a lane's 16 consecutive bytes
-// of a key feed four k positions, and values are paired across two keys by byte permutes.
-// Bound by HBM where CTAs run long (1 row of 131071 keys, 32 heads on 8: bf16 84.2 us, 6.4 TB/s; e4m3 46.7 us, 5.7 TB/s), by
-// what a CTA needs before its first keys and after its last where they run short (64 rows to 4096 in e4m3, CTAs of up to 1024
-// keys: 55.4 us, 4.6 TB/s).
+// share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.  The k order of the
+// products is free, so a lane's 16 consecutive bytes of a key feed four k positions, and values are paired across two keys
+// by byte permutes.
+// Bound by HBM where CTAs run long (1 row of 131071 keys, 32 heads on 8: bf16 82.1 us, 6.5 TB/s; 16 rows of 100 to 2048 keys, 32
+// key heads: 44.8 us, 6.3 TB/s; e4m3 1 row of 131071 46.0 us, 5.8 TB/s), by what a CTA needs before its first keys and after
+// its last where they run short (1 row of 4096 keys, 32 key heads: 16.5 us, 4.1 TB/s).  The rings (64 KB a CTA) keep
+// 190 KB in flight or in use on an SM; with the next tile in registers instead, 8 rows of 2048 keys took 51.5 us, now 42.1.
 template <int DH, int NT, bool F8, int W>
-__global__ void __launch_bounds__(W * 32, (NT == 1 ? 12 : 8) / W)
+__global__ void __launch_bounds__(W * 32, 4 * resident_ctas(NT) / W)
 paged_attention_kernel(PagedParams p) {
   using Lay = Layout<DH, F8>;
-  extern __shared__ __align__(16) float att_smem[];
+  constexpr int kStages = ring_stages(NT);
+  extern __shared__ __align__(128) float att_smem[];
   float (*sm_o)[8 * NT][DH + 1] = reinterpret_cast<float (*)[8 * NT][DH + 1]>(att_smem);
   __shared__ float sm_m[W][8 * NT], sm_l[W][8 * NT];
+  __shared__ int sm_n[W][kStages][Lay::kSubs];         // keys of the tiles in the rings
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int per_row = p.Hkv * p.chunks;
   const int row = blockIdx.x / per_row, hk = blockIdx.x % per_row / p.chunks, chunk = blockIdx.x % p.chunks;
@@ -406,90 +420,72 @@ paged_attention_kernel(PagedParams p) {
   }
   const int32_t* pages = p.table + (size_t)seq * p.width;
   const int in_block = (1 << p.log2_block) - 1;
-  // A tile's keys and values stay in registers from their loads to their use, and the next tile's are loaded as soon as
-  // the registers are free: its keys behind the scores, its values behind the second product.  The block id is known one
-  // tile ahead of that.
-  constexpr int S = Lay::kSubs, kTileKeys = Lay::kTileKeys;
-  uint4 kraw[S][2][Lay::kKeyLoads];
-  ValRaw<DH, F8> vraw[S][4];
-  const uint8_t* const k_lane = (const uint8_t*)p.ck + g * Lay::kRowBytes + 16 * t;
-  const uint8_t* const v_lane = (const uint8_t*)p.cv + 2 * t * Lay::kRowBytes + Lay::kValBytes * g;
-  size_t at[S];                        // of the tile that is loaded next: byte offsets, block ids, and where it ends
-  int page[S], next = 0;
-  bool whole = false;                  // it has all its keys, in blocks that exist
+  // Tiles come through a ring of each warp's own in shared memory, filled by 16-byte asynchronous copies two tiles ahead; rows
+  // behind the split's end and blocks out of range are filled with zeros.  Block ids are looked up one tile before that.
+  constexpr int S = Lay::kSubs, kTileKeys = Lay::kTileKeys, kStep = W * kTileKeys, kUnits = Lay::kRowBytes / 16;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem) + warp * kStages * kStageBytes;
+  int page[S];
   auto look_up = [&](int key0) {
 #pragma unroll
     for (int i = 0; i < S; ++i) page[i] = key0 + kSub * i < k1 ? pages[(key0 + kSub * i) >> p.log2_block] : 0;
   };
-  auto find = [&](int key0) {
-    next = key0;
-    whole = key0 + kTileKeys <= k1;
+  auto fill = [&](int key0, int slot) {
+    const uint32_t stage = ring + slot * kStageBytes;
 #pragma unroll
     for (int i = 0; i < S; ++i) {
+      int n = k1 - key0 - kSub * i;
       if ((unsigned)page[i] >= (unsigned)p.n_blocks) {               // uniform over the warp
         if (lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
-        whole = false;
+        n = page[i] = 0;
       }
-      at[i] = ((((size_t)page[i] * p.Hkv + hk) << p.log2_block) + ((key0 + kSub * i) & in_block)) * Lay::kRowBytes;
-    }
-  };
-  auto keys_of = [&](int i) { return (unsigned)page[i] >= (unsigned)p.n_blocks ? 0 : k1 - next - kSub * i; };
-  auto load_keys = [&]() {
-    if (whole) {                                                     // uniform: a whole tile needs no look at its rows
+      if (lane == 0) sm_n[warp][slot][i] = n;
+      const size_t at = ((((size_t)page[i] * p.Hkv + hk) << p.log2_block) + ((key0 + kSub * i) & in_block)) * Lay::kRowBytes + 16 * lane;
+      const uint8_t *kp = (const uint8_t*)p.ck + at, *vp = (const uint8_t*)p.cv + at;
+      const uint32_t dst = stage + i * kSub * Lay::kRowBytes;
 #pragma unroll
-      for (int i = 0; i < S; ++i) {
-        load_key<DH, F8>(k_lane + at[i], kraw[i][0]);
-        load_key<DH, F8>(k_lane + at[i] + 8 * Lay::kRowBytes, kraw[i][1]);
-      }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < S; ++i) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-#pragma unroll
-        for (int j = 0; j < Lay::kKeyLoads; ++j) kraw[i][r][j] = make_uint4(0u, 0u, 0u, 0u);
-        if (g + 8 * r < keys_of(i)) load_key<DH, F8>(k_lane + at[i] + 8 * r * Lay::kRowBytes, kraw[i][r]);
-      }
-    }
-  };
-  auto load_vals = [&]() {
-    if (whole) {
-#pragma unroll
-      for (int i = 0; i < S; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) load_val<DH, F8>(v_lane + at[i] + ((r & 1) + 8 * (r >> 1)) * Lay::kRowBytes, vraw[i][r]);
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < S; ++i) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int key = (r & 1) + 8 * (r >> 1);
-        vraw[i][r] = ValRaw<DH, F8>{};
-        if (2 * t + key < keys_of(i)) load_val<DH, F8>(v_lane + at[i] + key * Lay::kRowBytes, vraw[i][r]);
+      for (int j = 0; j < Lay::kRowBytes / 32; ++j) {                // a tile's rows lie side by side: 512 bytes at a time
+        const int unit = 32 * j + lane, row = unit / kUnits, c = unit % kUnits;
+        const int bytes = row < n ? 16 : 0;
+        copy16_or_zero(dst + 16 * (row * kUnits + (c ^ key_swizzle<kUnits>(row))), kp + 512 * j, bytes);
+        copy16_or_zero(dst + kStageBytes / 2 + 16 * (row * kUnits + (c ^ val_swizzle<kUnits>(row))), vp + 512 * j, bytes);
       }
     }
   };
   int key0 = k0 + warp * kTileKeys;
-  if (key0 < k1) {
-    look_up(key0);
-    find(key0);
-    load_keys();
-    load_vals();
-  }
-  for (; key0 < k1; key0 += W * kTileKeys) {
-    const bool more = key0 + W * kTileKeys < k1, full = whole;
-    int n_keys[S];
+  look_up(key0);
 #pragma unroll
-    for (int i = 0; i < S; ++i) n_keys[i] = full ? kSub : keys_of(i);
-    if (more) look_up(key0 + W * kTileKeys);
+  for (int s = 0; s < kStages - 1; ++s) {
+    if (key0 + s * kStep < k1) fill(key0 + s * kStep, s);
+    copies_commit();
+    look_up(key0 + (s + 1) * kStep);
+  }
+  int use = 0, free_stage = kStages - 1;
+  for (; key0 < k1; key0 += kStep) {
+    copies_wait<kStages - 2>();
+    __syncwarp();                                      // the tile has landed, and every lane is done with the one before it
+    if (key0 + (kStages - 1) * kStep < k1) fill(key0 + (kStages - 1) * kStep, free_stage);
+    copies_commit();
+    look_up(key0 + kStages * kStep);
+    const uint32_t stage = ring + use * kStageBytes;
+    int n_keys[S];
+    bool full = true;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      n_keys[i] = sm_n[warp][use][i];
+      full = full && n_keys[i] >= kSub;
+    }
     float sc[NT][S][4];
 #pragma unroll
     for (int i = 0; i < S; ++i) {
+      uint4 raw[2][Lay::kKeyLoads];
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int j = 0; j < Lay::kKeyLoads; ++j)
+          raw[r][j] = lds16(stage + 16 * (i * kSub * kUnits + (g + 8 * r) * kUnits + ((t + 4 * j) ^ key_swizzle<kUnits>(g))));
       uint32_t ka[Lay::kKeyWords], kb[Lay::kKeyWords];
-      key_words<DH, F8>(kraw[i][0], ka);
-      key_words<DH, F8>(kraw[i][1], kb);
+      key_words<DH, F8>(raw[0], ka);
+      key_words<DH, F8>(raw[1], kb);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         sc[nt][i][0] = sc[nt][i][1] = sc[nt][i][2] = sc[nt][i][3] = 0.0f;
@@ -497,10 +493,6 @@ paged_attention_kernel(PagedParams p) {
         for (int w = 0; w < Lay::kKeyWords; w += 2)
           mma_step<F8>(sc[nt][i], ka[w], kb[w], ka[w + 1], kb[w + 1], qf[nt][w], qf[nt][w + 1]);
       }
-    }
-    if (more) {
-      find(key0 + W * kTileKeys);
-      load_keys();
     }
     // The running maximum is only raised when a score passes it by 2^kSlack: until then the weights are at most
     // 2^kSlack, which costs no precision, and a tile needs neither the maximum over its keys nor a rescaling.
@@ -571,11 +563,15 @@ paged_attention_kernel(PagedParams p) {
     }
 #pragma unroll
     for (int i = 0; i < S; ++i) {
+      ValRaw<DH, F8> vraw[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        read_val<DH, F8>(stage + kStageBytes / 2 + i * kSub * Lay::kRowBytes, 2 * t + (r & 1) + 8 * (r >> 1), g, vraw[r]);
 #pragma unroll
       for (int u = 0; u < Lay::kValWords; u += 2) {
         uint32_t lo[4], hi[4];
-        val_pairs<DH, F8>(vraw[i][0], vraw[i][1], u, lo);
-        val_pairs<DH, F8>(vraw[i][2], vraw[i][3], u, hi);
+        val_pairs<DH, F8>(vraw[0], vraw[1], u, lo);
+        val_pairs<DH, F8>(vraw[2], vraw[3], u, hi);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -585,10 +581,12 @@ paged_attention_kernel(PagedParams p) {
           }
       }
     }
-    if (more) load_vals();
+    use = use + 1 == kStages ? 0 : use + 1;
+    free_stage = free_stage + 1 == kStages ? 0 : free_stage + 1;
   }
 
   serving_next();    // not earlier: CTAs that wait take room and issue slots from the loads (1 row of 131071 keys 83.6 us, 86.1 us if at the start)
+  __syncthreads();                     // the rings are free: the warps' results go there
   // join the warps
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -698,31 +696,33 @@ int log2_of(int v) {
   return n;
 }
 
+int head_chunks(int G) { return G <= 8 ? 1 : (G + 15) / 16; }      // CTAs that share a key head's query heads
+
 // How a launch divides its work.  `subs`: matrix tiles that make up 4 KB of keys (1 for 128 dimensions of bf16).
 struct Plan { int splits, wide, min_keys; };
 
-Plan attention_plan(int64_t R, int Hkv, int chunks, int subs, int64_t max_len) {
+Plan attention_plan(int64_t R, int Hkv, int G, int subs, int64_t max_len) {
+  const int chunks = head_chunks(G), head_tiles = G <= 8 ? 1 : 2;
   const int64_t ctas = R * Hkv * chunks;                     // without splits
   // At most one CTA per SM and a short cache: CTAs of eight warps and no split, which saves the join's launch.  Measured
-  // (32 heads of 128, bf16; us): 1 row of 250 keys 5.8 against 7.5, of 512 8.3 against 7.9; 4 rows of 512 9.7 against
-  // 11.5, of 1024 15.6 against 16.7.
-  if (ctas <= kSMs && max_len <= (ctas <= kSMs / 2 ? 448 : 1024) * subs) return {1, 1, 0};
-  // Few CTAs: as many splits as fill the SMs once, but none shorter than 128 keys (1 row of 4096 keys: 17.1 us with 13
-  // splits, 18.1 with 9, 20.9 with 18).  More rows: pieces of 512 keys, so that rows of different lengths share the SMs
-  // evenly, as long as the grid stays within eight times what the SMs hold (16 rows of 100 to 2048 keys: 50.1 us against
-  // 51.5 without; equal lengths do not need it: 8 rows of 2048 52 against 48; a long row among short ones does).
-  const int64_t slots = kSMs * 3;                            // resident CTAs of four warps
+  // (heads of 128, bf16; us): 1 row of 256 keys over 32 key heads 4.9 against 7.0, of 768 8.0 against 8.3, of 1024 9.5 against
+  // 8.9; 4 rows of 512 8.4 against 11.0, of 1536 18.3 against 20.5.
+  if (ctas <= kSMs && max_len <= (ctas <= kSMs / 2 ? 768 : 2048) * subs) return {1, 1, 0};
+  // Few CTAs: as many splits as fill the SMs once, but none shorter than 128 keys (1 row of 4096 keys over 32 key heads: 17.1 us
+  // with 13 splits, 18.1 with 9, 20.9 with 18).  More rows: pieces of 2048 keys, so that a long row among short ones does not
+  // outlast them, as long as the grid stays within eight times what the SMs hold (16 rows of 100 to 2048 keys, 32 key heads: 44.8
+  // us; with pieces of 512 keys 47.5, of 1024 47.3; 8 rows of 2048 42.1, 48.3 and 52.1; 64 rows of 1 to 4096 over 8 key heads
+  // 94.1, 88.6 and 89.3).
+  const int64_t slots = kSMs * resident_ctas(head_tiles);
   const int64_t fill = std::min<int64_t>(slots / ctas, max_len / (128 * subs));
-  const int64_t even = R > 1 ? std::min<int64_t>(max_len / (512 * subs), 8 * slots / ctas) : 1;
-  return {(int)std::max<int64_t>(1, std::max(fill, even)), 0, (even > fill ? 512 : 128) * subs};
+  const int64_t even = R > 1 ? std::min<int64_t>(max_len / (2048 * subs), 8 * slots / ctas) : 1;
+  return {(int)std::max<int64_t>(1, std::max(fill, even)), 0, (even > fill ? 2048 : 128) * subs};
 }
-int head_chunks(int G) { return G <= 8 ? 1 : (G + 15) / 16; }
-
 template <int DH, int NT, bool F8, int W>
 int run_attention_w(const PagedParams& p, cudaStream_t st) {
   const dim3 grid((unsigned)((int64_t)p.R * p.Hkv * p.chunks), p.splits);
-  constexpr int smem = W * 8 * NT * (DH + 1) * (int)sizeof(float);
-  if (smem > 40 * 1024) {
+  constexpr int smem = std::max(W * ring_stages(NT) * kStageBytes, W * 8 * NT * (DH + 1) * (int)sizeof(float));
+  {
     static std::atomic<unsigned long long> allowed{0};
     QZO_CUDA_TRY(allow_dynamic_smem(paged_attention_kernel<DH, NT, F8, W>, smem, allowed));
   }
@@ -777,7 +777,7 @@ int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat
 
 // Workspace for either type of cache: 8-bit keys are split less.
 size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
-  const int splits = attention_plan(R, Hkv, head_chunks(H / Hkv), 128 / dh, max_len).splits;
+  const int splits = attention_plan(R, Hkv, H / Hkv, 128 / dh, max_len).splits;
   return splits > 1 ? (size_t)R * H * splits * (dh + 2) * sizeof(float) : 0;
 }
 
@@ -787,7 +787,7 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
   const int G = H / c.n_kv_heads, chunks = head_chunks(G), max_len = width * c.block_size;
   if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
   const int subs = 256 / (c.head_dim * (c.dtype == QZO_DTYPE_E4M3 ? 1 : 2));
-  const Plan plan = attention_plan(R, c.n_kv_heads, chunks, subs, max_len);
+  const Plan plan = attention_plan(R, c.n_kv_heads, G, subs, max_len);
   int splits = plan.splits;
   const size_t per_split = (size_t)R * H * (c.head_dim + 2) * sizeof(float);
   if (fewer_splits)

@@ -271,17 +271,21 @@ def test_paged_attention_matches_oracle(lib, positions, H, Hkv, dh, block, kind,
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))
 
 
-@pytest.mark.parametrize("dh,split", [(64, False), (128, True)])
-def test_many_rows_of_different_lengths(lib, dh, split):
-    # more rows than the SMs hold: pieces of equal length, rows that need one and rows that need several
+@pytest.mark.parametrize("dh,kind", [(64, "bf16"), (128, "bf16"), (128, "e4m3")])
+def test_many_rows_of_different_lengths(lib, dh, kind):
+    # more rows than the SMs hold, whose keys are taken in pieces of equal length: rows that need none, one and several
+    longest = [9000, 4501, 77]
+    q, ck, cv, ks, vs, table = _attend_case([n - 1 for n in longest], 4, 4, dh, 16, kind, 0, 21)
     rng = np.random.default_rng(2)
-    positions = [int(n) for n in rng.integers(-1, 1100, 150)]
-    positions[7] = 1099
-    q, ck, cv, ks, vs, table = _attend_case(positions, 4, 4, dh, 16, "bf16", 0, 21)
-    assert (lib.qzo_paged_attention_workspace_bytes(150, 4, 4, dh, table.shape[1] * 16) > 0) == split
-    out = lib.qzo_paged_attention(q.cuda(), lib.KvCache(ck, cv, ks, vs), torch.from_numpy(table).cuda(),
-                                  torch.tensor(positions, dtype=torch.int32, device="cuda"))
-    _attend_check(out, q, ck, cv, ks, vs, table, np.arange(150), positions, dh ** -0.5)
+    R = 150
+    row_seq = rng.integers(0, 3, R).astype(np.int32)
+    positions = np.array([rng.integers(-1, longest[s] if r % 5 == 0 else min(longest[s], 300)) for r, s in enumerate(row_seq)], dtype=np.int32)
+    row_seq[:2], positions[:2] = [0, 1], [8999, 4500]
+    q = _randn((R, 4, dh), 22)
+    assert lib.qzo_paged_attention_workspace_bytes(R, 4, 4, dh, table.shape[1] * 16) > 0
+    out = lib.qzo_paged_attention(q.cuda(), lib.KvCache(ck, cv, ks, vs), torch.from_numpy(table).cuda(), torch.from_numpy(positions).cuda(),
+                                  row_seq=torch.from_numpy(row_seq).cuda())
+    _attend_check(out, q, ck, cv, ks, vs, table, row_seq, positions.tolist(), dh ** -0.5)
 
 
 @pytest.mark.parametrize("kind,H,Hkv", [("bf16", 4, 4), ("e4m3", 16, 2)])
