@@ -381,7 +381,7 @@ int qzo_step_host(qzo_model* m, const int32_t* h_tokens, const int32_t* h_labels
  * through the unperturbed model, their keys and values into the paged cache, and d_logits (float [R][vocab], 16-byte
  * aligned) receives the logits of each row.  Every row attends to its request's cached tokens up to itself, so a prompt is
  * a step of its own rows (the keys of all rows of a layer are written before its attention reads them).
- * h_caches: HOST array of n_layers cache descriptions (n_kv_heads = n_heads of the model); d_tokens, d_row_seq,
+ * h_caches: HOST array of n_layers cache descriptions (n_kv_heads = n_heads of the model, one block_size); d_tokens, d_row_seq,
  * d_positions, d_slots int32 [R], as qzo_assign_slots writes the last three; R <= max_tokens; positions < max_seq.
  * Rows of padding (negative position or slot) give logits that mean nothing and touch no cache.  An index out of range
  * (token, position, slot, block) sets bit 1 of the model's status word (qzo_device_status).

@@ -896,6 +896,7 @@ int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_toke
   for (int li = 0; li < d.n_layers; ++li) {
     const qzo_kv_cache& c = h_caches[li];
     if (!cache_ok(&c) || c.n_kv_heads != d.n_heads || c.head_dim != d.d_model / d.n_heads) return QZO_ERR_BAD_ARG;
+    if (c.block_size != h_caches[0].block_size) return QZO_ERR_BAD_ARG;      // one block table serves every layer
     if ((int64_t)table_width * c.block_size > kMostKeys) return QZO_ERR_BAD_ARG;
   }
   return decode(m, h_caches, d_tokens, d_row_seq, d_positions, d_slots, R, d_block_table, n_seqs, table_width, d_logits);

@@ -472,6 +472,7 @@ def qzo_assign_slots(lens, new, block_table, free, free_count, block_size, max_r
         at = maps.data_ptr()
         rows_at = at, at + 4 * max_rows, at + 8 * max_rows
     else:
+        assert row_seq is not None and positions is not None and slots is not None, "row_seq, positions, slots: all of them or none"
         _ints(dev, max_rows, row_seq, positions, slots)
         rows_at = row_seq.data_ptr(), positions.data_ptr(), slots.data_ptr()
     rc = _lib.qzo_assign_slots(lens.data_ptr(), new.data_ptr(), B, block_table.data_ptr(), width, block_size, free.data_ptr(),
@@ -560,10 +561,12 @@ class Model:
 
     def qzo_decode(self, caches, tokens, row_seq, positions, slots, block_table, logits=None):
         """One answering step of R rows over the layers' caches (list of KvCache, one per layer); tokens, row_seq, positions,
-        slots int32 [R], block_table int32 [n_seqs][width] -> float32 logits [R][vocab]."""
+        slots int32 [R], block_table int32 [n_seqs][width] -> float32 logits [R][vocab].  Runs on the stream the model was made on,
+        which has to be the current one."""
         R = tokens.numel()
         assert len(caches) == self.cfg["n_layers"], "expects one cache per layer"
         dev = _device_now()
+        assert _raw_stream(dev) == self.stream.cuda_stream, "expects the model's stream to be the current one"
         _ints(dev, R, tokens, row_seq, positions, slots)
         n_seqs, width = block_table.shape
         _ints(dev, 1, block_table)

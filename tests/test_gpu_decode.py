@@ -141,6 +141,10 @@ def test_decode_refusals_and_reports():
     refused(qzo.ERR_WORKSPACE, n=65)
     wrong = [qzo.KvCache(torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16, device="cuda"))] * 2
     refused(qzo.ERR_BAD_ARG, caches=wrong)
+    other = qzo.KvCache(*(torch.zeros((2, 4, 32, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    refused(qzo.ERR_BAD_ARG, caches=[srv.caches[0], other])
+    with torch.cuda.stream(torch.cuda.Stream()), pytest.raises(AssertionError):
+        gm.qzo_decode(srv.caches, one, one, one, one, table)
     # indices out of range: reported through the status word
     for tokens, pos, slot in ((cfg["vocab"], 0, 0), (0, cfg["max_seq"], 0), (0, 0, 64)):
         gm.qzo_decode(srv.caches, one + tokens, one, one + pos, one + slot, table)
