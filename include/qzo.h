@@ -390,6 +390,15 @@ int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_toke
                const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
                int table_width, float* d_logits);
 
+/* The same step from the requests' side: qzo_assign_slots on (d_lens, d_new, ...), in place and for R rows, then qzo_decode of the
+ * rows it numbers.  d_tokens int32 [R]: the new tokens, request by request, anything behind the last row; d_maps int32 [3][R]
+ * receives row_seq, positions and slots.  The block size is the caches', d_block_table int32 [B][table_width], the other
+ * arguments are those of the two calls.  d_status (may be NULL): bit 2 = the step could not be served; every row is padding
+ * then and nothing else has changed. */
+int qzo_decode_requests(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, int32_t* d_lens, const int32_t* d_new,
+                        int B, int32_t* d_block_table, int table_width, int32_t* d_free, int free_capacity,
+                        int32_t* d_free_count, int R, int32_t* d_maps, float* d_logits, int* d_status);
+
 /* The trainable state (the inputs of Algorithm 1: the quantisation scales Delta that the caller hands over
  * and gets back).  linear_id = layer * L + position, L = 7 (Llama: q,k,v,o,gate,up,down) or 6 (OPT:
  * q,k,v,o,fc1,fc2): copies that linear's bf16 [G][N] scales out of / into the model's flat buffer;

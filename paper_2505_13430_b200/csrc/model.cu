@@ -886,11 +886,8 @@ int qzo_forward_loss(qzo_model* m, const int32_t* d_tokens, const int32_t* d_lab
   return forward_loss(m, d_tokens, d_labels, B, S, seed, sign, eps, d_loss, nullptr, false);
 }
 
-int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
-               const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
-               int table_width, float* d_logits) {
-  if (!m || !h_caches || !d_tokens || !d_row_seq || !d_positions || !d_slots || !d_block_table || !d_logits) return QZO_ERR_BAD_ARG;
-  if (R <= 0 || n_seqs <= 0 || table_width <= 0 || ((uintptr_t)d_logits & 15)) return QZO_ERR_BAD_ARG;
+static int check_decode(const qzo_model* m, const qzo_kv_cache* h_caches, int R, int n_seqs, int table_width, const float* d_logits) {
+  if (!m || !h_caches || !d_logits || ((uintptr_t)d_logits & 15) || R <= 0 || n_seqs <= 0 || table_width <= 0) return QZO_ERR_BAD_ARG;
   if (R > m->max_tokens) return QZO_ERR_WORKSPACE;
   const qzo_model_desc& d = m->desc;
   for (int li = 0; li < d.n_layers; ++li) {
@@ -899,7 +896,26 @@ int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_toke
     if (c.block_size != h_caches[0].block_size) return QZO_ERR_BAD_ARG;      // one block table serves every layer
     if ((int64_t)table_width * c.block_size > kMostKeys) return QZO_ERR_BAD_ARG;
   }
+  return QZO_OK;
+}
+
+int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
+               const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
+               int table_width, float* d_logits) {
+  if (!d_tokens || !d_row_seq || !d_positions || !d_slots || !d_block_table) return QZO_ERR_BAD_ARG;
+  QZO_TRY(check_decode(m, h_caches, R, n_seqs, table_width, d_logits));
   return decode(m, h_caches, d_tokens, d_row_seq, d_positions, d_slots, R, d_block_table, n_seqs, table_width, d_logits);
+}
+
+int qzo_decode_requests(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, int32_t* d_lens, const int32_t* d_new,
+                        int B, int32_t* d_block_table, int table_width, int32_t* d_free, int free_capacity,
+                        int32_t* d_free_count, int R, int32_t* d_maps, float* d_logits, int* d_status) {
+  if (!d_tokens || !d_maps) return QZO_ERR_BAD_ARG;
+  QZO_TRY(check_decode(m, h_caches, R, B, table_width, d_logits));
+  int32_t *row_seq = d_maps, *positions = d_maps + R, *slots = d_maps + 2 * (size_t)R;
+  QZO_TRY(qzo_assign_slots(d_lens, d_new, B, d_block_table, table_width, h_caches[0].block_size, d_free, free_capacity, d_free_count,
+                           R, row_seq, positions, slots, d_lens, d_free_count, d_status, m->stream));
+  return decode(m, h_caches, d_tokens, row_seq, positions, slots, R, d_block_table, B, table_width, d_logits);
 }
 
 int qzo_update_scales(qzo_model* m, uint64_t seed, float lr, float g, float clip) {

@@ -30,7 +30,7 @@ EXPORTS = (
     "qzo_step_begin", "qzo_step_finish", "qzo_get_scales", "qzo_set_scales", "qzo_debug_set_status", "qzo_use_recorded_steps", "qzo_recorded_step_count", "qzo_perturbed_gemm_codebook16_channelwise",
     "qzo_joint_workspace_bytes", "qzo_enable_joint_spsa", "qzo_perturbed_gemm_table16", "qzo_debug_gemm_wait_expiry",
     "qzo_gemv_int4", "qzo_rope_table", "qzo_qk_norm_rope_cache", "qzo_paged_attention_workspace_bytes", "qzo_paged_attention",
-    "qzo_assign_slots", "qzo_decode",
+    "qzo_assign_slots", "qzo_decode", "qzo_decode_requests",
 )
 
 
@@ -114,6 +114,7 @@ def _load():
         "qzo_paged_attention_workspace_bytes": (ci, [ci, ci, ci, ci, ci, P(sz)]),
         "qzo_paged_attention": (ci, [vp, ci, P(KvCacheDesc), vp, ci, ci, vp, vp, cf, vp, ci, ci, ci, vp, sz, vp, vp]),
         "qzo_assign_slots": (ci, [vp, vp, ci, vp, ci, ci, vp, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp]),
+        "qzo_decode_requests": (ci, [vp, P(KvCacheDesc), vp, vp, vp, ci, vp, ci, vp, ci, vp, ci, vp, vp, vp]),
         "qzo_decode": (ci, [vp, P(KvCacheDesc), vp, vp, vp, vp, ci, vp, ci, ci, vp]),
         "qzo_profile_gemms": (ci, [vp, ci]),
         "qzo_profile_read": (ci, [vp, P(i64), P(ctypes.c_double), P(ctypes.c_double)]),
@@ -559,25 +560,43 @@ class Model:
                "qzo_forward_loss")
         return out
 
+    def _decode_args(self, caches, R, logits):
+        """Checks what the two decode calls share -> (device, cache descriptions, logits)."""
+        dev = _device_now()
+        assert _raw_stream(dev) == self.stream.cuda_stream, "expects the model's stream to be the current one"
+        assert len(caches) == self.cfg["n_layers"] and all(c.device == dev for c in caches), "expects one cache per layer, on the current device"
+        if logits is None:
+            logits = torch.empty((R, self.cfg["vocab"]), dtype=torch.float32, device="cuda")
+        assert logits.shape == (R, self.cfg["vocab"]), "logits: float32 [R][vocab]"
+        _floats(dev, R, logits, "logits")
+        return dev, (KvCacheDesc * len(caches))(*(c.desc for c in caches)), logits
+
     def qzo_decode(self, caches, tokens, row_seq, positions, slots, block_table, logits=None):
         """One answering step of R rows over the layers' caches (list of KvCache, one per layer); tokens, row_seq, positions,
         slots int32 [R], block_table int32 [n_seqs][width] -> float32 logits [R][vocab].  Runs on the stream the model was made on,
         which has to be the current one."""
         R = tokens.numel()
-        assert len(caches) == self.cfg["n_layers"], "expects one cache per layer"
-        dev = _device_now()
-        assert _raw_stream(dev) == self.stream.cuda_stream, "expects the model's stream to be the current one"
+        dev, descs, logits = self._decode_args(caches, R, logits)
         _ints(dev, R, tokens, row_seq, positions, slots)
         n_seqs, width = block_table.shape
         _ints(dev, 1, block_table)
-        if logits is None:
-            logits = torch.empty((R, self.cfg["vocab"]), dtype=torch.float32, device="cuda")
-        assert logits.shape == (R, self.cfg["vocab"]) and all(c.device == dev for c in caches), "logits: float32 [R][vocab]; caches on the current device"
-        _floats(dev, R, logits, "logits")
-        descs = (KvCacheDesc * len(caches))(*(c.desc for c in caches))
         _check(_lib.qzo_decode(self.handle, descs, tokens.data_ptr(), row_seq.data_ptr(), positions.data_ptr(), slots.data_ptr(), R,
                                block_table.data_ptr(), n_seqs, width, logits.data_ptr()), "qzo_decode")
         return logits
+
+    def qzo_decode_requests(self, caches, tokens, lens, new, block_table, free, free_count, logits=None, status=None):
+        """qzo_assign_slots (in place) and qzo_decode of its rows in one call: tokens int32 [R], the new tokens request by
+        request -> (float32 logits [R][vocab], int32 [3][R]: row_seq, positions, slots)."""
+        R = tokens.numel()
+        dev, descs, logits = self._decode_args(caches, R, logits)
+        B, width = block_table.shape
+        _ints(dev, B, lens, new)
+        _ints(dev, 1, tokens, block_table, free, free_count)
+        maps = lens.new_empty(3, R)
+        _check(_lib.qzo_decode_requests(self.handle, descs, tokens.data_ptr(), lens.data_ptr(), new.data_ptr(), B, block_table.data_ptr(),
+                                        width, free.data_ptr(), free.numel(), free_count.data_ptr(), R, maps.data_ptr(),
+                                        logits.data_ptr(), _status(dev, status)), "qzo_decode_requests")
+        return logits, maps
 
     def qzo_update_scales(self, seed, lr, g, clip):
         _check(_lib.qzo_update_scales(self.handle, seed, lr, g, clip), "qzo_update_scales")

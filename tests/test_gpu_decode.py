@@ -98,6 +98,35 @@ def test_long_context_in_a_small_workspace():
     gm.close()
 
 
+def test_decode_of_requests_is_the_two_calls_in_one():
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg("tiny")
+    gm = qzo.build_model_from_raw(inputs.raw_model_tensors(cfg, seed=1000), 64)
+    one, two = (Server(qzo, gm, cfg, 2, 16, 6) for _ in range(2))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for new, toks, rows in (([5, 9], list(range(14)), 14), ([1, 1], [7, 8], 4), ([-1, 20], list(range(20)), 20), ([3, 1], [1, 2, 3, 4], 4)):
+        add = torch.tensor(new, dtype=torch.int32, device="cuda")
+        tokens = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        tokens[:len(toks)] = torch.tensor(toks, dtype=torch.int32, device="cuda")
+        maps = qzo.qzo_assign_slots(one.lens, add, one.table, one.free, one.count, 16, rows)
+        want = gm.qzo_decode(one.caches, tokens, *maps, one.table)
+        got, got_maps = gm.qzo_decode_requests(two.caches, tokens, two.lens, add, two.table, two.free, two.count, status=status)
+        assert torch.equal(got_maps, torch.stack(maps)) and torch.equal(got[:len(toks)], want[:len(toks)])
+        for a, b in ((one.lens, two.lens), (one.count, two.count), (one.table, two.table)):
+            assert torch.equal(a, b)
+        for a, b in zip(one.caches, two.caches):
+            assert torch.equal(a.k.view(torch.int16), b.k.view(torch.int16)) and torch.equal(a.v.view(torch.int16), b.v.view(torch.int16))
+    assert int(status.item()) == 0
+    # more than the free blocks hold: reported, nothing changes, and the model's own status stays clear
+    lens, kept = two.lens.clone(), two.caches[0].k.clone()
+    add = torch.tensor([60, 4], dtype=torch.int32, device="cuda")
+    _, maps = gm.qzo_decode_requests(two.caches, torch.zeros(64, dtype=torch.int32, device="cuda"), two.lens, add, two.table, two.free,
+                                     two.count, status=status)
+    assert int(status.item()) == 4 and torch.equal(two.lens, lens) and (maps == -1).all() and gm.qzo_device_status() == 0
+    assert torch.equal(two.caches[0].k.view(torch.int16), kept.view(torch.int16))
+    gm.close()
+
+
 def test_decode_agrees_with_the_training_forward_and_leaves_it_alone():
     # the same tokens through qzo_forward_loss and qzo_decode; a training step after decoding gives what it gives without
     from paper_2505_13430_b200 import qzo
