@@ -151,6 +151,25 @@ def test_decode_agrees_with_the_training_forward_and_leaves_it_alone():
     assert outs[0][:2] == outs[1][:2] and torch.equal(outs[0][2], outs[1][2])
 
 
+@pytest.mark.parametrize("name,layers", [("llama7b", 2), ("opt6.7b", 1), ("llama13b", 1)])
+def test_full_width_decode_agrees_with_the_training_forward(name, layers):
+    # prompts by the GEMM path, then their last tokens again, one by one, by the matrix-vector path
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg(name, n_layers=layers)
+    gm = qzo.build_random_model_gpu(cfg, 128)
+    tok, lab = inputs.tokens_and_labels(cfg, 3, 40, seed=4)
+    gm.qzo_forward_loss(tok.cuda(), lab.cuda(), 0, 0, 1e-3)
+    want = gm.qzo_debug_layer_output(0, 1, 120).view(3, 40, -1).cpu().numpy()
+    srv = Server(qzo, gm, cfg, 3, 16, 12)
+    rows = srv.step({r: tok[r, :38].tolist() for r in range(3)}, 114)
+    for t in (38, 39):
+        rows += srv.step({r: tok[r, t:t + 1].tolist() for r in range(3)}, 3)
+    assert len(rows) == 120
+    for r, p, got in rows:
+        assert np.abs(got - want[r, p]).max() <= TOL * np.abs(want[r, p]).max(), (r, p)
+    gm.close()
+
+
 def test_decode_refusals_and_reports():
     from paper_2505_13430_b200 import qzo
     cfg = inputs.model_cfg("tiny")
