@@ -2,12 +2,13 @@
 //   Y[t][n] = sum_g s[g][n] (sum_{k in group g} X[t][k] q[k][n]) (+ bias[n]).
 // The weights are the bytes that count, and each is used for a few rows only; the contraction runs on warp-level matrix
 // instructions (m16n8k16: one for up to eight rows, two above), because the tensor-memory path of the GEMM costs more per
-// group in hand-offs than the weights take to read (the same linears at 16 rows: 10.8, 18.2, 18.0 and 24.0 us there, 5.9, 12.4,
-// 11.7 and 15.3 us here, for K x N = 4096 x 4096, 4096 x 11008, 11008 x 4096 and 5120 x 13824).
-// What bounds it: turning nibbles into bf16 takes three instructions per pair of weights (shift, mask-and-or, subtract), so
-// at one row the ALU pipe is 60 % busy at 3.5 TB/s (8192 x 18944, 22.7 us); the 7B-sized linears are bound by what a launch
-// costs before its first bytes arrive and after its last ones (1 x 4096 x 11008: 9.6 us, where a plain read of as many bytes
-// takes 6.2 us); at 16 rows the activations are twice the bytes of the weights in shared memory.
+// group in hand-offs than the weights take to read (the same linears at 16 rows: 10.8, 18.2, 18.0 and 24.0 us there, 6.0, 12.4,
+// 12.0 and 15.4 us here, for K x N = 4096 x 4096, 4096 x 11008, 11008 x 4096 and 5120 x 13824).
+// What bounds it: turning nibbles into bf16 takes three instructions per pair of weights (shift, mask-and-or, subtract), and
+// a warp's work around the 2 KB of a turn as many again, so at one row the ALU pipe is half busy and a warp in six can
+// issue at 3.9 TB/s (8192 x 18944, 20.4 us); the 7B-sized linears are bound by what a launch costs before its first bytes
+// arrive and after its last ones (1 x 4096 x 11008: 8.3 us, where a plain read of as many bytes takes 6.2 us); at 16 rows the
+// activations are twice the bytes of the weights in shared memory, which leaves twelve warps on an SM.
 #include "qzo_common.cuh"
 #include "launch.cuh"
 #include "layers.cuh"
@@ -35,7 +36,7 @@ struct GemvLinear {
 struct GemvParams {
   GemvLinear lin[kMaxGroupedLinears];
   const __nv_bfloat16* x;
-  int n_lin, ldx, M, K, KB, G, cluster;
+  int n_lin, ldx, M, K, KB, G;
 };
 
 // Two 4-bit values u (bits 4p.. of each half of w) as the bf16 pair u - 8: 0x4300 | u is 128 + u, less 136; both exact.
@@ -46,84 +47,98 @@ __device__ __forceinline__ uint32_t weight_pair(uint32_t w, int p) {
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// NT: tiles of eight activation rows; RT: tiles of sixteen output features of a warp; S: stages of its ring; W: warps of a CTA,
-// which share its output features and take the groups of K in turn.
+constexpr int kRT = 2;               // tiles of sixteen output features of a warp, which are also a CTA's
+constexpr int kCols = 16 * kRT;
+constexpr int kStages = 3;           // of a warp's ring: a group of 128 k of the weights, their scales, and of the activations
+constexpr int kWeightBytes = kRT * 1024, kScaleBytes = kRT * 32;
+
+// XR: rows of activations that a stage holds (1, 4, 8 or 16, at least M); W: warps of a CTA, which share its output features and
+// take the groups of K in turn.
 // The weights are the A operand.  A lane's share of a tile is features 2g and 2g + 1 and the 32 k of its quarter t of the
 // group: two neighbouring 16-byte units of the kernel layout; its B fragments are then the 32 consecutive activations
 // of that quarter.
-// Every warp has a ring of its own in shared memory, filled by 16-byte asynchronous copies: no barrier in the loop.
-// Places in a stage: the unit of feature f and quarter t at (t RT 16 + f) ^ pad(t), pads {0, 1, 4, 5}, and the
+// Every warp has a ring of its own in shared memory, filled by 16-byte asynchronous copies: no barrier in the loop, which is
+// unrolled over the stages, so that every address in them is a register and a constant (a warp sees 2 KB of weights at a
+// time: what it issues around them counts as much as what they cost themselves).
+// Places in a stage: the unit of feature f and quarter t at (32 t + f) ^ pad(t), pads {0, 1, 4, 5}, and the
 // activations' unit q of a row at q ^ (q >> 3) ^ 2 (row & 1), so that the eight lanes of a phase (two g, four t) read eight
 // different 16-byte banks.
-template <int NT, int RT, int S, int W>
+template <int XR, int W>
 __global__ void __launch_bounds__(W * 32)
 gemv_w4_kernel(GemvParams p) {
-  constexpr int kWeightBytes = RT * 1024, kScaleBytes = RT * 32;
+  constexpr int NT = XR > 8 ? 2 : 1;                   // tiles of eight rows
+  constexpr int kStageBytes = kWeightBytes + kScaleBytes + 256 * XR;
   extern __shared__ __align__(128) uint8_t gemv_smem[];
-  const int rank = blockIdx.x % p.cluster, block = blockIdx.x / p.cluster;
+  const int rank = blockIdx.x, block = blockIdx.y;     // CTA of the cluster, output features
   int j = 0;
   while (j + 1 < p.n_lin && block >= p.lin[j + 1].first_cta) ++j;
-  const GemvLinear L = p.lin[j];
-  const int n0 = (block - L.first_cta) * 16 * RT;
+  const GemvLinear& L = p.lin[j];
+  const int n0 = (block - L.first_cta) * kCols, N = L.N;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int stage_bytes = kWeightBytes + kScaleBytes + 256 * p.M;
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(gemv_smem) + warp * S * stage_bytes;
-  const uint4* panel = L.wq + (size_t)(n0 / kTileN) * p.KB * (kPackedTileBytes / 16) + n0 % kTileN;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(gemv_smem) + warp * kStages * kStageBytes;
+  const int step = W * gridDim.x, first = rank * W + warp;
 
-  // what a lane copies: of every quarter q units lane, lane + 32, ... of the 16 RT features, two neighbouring rows' units of
-  // activations at a time, one unit of scales (columns that do not exist: of ones that do, their outputs are not stored)
-  constexpr int kPad[4] = {0, 1, 4, 5};
-  const uint4* const w_src = panel + lane % (16 * RT);
-  const __nv_bfloat16* const s_src = L.scales + min(n0 + 8 * (lane % (2 * RT)), L.N - 8);
+  // what a lane copies of a group: of every quarter the unit of feature `lane`, one unit of scales (columns that do not exist: of
+  // ones that do, their outputs are not stored), and unit x_q of every other row of activations
+  const uint4* w_src = L.wq + ((size_t)(n0 / kTileN) * p.KB + 2 * (size_t)first) * (kPackedTileBytes / 16) + n0 % kTileN + lane;
+  const __nv_bfloat16* s_src = L.scales + (size_t)first * N + min(n0 + 8 * (lane % (2 * kRT)), N - 8);
   const int x_row = lane >> 4, x_q = lane & 15;
-  const __nv_bfloat16* const x_src = p.x + (size_t)x_row * p.ldx + 8 * x_q;
-  const uint32_t x_dst = kWeightBytes + kScaleBytes + 256 * x_row + 16 * (x_q ^ (x_q >> 3) ^ (x_row << 1));
-  auto fetch = [&](int grp, uint32_t at) {
+  const __nv_bfloat16* x_src = p.x + (size_t)x_row * p.ldx + (size_t)first * kGroup + 8 * x_q;
+  const uint32_t w_dst[4] = {ring + 16 * lane, ring + 16 * (32 + (lane ^ 1)), ring + 16 * (64 + (lane ^ 4)), ring + 16 * (96 + (lane ^ 5))};
+  const uint32_t s_dst = ring + kWeightBytes + 16 * lane;
+  const uint32_t x_dst = ring + kWeightBytes + kScaleBytes + 256 * x_row + 16 * (x_q ^ (x_q >> 3) ^ (x_row << 1));
+  int next = first;                                    // the group that is copied next
+  auto fetch = [&](int at) {                           // `at`: offset of its stage
+    const bool last = next == p.G - 1;
     // a last block of 64 that does not exist is read from the one before it: its activations are zeros
-    const uint4* src = w_src + (size_t)grp * (2 * kPackedTileBytes / 16);
-    const int second = 2 * grp + 1 < p.KB ? kPackedTileBytes / 16 : 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-      for (int f = 0; f < 16 * RT; f += 32)
-        copy16(at + 16 * (q * 16 * RT + f + (lane ^ kPad[q])), src + (q >> 1) * second + (q & 1) * kTileN + f);
-    if (lane < 2 * RT) copy16(at + kWeightBytes + 16 * lane, s_src + (size_t)grp * L.N);
-    const bool live = grp * kGroup + 8 * x_q < p.K;    // behind K: zeros, whatever stands there
-    const __nv_bfloat16* x = x_src + grp * kGroup;
-    uint32_t dst = at + x_dst;
-    for (int row = x_row; row < p.M; row += 2, x += 2 * (size_t)p.ldx, dst += 512) {
+    const int second = last && (p.KB & 1) ? 0 : kPackedTileBytes / 16;
+    copy16(w_dst[0] + at, w_src);
+    copy16(w_dst[1] + at, w_src + kTileN);
+    copy16(w_dst[2] + at, w_src + second);
+    copy16(w_dst[3] + at, w_src + second + kTileN);
+    if (lane < 2 * kRT) copy16(s_dst + at, s_src);
+    const bool live = !last || next * kGroup + 8 * x_q < p.K;          // behind K: zeros, whatever stands there
+    const __nv_bfloat16* x = x_src;
+    uint32_t dst = x_dst + at;
+    for (int row = x_row; row < (XR == 1 ? 1 : p.M); row += 2, x += 2 * (size_t)p.ldx, dst += 512) {
       if (live) copy16(dst, x);
       else zero16(dst);
     }
+    next += step;
+    w_src += (size_t)step * (2 * kPackedTileBytes / 16);
+    s_src += (size_t)step * N;
+    x_src += (size_t)step * kGroup;
   };
   // what it reads: the units of features 2g, 2g + 1 and quarter t of every tile, the activations of quarter t of its rows
-  const uint32_t w_lds0 = 16 * (t * 16 * RT + ((2 * g) ^ ((t & 1) + 4 * (t >> 1)))), w_lds1 = w_lds0 ^ 16;
-  uint32_t x_lds[NT];
+  const uint32_t w_lds = ring + 16 * (32 * t + ((2 * g) ^ ((t & 1) + 4 * (t >> 1))));
+  const uint32_t w_lds1 = w_lds ^ 16, s_lds = ring + kWeightBytes + 4 * g;
+  uint32_t x_lds[NT][4];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int row = min(nt * 8 + g, p.M - 1);          // rows that do not exist: any, their sums are not stored
-    x_lds[nt] = kWeightBytes + kScaleBytes + 256 * row + 16 * ((4 * t) ^ (t >> 1) ^ ((row & 1) << 1));
+    const int row = XR == 1 ? 0 : min(nt * 8 + g, p.M - 1);            // rows that do not exist: any, their sums are not stored
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      x_lds[nt][i] = ring + kWeightBytes + kScaleBytes + 256 * row + 16 * ((4 * t + i) ^ (t >> 1) ^ ((row & 1) << 1));
   }
-  float acc[RT][NT][4] = {};
-  auto contract = [&](uint32_t at) {
+  float acc[kRT][NT][4] = {};
+  auto contract = [&](int at) {
     uint4 x[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[nt][i] = lds16((at + x_lds[nt]) ^ (16 * i));
-    // the words of all tiles in turn, so that the matrix instructions of neighbouring ones do not wait for one another (16 x 5120
-    // x 13824 15.3 us, 16.1 us tile by tile)
-    uint4 ua[RT], ub[RT];
-    float c[RT][NT][4] = {};
+      for (int i = 0; i < 4; ++i) x[nt][i] = lds16(x_lds[nt][i] + at);
+    // the words of both tiles in turn, so that the matrix instructions of one do not wait for one another
+    uint4 ua[kRT], ub[kRT];
+    float c[kRT][NT][4] = {};
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      ua[r] = lds16(at + w_lds0 + 256 * r);
-      ub[r] = lds16(at + w_lds1 + 256 * r);
+    for (int r = 0; r < kRT; ++r) {
+      ua[r] = lds16(w_lds + at + 256 * r);
+      ub[r] = lds16(w_lds1 + at + 256 * r);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
+      for (int r = 0; r < kRT; ++r) {
         const uint32_t wa = i == 0 ? ua[r].x : i == 1 ? ua[r].y : i == 2 ? ua[r].z : ua[r].w;
         const uint32_t wb = i == 0 ? ub[r].x : i == 1 ? ub[r].y : i == 2 ? ub[r].z : ub[r].w;
         const uint32_t a0 = weight_pair(wa, 0), a1 = weight_pair(wa, 1), a2 = weight_pair(wa, 2), a3 = weight_pair(wa, 3);
@@ -135,8 +150,8 @@ gemv_w4_kernel(GemvParams p) {
       }
     }
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const uint32_t s2 = lds4(at + kWeightBytes + 32 * r + 4 * g);
+    for (int r = 0; r < kRT; ++r) {
+      const uint32_t s2 = lds4(s_lds + at + 32 * r);
       const float2 s = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&s2));
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -149,38 +164,40 @@ gemv_w4_kernel(GemvParams p) {
   };
   serving_begin();
   serving_next();
-  const int step = W * p.cluster, first = rank * W + warp;
 #pragma unroll
-  for (int s = 0; s < S - 1; ++s) {
-    if (first + s * step < p.G) fetch(first + s * step, ring + s * stage_bytes);
+  for (int s = 0; s < kStages - 1; ++s) {
+    if (next < p.G) fetch(s * kStageBytes);
     copies_commit();
   }
-  int use = 0, fill = S - 1;
-  for (int grp = first; grp < p.G; grp += step) {
-    copies_wait<S - 2>();
-    __syncwarp();                                      // this stage has landed, and every lane is done with the one before it
-    if (grp + (S - 1) * step < p.G) fetch(grp + (S - 1) * step, ring + fill * stage_bytes);
-    copies_commit();
-    contract(ring + use * stage_bytes);
-    use = use + 1 == S ? 0 : use + 1;
-    fill = fill + 1 == S ? 0 : fill + 1;
+  for (int grp = first; grp < p.G;) {
+#pragma unroll
+    for (int u = 0; u < kStages; ++u, grp += step) {
+      if (grp >= p.G) break;
+      copies_wait<kStages - 2>();
+      __syncwarp();                                    // this stage has landed, and every lane is done with the one before it
+      if (next < p.G) fetch((u + kStages - 1) % kStages * kStageBytes);
+      copies_commit();
+      contract(u * kStageBytes);
+    }
   }
   __syncthreads();                                     // the rings are free: the sums go there
-  float (*red)[8 * NT][16 * RT + 1] = reinterpret_cast<float (*)[8 * NT][16 * RT + 1]>(gemv_smem);
+  float (*red)[8 * NT][kCols + 1] = reinterpret_cast<float (*)[8 * NT][kCols + 1]>(gemv_smem);
 
   // the warps' sums in their order, then the cluster's CTAs' in theirs
 #pragma unroll
-  for (int r = 0; r < RT; ++r)
+  for (int r = 0; r < kRT; ++r)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) red[warp][nt * 8 + 2 * t + (e & 1)][16 * r + 2 * g + (e >> 1)] = acc[r][nt][e];
+      for (int e = 0; e < 4; ++e)
+        if (XR > 1 || (t == 0 && (e & 1) == 0)) red[warp][nt * 8 + 2 * t + (e & 1)][16 * r + 2 * g + (e >> 1)] = acc[r][nt][e];
   __syncthreads();
   cg::cluster_group cluster = cg::this_cluster();
-  constexpr int kOut = 16 * RT * 8 * NT;
-  if (p.cluster > 1) {
-    for (int i = threadIdx.x; i < kOut; i += W * 32) {
-      const int row = i / (16 * RT), n = i % (16 * RT);
+  const bool alone = gridDim.x == 1;
+  const int outs = kCols * (XR == 1 ? 1 : p.M);
+  if (!alone) {
+    for (int i = threadIdx.x; i < outs; i += W * 32) {
+      const int row = i / kCols, n = i % kCols;
       float y = red[0][row][n];
 #pragma unroll
       for (int w = 1; w < W; ++w) y += red[w][row][n];
@@ -189,42 +206,36 @@ gemv_w4_kernel(GemvParams p) {
     cluster.sync();
   }
   // each CTA of the cluster finishes its share of the outputs
-  for (int i = rank * W * 32 + threadIdx.x; i < kOut; i += W * 32 * p.cluster) {
-    const int row = i / (16 * RT), n = i % (16 * RT);
-    if (row >= p.M || n0 + n >= L.N) continue;
+  for (int i = rank * W * 32 + threadIdx.x; i < outs; i += W * 32 * gridDim.x) {
+    const int row = i / kCols, n = i % kCols;
+    if (n0 + n >= N) continue;
     float y = 0.0f;
-    if (p.cluster > 1) {
-      for (int c = 0; c < p.cluster; ++c) y += *cluster.map_shared_rank(&red[0][row][n], c);
-    } else {
+    if (alone) {
 #pragma unroll
       for (int w = 0; w < W; ++w) y += red[w][row][n];
+    } else {
+      for (int c = 0; c < (int)gridDim.x; ++c) y += *cluster.map_shared_rank(&red[0][row][n], c);
     }
     if (L.bias) y += L.bias[n0 + n];
     L.out[(size_t)row * L.ldo + n0 + n] = __float2bfloat16_rn(y);
   }
-  if (p.cluster > 1) cluster.sync();                  // no CTA leaves while another reads its sums
+  if (!alone) cluster.sync();                         // no CTA leaves while another reads its sums
 }
 
-template <int NT, int RT, int S, int W>
-int run_gemv(GemvParams& p, cudaStream_t st) {
-  int blocks = 0;
-  for (int j = 0; j < p.n_lin; ++j) {
-    p.lin[j].first_cta = blocks;
-    blocks += ceil_div(p.lin[j].N, 16 * RT);
-  }
+template <int XR, int W>
+int run_gemv(const GemvParams& p, int blocks, cudaStream_t st) {
   // Few output features: the CTAs of a cluster share the groups of K (measured at K = 11008, N = 256, one row: 9.4 us alone,
   // 4.2 us with clusters of eight; at K = N = 4096, 128 CTAs of 32 features, 5.5 us alone, 5.9 us with clusters of two).
   int cluster = 1;
   while (cluster < kMaxCluster && 2 * cluster * blocks <= kSMs && 2 * cluster * W <= p.G) cluster *= 2;
-  p.cluster = cluster;
-  constexpr int kSums = W * 8 * NT * (16 * RT + 1) * (int)sizeof(float);
+  constexpr int kRing = W * kStages * (kWeightBytes + kScaleBytes + 256 * XR), kSums = W * (XR > 8 ? 16 : 8) * (kCols + 1) * (int)sizeof(float);
   // The CTAs are spread evenly: each asks for so much shared memory that no SM takes more than its share of them (1 x 4096 x
-  // 11008, 344 CTAs: 9.7 us, 11.7 us where an SM may take a fourth one; 1 x 5120 x 13824 11.6 us against 14.5).
+  // 11008, 344 CTAs: 9.7 us, 11.7 us when an SM could take a fourth one; 1 x 5120 x 13824 11.6 us against 14.5).
   const int share = ceil_div(blocks * cluster, kSMs), even = (kSMem / (share + 1) - 1024) / 16 * 16 + 16;
-  const int smem = std::max({W * S * (RT * 1056 + 256 * p.M), kSums, even});
+  const int smem = std::max({kRing, kSums, even});
   static std::atomic<unsigned long long> allowed{0};
-  QZO_CUDA_TRY(allow_dynamic_smem(gemv_w4_kernel<NT, RT, S, W>, kSMem - 1024, allowed));
-  return launch_serving<GemvParams>(gemv_w4_kernel<NT, RT, S, W>, dim3(blocks * cluster), dim3(W * 32), smem, cluster, st, p);
+  QZO_CUDA_TRY(allow_dynamic_smem(gemv_w4_kernel<XR, W>, kSMem - 1024, allowed));
+  return launch_serving<GemvParams>(gemv_w4_kernel<XR, W>, dim3(cluster, blocks), dim3(W * 32), smem, cluster, st, p);
 }
 
 }  // namespace
@@ -232,21 +243,24 @@ int run_gemv(GemvParams& p, cudaStream_t st) {
 int launch_gemv_group(const __nv_bfloat16* d_x, int ldx, int M, int K, const GemmLinear* lins, int n_lin, cudaStream_t st) {
   if (M <= 0 || M > QZO_GEMV_MAX_ROWS || K <= 0 || (K % 8) || n_lin < 1 || n_lin > kMaxGroupedLinears) return QZO_ERR_BAD_ARG;
   GemvParams p{};
+  int64_t blocks = 0;
   for (int j = 0; j < n_lin; ++j) {
     if (lins[j].N <= 0 || (lins[j].N % 8)) return QZO_ERR_BAD_ARG;
-    p.lin[j] = GemvLinear{(const uint4*)lins[j].wq, lins[j].scales, lins[j].bias, lins[j].out, lins[j].ldo, lins[j].N, 0};
+    p.lin[j] = GemvLinear{(const uint4*)lins[j].wq, lins[j].scales, lins[j].bias, lins[j].out, lins[j].ldo, lins[j].N, (int)blocks};
+    blocks += ceil_div(lins[j].N, kCols);
   }
+  if (blocks > 65535) return QZO_ERR_BAD_ARG;            // the grid's second dimension: two million output features
   p.x = d_x;
   p.n_lin = n_lin; p.ldx = ldx; p.M = M; p.K = K;
   p.KB = ceil_div(K, kBlockK);
   p.G = ceil_div(K, kGroup);
-  if (M <= 8) return run_gemv<1, 2, 3, 8>(p, st);
+  if (M == 1) return run_gemv<1, 8>(p, (int)blocks, st);
+  if (M <= 4) return run_gemv<4, 8>(p, (int)blocks, st);
+  if (M <= 8) return run_gemv<8, 8>(p, (int)blocks, st);
   // Two tiles of rows: the activations take half of a stage, so CTAs of eight warps leave room for two of them on an SM
   // only, which pays where there is no more than one CTA per SM (measured with 16 rows: K = N = 4096 6.5 us against 8.0 us
   // with four warps, K = 5120, N = 13824 19.0 us against 16.6 us).
-  int blocks = 0;
-  for (int j = 0; j < n_lin; ++j) blocks += ceil_div(lins[j].N, 32);
-  return blocks <= kSMs ? run_gemv<2, 2, 3, 8>(p, st) : run_gemv<2, 2, 3, 4>(p, st);
+  return blocks <= kSMs ? run_gemv<16, 8>(p, (int)blocks, st) : run_gemv<16, 4>(p, (int)blocks, st);
 }
 
 }  // namespace qzo
