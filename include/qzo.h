@@ -385,7 +385,8 @@ int qzo_step_host(qzo_model* m, const int32_t* h_tokens, const int32_t* h_labels
  * d_positions, d_slots int32 [R], as qzo_assign_slots writes the last three; R <= max_tokens; positions < max_seq.
  * Rows of padding (negative position or slot) give logits that mean nothing and touch no cache.  An index out of range
  * (token, position, slot, block) sets bit 1 of the model's status word (qzo_device_status).
- * Up to QZO_GEMV_MAX_ROWS rows the linears run as qzo_gemv_int4, above as qzo_perturbed_gemm with sign 0.  Asynchronous on the model's stream. */
+ * Up to QZO_GEMV_MAX_ROWS rows the linears run as qzo_gemv_int4, above as qzo_perturbed_gemm with sign 0.  Asynchronous on the model's
+ * stream, and nothing but launches: a model whose stream is not the legacy default one can have its steps captured. */
 int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
                const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
                int table_width, float* d_logits);

@@ -151,6 +151,35 @@ def test_decode_agrees_with_the_training_forward_and_leaves_it_alone():
     assert outs[0][:2] == outs[1][:2] and torch.equal(outs[0][2], outs[1][2])
 
 
+def test_captured_decode_steps_replay():
+    # a model on a stream of its own: one captured step, replayed token after token, gives what direct steps give
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg("tiny_dh128")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        gm = qzo.build_model_from_raw(inputs.raw_model_tensors(cfg, seed=1000), 64)
+        direct, replayed = (Server(qzo, gm, cfg, 2, 16, 26) for _ in range(2))
+        prompt = {0: list(range(30)), 1: [5, 6, 7]}
+        for srv in (direct, replayed):
+            srv.step(prompt, 33)
+        new, tokens = (torch.ones(2, dtype=torch.int32, device="cuda") for _ in range(2))
+        logits = torch.empty((2, cfg["vocab"]), dtype=torch.float32, device="cuda")
+        step = lambda srv, out: gm.qzo_decode_requests(srv.caches, tokens, srv.lens, new, srv.table, srv.free, srv.count, logits=out)  # noqa: E731
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step(replayed, logits)
+        for _ in range(20):                                   # across a block's end
+            want, _ = step(direct, None)
+            graph.replay()
+            assert torch.equal(logits, want)
+            tokens.copy_(want.argmax(-1))
+        assert torch.equal(direct.lens, replayed.lens) and replayed.lens.tolist() == [50, 23] and gm.qzo_device_status() == 0
+        side.synchronize()
+        del graph
+        gm.close()
+
+
 @pytest.mark.parametrize("name,layers", [("llama7b", 2), ("opt6.7b", 1), ("llama13b", 1)])
 def test_full_width_decode_agrees_with_the_training_forward(name, layers):
     # prompts by the GEMM path, then their last tokens again, one by one, by the matrix-vector path
