@@ -228,8 +228,8 @@ __device__ __forceinline__ void e4m3x4_to_f16x2(uint32_t four, uint32_t& lo, uin
   asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(four));
 }
 
-// What one lane holds of a key row: NW words of two elements each, the row's 16-byte chunks t, t + 4, ... in order.
-// Values: the same for the chunks that belong to lane g.  8-bit codes become fp16 pairs, which hold them exactly.
+// What one lane holds of a key row: the row's 16-byte units t, t + 4, ... in order, as words of two elements; of a value row
+// the units that belong to lane g.  8-bit codes become fp16 pairs, which hold them exactly.
 template <int DH, bool F8>
 struct Layout {
   static constexpr int kRowBytes = DH * (F8 ? 1 : 2);
@@ -382,7 +382,7 @@ paged_attention_kernel(PagedParams p) {
   }
 
   // For 8-bit keys the queries become fp16, scaled by a power of two that brings the head's largest element to [64, 128):
-  // exact but for elements 2^-30 below it.
+  // exact but for elements below 2^-23 of it, which are off by at most 2^-31 of it.
   float unscale[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -420,8 +420,8 @@ paged_attention_kernel(PagedParams p) {
   }
   const int32_t* pages = p.table + (size_t)seq * p.width;
   const int in_block = (1 << p.log2_block) - 1;
-  // Tiles come through a ring of each warp's own in shared memory, filled by 16-byte asynchronous copies two tiles ahead; rows
-  // behind the split's end and blocks out of range are filled with zeros.  Block ids are looked up one tile before that.
+  // Tiles come through a ring of each warp's own in shared memory, filled by 16-byte asynchronous copies kStages - 1 tiles ahead;
+  // rows behind the split's end and blocks out of range are filled with zeros.  Block ids are looked up one tile before that.
   constexpr int S = Lay::kSubs, kTileKeys = Lay::kTileKeys, kStep = W * kTileKeys, kUnits = Lay::kRowBytes / 16;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(att_smem) + warp * kStages * kStageBytes;
   int page[S];
@@ -585,7 +585,7 @@ paged_attention_kernel(PagedParams p) {
     free_stage = free_stage + 1 == kStages ? 0 : free_stage + 1;
   }
 
-  serving_next();    // not earlier: CTAs that wait take room and issue slots from the loads (1 row of 131071 keys 83.6 us, 86.1 us if at the start)
+  serving_next();                      // not earlier: CTAs that wait take room from those that load (83.6 us, 86.1 us if at the start)
   __syncthreads();                     // the rings are free: the warps' results go there
   // join the warps
 #pragma unroll

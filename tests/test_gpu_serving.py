@@ -29,7 +29,8 @@ def _randn(shape, seed, std=1.0):
 # ------------------------------------------------------------------ matrix-vector products
 
 GEMV_CASES = [(1, 128, 8), (1, 64, 128), (3, 8, 16), (1, 256, 688), (2, 688, 256), (5, 1032, 136), (8, 4096, 384), (9, 200, 72), (16, 1920, 1000),
-              (1, 4096, 4096), (7, 11008, 264), (16, 72, 2056), (12, 13824, 128)]
+              (1, 4096, 4096), (7, 11008, 264), (16, 72, 2056), (12, 13824, 128),
+              (10, 384, 4808), (4, 1096, 4808), (1, 136, 9608)]
 
 
 def _gemv_case(lib, M, K, N, seed):
