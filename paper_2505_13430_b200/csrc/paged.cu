@@ -99,10 +99,10 @@ qk_norm_rope_cache_kernel(RopeCacheParams p) {
       hi_raw[i] = *reinterpret_cast<const uint4*>(src + DH / 2 + 8 * l);
     }
   }
-  const bool work = slot >= 0;                         // lanes of padding go along for the shuffles only
+  const bool work = slot >= 0 && given >= 0;           // lanes of padding go along for the shuffles only
   float4 cs[4];                                        // {cos, sin} of two pairs each
   if (p.table && work && first < p.H + p.Hkv) {
-    const int pos = min(max(given, 0), p.max_pos - 1);
+    const int pos = min(given, p.max_pos - 1);
     if (pos != given && l == 0 && p.status) atomicOr(p.status, kStatusBadToken);
     const float4* row = reinterpret_cast<const float4*>(p.table + 2 * ((size_t)pos * (DH / 2) + 8 * l));
 #pragma unroll

@@ -204,6 +204,26 @@ def test_queries_in_place_and_bad_indices(lib):
     assert torch.equal(far, near)
 
 
+@pytest.mark.parametrize("rot,kind", [(True, "bf16"), (False, "bf16"), (True, "e4m3")])
+def test_a_negative_position_is_padding_whatever_its_slot(lib, rot, kind):
+    T, H, dh = 4, 2, 64
+    ck, cv, ks, vs = _pages(kind, (2, H, 16, dh), 2)
+    kept = ck.clone(), cv.clone()
+    table = lib.qzo_rope_table(64, dh, 10000.0) if rot else None
+    q, k, v = (_randn((T, H, dh), 30 + i).cuda() for i in range(3))
+    pos = torch.tensor([0, -1, 5, -2 ** 31], dtype=torch.int32, device="cuda")
+    slots = torch.tensor([-1, 3, 4, 31], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = torch.full((T, H, dh), 7.0, dtype=torch.bfloat16, device="cuda")
+    lib.qzo_qk_norm_rope_cache(q, k, v, pos, slots, lib.KvCache(ck, cv, ks, vs), table=table, q_out=out, status=status)
+    assert int(status.item()) == 0
+    assert (out[[0, 1, 3]] == 7.0).all() and (out[2] != 7.0).any()
+    for pages, old in zip((ck, cv), kept):
+        assert not torch.equal(pages[0, :, 4].float(), old[0, :, 4].float())
+        pages[0, :, 4] = old[0, :, 4]
+        assert torch.equal(pages.float(), old.float())
+
+
 # ------------------------------------------------------------------ attention over the paged cache
 
 ATTEND_CASES = [
