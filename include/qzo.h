@@ -246,6 +246,8 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
  *  - rows are numbered request by request: d_row_seq, d_positions, d_slots int32 [max_rows], -1 behind the last row;
  *  - d_lens_out int32 [B] = the new lengths (0 for finished requests), d_free_count_out int32 [1] = the new count.
  * d_lens_out may be d_lens and d_free_count_out may be d_free_count; no other arguments overlap.
+ * Ids are handed on as they are found; a row whose block id no cache can hold (negative, or 2^31 / block_size and more) gets
+ * slot 2^31 - 1, which qzo_qk_norm_rope_cache reports.
  * When the step cannot be served (too few free blocks, a table too narrow, more rows than max_rows, a negative length, a
  * stack beyond its capacity), nothing is changed: lengths and count are handed on as they are, every row is padding, and
  * bit 2 of the status word is set.  B from 1 to QZO_MAX_REQUESTS, max_rows up to 2^30, block_size as in qzo_kv_cache. */

@@ -158,7 +158,8 @@ assign_slots_kernel(SlotParams p) {
         if (t[i] >= p.max_rows) continue;
         p.row_seq[t[i]] = t[i] < total.rows ? seq[i] : -1;
         p.positions[t[i]] = pos[i];
-        p.slots[t[i]] = id[i] < 0 ? -1 : (id[i] << p.log2_block) | (pos[i] & mask);
+        // an id that no pool can have (a table or stack of the caller's that holds one) must not wrap to a slot of another block
+        p.slots[t[i]] = pos[i] < 0 ? -1 : (unsigned)id[i] > (unsigned)(INT32_MAX >> p.log2_block) ? INT32_MAX : (id[i] << p.log2_block) | (pos[i] & mask);
       }
     }
     for (int i = me; i < (int)total.need; i += all) {

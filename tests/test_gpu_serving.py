@@ -455,6 +455,22 @@ def test_steps_that_cannot_be_served(lib, lens, new, count, rows):
         assert status == 0 and got["lens"][0] == want["lens"][0] and np.array_equal(got["slots"], want["slots"])
 
 
+@pytest.mark.parametrize("block", [16, 256])
+@pytest.mark.parametrize("bad", [-1, -2 ** 31, 2 ** 31 - 1, "first"])
+def test_ids_that_no_cache_can_hold_do_not_become_slots(lib, block, bad):
+    bad = 2 ** 31 // block if bad == "first" else bad
+    # request 0 holds a block with such an id, request 1 takes one from the stack, request 2 is clean
+    table = np.array([[bad, -1], [-1, -1], [3, -1]], np.int32)
+    got, status = _slots_run(lib, [2, 0, 5], [1, 1, 1], table, [1, bad], 2, block, 4)
+    assert status == 0 and got["free_count"] == 1
+    assert got["slots"].tolist() == [2 ** 31 - 1, 2 ** 31 - 1, 3 * block + 5, -1]
+    assert got["positions"].tolist() == [2, 0, 5, -1] and got["table"][1, 0] == bad
+    # the largest id that has slots: the same as any other
+    top = 2 ** 31 // block - 1
+    got, _ = _slots_run(lib, [0], [2], np.full((1, 1), -1, np.int32), [top], 1, block, 2)
+    assert got["slots"].tolist() == [top * block, top * block + 1]
+
+
 # ------------------------------------------------------------------ streams, graphs, together
 
 def test_operators_on_a_side_stream_and_in_a_replayed_graph(lib):
