@@ -185,7 +185,7 @@ int qzo_gemv_int4(const void* d_x_bf16, int ldx, const void* d_wq, const void* d
 
 /* A paged key-value cache of one layer, described by the caller (host struct, read during the call): keys and
  * values in blocks [n_blocks][n_kv_heads][block_size][head_dim], 16-byte aligned.  dtype QZO_DTYPE_BF16 (both
- * scales 1) or QZO_DTYPE_E4M3: the stored code times the scale (> 0) is the value; codes saturate at +-448.
+ * scales 1) or QZO_DTYPE_E4M3: the stored code times the scale (2^-64 to 2^64) is the value; codes saturate at +-448.
  * block_size is a power of two from 16 to 256, head_dim 64 or 128, n_blocks * block_size < 2^31. */
 typedef struct {
   void* k;
@@ -226,7 +226,7 @@ int qzo_paged_attention_workspace_bytes(int R, int n_heads, int n_kv_heads, int 
  * Several rows may belong to one request (a prompt's rows, each of which sees the keys up to its own).
  * d_q bf16 [R][ldq] and d_out bf16 [R][ldo], head h at h * head_dim, 16-byte aligned, strides multiples of 8, not
  * overlapping; d_block_table int32 [n_seqs][table_width], at most 2^30 tokens wide; d_row_seq int32 [R] = the request of each row, NULL: row t is
- * request t (R <= n_seqs); scale > 0 (1 / sqrt(head_dim) as a rule); n_heads a multiple of n_kv_heads.
+ * request t (R <= n_seqs); scale from 2^-40 to 2^40 (1 / sqrt(head_dim) as a rule); n_heads a multiple of n_kv_heads.
  * d_workspace: qzo_paged_attention_workspace_bytes, 256-aligned; calls that may run at the same time (two streams, two
  * captured graphs) need one each.  Nothing in it outlives the call.
  * A request outside [0, n_seqs), a position beyond the table or a block id outside the cache sets bit 1 of the status

@@ -752,7 +752,9 @@ bool cache_ok(const qzo_kv_cache* c) {
   if ((int64_t)c->n_blocks * c->block_size > INT32_MAX) return false;
   if (c->head_dim != 64 && c->head_dim != 128) return false;
   if (c->dtype == QZO_DTYPE_BF16) return c->k_scale == 1.0f && c->v_scale == 1.0f;
-  return c->dtype == QZO_DTYPE_E4M3 && c->k_scale > 0.0f && c->v_scale > 0.0f && isfinite(c->k_scale) && isfinite(c->v_scale);
+  // both a scale and its reciprocal are used, and the keys' scale times the scores': far from where fp32 ends
+  auto fits = [](float v) { return v >= 0x1p-64f && v <= 0x1p64f; };
+  return c->dtype == QZO_DTYPE_E4M3 && fits(c->k_scale) && fits(c->v_scale);
 }
 
 int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat16* k, int ldk, const __nv_bfloat16* v, int ldv,
@@ -850,7 +852,7 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
   if (!d_q_bf16 || !d_block_table || !d_positions || !d_out_bf16) return QZO_ERR_BAD_ARG;
   if (!cache_ok(cache) || R <= 0 || n_seqs <= 0 || table_width <= 0 || n_heads <= 0 || n_heads % cache->n_kv_heads) return QZO_ERR_BAD_ARG;
   if (!d_row_seq && R > n_seqs) return QZO_ERR_BAD_ARG;
-  if ((int64_t)table_width * cache->block_size > kMostKeys || !(scale > 0.0f) || !isfinite(scale)) return QZO_ERR_BAD_ARG;
+  if ((int64_t)table_width * cache->block_size > kMostKeys || !(scale >= 0x1p-40f && scale <= 0x1p40f)) return QZO_ERR_BAD_ARG;
   const int64_t wq = (int64_t)n_heads * cache->head_dim;
   if (ldq < wq || ldo < wq || (ldq % 8) || (ldo % 8)) return QZO_ERR_BAD_ARG;
   if (((uintptr_t)d_q_bf16 & 15) || ((uintptr_t)d_out_bf16 & 15)) return QZO_ERR_BAD_ARG;

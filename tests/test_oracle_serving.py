@@ -141,6 +141,19 @@ def test_paged_attention_refusals():
             qzo.qzo_paged_attention_workspace_bytes(*args)
 
 
+def test_scales_whose_reciprocal_or_product_leaves_fp32_are_refused():
+    qzo = _lib()
+    def rope(cache):
+        return qzo._lib.qzo_qk_norm_rope_cache(P, 256, P, 128, P, 128, NONE, NONE, 0.0, NONE, 0, P, P, P, 256, ctypes.byref(cache), 3, 4, None, None)
+    def attend(cache, scale):
+        return qzo._lib.qzo_paged_attention(P, 256, ctypes.byref(cache), P, 3, 4, NONE, P, scale, ctypes.c_void_p(0x20000), 256, 3, 4, NONE, 0, None, None)
+    for side in ("k_scale", "v_scale"):
+        _refused(rope, dict(cache=_cache(dtype=4, **{side: 2.0 ** -64})),
+                 [dict(cache=_cache(dtype=4, **{side: v})) for v in (1e-40, 2.0 ** -65, 2.0 ** 65, -1.0, float("nan"))])
+    _refused(attend, dict(cache=_cache(dtype=4, k_scale=2.0 ** 64), scale=2.0 ** 40),
+             [dict(scale=s) for s in (2.0 ** 41, 2.0 ** -41, -1.0, float("inf"))])
+
+
 def test_assign_slots_refusals():
     def call(lens, new, B, tab, w, bs, free, cap, cnt, rows, a, b, c, lo, co):
         return _lib()._lib.qzo_assign_slots(lens, new, B, tab, w, bs, free, cap, cnt, rows, a, b, c, lo, co, None, None)
