@@ -170,6 +170,7 @@ int qzo_update_scales_flat(void* d_scales_bf16, int64_t count, uint64_t seed, ui
  * Words "row", "slot", "position": a row is one token of this step; its position is its place in its
  * request, 0 for the first token; its slot is where its key and value live in the paged cache, block id *
  * block_size + place in the block.  A row with a negative position or slot is padding.
+ * All int32 and float arrays lie on 4-byte boundaries.
  * d_status (int on the device, may be NULL): bit 1 is set when an index out of range is met (see each call).
  * ---------------------------------------------------------------------------------- */
 

@@ -903,6 +903,7 @@ int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_toke
                const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
                int table_width, float* d_logits) {
   if (!d_tokens || !d_row_seq || !d_positions || !d_slots || !d_block_table) return QZO_ERR_BAD_ARG;
+  if (!words_aligned(d_tokens, d_row_seq, d_positions, d_slots, d_block_table)) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_decode(m, h_caches, R, n_seqs, table_width, d_logits));
   return decode(m, h_caches, d_tokens, d_row_seq, d_positions, d_slots, R, d_block_table, n_seqs, table_width, d_logits);
 }
@@ -910,7 +911,7 @@ int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_toke
 int qzo_decode_requests(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, int32_t* d_lens, const int32_t* d_new,
                         int B, int32_t* d_block_table, int table_width, int32_t* d_free, int free_capacity,
                         int32_t* d_free_count, int R, int32_t* d_maps, float* d_logits, int* d_status) {
-  if (!d_tokens || !d_maps) return QZO_ERR_BAD_ARG;
+  if (!d_tokens || !d_maps || !words_aligned(d_tokens, d_maps)) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_decode(m, h_caches, R, B, table_width, d_logits));
   int32_t *row_seq = d_maps, *positions = d_maps + R, *slots = d_maps + 2 * (size_t)R;
   QZO_TRY(qzo_assign_slots(d_lens, d_new, B, d_block_table, table_width, h_caches[0].block_size, d_free, free_capacity, d_free_count,

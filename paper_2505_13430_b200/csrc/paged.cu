@@ -825,6 +825,7 @@ int qzo_qk_norm_rope_cache(const void* d_q_bf16, int ldq, const void* d_k_bf16, 
                            const int32_t* d_positions, const int32_t* d_slots, void* d_q_out_bf16, int ldqo,
                            const qzo_kv_cache* cache, int T, int n_heads, int* d_status, void* stream) {
   if (!d_q_bf16 || !d_k_bf16 || !d_v_bf16 || !d_positions || !d_slots || !d_q_out_bf16) return QZO_ERR_BAD_ARG;
+  if (!words_aligned(d_positions, d_slots, d_status)) return QZO_ERR_BAD_ARG;
   if (!cache_ok(cache) || T <= 0 || n_heads <= 0 || n_heads % cache->n_kv_heads) return QZO_ERR_BAD_ARG;
   if ((d_q_gain || d_k_gain) && !(norm_eps > 0.0f)) return QZO_ERR_BAD_ARG;
   if (d_table && max_pos <= 0) return QZO_ERR_BAD_ARG;
@@ -850,6 +851,7 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
                         int table_width, const int32_t* d_row_seq, const int32_t* d_positions, float scale, void* d_out_bf16,
                         int ldo, int R, int n_heads, void* d_workspace, size_t workspace_bytes, int* d_status, void* stream) {
   if (!d_q_bf16 || !d_block_table || !d_positions || !d_out_bf16) return QZO_ERR_BAD_ARG;
+  if (!words_aligned(d_block_table, d_row_seq, d_positions, d_status)) return QZO_ERR_BAD_ARG;
   if (!cache_ok(cache) || R <= 0 || n_seqs <= 0 || table_width <= 0 || n_heads <= 0 || n_heads % cache->n_kv_heads) return QZO_ERR_BAD_ARG;
   if (!d_row_seq && R > n_seqs) return QZO_ERR_BAD_ARG;
   if ((int64_t)table_width * cache->block_size > kMostKeys || !(scale >= 0x1p-40f && scale <= 0x1p40f)) return QZO_ERR_BAD_ARG;

@@ -76,6 +76,9 @@ inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int kMostKeys = 1 << 30;   // tokens that a row of a block table may hold
 // Block sizes of a paged cache: powers of two from 16 (the keys of one matrix tile) to 256.
 inline bool block_size_ok(int b) { return b >= 16 && b <= 256 && (b & (b - 1)) == 0; }
+// Device pointers (null ones too) on 4-byte boundaries.
+template <typename... P>
+bool words_aligned(const P*... p) { return (((uintptr_t)p | ...) & 3) == 0; }
 
 // Checks that the current device is a compute-capability 10.x part; there is no other backend.
 int check_device();

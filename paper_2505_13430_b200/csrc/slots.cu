@@ -189,6 +189,8 @@ extern "C" int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int
   if (!d_lens || !d_new || !d_block_table || !d_free || !d_free_count || !d_row_seq || !d_positions || !d_slots ||
       !d_lens_out || !d_free_count_out)
     return QZO_ERR_BAD_ARG;
+  if (!words_aligned(d_lens, d_new, d_block_table, d_free, d_free_count, d_row_seq, d_positions, d_slots, d_lens_out, d_free_count_out, d_status))
+    return QZO_ERR_BAD_ARG;
   if (B <= 0 || B > QZO_MAX_REQUESTS || table_width <= 0 || free_capacity <= 0 || max_rows <= 0 || max_rows > (1 << 30)) return QZO_ERR_BAD_ARG;
   if (!block_size_ok(block_size)) return QZO_ERR_BAD_ARG;
   // a request's length and the slots of the pool are 32-bit numbers

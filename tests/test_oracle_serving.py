@@ -141,6 +141,20 @@ def test_paged_attention_refusals():
             qzo.qzo_paged_attention_workspace_bytes(*args)
 
 
+def test_index_arrays_off_their_boundary_are_refused():
+    lib = _lib()._lib
+    cache = _cache()
+    def rope(pos=P, slots=P, status=NONE):
+        return lib.qzo_qk_norm_rope_cache(P, 256, P, 128, P, 128, NONE, NONE, 0.0, NONE, 0, pos, slots, P, 256, ctypes.byref(cache), 3, 4, status, None)
+    def attend(tab=P, seq=NONE, pos=P, status=NONE):
+        return lib.qzo_paged_attention(P, 256, ctypes.byref(cache), tab, 3, 4, seq, pos, 0.1, ctypes.c_void_p(0x20000), 256, 3, 4, NONE, 0, status, None)
+    def slots(lens=P, new=P, tab=P, free=P, cnt=P, a=P, b=P, c=P, lo=P, co=P, status=NONE):
+        return lib.qzo_assign_slots(lens, new, 4, tab, 4, 16, free, 16, cnt, 8, a, b, c, lo, co, status, None)
+    for call in (rope, attend, slots):
+        names = call.__code__.co_varnames[:call.__code__.co_argcount]
+        _refused(call, {}, [{n: ODD} for n in names])
+
+
 def test_scales_whose_reciprocal_or_product_leaves_fp32_are_refused():
     qzo = _lib()
     def rope(cache):
