@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(W * 32)
 gemv_w4_kernel(GemvParams p) {
   constexpr int NT = XR > 8 ? 2 : 1;                   // tiles of eight rows
   constexpr int kStageBytes = kWeightBytes + kScaleBytes + 256 * XR;
+  constexpr bool kTurned = XR > 8;
   extern __shared__ __align__(128) uint8_t gemv_smem[];
   const int rank = blockIdx.x, block = blockIdx.y;     // CTA of the cluster, output features
   int j = 0;
@@ -76,7 +77,8 @@ gemv_w4_kernel(GemvParams p) {
   const int n0 = (block - L.first_cta) * kCols, N = L.N;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(gemv_smem) + warp * kStages * kStageBytes;
-  const int step = W * gridDim.x, first = rank * W + warp;
+  const int step = W * (int)gridDim.x, mine = (p.G - 1 - (rank * W + warp) + step) / step;       // groups of this warp
+  const int first = rank * W + warp + (kTurned && mine > 0 ? block % mine * step : 0);
 
   // what a lane copies of a group: of every quarter the unit of feature `lane`, one unit of scales (columns that do not exist: of
   // ones that do, their outputs are not stored), and unit x_q of every other row of activations
@@ -87,7 +89,7 @@ gemv_w4_kernel(GemvParams p) {
   const uint32_t w_dst[4] = {ring + 16 * lane, ring + 16 * (32 + (lane ^ 1)), ring + 16 * (64 + (lane ^ 4)), ring + 16 * (96 + (lane ^ 5))};
   const uint32_t s_dst = ring + kWeightBytes + 16 * lane;
   const uint32_t x_dst = ring + kWeightBytes + kScaleBytes + 256 * x_row + 16 * (x_q ^ (x_q >> 3) ^ (x_row << 1));
-  int next = first;                                    // the group that is copied next
+  int next = first, fetched = 0;                       // the group that is copied next
   auto fetch = [&](int at) {                           // `at`: offset of its stage
     const bool last = next == p.G - 1;
     // a last block of 64 that does not exist is read from the one before it: its activations are zeros
@@ -98,17 +100,21 @@ gemv_w4_kernel(GemvParams p) {
     copy16(w_dst[3] + at, w_src + second + kTileN);
     if (lane < 2 * kRT) copy16(s_dst + at, s_src);
     const bool live = !last || next * kGroup + 8 * x_q < p.K;          // behind K: zeros, whatever stands there
-    const __nv_bfloat16* x = x_src;
-    uint32_t dst = x_dst + at;
-    for (int row = x_row; row < (XR == 1 ? 1 : p.M); row += 2, x += 2 * (size_t)p.ldx, dst += 512) {
-      if (live) copy16(dst, x);
-      else zero16(dst);
-    }
+    const __nv_bfloat16* x = live ? x_src : p.x + (size_t)x_row * p.ldx;
+#pragma unroll
+    for (int i = 0; i < (XR + 1) / 2; ++i, x += 2 * (size_t)p.ldx)
+      if (x_row + 2 * i < (XR == 1 ? 1 : p.M)) copy16_or_zero(x_dst + at + 512 * i, x, live ? 16 : 0);
     next += step;
-    w_src += (size_t)step * (2 * kPackedTileBytes / 16);
-    s_src += (size_t)step * N;
-    x_src += (size_t)step * kGroup;
+    int jump = step;
+    if (kTurned) {
+      ++fetched;
+      if (next >= p.G) { next -= mine * step; jump -= mine * step; }
+    }
+    w_src += (int64_t)jump * (2 * kPackedTileBytes / 16);
+    s_src += (int64_t)jump * N;
+    x_src += (int64_t)jump * kGroup;
   };
+  auto more = [&] { return kTurned ? fetched < mine : next < p.G; };
   // what it reads: the units of features 2g, 2g + 1 and quarter t of every tile, the activations of quarter t of its rows
   const uint32_t w_lds = ring + 16 * (32 * t + ((2 * g) ^ ((t & 1) + 4 * (t >> 1))));
   const uint32_t w_lds1 = w_lds ^ 16, s_lds = ring + kWeightBytes + 4 * g;
@@ -166,16 +172,16 @@ gemv_w4_kernel(GemvParams p) {
   serving_next();
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) {
-    if (next < p.G) fetch(s * kStageBytes);
+    if (more()) fetch(s * kStageBytes);
     copies_commit();
   }
-  for (int grp = first; grp < p.G;) {
+  for (int i = kTurned ? 0 : first; i < (kTurned ? mine : p.G);) {
 #pragma unroll
-    for (int u = 0; u < kStages; ++u, grp += step) {
-      if (grp >= p.G) break;
+    for (int u = 0; u < kStages; ++u, i += kTurned ? 1 : step) {
+      if (i >= (kTurned ? mine : p.G)) break;
       copies_wait<kStages - 2>();
       __syncwarp();                                    // this stage has landed, and every lane is done with the one before it
-      if (next < p.G) fetch((u + kStages - 1) % kStages * kStageBytes);
+      if (more()) fetch((u + kStages - 1) % kStages * kStageBytes);
       copies_commit();
       contract(u * kStageBytes);
     }
