@@ -241,7 +241,7 @@ int run_gemv(const GemvParams& p, int blocks, cudaStream_t st) {
   const int smem = std::max({kRing, kSums, even});
   static std::atomic<unsigned long long> allowed{0};
   QZO_CUDA_TRY(allow_dynamic_smem(gemv_w4_kernel<XR, W>, kSMem - 1024, allowed));
-  return launch_serving<GemvParams>(gemv_w4_kernel<XR, W>, dim3(cluster, blocks), dim3(W * 32), smem, cluster, st, p);
+  return launch_serving(gemv_w4_kernel<XR, W>, dim3(cluster, blocks), dim3(W * 32), smem, cluster, st, p);
 }
 
 }  // namespace

@@ -21,8 +21,8 @@ void add_launches(long long n);   // kernels run by replaying a recorded step
 // Launch of a serving kernel: allowed to start while the kernel before it in the stream ends (a decode step is a chain of
 // launches of a few microseconds).  Such a kernel calls serving_begin() before it touches global memory, in every CTA.
 // cluster > 1: CTAs of a cluster.
-template <typename Params>
-int launch_serving(void (*kernel)(Params), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, const Params& params) {
+template <typename... Params, typename... Args>
+int launch_serving(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, const Args&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -36,14 +36,15 @@ int launch_serving(void (*kernel)(Params), dim3 grid, dim3 block, size_t smem, i
   attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   cfg.attrs = attrs;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
-  QZO_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, params));
+  QZO_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...));
   count_launch();
   return QZO_OK;
 }
 
 #ifdef __CUDACC__
 // Waits for the end of the kernel before this one and sees its writes.  Every CTA calls it, those without work too: the end
-// of this kernel stands for the end of all before it.
+// of this kernel stands for the end of all before it.  Returns at once in a kernel launched the ordinary way.  What is loaded
+// behind it must not come through a __restrict__ pointer: the compiler may move such a load in front of it.
 __device__ __forceinline__ void serving_begin() { cudaGridDependencySynchronize(); }
 // From here on the next kernel's CTAs may take their places (once every CTA has come here or ended).
 __device__ __forceinline__ void serving_next() { cudaTriggerProgrammaticLaunchCompletion(); }

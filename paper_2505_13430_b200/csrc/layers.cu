@@ -97,9 +97,11 @@ constexpr int kNormVecs = 4;
 
 template <bool LAYERNORM>
 __global__ void __launch_bounds__(kNormThreads)
-add_norm_kernel(__nv_bfloat16* __restrict__ x, const __nv_bfloat16* delta, const float* __restrict__ w,
+add_norm_kernel(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* __restrict__ w,
                 const float* __restrict__ b, const float* __restrict__ w2, const float* __restrict__ b2, int pair_rows,
                 float eps, int d, __nv_bfloat16* y) {
+  serving_begin();
+  serving_next();
   // rows from pair_rows on (second copy of a paired step in joint mode) use the second gain / bias set
   if (pair_rows > 0 && (int)blockIdx.x >= pair_rows) { w = w2; b = b2; }
   __shared__ float red[32];
@@ -395,8 +397,9 @@ attention_mma_kernel(const __nv_bfloat16* __restrict__ q, const __nv_bfloat16* _
 }
 
 // act = silu(gate) * up, eight elements per thread (n is a multiple of 8)
-__global__ void silu_mul_kernel(const __nv_bfloat16* __restrict__ gate, const __nv_bfloat16* __restrict__ up,
-                                __nv_bfloat16* __restrict__ out, int64_t nvec) {
+__global__ void silu_mul_kernel(const __nv_bfloat16* gate, const __nv_bfloat16* up, __nv_bfloat16* out, int64_t nvec) {
+  serving_begin();
+  serving_next();
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= nvec) return;
   const uint4 g4 = reinterpret_cast<const uint4*>(gate)[i], u4 = reinterpret_cast<const uint4*>(up)[i];
@@ -411,7 +414,9 @@ __global__ void silu_mul_kernel(const __nv_bfloat16* __restrict__ gate, const __
   reinterpret_cast<uint4*>(out)[i] = *reinterpret_cast<const uint4*>(o);
 }
 
-__global__ void relu_kernel(__nv_bfloat16* __restrict__ x, int64_t nvec) {
+__global__ void relu_kernel(__nv_bfloat16* x, int64_t nvec) {
+  serving_begin();
+  serving_next();
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= nvec) return;
   uint4 v = reinterpret_cast<uint4*>(x)[i];
@@ -507,14 +512,18 @@ int launch_embedding(const int32_t* tokens, const __nv_bfloat16* embed, const __
   return QZO_OK;
 }
 int launch_add_rmsnorm(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* w2, int pair_rows,
-                       float eps, int T, int d, __nv_bfloat16* y, cudaStream_t st) {
+                       float eps, int T, int d, __nv_bfloat16* y, cudaStream_t st, bool serving) {
   if ((d % 8) || d > kNormVecs * kNormThreads * 8) return QZO_ERR_BAD_ARG;
+  if (serving)
+    return launch_serving(add_norm_kernel<false>, dim3(T), dim3(kNormThreads), 0, 1, st, x, delta, w, nullptr, w2, nullptr, pair_rows, eps, d, y);
   QZO_LAUNCH(add_norm_kernel<false>, dim3(T), dim3(kNormThreads), 0, st, x, delta, w, nullptr, w2, nullptr, pair_rows, eps, d, y);
   return QZO_OK;
 }
 int launch_add_layernorm(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* b, const float* w2,
-                         const float* b2, int pair_rows, float eps, int T, int d, __nv_bfloat16* y, cudaStream_t st) {
+                         const float* b2, int pair_rows, float eps, int T, int d, __nv_bfloat16* y, cudaStream_t st, bool serving) {
   if ((d % 8) || d > kNormVecs * kNormThreads * 8) return QZO_ERR_BAD_ARG;
+  if (serving)
+    return launch_serving(add_norm_kernel<true>, dim3(T), dim3(kNormThreads), 0, 1, st, x, delta, w, b, w2, b2, pair_rows, eps, d, y);
   QZO_LAUNCH(add_norm_kernel<true>, dim3(T), dim3(kNormThreads), 0, st, x, delta, w, b, w2, b2, pair_rows, eps, d, y);
   return QZO_OK;
 }
@@ -552,13 +561,15 @@ int launch_attention(const __nv_bfloat16* q, const __nv_bfloat16* k, const __nv_
   }
   return QZO_OK;
 }
-int launch_silu_mul(const __nv_bfloat16* gate, const __nv_bfloat16* up, __nv_bfloat16* out, int64_t n, cudaStream_t st) {
+int launch_silu_mul(const __nv_bfloat16* gate, const __nv_bfloat16* up, __nv_bfloat16* out, int64_t n, cudaStream_t st, bool serving) {
   if (n % 8) return QZO_ERR_BAD_ARG;
+  if (serving) return launch_serving(silu_mul_kernel, dim3((unsigned)ceil_div64(n / 8, 256)), dim3(256), 0, 1, st, gate, up, out, n / 8);
   QZO_LAUNCH(silu_mul_kernel, dim3((unsigned)ceil_div64(n / 8, 256)), dim3(256), 0, st, gate, up, out, n / 8);
   return QZO_OK;
 }
-int launch_relu(__nv_bfloat16* x, int64_t n, cudaStream_t st) {
+int launch_relu(__nv_bfloat16* x, int64_t n, cudaStream_t st, bool serving) {
   if (n % 8) return QZO_ERR_BAD_ARG;
+  if (serving) return launch_serving(relu_kernel, dim3((unsigned)ceil_div64(n / 8, 256)), dim3(256), 0, 1, st, x, n / 8);
   QZO_LAUNCH(relu_kernel, dim3((unsigned)ceil_div64(n / 8, 256)), dim3(256), 0, st, x, n / 8);
   return QZO_OK;
 }

@@ -11,16 +11,16 @@ int launch_embedding(const int32_t* tokens, const __nv_bfloat16* embed, const __
 // x <- x + delta (skipped when delta is null), then y = norm(x); y may alias delta.  pair_rows > 0: rows from
 // pair_rows on use the gains (and biases) w2 (b2).
 int launch_add_rmsnorm(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* w2, int pair_rows,
-                       float eps, int T, int d, __nv_bfloat16* y, cudaStream_t st);
+                       float eps, int T, int d, __nv_bfloat16* y, cudaStream_t st, bool serving = false);
 int launch_add_layernorm(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* b, const float* w2,
-                         const float* b2, int pair_rows, float eps, int T, int d, __nv_bfloat16* y, cudaStream_t st);
+                         const float* b2, int pair_rows, float eps, int T, int d, __nv_bfloat16* y, cudaStream_t st, bool serving = false);
 int launch_rope_table(float* cs, int max_seq, int dh, float theta, cudaStream_t st);
 int launch_rope(__nv_bfloat16* q, __nv_bfloat16* k, int ldq, int ldk, const float* cs, int T, int S, int H, int dh,
                 cudaStream_t st);
 int launch_attention(const __nv_bfloat16* q, const __nv_bfloat16* k, const __nv_bfloat16* v, int ldq, int ldk, int ldv,
                      __nv_bfloat16* out, int ldo, int B, int S, int H, int dh, cudaStream_t st);
-int launch_silu_mul(const __nv_bfloat16* gate, const __nv_bfloat16* up, __nv_bfloat16* out, int64_t n, cudaStream_t st);
-int launch_relu(__nv_bfloat16* x, int64_t n, cudaStream_t st);
+int launch_silu_mul(const __nv_bfloat16* gate, const __nv_bfloat16* up, __nv_bfloat16* out, int64_t n, cudaStream_t st, bool serving = false);
+int launch_relu(__nv_bfloat16* x, int64_t n, cudaStream_t st, bool serving = false);
 // loss (mean), sum_out and count_out may each be null
 int launch_cross_entropy(const float* logits, const int32_t* labels, int T, int V, float* row_loss, float* loss,
                          float* sum_out, float* count_out, cudaStream_t st);

@@ -207,7 +207,7 @@ int plan_workspace(const qzo_model_desc& d, int max_tokens, WsPlan* p) {
 // vec: position of the gain among the joint mode's vectors (its bias, if any, follows it); sign and
 // pair_rows say which perturbed copy a row takes in joint mode (sign 0: the stored vectors).
 static int add_norm(qzo_model* m, __nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* b, int vec,
-                    int sign, int pair_rows, int T, __nv_bfloat16* out) {
+                    int sign, int pair_rows, int T, __nv_bfloat16* out, bool serving = false) {
   const float *w2 = nullptr, *b2 = nullptr;
   int pr = 0;
   if (m->joint && sign != 0) {
@@ -223,8 +223,8 @@ static int add_norm(qzo_model* m, __nv_bfloat16* x, const __nv_bfloat16* delta, 
     }
   }
   if (m->desc.arch == QZO_ARCH_LLAMA)
-    return launch_add_rmsnorm(x, delta, w, w2, pr, m->desc.norm_eps, T, m->desc.d_model, out, m->stream);
-  return launch_add_layernorm(x, delta, w, b, w2, b2, pr, m->desc.norm_eps, T, m->desc.d_model, out, m->stream);
+    return launch_add_rmsnorm(x, delta, w, w2, pr, m->desc.norm_eps, T, m->desc.d_model, out, m->stream, serving);
+  return launch_add_layernorm(x, delta, w, b, w2, b2, pr, m->desc.norm_eps, T, m->desc.d_model, out, m->stream, serving);
 }
 
 // Up to three block linears that read the same input, in one launch.
@@ -364,7 +364,7 @@ int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, cons
   const __nv_bfloat16* pending = nullptr;
   for (int li = 0; li < d.n_layers; ++li) {
     const Layer& L = m->layers[li];
-    QZO_TRY(add_norm(m, m->x, pending, L.norm1_w, L.norm1_b, 0, 0, 0, R, m->xn));
+    QZO_TRY(add_norm(m, m->x, pending, L.norm1_w, L.norm1_b, 0, 0, 0, R, m->xn, true));
     const Linear* qkv_l[3] = {&L.lin[0], &L.lin[1], &L.lin[2]};
     __nv_bfloat16* qkv_o[3] = {m->qkv, m->qkv + dm, m->qkv + 2 * dm};
     QZO_TRY(decode_linears(m, qkv_l, qkv_o, 3, 3 * dm, m->xn, R));
@@ -376,23 +376,23 @@ int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, cons
     const Linear* o_l[1] = {&L.lin[3]};
     __nv_bfloat16* xn_o[1] = {m->xn};
     QZO_TRY(decode_linears(m, o_l, xn_o, 1, dm, m->att, R));
-    QZO_TRY(add_norm(m, m->x, m->xn, L.norm2_w, L.norm2_b, 0, 0, 0, R, m->xn));
+    QZO_TRY(add_norm(m, m->x, m->xn, L.norm2_w, L.norm2_b, 0, 0, 0, R, m->xn, true));
     if (llama) {
       const Linear* gu_l[2] = {&L.lin[4], &L.lin[5]};
       __nv_bfloat16* gu_o[2] = {m->mlp_a, m->mlp_b};
       QZO_TRY(decode_linears(m, gu_l, gu_o, 2, F, m->xn, R));
-      QZO_TRY(launch_silu_mul(m->mlp_a, m->mlp_b, m->mlp_a, (int64_t)R * F, st));
+      QZO_TRY(launch_silu_mul(m->mlp_a, m->mlp_b, m->mlp_a, (int64_t)R * F, st, true));
     } else {
       const Linear* fc1_l[1] = {&L.lin[4]};
       __nv_bfloat16* fc1_o[1] = {m->mlp_a};
       QZO_TRY(decode_linears(m, fc1_l, fc1_o, 1, F, m->xn, R));
-      QZO_TRY(launch_relu(m->mlp_a, (int64_t)R * F, st));
+      QZO_TRY(launch_relu(m->mlp_a, (int64_t)R * F, st, true));
     }
     const Linear* down_l[1] = {&L.lin[llama ? 6 : 5]};
     QZO_TRY(decode_linears(m, down_l, xn_o, 1, dm, m->mlp_a, R));
     pending = m->xn;
   }
-  QZO_TRY(add_norm(m, m->x, pending, m->final_norm_w, m->final_norm_b, 0, 0, 0, R, m->xn));
+  QZO_TRY(add_norm(m, m->x, pending, m->final_norm_w, m->final_norm_b, 0, 0, 0, R, m->xn, true));
   return launch_bf16_gemm_f32out(m->xn, m->lm_head, d_logits, R, dm, d.vocab, m->status, st);
 }
 

@@ -726,12 +726,12 @@ int run_attention_w(const PagedParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> allowed{0};
     QZO_CUDA_TRY(allow_dynamic_smem(paged_attention_kernel<DH, NT, F8, W>, smem, allowed));
   }
-  return launch_serving<PagedParams>(paged_attention_kernel<DH, NT, F8, W>, grid, dim3(W * 32), smem, 1, st, p);
+  return launch_serving(paged_attention_kernel<DH, NT, F8, W>, grid, dim3(W * 32), smem, 1, st, p);
 }
 
 template <int DH, int COLS, int ROWS>
 int run_join(const PagedParams& p, cudaStream_t st) {
-  return launch_serving<PagedParams>(paged_join_kernel<DH, COLS, ROWS>, dim3((unsigned)((int64_t)p.R * p.H * (DH / 4 / COLS))),
+  return launch_serving(paged_join_kernel<DH, COLS, ROWS>, dim3((unsigned)((int64_t)p.R * p.H * (DH / 4 / COLS))),
                                      dim3(COLS * ROWS), p.splits * sizeof(float), 1, st, p);
 }
 
@@ -774,7 +774,7 @@ int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat
   const bool f8 = c.dtype == QZO_DTYPE_E4M3;
   auto kernel = c.head_dim == 128 ? (f8 ? qk_norm_rope_cache_kernel<128, true> : qk_norm_rope_cache_kernel<128, false>)
                                   : (f8 ? qk_norm_rope_cache_kernel<64, true> : qk_norm_rope_cache_kernel<64, false>);
-  return launch_serving<RopeCacheParams>(kernel, grid, block, 0, 1, st, p);
+  return launch_serving(kernel, grid, block, 0, 1, st, p);
 }
 
 // Workspace for either type of cache: 8-bit keys are split less.

@@ -206,7 +206,7 @@ extern "C" int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int
     static std::atomic<unsigned long long> allowed{0};
     QZO_CUDA_TRY(allow_dynamic_smem(assign_slots_kernel<1>, kMostSmem, allowed));
     const int threads = std::min(kSlotThreads, ceil_div(std::max(B, max_rows), 32) * 32);
-    return launch_serving<SlotParams>(assign_slots_kernel<1>, dim3(1), dim3(threads), smem, 1, (cudaStream_t)stream, p);
+    return launch_serving(assign_slots_kernel<1>, dim3(1), dim3(threads), smem, 1, (cudaStream_t)stream, p);
   }
   // several CTAs for the rows; where lengths or count are replaced in place, a CTA of its own does that behind them
   static std::atomic<unsigned long long> allowed{0};
@@ -214,9 +214,9 @@ extern "C" int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int
   constexpr int kThreads = 512;
   const bool in_place = d_lens_out == d_lens || d_free_count_out == d_free_count;
   if (in_place) p.parts = kRowsAndBlocks;
-  QZO_TRY(launch_serving<SlotParams>(assign_slots_kernel<4>, dim3(std::min(64, ceil_div(max_rows, 4 * kThreads))), dim3(kThreads), smem,
+  QZO_TRY(launch_serving(assign_slots_kernel<4>, dim3(std::min(64, ceil_div(max_rows, 4 * kThreads))), dim3(kThreads), smem,
                                      1, (cudaStream_t)stream, p));
   if (!in_place) return QZO_OK;
   p.parts = kLengths;
-  return launch_serving<SlotParams>(assign_slots_kernel<4>, dim3(1), dim3(kThreads), smem, 1, (cudaStream_t)stream, p);
+  return launch_serving(assign_slots_kernel<4>, dim3(1), dim3(kThreads), smem, 1, (cudaStream_t)stream, p);
 }
