@@ -2,11 +2,11 @@
 //   Y[t][n] = sum_g s[g][n] (sum_{k in group g} X[t][k] q[k][n]) (+ bias[n]).
 // The weights are the bytes that count, and each is used for a few rows only; the contraction runs on warp-level matrix
 // instructions (m16n8k16: one for up to eight rows, two above), because the tensor-memory path of the GEMM costs more per
-// group in hand-offs than the weights take to read (the same linears at 16 rows: 10.8, 18.2, 18.0 and 24.0 us there, 6.0, 12.4,
-// 12.0 and 15.4 us here, for K x N = 4096 x 4096, 4096 x 11008, 11008 x 4096 and 5120 x 13824).
+// group in hand-offs than the weights take to read (the same linears at 16 rows: 10.8, 18.2, 18.0 and 24.0 us there, 5.4, 12.0,
+// 10.5 and 14.5 us here, for K x N = 4096 x 4096, 4096 x 11008, 11008 x 4096 and 5120 x 13824).
 // What bounds it: turning nibbles into bf16 takes three instructions per pair of weights (shift, mask-and-or, subtract), and
-// a warp's work around the 2 KB of a turn as many again, so at one row the ALU pipe is half busy and a warp in six can
-// issue at 3.9 TB/s (8192 x 18944, 20.4 us); the 7B-sized linears are bound by what a launch costs before its first bytes
+// a warp's work around the 2 KB of a turn as many again, so at one row the ALU pipe is half busy at
+// 4.3 TB/s (8192 x 18944, 18.5 us); the 7B-sized linears are bound by what a launch costs before its first bytes
 // arrive and after its last ones (1 x 4096 x 11008: 8.3 us, where a plain read of as many bytes takes 6.2 us); at 16 rows the
 // activations are twice the bytes of the weights in shared memory, which leaves twelve warps on an SM.
 #include "qzo_common.cuh"
@@ -53,7 +53,8 @@ constexpr int kStages = 3;           // of a warp's ring: a group of 128 k of th
 constexpr int kWeightBytes = kRT * 1024, kScaleBytes = kRT * 32;
 
 // XR: rows of activations that a stage holds (1, 4, 8 or 16, at least M); W: warps of a CTA, which share its output features and
-// take the groups of K in turn.
+// take the groups of K in turn.  CTAs begin at different groups, so that they do not all ask the L2 for the same activations
+// at once (16 x 5120 x 13824: 14.5 us, 15.6 if all begin at the first; 1 x 5120 x 13824: 9.8 and 10.1).
 // The weights are the A operand.  A lane's share of a tile is features 2g and 2g + 1 and the 32 k of its quarter t of the
 // group: two neighbouring 16-byte units of the kernel layout; its B fragments are then the 32 consecutive activations
 // of that quarter.
@@ -68,7 +69,6 @@ __global__ void __launch_bounds__(W * 32)
 gemv_w4_kernel(GemvParams p) {
   constexpr int NT = XR > 8 ? 2 : 1;                   // tiles of eight rows
   constexpr int kStageBytes = kWeightBytes + kScaleBytes + 256 * XR;
-  constexpr bool kTurned = XR > 8;
   extern __shared__ __align__(128) uint8_t gemv_smem[];
   const int rank = blockIdx.x, block = blockIdx.y;     // CTA of the cluster, output features
   int j = 0;
@@ -78,7 +78,7 @@ gemv_w4_kernel(GemvParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(gemv_smem) + warp * kStages * kStageBytes;
   const int step = W * (int)gridDim.x, mine = (p.G - 1 - (rank * W + warp) + step) / step;       // groups of this warp
-  const int first = rank * W + warp + (kTurned && mine > 0 ? block % mine * step : 0);
+  const int first = rank * W + warp + (mine > 0 ? block % mine * step : 0);
 
   // what a lane copies of a group: of every quarter the unit of feature `lane`, one unit of scales (columns that do not exist: of
   // ones that do, their outputs are not stored), and unit x_q of every other row of activations
@@ -104,17 +104,13 @@ gemv_w4_kernel(GemvParams p) {
 #pragma unroll
     for (int i = 0; i < (XR + 1) / 2; ++i, x += 2 * (size_t)p.ldx)
       if (x_row + 2 * i < (XR == 1 ? 1 : p.M)) copy16_or_zero(x_dst + at + 512 * i, x, live ? 16 : 0);
-    next += step;
-    int jump = step;
-    if (kTurned) {
-      ++fetched;
-      if (next >= p.G) { next -= mine * step; jump -= mine * step; }
-    }
+    ++fetched;
+    const int jump = next + step < p.G ? step : step - mine * step;    // on to the next group, behind the last one to the first
+    next += jump;
     w_src += (int64_t)jump * (2 * kPackedTileBytes / 16);
     s_src += (int64_t)jump * N;
     x_src += (int64_t)jump * kGroup;
   };
-  auto more = [&] { return kTurned ? fetched < mine : next < p.G; };
   // what it reads: the units of features 2g, 2g + 1 and quarter t of every tile, the activations of quarter t of its rows
   const uint32_t w_lds = ring + 16 * (32 * t + ((2 * g) ^ ((t & 1) + 4 * (t >> 1))));
   const uint32_t w_lds1 = w_lds ^ 16, s_lds = ring + kWeightBytes + 4 * g;
@@ -172,16 +168,16 @@ gemv_w4_kernel(GemvParams p) {
   serving_next();
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) {
-    if (more()) fetch(s * kStageBytes);
+    if (fetched < mine) fetch(s * kStageBytes);
     copies_commit();
   }
-  for (int i = kTurned ? 0 : first; i < (kTurned ? mine : p.G);) {
+  for (int i = 0; i < mine;) {
 #pragma unroll
-    for (int u = 0; u < kStages; ++u, i += kTurned ? 1 : step) {
-      if (i >= (kTurned ? mine : p.G)) break;
+    for (int u = 0; u < kStages; ++u, ++i) {
+      if (i >= mine) break;
       copies_wait<kStages - 2>();
       __syncwarp();                                    // this stage has landed, and every lane is done with the one before it
-      if (more()) fetch((u + kStages - 1) % kStages * kStageBytes);
+      if (fetched < mine) fetch((u + kStages - 1) % kStages * kStageBytes);
       copies_commit();
       contract(u * kStageBytes);
     }
@@ -230,13 +226,13 @@ gemv_w4_kernel(GemvParams p) {
 
 template <int XR, int W>
 int run_gemv(const GemvParams& p, int blocks, cudaStream_t st) {
-  // Few output features: the CTAs of a cluster share the groups of K (measured at K = 11008, N = 256, one row: 9.4 us alone,
-  // 4.2 us with clusters of eight; at K = N = 4096, 128 CTAs of 32 features, 5.5 us alone, 5.9 us with clusters of two).
+  // Few output features: the CTAs of a cluster share the groups of K (measured at K = 11008, N = 256, one row: 7.5 us alone,
+  // 3.5 us with clusters of eight; at K = N = 4096, 128 CTAs of 32 features, 4.4 us alone, 5.0 us with clusters of two).
   int cluster = 1;
   while (cluster < kMaxCluster && 2 * cluster * blocks <= kSMs && 2 * cluster * W <= p.G) cluster *= 2;
   constexpr int kRing = W * kStages * (kWeightBytes + kScaleBytes + 256 * XR), kSums = W * (XR > 8 ? 16 : 8) * (kCols + 1) * (int)sizeof(float);
-  // The CTAs are spread evenly: each asks for so much shared memory that no SM takes more than its share of them (1 x 4096 x
-  // 11008, 344 CTAs: 9.7 us, 11.7 us when an SM could take a fourth one; 1 x 5120 x 13824 11.6 us against 14.5).
+  // The CTAs are spread evenly: each asks for so much shared memory that no SM takes more than its share of them (4096 x
+  // 9472, 296 CTAs: 6.5 us at one row and 9.2 at sixteen; 7.7 and 11.4 where some SMs take three of them and some one).
   const int share = ceil_div(blocks * cluster, kSMs), even = (kSMem / (share + 1) - 1024) / 16 * 16 + 16;
   const int smem = std::max({kRing, kSums, even});
   static std::atomic<unsigned long long> allowed{0};
@@ -264,8 +260,8 @@ int launch_gemv_group(const __nv_bfloat16* d_x, int ldx, int M, int K, const Gem
   if (M <= 4) return run_gemv<4, 8>(p, (int)blocks, st);
   if (M <= 8) return run_gemv<8, 8>(p, (int)blocks, st);
   // Two tiles of rows: the activations take half of a stage, so CTAs of eight warps leave room for two of them on an SM
-  // only, which pays where there is no more than one CTA per SM (measured with 16 rows: K = N = 4096 6.5 us against 8.0 us
-  // with four warps, K = 5120, N = 13824 19.0 us against 16.6 us).
+  // only, which pays where there is no more than one CTA per SM (measured with 16 rows: K = N = 4096 5.4 us against 6.1 us
+  // with four warps, K = 5120, N = 13824 17.2 us against 14.5 us).
   return blocks <= kSMs ? run_gemv<16, 8>(p, (int)blocks, st) : run_gemv<16, 4>(p, (int)blocks, st);
 }
 
