@@ -207,7 +207,7 @@ int qzo_rope_table(float* d_table, int max_pos, int head_dim, float theta, void*
  * d_q_out, k' and v' into the cache at the row's slot; each is rounded once, from fp32.
  * d_q bf16 [T][ldq] with head h at h * head_dim, d_k and d_v alike with n_kv_heads heads; 16-byte aligned, strides
  * multiples of 8; d_q_out bf16 [T][ldqo], may be d_q itself (same stride) but not overlap it otherwise; gains float
- * [head_dim], d_table as qzo_rope_table writes it (16-byte aligned).  d_positions, d_slots int32 [T]; the slots of one call are distinct.
+ * [head_dim], d_table as qzo_rope_table writes it (gains and table 32-byte aligned).  d_positions, d_slots int32 [T]; the slots of one call are distinct.
  * A row with a negative position or slot is padding: nothing is written for it.  A slot beyond the cache or a position
  * beyond the table sets bit 1 of the status word: the first is not written, the second is turned by the table's last. */
 int qzo_qk_norm_rope_cache(const void* d_q_bf16, int ldq, const void* d_k_bf16, int ldk, const void* d_v_bf16, int ldv,

@@ -58,12 +58,25 @@ __device__ __forceinline__ uint32_t pack4_e4m3(const float v[4], float inv) {
 }
 __device__ __forceinline__ uint2 pack8_e4m3(const float v[8], float inv) { return make_uint2(pack4_e4m3(v, inv), pack4_e4m3(v + 4, inv)); }
 
+// Eight consecutive floats, 32-byte aligned, of data that no kernel in flight writes: one load instead of two, which asks the
+// L1 for every line once
+struct Floats8 { float v[8]; };
+__device__ __forceinline__ Floats8 load8(const float* p) {
+  Floats8 r;
+  asm volatile("ld.global.nc.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(r.v[0]), "=f"(r.v[1]), "=f"(r.v[2]), "=f"(r.v[3]), "=f"(r.v[4]), "=f"(r.v[5]), "=f"(r.v[6]), "=f"(r.v[7])
+               : "l"(p));
+  return r;
+}
+
 // DH / 16 lanes per pair of neighbouring heads; a lane holds elements 8 l .. 8 l + 7 of a head's lower half and their
 // partners of the upper half (a 16-byte load each), so a pair of elements is turned inside a lane and the norm's sum takes
 // log2(DH / 16) shuffles.  Two heads to a lane: they share the angles, and twice the bytes are in flight.  A CTA holds whole
 // rows where they are short, part of a row's heads where they are long.
-// Measured: 4096 rows of 32 + 32 heads of 128, bf16: 36.7 us, 5.5 TB/s (HBM); 4099 rows of 32 + 8 heads with norms and e4m3 pages
-// 23.7 us, 4.0 TB/s (issue slots: 560 warp instructions per two heads); one row 1.9 us (a launch and two dependent loads).
+// Measured: 4096 rows of 32 + 32 heads of 128, bf16: 36.4 us, 5.6 TB/s (HBM); 4099 rows of 32 + 8 heads with norms and e4m3 pages
+// 22.5 us, 4.2 TB/s (latency: the angles wait for the position, 66 registers leave 27 warps on an SM, a scheduler issues 0.6
+// instructions a cycle); with 16-byte loads of angles and gains 23.4 us (every line is then asked for two to four times); one row
+// 1.8 us (a launch and two dependent loads).
 constexpr int kRopeThreads = 128, kLaneHeads = 2;
 
 template <int DH, bool F8>
@@ -100,13 +113,13 @@ qk_norm_rope_cache_kernel(RopeCacheParams p) {
     }
   }
   const bool work = slot >= 0 && given >= 0;           // lanes of padding go along for the shuffles only
-  float4 cs[4];                                        // {cos, sin} of two pairs each
+  Floats8 cs[2];                                       // {cos, sin} of four pairs each
   if (p.table && work && first < p.H + p.Hkv) {
     const int pos = min(given, p.max_pos - 1);
     if (pos != given && l == 0 && p.status) atomicOr(p.status, kStatusBadToken);
-    const float4* row = reinterpret_cast<const float4*>(p.table + 2 * ((size_t)pos * (DH / 2) + 8 * l));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) cs[e] = __ldg(row + e);
+    const float* row = p.table + 2 * ((size_t)pos * (DH / 2) + 8 * l);
+    cs[0] = load8(row);
+    cs[1] = load8(row + 8);
   }
   const bool writes = work && slot < p.n_slots;
   if (work && !writes && l == 0 && first == 0 && p.status) atomicOr(p.status, kStatusBadToken);
@@ -137,23 +150,24 @@ qk_norm_rope_cache_kernel(RopeCacheParams p) {
     unpack4(make_uint2(hi_raw[i].x, hi_raw[i].y), hi); unpack4(make_uint2(hi_raw[i].z, hi_raw[i].w), hi + 4);
     const float* gain = is_v ? nullptr : is_q ? p.q_gain : p.k_gain;
     if (gain) {
+      const Floats8 ga = load8(gain + 8 * l), gb = load8(gain + DH / 2 + 8 * l);
+      const float r = root[i];
 #pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        const float4 ga = __ldg(reinterpret_cast<const float4*>(gain + 8 * l + e)), gb = __ldg(reinterpret_cast<const float4*>(gain + DH / 2 + 8 * l + e));
-        const float r = root[i];
-        lo[e] *= r * ga.x; lo[e + 1] *= r * ga.y; lo[e + 2] *= r * ga.z; lo[e + 3] *= r * ga.w;
-        hi[e] *= r * gb.x; hi[e + 1] *= r * gb.y; hi[e + 2] *= r * gb.z; hi[e + 3] *= r * gb.w;
+      for (int e = 0; e < 8; ++e) {
+        lo[e] *= r * ga.v[e];
+        hi[e] *= r * gb.v[e];
       }
     }
     if (!work || hh >= heads) continue;
     if (p.table && !is_v) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
+        const float* c = cs[e >> 1].v + 4 * (e & 1);
         const float x0 = lo[2 * e], y0 = hi[2 * e], x1 = lo[2 * e + 1], y1 = hi[2 * e + 1];
-        lo[2 * e] = x0 * cs[e].x - y0 * cs[e].y;
-        hi[2 * e] = y0 * cs[e].x + x0 * cs[e].y;
-        lo[2 * e + 1] = x1 * cs[e].z - y1 * cs[e].w;
-        hi[2 * e + 1] = y1 * cs[e].z + x1 * cs[e].w;
+        lo[2 * e] = x0 * c[0] - y0 * c[1];
+        hi[2 * e] = y0 * c[0] + x0 * c[1];
+        lo[2 * e + 1] = x1 * c[2] - y1 * c[3];
+        hi[2 * e + 1] = y1 * c[2] + x1 * c[3];
       }
     }
     if (is_q) {
@@ -832,7 +846,7 @@ int qzo_qk_norm_rope_cache(const void* d_q_bf16, int ldq, const void* d_k_bf16, 
   const int64_t wq = (int64_t)n_heads * cache->head_dim, wk = (int64_t)cache->n_kv_heads * cache->head_dim;
   if (ldq < wq || ldqo < wq || ldk < wk || ldv < wk || (ldq % 8) || (ldk % 8) || (ldv % 8) || (ldqo % 8)) return QZO_ERR_BAD_ARG;
   if (((uintptr_t)d_q_bf16 | (uintptr_t)d_k_bf16 | (uintptr_t)d_v_bf16 | (uintptr_t)d_q_out_bf16) & 15) return QZO_ERR_BAD_ARG;
-  if (((uintptr_t)d_q_gain | (uintptr_t)d_k_gain | (uintptr_t)d_table) & 15) return QZO_ERR_BAD_ARG;
+  if (((uintptr_t)d_q_gain | (uintptr_t)d_k_gain | (uintptr_t)d_table) & 31) return QZO_ERR_BAD_ARG;
   if (d_q_out_bf16 == d_q_bf16 && ldq != ldqo) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_device());
   return launch_qk_norm_rope_cache((const __nv_bfloat16*)d_q_bf16, ldq, (const __nv_bfloat16*)d_k_bf16, ldk,

@@ -155,6 +155,13 @@ def test_index_arrays_off_their_boundary_are_refused():
         _refused(call, {}, [{n: ODD} for n in names])
 
 
+def test_gains_and_angles_off_their_32_bytes_are_refused():
+    cache, half = _cache(), ctypes.c_void_p(0x10010)
+    def rope(qg=P, kg=P, tab=P):
+        return _lib()._lib.qzo_qk_norm_rope_cache(P, 256, P, 128, P, 128, qg, kg, 1e-5, tab, 64, P, P, P, 256, ctypes.byref(cache), 3, 4, NONE, None)
+    _refused(rope, {}, [dict(qg=half), dict(kg=half), dict(tab=half)])
+
+
 def test_scales_whose_reciprocal_or_product_leaves_fp32_are_refused():
     qzo = _lib()
     def rope(cache):
