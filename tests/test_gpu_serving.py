@@ -557,3 +557,47 @@ def test_tensors_off_the_current_device_or_of_another_shape_are_refused(lib):
         lib.qzo_paged_attention(_randn((1, 2, 64), 1).cuda(), cache, table, pos.long())
     with pytest.raises(AssertionError):
         lib.qzo_paged_attention(_randn((1, 64, 2), 1).cuda().transpose(1, 2), cache, table, pos)
+
+
+def test_captured_behind_copies_and_behind_another_stream(lib):
+    # the kernel in front of a captured call may be no kernel at all (a copy of device memory), or run on another stream
+    M, K, N, H, dh, block = 3, 512, 512, 4, 128, 16
+    x, qw, s, wq = _gemv_case(lib, M, K, N, 31)
+    s = s.cuda()
+    ck, cv, ks, vs = _pages("bf16", (8, H, block, dh), 32)
+    cache = lib.KvCache(ck, cv, ks, vs)
+    table = torch.arange(6, dtype=torch.int32, device="cuda").view(M, 2)
+    given = torch.empty((M, K), dtype=torch.bfloat16, device="cuda")
+    at, pos = torch.empty((M, K), dtype=torch.bfloat16, device="cuda"), torch.empty(M, dtype=torch.int32, device="cuda")
+    pos_given = torch.empty(M, dtype=torch.int32, device="cuda")
+    y, out, z = (torch.empty((M, N), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def run(main, second):
+        at.copy_(given)                                        # a copy, then a kernel
+        lib.qzo_gemv_int4(at, wq, s, K, N, y=y)
+        second.wait_stream(main)
+        with torch.cuda.stream(second):
+            pos.copy_(pos_given)
+            lib.qzo_gemv_int4(y, wq, s, K, N, y=z)
+        main.wait_stream(second)
+        lib.qzo_paged_attention(z.view(M, H, dh), cache, table, pos, out=out.view(M, H, dh))
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        given.zero_(), pos_given.zero_()
+        run(side, other)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            run(side, other)
+    for seed in range(3):
+        fresh, last = _randn((M, K), 40 + seed, 0.1).cuda(), torch.tensor([seed, 9 + seed, 29 + seed], dtype=torch.int32, device="cuda")
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.default_stream())
+            given.copy_(fresh), pos_given.copy_(last)
+            graph.replay()
+        torch.cuda.synchronize()
+        first = lib.qzo_gemv_int4(fresh, wq, s, K, N)
+        second = lib.qzo_gemv_int4(first, wq, s, K, N)
+        want = lib.qzo_paged_attention(second.view(M, H, dh), cache, table, last).view(M, N)
+        assert torch.equal(y, first) and torch.equal(z, second) and torch.equal(out, want)
