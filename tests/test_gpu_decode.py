@@ -78,6 +78,40 @@ def test_decode_follows_the_oracle(name, block, dtype, tol):
     gm.close()
 
 
+@pytest.mark.parametrize("name,block", [("tiny", 16), ("tiny_opt", 64), ("tiny_dh128", 32)])
+def test_decode_over_8_bit_pages(monkeypatch, name, block):
+    # the oracle attends to the keys and values that stand in the pages, and these are its own within half a step of their
+    # type (2^-4 of the value, 2^-10 of the scale where steps no longer shrink) and what the linears before may differ by
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg(name)
+    raw = inputs.raw_model_tensors(cfg, seed=1000)
+    gm = qzo.build_model_from_raw(raw, 256)
+    om = build_oracle_model(raw)
+    rng = np.random.default_rng(11)
+    srv = Server(qzo, gm, cfg, B=2, block=block, n_blocks=2 * -(-cfg["max_seq"] // block), dtype=torch.float8_e4m3fn)
+    take = lambda n: rng.integers(0, cfg["vocab"], n).tolist()  # noqa: E731
+    plain, calls = omodel.causal_attention, []
+
+    def over_pages(q, k, v):
+        cache, r = srv.caches[len(calls) % cfg["n_layers"]], calls.append(0) or srv.asked
+        S = k.shape[1]
+        at = np.arange(S)
+        page = srv.table.cpu().numpy()[r][at // block]
+        held = [(t.float().cpu().numpy().astype(np.float64) * c)[page, :, at % block][None] for t, c in ((cache.k, cache.k_scale), (cache.v, cache.v_scale))]
+        for got, want, scale in zip(held, (k, v), (cache.k_scale, cache.v_scale)):
+            assert (np.abs(got - want) <= 2.0 ** -4 * np.abs(want) + scale * 2.0 ** -10 + TOL * (1 + 2.0 ** -3) * np.abs(want).max()).all()
+        return plain(q, *held)
+
+    monkeypatch.setattr(omodel, "causal_attention", over_pages)
+    for new, rows in (({0: take(5)}, 8), ({0: take(1), 1: take(40)}, 48), ({0: take(1), 1: take(1)}, 2), ({0: None, 1: take(1)}, 4), ({0: take(9), 1: take(1)}, 12)):
+        for r, p, got in srv.step(new, rows):
+            srv.asked = r
+            want = _logits(om, srv.text[r][:p + 1])[-1]
+            assert np.abs(got - want).max() <= TOL * np.abs(want).max(), (r, p)
+    assert len(calls) % cfg["n_layers"] == 0
+    gm.close()
+
+
 def test_long_context_in_a_small_workspace():
     # a prompt of several steps; the workspace holds fewer splits of the cache than the attention would take
     from paper_2505_13430_b200 import qzo

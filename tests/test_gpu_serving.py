@@ -601,3 +601,27 @@ def test_captured_behind_copies_and_behind_another_stream(lib):
         second = lib.qzo_gemv_int4(first, wq, s, K, N)
         want = lib.qzo_paged_attention(second.view(M, H, dh), cache, table, last).view(M, N)
         assert torch.equal(y, first) and torch.equal(z, second) and torch.equal(out, want)
+
+
+def test_calls_on_two_streams_at_once(lib):
+    # the same caches and weights read from two streams, a workspace each: what one stream gives alone
+    positions = [6000, 4097]
+    q, ck, cv, ks, vs, table = _attend_case(positions, 8, 2, 128, 16, "bf16", 0, 51)
+    cache, table, pos = lib.KvCache(ck, cv, ks, vs), torch.from_numpy(table).cuda(), torch.tensor(positions, dtype=torch.int32, device="cuda")
+    x, _, s, wq = _gemv_case(lib, 9, 2048, 4096, 52)
+    x, s = x.cuda(), s.cuda()
+    need = lib.qzo_paged_attention_workspace_bytes(2, 8, 2, 128, table.shape[1] * 16)
+    assert need > 0
+    queries = [q.cuda(), _randn((2, 8, 128), 53).cuda()]
+    want = [(lib.qzo_paged_attention(a, cache, table, pos), lib.qzo_gemv_int4(x[i:i + 8], wq, s, 2048, 4096)) for i, a in enumerate(queries)]
+    streams, spaces = [torch.cuda.Stream() for _ in queries], [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in queries]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, a in enumerate(queries):
+            with torch.cuda.stream(streams[i]):
+                got[i].append((lib.qzo_paged_attention(a, cache, table, pos, workspace=spaces[i]), lib.qzo_gemv_int4(x[i:i + 8], wq, s, 2048, 4096)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for pair in got[i]:
+            assert torch.equal(pair[0], want[i][0]) and torch.equal(pair[1], want[i][1])
