@@ -636,7 +636,7 @@ paged_attention_kernel(PagedParams p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) val[e] = fmaf(c, sm_o[w][h][d + e], val[e]);
     }
-    if (p.splits == 1) {
+    if (len <= per) {                                  // one split: nothing to join
       const float f = inverse_sum(p, sum);
 #pragma unroll
       for (int e = 0; e < 4; ++e) val[e] *= f;
@@ -664,8 +664,8 @@ paged_join_kernel(PagedParams p) {
   const int row = (int)(item / p.H), h = (int)(item % p.H);
   int seq = 0;
   const int len = row_keys(p, row, &seq, false);
-  if (len == 0) return;                                // the first split wrote the zeros
   const int per = split_keys(p, len), n = (len + per - 1) / per;
+  if (n <= 1) return;                                  // written already
   const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + item * p.splits;
   float mx = -INFINITY;
   for (int s = threadIdx.x; s < n; s += kThreads) mx = fmaxf(mx, ml[s].x);
