@@ -50,13 +50,14 @@ __device__ __forceinline__ float block_max(float v, float* red) {
 // index pert.base + tok * d + j; rows from pert.pair_rows on (the second copy of a paired step) take -eps.
 struct EmbedPerturb { unsigned long long seed, base; float sign_eps; int pair_rows; };
 
-// positions (may be null): the row's position, of S learned ones, instead of t % S; a negative one marks a row of
-// padding, whose token is not looked at; one beyond S - 1 is reported like a bad token.
+// positions (may be null, slots then too): the row's position, of S learned ones, instead of t % S; a row with a negative
+// position or slot is padding, whose token is not looked at; a position beyond S - 1 is reported like a bad token.
 __global__ void embedding_kernel(const int32_t* __restrict__ tokens, const __nv_bfloat16* __restrict__ embed,
-                                 const __nv_bfloat16* __restrict__ pos, const int32_t* __restrict__ positions, int S, int d,
-                                 int vocab, __nv_bfloat16* __restrict__ x, int* __restrict__ status, EmbedPerturb pert) {
+                                 const __nv_bfloat16* __restrict__ pos, const int32_t* __restrict__ positions,
+                                 const int32_t* __restrict__ slots, int S, int d, int vocab, __nv_bfloat16* __restrict__ x,
+                                 int* __restrict__ status, EmbedPerturb pert) {
   const int t = blockIdx.x;
-  int at = positions ? positions[t] : t % S;
+  int at = positions ? min(positions[t], slots[t] < 0 ? -1 : INT32_MAX) : t % S;
   int tok = at < 0 ? 0 : tokens[t];
   if (at >= S && threadIdx.x == 0 && status != nullptr) atomicOr(status, kStatusBadToken);
   at = min(max(at, 0), S - 1);
@@ -505,10 +506,10 @@ __global__ void set_step_params_kernel(StepParams* __restrict__ dst, StepParams 
 
 int launch_embedding(const int32_t* tokens, const __nv_bfloat16* embed, const __nv_bfloat16* pos, int T, int S, int d,
                      int vocab, __nv_bfloat16* x, int* status, uint64_t seed, uint64_t index_base, float sign_eps,
-                     int pair_rows, cudaStream_t st, const int32_t* positions) {
+                     int pair_rows, cudaStream_t st, const int32_t* positions, const int32_t* slots) {
   if ((d % 8) || (index_base % 4)) return QZO_ERR_BAD_ARG;
   const EmbedPerturb pert{seed, index_base, sign_eps, pair_rows};
-  QZO_LAUNCH(embedding_kernel, dim3(T), dim3(128), 0, st, tokens, embed, pos, positions, S, d, vocab, x, status, pert);
+  QZO_LAUNCH(embedding_kernel, dim3(T), dim3(128), 0, st, tokens, embed, pos, positions, slots, S, d, vocab, x, status, pert);
   return QZO_OK;
 }
 int launch_add_rmsnorm(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* w2, int pair_rows,

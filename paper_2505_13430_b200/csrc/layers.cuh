@@ -3,11 +3,11 @@
 #include "qzo_common.cuh"
 
 namespace qzo {
-// positions (may be null): each row's position instead of t % S, negative for padding
+// positions, slots (both null or neither): each row's position instead of t % S; a negative position or slot is padding
 // sign_eps != 0: rows are perturbed as E + sign_eps z(seed, index_base + tok d + j); rows from pair_rows on take -sign_eps
 int launch_embedding(const int32_t* tokens, const __nv_bfloat16* embed, const __nv_bfloat16* pos, int T, int S, int d,
                      int vocab, __nv_bfloat16* x, int* status, uint64_t seed, uint64_t index_base, float sign_eps,
-                     int pair_rows, cudaStream_t st, const int32_t* positions = nullptr);
+                     int pair_rows, cudaStream_t st, const int32_t* positions = nullptr, const int32_t* slots = nullptr);
 // x <- x + delta (skipped when delta is null), then y = norm(x); y may alias delta.  pair_rows > 0: rows from
 // pair_rows on use the gains (and biases) w2 (b2).
 int launch_add_rmsnorm(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* w2, int pair_rows,
@@ -69,8 +69,9 @@ int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat
                               const int32_t* positions, const int32_t* slots, __nv_bfloat16* q_out, int ldqo,
                               const qzo_kv_cache& c, int T, int H, int* status, cudaStream_t st);
 size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len);
+// slots (may be null): rows with a negative slot are padding, as those with a negative position are
 // fewer_splits: a workspace that is too small for the splits of paged_attention_bytes gets as many as it holds
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
-                           const int32_t* row_seq, const int32_t* positions, float scale, __nv_bfloat16* out, int ldo, int R,
-                           int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st);
+                           const int32_t* row_seq, const int32_t* positions, const int32_t* slots, float scale, __nv_bfloat16* out,
+                           int ldo, int R, int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st);
 }  // namespace qzo

@@ -360,7 +360,7 @@ int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, cons
   const size_t ws_bytes = (size_t)2 * m->max_tokens * d.vocab * sizeof(float);
   m->last_T = 0;
   QZO_TRY(launch_embedding(tokens, m->embed, llama ? nullptr : m->pos_embed, R, d.max_seq, dm, d.vocab, m->x, m->status, 0, 0,
-                           0.0f, 0, st, positions));
+                           0.0f, 0, st, positions, slots));
   const __nv_bfloat16* pending = nullptr;
   for (int li = 0; li < d.n_layers; ++li) {
     const Layer& L = m->layers[li];
@@ -371,7 +371,7 @@ int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, cons
     QZO_TRY(launch_qk_norm_rope_cache(m->qkv, 3 * dm, m->qkv + dm, 3 * dm, m->qkv + 2 * dm, 3 * dm, nullptr, nullptr, 0.0f,
                                       llama ? m->rope_cs : nullptr, d.max_seq, positions, slots, m->qkv, 3 * dm, caches[li], R, H,
                                       m->status, st));
-    QZO_TRY(launch_paged_attention(m->qkv, 3 * dm, caches[li], table, n_seqs, width, row_seq, positions, scale, m->att, dm, R, H,
+    QZO_TRY(launch_paged_attention(m->qkv, 3 * dm, caches[li], table, n_seqs, width, row_seq, positions, slots, scale, m->att, dm, R, H,
                                    m->logits, ws_bytes, true, m->status, st));
     const Linear* o_l[1] = {&L.lin[3]};
     __nv_bfloat16* xn_o[1] = {m->xn};

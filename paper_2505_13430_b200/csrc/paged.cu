@@ -205,7 +205,7 @@ struct PagedParams {
   const void *ck, *cv;
   const int32_t* table;
   int n_seqs, width;
-  const int32_t *row_seq, *positions;
+  const int32_t *row_seq, *positions, *slots;          // slots may be null
   float scale_log2e, v_scale;                          // the keys' scale is in the first
   __nv_bfloat16* out;
   int ldo, R, H, Hkv, G, chunks, splits, min_keys, round_keys, n_blocks, log2_block;
@@ -220,7 +220,7 @@ __device__ __forceinline__ int split_keys(const PagedParams& p, int len) {
 // Number of keys a row sees, 0 for padding; seq receives its request.  One thread reports what is out of range.
 __device__ __forceinline__ int row_keys(const PagedParams& p, int row, int* seq, bool report) {
   const int pos = p.positions[row], s = p.row_seq ? p.row_seq[row] : row;
-  if (pos < 0) return 0;
+  if (pos < 0 || (p.slots && p.slots[row] < 0)) return 0;
   *seq = s;
   const int most = p.width << p.log2_block;
   const bool bad_seq = s < 0 || s >= p.n_seqs;
@@ -798,8 +798,8 @@ size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
 }
 
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
-                           const int32_t* row_seq, const int32_t* positions, float scale, __nv_bfloat16* out, int ldo, int R,
-                           int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st) {
+                           const int32_t* row_seq, const int32_t* positions, const int32_t* slots, float scale, __nv_bfloat16* out,
+                           int ldo, int R, int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st) {
   const int G = H / c.n_kv_heads, chunks = head_chunks(G), max_len = width * c.block_size;
   if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
   const int subs = 256 / (c.head_dim * (c.dtype == QZO_DTYPE_E4M3 ? 1 : 2));
@@ -810,7 +810,7 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
     splits = (int)std::max<size_t>(1, std::min<size_t>(splits, ws_bytes / per_split));
   else if (const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
     if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
-  PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
+  PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, slots, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
                 R, H, c.n_kv_heads, G, chunks, splits, plan.min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
   if (splits > 1) {
     p.part_o = (float*)ws;
@@ -874,7 +874,7 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
   if (((uintptr_t)d_q_bf16 & 15) || ((uintptr_t)d_out_bf16 & 15)) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_device());
   return launch_paged_attention((const __nv_bfloat16*)d_q_bf16, ldq, *cache, d_block_table, n_seqs, table_width, d_row_seq, d_positions,
-                                scale, (__nv_bfloat16*)d_out_bf16, ldo, R, n_heads, d_workspace, workspace_bytes, false,
+                                nullptr, scale, (__nv_bfloat16*)d_out_bf16, ldo, R, n_heads, d_workspace, workspace_bytes, false,
                                 d_status, (cudaStream_t)stream);
 }
 

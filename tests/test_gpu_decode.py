@@ -263,3 +263,32 @@ def test_decode_refusals_and_reports():
         gm.qzo_debug_set_status(0)
     assert gm.qzo_device_status() == 0
     gm.close()
+
+
+@pytest.mark.parametrize("name", ["tiny", "tiny_opt"])
+@pytest.mark.parametrize("rows", [8, 24])
+def test_rows_without_a_slot_are_padding_whatever_else_they_hold(name, rows):
+    # slot -1 beside a position, a token, a request and a block table that nothing can look up: as position and slot -1
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg(name)
+    gm = qzo.build_model_from_raw(inputs.raw_model_tensors(cfg, seed=1000), 64)
+    results = []
+    for junk in (False, True):
+        srv = Server(qzo, gm, cfg, 2, 16, 6)
+        live = [0, 2, 3, 5]
+        i32 = dict(dtype=torch.int32, device="cuda")
+        table = torch.full((3, 4), -1, **i32)
+        table[0, 0], table[1, 0] = 5, 2
+        tokens, seq, pos, slots = (torch.full((rows,), v, **i32) for v in (-12345, -1, -1, -1))
+        if junk:
+            seq[1::2], seq[4::4], pos[:] = 2, 77, torch.arange(rows, **i32) * 7
+            pos[rows - 1], slots[rows - 2] = 10 ** 6, -2 ** 31
+        for t, (s, p) in zip(live, ((0, 0), (0, 1), (1, 0), (0, 2))):
+            tokens[t], seq[t], pos[t], slots[t] = 3 + t, s, p, int(table[s, 0]) * 16 + p
+        logits = gm.qzo_decode(srv.caches, tokens, seq, pos, slots, table)
+        assert gm.qzo_device_status() == 0
+        results.append([logits[live].clone()] + [c.view(torch.int16).clone() for kv in srv.caches for c in (kv.k, kv.v)])
+    assert torch.isfinite(results[0][0]).all()
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    gm.close()
