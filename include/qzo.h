@@ -387,7 +387,7 @@ int qzo_step_host(qzo_model* m, const int32_t* h_tokens, const int32_t* h_labels
  * h_caches: HOST array of n_layers cache descriptions (n_kv_heads = n_heads of the model, one block_size); d_tokens, d_row_seq,
  * d_positions, d_slots int32 [R], as qzo_assign_slots writes the last three; R <= max_tokens; positions < max_seq.
  * Rows of padding (negative position or slot) give logits that mean nothing and touch no cache.  An index out of range
- * (token, position, slot, block) sets bit 1 of the model's status word (qzo_device_status).
+ * (token, position, slot, block) sets bit 1 of what qzo_device_status reads; training steps go on as if it had not been met.
  * Up to QZO_GEMV_MAX_ROWS rows the linears run as qzo_gemv_int4, above as qzo_perturbed_gemm with sign 0.  Asynchronous on the model's
  * stream, and nothing but launches: a model whose stream is not the legacy default one can have its steps captured. */
 int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
@@ -431,13 +431,13 @@ int qzo_debug_gemm_wait_expiry(const void* d_x_bf16, const void* d_wq, const voi
                                int M, int K, int N, int skip_group, int64_t wait_limit_cycles, int* d_status,
                                void* stream);
 
-/* Reads the device status word: bit 0 = a bounded device-side wait expired in some launch since init
+/* Reads the device status: bit 0 = a bounded device-side wait expired in some launch since init
  * (returns QZO_ERR_DEVICE_TIMEOUT), bit 1 = a token id outside [0, vocab) was seen, or in qzo_decode another index
- * out of range (QZO_ERR_BAD_ARG);
- * 0 = nothing to report.  Synchronises. */
+ * out of range (QZO_ERR_BAD_ARG); 0 = nothing to report.  What qzo_decode reports of indices stands in a word of its own,
+ * which is read here with the training's but keeps no step from updating.  Synchronises. */
 int qzo_device_status(qzo_model* m, int* h_status);
-/* Overwrites the status word from the host (0 clears it).  For tests of the error path of a step and
- * for clearing the word after the caller has dealt with a report.  Synchronises. */
+/* Overwrites the training's status word from the host and clears qzo_decode's (0 clears both).  For tests of the error path
+ * of a step and for clearing the words after the caller has dealt with a report.  Synchronises. */
 int qzo_debug_set_status(qzo_model* m, int value);
 
 /* Per-GEMM timing: with max_launches > 0 every later perturbed-GEMM launch of this model (up to

@@ -120,7 +120,8 @@ struct qzo_model {
   int32_t *tok_dev = nullptr, *lab_dev = nullptr;
   void* gemm_ws = nullptr;
   size_t gemm_ws_bytes = 0;
-  int* status = nullptr;
+  int* status = nullptr;        // what launches report: a step's update is left out while it is not 0
+  int* answer_status = nullptr; // indices out of range that decode steps met: status[1], which training does not look at
   int capture_layer = -1;
   int last_T = 0;
   // joint mode (plain SPSA on the un-quantised tensors), off unless qzo_enable_joint_spsa was called
@@ -359,7 +360,7 @@ int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, cons
   // the logits of the training forwards are not needed here: their buffer holds the attention's partial results
   const size_t ws_bytes = (size_t)2 * m->max_tokens * d.vocab * sizeof(float);
   m->last_T = 0;
-  QZO_TRY(launch_embedding(tokens, m->embed, llama ? nullptr : m->pos_embed, R, d.max_seq, dm, d.vocab, m->x, m->status, 0, 0,
+  QZO_TRY(launch_embedding(tokens, m->embed, llama ? nullptr : m->pos_embed, R, d.max_seq, dm, d.vocab, m->x, m->answer_status, 0, 0,
                            0.0f, 0, st, positions, slots));
   const __nv_bfloat16* pending = nullptr;
   for (int li = 0; li < d.n_layers; ++li) {
@@ -370,9 +371,9 @@ int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, cons
     QZO_TRY(decode_linears(m, qkv_l, qkv_o, 3, 3 * dm, m->xn, R));
     QZO_TRY(launch_qk_norm_rope_cache(m->qkv, 3 * dm, m->qkv + dm, 3 * dm, m->qkv + 2 * dm, 3 * dm, nullptr, nullptr, 0.0f,
                                       llama ? m->rope_cs : nullptr, d.max_seq, positions, slots, m->qkv, 3 * dm, caches[li], R, H,
-                                      m->status, st));
+                                      m->answer_status, st));
     QZO_TRY(launch_paged_attention(m->qkv, 3 * dm, caches[li], table, n_seqs, width, row_seq, positions, slots, scale, m->att, dm, R, H,
-                                   m->logits, ws_bytes, true, m->status, st));
+                                   m->logits, ws_bytes, true, m->answer_status, st));
     const Linear* o_l[1] = {&L.lin[3]};
     __nv_bfloat16* xn_o[1] = {m->xn};
     QZO_TRY(decode_linears(m, o_l, xn_o, 1, dm, m->att, R));
@@ -821,6 +822,7 @@ int qzo_init_model(const qzo_model_desc* desc, const qzo_tensor* tensors, int n_
   m->sums = scal + 4;         // [4..7]
   m->out7 = scal + 8;         // [8..14]
   m->status = (int*)(scal + 32);
+  m->answer_status = m->status + 1;
   m->sp_dev = reinterpret_cast<StepParams*>(scal + 40);
   m->rope_cs = (float*)(ws + p.off_rope);
   m->tok_dev = (int32_t*)(ws + p.off_tok);
@@ -1071,7 +1073,8 @@ int qzo_debug_set_status(qzo_model* m, int value) {
   if (!m || value < 0) return QZO_ERR_BAD_ARG;
   // a host-side write of the word the kernels report through: lets a test walk the error path of a
   // step without making any device-side wait expire
-  QZO_CUDA_TRY(cudaMemcpyAsync(m->status, &value, sizeof(int), cudaMemcpyHostToDevice, m->stream));
+  const int words[2] = {value, 0};
+  QZO_CUDA_TRY(cudaMemcpyAsync(m->status, words, sizeof(words), cudaMemcpyHostToDevice, m->stream));
   QZO_CUDA_TRY(cudaStreamSynchronize(m->stream));
   return QZO_OK;
 }
@@ -1101,8 +1104,10 @@ int qzo_debug_layer_output(qzo_model* m, int layer, int which, void* d_out, size
 
 int qzo_device_status(qzo_model* m, int* h_status) {
   if (!m || !h_status) return QZO_ERR_BAD_ARG;
-  QZO_CUDA_TRY(cudaMemcpyAsync(h_status, m->status, sizeof(int), cudaMemcpyDeviceToHost, m->stream));
+  int words[2];
+  QZO_CUDA_TRY(cudaMemcpyAsync(words, m->status, sizeof(words), cudaMemcpyDeviceToHost, m->stream));
   QZO_CUDA_TRY(cudaStreamSynchronize(m->stream));
+  *h_status = words[0] | words[1];
   if (*h_status & kStatusTimeout) return QZO_ERR_DEVICE_TIMEOUT;
   return (*h_status & kStatusBadToken) ? QZO_ERR_BAD_ARG : QZO_OK;
 }

@@ -292,3 +292,31 @@ def test_rows_without_a_slot_are_padding_whatever_else_they_hold(name, rows):
     for a, b in zip(*results):
         assert torch.equal(a, b)
     gm.close()
+
+
+def test_training_goes_on_after_a_decode_that_met_a_bad_index():
+    # what a decode reports is said by the status word until it is cleared; training steps give what they give without it
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg("tiny")
+    raw = inputs.raw_model_tensors(cfg, seed=1000)
+    tok, lab = inputs.tokens_and_labels(cfg, 2, 32, seed=9)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    zero = torch.zeros(1, **i32)
+    outs = []
+    for bad in (False, True):
+        gm = qzo.build_model_from_raw(raw, 256)
+        steps = [gm.qzo_step(tok.cuda(), lab.cuda(), 5, 1e-3, 1e-3, 100.0)]
+        before = gm.scales.clone()
+        if bad:
+            srv = Server(qzo, gm, cfg, 1, 16, 4)
+            for tokens, pos, slot, block in ((cfg["vocab"], 0, 0, 0), (0, cfg["max_seq"], 0, 0), (0, 0, 64, 0), (0, 0, 0, 4)):
+                gm.qzo_decode(srv.caches, zero + tokens, zero, zero + pos, zero + slot, torch.full((1, 4), block, **i32))
+                assert gm.qzo_device_status() == 2
+        steps += [gm.qzo_step(tok.cuda(), lab.cuda(), 6 + i, 1e-3, 1e-3, 100.0) for i in range(2)]     # the second is replayed
+        assert not torch.equal(gm.scales, before)
+        assert gm.qzo_device_status() == (2 if bad else 0)
+        gm.qzo_debug_set_status(0)
+        assert gm.qzo_device_status() == 0
+        outs.append((steps, gm.scales.clone()))
+        gm.close()
+    assert outs[0][0] == outs[1][0] and torch.equal(outs[0][1], outs[1][1])
