@@ -336,9 +336,18 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
 // What scores are taken relative to: their maximum, or 0 where there is none (all -inf).
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 
+// A weight is 2^d, d = score - (maximum so far) + lift().  The maximum is only raised when a score passes it by 2^kSlack: until
+// then a tile needs neither the maximum over its keys nor a rescaling, and weights that reach 2^8 cost no precision.  Where weights
+// become fp16 they are lifted, and those below 2^-14, where fp16 has no more relative steps, are raised by 2^kBoost for a product of
+// their own.
+constexpr float kSlack = 8.0f;
+template <bool F8> __device__ constexpr float lift() { return F8 ? 6.0f : 0.0f; }
+constexpr float kMostD8 = 14.0f;                       // 8-bit pages: |d| within which a tile needs nothing of its own
+constexpr float kBoost = 29.0f, kUnboost = 0x1p-29f;
+
 // Stages of a ring and CTAs of four warps on an SM, for NT tiles of eight heads: three CTAs with two stages each where their
 // registers allow it, two with three stages otherwise (64 rows to 4096 in e4m3: 55.3 us against 58.3 with two CTAs; 16 rows of
-// 8192 keys, 24 heads on one: 13.9 us against 17.2 with three).
+// 8192 keys, 24 heads on one: 14.3 us, with three 17.2 when two took 13.9).
 __host__ __device__ constexpr int resident_ctas(int NT) { return NT == 1 ? 3 : 2; }
 __host__ __device__ constexpr int ring_stages(int NT) { return NT == 1 ? 2 : 3; }
 
@@ -424,10 +433,12 @@ paged_attention_kernel(PagedParams p) {
   }
 
   float o[NT][DH / 16][4];
-  float m[NT][2], l[NT][2];
+  float m[NT][2], l[NT][2], ref[NT][2];                // maximum so far, sum of weights, what is taken off a score
+  bool fresh = true;                                   // no maximum yet for some of the heads
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     m[nt][0] = m[nt][1] = -INFINITY;
+    ref[nt][0] = ref[nt][1] = -lift<F8>();
     l[nt][0] = l[nt][1] = 0.0f;
 #pragma unroll
     for (int u = 0; u < DH / 16; ++u) o[nt][u][0] = o[nt][u][1] = o[nt][u][2] = o[nt][u][3] = 0.0f;
@@ -508,25 +519,53 @@ paged_attention_kernel(PagedParams p) {
           mma_step<F8>(sc[nt][i], ka[w], kb[w], ka[w + 1], kb[w + 1], qf[nt][w], qf[nt][w + 1]);
       }
     }
-    // The running maximum is only raised when a score passes it by 2^kSlack: until then the weights are at most
-    // 2^kSlack, which costs no precision, and a tile needs neither the maximum over its keys nor a rescaling.
-    constexpr float kSlack = 8.0f;
-    bool raise = false;
+    bool odd = fresh;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float f0 = F8 ? p.scale_log2e * unscale[nt][0] : p.scale_log2e, f1 = F8 ? p.scale_log2e * unscale[nt][1] : p.scale_log2e;
+      float most = 0.0f;
 #pragma unroll
       for (int i = 0; i < S; ++i) {
         float (&s)[4] = sc[nt][i];
-        s[0] *= f0; s[1] *= f1; s[2] *= f0; s[3] *= f1;
-        if (!full) {
+        s[0] = fmaf(s[0], f0, -ref[nt][0]); s[1] = fmaf(s[1], f1, -ref[nt][1]);
+        s[2] = fmaf(s[2], f0, -ref[nt][0]); s[3] = fmaf(s[3], f1, -ref[nt][1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = fmaxf(most, F8 ? fabsf(s[e]) : s[e]);
+        if (!full) {                                   // rows of zeros behind the last key: they may make a tile odd, no more
           if (g >= n_keys[i]) s[0] = s[1] = -INFINITY;
           if (g + 8 >= n_keys[i]) s[2] = s[3] = -INFINITY;
         }
-        raise = raise || fmaxf(s[0], s[2]) > m[nt][0] + kSlack || fmaxf(s[1], s[3]) > m[nt][1] + kSlack;
       }
+      odd = odd || most > (F8 ? kMostD8 : kSlack);
     }
-    if (__any_sync(0xffffffffu, raise)) {
+    // the tile's weights, as they enter the product with the values, and that product
+    constexpr int kParts = F8 ? 1 : 2;
+    uint32_t pb[kParts][NT][S][2];
+    auto add_values = [&]() {
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        ValRaw<DH, F8> vraw[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          read_val<DH, F8>(stage + kStageBytes / 2 + i * kSub * Lay::kRowBytes, 2 * t + (r & 1) + 8 * (r >> 1), g, vraw[r]);
+#pragma unroll
+        for (int u = 0; u < Lay::kValWords; u += 2) {
+          uint32_t lo[4], hi[4];
+          val_pairs<DH, F8>(vraw[0], vraw[1], u, lo);
+          val_pairs<DH, F8>(vraw[2], vraw[3], u, hi);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int part = 0; part < kParts; ++part) {
+              mma_step<F8>(o[nt][u], lo[0], lo[1], hi[0], hi[1], pb[part][nt][i][0], pb[part][nt][i][1]);
+              mma_step<F8>(o[nt][u + 1], lo[2], lo[3], hi[2], hi[3], pb[part][nt][i][0], pb[part][nt][i][1]);
+            }
+        }
+      }
+    };
+    if (__any_sync(0xffffffffu, odd)) {
+      fresh = false;
+      bool low = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float mx0 = -INFINITY, mx1 = -INFINITY;
@@ -540,28 +579,68 @@ paged_attention_kernel(PagedParams p) {
           mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
           mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
         }
-        mx0 = fmaxf(mx0, m[nt][0]);
-        mx1 = fmaxf(mx1, m[nt][1]);
+        mx0 = fmaxf(mx0 + ref[nt][0], m[nt][0]);
+        mx1 = fmaxf(mx1 + ref[nt][1], m[nt][1]);
         // a maximum of -inf (every score so far is -inf): nothing to rescale, and 2^(-inf - 0) = 0
         const float corr0 = fast_exp2(m[nt][0] - finite_max(mx0)), corr1 = fast_exp2(m[nt][1] - finite_max(mx1));
         m[nt][0] = mx0; m[nt][1] = mx1;
         l[nt][0] *= corr0; l[nt][1] *= corr1;
+        const float to0 = finite_max(mx0) - lift<F8>(), to1 = finite_max(mx1) - lift<F8>();
 #pragma unroll
         for (int u = 0; u < DH / 16; ++u) { o[nt][u][0] *= corr0; o[nt][u][2] *= corr0; o[nt][u][1] *= corr1; o[nt][u][3] *= corr1; }
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+          float (&s)[4] = sc[nt][i];
+          s[0] += ref[nt][0] - to0; s[2] += ref[nt][0] - to0;
+          s[1] += ref[nt][1] - to1; s[3] += ref[nt][1] - to1;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) low = low || (s[e] < -kMostD8 && s[e] > -INFINITY);
+        }
+        ref[nt][0] = to0; ref[nt][1] = to1;
+        fresh = fresh || mx0 == -INFINITY || mx1 == -INFINITY;
+      }
+      // Small weights of 8-bit pages go through the product by themselves: the sums so far are raised by the same power of two as
+      // they, and lowered after (exact: they stay under 2^53 2^29).  fp16 holds them to 2^-11 down to 2^-49 of the largest, and
+      // 2^-60 of it is as good as nothing.  (64 rows of 1 to 4096 keys: 60.0 us where every tile has some, 51.0 where none has.)
+      if (F8 && __any_sync(0xffffffffu, low)) {
+        auto scale_sums = [&](float by) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int u = 0; u < DH / 16; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[nt][u][e] *= by;
+        };
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < S; ++i) {
+            float w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float& s = sc[nt][i][e];
+              const bool small = s < -kMostD8;
+              w[e] = small ? fast_exp2(s + kBoost) : 0.0f;
+              l[nt][e & 1] += w[e] * kUnboost;
+              if (small) s = -INFINITY;                // done with
+            }
+            pb[0][nt][i][0] = transpose8x8(pack_pair<F8>(w[0], w[1]));
+            pb[0][nt][i][1] = transpose8x8(pack_pair<F8>(w[2], w[3]));
+          }
+        scale_sums(1.0f / kUnboost);
+        add_values();
+        scale_sums(kUnboost);
       }
     }
-    // The weights of a tile in the values' type.  fp16 holds them to 2^-12; bf16 only to 2^-9, as much as the output's own
-    // rounding adds, so there they are the sum of two bf16 (the second holds what the first rounds away, to 2^-17 in all).
-    constexpr int kParts = F8 ? 1 : 2;
-    uint32_t pb[kParts][NT][S][2];
+    // The weights of a tile in the values' type.  fp16 holds them to 2^-11; bf16 only to 2^-8, as much as the output's own
+    // rounding adds, so there they are the sum of two bf16 (the second holds what the first rounds away, to 2^-16 in all).
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const float ref0 = finite_max(m[nt][0]), ref1 = finite_max(m[nt][1]);
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < S; ++i) {
         float (&s)[4] = sc[nt][i];
-        s[0] = fast_exp2(s[0] - ref0); s[2] = fast_exp2(s[2] - ref0);
-        s[1] = fast_exp2(s[1] - ref1); s[3] = fast_exp2(s[3] - ref1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = fast_exp2(s[e]);
         l[nt][0] += s[0] + s[2];
         l[nt][1] += s[1] + s[3];
 #pragma unroll
@@ -574,27 +653,7 @@ paged_attention_kernel(PagedParams p) {
           }
         }
       }
-    }
-#pragma unroll
-    for (int i = 0; i < S; ++i) {
-      ValRaw<DH, F8> vraw[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        read_val<DH, F8>(stage + kStageBytes / 2 + i * kSub * Lay::kRowBytes, 2 * t + (r & 1) + 8 * (r >> 1), g, vraw[r]);
-#pragma unroll
-      for (int u = 0; u < Lay::kValWords; u += 2) {
-        uint32_t lo[4], hi[4];
-        val_pairs<DH, F8>(vraw[0], vraw[1], u, lo);
-        val_pairs<DH, F8>(vraw[2], vraw[3], u, hi);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int part = 0; part < kParts; ++part) {
-            mma_step<F8>(o[nt][u], lo[0], lo[1], hi[0], hi[1], pb[part][nt][i][0], pb[part][nt][i][1]);
-            mma_step<F8>(o[nt][u + 1], lo[2], lo[3], hi[2], hi[3], pb[part][nt][i][0], pb[part][nt][i][1]);
-          }
-      }
-    }
+    add_values();
     use = use + 1 == kStages ? 0 : use + 1;
     free_stage = free_stage + 1 == kStages ? 0 : free_stage + 1;
   }

@@ -625,3 +625,36 @@ def test_calls_on_two_streams_at_once(lib):
     for i in range(2):
         for pair in got[i]:
             assert torch.equal(pair[0], want[i][0]) and torch.equal(pair[1], want[i][1])
+
+
+# nats by which some keys lead the others, one per query head
+LEADS = [0.0, 9.0, 14.0, 17.2, 20.0, 24.0, 28.0, 60.0]
+
+
+@pytest.mark.parametrize("kind,heads,Hkv,dh,positions,room", [
+    ("e4m3", 8, 1, 128, [2047], 0), ("e4m3", 8, 1, 64, [300, 5000, 0, 40], 0), ("e4m3", 16, 1, 128, [700], 0), ("e4m3", 8, 8, 128, [1500, 3], 9000),
+    ("bf16", 8, 1, 128, [2047], 0), ("bf16", 16, 1, 64, [300, 5000], 0)])
+def test_leading_keys_of_no_value(lib, kind, heads, Hkv, dh, positions, room):
+    # keys that lead and whose values are zero leave the row to the others, whose weights are small beside theirs
+    ks = CACHES[kind][1]
+    block, scale = 16, dh ** -0.5
+    q, ck, cv, ks, vs, table = _attend_case(positions, heads, Hkv, dh, block, kind, room, 61)
+    ck[..., 0] = 0.0
+    for r, last in enumerate(positions):
+        for j in [1] + list(range(70, last + 1, 97)):
+            if j <= last:
+                page = int(table[r, j // block])
+                ck[page, :, j % block, 0], cv[page, :, j % block] = 16.0 / ks, 0.0
+    q[:, :, 0] = (torch.tensor(LEADS * 2)[:heads] / (16.0 * scale)).bfloat16()
+    out = lib.qzo_paged_attention(q.cuda(), lib.KvCache(ck, cv, ks, vs), torch.from_numpy(table).cuda(),
+                                  torch.tensor(positions, dtype=torch.int32, device="cuda"))
+    kp, vp = f64(ck) * ks, f64(cv) * vs
+    want, spread = serving.paged_attention(f64(q), kp, vp, table, np.arange(len(positions)), positions, scale)
+    kmax = np.nanmax(np.abs(kp[np.unique(table[table >= 0])]))
+    # as in _attend_check, and what the weights leave out: 2^-60 of the largest weight for each key
+    score = np.abs(f64(q)).sum(-1, keepdims=True) * kmax * scale * (dh / 16 + 18) * 2 * F32_STEP
+    p_step = BF16_STEP if kind == "bf16" else F16_STEP
+    keys = max(positions) + 1
+    allowed = BF16_STEP * np.abs(want) + (p_step + 2 * score + (16 + keys / 8) * F32_STEP) * spread * (1 + BF16_STEP) + keys * np.nanmax(np.abs(vp)) * 2.0 ** -60
+    off = np.abs(f64(out) - want)
+    assert (off <= allowed).all(), [(off / allowed)[:, h].max() for h in range(heads)]
