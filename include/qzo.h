@@ -223,7 +223,8 @@ int qzo_paged_attention_workspace_bytes(int R, int n_heads, int n_kv_heads, int 
  *   out[t][h] = sum_j softmax_j(scale q[t][h] . k_j) v_j,  j = 0 .. position[t] (the row's own key among them),
  * with keys and values of head h / (n_heads / n_kv_heads) found through the block table: token j of request r lives in
  * block d_block_table[r][j / block_size].  A row with a negative position gives zeros, and so does one none of whose keys
- * scores above -inf.  Entries of the table behind a row's position, and the rest of its last block, are not looked at.
+ * scores above -inf.  Infinite and NaN values of keys that a row sees count as the sum says (an infinite value under a weight of
+ * less than 2^-100 of the row's largest may give NaN).  Entries of the table behind a row's position, and the rest of its last block, are not looked at.
  * Several rows may belong to one request (a prompt's rows, each of which sees the keys up to its own).
  * d_q bf16 [R][ldq] and d_out bf16 [R][ldo], head h at h * head_dim, 16-byte aligned, strides multiples of 8, not
  * overlapping; d_block_table int32 [n_seqs][table_width], at most 2^30 tokens wide; d_row_seq int32 [R] = the request of each row, NULL: row t is

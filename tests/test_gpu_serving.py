@@ -658,3 +658,25 @@ def test_leading_keys_of_no_value(lib, kind, heads, Hkv, dh, positions, room):
     allowed = BF16_STEP * np.abs(want) + (p_step + 2 * score + (16 + keys / 8) * F32_STEP) * spread * (1 + BF16_STEP) + keys * np.nanmax(np.abs(vp)) * 2.0 ** -60
     off = np.abs(f64(out) - want)
     assert (off <= allowed).all(), [(off / allowed)[:, h].max() for h in range(heads)]
+
+
+@pytest.mark.parametrize("H,Hkv,dh,positions", [(2, 2, 64, [0, 1, 300]), (12, 1, 128, [40, 2500]), (4, 4, 128, [0, 900] * 30)])
+def test_infinite_values_of_live_keys(lib, H, Hkv, dh, positions):
+    # an infinite value makes its dimension infinite, both signs make it NaN, the other dimensions stay as they are
+    q, ck, cv, ks, vs, table = _attend_case(positions, H, Hkv, dh, 16, "bf16", 0, 71)
+    for r, last in enumerate(positions):
+        for j, dim, v in ((0, 3, "inf"), (last // 2, 17, "-inf"), (last, dh - 1, "inf"), (0, 40, "inf"), (last, 40, "-inf"), (last, 5, "nan")):
+            cv[int(table[r, j // 16]), :, j % 16, dim] = float(v)
+    out = f64(lib.qzo_paged_attention(q.cuda(), lib.KvCache(ck, cv), torch.from_numpy(table).cuda(),
+                                      torch.tensor(positions, dtype=torch.int32, device="cuda")))
+    with np.errstate(invalid="ignore"):
+        want, _ = serving.paged_attention(f64(q), f64(ck), f64(cv), table, np.arange(len(positions)), positions, dh ** -0.5)
+    special = ~np.isfinite(want)
+    assert special.any() and np.isfinite(want).any()
+    assert np.array_equal(np.isnan(out), np.isnan(want)) and np.array_equal(out[special & ~np.isnan(want)], want[special & ~np.isnan(want)])
+    clean = f64(cv)
+    clean[~np.isfinite(clean)] = 0.0
+    for dim in (3, 17, dh - 1, 40, 5):
+        out[..., dim] = want[..., dim] = 0.0
+        clean[..., dim] = 0.0
+    _attend_check(torch.from_numpy(out), q, ck, torch.from_numpy(clean), 1.0, 1.0, table, np.arange(len(positions)), positions, dh ** -0.5)
