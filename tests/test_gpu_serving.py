@@ -680,3 +680,23 @@ def test_infinite_values_of_live_keys(lib, H, Hkv, dh, positions):
         out[..., dim] = want[..., dim] = 0.0
         clean[..., dim] = 0.0
     _attend_check(torch.from_numpy(out), q, ck, torch.from_numpy(clean), 1.0, 1.0, table, np.arange(len(positions)), positions, dh ** -0.5)
+
+
+@pytest.mark.parametrize("positions,H,Hkv,dh", [([2000, 70], 8, 8, 128), ([3000], 12, 1, 64), ([300], 4, 4, 128)])
+def test_weights_over_bf16_pages_keep_more_bits_than_their_type(lib, positions, H, Hkv, dh):
+    # values of both signs that cancel: the weights' rounding shows beside the output's
+    q, ck, cv, ks, vs, table = _attend_case(positions, H, Hkv, dh, 16, "bf16", 0, 81)
+    sign = torch.where(torch.rand(cv.shape[:3], generator=torch.Generator().manual_seed(1)) < 0.5, -1.0, 1.0)[..., None].cuda()
+    cv.copy_(torch.where(torch.isnan(cv), cv, (40.0 * sign + 0.5 * cv.float()).bfloat16()))
+    out = lib.qzo_paged_attention(q.cuda(), lib.KvCache(ck, cv), torch.from_numpy(table).cuda(),
+                                  torch.tensor(positions, dtype=torch.int32, device="cuda"))
+    want, spread = serving.paged_attention(f64(q), f64(ck), f64(cv), table, np.arange(len(positions)), positions, dh ** -0.5)
+    assert np.median(np.abs(want) / spread) < 0.1
+    # score: dh exact products summed in fp32 (chains of 16, truncated at worst), one scaling; its exponential within 4 steps
+    kmax = np.nanmax(np.abs(f64(ck)[np.unique(table[table >= 0])]))
+    score = np.abs(f64(q)).sum(-1, keepdims=True) * kmax * dh ** -0.5 * (dh / 16 + 18) * 2 * F32_STEP
+    # weights as the sum of two bf16: the first off by less than 2^-7 of the weight, the second by 2^-8 of that
+    keys = max(positions) + 1
+    allowed = BF16_STEP * np.abs(want) + (2.0 ** -15 + 2 * score + (16 + keys / 8) * F32_STEP) * spread * (1 + BF16_STEP)
+    off = np.abs(f64(out) - want)
+    assert (off <= allowed).all(), (off / allowed).max()
