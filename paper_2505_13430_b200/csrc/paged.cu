@@ -7,6 +7,7 @@
 
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -409,10 +410,10 @@ paged_attention_kernel(PagedParams p) {
 
   // For 8-bit keys the queries become fp16, scaled by a power of two that brings the head's largest element to [64, 128):
   // exact but for elements below 2^-23 of it, which are off by at most 2^-31 of it.
-  float unscale[NT][2];
+  float factor[NT][2];                                 // from products to scores in powers of two; finite, so that 0 stays 0
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    unscale[nt][0] = unscale[nt][1] = 1.0f;
+    factor[nt][0] = factor[nt][1] = p.scale_log2e;
     if (F8) {
       float big = 0.0f;
 #pragma unroll
@@ -430,8 +431,8 @@ paged_attention_kernel(PagedParams p) {
         const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[nt][i]));
         qf[nt][i] = pack_pair<true>(f.x * down, f.y * down);
       }
-      unscale[nt][0] = __shfl_sync(0xffffffffu, up, 8 * t);
-      unscale[nt][1] = __shfl_sync(0xffffffffu, up, 8 * t + 4);
+      factor[nt][0] = fminf(p.scale_log2e * __shfl_sync(0xffffffffu, up, 8 * t), FLT_MAX);
+      factor[nt][1] = fminf(p.scale_log2e * __shfl_sync(0xffffffffu, up, 8 * t + 4), FLT_MAX);
     }
   }
 
@@ -525,7 +526,7 @@ paged_attention_kernel(PagedParams p) {
     bool odd = fresh;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const float f0 = F8 ? p.scale_log2e * unscale[nt][0] : p.scale_log2e, f1 = F8 ? p.scale_log2e * unscale[nt][1] : p.scale_log2e;
+      const float f0 = factor[nt][0], f1 = factor[nt][1];
       float most = 0.0f;
 #pragma unroll
       for (int i = 0; i < S; ++i) {

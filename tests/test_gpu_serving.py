@@ -700,3 +700,14 @@ def test_weights_over_bf16_pages_keep_more_bits_than_their_type(lib, positions, 
     allowed = BF16_STEP * np.abs(want) + (2.0 ** -15 + 2 * score + (16 + keys / 8) * F32_STEP) * spread * (1 + BF16_STEP)
     off = np.abs(f64(out) - want)
     assert (off <= allowed).all(), (off / allowed).max()
+
+
+def test_keys_of_zeros_under_the_largest_queries_and_scales(lib):
+    # every score is 0, however large the factors that stand before it: the mean of the values
+    H, dh, positions = 2, 64, [50]
+    q, ck, cv, ks, vs, table = _attend_case(positions, H, H, dh, 16, "e4m3", 0, 91)
+    ck.zero_()
+    q = q.sign() * torch.tensor(3.0e38).bfloat16()
+    out = lib.qzo_paged_attention(q.cuda(), lib.KvCache(ck, cv, 2.0 ** 64, vs), torch.from_numpy(table).cuda(),
+                                  torch.tensor(positions, dtype=torch.int32, device="cuda"), scale=2.0 ** 40)
+    _attend_check(out, q * 0, ck, cv, ks, vs, table, np.arange(1), positions, 1.0)
