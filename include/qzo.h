@@ -186,7 +186,8 @@ int qzo_gemv_int4(const void* d_x_bf16, int ldx, const void* d_wq, const void* d
 
 /* A paged key-value cache of one layer, described by the caller (host struct, read during the call): keys and
  * values in blocks [n_blocks][n_kv_heads][block_size][head_dim], 16-byte aligned.  dtype QZO_DTYPE_BF16 (both
- * scales 1) or QZO_DTYPE_E4M3: the stored code times the scale (2^-64 to 2^64) is the value; codes saturate at +-448.
+ * scales 1) or QZO_DTYPE_E4M3: the stored code times the scale (2^-64 to 2^64) is the value; codes saturate at +-448 and are
+ * those of the value times the scale's reciprocal in fp32.
  * block_size is a power of two from 16 to 256, head_dim 64 or 128, n_blocks * block_size < 2^31. */
 typedef struct {
   void* k;

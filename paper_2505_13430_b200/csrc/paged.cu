@@ -52,6 +52,9 @@ __device__ __forceinline__ uint4 pack8_bf16(const float v[8]) {
   const uint2 a = pack4_bf16(v), b = pack4_bf16(v + 4);
   return make_uint4(a.x, a.y, b.x, b.y);
 }
+// Codes of v times the scale's fp32 reciprocal: that product is off from v / scale by 2^-23 of it, which shows only where v / scale is
+// as near to the middle between two codes (divisions: 4099 rows with norms 26.2 us instead of 22.5, 4096 rows of 32 + 32 heads
+// 45.2 instead of 34.7).
 __device__ __forceinline__ uint32_t pack4_e4m3(const float v[4], float inv) {
   const __nv_fp8x2_storage_t a = __nv_cvt_float2_to_fp8x2(make_float2(v[0] * inv, v[1] * inv), __NV_SATFINITE, __NV_E4M3);
   const __nv_fp8x2_storage_t b = __nv_cvt_float2_to_fp8x2(make_float2(v[2] * inv, v[3] * inv), __NV_SATFINITE, __NV_E4M3);

@@ -711,3 +711,20 @@ def test_keys_of_zeros_under_the_largest_queries_and_scales(lib):
     out = lib.qzo_paged_attention(q.cuda(), lib.KvCache(ck, cv, 2.0 ** 64, vs), torch.from_numpy(table).cuda(),
                                   torch.tensor(positions, dtype=torch.int32, device="cuda"), scale=2.0 ** 40)
     _attend_check(out, q * 0, ck, cv, ks, vs, table, np.arange(1), positions, 1.0)
+
+
+def test_8_bit_codes_at_ordinary_scales(lib):
+    # scales as a program takes them, the largest value over 448: every code within half a step of value / scale
+    T, H, dh = 300, 2, 128
+    q, k, v = (_randn((T, H, dh), 90 + i, 2.0) for i in range(3))
+    ks, vs = float(k.abs().max().float()) / 448, float(v.abs().max().float()) / 448
+    ck, cv = (torch.zeros((20, H, 16, dh), dtype=torch.float8_e4m3fn, device="cuda") for _ in range(2))
+    i = torch.arange(T, dtype=torch.int32, device="cuda")
+    lib.qzo_qk_norm_rope_cache(q.cuda(), k.cuda(), v.cuda(), i, i, lib.KvCache(ck, cv, ks, vs))
+    for pages, rows, scale in ((ck, k, ks), (cv, v, vs)):
+        got = f64(pages).transpose(0, 2, 1, 3).reshape(-1, H, dh)[:T]
+        want = np.clip(f64(rows) / np.float64(np.float32(scale)), -448, 448)
+        step = 2.0 ** np.maximum(np.floor(np.log2(np.maximum(np.abs(want), 1e-30))), -6) * 2.0 ** -3
+        # in fp32 the reciprocal and the product are off by half a step each
+        assert (np.abs(got - want) <= step / 2 + 2 * F32_STEP * 1.001 * np.abs(want)).all()
+        assert np.abs(got).max() == 448
