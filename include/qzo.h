@@ -198,7 +198,7 @@ typedef struct {
 } qzo_kv_cache;
 
 /* Table of the rotation: float [max_pos][head_dim/2][2] = {cos, sin}(pos * theta^(-2i/head_dim)), the angles
- * formed in fp64 (the table the model builds for itself).  max_pos * head_dim <= 2^30, head_dim 64 or 128. */
+ * formed in fp64 (the table the model builds for itself).  32-byte aligned, max_pos * head_dim <= 2^30, head_dim 64 or 128. */
 int qzo_rope_table(float* d_table, int max_pos, int head_dim, float theta, void* stream);
 
 /* One pass over the new rows' queries, keys and values in front of the attention:

@@ -898,7 +898,7 @@ extern "C" {
 
 int qzo_rope_table(float* d_table, int max_pos, int head_dim, float theta, void* stream) {
   if (!d_table || max_pos <= 0 || (head_dim != 64 && head_dim != 128) || !(theta > 0.0f) || !isfinite(theta)) return QZO_ERR_BAD_ARG;
-  if ((int64_t)max_pos * head_dim > (1 << 30) || ((uintptr_t)d_table & 15)) return QZO_ERR_BAD_ARG;
+  if ((int64_t)max_pos * head_dim > (1 << 30) || ((uintptr_t)d_table & 31)) return QZO_ERR_BAD_ARG;   // as its reader asks for
   QZO_TRY(check_device());
   return launch_rope_table(d_table, max_pos, head_dim, theta, (cudaStream_t)stream);
 }

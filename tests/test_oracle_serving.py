@@ -162,6 +162,12 @@ def test_gains_and_angles_off_their_32_bytes_are_refused():
     _refused(rope, {}, [dict(qg=half), dict(kg=half), dict(tab=half)])
 
 
+def test_a_table_off_its_32_bytes_is_refused_where_it_is_made():
+    def call(t):
+        return _lib()._lib.qzo_rope_table(t, 64, 64, 1e4, None)
+    _refused(call, dict(t=P), [dict(t=ctypes.c_void_p(0x10010)), dict(t=ctypes.c_void_p(0x10008))])
+
+
 def test_scales_whose_reciprocal_or_product_leaves_fp32_are_refused():
     qzo = _lib()
     def rope(cache):
