@@ -98,9 +98,8 @@ constexpr int kNormVecs = 4;
 
 template <bool LAYERNORM>
 __global__ void __launch_bounds__(kNormThreads)
-add_norm_kernel(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* __restrict__ w,
-                const float* __restrict__ b, const float* __restrict__ w2, const float* __restrict__ b2, int pair_rows,
-                float eps, int d, __nv_bfloat16* y) {
+add_norm_kernel(__nv_bfloat16* x, const __nv_bfloat16* delta, const float* w, const float* b, const float* w2, const float* b2,
+                int pair_rows, float eps, int d, __nv_bfloat16* y) {   // gains too are updated on the device (joint mode)
   serving_begin();
   serving_next();
   // rows from pair_rows on (second copy of a paired step in joint mode) use the second gain / bias set

@@ -320,3 +320,41 @@ def test_training_goes_on_after_a_decode_that_met_a_bad_index():
         outs.append((steps, gm.scales.clone()))
         gm.close()
     assert outs[0][0] == outs[1][0] and torch.equal(outs[0][1], outs[1][1])
+
+
+@pytest.mark.parametrize("name", ["tiny", "tiny_opt"])
+def test_decode_behind_joint_updates_uses_what_they_wrote(name):
+    # joint mode changes norms and matrices on the device: the decode in the queue behind it answers with the new ones
+    from paper_2505_13430_b200 import qzo
+    cfg = inputs.model_cfg(name)
+    gm = qzo.build_model_from_raw(inputs.raw_model_tensors(cfg, seed=1000), 64)
+    gm.qzo_enable_joint_spsa(0.05)
+    tok, lab = inputs.tokens_and_labels(cfg, 2, 32, seed=9)
+    tok, lab = tok.cuda(), lab.cuda()
+    srv = Server(qzo, gm, cfg, 2, 16, 16)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table = torch.arange(8, **i32).view(2, 4)
+    pos = torch.arange(32, **i32).repeat(2)
+    seq = torch.arange(2, **i32).repeat_interleave(32)
+    slots = table[seq.long(), (pos // 16).long()] * 16 + pos % 16
+    one = lambda r, p: [t[32 * r + p:32 * r + p + 1].contiguous() for t in (tok.view(-1), seq, pos, slots)]  # noqa: E731
+    answers = []
+    for step in range(3):
+        if step:
+            gm.qzo_step(tok, lab, 5 + step, 1e-3, 1e-3, 100.0)
+        many = gm.qzo_decode(srv.caches, tok.view(-1), seq, pos, slots, table)
+        few = gm.qzo_decode(srv.caches, *one(1, 31), table)
+        torch.cuda.synchronize()
+        assert torch.equal(gm.qzo_decode(srv.caches, tok.view(-1), seq, pos, slots, table), many)
+        torch.cuda.synchronize()
+        assert torch.equal(gm.qzo_decode(srv.caches, *one(1, 31), table), few)
+        gm.qzo_forward_loss(tok, lab, 0, 0, 1e-3)
+        want = gm.qzo_debug_layer_output(0, 1, 64)
+        # each side within TOL of the exact logits: two of them within twice that of one another
+        assert (many - want).abs().max() <= 2 * TOL * want.abs().max()
+        assert (few - want[63:]).abs().max() <= 2 * TOL * want.abs().max()
+        answers.append(want.clone())
+    for a, b in zip(answers, answers[1:]):
+        assert (a - b).abs().max() > 0.1 * a.abs().max()
+    assert gm.qzo_device_status() == 0
+    gm.close()
