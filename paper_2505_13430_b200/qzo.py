@@ -295,6 +295,7 @@ def qzo_update_scales_flat(scales, seed, index_base, lr, g, clip):
 
 # ---- serving operators ----
 
+# limits of qzo_gemv_int4 (above, qzo_perturbed_gemm at sign 0) and qzo_assign_slots, for a program that divides its work by them
 GEMV_MAX_ROWS = 16
 MAX_REQUESTS = 4096
 

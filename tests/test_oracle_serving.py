@@ -188,3 +188,12 @@ def test_assign_slots_refusals():
     bad = [{n: NONE} for n in ("lens", "new", "tab", "free", "cnt", "a", "b", "c", "lo", "co")]
     bad += [dict(B=0), dict(B=4097), dict(w=0), dict(bs=8), dict(bs=24), dict(cap=0), dict(rows=0), dict(rows=(1 << 30) + 1), dict(w=1 << 28), dict(cap=1 << 28)]
     _refused(call, good, bad)
+
+
+def test_the_binding_names_the_limits_of_the_header():
+    import os
+    import re
+    qzo = _lib()
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "qzo.h")).read()
+    for name in ("GEMV_MAX_ROWS", "MAX_REQUESTS"):
+        assert getattr(qzo, name) == int(re.search(rf"#define QZO_{name} (\d+)", header).group(1))
