@@ -177,7 +177,8 @@ int qzo_update_scales_flat(void* d_scales_bf16, int64_t count, uint64_t seed, ui
 /* Matrix-vector products with int4 weights and group scales, for up to QZO_GEMV_MAX_ROWS rows (the linear of
  * qzo_perturbed_gemm at sign 0 for a step of few tokens):
  *   Y[t][n] = sum_k X[t][k] s[k/128][n] q[k][n] (+ bias[n]).
- * The products X q of a group of 128 are summed in fp32 (each is exact), then scaled in fp32.  Y is rounded once.
+ * The products X q of a group of 128 are summed in fp32 (each is exact; lowered by 2^10 until the end, so that no finite X
+ * overflows there), then scaled in fp32.  Y is rounded once.
  * d_x bf16 [M][ldx], 16-byte aligned, ldx a multiple of 8 and >= K; d_wq kernel layout (qzo_repack_int4); d_scales bf16
  * [ceil(K/128)][N], both 16-byte aligned; d_bias float [N] or NULL; d_y bf16 [M][ldy], ldy >= N, must not overlap d_x.  K and N multiples of 8. */
 #define QZO_GEMV_MAX_ROWS 16

@@ -39,11 +39,13 @@ struct GemvParams {
   int n_lin, ldx, M, K, KB, G;
 };
 
-// Two 4-bit values u (bits 4p.. of each half of w) as the bf16 pair u - 8: 0x4300 | u is 128 + u, less 136; both exact.
+// Two 4-bit values u (bits 4p.. of each half of w) as the bf16 pair (u - 8) / kLowered: 0x3E00 | u is (128 + u) / 1024, less 136 /
+// 1024; both exact.  So lowered, the products of a group of 128 stay finite whatever the activations; the sums are raised at the end.
+constexpr float kLowered = 1024.0f;
 __device__ __forceinline__ uint32_t weight_pair(uint32_t w, int p) {
   uint32_t u;                           // (shifted & mask) | 0x4300 in one instruction
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(u) : "r"(w >> (4 * p)), "r"(0x000F000Fu), "r"(0x43004300u));
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), __floats2bfloat162_rn(136.0f, 136.0f));
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(u) : "r"(w >> (4 * p)), "r"(0x000F000Fu), "r"(0x3E003E00u));
+  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), __floats2bfloat162_rn(136.0f / kLowered, 136.0f / kLowered));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
@@ -218,6 +220,7 @@ gemv_w4_kernel(GemvParams p) {
     } else {
       for (int c = 0; c < (int)gridDim.x; ++c) y += *cluster.map_shared_rank(&red[0][row][n], c);
     }
+    y *= kLowered;
     if (L.bias) y += L.bias[n0 + n];
     L.out[(size_t)row * L.ldo + n0 + n] = __float2bfloat16_rn(y);
   }

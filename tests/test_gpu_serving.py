@@ -728,3 +728,16 @@ def test_8_bit_codes_at_ordinary_scales(lib):
         # in fp32 the reciprocal and the product are off by half a step each
         assert (np.abs(got - want) <= step / 2 + 2 * F32_STEP * 1.001 * np.abs(want)).all()
         assert np.abs(got).max() == 448
+
+
+@pytest.mark.parametrize("M", [1, 3, 8, 16])
+def test_gemv_of_the_largest_activations(lib, M):
+    # groups whose products without the scales pass fp32's largest number, and whose outputs do not
+    K, N = 512, 72
+    x, q, s, wq = _gemv_case(lib, M, K, N, 3)
+    big = torch.finfo(torch.bfloat16).max
+    x[0, 130:140], x[M - 1, 511] = big, -big
+    s = (s.float() * 2.0 ** -5).bfloat16()
+    want = f64(x) @ (f64(s)[np.arange(K) // 128] * q.numpy().astype(np.float64))
+    assert (np.abs(f64(x)[0, 130:140] @ q.numpy()[130:140].astype(np.float64)) > 3.5e38).any() and np.abs(want).max() < 3e38
+    _gemv_check(lib.qzo_gemv_int4(x.cuda(), wq, s.cuda(), K, N), x, q, s)
