@@ -208,7 +208,7 @@ int qzo_rope_table(float* d_table, int max_pos, int head_dim, float theta, void*
  * rotation of the pairs (i, i + head_dim/2) by the row's position (left out when d_table is NULL).  q' goes to
  * d_q_out, k' and v' into the cache at the row's slot; each is rounded once, from fp32.
  * d_q bf16 [T][ldq] with head h at h * head_dim, d_k and d_v alike with n_kv_heads heads; 16-byte aligned, strides
- * multiples of 8; d_q_out bf16 [T][ldqo], may be d_q itself (same stride) but not overlap it otherwise; gains float
+ * multiples of 8; d_q_out bf16 [T][ldqo], may be d_q itself (same stride) but not overlap it otherwise, nor d_k, d_v; gains float
  * [head_dim], d_table as qzo_rope_table writes it (gains and table 32-byte aligned).  d_positions, d_slots int32 [T]; the slots of one call are distinct.
  * A row with a negative position or slot is padding: nothing is written for it.  A slot beyond the cache or a position
  * beyond the table sets bit 1 of the status word: the first is not written, the second is turned by the table's last. */
@@ -392,7 +392,8 @@ int qzo_step_host(qzo_model* m, const int32_t* h_tokens, const int32_t* h_labels
  * Rows of padding (negative position or slot) give logits that mean nothing and touch no cache.  An index out of range
  * (token, position, slot, block) sets bit 1 of what qzo_device_status reads; training steps go on as if it had not been met.
  * Up to QZO_GEMV_MAX_ROWS rows the linears run as qzo_gemv_int4, above as qzo_perturbed_gemm with sign 0.  Asynchronous on the model's
- * stream, and nothing but launches: a model whose stream is not the legacy default one can have its steps captured. */
+ * stream, and nothing but launches: a model whose stream is not the legacy default one can have its steps captured (they use the
+ * model's buffers, so replays belong on that stream, in turn with its other work). */
 int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
                const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
                int table_width, float* d_logits);

@@ -5,9 +5,10 @@
 // group in hand-offs than the weights take to read (the same linears at 16 rows: 10.8, 18.2, 18.0 and 24.0 us there, 5.4, 12.0,
 // 10.5 and 14.5 us here, for K x N = 4096 x 4096, 4096 x 11008, 11008 x 4096 and 5120 x 13824).
 // What bounds it: turning nibbles into bf16 takes three instructions per pair of weights (shift, mask-and-or, subtract), and
-// a warp's work around the 2 KB of a turn as many again, so at one row the ALU pipe is half busy at
-// 4.3 TB/s (8192 x 18944, 18.5 us); the 7B-sized linears are bound by what a launch costs before its first bytes
-// arrive and after its last ones (1 x 4096 x 11008: 8.3 us, where a plain read of as many bytes takes 6.2 us); at 16 rows the
+// a warp's work around the 2 KB of a turn as many again, so at one row the ALU pipe is 60 % busy at
+// 4.4 TB/s (8192 x 18944, 18.2 us; its 592 CTAs take a third more than the 444 that fit at a time: 68 registers a thread leave
+// an SM three CTAs of eight warps); the 7B-sized linears are bound by what a launch costs before its first bytes
+// arrive and after its last ones (1 x 4096 x 11008: 8.2 us, where a plain read of as many bytes takes 6.2 us); at 16 rows the
 // activations are twice the bytes of the weights in shared memory, which leaves twelve warps on an SM.
 #include "qzo_common.cuh"
 #include "launch.cuh"
@@ -24,7 +25,7 @@ namespace qzo {
 namespace {
 
 constexpr int kMaxCluster = 8;
-constexpr int kSMs = 148, kSMem = 228 * 1024;   // SMs, and the shared memory of one (a CTA may have 1 KB less)
+constexpr int kSMem = 228 * 1024;    // shared memory of an SM (a CTA may have 1 KB less)
 
 struct GemvLinear {
   const uint4* wq;
@@ -235,7 +236,8 @@ int run_gemv(const GemvParams& p, int blocks, cudaStream_t st) {
   while (cluster < kMaxCluster && 2 * cluster * blocks <= kSMs && 2 * cluster * W <= p.G) cluster *= 2;
   constexpr int kRing = W * kStages * (kWeightBytes + kScaleBytes + 256 * XR), kSums = W * (XR > 8 ? 16 : 8) * (kCols + 1) * (int)sizeof(float);
   // The CTAs are spread evenly: each asks for so much shared memory that no SM takes more than its share of them (4096 x
-  // 9472, 296 CTAs: 6.5 us at one row and 9.2 at sixteen; 7.7 and 11.4 where some SMs take three of them and some one).
+  // 9472, 296 CTAs: 6.5 us at one row and 9.2 at sixteen; 7.7 and 11.4 where some SMs take three of them and some one).  From a
+  // share of four on it changes nothing for CTAs of eight warps: their registers let an SM hold three.
   const int share = ceil_div(blocks * cluster, kSMs), even = (kSMem / (share + 1) - 1024) / 16 * 16 + 16;
   const int smem = std::max({kRing, kSums, even});
   static std::atomic<unsigned long long> allowed{0};
@@ -262,8 +264,8 @@ int launch_gemv_group(const __nv_bfloat16* d_x, int ldx, int M, int K, const Gem
   if (M == 1) return run_gemv<1, 8>(p, (int)blocks, st);
   if (M <= 4) return run_gemv<4, 8>(p, (int)blocks, st);
   if (M <= 8) return run_gemv<8, 8>(p, (int)blocks, st);
-  // Two tiles of rows: the activations take half of a stage, so CTAs of eight warps leave room for two of them on an SM
-  // only, which pays where there is no more than one CTA per SM (measured with 16 rows: K = N = 4096 5.4 us against 6.1 us
+  // Two tiles of rows: the activations take two thirds of a stage, and CTAs of eight warps (149 KB) leave room for one of them
+  // on an SM only, which pays where there is no more than one CTA per SM (measured with 16 rows: K = N = 4096 5.4 us against 6.1 us
   // with four warps, K = 5120, N = 13824 17.2 us against 14.5 us).
   return blocks <= kSMs ? run_gemv<16, 8>(p, (int)blocks, st) : run_gemv<16, 4>(p, (int)blocks, st);
 }

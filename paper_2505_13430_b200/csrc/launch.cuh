@@ -18,6 +18,8 @@ void add_launches(long long n);   // kernels run by replaying a recorded step
     }                                                                       \
   } while (0)
 
+constexpr int kSMs = 148;   // of a B200: what the serving kernels' launch rules fill (on another count of SMs they only spread work less evenly)
+
 // Launch of a serving kernel: allowed to start while the kernel before it in the stream ends (a decode step is a chain of
 // launches of a few microseconds).  Such a kernel calls serving_begin() before it touches global memory, in every CTA.
 // cluster > 1: CTAs of a cluster.

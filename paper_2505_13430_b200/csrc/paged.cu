@@ -15,7 +15,6 @@
 namespace qzo {
 namespace {
 
-constexpr int kSMs = 148;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // =========================================================================================
@@ -364,8 +363,8 @@ __host__ __device__ constexpr int ring_stages(int NT) { return NT == 1 ? 2 : 3; 
 // share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.  The k order of the
 // products is free, so a lane's 16 consecutive bytes of a key feed four k positions, and values are paired across two keys
 // by byte permutes.
-// Bound by HBM where CTAs run long (1 row of 131071 keys, 32 heads on 8: bf16 82.1 us, 6.5 TB/s; 16 rows of 100 to 2048 keys, 32
-// key heads: 44.8 us, 6.3 TB/s; e4m3 1 row of 131071 46.0 us, 5.8 TB/s), by what a CTA needs before its first keys and after
+// Bound by HBM where CTAs run long (1 row of 131071 keys, 32 heads on 8: bf16 81.7 us, 6.6 TB/s; 16 rows of 100 to 2048 keys, 32
+// key heads: 44.7 us, 6.3 TB/s; e4m3 1 row of 131071 45.9 us, 5.8 TB/s), by what a CTA needs before its first keys and after
 // its last where they run short (1 row of 4096 keys, 32 key heads: 16.5 us, 4.1 TB/s).  The rings (64 KB a CTA) keep
 // 190 KB in flight or in use on an SM; with the next tile in registers instead, 8 rows of 2048 keys took 51.5 us, now 42.1.
 template <int DH, int NT, bool F8, int W>
@@ -793,9 +792,11 @@ Plan attention_plan(int64_t R, int Hkv, int G, int subs, int64_t max_len) {
   if (ctas <= kSMs && max_len <= (ctas <= kSMs / 2 ? 768 : 2048) * subs) return {1, 1, 0};
   // Few CTAs: as many splits as fill the SMs once, but none shorter than 128 keys (1 row of 4096 keys over 32 key heads: 17.1 us
   // with 13 splits, 18.1 with 9, 20.9 with 18).  More rows: pieces of 2048 keys, so that a long row among short ones does not
-  // outlast them, as long as the grid stays within eight times what the SMs hold (16 rows of 100 to 2048 keys, 32 key heads: 44.8
-  // us; with pieces of 512 keys 47.5, of 1024 47.3; 8 rows of 2048 42.1, 48.3 and 52.1; 64 rows of 1 to 4096 over 8 key heads
-  // 94.1, 88.6 and 89.3).
+  // outlast them, as long as the grid stays within eight times what the SMs hold (16 rows of 100 to 2048 keys, 32 key heads: 44.7
+  // us; with pieces of 512 keys 47.5, of 1024 47.3; 8 rows of 2048 41.6, 48.3 and 52.1).  The length follows key heads that are
+  // not shared, as in this library's models; shorter pieces suit batches over few key heads better (64 rows of 1 to 4096 over 8:
+  // 92.5 us, with 512 keys 88.6, of 1024 89.3).  All of this goes by the table's width, the longest a row may be: the rows' own
+  // lengths are known on the device only.
   const int64_t slots = kSMs * resident_ctas(head_tiles);
   const int64_t fill = std::min<int64_t>(slots / ctas, max_len / (128 * subs));
   const int64_t even = R > 1 ? std::min<int64_t>(max_len / (2048 * subs), 8 * slots / ctas) : 1;
