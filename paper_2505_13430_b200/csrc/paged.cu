@@ -342,18 +342,17 @@ __device__ __forceinline__ float upper_half(uint32_t bits) { return __uint_as_fl
 // What scores are taken relative to: their maximum, or 0 where there is none (all -inf).
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 
-// A weight is 2^d, d = score - (maximum so far) + lift().  The maximum is only raised when a score passes it by 2^kSlack: until
-// then a tile needs neither the maximum over its keys nor a rescaling, and weights that reach 2^8 cost no precision.  Where weights
-// become fp16 they are lifted, and those below 2^-14, where fp16 has no more relative steps, are raised by 2^kBoost for a product of
-// their own.
-constexpr float kSlack = 8.0f;
-template <bool F8> __device__ constexpr float lift() { return F8 ? 6.0f : 0.0f; }
-constexpr float kMostD8 = 14.0f;                       // 8-bit pages: |d| within which a tile needs nothing of its own
-constexpr float kBoost = 29.0f, kUnboost = 0x1p-29f;
+// A weight is 2^(score - reference), the reference being the maximum so far less lift().  The maximum is only raised when a score
+// passes it by kSlack: until then a tile needs neither the maximum over its keys nor a rescaling, and weights that reach 2^8
+// cost no precision.  Where weights become fp16 they are lifted, and those below 2^-kUnder, where fp16 has no more relative steps,
+// are raised by 2^kBoost for a product of their own.
+constexpr float kSlack = 8.0f, kUnder = 14.0f, kBoost = 29.0f, kUnboost = 0x1p-29f;
+template <bool F8> __host__ __device__ constexpr float lift() { return F8 ? 6.0f : 0.0f; }
+template <bool F8> __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.0f : m - lift<F8>(); }
 
 // Stages of a ring and CTAs of four warps on an SM, for NT tiles of eight heads: three CTAs with two stages each where their
 // registers allow it, two with three stages otherwise (64 rows to 4096 in e4m3: 55.3 us against 58.3 with two CTAs; 16 rows of
-// 8192 keys, 24 heads on one: 14.3 us, with three 17.2 when two took 13.9).
+// 8192 keys, 24 heads on one: 14.6 us, with three 17.2 when two took 13.9).
 __host__ __device__ constexpr int resident_ctas(int NT) { return NT == 1 ? 3 : 2; }
 __host__ __device__ constexpr int ring_stages(int NT) { return NT == 1 ? 2 : 3; }
 
@@ -439,12 +438,12 @@ paged_attention_kernel(PagedParams p) {
   }
 
   float o[NT][DH / 16][4];
-  float m[NT][2], l[NT][2], ref[NT][2];                // maximum so far, sum of weights, what is taken off a score
+  float m[NT][2], l[NT][2], ref[NT][2];                // maximum so far, sum of weights, reference
   bool fresh = true;                                   // no maximum yet for some of the heads
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     m[nt][0] = m[nt][1] = -INFINITY;
-    ref[nt][0] = ref[nt][1] = -lift<F8>();
+    ref[nt][0] = ref[nt][1] = 0.0f;
     l[nt][0] = l[nt][1] = 0.0f;
 #pragma unroll
     for (int u = 0; u < DH / 16; ++u) o[nt][u][0] = o[nt][u][1] = o[nt][u][2] = o[nt][u][3] = 0.0f;
@@ -529,20 +528,23 @@ paged_attention_kernel(PagedParams p) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const float f0 = factor[nt][0], f1 = factor[nt][1];
-      float most = 0.0f;
+      float most0 = -INFINITY, most1 = -INFINITY, least0 = INFINITY, least1 = INFINITY;
 #pragma unroll
       for (int i = 0; i < S; ++i) {
         float (&s)[4] = sc[nt][i];
-        s[0] = fmaf(s[0], f0, -ref[nt][0]); s[1] = fmaf(s[1], f1, -ref[nt][1]);
-        s[2] = fmaf(s[2], f0, -ref[nt][0]); s[3] = fmaf(s[3], f1, -ref[nt][1]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) most = fmaxf(most, F8 ? fabsf(s[e]) : s[e]);
+        s[0] *= f0; s[1] *= f1; s[2] *= f0; s[3] *= f1;
+        most0 = fmaxf(most0, fmaxf(s[0], s[2]));
+        most1 = fmaxf(most1, fmaxf(s[1], s[3]));
+        least0 = fminf(least0, fminf(s[0], s[2]));
+        least1 = fminf(least1, fminf(s[1], s[3]));
         if (!full) {                                   // rows of zeros behind the last key: they may make a tile odd, no more
           if (g >= n_keys[i]) s[0] = s[1] = -INFINITY;
           if (g + 8 >= n_keys[i]) s[2] = s[3] = -INFINITY;
         }
       }
-      odd = odd || most > (F8 ? kMostD8 : kSlack);
+      constexpr float kOver = kSlack + lift<F8>();
+      odd = odd || most0 > ref[nt][0] + kOver || most1 > ref[nt][1] + kOver;
+      if (F8) odd = odd || least0 < ref[nt][0] - kUnder || least1 < ref[nt][1] - kUnder;
     }
     // the tile's weights, as they enter the product with the values, and that product
     constexpr int kParts = F8 ? 1 : 2;
@@ -585,29 +587,27 @@ paged_attention_kernel(PagedParams p) {
           mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, d));
           mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, d));
         }
-        mx0 = fmaxf(mx0 + ref[nt][0], m[nt][0]);
-        mx1 = fmaxf(mx1 + ref[nt][1], m[nt][1]);
-        // a maximum of -inf (every score so far is -inf): nothing to rescale, and 2^(-inf - 0) = 0
-        const float corr0 = fast_exp2(m[nt][0] - finite_max(mx0)), corr1 = fast_exp2(m[nt][1] - finite_max(mx1));
+        mx0 = fmaxf(mx0, m[nt][0]);
+        mx1 = fmaxf(mx1, m[nt][1]);
+        // from one reference to the next: for the largest scores they are not the maxima less the lift to the bit.  Before the first
+        // score above -inf there is nothing to rescale.
+        const float to0 = reference<F8>(mx0), to1 = reference<F8>(mx1);
+        const float corr0 = m[nt][0] == -INFINITY ? 0.0f : fast_exp2(ref[nt][0] - to0);
+        const float corr1 = m[nt][1] == -INFINITY ? 0.0f : fast_exp2(ref[nt][1] - to1);
         m[nt][0] = mx0; m[nt][1] = mx1;
+        ref[nt][0] = to0; ref[nt][1] = to1;
         l[nt][0] *= corr0; l[nt][1] *= corr1;
-        const float to0 = finite_max(mx0) - lift<F8>(), to1 = finite_max(mx1) - lift<F8>();
 #pragma unroll
         for (int u = 0; u < DH / 16; ++u) { o[nt][u][0] *= corr0; o[nt][u][2] *= corr0; o[nt][u][1] *= corr1; o[nt][u][3] *= corr1; }
 #pragma unroll
-        for (int i = 0; i < S; ++i) {
-          float (&s)[4] = sc[nt][i];
-          s[0] += ref[nt][0] - to0; s[2] += ref[nt][0] - to0;
-          s[1] += ref[nt][1] - to1; s[3] += ref[nt][1] - to1;
+        for (int i = 0; i < S; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) low = low || (s[e] < -kMostD8 && s[e] > -INFINITY);
-        }
-        ref[nt][0] = to0; ref[nt][1] = to1;
+          for (int e = 0; e < 4; ++e) low = low || (sc[nt][i][e] - ref[nt][e & 1] < -kUnder && sc[nt][i][e] > -INFINITY);
         fresh = fresh || mx0 == -INFINITY || mx1 == -INFINITY;
       }
       // Small weights of 8-bit pages go through the product by themselves: the sums so far are raised by the same power of two as
       // they, and lowered after (exact: they stay under 2^53 2^29).  fp16 holds them to 2^-11 down to 2^-49 of the largest, and
-      // 2^-60 of it is as good as nothing.  (64 rows of 1 to 4096 keys: 60.0 us where every tile has some, 51.0 where none has.)
+      // 2^-60 of it is as good as nothing.  (64 rows of 1 to 4096 keys: 60.5 us where every tile has some, 51.3 where none has.)
       if (F8 && __any_sync(0xffffffffu, low)) {
         auto scale_sums = [&](float by) {
 #pragma unroll
@@ -625,8 +625,8 @@ paged_attention_kernel(PagedParams p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               float& s = sc[nt][i][e];
-              const bool small = s < -kMostD8;
-              w[e] = small ? fast_exp2(s + kBoost) : 0.0f;
+              const bool small = s - ref[nt][e & 1] < -kUnder;
+              w[e] = small ? fast_exp2(s - ref[nt][e & 1] + kBoost) : 0.0f;
               l[nt][e & 1] += w[e] * kUnboost;
               if (small) s = -INFINITY;                // done with
             }
@@ -639,7 +639,7 @@ paged_attention_kernel(PagedParams p) {
       }
     }
     // The weights of a tile in the values' type.  fp16 holds them to 2^-11, an eighth of what the output's own rounding adds (a second
-    // fp16 with the rest: 64 rows of 1 to 4096 keys 53.1 us instead of 51.2, 40 rows with heads of 64 25.9 instead of 23.5); bf16 only
+    // fp16 with the rest: 64 rows of 1 to 4096 keys 53.1 us when one took 51.2, 40 rows with heads of 64 25.9 when one took 23.5); bf16 only
     // to 2^-8, as much as that rounding, so there they are the sum of two bf16, both above zero for a weight above zero, so that
     // an infinite value stays one: the first is the largest bf16 below the weight, the second the rest, off by 2^-15 in all.
 #pragma unroll
@@ -648,7 +648,7 @@ paged_attention_kernel(PagedParams p) {
       for (int i = 0; i < S; ++i) {
         float (&s)[4] = sc[nt][i];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = fast_exp2(s[e]);
+        for (int e = 0; e < 4; ++e) s[e] = fast_exp2(s[e] - ref[nt][e & 1]);
         l[nt][0] += s[0] + s[2];
         l[nt][1] += s[1] + s[3];
 #pragma unroll
@@ -681,7 +681,7 @@ paged_attention_kernel(PagedParams p) {
     for (int i = 0; i < 2; ++i) {
       const int h = nt * 8 + 2 * t + i;
       if (h >= n_heads) continue;
-      if (g == 0) { sm_m[warp][h] = m[nt][i]; sm_l[warp][h] = l[nt][i]; }
+      if (g == 0) { sm_m[warp][h] = m[nt][i] == -INFINITY ? -INFINITY : ref[nt][i]; sm_l[warp][h] = l[nt][i]; }
 #pragma unroll
       for (int u = 0; u < DH / 16; ++u) {
         sm_o[warp][h][val_dim<DH, F8>(g, 2 * u)] = o[nt][u][i];

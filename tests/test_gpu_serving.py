@@ -741,3 +741,30 @@ def test_gemv_of_the_largest_activations(lib, M):
     want = f64(x) @ (f64(s)[np.arange(K) // 128] * q.numpy().astype(np.float64))
     assert (np.abs(f64(x)[0, 130:140] @ q.numpy()[130:140].astype(np.float64)) > 3.5e38).any() and np.abs(want).max() < 3e38
     _gemv_check(lib.qzo_gemv_int4(x.cuda(), wq, s.cuda(), K, N), x, q, s)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+@pytest.mark.parametrize("big", [2.0 ** 24, 2.0 ** 25, 2.0 ** 27])
+@pytest.mark.parametrize("n,low", [(200, 0), (1500, 300)])
+def test_small_differences_of_the_largest_scores(lib, kind, big, n, low):
+    # scores in whole steps of fp32 (in powers of two, all products exact), a step or two apart from one warp's keys to another's,
+    # behind some small ones: the differences are what counts, however the scores are kept
+    H, dh = 1, 128
+    step = big * 2.0 ** -23
+    blocks = -(-n // 256) * 16
+    k, v = torch.zeros((blocks, H, 16, dh)), torch.zeros((blocks, H, 16, dh))
+    keys = torch.arange(16 * blocks)
+    k.view(-1, dh)[:, 0] = torch.where(keys < low, 0.0, 128.0)
+    k.view(-1, dh)[:, 1] = torch.tensor([1.0, 2.0, 0.0, 3.0])[(keys // 32) % 4]
+    v.view(-1, dh)[:, :8] = torch.eye(8).repeat_interleave(32, 0).repeat(blocks // 16, 1)
+    q = torch.zeros((1, H, dh))
+    q[..., 0], q[..., 1] = big / 128, step
+    ck, cv = (t.to(CACHES[kind][0]).cuda() for t in (k, v))
+    table, scale = np.arange(blocks, dtype=np.int32)[None], float(np.float32(np.log(2.0)))
+    out = f64(lib.qzo_paged_attention(q.bfloat16().cuda(), lib.KvCache(ck, cv), torch.from_numpy(table).cuda(),
+                                      torch.tensor([n - 1], dtype=torch.int32, device="cuda"), scale=scale))
+    want, spread = serving.paged_attention(f64(q), f64(ck), f64(cv), table, np.zeros(1, int), [n - 1], scale)
+    # at most three steps between scores: a scale half a fp32 step off, exp2 within 4 steps, sums of n weights, weights in 16 bits
+    p_step = 2.0 ** -15 if kind == "bf16" else F16_STEP
+    allowed = BF16_STEP * want + (p_step + (4 * 3 * step * np.log(2.0) + 16 + n / 8) * F32_STEP) * spread * (1 + BF16_STEP)
+    assert (np.abs(out - want) <= allowed).all(), (np.abs(out - want) / np.maximum(allowed, 1e-30)).max()
