@@ -768,3 +768,16 @@ def test_small_differences_of_the_largest_scores(lib, kind, big, n, low):
     p_step = 2.0 ** -15 if kind == "bf16" else F16_STEP
     allowed = BF16_STEP * want + (p_step + (4 * 3 * step * np.log(2.0) + 16 + n / 8) * F32_STEP) * spread * (1 + BF16_STEP)
     assert (np.abs(out - want) <= allowed).all(), (np.abs(out - want) / np.maximum(allowed, 1e-30)).max()
+
+
+@pytest.mark.parametrize("M", [1, 16])
+def test_gemv_of_tiny_activations(lib, M):
+    # products below fp32's smallest normal number: what is lost is steps of 2^-149, taken 2^10 higher at the end
+    K, N = 512, 72
+    x, q, s, wq = _gemv_case(lib, M, K, N, 4)
+    x, s = (x.float() * 2.0 ** -118).bfloat16(), torch.full_like(s, 4.0)
+    want = f64(x) @ (4.0 * q.numpy().astype(np.float64))
+    got = f64(lib.qzo_gemv_int4(x.cuda(), wq, s.cuda(), K, N))
+    steps = 2 * K * 4.0 * 2.0 ** (10 - 149)
+    off, size = np.abs(got - want), np.abs(f64(x)) @ np.abs(4.0 * q.numpy().astype(np.float64))
+    assert (off <= BF16_STEP * np.abs(want) + (128 + K / 128 + 16) * 2 * F32_STEP * size + steps).all() and steps < 2.0 ** -9 * np.abs(want).max()
