@@ -362,7 +362,7 @@ __host__ __device__ constexpr int ring_stages(int NT) { return NT == 1 ? 2 : 3; 
 // share one pass and the accumulators hold no padding but the heads that are missing from a tile of eight.  The k order of the
 // products is free, so a lane's 16 consecutive bytes of a key feed four k positions, and values are paired across two keys
 // by byte permutes.
-// Bound by HBM where CTAs run long (1 row of 131071 keys, 32 heads on 8: bf16 81.7 us, 6.6 TB/s; 16 rows of 100 to 2048 keys, 32
+// Bound by HBM where CTAs run long (1 row of 131071 keys, 32 heads on 8: bf16 82.0 us, 6.5 TB/s; 16 rows of 100 to 2048 keys, 32
 // key heads: 44.7 us, 6.3 TB/s; e4m3 1 row of 131071 45.9 us, 5.8 TB/s), by what a CTA needs before its first keys and after
 // its last where they run short (1 row of 4096 keys, 32 key heads: 16.5 us, 4.1 TB/s).  The rings (64 KB a CTA) keep
 // 190 KB in flight or in use on an SM; with the next tile in registers instead, 8 rows of 2048 keys took 51.5 us, now 42.1.
