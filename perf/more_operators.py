@@ -167,7 +167,7 @@ def _prepare_pool(case, g):
         from paper_2505_13430_b200 import qzo
         st["caches"] = [qzo.KvCache(st["pool"][2 * i], st["pool"][2 * i + 1]) for i in range(layers)]
         st["table_out"] = torch.empty_like(st["table"])
-        st["free_out"] = torch.full_like(st["free"], -1)
+        st["free_out"], st["n_free_out"] = torch.full_like(st["free"], -1), st["n_free"].clone()
     return st
 
 
@@ -302,7 +302,7 @@ def _compact(st):
     if own:
         from paper_2505_13430_b200 import qzo
         table, n_free, copies, count = qzo.qzo_compact_blocks(st["lens"], st["table"], st["free_out"], st["block"], st["n_blocks"], st["keep"],
-                                                              table_out=st["table_out"])
+                                                              free_count=st["n_free_out"], table_out=st["table_out"])
         qzo.qzo_copy_blocks(st["caches"], copies, count)
         return table, n_free, st["free_out"], copies, count, st["pool"]
     table, block, n, keep = st["table"], st["block"], st["n_blocks"], st["keep"]
