@@ -261,6 +261,69 @@ int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int B, int32_t
                      int32_t* d_row_seq, int32_t* d_positions, int32_t* d_slots, int32_t* d_lens_out,
                      int32_t* d_free_count_out, int* d_status, void* stream);
 
+/* Several continuations of one prompt (beams, samples, the options of a question): their selection, and the caches they share.
+ *
+ * The next beams of a beam search.  Request b has W beams, number b W + w, each with its cumulative log-probability
+ * d_scores float [B][W] (-inf: no such beam), the token it took last (d_last_tokens int32 [B][W], may be NULL) and the number of
+ * tokens generated so far (d_lengths int32 [B][W], may be NULL where length_power is 0).  A beam whose last token is end_token
+ * has ended: its one candidate is itself, token end_token, score and length as they are.  Any other has the candidates
+ *   score + x_t - log sum_u exp x_u,   t = 0 .. V - 1,   length + 1,
+ * x = row d_rows[b W + w] of d_logits (d_rows int32 [B][W]; NULL: row b W + w; a negative row: no candidates).
+ * Of all candidates of a request the W largest by score / length^length_power (a length below 1 counts as 1) come out, largest
+ * first, equal ones by beam, then by token:
+ *   d_parents int32 [B][W]: number of the beam it continues (-1 where there are no more candidates),  d_tokens int32 [B][W] (-1),
+ *   d_scores_out float [B][W] (-inf),  d_lengths_out int32 [B][W] (0; may be NULL, has to be where d_lengths is).
+ * Tokens that are not allowed have logits of -inf.  NaN and +inf logits count as -inf, and a beam with such a score or with a row from
+ * n_rows on has no candidates; each sets bit 1 of the status word.  Sums of exponentials are fp32 per thread and fp64 from there, values and ranks fp64.
+ * d_logits float [n_rows][ldl], ldl >= V (16-byte rows are read fastest); length_power from 0 to 8; W up to QZO_MAX_BEAMS.
+ * The outputs may be the inputs of the same kind (tokens for last tokens); nothing else overlaps.
+ * d_workspace: qzo_beam_select_workspace_bytes, 256-aligned; calls that may run at the same time need one each. */
+#define QZO_MAX_BEAMS 32
+int qzo_beam_select_workspace_bytes(int B, int W, int V, size_t* bytes);
+int qzo_beam_select(const float* d_logits, int64_t ldl, int n_rows, const int32_t* d_rows, const float* d_scores,
+                    const int32_t* d_last_tokens, int end_token, const int32_t* d_lengths, float length_power, int B, int W, int V,
+                    int32_t* d_parents, int32_t* d_tokens, float* d_scores_out, int32_t* d_lengths_out, void* d_workspace,
+                    size_t workspace_bytes, int* d_status, void* stream);
+
+/* Requests that go on as copies of one another.  Request r becomes a copy of what request d_parents[r] was (itself, as a rule, or
+ * another; several may copy the same one), or is empty where that is negative: d_lens_out int32 [B], d_block_table_out
+ * int32 [B][table_width] (-1 behind the blocks a request holds).  Full blocks are shared.  An unfinished last block, to which more tokens
+ * will be added, belongs to one request: the first (lowest r) that copies it keeps it, every other takes a block from the stack,
+ * in the order of the requests, and the tokens to be copied are listed, in that order: d_copies int32 [B][3] = {block to copy from, block to copy
+ * to, tokens}, -1 behind the last; d_copy_count int32 [1].  qzo_copy_blocks does the copies, before the next tokens are written.
+ * Before that, the blocks which requests held that nobody copies, and which no other holds, are pushed on the stack, in ascending order.
+ * Who holds a block is read from the tables of the B requests: they have to be all that share this pool, and each of their
+ * unfinished blocks has to be held by one of them only (as qzo_assign_slots and this call leave them).
+ * Requests that share blocks end through this call; qzo_assign_slots gives the blocks of a finished request back whoever else holds them.
+ * d_free, d_free_count as for qzo_assign_slots; n_blocks: blocks of the pool, up to QZO_MAX_POOL_BLOCKS.  d_lens_out may be d_lens and
+ * d_free_count_out may be d_free_count; no other arguments overlap (d_block_table_out is a table of its own).
+ * When it cannot be served (too few free blocks, a stack beyond its capacity, a negative length or one beyond the table, a block
+ * id outside the pool, a parent >= B), nothing is changed: tables, lengths and count are handed on as they are, no copies are listed, and bit 2 of
+ * the status word is set.  B up to QZO_MAX_REQUESTS, table_width * block_size up to 2^30. */
+#define QZO_MAX_POOL_BLOCKS 524288
+int qzo_fork_requests(const int32_t* d_lens, const int32_t* d_parents, int B, const int32_t* d_block_table, int table_width, int block_size,
+                      int n_blocks, int32_t* d_free, int free_capacity, const int32_t* d_free_count, int32_t* d_lens_out,
+                      int32_t* d_block_table_out, int32_t* d_free_count_out, int32_t* d_copies, int32_t* d_copy_count, int* d_status, void* stream);
+
+/* The blocks that requests hold move to the front of the pool.  With n blocks held, those with ids from n on move to the ids below n that nobody
+ * holds, both taken in ascending order: d_copies int32 [max_copies][3] = {from, to, block_size} (-1 behind the last),
+ * d_copy_count int32 [1], d_block_table_out int32 [B][table_width] names the new ids (-1 behind the blocks a request holds; may be
+ * d_block_table).  The pool then has `keep` blocks: d_free = keep - 1, keep - 2, ... n (the lowest ids are taken first), d_free_count_out int32 [1] =
+ * keep - n; the memory of blocks from keep on is no longer named.  qzo_copy_blocks does the copies, before anything reads the cache.
+ * Who holds a block is read from the tables, as in qzo_fork_requests.  When it cannot be done (more than keep blocks held, more
+ * copies than max_copies, a stack beyond its capacity, a negative length or one beyond the table, a block id outside the pool), the table
+ * is handed on as it is, no copies are listed, d_free and d_free_count_out stay as they are and bit 2 of the status word is set. */
+int qzo_compact_blocks(const int32_t* d_lens, int B, const int32_t* d_block_table, int table_width, int block_size, int n_blocks, int keep,
+                       int32_t* d_block_table_out, int32_t* d_free, int free_capacity, int32_t* d_free_count_out, int32_t* d_copies,
+                       int max_copies, int32_t* d_copy_count, int* d_status, void* stream);
+
+/* Copies of pages: for i = 0 .. min(*d_copy_count, max_copies) - 1, in every one of the caches (HOST array, all of one shape and type, as the
+ * layers of a model), the first d_copies[i][2] tokens of all heads of block d_copies[i][0], keys and values, become those of
+ * block d_copies[i][1], whose other tokens stay as they are.  The blocks copied to are distinct, and none of them is copied from.
+ * A block id outside the cache or a number of tokens outside [0, block_size] sets bit 1 of the status word; such a copy is left out. */
+int qzo_copy_blocks(const qzo_kv_cache* h_caches, int n_caches, const int32_t* d_copies, const int32_t* d_copy_count, int max_copies,
+                    int* d_status, void* stream);
+
 /* ------------------------------------------------------------------------------------
  * Model-level entry points
  * ---------------------------------------------------------------------------------- */

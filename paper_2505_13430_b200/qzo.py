@@ -31,6 +31,7 @@ EXPORTS = (
     "qzo_joint_workspace_bytes", "qzo_enable_joint_spsa", "qzo_perturbed_gemm_table16", "qzo_debug_gemm_wait_expiry",
     "qzo_gemv_int4", "qzo_rope_table", "qzo_qk_norm_rope_cache", "qzo_paged_attention_workspace_bytes", "qzo_paged_attention",
     "qzo_assign_slots", "qzo_decode", "qzo_decode_requests",
+    "qzo_beam_select_workspace_bytes", "qzo_beam_select", "qzo_fork_requests", "qzo_compact_blocks", "qzo_copy_blocks",
 )
 
 
@@ -116,6 +117,11 @@ def _load():
         "qzo_assign_slots": (ci, [vp, vp, ci, vp, ci, ci, vp, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp]),
         "qzo_decode_requests": (ci, [vp, P(KvCacheDesc), vp, vp, vp, ci, vp, ci, vp, ci, vp, ci, vp, vp, vp]),
         "qzo_decode": (ci, [vp, P(KvCacheDesc), vp, vp, vp, vp, ci, vp, ci, ci, vp]),
+        "qzo_beam_select_workspace_bytes": (ci, [ci, ci, ci, P(sz)]),
+        "qzo_beam_select": (ci, [vp, i64, ci, vp, vp, vp, ci, vp, cf, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp, vp]),
+        "qzo_fork_requests": (ci, [vp, vp, ci, vp, ci, ci, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "qzo_compact_blocks": (ci, [vp, ci, vp, ci, ci, ci, ci, vp, vp, ci, vp, vp, ci, vp, vp, vp]),
+        "qzo_copy_blocks": (ci, [P(KvCacheDesc), ci, vp, vp, ci, vp, vp]),
         "qzo_profile_gemms": (ci, [vp, ci]),
         "qzo_profile_read": (ci, [vp, P(i64), P(ctypes.c_double), P(ctypes.c_double)]),
     }
@@ -298,6 +304,9 @@ def qzo_update_scales_flat(scales, seed, index_base, lr, g, clip):
 # limits of qzo_gemv_int4 (above, qzo_perturbed_gemm at sign 0) and qzo_assign_slots, for a program that divides its work by them
 GEMV_MAX_ROWS = 16
 MAX_REQUESTS = 4096
+# of qzo_beam_select, and of the calls that read from the tables who holds a block
+MAX_BEAMS = 32
+MAX_POOL_BLOCKS = 524288
 
 
 _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
@@ -483,6 +492,119 @@ def qzo_assign_slots(lens, new, block_table, free, free_count, block_size, max_r
     if rc:
         _check(rc, "qzo_assign_slots")
     return row_seq, positions, slots
+
+
+def qzo_beam_select_workspace_bytes(B, W, V):
+    out = ctypes.c_size_t(0)
+    _check(_lib.qzo_beam_select_workspace_bytes(B, W, V, ctypes.byref(out)), "qzo_beam_select_workspace_bytes")
+    return out.value
+
+
+def qzo_beam_select(logits, scores, rows=None, last_tokens=None, end_token=-1, lengths=None, length_power=0.0, parents=None, tokens=None,
+                    scores_out=None, lengths_out=None, workspace=None, status=None):
+    """The next beams of every request: logits float32 [rows][V] (any row stride), scores float32 [B][W] (-inf = no such beam), rows int32 [B][W]
+    (the row of each beam, negative = none) or None (row b * W + w), last_tokens int32 [B][W] or None (beams that took end_token have
+    ended), lengths int32 [B][W] or None -> (parents, tokens int32 [B][W], scores float32 [B][W], lengths int32 [B][W] or None), best first by
+    score / length**length_power; -1, -1, -inf, 0 where there are no more candidates.  parents are numbers b * W + w."""
+    dev = _device_now()
+    B, W = scores.shape
+    n_rows, V = logits.shape
+    ldl, one = logits.stride()
+    assert logits.dtype is _F32 and (one == 1 or V == 1) and logits.get_device() == dev, "logits: expects float32 [rows][V] on the current device"
+    _floats(dev, B * W, scores, "scores")
+    _ints(dev, B * W, *(t for t in (rows, last_tokens, lengths, parents, tokens, lengths_out) if t is not None))
+    if parents is None:
+        parents = scores.new_empty(B, W, dtype=_I32)
+    if tokens is None:
+        tokens = scores.new_empty(B, W, dtype=_I32)
+    if scores_out is None:
+        scores_out = scores.new_empty(B, W)
+    else:
+        _floats(dev, B * W, scores_out, "scores_out")
+    if lengths is not None and lengths_out is None:
+        lengths_out = scores.new_empty(B, W, dtype=_I32)
+    if workspace is None:
+        workspace = scores.new_empty(qzo_beam_select_workspace_bytes(B, W, V), dtype=_U8)
+    assert workspace.is_contiguous() and workspace.get_device() == dev, "workspace: contiguous, on the current device"
+    opt = lambda t: None if t is None else t.data_ptr()
+    rc = _lib.qzo_beam_select(logits.data_ptr(), ldl if n_rows > 1 else V, n_rows, opt(rows), scores.data_ptr(), opt(last_tokens), end_token, opt(lengths),
+                              length_power, B, W, V, parents.data_ptr(), tokens.data_ptr(), scores_out.data_ptr(), opt(lengths_out),
+                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), None if status is None else _status(dev, status),
+                              _raw_stream(dev))
+    if rc:
+        _check(rc, "qzo_beam_select")
+    return parents, tokens, scores_out, lengths_out
+
+
+def qzo_fork_requests(lens, parents, block_table, free, free_count, block_size, n_blocks, table_out=None, lens_out=None, free_count_out=None,
+                      copies=None, copy_count=None, status=None):
+    """Requests go on as copies of one another (all int32): lens [B], parents [B] (any shape; negative = the request ends), block_table [B][width],
+    free = stack of free blocks, free_count [1], n_blocks = blocks of the pool.  Lengths and count are new tensors unless given (they may be the
+    inputs); the table is always another one.  -> (table_out, lens_out, free_count_out, copies [B][3], copy_count [1]); the copies are for
+    qzo_copy_blocks."""
+    dev = _device_now()
+    B, width = block_table.shape
+    _ints(dev, B, lens, parents)
+    _ints(dev, 1, block_table, free, free_count)
+    if table_out is None:
+        table_out = torch.empty_like(block_table)
+    else:
+        assert table_out.shape == block_table.shape, "table_out: as block_table"
+        _ints(dev, 1, table_out)
+    if lens_out is None:
+        lens_out = lens.new_empty(B)
+    if free_count_out is None:
+        free_count_out = lens.new_empty(1)
+    if copies is None:
+        copies = lens.new_empty(B, 3)
+    if copy_count is None:
+        copy_count = lens.new_empty(1)
+    _ints(dev, B, lens_out)
+    _ints(dev, 1, free_count_out, copy_count)
+    _ints(dev, 3 * B, copies)
+    rc = _lib.qzo_fork_requests(lens.data_ptr(), parents.data_ptr(), B, block_table.data_ptr(), width, block_size, n_blocks, free.data_ptr(), free.numel(),
+                                free_count.data_ptr(), lens_out.data_ptr(), table_out.data_ptr(), free_count_out.data_ptr(), copies.data_ptr(),
+                                copy_count.data_ptr(), None if status is None else _status(dev, status), _raw_stream(dev))
+    if rc:
+        _check(rc, "qzo_fork_requests")
+    return table_out, lens_out, free_count_out, copies, copy_count
+
+
+def qzo_compact_blocks(lens, block_table, free, block_size, n_blocks, keep, free_count=None, table_out=None, copies=None, copy_count=None, status=None):
+    """The blocks that requests hold move to the front of the pool, which then has `keep` blocks (all int32): lens [B], block_table [B][width] (written in
+    place unless table_out is given), free = the stack of free blocks, written anew, free_count [1] = its count, written too ->
+    (table, free_count, copies [n][3], copy_count [1]); the copies are for qzo_copy_blocks."""
+    dev = _device_now()
+    B, width = block_table.shape
+    if table_out is None:
+        table_out = block_table
+    assert table_out.shape == block_table.shape, "table_out: as block_table"
+    if free_count is None:
+        free_count = lens.new_full((1,), -1)
+    if copies is None:
+        copies = lens.new_empty(n_blocks, 3)
+    if copy_count is None:
+        copy_count = lens.new_empty(1)
+    _ints(dev, B, lens)
+    _ints(dev, 1, block_table, table_out, free, free_count, copies, copy_count)
+    rc = _lib.qzo_compact_blocks(lens.data_ptr(), B, block_table.data_ptr(), width, block_size, n_blocks, keep, table_out.data_ptr(), free.data_ptr(),
+                                 free.numel(), free_count.data_ptr(), copies.data_ptr(), copies.numel() // 3, copy_count.data_ptr(),
+                                 None if status is None else _status(dev, status), _raw_stream(dev))
+    if rc:
+        _check(rc, "qzo_compact_blocks")
+    return table_out, free_count, copies, copy_count
+
+
+def qzo_copy_blocks(caches, copies, copy_count, status=None):
+    """The listed copies of pages (int32 [n][3]: from, to, tokens; copy_count int32 [1]: how many) in every one of the caches (list of KvCache of
+    one shape and type, as the layers of a model)."""
+    dev = _device_now()
+    assert len(caches) > 0 and all(c.device == dev for c in caches), "caches: expects KvCache on the current device"
+    _ints(dev, 1, copies, copy_count)
+    rc = _lib.qzo_copy_blocks((KvCacheDesc * len(caches))(*[c.desc for c in caches]), len(caches), copies.data_ptr(), copy_count.data_ptr(),
+                              copies.numel() // 3, None if status is None else _status(dev, status), _raw_stream(dev))
+    if rc:
+        _check(rc, "qzo_copy_blocks")
 
 
 def make_desc(cfg):
