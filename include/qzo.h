@@ -324,6 +324,22 @@ int qzo_compact_blocks(const int32_t* d_lens, int B, const int32_t* d_block_tabl
 int qzo_copy_blocks(const qzo_kv_cache* h_caches, int n_caches, const int32_t* d_copies, const int32_t* d_copy_count, int max_copies,
                     int* d_status, void* stream);
 
+/* qzo_paged_attention for rows that share the beginning of their cache: the rows of a group, d_group_rows[i] .. d_group_rows[i + 1] - 1
+ * (int32 [n_groups + 1], ascending, from 0 to R at most; rows outside of all groups and groups without rows are allowed), have the
+ * first d_prefix_len[i] tokens of request d_prefix_seq[i] (int32 [n_groups] each) as the first tokens of their own requests, which
+ * may name the same blocks for them or hold copies.  Those keys and values are read once for a group and key head, not once for every row:
+ * through the table of request d_prefix_seq[i], in whole runs of 64 tokens; what remains of them, and the rows' own tokens, through the
+ * rows' own tables.  A row that does not see the whole prefix reads everything through its own table, as does every row of a group whose
+ * request or length is out of range (bit 1 of the status word).  Bounds that do not ascend within 0 .. R make no groups (bit 1 too).
+ * Everything else as in qzo_paged_attention, the meaning of every output among it: the sums are those, taken in another order.  Bit 0 of the
+ * status word: a bounded wait inside a kernel ran out, and the output means nothing.
+ * n_blocks * block_size * n_kv_heads < 2^31.  d_workspace: qzo_shared_prefix_attention_workspace_bytes, 256-aligned, never 0. */
+int qzo_shared_prefix_attention_workspace_bytes(int R, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes);
+int qzo_shared_prefix_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache, const int32_t* d_block_table, int n_seqs, int table_width,
+                                const int32_t* d_row_seq, const int32_t* d_positions, const int32_t* d_group_rows, const int32_t* d_prefix_seq,
+                                const int32_t* d_prefix_len, int n_groups, float scale, void* d_out_bf16, int ldo, int R, int n_heads,
+                                void* d_workspace, size_t workspace_bytes, int* d_status, void* stream);
+
 /* ------------------------------------------------------------------------------------
  * Model-level entry points
  * ---------------------------------------------------------------------------------- */

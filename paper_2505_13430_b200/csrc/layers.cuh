@@ -63,6 +63,7 @@ int launch_bf16_gemm_f32out(const __nv_bfloat16* d_x, const __nv_bfloat16* d_w, 
 int launch_gemv_group(const __nv_bfloat16* d_x, int ldx, int M, int K, const GemmLinear* lins, int n_lin, cudaStream_t st);
 
 // paged.cu
+struct PrefixGroups;   // groups of rows that share the beginning of their cache (paged.cuh)
 bool cache_ok(const qzo_kv_cache* c);
 int launch_qk_norm_rope_cache(const __nv_bfloat16* q, int ldq, const __nv_bfloat16* k, int ldk, const __nv_bfloat16* v, int ldv,
                               const float* q_gain, const float* k_gain, float norm_eps, const float* table, int max_pos,
@@ -73,5 +74,6 @@ size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len);
 // fewer_splits: a workspace that is too small for the splits of paged_attention_bytes gets as many as it holds
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
                            const int32_t* row_seq, const int32_t* positions, const int32_t* slots, float scale, __nv_bfloat16* out,
-                           int ldo, int R, int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st);
+                           int ldo, int R, int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st,
+                           const PrefixGroups* groups = nullptr);
 }  // namespace qzo

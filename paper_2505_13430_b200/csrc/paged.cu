@@ -4,6 +4,7 @@
 #include "launch.cuh"
 #include "layers.cuh"
 #include "mma.cuh"
+#include "paged.cuh"
 
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -14,8 +15,6 @@
 
 namespace qzo {
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f;
 
 // =========================================================================================
 // Head norms, rotation, cache write
@@ -202,44 +201,6 @@ qk_norm_rope_cache_kernel(RopeCacheParams p) {
 constexpr int kStageBytes = 8192;                      // of a warp's ring: 4 KB of keys and 4 KB of values
 constexpr int kSub = 16;                               // keys of one matrix tile; a block of the cache holds whole ones
 
-struct PagedParams {
-  const __nv_bfloat16* q;
-  int ldq;
-  const void *ck, *cv;
-  const int32_t* table;
-  int n_seqs, width;
-  const int32_t *row_seq, *positions, *slots;          // slots may be null
-  float scale_log2e, v_scale;                          // the keys' scale is in the first
-  __nv_bfloat16* out;
-  int ldo, R, H, Hkv, G, chunks, splits, min_keys, round_keys, n_blocks, log2_block;
-  float *part_o, *part_ml;                             // [R][H][splits][DH], [R][H][splits][2]
-  int* status;
-};
-
-// Keys of split s of a row that sees len keys: [s * per, min(len, (s + 1) * per)), per at least the launch's minimum.
-__device__ __forceinline__ int split_keys(const PagedParams& p, int len) {
-  return max(p.min_keys, ((len + p.splits - 1) / p.splits + p.round_keys - 1) / p.round_keys * p.round_keys);
-}
-// Number of keys a row sees, 0 for padding; seq receives its request.  One thread reports what is out of range.
-__device__ __forceinline__ int row_keys(const PagedParams& p, int row, int* seq, bool report) {
-  const int pos = p.positions[row], s = p.row_seq ? p.row_seq[row] : row;
-  if (pos < 0 || (p.slots && p.slots[row] < 0)) return 0;
-  *seq = s;
-  const int most = p.width << p.log2_block;
-  const bool bad_seq = s < 0 || s >= p.n_seqs;
-  if ((bad_seq || pos >= most) && report && p.status) atomicOr(p.status, kStatusBadToken);
-  return bad_seq ? 0 : min(pos, most - 1) + 1;
-}
-
-// A row none of whose keys has a score above -inf (no key at all, or only blocks that are out of range) gives zeros.
-__device__ __forceinline__ float inverse_sum(const PagedParams& p, float sum) { return sum == 0.0f ? 0.0f : p.v_scale / sum; }
-
-// 2^x, relative error 2^-22, 0 for -inf
-__device__ __forceinline__ float fast_exp2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // four codes as two fp16 pairs (exact)
 __device__ __forceinline__ void e4m3x4_to_f16x2(uint32_t four, uint32_t& lo, uint32_t& hi) {
   asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(four));
@@ -336,11 +297,6 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// The fp32 number next below w > 0 (0 for 0), as bits: its upper half is the largest bf16 below w
-__device__ __forceinline__ uint32_t below(float w) { return (uint32_t)__viaddmax_s32(__float_as_int(w), -1, 0); }
-__device__ __forceinline__ float upper_half(uint32_t bits) { return __uint_as_float(bits & 0xffff0000u); }
-// What scores are taken relative to: their maximum, or 0 where there is none (all -inf).
-__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 
 // A weight is 2^(score - reference), the reference being the maximum so far less lift().  The maximum is only raised when a score
 // passes it by kSlack: until then a tile needs neither the maximum over its keys nor a rescaling, and weights that reach 2^8
@@ -366,7 +322,8 @@ __host__ __device__ constexpr int ring_stages(int NT) { return NT == 1 ? 2 : 3; 
 // key heads: 44.7 us, 6.3 TB/s; e4m3 1 row of 131071 45.9 us, 5.8 TB/s), by what a CTA needs before its first keys and after
 // its last where they run short (1 row of 4096 keys, 32 key heads: 16.5 us, 4.1 TB/s).  The rings (64 KB a CTA) keep
 // 190 KB in flight or in use on an SM; with the next tile in registers instead, 8 rows of 2048 keys took 51.5 us, now 42.1.
-template <int DH, int NT, bool F8, int W>
+// GROUPS: rows of a group start behind the prefix that the group's rows share, and leave their part to the join.
+template <int DH, int NT, bool F8, int W, bool GROUPS>
 __global__ void __launch_bounds__(W * 32, 4 * resident_ctas(NT) / W)
 paged_attention_kernel(PagedParams p) {
   using Lay = Layout<DH, F8>;
@@ -400,8 +357,9 @@ paged_attention_kernel(PagedParams p) {
   }
   int seq = 0;
   const int len = row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
-  const int per = split_keys(p, len);
-  const int k0 = split * per, k1 = min(len, k0 + per);
+  const int first = GROUPS ? row_prefix(p, row, len) : 0;
+  const int per = split_keys(p, len - first);
+  const int k0 = first + split * per, k1 = min(len, k0 + per);
   if (k0 >= k1) {
     if (len == 0 && split == 0)
       for (int i = threadIdx.x; i < n_heads * DH / 8; i += W * 32)
@@ -704,13 +662,13 @@ paged_attention_kernel(PagedParams p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) val[e] = fmaf(c, sm_o[w][h][d + e], val[e]);
     }
-    if (len <= per) {                                  // one split: nothing to join
+    if (len <= per && first == 0) {                    // one split: nothing to join
       const float f = inverse_sum(p, sum);
 #pragma unroll
       for (int e = 0; e < 4; ++e) val[e] *= f;
       *reinterpret_cast<uint2*>(p.out + (size_t)row * p.ldo + (size_t)(head0 + h) * DH + d) = pack4_bf16(val);
     } else {
-      const size_t at = ((size_t)row * p.H + head0 + h) * p.splits + split;
+      const size_t at = ((size_t)row * p.H + head0 + h) * (GROUPS ? p.prefix_splits + p.splits : p.splits) + (GROUPS ? p.prefix_splits + split : split);
       *reinterpret_cast<float4*>(p.part_o + at * DH + d) = make_float4(val[0], val[1], val[2], val[3]);
       if (d == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(mx, sum);
     }
@@ -719,7 +677,7 @@ paged_attention_kernel(PagedParams p) {
 
 // Joins the splits of a row's head: a CTA's COLS columns of threads take four dimensions each, its ROWS rows of threads
 // every so many of the splits; the rows are then summed in their order.  COLS * 4 < DH: several CTAs share a head.
-template <int DH, int COLS, int ROWS>
+template <int DH, int COLS, int ROWS, bool GROUPS>
 __global__ void __launch_bounds__(COLS * ROWS)
 paged_join_kernel(PagedParams p) {
   constexpr int kThreads = COLS * ROWS, kParts = DH / 4 / COLS;
@@ -732,11 +690,14 @@ paged_join_kernel(PagedParams p) {
   const int row = (int)(item / p.H), h = (int)(item % p.H);
   int seq = 0;
   const int len = row_keys(p, row, &seq, false);
-  const int per = split_keys(p, len), n = (len + per - 1) / per;
-  if (n <= 1) return;                                  // written already
-  const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + item * p.splits;
+  const int first = GROUPS ? row_prefix(p, row, len) : 0, n_first = first ? (first + prefix_keys(p, first) - 1) / prefix_keys(p, first) : 0;
+  const int own = len - first, per = split_keys(p, own), n = n_first + (own > 0 ? (own + per - 1) / per : 0);
+  if (n <= 1 && n_first == 0) return;                  // written already
+  const int stride = GROUPS ? p.prefix_splits + p.splits : p.splits;
+  auto place = [&](int s) { return GROUPS && s >= n_first ? s - n_first + p.prefix_splits : s; };      // of part s of n
+  const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + item * stride;
   float mx = -INFINITY;
-  for (int s = threadIdx.x; s < n; s += kThreads) mx = fmaxf(mx, ml[s].x);
+  for (int s = threadIdx.x; s < n; s += kThreads) mx = fmaxf(mx, ml[place(s)].x);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
   if ((threadIdx.x & 31) == 0) part_max[threadIdx.x >> 5] = mx;
@@ -744,18 +705,18 @@ paged_join_kernel(PagedParams p) {
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) mx = fmaxf(mx, part_max[w]);
   const float ref = finite_max(mx);
-  for (int s = threadIdx.x; s < n; s += kThreads) weight[s] = fast_exp2(ml[s].x - ref);
+  for (int s = threadIdx.x; s < n; s += kThreads) weight[s] = fast_exp2(ml[place(s)].x - ref);
   __syncthreads();
   const int c = threadIdx.x % COLS, r = threadIdx.x / COLS, d0 = 4 * (c + COLS * (blockIdx.x % kParts));
-  const float4* o = reinterpret_cast<const float4*>(p.part_o + item * p.splits * DH + d0);
+  const float4* o = reinterpret_cast<const float4*>(p.part_o + item * stride * DH + d0);
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float sum = 0.0f;
 #pragma unroll 4
   for (int s = r; s < n; s += ROWS) {
     const float w = weight[s];
-    const float4 x = o[(size_t)s * (DH / 4)];
+    const float4 x = o[(size_t)place(s) * (DH / 4)];
     v.x = fmaf(w, x.x, v.x); v.y = fmaf(w, x.y, v.y); v.z = fmaf(w, x.z, v.z); v.w = fmaf(w, x.w, v.w);
-    sum = fmaf(w, ml[s].y, sum);
+    sum = fmaf(w, ml[place(s)].y, sum);
   }
   part[r][c] = v;
   if (c == 0) part_sum[r] = sum;
@@ -802,30 +763,38 @@ Plan attention_plan(int64_t R, int Hkv, int G, int subs, int64_t max_len) {
   const int64_t even = R > 1 ? std::min<int64_t>(max_len / (2048 * subs), 8 * slots / ctas) : 1;
   return {(int)std::max<int64_t>(1, std::max(fill, even)), 0, (even > fill ? 2048 : 128) * subs};
 }
-template <int DH, int NT, bool F8, int W>
+template <int DH, int NT, bool F8, int W, bool GROUPS>
 int run_attention_w(const PagedParams& p, cudaStream_t st) {
   const dim3 grid((unsigned)((int64_t)p.R * p.Hkv * p.chunks), p.splits);
   constexpr int smem = std::max(W * ring_stages(NT) * kStageBytes, W * 8 * NT * (DH + 1) * (int)sizeof(float));
   {
     static std::atomic<unsigned long long> allowed{0};
-    QZO_CUDA_TRY(allow_dynamic_smem(paged_attention_kernel<DH, NT, F8, W>, smem, allowed));
+    QZO_CUDA_TRY(allow_dynamic_smem(paged_attention_kernel<DH, NT, F8, W, GROUPS>, smem, allowed));
   }
-  return launch_serving(paged_attention_kernel<DH, NT, F8, W>, grid, dim3(W * 32), smem, 1, st, p);
+  return launch_serving(paged_attention_kernel<DH, NT, F8, W, GROUPS>, grid, dim3(W * 32), smem, 1, st, p);
 }
 
-template <int DH, int COLS, int ROWS>
+template <int DH, int COLS, int ROWS, bool GROUPS>
 int run_join(const PagedParams& p, cudaStream_t st) {
-  return launch_serving(paged_join_kernel<DH, COLS, ROWS>, dim3((unsigned)((int64_t)p.R * p.H * (DH / 4 / COLS))),
-                                     dim3(COLS * ROWS), p.splits * sizeof(float), 1, st, p);
+  return launch_serving(paged_join_kernel<DH, COLS, ROWS, GROUPS>, dim3((unsigned)((int64_t)p.R * p.H * (DH / 4 / COLS))),
+                        dim3(COLS * ROWS), (p.splits + p.prefix_splits) * sizeof(float), 1, st, p);
 }
 
-template <int DH, bool F8>
+template <int DH, bool F8, bool GROUPS>
 int run_attention(const PagedParams& p, bool wide, cudaStream_t st) {
-  if (p.G <= 8) QZO_TRY(wide ? (run_attention_w<DH, 1, F8, 8>(p, st)) : (run_attention_w<DH, 1, F8, 4>(p, st)));
-  else QZO_TRY(wide ? (run_attention_w<DH, 2, F8, 8>(p, st)) : (run_attention_w<DH, 2, F8, 4>(p, st)));
-  if (p.splits <= 1) return QZO_OK;
+  if (p.G <= 8) QZO_TRY(wide ? (run_attention_w<DH, 1, F8, 8, GROUPS>(p, st)) : (run_attention_w<DH, 1, F8, 4, GROUPS>(p, st)));
+  else QZO_TRY(wide ? (run_attention_w<DH, 2, F8, 8, GROUPS>(p, st)) : (run_attention_w<DH, 2, F8, 4, GROUPS>(p, st)));
+  const int splits = p.splits + p.prefix_splits;
+  if (splits <= 1) return QZO_OK;
   // many splits of few heads: a head's dimensions go to several CTAs, so that a thread adds up fewer of them
-  return p.splits > 16 ? run_join<DH, 8, 32>(p, st) : run_join<DH, DH / 4, 4>(p, st);
+  return splits > 16 ? run_join<DH, 8, 32, GROUPS>(p, st) : run_join<DH, DH / 4, 4, GROUPS>(p, st);
+}
+
+template <bool GROUPS>
+int run_attention_of(const PagedParams& p, const qzo_kv_cache& c, bool wide, cudaStream_t st) {
+  const bool f8 = c.dtype == QZO_DTYPE_E4M3;
+  if (c.head_dim == 128) return f8 ? run_attention<128, true, GROUPS>(p, wide, st) : run_attention<128, false, GROUPS>(p, wide, st);
+  return f8 ? run_attention<64, true, GROUPS>(p, wide, st) : run_attention<64, false, GROUPS>(p, wide, st);
 }
 
 }  // namespace
@@ -867,28 +836,45 @@ size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
   return splits > 1 ? (size_t)R * H * splits * (dh + 2) * sizeof(float) : 0;
 }
 
+// Bytes of the partial results for the prefixes of n_groups groups and the rows' own keys, splits of each
+size_t shared_prefix_bytes(int R, int n_groups, int H, int Hkv, int dh, int max_len) {
+  const int splits = prefix_splits(R, n_groups, H / Hkv, Hkv, max_len) + attention_plan(R, Hkv, H / Hkv, 128 / dh, max_len).splits;
+  return (size_t)R * H * splits * (dh + 2) * sizeof(float);
+}
+
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
                            const int32_t* row_seq, const int32_t* positions, const int32_t* slots, float scale, __nv_bfloat16* out,
-                           int ldo, int R, int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st) {
+                           int ldo, int R, int H, void* ws, size_t ws_bytes, bool fewer_splits, int* status, cudaStream_t st,
+                           const PrefixGroups* groups) {
   const int G = H / c.n_kv_heads, chunks = head_chunks(G), max_len = width * c.block_size;
   if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
   const int subs = 256 / (c.head_dim * (c.dtype == QZO_DTYPE_E4M3 ? 1 : 2));
   const Plan plan = attention_plan(R, c.n_kv_heads, G, subs, max_len);
-  int splits = plan.splits;
+  int splits = plan.splits, first_splits = groups ? prefix_splits(R, groups->n, G, c.n_kv_heads, max_len) : 0;
+  if (groups && prefix_ctas(R, groups->n, G, c.n_kv_heads) * first_splits > INT32_MAX) return QZO_ERR_BAD_ARG;
+  if (groups && (int64_t)c.n_blocks * c.block_size * c.n_kv_heads > INT32_MAX) return QZO_ERR_BAD_ARG;      // rows that a tensor map can name
   const size_t per_split = (size_t)R * H * (c.head_dim + 2) * sizeof(float);
-  if (fewer_splits)
-    splits = (int)std::max<size_t>(1, std::min<size_t>(splits, ws_bytes / per_split));
-  else if (const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
+  if (fewer_splits) {
+    const size_t room = ws_bytes / per_split;
+    if (groups) {
+      if (room < 2) return QZO_ERR_WORKSPACE;
+      first_splits = (int)std::min<size_t>(first_splits, room - 1);
+    }
+    splits = (int)std::max<size_t>(1, std::min<size_t>(splits, room - first_splits));
+  } else if (const size_t need = groups ? (first_splits + splits) * per_split : paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0) {
     if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
-  PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, slots, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
-                R, H, c.n_kv_heads, G, chunks, splits, plan.min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status};
-  if (splits > 1) {
-    p.part_o = (float*)ws;
-    p.part_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
   }
-  const bool f8 = c.dtype == QZO_DTYPE_E4M3;
-  if (c.head_dim == 128) return f8 ? run_attention<128, true>(p, plan.wide, st) : run_attention<128, false>(p, plan.wide, st);
-  return f8 ? run_attention<64, true>(p, plan.wide, st) : run_attention<64, false>(p, plan.wide, st);
+  PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, slots, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
+                R, H, c.n_kv_heads, G, chunks, splits, plan.min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status,
+                {nullptr, nullptr, nullptr, 0}, first_splits};
+  if (splits + first_splits > 1) {
+    p.part_o = (float*)ws;
+    p.part_ml = p.part_o + (size_t)R * H * (splits + first_splits) * c.head_dim;
+  }
+  if (!groups) return run_attention_of<false>(p, c, plan.wide, st);
+  p.groups = *groups;
+  QZO_TRY(launch_prefix_attention(p, c, st));
+  return run_attention_of<true>(p, c, plan.wide, st);
 }
 
 }  // namespace qzo
@@ -896,6 +882,17 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
 using namespace qzo;
 
 extern "C" {
+
+static int check_attention(const void* q, int ldq, const qzo_kv_cache* cache, int n_seqs, int table_width, const int32_t* row_seq, float scale,
+                           const void* out, int ldo, int R, int n_heads) {
+  if (!cache_ok(cache) || R <= 0 || n_seqs <= 0 || table_width <= 0 || n_heads <= 0 || n_heads % cache->n_kv_heads) return QZO_ERR_BAD_ARG;
+  if (!row_seq && R > n_seqs) return QZO_ERR_BAD_ARG;
+  if ((int64_t)table_width * cache->block_size > kMostKeys || !(scale >= 0x1p-40f && scale <= 0x1p40f)) return QZO_ERR_BAD_ARG;
+  const int64_t wq = (int64_t)n_heads * cache->head_dim;
+  if (ldq < wq || ldo < wq || (ldq % 8) || (ldo % 8)) return QZO_ERR_BAD_ARG;
+  if (((uintptr_t)q & 15) || ((uintptr_t)out & 15)) return QZO_ERR_BAD_ARG;
+  return QZO_OK;
+}
 
 int qzo_rope_table(float* d_table, int max_pos, int head_dim, float theta, void* stream) {
   if (!d_table || max_pos <= 0 || (head_dim != 64 && head_dim != 128) || !(theta > 0.0f) || !isfinite(theta)) return QZO_ERR_BAD_ARG;
@@ -936,16 +933,32 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
                         int ldo, int R, int n_heads, void* d_workspace, size_t workspace_bytes, int* d_status, void* stream) {
   if (!d_q_bf16 || !d_block_table || !d_positions || !d_out_bf16) return QZO_ERR_BAD_ARG;
   if (!words_aligned(d_block_table, d_row_seq, d_positions, d_status)) return QZO_ERR_BAD_ARG;
-  if (!cache_ok(cache) || R <= 0 || n_seqs <= 0 || table_width <= 0 || n_heads <= 0 || n_heads % cache->n_kv_heads) return QZO_ERR_BAD_ARG;
-  if (!d_row_seq && R > n_seqs) return QZO_ERR_BAD_ARG;
-  if ((int64_t)table_width * cache->block_size > kMostKeys || !(scale >= 0x1p-40f && scale <= 0x1p40f)) return QZO_ERR_BAD_ARG;
-  const int64_t wq = (int64_t)n_heads * cache->head_dim;
-  if (ldq < wq || ldo < wq || (ldq % 8) || (ldo % 8)) return QZO_ERR_BAD_ARG;
-  if (((uintptr_t)d_q_bf16 & 15) || ((uintptr_t)d_out_bf16 & 15)) return QZO_ERR_BAD_ARG;
+  QZO_TRY(check_attention(d_q_bf16, ldq, cache, n_seqs, table_width, d_row_seq, scale, d_out_bf16, ldo, R, n_heads));
   QZO_TRY(check_device());
   return launch_paged_attention((const __nv_bfloat16*)d_q_bf16, ldq, *cache, d_block_table, n_seqs, table_width, d_row_seq, d_positions,
                                 nullptr, scale, (__nv_bfloat16*)d_out_bf16, ldo, R, n_heads, d_workspace, workspace_bytes, false,
                                 d_status, (cudaStream_t)stream);
+}
+
+int qzo_shared_prefix_attention_workspace_bytes(int R, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes) {
+  if (!bytes || R <= 0 || n_groups <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || max_len > kMostKeys) return QZO_ERR_BAD_ARG;
+  if (head_dim != 64 && head_dim != 128) return QZO_ERR_BAD_ARG;
+  *bytes = shared_prefix_bytes(R, n_groups, n_heads, n_kv_heads, head_dim, max_len);
+  return QZO_OK;
+}
+
+int qzo_shared_prefix_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache, const int32_t* d_block_table, int n_seqs, int table_width,
+                                const int32_t* d_row_seq, const int32_t* d_positions, const int32_t* d_group_rows, const int32_t* d_prefix_seq,
+                                const int32_t* d_prefix_len, int n_groups, float scale, void* d_out_bf16, int ldo, int R, int n_heads,
+                                void* d_workspace, size_t workspace_bytes, int* d_status, void* stream) {
+  if (!d_q_bf16 || !d_block_table || !d_positions || !d_out_bf16 || !d_group_rows || !d_prefix_seq || !d_prefix_len || n_groups <= 0) return QZO_ERR_BAD_ARG;
+  if (!words_aligned(d_block_table, d_row_seq, d_positions, d_group_rows, d_prefix_seq, d_prefix_len, d_status)) return QZO_ERR_BAD_ARG;
+  QZO_TRY(check_attention(d_q_bf16, ldq, cache, n_seqs, table_width, d_row_seq, scale, d_out_bf16, ldo, R, n_heads));
+  QZO_TRY(check_device());
+  const PrefixGroups groups{d_group_rows, d_prefix_seq, d_prefix_len, n_groups};
+  return launch_paged_attention((const __nv_bfloat16*)d_q_bf16, ldq, *cache, d_block_table, n_seqs, table_width, d_row_seq, d_positions,
+                                nullptr, scale, (__nv_bfloat16*)d_out_bf16, ldo, R, n_heads, d_workspace, workspace_bytes, false,
+                                d_status, (cudaStream_t)stream, &groups);
 }
 
 }  // extern "C"

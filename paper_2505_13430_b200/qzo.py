@@ -32,6 +32,7 @@ EXPORTS = (
     "qzo_gemv_int4", "qzo_rope_table", "qzo_qk_norm_rope_cache", "qzo_paged_attention_workspace_bytes", "qzo_paged_attention",
     "qzo_assign_slots", "qzo_decode", "qzo_decode_requests",
     "qzo_beam_select_workspace_bytes", "qzo_beam_select", "qzo_fork_requests", "qzo_compact_blocks", "qzo_copy_blocks",
+    "qzo_shared_prefix_attention_workspace_bytes", "qzo_shared_prefix_attention",
 )
 
 
@@ -121,6 +122,8 @@ def _load():
         "qzo_beam_select": (ci, [vp, i64, ci, vp, vp, vp, ci, vp, cf, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp, vp]),
         "qzo_fork_requests": (ci, [vp, vp, ci, vp, ci, ci, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp, vp]),
         "qzo_compact_blocks": (ci, [vp, ci, vp, ci, ci, ci, ci, vp, vp, ci, vp, vp, ci, vp, vp, vp]),
+        "qzo_shared_prefix_attention_workspace_bytes": (ci, [ci, ci, ci, ci, ci, ci, P(sz)]),
+        "qzo_shared_prefix_attention": (ci, [vp, ci, P(KvCacheDesc), vp, ci, ci, vp, vp, vp, vp, vp, ci, cf, vp, ci, ci, ci, vp, sz, vp, vp]),
         "qzo_copy_blocks": (ci, [P(KvCacheDesc), ci, vp, vp, ci, vp, vp]),
         "qzo_profile_gemms": (ci, [vp, ci]),
         "qzo_profile_read": (ci, [vp, P(i64), P(ctypes.c_double), P(ctypes.c_double)]),
@@ -492,6 +495,49 @@ def qzo_assign_slots(lens, new, block_table, free, free_count, block_size, max_r
     if rc:
         _check(rc, "qzo_assign_slots")
     return row_seq, positions, slots
+
+
+def qzo_shared_prefix_attention_workspace_bytes(R, n_groups, n_heads, n_kv_heads, head_dim, max_len):
+    out = ctypes.c_size_t(0)
+    _check(_lib.qzo_shared_prefix_attention_workspace_bytes(R, n_groups, n_heads, n_kv_heads, head_dim, max_len, ctypes.byref(out)),
+           "qzo_shared_prefix_attention_workspace_bytes")
+    return out.value
+
+
+def qzo_shared_prefix_attention(q, cache, block_table, positions, group_rows, prefix_seq, prefix_len, row_seq=None, scale=None, out=None,
+                                workspace=None, status=None):
+    """qzo_paged_attention for groups of rows that share the beginning of their cache (int32): rows group_rows[i] .. group_rows[i + 1] - 1
+    ([n + 1], ascending) have the first prefix_len[i] tokens of request prefix_seq[i] ([n] each) as the first tokens of their own
+    requests.  The other arguments and the result are those of qzo_paged_attention."""
+    dev = _device_now()
+    R, H, dh = q.shape
+    ldq = _heads(dev, q, "q")
+    assert dh == cache.head_dim and cache.device == dev, "q: expects the head_dim of the cache, which is on the current device"
+    if out is None:
+        out, ldo = q.new_empty(R, H, dh), H * dh
+    else:
+        assert out.shape == (R, H, dh), "out: as q"
+        ldo = _heads(dev, out, "out")
+    n_seqs, width = block_table.shape
+    n = prefix_seq.numel()
+    _ints(dev, 0, block_table)
+    _ints(dev, R, positions)
+    _ints(dev, n, prefix_seq, prefix_len)
+    _ints(dev, n + 1, group_rows)
+    seqs = None
+    if row_seq is not None:
+        _ints(dev, R, row_seq)
+        seqs = row_seq.data_ptr()
+    if workspace is None:
+        workspace = q.new_empty(qzo_shared_prefix_attention_workspace_bytes(R, n, H, cache.n_kv_heads, dh, width * cache.block_size), dtype=_U8)
+    assert workspace.is_contiguous() and workspace.get_device() == dev, "workspace: contiguous, on the current device"
+    rc = _lib.qzo_shared_prefix_attention(q.data_ptr(), ldq, cache._ref, block_table.data_ptr(), n_seqs, width, seqs, positions.data_ptr(),
+                                          group_rows.data_ptr(), prefix_seq.data_ptr(), prefix_len.data_ptr(), n, dh ** -0.5 if scale is None else scale,
+                                          out.data_ptr(), ldo, R, H, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                          None if status is None else _status(dev, status), _raw_stream(dev))
+    if rc:
+        _check(rc, "qzo_shared_prefix_attention")
+    return out
 
 
 def qzo_beam_select_workspace_bytes(B, W, V):

@@ -6,11 +6,12 @@ import numpy as np
 import pytest
 import torch
 
-from oracle import continuations as oracle
+from oracle import continuations as oracle, serving
+from paper_2505_13430_b200 import inputs
 
 pytestmark = pytest.mark.gpu
 
-F32_STEP = 2.0 ** -24
+BF16_STEP, F16_STEP, F32_STEP = 2.0 ** -8, 2.0 ** -11, 2.0 ** -24
 INF = math.inf
 
 
@@ -293,3 +294,239 @@ def test_copies_beyond_32_bit_offsets(lib):
     k[3], v[n_blocks - 2] = 1.5, 2.5
     lib.qzo_copy_blocks([lib.KvCache(k, v)], ints([(3, n_blocks - 1, 40), (n_blocks - 2, 5, 64)]), ints([2]))
     assert (k[n_blocks - 1, :, :40] == 1.5).all() and (k[n_blocks - 1, :, 40:] == 0).all() and (v[5] == 2.5).all() and (v[n_blocks - 1] == 0).all() and (k[5] == 0).all()
+
+
+# ------------------------------------------------------------------ attention over shared beginnings
+
+CACHES = {"bf16": (torch.bfloat16, 1.0, 1.0), "e4m3": (torch.float8_e4m3fn, 0.25, 0.5)}
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+class Shared:
+    """Rows of groups whose requests share the beginning of their cache.  groups: (rows, prefix, what each row has beyond it, a number or a
+    list; None = padding, negative = the row sees that much less than the prefix).  Requests 0 .. n - 1 hold the prefixes and do nothing
+    else, request n + t is row t's.  Full blocks of a prefix are shared, the rest of it is copied."""
+
+    def __init__(self, groups, H, Hkv, dh, block, kind, seed, q_std=1.0, loose=0):
+        rng = _gen(seed)
+        dt, self.ks, self.vs = CACHES[kind]
+        n = len(groups)
+        own = [(i, o) for i, (rows, _, more) in enumerate(groups) for o in (more if isinstance(more, list) else [more] * rows)]
+        own += [(None, o) for o in rng.integers(1, 200, loose)]
+        bounds = np.cumsum([0] + [g[0] for g in groups])
+        self.R, self.H, self.block, self.dh = len(own), H, block, dh
+        assert bounds[-1] + loose == self.R
+        self.lens = [0 if o is None else (groups[i][1] if i is not None else 0) + int(o) for i, o in own]
+        self.prefix = [g[1] for g in groups]
+        width = max(1, -(-max(self.lens + self.prefix) // block))
+        count = lambda tokens: -(-tokens // block)
+        need = sum(count(p) for p in self.prefix) + sum(count(v) for v in self.lens)
+        n_blocks = need + 3
+        shape = (n_blocks, Hkv, block, dh)
+        self.ck, self.cv = (inputs.normal_fp32(shape, 1.0, seed + i).numpy() / s for i, s in enumerate((self.ks, self.vs)))
+        ids = iter(rng.permutation(n_blocks).tolist())
+        table = np.full((n + self.R, width), -1, np.int32)
+        for i, p in enumerate(self.prefix):
+            table[i, :count(p)] = [next(ids) for _ in range(count(p))]
+        for t, (i, o) in enumerate(own):
+            p = 0 if i is None else self.prefix[i]
+            whole, rest = min(p, self.lens[t]) // block, p % block
+            table[n + t, :whole] = table[i, :whole] if i is not None else []
+            table[n + t, whole:count(self.lens[t])] = [next(ids) for _ in range(count(self.lens[t]) - whole)]
+            if i is not None and self.lens[t] > whole * block and whole < count(p):
+                n_copied = rest if whole == p // block else block
+                for pages in (self.ck, self.cv):
+                    pages[table[n + t, whole], :, :n_copied] = pages[table[i, whole], :, :n_copied]
+        # nothing behind a request's length is looked at
+        for r, length in enumerate(self.prefix + self.lens):
+            if length % block:
+                for pages in (self.ck, self.cv):
+                    pages[table[r, length // block], :, length % block:] = float("nan")
+        self.ck, self.cv = (torch.from_numpy(v).to(dt).cuda() for v in (self.ck, self.cv))
+        self.q = inputs.normal_fp32((self.R, H, dh), q_std, seed + 5).bfloat16()
+        self.table, self.seqs = table, np.arange(n, n + self.R)
+        self.positions = [v - 1 for v in self.lens]
+        self.rows = bounds.tolist()
+        self.kind, self.scale = kind, dh ** -0.5
+
+    def run(self, lib, reported=0, **change):
+        a = dict(rows=self.rows, prefix=self.prefix, seq=list(range(len(self.prefix))))
+        a.update(change)
+        status = ints([0])
+        out = lib.qzo_shared_prefix_attention(self.q.cuda(), lib.KvCache(self.ck, self.cv, self.ks, self.vs), torch.from_numpy(self.table).cuda(),
+                                              ints(self.positions), ints(a["rows"]), ints(a["seq"]), ints(a["prefix"]), row_seq=ints(self.seqs.tolist()),
+                                              scale=self.scale, status=status)
+        assert int(status) == reported
+        return out
+
+    def check(self, out, only=None):
+        kp, vp = f64(self.ck) * self.ks, f64(self.cv) * self.vs
+        want, spread = serving.paged_attention(f64(self.q), kp, vp, self.table, self.seqs, self.positions, self.scale)
+        kmax = np.nanmax(np.abs(kp[np.unique(self.table[self.table >= 0])])) if (self.table >= 0).any() else 0.0
+        # score: dh exact products summed in fp32 (truncated at worst), one scaling; weight: exp2 within 4 steps, and as it enters the product:
+        # the sum of two bf16 (2^-15), or of one fp16 (2^-11) where a row's own keys are 8-bit; the sums: two additions for every 16 keys
+        score = np.abs(f64(self.q)).sum(-1, keepdims=True) * kmax * self.scale * (self.dh / 16 + 18) * 2 * F32_STEP
+        p_step = 2.0 ** -15 if self.kind == "bf16" else F16_STEP
+        keys = max(self.lens) + 1
+        allowed = BF16_STEP * np.abs(want) + (p_step + 2 * score + (16 + keys / 4) * F32_STEP) * spread * (1 + BF16_STEP) + 1e-30
+        off = np.abs(f64(out) - want)
+        rows = range(self.R) if only is None else only
+        assert all((off[r] <= allowed[r]).all() for r in rows), [(off / allowed)[r].max() for r in rows]
+        for r in rows:
+            if self.positions[r] < 0:
+                assert (out[r] == 0).all()
+
+
+SHARED_CASES = [
+    # groups, H, Hkv, dh, block, cache, rows without a group
+    ([(4, 40, [1, 5, 20, 7])], 4, 4, 64, 16, "bf16", 0),            # shorter than a tile: nothing is shared
+    ([(4, 64, 1)], 4, 4, 64, 16, "bf16", 0),
+    ([(1, 130, 3)], 1, 1, 128, 16, "bf16", 0),
+    ([(3, 1000, [24, 1, 300])], 2, 2, 128, 16, "bf16", 2),
+    ([(5, 999, [None, 1, 0, -1, 50]), (0, 500, 1), (2, 64, 0), (1, 63, 9)], 8, 2, 64, 32, "bf16", 3),
+    ([(33, 700, 17)], 12, 3, 128, 64, "bf16", 0),                   # 132 queries of a key head: a tile of 128 and one of 4
+    ([(20, 500, 33), (3, 2000, 1), (16, 64, 5)], 24, 1, 64, 128, "bf16", 1),
+    ([(2, 300, 70)], 71, 1, 128, 16, "bf16", 0),
+    ([(4, 9000, [1, 70, 200, 64])], 8, 2, 128, 256, "bf16", 0),
+    ([(70, 2048, 1)], 8, 2, 128, 16, "bf16", 5),
+    ([(4, 200, [1, 5, 20, 7])], 4, 4, 64, 16, "e4m3", 0),
+    ([(6, 1000, [24, None, 1, 300, -900, 2]), (9, 321, 3)], 8, 2, 128, 32, "e4m3", 2),
+    ([(40, 600, 30)], 16, 4, 64, 64, "e4m3", 0),
+    ([(3, 6000, 257)], 4, 1, 128, 256, "e4m3", 0),
+    ([(2, 130 + 7 * i, i) for i in range(70)], 2, 2, 64, 16, "bf16", 4),        # more groups than a warp has lanes
+]
+
+
+@pytest.mark.parametrize("groups,H,Hkv,dh,block,kind,loose", SHARED_CASES)
+def test_shared_prefix_attention_matches_oracle(lib, groups, H, Hkv, dh, block, kind, loose):
+    case = Shared(groups, H, Hkv, dh, block, kind, 300 + H + dh, loose=loose)
+    out = case.run(lib)
+    case.check(out)
+    assert torch.equal(out.view(torch.int16), case.run(lib).view(torch.int16))
+
+
+@pytest.mark.parametrize("kind,dh", [("bf16", 64), ("bf16", 128), ("e4m3", 64), ("e4m3", 128)])
+@pytest.mark.parametrize("rising", [False, True])
+def test_long_runs_of_tiles(lib, kind, dh, rising):
+    # so many groups that a prefix is not split: dozens of tiles one after the other, two CTAs on an SM.  Rising: scores that pass the
+    # running maximum again and again, so that the sums are rescaled between products; some rows fall instead
+    case = Shared([(2, 450 + 13 * i, 1 + 3 * i) for i in range(40)], 8, 8, dh, 32, kind, 900 + dh)
+    if rising:
+        case.q[:, :, 0] = torch.tensor([60.0, -60.0, 0.0, 30.0]).repeat(20)[:, None].bfloat16()
+        for r, length in enumerate(case.prefix + case.lens):
+            j = np.arange(length)
+            page = torch.from_numpy(case.table[r][j // case.block].astype(np.int64)).cuda()
+            case.ck[page, :, torch.from_numpy(j % case.block).cuda(), 0] = torch.from_numpy((j // 64 * 0.75).astype(np.float32)).cuda()[:, None].to(case.ck.dtype)
+    out = case.run(lib)
+    case.check(out)
+    for _ in range(20):
+        assert torch.equal(out.view(torch.int16), case.run(lib).view(torch.int16))
+
+
+def test_peaked_scores_over_a_shared_prefix(lib):
+    case = Shared([(5, 1500, 100), (4, 300, 3)], 8, 2, 128, 16, "bf16", 31, q_std=12.0)
+    case.check(case.run(lib))
+    case.scale = 0.7
+    case.check(case.run(lib))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_leading_keys_of_no_value_in_a_prefix(lib, kind):
+    # keys that lead and whose values are zero leave the row to the others, whose weights are 2^-10 to 2^-40 of theirs
+    case = Shared([(4, 900, 60)], 8, 2, 64, 16, kind, 32)
+    case.ck[..., 0] = 0.0
+    for j in [1] + list(range(70, 900, 97)):
+        for r in range(5):
+            page = int(case.table[r, j // 16])
+            case.ck[page, :, j % 16, 0], case.cv[page, :, j % 16] = 16.0 / case.ks, 0.0
+    leads = torch.tensor([7.0, 14.0, 21.0, 28.0, 3.0, 10.0, 17.0, 24.0])
+    case.q[:, :, 0] = (leads / (16.0 * case.scale)).bfloat16()
+    case.check(case.run(lib))
+
+
+def test_infinite_values_and_scores_in_a_prefix(lib):
+    case = Shared([(3, 500, [1, 64, 300])], 4, 2, 64, 16, "bf16", 33)
+    for j, dim, v in ((0, 3, "inf"), (200, 17, "-inf"), (447, 63, "inf"), (0, 40, "inf"), (300, 40, "-inf"), (100, 5, "nan")):
+        case.cv[int(case.table[0, j // 16]), :, j % 16, dim] = float(v)
+    out = f64(case.run(lib))
+    with np.errstate(invalid="ignore"):
+        want, _ = serving.paged_attention(f64(case.q), f64(case.ck), f64(case.cv), case.table, case.seqs, case.positions, case.scale)
+    special = ~np.isfinite(want)
+    assert special.any() and np.isfinite(want).any()
+    assert np.array_equal(np.isnan(out), np.isnan(want)) and np.array_equal(out[special & ~np.isnan(want)], want[special & ~np.isnan(want)])
+    # a key of -inf scores is left out where it counts against a query, and makes the row NaN where it counts for it
+    case = Shared([(3, 500, [1, 64, 300])], 4, 2, 64, 16, "bf16", 34)
+    case.ck[int(case.table[0, 3]), :, 5, 0] = -INF
+    case.q[:2, :, 0], case.q[2, :, 0] = 1.0, -1.0
+    out = case.run(lib)
+    assert torch.isnan(out[2]).all() and torch.isfinite(out[:2]).all()
+    case.ck[int(case.table[0, 3]), :, 5, 0] = -3e4      # as good as nothing too, and the oracle can take it
+    case.check(out, only=[0, 1])
+
+
+def test_what_is_out_of_range_in_groups_is_reported(lib):
+    groups = [(3, 500, [1, 64, 300]), (2, 200, 30), (2, 300, 5)]
+    case = Shared(groups, 8, 2, 64, 16, "bf16", 35)
+    plain = case.run(lib)
+    case.check(plain)
+    # a group whose request or length is impossible reads its rows' own tables; so do all when the bounds do not ascend
+    n, width = case.table.shape
+    for change in (dict(seq=[0, n, 2]), dict(seq=[-1, 1, 2]), dict(prefix=[500, -1, 300]), dict(prefix=[500, 200, width * 16 + 1])):
+        case.check(case.run(lib, reported=2, **change))
+    for rows in ([0, 5, 3, 7], [-1, 3, 5, 7], [0, 3, 5, 8], [7, 5, 3, 0]):
+        case.check(case.run(lib, reported=2, rows=rows))
+    # bounds that leave rows out, and groups that are smaller than what shares the prefix
+    for rows, prefix in (([1, 3, 5, 7], case.prefix), ([0, 2, 2, 2], [500, 1, 1]), ([0, 3, 5, 5], [400, 200, 0]), ([3, 3, 5, 7], [0, 128, 300])):
+        case.check(case.run(lib, rows=rows, prefix=prefix))
+    # a block outside the cache: nothing of it is seen, through either table
+    for bad in (-1, case.ck.shape[0], 2 ** 31 - 1):
+        broken = Shared(groups, 8, 2, 64, 16, "bf16", 35)
+        page = broken.table[0, 7]
+        broken.table[broken.table == page] = bad
+        out = broken.run(lib, reported=2)
+        for t in range(3):
+            seen = np.setdiff1d(np.arange(broken.lens[t]), np.arange(7 * 16, 8 * 16))
+            for h in range(8):
+                pages = broken.table[3 + t][seen // 16]
+                k, v = f64(broken.ck)[pages, h // 4, seen % 16], f64(broken.cv)[pages, h // 4, seen % 16]
+                s = k @ f64(broken.q)[t, h] * broken.scale
+                w = np.exp(s - s.max())
+                want = w @ v / w.sum()
+                assert np.abs(f64(out[t, h]) - want).max() <= BF16_STEP * np.abs(want).max() + 1e-3
+
+
+def test_several_rows_of_a_request_and_strided_rows(lib):
+    # the options of a question: every request has several new rows, which see the shared prefix and their own tokens up to themselves
+    case = Shared([(4, 333, [40, 41, 42, 43])], 8, 4, 128, 16, "bf16", 36)
+    take = [(t, p) for t in range(4) for p in range(330 + 20 * t, case.lens[t], 3)]
+    R = len(take)
+    q = inputs.normal_fp32((R, 8, 128), 1.0, 9).bfloat16()
+    wide = torch.full((R, 3, 8, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide[:, 1] = q.cuda()
+    out = torch.full((R, 9, 128), 5.0, dtype=torch.bfloat16, device="cuda")
+    status = ints([0])
+    lib.qzo_shared_prefix_attention(wide[:, 1], lib.KvCache(case.ck, case.cv), torch.from_numpy(case.table).cuda(), ints([p for _, p in take]), ints([0, R]), ints([0]),
+                                    ints([333]), row_seq=ints([1 + t for t, _ in take]), out=out[:, :8], status=status)
+    assert int(status) == 0 and (out[:, 8] == 5.0).all()
+    case.R, case.q, case.seqs, case.positions, case.lens = R, q, np.array([1 + t for t, _ in take]), [p for _, p in take], [p + 1 for _, p in take]
+    case.check(out[:, :8])
+
+
+def test_a_prefix_of_a_cache_beyond_32_bit_offsets(lib):
+    Hkv, block, dh = 8, 64, 128
+    n_blocks = (1 << 32) // (Hkv * block * dh * 2) + 6            # 4 GB and a little of keys, as many of values
+    small = Shared([(3, 640, [5, 70, 1])], 16, Hkv, dh, block, "bf16", 37)
+    k, v = (torch.zeros((n_blocks, Hkv, block, dh), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    used = np.unique(small.table[small.table >= 0])
+    to = np.concatenate([np.arange(n_blocks - (len(used) + 1) // 2, n_blocks), np.arange(len(used) // 2)])
+    far = small.table.copy()
+    for a, b in zip(used, to):
+        k[int(b)], v[int(b)] = small.ck[int(a)], small.cv[int(a)]
+        far[small.table == a] = b
+    near = small.run(lib)
+    small.table, small.ck, small.cv = far, k, v
+    assert torch.equal(near, small.run(lib))
+    del k, v

@@ -165,6 +165,29 @@ def test_fork_compact_and_copy_refusals():
     _refused(copy, {}, bad + [dict(caches=(_cache(), _cache(**c))) for c in other] + [dict(caches=(_cache(**c), _cache())) for c in other])
 
 
+@made_up
+def test_shared_prefix_attention_refusals():
+    qzo = _lib()
+    need = qzo.qzo_shared_prefix_attention_workspace_bytes(3, 2, 4, 2, 64, 64)
+    assert need > 0
+    for args in ((0, 1, 4, 2, 64, 64), (1, 0, 4, 2, 64, 64), (1, 1, 3, 2, 64, 64), (1, 1, 4, 0, 64, 64), (1, 1, 4, 2, 80, 64), (1, 1, 4, 2, 64, 0),
+                 (1, 1, 4, 2, 64, (1 << 30) + 1)):
+        with pytest.raises(qzo.QzoError):
+            qzo.qzo_shared_prefix_attention_workspace_bytes(*args)
+
+    def call(q, ldq, cache, tab, n, w, seq, pos, rows, pseq, plen, g, scale, out, ldo, R, H, ws=P, b=need, status=NONE):
+        return qzo._lib.qzo_shared_prefix_attention(q, ldq, None if cache is None else ctypes.byref(cache), tab, n, w, seq, pos, rows, pseq, plen, g, scale, out,
+                                                    ldo, R, H, ws, b, status, None)
+    good = dict(q=P, ldq=256, cache=_cache(), tab=P, n=3, w=4, seq=NONE, pos=P, rows=P, pseq=P, plen=P, g=2, scale=0.125, out=Q, ldo=256, R=3, H=4)
+    bad = [{n: v} for n in ("q", "tab", "pos", "rows", "pseq", "plen", "out") for v in (NONE, ODD)] + [dict(seq=ODD), dict(status=ODD)]
+    bad += [dict(ldq=248), dict(ldq=260), dict(ldo=64), dict(n=0), dict(w=0), dict(w=(1 << 26) + 1), dict(R=0), dict(R=4), dict(H=3), dict(H=0), dict(g=0),
+            dict(scale=0.0), dict(scale=float("nan")), dict(cache=None)]
+    caches = (dict(k=0), dict(v=0x20008), dict(dtype=1), dict(block_size=8), dict(head_dim=96), dict(k_scale=2.0), dict(dtype=4, v_scale=0.0), dict(n_blocks=1 << 27))
+    assert call(**good) in (qzo.QZO_OK, qzo.ERR_UNSUPPORTED_DEVICE)
+    for change in bad + [dict(cache=_cache(**c)) for c in caches]:
+        assert call(**{**good, **change}) == qzo.ERR_BAD_ARG, change
+
+
 def test_the_binding_names_the_limits_of_the_header():
     qzo = _lib()
     header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "qzo.h")).read()
