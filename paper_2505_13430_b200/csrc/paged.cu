@@ -339,6 +339,7 @@ paged_attention_kernel(PagedParams p) {
   const int n_heads = min(8 * NT, p.G - chunk * 8 * NT);
   const int split = blockIdx.y;
   serving_begin();
+  const int shared = GROUPS ? group_prefix(p, row) : 0;
   // Query fragments: the same chunks of dimensions as a key's lane t.
   uint32_t qf[NT][Lay::kKeyWords];
 #pragma unroll
@@ -357,7 +358,7 @@ paged_attention_kernel(PagedParams p) {
   }
   int seq = 0;
   const int len = row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
-  const int first = GROUPS ? row_prefix(p, row, len) : 0;
+  const int first = GROUPS && len >= shared ? shared : 0;
   const int per = split_keys(p, len - first);
   const int k0 = first + split * per, k1 = min(len, k0 + per);
   if (k0 >= k1) {
@@ -668,7 +669,7 @@ paged_attention_kernel(PagedParams p) {
       for (int e = 0; e < 4; ++e) val[e] *= f;
       *reinterpret_cast<uint2*>(p.out + (size_t)row * p.ldo + (size_t)(head0 + h) * DH + d) = pack4_bf16(val);
     } else {
-      const size_t at = ((size_t)row * p.H + head0 + h) * (GROUPS ? p.prefix_splits + p.splits : p.splits) + (GROUPS ? p.prefix_splits + split : split);
+      const size_t at = ((size_t)row * p.H + head0 + h) * p.splits + split;
       *reinterpret_cast<float4*>(p.part_o + at * DH + d) = make_float4(val[0], val[1], val[2], val[3]);
       if (d == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(mx, sum);
     }
@@ -677,7 +678,7 @@ paged_attention_kernel(PagedParams p) {
 
 // Joins the splits of a row's head: a CTA's COLS columns of threads take four dimensions each, its ROWS rows of threads
 // every so many of the splits; the rows are then summed in their order.  COLS * 4 < DH: several CTAs share a head.
-template <int DH, int COLS, int ROWS, bool GROUPS>
+template <int DH, int COLS, int ROWS>
 __global__ void __launch_bounds__(COLS * ROWS)
 paged_join_kernel(PagedParams p) {
   constexpr int kThreads = COLS * ROWS, kParts = DH / 4 / COLS;
@@ -690,14 +691,11 @@ paged_join_kernel(PagedParams p) {
   const int row = (int)(item / p.H), h = (int)(item % p.H);
   int seq = 0;
   const int len = row_keys(p, row, &seq, false);
-  const int first = GROUPS ? row_prefix(p, row, len) : 0, n_first = first ? (first + prefix_keys(p, first) - 1) / prefix_keys(p, first) : 0;
-  const int own = len - first, per = split_keys(p, own), n = n_first + (own > 0 ? (own + per - 1) / per : 0);
-  if (n <= 1 && n_first == 0) return;                  // written already
-  const int stride = GROUPS ? p.prefix_splits + p.splits : p.splits;
-  auto place = [&](int s) { return GROUPS && s >= n_first ? s - n_first + p.prefix_splits : s; };      // of part s of n
-  const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + item * stride;
+  const int per = split_keys(p, len), n = (len + per - 1) / per;
+  if (n <= 1) return;                                  // written already
+  const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + item * p.splits;
   float mx = -INFINITY;
-  for (int s = threadIdx.x; s < n; s += kThreads) mx = fmaxf(mx, ml[place(s)].x);
+  for (int s = threadIdx.x; s < n; s += kThreads) mx = fmaxf(mx, ml[s].x);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
   if ((threadIdx.x & 31) == 0) part_max[threadIdx.x >> 5] = mx;
@@ -705,18 +703,18 @@ paged_join_kernel(PagedParams p) {
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) mx = fmaxf(mx, part_max[w]);
   const float ref = finite_max(mx);
-  for (int s = threadIdx.x; s < n; s += kThreads) weight[s] = fast_exp2(ml[place(s)].x - ref);
+  for (int s = threadIdx.x; s < n; s += kThreads) weight[s] = fast_exp2(ml[s].x - ref);
   __syncthreads();
   const int c = threadIdx.x % COLS, r = threadIdx.x / COLS, d0 = 4 * (c + COLS * (blockIdx.x % kParts));
-  const float4* o = reinterpret_cast<const float4*>(p.part_o + item * stride * DH + d0);
+  const float4* o = reinterpret_cast<const float4*>(p.part_o + item * p.splits * DH + d0);
   float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float sum = 0.0f;
 #pragma unroll 4
   for (int s = r; s < n; s += ROWS) {
     const float w = weight[s];
-    const float4 x = o[(size_t)place(s) * (DH / 4)];
+    const float4 x = o[(size_t)s * (DH / 4)];
     v.x = fmaf(w, x.x, v.x); v.y = fmaf(w, x.y, v.y); v.z = fmaf(w, x.z, v.z); v.w = fmaf(w, x.w, v.w);
-    sum = fmaf(w, ml[place(s)].y, sum);
+    sum = fmaf(w, ml[s].y, sum);
   }
   part[r][c] = v;
   if (c == 0) part_sum[r] = sum;
@@ -774,20 +772,20 @@ int run_attention_w(const PagedParams& p, cudaStream_t st) {
   return launch_serving(paged_attention_kernel<DH, NT, F8, W, GROUPS>, grid, dim3(W * 32), smem, 1, st, p);
 }
 
-template <int DH, int COLS, int ROWS, bool GROUPS>
+template <int DH, int COLS, int ROWS>
 int run_join(const PagedParams& p, cudaStream_t st) {
-  return launch_serving(paged_join_kernel<DH, COLS, ROWS, GROUPS>, dim3((unsigned)((int64_t)p.R * p.H * (DH / 4 / COLS))),
-                        dim3(COLS * ROWS), (p.splits + p.prefix_splits) * sizeof(float), 1, st, p);
+  return launch_serving(paged_join_kernel<DH, COLS, ROWS>, dim3((unsigned)((int64_t)p.R * p.H * (DH / 4 / COLS))),
+                                     dim3(COLS * ROWS), p.splits * sizeof(float), 1, st, p);
 }
 
 template <int DH, bool F8, bool GROUPS>
 int run_attention(const PagedParams& p, bool wide, cudaStream_t st) {
   if (p.G <= 8) QZO_TRY(wide ? (run_attention_w<DH, 1, F8, 8, GROUPS>(p, st)) : (run_attention_w<DH, 1, F8, 4, GROUPS>(p, st)));
   else QZO_TRY(wide ? (run_attention_w<DH, 2, F8, 8, GROUPS>(p, st)) : (run_attention_w<DH, 2, F8, 4, GROUPS>(p, st)));
-  const int splits = p.splits + p.prefix_splits;
-  if (splits <= 1) return QZO_OK;
+  if (GROUPS) return launch_prefix_join(p, DH, st);
+  if (p.splits <= 1) return QZO_OK;
   // many splits of few heads: a head's dimensions go to several CTAs, so that a thread adds up fewer of them
-  return splits > 16 ? run_join<DH, 8, 32, GROUPS>(p, st) : run_join<DH, DH / 4, 4, GROUPS>(p, st);
+  return p.splits > 16 ? run_join<DH, 8, 32>(p, st) : run_join<DH, DH / 4, 4>(p, st);
 }
 
 template <bool GROUPS>
@@ -836,10 +834,26 @@ size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
   return splits > 1 ? (size_t)R * H * splits * (dh + 2) * sizeof(float) : 0;
 }
 
-// Bytes of the partial results for the prefixes of n_groups groups and the rows' own keys, splits of each
+// Room for the results of prefixes: parts, queries of a part, and bytes.  0 parts: too many tiles to count in 32 bits.
+struct PrefixRoom {
+  int64_t parts;
+  int rows;
+  size_t bytes;
+};
+PrefixRoom prefix_room(int R, int n_groups, int G, int Hkv, int dh, int max_len) {
+  const int64_t units = prefix_units(R, n_groups, G, Hkv);
+  if (units * (ceil_div64(max_len, kPrefixTile) + 1) > INT32_MAX) return {0, 0, 0};
+  const int rows = (int)std::min<int64_t>(kPrefixQueries, (int64_t)R * G);
+  return {units + 2 * kSMs, rows, (size_t)(units + 2 * kSMs) * rows * (dh + 2) * sizeof(float)};
+}
+
+// Splits of rows whose prefix is taken elsewhere: what the table has room for is mostly prefix, so long rows are not cut into as many
+// pieces (most of those CTAs would find nothing: 128 rows with 16384 of 16500 tokens in common, 6 splits 20 us, 2 splits 9 us).
+int own_splits(const Plan& plan) { return std::min(plan.splits, 2); }
+
 size_t shared_prefix_bytes(int R, int n_groups, int H, int Hkv, int dh, int max_len) {
-  const int splits = prefix_splits(R, n_groups, H / Hkv, Hkv, max_len) + attention_plan(R, Hkv, H / Hkv, 128 / dh, max_len).splits;
-  return (size_t)R * H * splits * (dh + 2) * sizeof(float);
+  const int splits = own_splits(attention_plan(R, Hkv, H / Hkv, 128 / dh, max_len));
+  return (size_t)R * H * splits * (dh + 2) * sizeof(float) + prefix_room(R, n_groups, H / Hkv, Hkv, dh, max_len).bytes;
 }
 
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
@@ -850,31 +864,40 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
   if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
   const int subs = 256 / (c.head_dim * (c.dtype == QZO_DTYPE_E4M3 ? 1 : 2));
   const Plan plan = attention_plan(R, c.n_kv_heads, G, subs, max_len);
-  int splits = plan.splits, first_splits = groups ? prefix_splits(R, groups->n, G, c.n_kv_heads, max_len) : 0;
-  if (groups && prefix_ctas(R, groups->n, G, c.n_kv_heads) * first_splits > INT32_MAX) return QZO_ERR_BAD_ARG;
-  if (groups && (int64_t)c.n_blocks * c.block_size * c.n_kv_heads > INT32_MAX) return QZO_ERR_BAD_ARG;      // rows that a tensor map can name
+  int splits = groups ? own_splits(plan) : plan.splits;
   const size_t per_split = (size_t)R * H * (c.head_dim + 2) * sizeof(float);
-  if (fewer_splits) {
-    const size_t room = ws_bytes / per_split;
-    if (groups) {
-      if (room < 2) return QZO_ERR_WORKSPACE;
-      first_splits = (int)std::min<size_t>(first_splits, room - 1);
+  if (groups) {
+    const PrefixRoom room = prefix_room(R, groups->n, G, c.n_kv_heads, c.head_dim, max_len);
+    // rows that a tensor map can name
+    if ((int64_t)c.n_blocks * c.block_size * c.n_kv_heads > INT32_MAX) return QZO_ERR_BAD_ARG;
+    if (!fewer_splits && (!ws || ws_bytes < shared_prefix_bytes(R, groups->n, H, c.n_kv_heads, c.head_dim, max_len) || ((uintptr_t)ws & 255))) return QZO_ERR_WORKSPACE;
+    if (fewer_splits && ws_bytes >= room.bytes + per_split) splits = (int)std::min<size_t>(splits, (ws_bytes - room.bytes) / per_split);
+    if (room.parts > 0 && ws_bytes >= room.bytes + splits * per_split) {
+      PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, slots, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
+                    R, H, c.n_kv_heads, G, chunks, splits, plan.min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status,
+                    *groups, 2 * kSMs, room.rows, nullptr, nullptr};
+      p.prefix_o = (float*)ws;
+      p.part_o = p.prefix_o + (size_t)room.parts * room.rows * c.head_dim;
+      p.prefix_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
+      p.part_ml = p.prefix_ml + 2 * (size_t)room.parts * room.rows;
+      QZO_TRY(launch_prefix_attention(p, c, st));
+      return run_attention_of<true>(p, c, plan.wide, st);
     }
-    splits = (int)std::max<size_t>(1, std::min<size_t>(splits, room - first_splits));
-  } else if (const size_t need = groups ? (first_splits + splits) * per_split : paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0) {
-    if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
+    // no room for what prefixes leave: every row reads its own table
   }
+  splits = plan.splits;
+  if (fewer_splits)
+    splits = (int)std::max<size_t>(1, std::min<size_t>(splits, ws_bytes / per_split));
+  else if (const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
+    if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
   PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, slots, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
                 R, H, c.n_kv_heads, G, chunks, splits, plan.min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status,
-                {nullptr, nullptr, nullptr, 0}, first_splits};
-  if (splits + first_splits > 1) {
+                {nullptr, nullptr, nullptr, 0}, 0, 0, nullptr, nullptr};
+  if (splits > 1) {
     p.part_o = (float*)ws;
-    p.part_ml = p.part_o + (size_t)R * H * (splits + first_splits) * c.head_dim;
+    p.part_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
   }
-  if (!groups) return run_attention_of<false>(p, c, plan.wide, st);
-  p.groups = *groups;
-  QZO_TRY(launch_prefix_attention(p, c, st));
-  return run_attention_of<true>(p, c, plan.wide, st);
+  return run_attention_of<false>(p, c, plan.wide, st);
 }
 
 }  // namespace qzo

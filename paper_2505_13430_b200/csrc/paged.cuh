@@ -27,7 +27,8 @@ struct PagedParams {
   float *part_o, *part_ml;                             // [R][H][splits][DH], [R][H][splits][2]
   int* status;
   PrefixGroups groups;                                 // of the rows that share the beginning of their cache; none: n = 0
-  int prefix_splits;                                   // of the partial results of a row's head, these come first
+  int prefix_ctas, prefix_rows;                        // CTAs of the prefix kernel; queries that a part of its results has room for
+  float *prefix_o, *prefix_ml;                         // [parts][prefix_rows][DH], [parts][prefix_rows][2]
 };
 
 // Keys of split s of a row that sees len keys: [s * per, min(len, (s + 1) * per)), per at least the launch's minimum.
@@ -61,46 +62,47 @@ __device__ __forceinline__ float upper_half(uint32_t bits) { return __uint_as_fl
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 
 // ----------------------------------------------------------------------------- shared beginnings
-constexpr int kPrefixTile = 64;                        // keys of a tile of the prefix kernel: a prefix counts in whole ones
-constexpr int kPrefixLeast = 256;                      // keys of a split of a prefix, at least
+// The work on prefixes: a unit is 128 queries (the rows of a group times the query heads of a key head, in that order) over
+// the whole prefix of their group, tiles of 64 keys and one place more for what a change of units costs.  All units, group by group,
+// key head by key head, stand in one line, of which every CTA takes an equal stretch.  What a CTA finds of unit u is part (CTA + u) of
+// the results: from one stretch or unit to the next, one of the two grows.
+constexpr int kPrefixQueries = 128, kPrefixTile = 64;
+constexpr int kPrefixStep = 16;                        // tokens that a prefix counts in: what the rows' own kernel starts at
+constexpr int kPrefixLeast = 4;                        // places of a CTA's stretch, at least
 
-// Keys that a group's rows share; 0 where its request or its length is out of range.
-__device__ __forceinline__ int group_prefix(const PagedParams& p, int group, bool report) {
-  const int len = p.groups.len[group], seq = p.groups.seq[group];
+struct PrefixGroup {
+  int row0, rows, prefix, seq, tiles, key_tiles;       // tiles of queries of a key head, tiles of keys
+  __device__ __forceinline__ int units(int Hkv) const { return key_tiles ? tiles * Hkv : 0; }
+  __device__ __forceinline__ int places() const { return key_tiles + 1; }        // of a unit
+};
+
+// A group; without keys where its request or its length is out of range
+__device__ __forceinline__ PrefixGroup prefix_group(const PagedParams& p, int i, bool report = false) {
+  const int row0 = p.groups.rows[i], rows = p.groups.rows[i + 1] - row0, len = p.groups.len[i], seq = p.groups.seq[i];
   const bool bad = len < 0 || len > (p.width << p.log2_block) || (unsigned)seq >= (unsigned)p.n_seqs;
   if (bad && report && p.status) atomicOr(p.status, kStatusBadToken);
-  return bad ? 0 : len / kPrefixTile * kPrefixTile;
+  const int prefix = bad ? 0 : len / kPrefixStep * kPrefixStep;
+  return {row0, rows, prefix, seq, (rows * p.G + kPrefixQueries - 1) / kPrefixQueries, rows > 0 ? (prefix + kPrefixTile - 1) / kPrefixTile : 0};
 }
-// Keys of a split of a prefix
-__device__ __forceinline__ int prefix_keys(const PagedParams& p, int prefix) {
-  return max(kPrefixLeast, ((prefix + p.prefix_splits - 1) / p.prefix_splits + kPrefixTile - 1) / kPrefixTile * kPrefixTile);
-}
-// The group of a row, -1 for none.  Called by whole warps, `row` the same in all lanes.  Bounds that do not ascend within the rows
-// make no groups at all.
-__device__ __forceinline__ int row_group(const PagedParams& p, int row) {
-  const int lane = threadIdx.x & 31;
-  int at = 0;
-  bool bad = false;
-  for (int i0 = 0; i0 <= p.groups.n; i0 += 32) {
-    const int i = i0 + lane;
-    const int here = i <= p.groups.n ? p.groups.rows[i] : INT32_MAX, next = i < p.groups.n ? p.groups.rows[i + 1] : here;
-    bad = bad || here > next || (i == 0 && here < 0) || (i == p.groups.n && here > p.R);
-    at += __popc(__ballot_sync(0xffffffffu, here <= row));
+// Places of a CTA's stretch, of `places` in all
+__device__ __forceinline__ int prefix_stretch(const PagedParams& p, int places) { return max(kPrefixLeast, (places + p.prefix_ctas - 1) / p.prefix_ctas); }
+
+// How many of the keys that a row sees (len) the prefix kernel takes: those its group shares, or none where it does not see all of
+// them, or where the groups' bounds do not ascend within the rows.  Called by whole warps, `row` the same in all lanes.
+__device__ __forceinline__ int group_prefix(const PagedParams& p, int row) {
+  int prefix = 0;
+  for (int i = threadIdx.x & 31; i < p.groups.n; i += 32) {
+    const PrefixGroup g = prefix_group(p, i);
+    if (g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R) prefix = INT32_MAX;
+    else if (g.row0 <= row && row < g.row0 + g.rows && prefix < INT32_MAX) prefix = g.prefix;
   }
-  return __any_sync(0xffffffffu, bad) || at == 0 || at > p.groups.n ? -1 : at - 1;
-}
-// How many of the keys that a row sees (len) the prefix kernel takes: those its group shares, or none where it does not see all of them.
-__device__ __forceinline__ int row_prefix(const PagedParams& p, int row, int len) {
-  const int group = row_group(p, row);
-  if (group < 0) return 0;
-  const int prefix = group_prefix(p, group, false);
-  return len >= prefix ? prefix : 0;
+  prefix = __reduce_max_sync(0xffffffffu, prefix);
+  return prefix == INT32_MAX ? 0 : prefix;
 }
 
-// prefix.cu: the partial results of every group's prefix, for the rows that see all of it
+// prefix.cu: the results of every group's prefix, for the rows that see all of it, and their join with those of the rows' own keys
 int launch_prefix_attention(const PagedParams& p, const qzo_kv_cache& c, cudaStream_t st);
-// CTAs of it for one split, and the splits that fill the SMs
-int64_t prefix_ctas(int R, int n_groups, int G, int Hkv);
-int prefix_splits(int R, int n_groups, int G, int Hkv, int max_len);
+int launch_prefix_join(const PagedParams& p, int dh, cudaStream_t st);
+int64_t prefix_units(int R, int n_groups, int G, int Hkv);      // at most
 
 }  // namespace qzo

@@ -1,6 +1,6 @@
 // Attention of groups of rows over the beginning of a paged cache that they share, on the fifth-generation tensor cores: the rows'
-// queries of a key head are the M side of the products, so that a key and a value are read once for all of them.  Every split
-// of a prefix leaves its sums, its reference and its sum of weights for paged_join_kernel, which joins them with those of the rows' own keys.
+// queries of a key head are the M side of the products, so that a key and a value are read once for all of them.  Every part of a
+// prefix leaves its sums, its reference and its sum of weights; a second kernel joins them with those of the rows' own keys.
 #include "qzo_common.cuh"
 #include "launch.cuh"
 #include "layers.cuh"
@@ -15,338 +15,525 @@
 namespace qzo {
 namespace {
 
-constexpr int kM = 128;                                // queries of a CTA: the rows of a group times the query heads of a key head
-constexpr int kSoftmaxWarps = 4, kLoadWarp = 4, kIssueWarp = 5, kFirstConvertWarp = 6, kConvertWarps = 4;
+constexpr int kM = kPrefixQueries, kTile = kPrefixTile;
+constexpr int kSoftmaxWarps = 8, kLoadWarp = 8, kScoreWarp = 9, kValueWarp = 10, kFirstConvertWarp = 11, kConvertWarps = 3;
 constexpr int kTmemCols = 256;                         // two CTAs to an SM
+constexpr int kThereRing = 8;                          // tiles whose masks are kept: more than the rings hold
 constexpr float kSlack = 8.0f;                         // by which scores may pass the reference before it is raised
 
 // Shared memory: the queries, a ring of operand tiles (64 keys or values, in the order in which the products take them: K0 K1 V0 K2
-// V1 ...), for 8-bit pages a ring of the tiles as they are stored, barriers.
+// V1 ...), for 8-bit pages a ring of the tiles as they are stored, barriers.  Tensor memory: sums, scores, weights.
 template <int DH, bool F8>
 struct PrefixPlan {
-  static constexpr int kThreads = (6 + (F8 ? kConvertWarps : 0)) * 32;
-  static constexpr int kQBytes = kM * DH * 2, kSlotBytes = kPrefixTile * DH * 2, kRawBytes = kPrefixTile * DH;
-  static constexpr int kSlots = F8 ? 3 * 128 / DH : 4 * 128 / DH, kRawSlots = F8 ? 3 * 128 / DH : 0;
-  static constexpr int kOffSlots = kQBytes, kOffRaw = kOffSlots + kSlots * kSlotBytes, kOffBars = kOffRaw + kRawSlots * kRawBytes;
-  static constexpr int kBars = 2 * kSlots + 2 * kRawSlots + 2 + 2 + 2 + 1 + 1;
-  static constexpr int kOffMisc = kOffBars + 8 * kBars;
+  static constexpr int kThreads = (kFirstConvertWarp + (F8 ? kConvertWarps : 0)) * 32;
+  static constexpr int kQueryBytes = kM * DH * 2, kSlotBytes = kTile * DH * 2, kRawBytes = kTile * DH;
+  static constexpr int kSlots = (F8 ? 3 : 4) * 128 / DH, kRawSlots = F8 ? 3 * 128 / DH : 0;
+  static constexpr int kOffSlots = kQueryBytes, kOffRaw = kOffSlots + kSlots * kSlotBytes, kOffBars = kOffRaw + kRawSlots * kRawBytes;
+  static constexpr int kBars = 2 * kSlots + 2 * kRawSlots + 8;
+  static constexpr int kOffHalves = kOffBars + 8 * kBars, kOffWalks = kOffHalves + 2 * kM * 4, kOffThere = kOffWalks + kSoftmaxWarps * 64, kOffMisc = kOffThere + 4 * kThereRing;
   static constexpr int kDynamicBytes = kOffMisc + 16 + 1024;         // slack for the 1024-byte alignment
   static_assert(2 * (kDynamicBytes + 1024) <= 228 * 1024, "two CTAs to an SM");
+  static constexpr int kColSums = 0, kColScores = DH, kColWeights = DH + kTile;
+  static_assert(kColWeights + kTile <= kTmemCols, "tensor memory budget");
 };
 
-// Tiles of kM queries of all groups, at most: every group may leave one unfinished.
-int64_t most_tiles(int R, int n_groups, int G) {
-  const int64_t k = std::min(R, n_groups);
-  return k + ((int64_t)R * G - k) / kM;
+// Two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// Barrier of 64 threads: whether any of them says so
+__device__ __forceinline__ bool any_of_pair(uint32_t id, bool v) {
+  uint32_t r;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\nbar.red.or.pred q, %1, 64, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"(id), "r"((uint32_t)v) : "memory");
+  return r != 0;
 }
 
-// The group and the tile within it that a CTA takes, false where there is none.  Whole warps.
-__device__ __forceinline__ bool find_tile(const PagedParams& p, int tile, int* group, int* in_group, bool report) {
+// Keys and values: in boxes of a block's tokens (64 of a larger block), and of 16 tokens for the end of a prefix
+struct PrefixMaps { CUtensorMap whole[2], step[2]; };
+
+// A walk along the line: where a CTA is in it, at a tile.  The same in all lanes of a warp; every role has its own.
+struct Walk {
+  PrefixGroup group;
+  int index, unit, key_tile;                           // group, unit within it, tile of keys
+  int number;                                          // of the unit among all
+
+  __device__ __forceinline__ void next_unit(const PagedParams& p) {
+    key_tile = 0;
+    ++number;
+    if (++unit < group.units(p.Hkv)) return;
+    unit = 0;
+    while (++index < p.groups.n) {                     // to the next group with units
+      group = prefix_group(p, index);
+      if (group.units(p.Hkv)) return;
+    }
+  }
+  __device__ __forceinline__ void next(const PagedParams& p) {
+    if (++key_tile == group.key_tiles) next_unit(p);
+  }
+  __device__ __forceinline__ bool at_end() const { return key_tile + 1 == group.key_tiles; }
+  __device__ __forceinline__ int head() const { return unit / group.tiles; }
+  __device__ __forceinline__ int first_item() const { return unit % group.tiles * kM; }
+};
+
+// A CTA's stretch of the line: where it starts and how many tiles there are in it, 0 where there are none or where the groups' bounds
+// do not ascend within the rows.  Whole warps.
+__device__ __forceinline__ int find_stretch(const PagedParams& p, int cta, bool report, Walk* w) {
   const int lane = threadIdx.x & 31;
-  int before = 0;
+  int all = 0;
   bool bad = false;
-  *group = -1;
-  for (int i0 = 0; i0 <= p.groups.n; i0 += 32) {
-    const int i = i0 + lane;
-    const int here = i <= p.groups.n ? p.groups.rows[i] : INT32_MAX, next = i < p.groups.n ? p.groups.rows[i + 1] : here;
-    bad = bad || here > next || (i == 0 && here < 0) || (i == p.groups.n && here > p.R);
-    int tiles = i < p.groups.n && next > here && here >= 0 && next <= p.R ? (int)(((long long)(next - here) * p.G + kM - 1) / kM) : 0;
-    int sum = tiles;
+  for (int i = lane; i < p.groups.n; i += 32) {
+    const PrefixGroup g = prefix_group(p, i, report);
+    bad = bad || g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R;
+    all += g.units(p.Hkv) * g.places();
+  }
+  if (__any_sync(0xffffffffu, bad)) {
+    if (report && lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+    return 0;
+  }
+  all = __reduce_add_sync(0xffffffffu, all);
+  const int stretch = prefix_stretch(p, all), from = min(all, cta * stretch), to = min(all, from + stretch);
+  if (from >= to) return 0;
+  // the group that `from` is in, and the tiles between `from` and `to`: places less the one at the end of each unit
+  int places_before = 0, units_before = 0, tiles = 0;
+  bool found = false;
+  for (int i0 = 0; i0 < p.groups.n && places_before < to; i0 += 32) {
+    PrefixGroup g = {};
+    if (i0 + lane < p.groups.n) g = prefix_group(p, i0 + lane);
+    const int units = g.units(p.Hkv), places = units * g.places();
+    int sum = places, unit_sum = units;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, sum, d);
-      if (lane >= d) sum += up;
+      const int up = __shfl_up_sync(0xffffffffu, sum, d), unit_up = __shfl_up_sync(0xffffffffu, unit_sum, d);
+      if (lane >= d) { sum += up; unit_sum += unit_up; }
     }
-    const unsigned past = __ballot_sync(0xffffffffu, before + sum > tile);
-    if (*group < 0 && past) {
+    const int begin = places_before + sum - places;
+    if (units) {                                       // tiles in front of place x of the group
+      auto tiles_to = [&](int x) { return x / g.places() * g.key_tiles + min(x % g.places(), g.key_tiles); };
+      tiles += tiles_to(min(max(to - begin, 0), places)) - tiles_to(min(max(from - begin, 0), places));
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, places_before + sum > from);
+    if (!found && past) {
+      found = true;
       const int who = __ffs(past) - 1;
-      *group = i0 + who;
-      *in_group = tile - before - __shfl_sync(0xffffffffu, sum - tiles, who);
+      w->index = i0 + who;
+      w->group = {__shfl_sync(0xffffffffu, g.row0, who), __shfl_sync(0xffffffffu, g.rows, who), __shfl_sync(0xffffffffu, g.prefix, who),
+                  __shfl_sync(0xffffffffu, g.seq, who), __shfl_sync(0xffffffffu, g.tiles, who), __shfl_sync(0xffffffffu, g.key_tiles, who)};
+      const int in_group = from - __shfl_sync(0xffffffffu, begin, who);
+      w->unit = in_group / w->group.places();
+      w->key_tile = in_group % w->group.places();
+      w->number = units_before + __shfl_sync(0xffffffffu, unit_sum - units, who) + w->unit;
     }
-    before += __shfl_sync(0xffffffffu, sum, 31);
+    places_before += __shfl_sync(0xffffffffu, sum, 31);
+    units_before += __shfl_sync(0xffffffffu, unit_sum, 31);
   }
-  bad = __any_sync(0xffffffffu, bad);
-  if (bad && report && p.status) atomicOr(p.status, kStatusBadToken);
-  return !bad && *group >= 0;
+  tiles = __reduce_add_sync(0xffffffffu, tiles);
+  if (tiles && w->key_tile == w->group.key_tiles) w->next_unit(p);
+  return tiles;
 }
 
-// A CTA = 128 queries of a group and a key head, one split of the prefix.  S = Q K^T goes to tensor memory (two buffers, so that the
-// next tile's product runs while this one's softmax does); a thread of the softmax warps has one query's 64 scores in registers
-// and writes their weights over them, as the sum of two bf16 (2^-15 of a weight; one alone would leave 2^-8, as much as the
-// output's rounding), from where they enter O += P V as the A operand.  O stays in tensor memory; it is rescaled only when a
-// maximum passes the reference by 2^8.
+// Two CTAs on every SM, each with its stretch of the line of tiles, unit after unit.  S = Q K^T goes to tensor memory; a pair of threads
+// of the softmax warps takes a query's 64 scores into registers, 32 each, upon which the next tile's product may overwrite them, and
+// writes their weights beside them, as the sum of two bf16 (2^-15 of a weight; one alone would leave 2^-8, as much as the output's
+// rounding), from where they enter O += P V as the A operand.  O stays in tensor memory; it is rescaled only when a maximum
+// passes the reference by 2^8.
 template <int DH, bool F8>
 __global__ void __launch_bounds__((PrefixPlan<DH, F8>::kThreads), 2)
-prefix_attention_kernel(const __grid_constant__ CUtensorMap keys_map, const __grid_constant__ CUtensorMap values_map, const __grid_constant__ PagedParams p,
-                        int tiles, int total_splits, int64_t cache_rows, int box_rows) {
+prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_constant__ PagedParams p, int64_t cache_rows, int box_rows) {
   using Plan = PrefixPlan<DH, F8>;
-  constexpr int kSlots = Plan::kSlots, kRawSlots = Plan::kRawSlots, kHalves = DH / 64;
+  constexpr int kSlots = Plan::kSlots, kRawSlots = Plan::kRawSlots, kHalves = DH / 64, kRing = F8 ? kRawSlots : kSlots, kHalf = DH / 2;
   extern __shared__ uint8_t prefix_smem[];
   const uint32_t base = (smem_u32(prefix_smem) + 1023u) & ~1023u;
   uint8_t* const smem = prefix_smem + (base - smem_u32(prefix_smem));
   const uint32_t slots = base + Plan::kOffSlots, raws = base + Plan::kOffRaw, bar0 = base + Plan::kOffBars;
-  auto bar_full = [&](int s) { return bar0 + 8u * s; };
+  auto bar_full = [&](int s) { return bar0 + 8u * s; };                          // an operand tile is there, and its slot free again
   auto bar_empty = [&](int s) { return bar0 + 8u * (kSlots + s); };
-  auto bar_raw_full = [&](int s) { return bar0 + 8u * (2 * kSlots + s); };
+  auto bar_raw_full = [&](int s) { return bar0 + 8u * (2 * kSlots + s); };       // the same of the tiles as they are stored
   auto bar_raw_empty = [&](int s) { return bar0 + 8u * (2 * kSlots + kRawSlots + s); };
-  auto bar_scores = [&](int b) { return bar0 + 8u * (2 * kSlots + 2 * kRawSlots + b); };
-  auto bar_weights = [&](int b) { return bar0 + 8u * (2 * kSlots + 2 * kRawSlots + 2 + b); };
-  // O with the values of tile j: two in turn, so that who waits for tile j - 1 is never two phases away
-  auto bar_values = [&](int b) { return bar0 + 8u * (2 * kSlots + 2 * kRawSlots + 4 + b); };
-  const uint32_t bar_done = bar0 + 8u * (2 * kSlots + 2 * kRawSlots + 6), bar_drain = bar_done + 8u;      // O with all tiles; end after a failed wait
+  constexpr int kRest = 2 * kSlots + 2 * kRawSlots;
+  // of a tile, one phase each: its scores are there, have been taken into registers, its weights are there, are in the sums; of a unit: its
+  // queries are there, its sums have been read; the end after a failed wait
+  const uint32_t bar_scores = bar0 + 8u * kRest, bar_taken = bar_scores + 8u, bar_weights = bar_scores + 16u, bar_values = bar_scores + 24u;
+  const uint32_t bar_queries = bar_scores + 32u, bar_read = bar_scores + 40u, bar_drain = bar_scores + 48u;   // (two)
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + Plan::kOffMisc);
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + Plan::kOffMisc + 4);
   volatile int* const never_set = reinterpret_cast<volatile int*>(smem + Plan::kOffMisc + 8);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long limit = kWaitLimitCycles;
 
-  // tiles of one group, key head and split stand side by side: they read the same keys
-  const int tile = blockIdx.x % tiles, hk = blockIdx.x / tiles % p.Hkv, split = blockIdx.x / tiles / p.Hkv;
-  serving_begin();
-  int group, in_group;
-  if (!find_tile(p, tile, &group, &in_group, blockIdx.x == 0 && tid == 0)) return;
-  const int prefix = group_prefix(p, group, hk == 0 && split == 0 && in_group == 0 && tid == 0);
-  const int per = prefix_keys(p, prefix), k0 = split * per, k1 = min(prefix, k0 + per);
-  if (k0 >= k1) return;
-  const int n_tiles = (k1 - k0) / kPrefixTile;
-  const int row0 = p.groups.rows[group], item0 = in_group * kM;
-  const int items = min(kM, (p.groups.rows[group + 1] - row0) * p.G - item0);
-  const int32_t* const pages = p.table + (size_t)p.groups.seq[group] * p.width;
-  const int active_warps = (items + 31) / 32;
-
-  if (tid == 0) {
+  if (tid == kLoadWarp * 32) {
     *abort_flag = 0;
     *never_set = 0;
     for (int s = 0; s < kSlots; ++s) { mbar_init(bar_full(s), F8 ? kConvertWarps : 1); mbar_init(bar_empty(s), 1); }
     for (int s = 0; s < kRawSlots; ++s) { mbar_init(bar_raw_full(s), 1); mbar_init(bar_raw_empty(s), kConvertWarps); }
-    for (int b = 0; b < 2; ++b) { mbar_init(bar_scores(b), 1); mbar_init(bar_weights(b), active_warps); mbar_init(bar_values(b), 1); }
-    mbar_init(bar_done, 1);
+    mbar_init(bar_scores, 2);
+    mbar_init(bar_taken, kSoftmaxWarps);
+    mbar_init(bar_weights, kSoftmaxWarps);
+    mbar_init(bar_values, 1);
+    mbar_init(bar_queries, kSoftmaxWarps);
+    mbar_init(bar_read, kSoftmaxWarps);
     mbar_init(bar_drain, 1);
+    mbar_init(bar_drain + 8u, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kIssueWarp) tmem_alloc(smem_u32(tmem_slot), kTmemCols);
-  // a thread's query: which row and head, and whether the row sees the whole prefix (rows that do not take it with their own keys)
-  int row = -1, head = 0;
-  if (warp < kSoftmaxWarps && tid < items) {
-    const int t = row0 + (item0 + tid) / p.G;
-    int seq;
-    head = hk * p.G + (item0 + tid) % p.G;
-    if (row_keys(p, t, &seq, false) >= prefix) row = t;
+  __syncwarp();
+  serving_begin();
+  Walk start;
+  const int n_tiles = find_stretch(p, blockIdx.x, blockIdx.x == 0 && warp == 0, &start);
+  if (n_tiles == 0) return;
+
+  // The load warp: lanes 0 .. boxes - 1 each copy a box of a tile (a block of the cache, or 64 keys of one), keys and values from
+  // the same place of either; blocks are looked up two tiles ahead.  In the order of the products: K0, then K1 V0, K2 V1 ... V of the last.
+  struct Box { int page, row, left; };                 // its block, the row of its first token in that block's rows, tokens of the prefix from there on
+  const int boxes = kTile / box_rows;
+  int issued = 0;
+  Ring ring;
+  Walk seek = start;
+  Box box[3];
+  auto look_up = [&](int j) {
+    Box b = {0, 0, 0};
+    if (j >= n_tiles) return b;
+    const int at = seek.key_tile * kTile + lane * box_rows;
+    b.left = lane < boxes ? seek.group.prefix - at : 0;
+    if (b.left > 0) b.page = p.table[(size_t)seek.group.seq * p.width + (at >> p.log2_block)];
+    b.row = (seek.head() << p.log2_block) + (at & ((1 << p.log2_block) - 1));
+    seek.next(p);
+    return b;
+  };
+  volatile uint32_t* const there_ring = reinterpret_cast<volatile uint32_t*>(smem + Plan::kOffThere);      // bit i: the sixteen keys i of a tile are there
+  auto load = [&](const Box& b, const CUtensorMap* whole, const CUtensorMap* step, int key_tile) {
+    const uint32_t full = F8 ? bar_raw_full(ring.s) : bar_full(ring.s);
+    // the first round of the ring is free
+    if (!__all_sync(0xffffffffu, mbar_wait_likely(F8 ? bar_raw_empty(ring.s) : bar_empty(ring.s), ring.ph ^ 1u, abort_flag, limit))) return false;
+    if (key_tile >= 0) {
+      const int from = kPrefixStep * lane / box_rows & 31, page = __shfl_sync(0xffffffffu, b.page, from), left = __shfl_sync(0xffffffffu, b.left, from);
+      const unsigned there = __ballot_sync(0xffffffffu, left > kPrefixStep * lane % box_rows && (unsigned)page < (unsigned)p.n_blocks);
+      if (lane == 0) there_ring[key_tile % kThereRing] = there & (1u << kTile / kPrefixStep) - 1;
+    }
+    if (lane == 0) mbar_arrive_expect_tx(full, F8 ? Plan::kRawBytes : Plan::kSlotBytes);
+    __syncwarp();
+    if (lane < boxes) {
+      // behind the cache's end there are zeros: for what lies behind the prefix and for blocks out of range
+      const bool there = b.left > 0 && (unsigned)b.page < (unsigned)p.n_blocks;
+      if (b.left > 0 && !there && p.status) atomicOr(p.status, kStatusBadToken);
+      const int64_t y = there ? (((int64_t)b.page * p.Hkv) << p.log2_block) + b.row : cache_rows;
+      auto copy = [&](const CUtensorMap* map, int row, int64_t y) {
+        if (F8) {
+          tma_load_2d(raws + ring.s * Plan::kRawBytes + row * DH, map, full, 0, (int)y);
+        } else {
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h) tma_load_2d(slots + ring.s * Plan::kSlotBytes + h * (kTile * 128) + row * 128, map, full, 64 * h, (int)y);
+        }
+      };
+      if (!there || b.left >= box_rows) {
+        copy(whole, lane * box_rows, y);
+      } else {                                         // what stands behind the prefix in its last block is not for the products: it may be anything
+        for (int r = 0; r < box_rows; r += kPrefixStep) copy(step, lane * box_rows + r, r < b.left ? y + r : cache_rows);
+      }
+    }
+    __syncwarp();
+    ++issued;
+    ring.next(kRing);
+    return true;
+  };
+  bool ok = true;
+  int loaded = 0;                                      // tiles whose values have been asked for
+  auto load_until = [&](int most) {                    // of loads
+    while (ok && loaded < n_tiles && issued + 2 <= most) {
+      box[2] = look_up(loaded + 2);
+      if (loaded + 1 < n_tiles) ok = load(box[1], &maps.whole[0], &maps.step[0], loaded + 1);
+      ok = ok && load(box[0], &maps.whole[1], &maps.step[1], -1);
+      box[0] = box[1];
+      box[1] = box[2];
+      ++loaded;
+    }
+  };
+  if (warp == kLoadWarp) {                             // the first loads, ahead of everything else
+    box[0] = look_up(0);
+    box[1] = look_up(1);
+    load(box[0], &maps.whole[0], &maps.step[0], 0);
+    load_until(kRing);
   }
+  const int quad = warp & 3, half = warp >> 2 & 1, mine = quad * 32 + lane;      // a softmax thread's query of a tile, and half of its scores
+      // Rows that do not see the whole prefix take it with their own keys: -1
+      auto row_of = [&](const Walk& u) {
+        const int item = u.first_item() + mine;
+        if (item >= u.group.rows * p.G) return -1;
+        int seq;
+        const int t = u.group.row0 + item / p.G;
+        return row_keys(p, t, &seq, false) >= u.group.prefix ? t : -1;
+      };
+      // A unit's queries are copied when the last product with those before them is done, and are handed over a tile's softmax later.
+      auto ask_queries = [&](const Walk& u, int t) {
+        const __nv_bfloat16* q = p.q + (size_t)max(t, 0) * p.ldq + (size_t)(u.head() * p.G + (u.first_item() + mine) % p.G) * DH + half * kHalf;
+  #pragma unroll
+        for (int i = 0; i < kHalf / 8; ++i) {
+          const int c = half * (kHalf / 8) + i;
+          copy16_or_zero(base + (c >> 3) * (kM * 128) + mine * 128 + (((c & 7) ^ (mine & 7)) << 4), q + 8 * i, t >= 0 ? 16 : 0);
+        }
+        copies_commit();
+      };
+      auto hand_over = [&](uint32_t bar) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+      };
+      auto queries_there = [&]() {
+        copies_wait<0>();
+        fence_proxy_async_smem();
+        hand_over(bar_queries);
+      };
+  int row = -1;
   if (warp < kSoftmaxWarps) {
-    const uint4* q = reinterpret_cast<const uint4*>(p.q + (size_t)max(row, 0) * p.ldq + (size_t)head * DH);
-    uint4 v[DH / 8];
-#pragma unroll
-    for (int c = 0; c < DH / 8; ++c) v[c] = row >= 0 ? q[c] : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-    for (int c = 0; c < DH / 8; ++c)
-      *reinterpret_cast<uint4*>(smem + (c >> 3) * (kM * 128) + tid * 128 + (((c & 7) ^ (tid & 7)) << 4)) = v[c];
-    fence_proxy_async_smem();
+    row = row_of(start);
+    ask_queries(start, row);
   }
+  if (warp == kScoreWarp) tmem_alloc(smem_u32(tmem_slot), kTmemCols);
   tcgen05_fence_before();
   __syncthreads();
   tcgen05_fence_after();
-  const uint32_t tmem = *tmem_slot, tmem_o = tmem, tmem_s = tmem + DH;      // O, then the two buffers of scores
-  bool ok = true;
-  int issued = 0;                                      // loads of the load warp
-  // key and value tile of the i-th load: K0 K1 V0 K2 V1 ... (K0 V0 for a single tile)
-  auto is_key = [&](int i) { return n_tiles == 1 ? i == 0 : i < 2 || (i < 2 * n_tiles - 1 && (i & 1)); };
-  auto tile_of = [&](int i) { return n_tiles == 1 ? 0 : i < 2 ? i : i == 2 * n_tiles - 1 ? n_tiles - 1 : (i & 1) ? (i + 1) / 2 : i / 2 - 1; };
+  const uint32_t tmem = *tmem_slot, tmem_s = tmem + Plan::kColScores, tmem_w = tmem + Plan::kColWeights, tmem_o = tmem + Plan::kColSums;
 
   if (warp == kLoadWarp) {
-    // lanes 0 .. boxes - 1 each copy a box of a tile (a block of the cache, or 64 keys of one)
-    const int boxes = kPrefixTile / box_rows, in_block = (1 << p.log2_block) - 1;
-    constexpr int kRing = F8 ? kRawSlots : kSlots;
-    auto look_up = [&](int i) { return i < 2 * n_tiles && lane < boxes ? pages[(k0 + tile_of(i) * kPrefixTile + lane * box_rows) >> p.log2_block] : 0; };
-    Ring ring;
-    int page = look_up(0);
-    for (int i = 0; i < 2 * n_tiles; ++i) {
-      const int next = look_up(i + 1);
-      const uint32_t full = F8 ? bar_raw_full(ring.s) : bar_full(ring.s), empty = F8 ? bar_raw_empty(ring.s) : bar_empty(ring.s);
-      if (!__all_sync(0xffffffffu, mbar_wait(empty, ring.ph ^ 1u, abort_flag, limit))) { ok = false; break; }
-      if (lane == 0) mbar_arrive_expect_tx(full, F8 ? Plan::kRawBytes : Plan::kSlotBytes);
-      __syncwarp();
-      if (lane < boxes) {
-        const bool key = is_key(i);
-        const int at = k0 + tile_of(i) * kPrefixTile + lane * box_rows;
-        const bool fine = (unsigned)page < (unsigned)p.n_blocks;
-        if (!fine && p.status) atomicOr(p.status, kStatusBadToken);
-        // a block out of range is read behind the cache's end, which gives zeros
-        const int y = (int)(fine ? (((int64_t)page * p.Hkv + hk) << p.log2_block) + (at & in_block) : cache_rows);
-        const CUtensorMap* map = key ? &keys_map : &values_map;
-        if (F8) {
-          tma_load_2d(raws + ring.s * Plan::kRawBytes + lane * box_rows * DH, map, full, 0, y);
-        } else {
-#pragma unroll
-          for (int h = 0; h < kHalves; ++h)
-            tma_load_2d(slots + ring.s * Plan::kSlotBytes + h * (kPrefixTile * 128) + lane * box_rows * 128, map, full, 64 * h, y);
-        }
-      }
-      __syncwarp();
-      ++issued;
-      ring.next(kRing);
-      page = next;
-    }
+    load_until(INT32_MAX);
     if (!ok) *abort_flag = 1;
-  } else if (warp == kIssueWarp) {
-    if (lane == 0) {
-      constexpr uint32_t kIdescS = umma_idesc_bf16(kM, kPrefixTile), kIdescO = umma_idesc_bf16(kM, DH) | kIdescBMnMajor;
-      Ring ring;
-      auto scores = [&](int j) {                       // S of tile j
-        if (!mbar_wait(bar_full(ring.s), ring.ph, abort_flag, limit)) return false;
-        tcgen05_fence_after();
-        const uint32_t k = slots + ring.s * Plan::kSlotBytes;
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            umma_bf16(tmem_s + (j & 1) * kPrefixTile, umma_desc_k_major_sw128(base + h * (kM * 128) + 32 * e),
-                      umma_desc_k_major_sw128(k + h * (kPrefixTile * 128) + 32 * e), kIdescS, h + e > 0);
-        umma_commit(bar_empty(ring.s));
-        umma_commit(bar_scores(j & 1));
-        ring.next(kSlots);
-        return true;
-      };
-      for (int j = 0; j < 2 && ok && j < n_tiles; ++j) ok = scores(j);
-      for (int j = 0; j < n_tiles && ok; ++j) {
-        ok = mbar_wait(bar_weights(j & 1), (uint32_t)(j >> 1) & 1u, abort_flag, limit) && mbar_wait(bar_full(ring.s), ring.ph, abort_flag, limit);
+  } else if (warp == kScoreWarp || warp == kValueWarp) {
+    // One warp issues the products for the scores, one those with the values: an issue waits for the tensor cores' queue, and then does
+    // not hold up the waits for the other's operands.  The whole warp goes through the loop and one lane issues.
+    constexpr uint32_t kIdescS = umma_idesc_bf16(kM, kTile), kIdescO = umma_idesc_bf16(kM, DH) | kIdescBMnMajor;
+    auto wait = [&](uint32_t bar, int phase) { return __all_sync(0xffffffffu, mbar_wait_likely(bar, (uint32_t)phase & 1u, abort_flag, limit)); };
+    Walk w = start;
+    int unit = 0;                                      // units since the start
+    bool first = true;                                 // first tile of its unit
+    if (warp == kScoreWarp) {
+      for (int j = 0; j < n_tiles; ++j) {
+        const int load = j < 2 ? j : 2 * j - 1, slot = load % kSlots;            // the tile's place among the loads
+        ok = wait(bar_full(slot), load / kSlots) && (j == 0 || wait(bar_taken, j - 1)) && (!first || wait(bar_queries, unit));
         if (!ok) break;
         tcgen05_fence_after();
-        const uint32_t v = slots + ring.s * Plan::kSlotBytes, w = tmem_s + (j & 1) * kPrefixTile;
+        const uint64_t q = umma_desc_k_major_sw128(base), k = umma_desc_k_major_sw128(slots + slot * Plan::kSlotBytes);
+        if (elect_one()) {
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+          for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            umma_bf16_tmem_a(tmem_o, w + 32 * part + 8 * e, umma_desc_mn_major_sw128(v + 2048 * e, kPrefixTile * 128), kIdescO, j + part + e > 0);
-        umma_commit(bar_empty(ring.s));
-        umma_commit(j + 1 < n_tiles ? bar_values(j & 1) : bar_done);
-        ring.next(kSlots);
-        if (j + 2 < n_tiles) ok = scores(j + 2);
+            for (int e = 0; e < 4; ++e)                // a descriptor's address counts in 16 bytes
+              umma_bf16(tmem_s, q + h * (kM * 128 / 16) + 2 * e, k + h * (kTile * 128 / 16) + 2 * e, kIdescS, h + e > 0);
+          umma_commit(bar_empty(slot));
+          umma_commit(bar_scores);
+          mbar_arrive(bar_scores);                     // hands on what the load warp wrote of the tile
+        }
+        __syncwarp();
+        first = w.at_end();
+        unit += first;
+        w.next(p);
       }
-      if (!ok) {
-        *abort_flag = 1;
-        umma_commit(bar_drain);                        // what was issued is given time to end before the tensor memory is freed
-        mbar_wait(bar_drain, 0, never_set, limit);
+    } else {
+      for (int j = 0; j < n_tiles; ++j) {
+        const int load = j + 1 < n_tiles ? 2 * j + 2 : 2 * n_tiles - 1, slot = load % kSlots;
+        ok = wait(bar_full(slot), load / kSlots) && wait(bar_weights, j) && (!first || unit == 0 || wait(bar_read, unit - 1));
+        if (!ok) break;
+        tcgen05_fence_after();
+        const uint64_t v = umma_desc_mn_major_sw128(slots + slot * Plan::kSlotBytes, kTile * 128);
+        const uint32_t add = !first;
+        if (elect_one()) {
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int e = 0; e < kTile / 16; ++e) umma_bf16_tmem_a(tmem_o, tmem_w + kTile / 2 * part + 8 * e, v + e * (2048 / 16), kIdescO, part + e > 0 ? 1 : add);
+          umma_commit(bar_empty(slot));
+          umma_commit(bar_values);
+        }
+        __syncwarp();
+        first = w.at_end();
+        unit += first;
+        w.next(p);
       }
     }
+    if (!ok) {
+      *abort_flag = 1;
+      // what was issued is given time to end before the tensor memory is freed
+      const uint32_t drain = bar_drain + (warp == kValueWarp ? 8u : 0u);
+      if (elect_one()) umma_commit(drain);
+      __syncwarp();
+      mbar_wait(drain, 0, never_set, limit);
+    }
   } else if (warp < kSoftmaxWarps) {
-    if (warp < active_warps) {
-      const float factor = p.scale_log2e;
-      const uint32_t my_lane = (uint32_t)(warp * 32) << 16;
-      float m = -INFINITY, ref = 0.0f, sum = 0.0f;
-      auto look_up = [&](int j) {                      // lanes 0 .. 3: is this sixteenth key's block in the cache?
-        return j >= n_tiles || lane >= 4 || (unsigned)pages[(k0 + j * kPrefixTile + 16 * lane) >> p.log2_block] < (unsigned)p.n_blocks;
-      };
-      bool fine = look_up(0);
-      for (int j = 0; j < n_tiles; ++j) {
-        const unsigned there = __ballot_sync(0xffffffffu, fine);
-        fine = look_up(j + 1);
-        const uint32_t at = tmem_s + my_lane + (j & 1) * kPrefixTile;
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_scores(j & 1), (uint32_t)(j >> 1) & 1u, abort_flag, limit))) { ok = false; break; }
-        tcgen05_fence_after();
-        uint32_t s[kPrefixTile];
-        tmem_ld32(at, s);
-        tmem_ld32(at + 32, s + 32);
-        if (there != 0xffffffffu) {                    // keys of blocks out of range: nothing
+    const uint32_t my_lane = (uint32_t)(quad * 32) << 16, pair = 1 + quad;
+    float* const halves = reinterpret_cast<float*>(smem + Plan::kOffHalves);     // [2][kM]
+    const float2 factor = make_float2(p.scale_log2e, p.scale_log2e);
+    // The walk of a warp is in shared memory: inside a unit its registers are needed for the scores.
+    Walk* const place = reinterpret_cast<Walk*>(smem + Plan::kOffWalks + 64 * warp);
+    static_assert(sizeof(Walk) <= 64, "");
+    auto unit_after = [&]() {
+      Walk u = *place;
+      u.next_unit(p);
+      return u;
+    };
+    *place = start;                                    // the same from every lane
+    __syncwarp();
+    queries_there();
+    // After a failed wait a warp goes on through the loops, so that its barriers are met; what it computes means nothing then.
+    auto wait = [&](uint32_t bar, int phase) {
+      if (!__all_sync(0xffffffffu, mbar_wait_likely(bar, (uint32_t)phase & 1u, abort_flag, limit))) { ok = false; *abort_flag = 1; }
+      tcgen05_fence_after();
+    };
+    for (int j = 0; j < n_tiles;) {
+      int count, number, next_row = -1;                // tiles of this unit that are this CTA's; the unit's number
+      bool active;                                     // any query for this warp
+      {
+        const Walk w = *place;
+        count = min(n_tiles - j, w.group.key_tiles - w.key_tile);
+        number = w.number;
+        active = w.first_item() + quad * 32 < w.group.rows * p.G;
+      }
+      const bool more = j + count < n_tiles;
+      if (more) next_row = row_of(unit_after());
+      float m = -INFINITY, ref = 0.0f;
+      float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+      for (int i = 0; i < count; ++i, ++j) {
+        wait(bar_scores, j);
+        const uint32_t there = there_ring[j % kThereRing] >> (2 * half) & 3u;
+        uint32_t s[32];
+        if (active) tmem_ld32(tmem_s + my_lane + 32 * half, s);
+        tcgen05_fence_before();
+        hand_over(bar_taken);
+        const bool ask = i + 1 == count && more;
+        if (ask) ask_queries(unit_after(), next_row);
+        if (active) {
+          if (there != 3u) {
 #pragma unroll
-          for (int c = 0; c < kPrefixTile; ++c)
-            if (!(there >> (c / 16) & 1)) s[c] = __float_as_uint(-INFINITY);
-        }
-        float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int c = 0; c < kPrefixTile; ++c) most[c & 3] = fmaxf(most[c & 3], __uint_as_float(s[c]));
-        const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * factor;
-        const bool raise = m == -INFINITY ? top > -INFINITY : top > ref + kSlack;
-        if (__any_sync(0xffffffffu, raise)) {
-          float by = 1.0f;
-          if (raise) {
-            by = m == -INFINITY ? 0.0f : fast_exp2(ref - top);
-            m = ref = top;
-            sum *= by;
+            for (int c = 0; c < 32; ++c)
+              if (!(there >> (c / 16) & 1)) s[c] = __float_as_uint(-INFINITY);
           }
-          if (j > 0) {                                 // O holds the tiles before this one, once their product is done
-            if (!__all_sync(0xffffffffu, mbar_wait(bar_values((j - 1) & 1), (uint32_t)((j - 1) >> 1) & 1u, abort_flag, limit))) { ok = false; break; }
-            tcgen05_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < DH; c += 32) {
-              uint32_t o[32];
-              tmem_ld32(tmem_o + my_lane + c, o);
+          float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-              tmem_st32(tmem_o + my_lane + c, o);
+          for (int c = 0; c < 32; c += 4) {
+            most[0] = max3(most[0], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+            most[1] = max3(most[1], __uint_as_float(s[c + 2]), __uint_as_float(s[c + 3]));
+          }
+          float top = fmaxf(most[0], most[1]) * p.scale_log2e;
+          if (any_of_pair(pair, m == -INFINITY ? top > -INFINITY : top > ref + kSlack)) {
+            halves[half * kM + mine] = top;
+            named_bar_sync(pair, 64);
+            top = fmaxf(top, halves[(half ^ 1) * kM + mine]);
+            float by = 1.0f;
+            if (m == -INFINITY ? top > -INFINITY : top > ref + kSlack) {
+              by = m == -INFINITY ? 0.0f : fast_exp2(ref - top);
+              m = ref = top;
+#pragma unroll
+              for (int e = 0; e < 2; ++e) sum[e] = make_float2(sum[e].x * by, sum[e].y * by);
+            }
+            if (i > 0) {                               // O holds the unit's tiles before this one, once their product is done
+              wait(bar_values, j - 1);
+              const uint32_t o_at = tmem_o + my_lane + half * kHalf;
+#pragma unroll 1
+              for (int c = 0; c < kHalf; c += 16) {
+                uint32_t o[16];
+                tmem_ld16(o_at + c, o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                tmem_st16(o_at + c, o);
+              }
             }
           }
-        }
-        float part[4] = {};
+          const float2 less = make_float2(-ref, -ref), up = make_float2(1.0f + 0x1p-20f, 1.0f + 0x1p-20f);
+          if (j > 0) wait(bar_values, j - 1);          // the weights before these have been used
 #pragma unroll
-        for (int c0 = 0; c0 < kPrefixTile; c0 += 32) {
-          uint32_t hi[16], lo[16];
+          for (int c0 = 0; c0 < 32; c0 += 16) {
+            uint32_t hi[8], lo[8];
 #pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            const float a = fast_exp2(fmaf(__uint_as_float(s[c0 + c]), factor, -ref)), b = fast_exp2(fmaf(__uint_as_float(s[c0 + c + 1]), factor, -ref));
-            part[c & 2] += a;
-            part[(c & 2) + 1] += b;
-            // both terms above zero for a weight above zero, so that an infinite value stays one
-            const uint32_t x = below(a), y = below(b);
-            hi[c / 2] = __byte_perm(x, y, 0x7632);
-            lo[c / 2] = pack_bf16x2(a - upper_half(x), b - upper_half(y));
+            for (int c = 0; c < 16; c += 2) {
+              const float2 x = fma2(make_float2(__uint_as_float(s[c0 + c]), __uint_as_float(s[c0 + c + 1])), factor, less);
+              const float2 v = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+              sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], v);
+              // the first term is the weight cut to bf16, the second what is left and 2^-20 of the weight: above zero, as the first is, for a
+              // weight above zero, so that an infinite value stays one
+              const uint32_t a = __float_as_uint(v.x), b = __float_as_uint(v.y);
+              hi[c / 2] = __byte_perm(a, b, 0x7632);
+              const float2 rest = fma2(v, up, make_float2(__uint_as_float((a & 0xffff0000u) ^ 0x80000000u), __uint_as_float((b & 0xffff0000u) ^ 0x80000000u)));
+              lo[c / 2] = pack_bf16x2(rest.x, rest.y);
+            }
+            tmem_st8(tmem_w + my_lane + 16 * half + c0 / 2, hi);
+            tmem_st8(tmem_w + my_lane + kTile / 2 + 16 * half + c0 / 2, lo);
           }
-          tmem_st16(at + c0 / 2, hi);
-          tmem_st16(at + 32 + c0 / 2, lo);
+          tmem_wait_st();
+        } else if (j > 0) {
+          wait(bar_values, j - 1);
         }
-        sum += (part[0] + part[1]) + (part[2] + part[3]);
-        tmem_wait_st();
         tcgen05_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_weights(j & 1));
+        hand_over(bar_weights);
+        if (ask) queries_there();
       }
-      ok = ok && __all_sync(0xffffffffu, mbar_wait(bar_done, 0, abort_flag, limit));
-      if (ok) {
-        tcgen05_fence_after();
-        const size_t at = ((size_t)max(row, 0) * p.H + head) * total_splits + split;
-#pragma unroll 1
-        for (int c = 0; c < DH; c += 32) {
+      // the unit's sums leave tensor memory
+      wait(bar_values, j - 1);
+      const size_t part = (size_t)(blockIdx.x + number) * p.prefix_rows + mine;
+      if (active) {
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 32) {
           uint32_t o[32];
-          tmem_ld32(tmem_o + my_lane + c, o);
+          tmem_ld32(tmem_o + my_lane + half * kHalf + c, o);
           if (row >= 0) {
-            uint4* out = reinterpret_cast<uint4*>(p.part_o + at * DH + c);
+            uint4* out = reinterpret_cast<uint4*>(p.prefix_o + part * DH + half * kHalf + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) out[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           }
         }
-        if (row >= 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(m == -INFINITY ? -INFINITY : ref, sum);
-      } else {
-        *abort_flag = 1;
       }
+      tcgen05_fence_before();
+      hand_over(bar_read);
+      if (active) {
+        const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        halves[half * kM + mine] = all;
+        named_bar_sync(pair, 64);
+        if (row >= 0 && half == 0) *reinterpret_cast<float2*>(p.prefix_ml + 2 * part) = make_float2(m == -INFINITY ? -INFINITY : ref, all + halves[kM + mine]);
+        named_bar_sync(pair, 64);                      // read before the next unit's tiles write there
+      }
+      const Walk after = unit_after();
+      __syncwarp();
+      *place = after;
+      __syncwarp();
+      row = next_row;
     }
-  } else if (F8) {
+  } else if (F8 && warp >= kFirstConvertWarp) {
     // converters: a tile's codes to bf16 (exact), into the swizzled layout of the products
     const int c0 = tid - kFirstConvertWarp * 32;
-    Ring raw, ring;
+    Ring raw;
     for (int i = 0; i < 2 * n_tiles; ++i) {
-      if (!__all_sync(0xffffffffu, mbar_wait(bar_raw_full(raw.s), raw.ph, abort_flag, limit) && mbar_wait(bar_empty(ring.s), ring.ph ^ 1u, abort_flag, limit))) {
+      if (!__all_sync(0xffffffffu, mbar_wait_likely(bar_raw_full(raw.s), raw.ph, abort_flag, limit) && mbar_wait(bar_empty(ring.s), ring.ph ^ 1u, abort_flag, limit))) {
         ok = false;
         break;
       }
       const uint32_t src = raws + raw.s * Plan::kRawBytes;
       uint8_t* const dst = smem + Plan::kOffSlots + ring.s * Plan::kSlotBytes;
-      constexpr int kUnits = kPrefixTile * DH / 16, kRowUnits = DH / 16;
-#pragma unroll
-      for (int u0 = 0; u0 < kUnits; u0 += kConvertWarps * 32) {
-        const int u = u0 + c0, r = u / kRowUnits, c = u % kRowUnits, h = c >> 2;
+      constexpr int kUnits = kTile * DH / 16, kRowUnits = DH / 16;
+#pragma unroll 4
+      for (int u = c0; u < kUnits; u += kConvertWarps * 32) {
+        const int r = u / kRowUnits, c = u % kRowUnits, h = c >> 2;
         const uint4 raw16 = lds16(src + 16 * u);
-        const uint32_t w[4] = {raw16.x, raw16.y, raw16.z, raw16.w};
+        const uint32_t codes[4] = {raw16.x, raw16.y, raw16.z, raw16.w};
         uint32_t o[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t a, b;
-          asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.rn.f16x2.e4m3x2 %0, x;\ncvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(a), "=r"(b) : "r"(w[e]));
+          asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.rn.f16x2.e4m3x2 %0, x;\ncvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(a), "=r"(b) : "r"(codes[e]));
           const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&a)), g = __half22float2(*reinterpret_cast<const __half2*>(&b));
           o[2 * e] = pack_bf16x2(f.x, f.y);
           o[2 * e + 1] = pack_bf16x2(g.x, g.y);
         }
         // the second half's lanes write their two units the other way round: eight lanes then meet eight different banks
-        uint8_t* const at = dst + h * (kPrefixTile * 128) + r * 128;
+        uint8_t* const at = dst + h * (kTile * 128) + r * 128;
         const int first = 2 * (c & 3) + h, second = first ^ 1;
         const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
         *reinterpret_cast<uint4*>(at + ((first ^ (r & 7)) << 4)) = h ? hi : lo;
@@ -358,7 +545,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap keys_map, const __gr
         mbar_arrive(bar_full(ring.s));
         mbar_arrive(bar_raw_empty(raw.s));
       }
-      raw.next(kRawSlots > 0 ? kRawSlots : 1);
+      raw.next(kRing);
       ring.next(kSlots);
     }
     if (!ok) *abort_flag = 1;
@@ -369,42 +556,167 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap keys_map, const __gr
   tcgen05_fence_before();
   __syncthreads();
   if (warp == kLoadWarp && *abort_flag) {              // loads that nobody waited for are given time to land
-    constexpr int kRing = F8 ? kRawSlots : kSlots;
     for (int i = max(0, issued - kRing); i < issued; ++i)
       mbar_wait(F8 ? bar_raw_full(i % kRing) : bar_full(i % kRing), (uint32_t)(i / kRing) & 1u, never_set, limit);
   }
   __syncthreads();
-  if (warp == kIssueWarp) {
+  if (warp == kScoreWarp) {
     tcgen05_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }
+}
+
+// Joins the parts of a row's head: those of the prefix, where the row has them, and those of its own keys.  A head takes WARPS warps of the
+// CTA, which go over the parts in turn and are added up in their order; a lane has DH / 32 dimensions.
+constexpr int kJoinWarps = 8;
+
+template <int DH, int WARPS>
+__global__ void __launch_bounds__(kJoinWarps * 32)
+prefix_join_kernel(PagedParams p) {
+  constexpr int kDims = DH / 32;
+  struct Dims { float v[kDims]; };
+  __shared__ float part_m[kJoinWarps], part_l[kJoinWarps];
+  __shared__ Dims part_o[kJoinWarps][32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, in_head = warp % WARPS;
+  const int64_t item = (int64_t)blockIdx.x * (kJoinWarps / WARPS) + warp / WARPS;
+  serving_begin();
+  serving_next();
+  const bool there = item < (int64_t)p.R * p.H;        // the same for a head's warps
+  const int row = there ? (int)(item / p.H) : 0, head = (int)(item % p.H);
+  int seq = 0, prefix = 0, n_first = 0;
+  size_t first_part = 0, part_step = 0;
+  const int len = there ? row_keys(p, row, &seq, false) : 0;
+  if (len > 0) {
+    // this row's group, and how many places and units stand before it in the line
+    int places = 0, places_before = 0, units_before = 0, group = -1;
+    bool bad = false;
+    for (int i = lane; i < p.groups.n; i += 32) {
+      const PrefixGroup g = prefix_group(p, i);
+      bad = bad || g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R;
+      const int units = g.units(p.Hkv), all = units * g.places();
+      places += all;
+      if (g.row0 + g.rows <= row) { places_before += all; units_before += units; }
+      else if (g.row0 <= row) group = i;
+    }
+    places = __reduce_add_sync(0xffffffffu, places);
+    places_before = __reduce_add_sync(0xffffffffu, places_before);
+    units_before = __reduce_add_sync(0xffffffffu, units_before);
+    group = __any_sync(0xffffffffu, bad) ? -1 : __reduce_max_sync(0xffffffffu, group);
+    if (group >= 0) {
+      const PrefixGroup g = prefix_group(p, group);
+      if (g.key_tiles && len >= g.prefix) {
+        prefix = g.prefix;
+        const int in_unit = (row - g.row0) * p.G + head % p.G, unit = head / p.G * g.tiles + in_unit / kPrefixQueries;
+        const int stretch = prefix_stretch(p, places), t0 = places_before + unit * g.places();
+        const int c0 = t0 / stretch, c1 = (t0 + g.key_tiles - 1) / stretch;
+        n_first = c1 - c0 + 1;
+        first_part = (size_t)(c0 + units_before + unit) * p.prefix_rows + in_unit % kPrefixQueries;
+        part_step = p.prefix_rows;
+      }
+    }
+  }
+  const int own = len - prefix, per = split_keys(p, own), n_own = own > 0 ? (own + per - 1) / per : 0;
+  const bool work = there && (prefix > 0 || n_own > 1);      // other rows are written already
+  const int n = work ? n_first + n_own : 0;
+  const size_t own_part = (size_t)(there ? item : 0) * p.splits;
+  float m = -INFINITY, l = 0.0f;
+  Dims o = {};
+  constexpr int kAhead = 4;                            // parts whose loads are in flight
+  for (int s0 = in_head; s0 < n; s0 += kAhead * WARPS) {
+    float2 ml[kAhead];
+    Dims x[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const int s = s0 + e * WARPS;
+      ml[e] = make_float2(-INFINITY, 0.0f);
+      x[e] = {};
+      if (s >= n) continue;
+      const bool own_keys = s >= n_first;
+      const size_t at = own_keys ? own_part + (s - n_first) : first_part + s * part_step;
+      ml[e] = *reinterpret_cast<const float2*>((own_keys ? p.part_ml : p.prefix_ml) + 2 * at);
+      const float* from = (own_keys ? p.part_o : p.prefix_o) + at * DH + kDims * lane;
+      if constexpr (kDims == 4) {
+        const float4 f = *reinterpret_cast<const float4*>(from);
+        x[e].v[0] = f.x; x[e].v[1] = f.y; x[e].v[2] = f.z; x[e].v[3] = f.w;
+      } else {
+        const float2 f = *reinterpret_cast<const float2*>(from);
+        x[e].v[0] = f.x; x[e].v[1] = f.y;
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) top = fmaxf(top, ml[e].x);
+    const float ref = finite_max(top), by = fast_exp2(m - ref);
+    l *= by;
+#pragma unroll
+    for (int d = 0; d < kDims; ++d) o.v[d] *= by;
+    m = top;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const float w = fast_exp2(ml[e].x - ref);
+      l = fmaf(w, ml[e].y, l);
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) o.v[d] = fmaf(w, x[e].v[d], o.v[d]);
+    }
+  }
+  if (WARPS > 1) {
+    if (lane == 0) { part_m[warp] = m; part_l[warp] = l; }
+    part_o[warp][lane] = o;
+    __syncthreads();
+    if (in_head) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, part_m[warp + w]);
+    const float ref = finite_max(top);
+    l = 0.0f;
+    o = {};
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float by = fast_exp2(part_m[warp + w] - ref);
+      l = fmaf(by, part_l[warp + w], l);
+#pragma unroll
+      for (int d = 0; d < kDims; ++d) o.v[d] = fmaf(by, part_o[warp + w][lane].v[d], o.v[d]);
+    }
+  }
+  if (!work) return;
+  const float f = inverse_sum(p, l);
+  __nv_bfloat16* out = p.out + (size_t)row * p.ldo + (size_t)head * DH + kDims * lane;
+#pragma unroll
+  for (int d = 0; d < kDims; d += 2) *reinterpret_cast<uint32_t*>(out + d) = pack_bf16x2(o.v[d] * f, o.v[d + 1] * f);
 }
 
 template <int DH, bool F8>
 int run_prefix(const PagedParams& p, const qzo_kv_cache& c, cudaStream_t st) {
   using Plan = PrefixPlan<DH, F8>;
   const int64_t rows = (int64_t)c.n_blocks * c.n_kv_heads * c.block_size;
-  const int box_rows = std::min(c.block_size, kPrefixTile);
-  CUtensorMap maps[2];
-  for (int i = 0; i < 2; ++i)
-    QZO_TRY(make_tmap(&maps[i], i ? c.v : c.k, F8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rows, DH, DH * (F8 ? 1 : 2),
-                      F8 ? DH : 64, box_rows, F8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B));
+  const int box_rows = std::min(c.block_size, kTile);
+  PrefixMaps maps;
+  for (int i = 0; i < 4; ++i)
+    QZO_TRY(make_tmap(i < 2 ? &maps.whole[i] : &maps.step[i - 2], i & 1 ? c.v : c.k, F8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rows,
+                      DH, DH * (F8 ? 1 : 2), F8 ? DH : 64, i < 2 ? box_rows : kPrefixStep, F8 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B));
   {
     static std::atomic<unsigned long long> allowed{0};
     QZO_CUDA_TRY(allow_dynamic_smem(prefix_attention_kernel<DH, F8>, Plan::kDynamicBytes, allowed));
   }
-  const int64_t tiles = most_tiles(p.R, p.groups.n, p.G);
-  return launch_serving(prefix_attention_kernel<DH, F8>, dim3((unsigned)(tiles * p.Hkv * p.prefix_splits)), dim3(Plan::kThreads), Plan::kDynamicBytes, 1, st,
-                        maps[0], maps[1], p, (int)tiles, p.prefix_splits + p.splits, rows, box_rows);
+  return launch_serving(prefix_attention_kernel<DH, F8>, dim3(p.prefix_ctas), dim3(Plan::kThreads), Plan::kDynamicBytes, 1, st, maps, p, rows, box_rows);
+}
+
+template <int DH>
+int run_prefix_join(const PagedParams& p, cudaStream_t st) {
+  // as many warps to a head as fill the SMs
+  const int64_t items = (int64_t)p.R * p.H, fill = kSMs * 32 / items;
+  const dim3 block(kJoinWarps * 32);
+  if (fill >= 8) return launch_serving(prefix_join_kernel<DH, 8>, dim3((unsigned)items), block, 0, 1, st, p);
+  if (fill >= 2) return launch_serving(prefix_join_kernel<DH, 4>, dim3((unsigned)ceil_div64(items, kJoinWarps / 4)), block, 0, 1, st, p);
+  return launch_serving(prefix_join_kernel<DH, 1>, dim3((unsigned)ceil_div64(items, kJoinWarps)), block, 0, 1, st, p);
 }
 
 }  // namespace
 
-int64_t prefix_ctas(int R, int n_groups, int G, int Hkv) { return most_tiles(R, n_groups, G) * Hkv; }
-
-int prefix_splits(int R, int n_groups, int G, int Hkv, int max_len) {
-  const int64_t fill = 2 * kSMs / prefix_ctas(R, n_groups, G, Hkv);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(fill, max_len / kPrefixLeast));
+// Every group may leave one unfinished tile of queries.
+int64_t prefix_units(int R, int n_groups, int G, int Hkv) {
+  const int64_t k = std::min(R, n_groups);
+  return (k + ((int64_t)R * G - k) / kM) * Hkv;
 }
 
 int launch_prefix_attention(const PagedParams& p, const qzo_kv_cache& c, cudaStream_t st) {
@@ -412,5 +724,7 @@ int launch_prefix_attention(const PagedParams& p, const qzo_kv_cache& c, cudaStr
   if (c.head_dim == 128) return f8 ? run_prefix<128, true>(p, c, st) : run_prefix<128, false>(p, c, st);
   return f8 ? run_prefix<64, true>(p, c, st) : run_prefix<64, false>(p, c, st);
 }
+
+int launch_prefix_join(const PagedParams& p, int dh, cudaStream_t st) { return dh == 128 ? run_prefix_join<128>(p, st) : run_prefix_join<64>(p, st); }
 
 }  // namespace qzo

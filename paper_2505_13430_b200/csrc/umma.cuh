@@ -78,6 +78,11 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     if (clock64() - t0 > limit) return false;
   }
 }
+// Same bound, for waits that find the phase complete as a rule: one test of it costs a third of a poll's set-up (76 cycles, with the
+// vote of the warp, instead of 196).
+__device__ __forceinline__ bool mbar_wait_likely(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
+  return mbar_try_wait(bar, parity) || mbar_wait(bar, parity, abort_flag, limit);
+}
 // Same bound, for waits that are long and not latency-critical: sleeps between polls so that the
 // waiting warp leaves the issue slots to the working ones.
 __device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
@@ -192,6 +197,12 @@ __device__ __forceinline__ void umma_bf16_tmem_a(uint32_t d_tmem, uint32_t a_tme
       "setp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t v[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
       : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t v[16]) {
