@@ -16,7 +16,7 @@ namespace qzo {
 namespace {
 
 constexpr int kM = kPrefixQueries, kTile = kPrefixTile;
-constexpr int kSoftmaxWarps = 8, kLoadWarp = 8, kScoreWarp = 9, kValueWarp = 10, kFirstConvertWarp = 11, kConvertWarps = 3;
+constexpr int kSoftmaxWarps = 4, kLoadWarp = 4, kScoreWarp = 5, kValueWarp = 6, kFirstConvertWarp = 7, kConvertWarps = 4;
 constexpr int kTmemCols = 256;                         // two CTAs to an SM
 constexpr int kThereRing = 8;                          // tiles whose masks are kept: more than the rings hold
 constexpr float kSlack = 8.0f;                         // by which scores may pass the reference before it is raised
@@ -30,7 +30,7 @@ struct PrefixPlan {
   static constexpr int kSlots = (F8 ? 3 : 4) * 128 / DH, kRawSlots = F8 ? 3 * 128 / DH : 0;
   static constexpr int kOffSlots = kQueryBytes, kOffRaw = kOffSlots + kSlots * kSlotBytes, kOffBars = kOffRaw + kRawSlots * kRawBytes;
   static constexpr int kBars = 2 * kSlots + 2 * kRawSlots + 8;
-  static constexpr int kOffHalves = kOffBars + 8 * kBars, kOffWalks = kOffHalves + 2 * kM * 4, kOffThere = kOffWalks + kSoftmaxWarps * 64, kOffMisc = kOffThere + 4 * kThereRing;
+  static constexpr int kOffWalks = kOffBars + 8 * kBars, kOffThere = kOffWalks + kSoftmaxWarps * 64, kOffMisc = kOffThere + 4 * kThereRing;
   static constexpr int kDynamicBytes = kOffMisc + 16 + 1024;         // slack for the 1024-byte alignment
   static_assert(2 * (kDynamicBytes + 1024) <= 228 * 1024, "two CTAs to an SM");
   static constexpr int kColSums = 0, kColScores = DH, kColWeights = DH + kTile;
@@ -55,13 +55,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// Barrier of 64 threads: whether any of them says so
-__device__ __forceinline__ bool any_of_pair(uint32_t id, bool v) {
-  uint32_t r;
-  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\nbar.red.or.pred q, %1, 64, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"(id), "r"((uint32_t)v) : "memory");
-  return r != 0;
-}
-
 // Keys and values: in boxes of a block's tokens (64 of a larger block), and of 16 tokens for the end of a prefix
 struct PrefixMaps { CUtensorMap whole[2], step[2]; };
 
@@ -145,8 +138,8 @@ __device__ __forceinline__ int find_stretch(const PagedParams& p, int cta, bool 
   return tiles;
 }
 
-// Two CTAs on every SM, each with its stretch of the line of tiles, unit after unit.  S = Q K^T goes to tensor memory; a pair of threads
-// of the softmax warps takes a query's 64 scores into registers, 32 each, upon which the next tile's product may overwrite them, and
+// Two CTAs on every SM, each with its stretch of the line of tiles, unit after unit.  S = Q K^T goes to tensor memory; a thread of
+// the softmax warps takes a query's 64 scores into registers, upon which the next tile's product may overwrite them, and
 // writes their weights beside them, as the sum of two bf16 (2^-15 of a weight; one alone would leave 2^-8, as much as the output's
 // rounding), from where they enter O += P V as the A operand.  O stays in tensor memory; it is rescaled only when a maximum
 // passes the reference by 2^8.
@@ -154,7 +147,7 @@ template <int DH, bool F8>
 __global__ void __launch_bounds__((PrefixPlan<DH, F8>::kThreads), 2)
 prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_constant__ PagedParams p, int64_t cache_rows, int box_rows) {
   using Plan = PrefixPlan<DH, F8>;
-  constexpr int kSlots = Plan::kSlots, kRawSlots = Plan::kRawSlots, kHalves = DH / 64, kRing = F8 ? kRawSlots : kSlots, kHalf = DH / 2;
+  constexpr int kSlots = Plan::kSlots, kRawSlots = Plan::kRawSlots, kHalves = DH / 64, kRing = F8 ? kRawSlots : kSlots;
   extern __shared__ uint8_t prefix_smem[];
   const uint32_t base = (smem_u32(prefix_smem) + 1023u) & ~1023u;
   uint8_t* const smem = prefix_smem + (base - smem_u32(prefix_smem));
@@ -267,34 +260,32 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
     load(box[0], &maps.whole[0], &maps.step[0], 0);
     load_until(kRing);
   }
-  const int quad = warp & 3, half = warp >> 2 & 1, mine = quad * 32 + lane;      // a softmax thread's query of a tile, and half of its scores
-      // Rows that do not see the whole prefix take it with their own keys: -1
-      auto row_of = [&](const Walk& u) {
-        const int item = u.first_item() + mine;
-        if (item >= u.group.rows * p.G) return -1;
-        int seq;
-        const int t = u.group.row0 + item / p.G;
-        return row_keys(p, t, &seq, false) >= u.group.prefix ? t : -1;
-      };
-      // A unit's queries are copied when the last product with those before them is done, and are handed over a tile's softmax later.
-      auto ask_queries = [&](const Walk& u, int t) {
-        const __nv_bfloat16* q = p.q + (size_t)max(t, 0) * p.ldq + (size_t)(u.head() * p.G + (u.first_item() + mine) % p.G) * DH + half * kHalf;
-  #pragma unroll
-        for (int i = 0; i < kHalf / 8; ++i) {
-          const int c = half * (kHalf / 8) + i;
-          copy16_or_zero(base + (c >> 3) * (kM * 128) + mine * 128 + (((c & 7) ^ (mine & 7)) << 4), q + 8 * i, t >= 0 ? 16 : 0);
-        }
-        copies_commit();
-      };
-      auto hand_over = [&](uint32_t bar) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar);
-      };
-      auto queries_there = [&]() {
-        copies_wait<0>();
-        fence_proxy_async_smem();
-        hand_over(bar_queries);
-      };
+  const int mine = tid & (kM - 1);                     // a softmax thread's query of a tile
+  // Rows that do not see the whole prefix take it with their own keys: -1
+  auto row_of = [&](const Walk& u) {
+    const int item = u.first_item() + mine;
+    if (item >= u.group.rows * p.G) return -1;
+    int seq;
+    const int t = u.group.row0 + item / p.G;
+    return row_keys(p, t, &seq, false) >= u.group.prefix ? t : -1;
+  };
+  // A unit's queries are copied when the last product with those before them is done, and are handed over a tile's softmax later.
+  auto ask_queries = [&](const Walk& u, int t) {
+    const __nv_bfloat16* q = p.q + (size_t)max(t, 0) * p.ldq + (size_t)(u.head() * p.G + (u.first_item() + mine) % p.G) * DH;
+#pragma unroll
+    for (int c = 0; c < DH / 8; ++c)
+      copy16_or_zero(base + (c >> 3) * (kM * 128) + mine * 128 + (((c & 7) ^ (mine & 7)) << 4), q + 8 * c, t >= 0 ? 16 : 0);
+    copies_commit();
+  };
+  auto hand_over = [&](uint32_t bar) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+  };
+  auto queries_there = [&]() {
+    copies_wait<0>();
+    fence_proxy_async_smem();
+    hand_over(bar_queries);
+  };
   int row = -1;
   if (warp < kSoftmaxWarps) {
     row = row_of(start);
@@ -370,8 +361,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       mbar_wait(drain, 0, never_set, limit);
     }
   } else if (warp < kSoftmaxWarps) {
-    const uint32_t my_lane = (uint32_t)(quad * 32) << 16, pair = 1 + quad;
-    float* const halves = reinterpret_cast<float*>(smem + Plan::kOffHalves);     // [2][kM]
+    const uint32_t my_lane = (uint32_t)(warp * 32) << 16;
     const float2 factor = make_float2(p.scale_log2e, p.scale_log2e);
     // The walk of a warp is in shared memory: inside a unit its registers are needed for the scores.
     Walk* const place = reinterpret_cast<Walk*>(smem + Plan::kOffWalks + 64 * warp);
@@ -396,7 +386,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
         const Walk w = *place;
         count = min(n_tiles - j, w.group.key_tiles - w.key_tile);
         number = w.number;
-        active = w.first_item() + quad * 32 < w.group.rows * p.G;
+        active = w.first_item() + warp * 32 < w.group.rows * p.G;
       }
       const bool more = j + count < n_tiles;
       if (more) next_row = row_of(unit_after());
@@ -404,32 +394,43 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
       for (int i = 0; i < count; ++i, ++j) {
         wait(bar_scores, j);
-        const uint32_t there = there_ring[j % kThereRing] >> (2 * half) & 3u;
-        uint32_t s[32];
-        if (active) tmem_ld32(tmem_s + my_lane + 32 * half, s);
-        tcgen05_fence_before();
-        hand_over(bar_taken);
         const bool ask = i + 1 == count && more;
-        if (ask) ask_queries(unit_after(), next_row);
-        if (active) {
-          if (there != 3u) {
+        const uint32_t there = there_ring[j % kThereRing];
+        constexpr uint32_t kAll = (1u << kTile / kPrefixStep) - 1;
+        // Scores are kept in registers where there are enough, and read again otherwise.
+        constexpr bool kKeep = !F8;
+        uint32_t s[kKeep ? kTile : kTile / 2];
+        auto fetch = [&](int half) {
+          uint32_t* const to = s + (kKeep ? 32 * half : 0);
+          tmem_ld32(tmem_s + my_lane + 32 * half, to);
+          if (there != kAll) {                         // keys behind the prefix and of blocks out of range: nothing
 #pragma unroll
             for (int c = 0; c < 32; ++c)
-              if (!(there >> (c / 16) & 1)) s[c] = __float_as_uint(-INFINITY);
+              if (!(there >> (2 * half + c / kPrefixStep) & 1)) to[c] = __float_as_uint(-INFINITY);
           }
+        };
+        if (active) {
           float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 0; c < 32; c += 4) {
-            most[0] = max3(most[0], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
-            most[1] = max3(most[1], __uint_as_float(s[c + 2]), __uint_as_float(s[c + 3]));
+          for (int half = 0; half < 2; ++half) {
+            fetch(half);
+            const uint32_t* const from = s + (kKeep ? 32 * half : 0);
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+              most[0] = max3(most[0], __uint_as_float(from[c]), __uint_as_float(from[c + 1]));
+              most[1] = max3(most[1], __uint_as_float(from[c + 2]), __uint_as_float(from[c + 3]));
+            }
           }
-          float top = fmaxf(most[0], most[1]) * p.scale_log2e;
-          if (any_of_pair(pair, m == -INFINITY ? top > -INFINITY : top > ref + kSlack)) {
-            halves[half * kM + mine] = top;
-            named_bar_sync(pair, 64);
-            top = fmaxf(top, halves[(half ^ 1) * kM + mine]);
+          if (kKeep) {
+            tcgen05_fence_before();
+            hand_over(bar_taken);
+          }
+          if (ask) ask_queries(unit_after(), next_row);
+          const float top = fmaxf(most[0], most[1]) * p.scale_log2e;
+          const bool raise = m == -INFINITY ? top > -INFINITY : top > ref + kSlack;
+          if (__any_sync(0xffffffffu, raise)) {
             float by = 1.0f;
-            if (m == -INFINITY ? top > -INFINITY : top > ref + kSlack) {
+            if (raise) {
               by = m == -INFINITY ? 0.0f : fast_exp2(ref - top);
               m = ref = top;
 #pragma unroll
@@ -437,25 +438,31 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
             }
             if (i > 0) {                               // O holds the unit's tiles before this one, once their product is done
               wait(bar_values, j - 1);
-              const uint32_t o_at = tmem_o + my_lane + half * kHalf;
 #pragma unroll 1
-              for (int c = 0; c < kHalf; c += 16) {
+              for (int c = 0; c < DH; c += 16) {
                 uint32_t o[16];
-                tmem_ld16(o_at + c, o);
+                tmem_ld16(tmem_o + my_lane + c, o);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-                tmem_st16(o_at + c, o);
+                tmem_st16(tmem_o + my_lane + c, o);
               }
             }
           }
           const float2 less = make_float2(-ref, -ref), up = make_float2(1.0f + 0x1p-20f, 1.0f + 0x1p-20f);
-          if (j > 0) wait(bar_values, j - 1);          // the weights before these have been used
 #pragma unroll
-          for (int c0 = 0; c0 < 32; c0 += 16) {
+          for (int c0 = 0; c0 < kTile; c0 += 16) {
+            if (!kKeep && c0 % 32 == 0) {
+              fetch(c0 / 32);
+              if (c0 > 0) {
+                tcgen05_fence_before();
+                hand_over(bar_taken);
+              }
+            }
             uint32_t hi[8], lo[8];
 #pragma unroll
             for (int c = 0; c < 16; c += 2) {
-              const float2 x = fma2(make_float2(__uint_as_float(s[c0 + c]), __uint_as_float(s[c0 + c + 1])), factor, less);
+              const uint32_t* const from = s + (kKeep ? c0 : c0 % 32) + c;
+              const float2 x = fma2(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), factor, less);
               const float2 v = make_float2(fast_exp2(x.x), fast_exp2(x.y));
               sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], v);
               // the first term is the weight cut to bf16, the second what is left and 2^-20 of the weight: above zero, as the first is, for a
@@ -465,12 +472,15 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
               const float2 rest = fma2(v, up, make_float2(__uint_as_float((a & 0xffff0000u) ^ 0x80000000u), __uint_as_float((b & 0xffff0000u) ^ 0x80000000u)));
               lo[c / 2] = pack_bf16x2(rest.x, rest.y);
             }
-            tmem_st8(tmem_w + my_lane + 16 * half + c0 / 2, hi);
-            tmem_st8(tmem_w + my_lane + kTile / 2 + 16 * half + c0 / 2, lo);
+            if (c0 == 0 && j > 0) wait(bar_values, j - 1);       // the weights before these have been used
+            tmem_st8(tmem_w + my_lane + c0 / 2, hi);
+            tmem_st8(tmem_w + my_lane + kTile / 2 + c0 / 2, lo);
           }
           tmem_wait_st();
-        } else if (j > 0) {
-          wait(bar_values, j - 1);
+        } else {
+          hand_over(bar_taken);
+          if (ask) ask_queries(unit_after(), next_row);
+          if (j > 0) wait(bar_values, j - 1);
         }
         tcgen05_fence_before();
         hand_over(bar_weights);
@@ -480,26 +490,20 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       wait(bar_values, j - 1);
       const size_t part = (size_t)(blockIdx.x + number) * p.prefix_rows + mine;
       if (active) {
-#pragma unroll
-        for (int c = 0; c < kHalf; c += 32) {
+#pragma unroll 1
+        for (int c = 0; c < DH; c += 32) {
           uint32_t o[32];
-          tmem_ld32(tmem_o + my_lane + half * kHalf + c, o);
+          tmem_ld32(tmem_o + my_lane + c, o);
           if (row >= 0) {
-            uint4* out = reinterpret_cast<uint4*>(p.prefix_o + part * DH + half * kHalf + c);
+            uint4* out = reinterpret_cast<uint4*>(p.prefix_o + part * DH + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) out[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           }
         }
+        if (row >= 0) *reinterpret_cast<float2*>(p.prefix_ml + 2 * part) = make_float2(m == -INFINITY ? -INFINITY : ref, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
       }
       tcgen05_fence_before();
       hand_over(bar_read);
-      if (active) {
-        const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        halves[half * kM + mine] = all;
-        named_bar_sync(pair, 64);
-        if (row >= 0 && half == 0) *reinterpret_cast<float2*>(p.prefix_ml + 2 * part) = make_float2(m == -INFINITY ? -INFINITY : ref, all + halves[kM + mine]);
-        named_bar_sync(pair, 64);                      // read before the next unit's tiles write there
-      }
       const Walk after = unit_after();
       __syncwarp();
       *place = after;
