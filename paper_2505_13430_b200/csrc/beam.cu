@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace qzo {
 namespace {
@@ -82,13 +83,18 @@ __device__ __forceinline__ bool best_head(uint32_t order, uint32_t token, uint32
 }
 
 // A CTA = a chunk of a row.  One pass: every thread keeps a running maximum and sum of exponentials, every warp the W best logits
-// it has met, one to a lane in order.  A tile's logits come into the list as the largest that is above the list's last, then
-// the next, until none is: W turns for the first tile, few for those after it.
+// it has met, one to a lane in order.  A logit is a candidate only if it reaches what W others are known to reach: the last of the
+// warp's list, or the least, over the eight warps, of the (W / 8)-th largest of a warp's lanes' maxima, which leaves about twenty of
+// the first tile's 4096 for W = 8; a candidate is put in its place by the whole warp.
+// Exponentials are 2^(x c), c = log2 e in fp32: the sums' logarithm is divided by that c in the end, so that its rounding (2^-26) counts
+// for a distribution's entropy only.
 template <bool VEC>
 __global__ void __launch_bounds__(kScanThreads)
 beam_scan_kernel(BeamParams p) {
   __shared__ uint2 lists[kScanWarps][32];
   __shared__ float2 warp_sums[kScanWarps];
+  __shared__ uint2 found[kScanWarps][32 * kLaneValues];              // candidates of a tile
+  __shared__ volatile uint32_t reached[kScanWarps];    // order of a logit that ceil(W / 8) of a warp's lanes have reached
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int beam = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
   serving_begin();
@@ -98,17 +104,17 @@ beam_scan_kernel(BeamParams p) {
   const int t0 = chunk * p.per, t1 = min(p.V, t0 + p.per);
 
   uint32_t list_order = kNone, list_token = 0xffffffffu;
-  uint32_t least = kNone;                              // order of the list's last entry, the W-th
+  uint32_t least_order = kNone, least_token = 0xffffffffu;           // the list's last entry, the W-th
   float m = -INFINITY, sum = 0.0f;
   bool bad = false;
   float v[kLaneValues];
   auto token_of = [&](int base, int i) { return VEC ? base + ((i >> 2) * kScanThreads + tid) * 4 + (i & 3) : base + i * kScanThreads + tid; };
-  auto load = [&](int base) {
+  auto load = [&](int base, auto whole) {              // whole: the tile does not reach beyond the chunk
     if (VEC) {
 #pragma unroll
       for (int i = 0; i < kLaneValues; i += 4) {
         const int t = token_of(base, i);
-        if (t + 3 < t1) {
+        if (whole.value || t + 3 < t1) {
           const float4 q = *reinterpret_cast<const float4*>(x + t);
           v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
         } else {
@@ -120,56 +126,92 @@ beam_scan_kernel(BeamParams p) {
 #pragma unroll
       for (int i = 0; i < kLaneValues; ++i) {
         const int t = token_of(base, i);
-        v[i] = t < t1 ? x[t] : -INFINITY;
+        v[i] = whole.value || t < t1 ? x[t] : -INFINITY;
       }
     }
   };
   for (int base = t0; base < t1; base += kTileValues) {
-    load(base);
-    float most = -INFINITY;
+    if (base + kTileValues <= t1) load(base, std::true_type{});
+    else load(base, std::false_type{});
+    float most, part;
+    auto add_up = [&]() {
+      float a = -INFINITY, b = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) {
-      if (!(v[i] < INFINITY)) { bad = true; v[i] = -INFINITY; }      // NaN and +inf count as a token that is not allowed
-      v[i] += 0.0f;                                    // -0 and +0 are one value
-      most = fmaxf(most, v[i]);
-    }
-    const float to = fmaxf(m, most), ref = finite_max(to);
-    sum *= m == -INFINITY ? 0.0f : exp2_fast((m - ref) * kLog2e);
-    m = to;
-    float part[4] = {};
+      for (int i = 0; i < kLaneValues; i += 4) {
+        a = fmaxf(a, fmaxf(v[i], v[i + 1]));
+        b = fmaxf(b, fmaxf(v[i + 2], v[i + 3]));
+      }
+      most = fmaxf(a, b);
+      const float ref = finite_max(fmaxf(m, most)), scaled = ref * kLog2e;
+      float parts[4] = {};
+      if (fabsf(ref) < 0x1p16f) {                      // 2^(x c - scaled); what scaled is off from ref c (2^-8 at most) comes in behind
 #pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) part[i & 3] += exp2_fast((v[i] - ref) * kLog2e);    // the difference first: a product with log2 e would be off by 2^-24 of v
-    sum += (part[0] + part[1]) + (part[2] + part[3]);
-
-    // this lane's best that is not in the list yet
-    uint32_t mine = 0;
-    int at = 0;
-    auto look = [&]() {
-      float top = -INFINITY;
-      at = 0;
+        for (int i = 0; i < kLaneValues; ++i) parts[i & 3] += exp2_fast(fmaf(v[i], kLog2e, -scaled));
+        part = ((parts[0] + parts[1]) + (parts[2] + parts[3])) * exp2_fast(-fmaf(ref, kLog2e, -scaled));
+      } else {                                         // there the difference comes first
+#pragma unroll
+        for (int i = 0; i < kLaneValues; ++i) parts[i & 3] += exp2_fast((v[i] - ref) * kLog2e);
+        part = (parts[0] + parts[1]) + (parts[2] + parts[3]);
+      }
+    };
+    add_up();
+    if (!(most < INFINITY) || part != part) {          // NaN and +inf count as a token that is not allowed
+      bad = true;
 #pragma unroll
       for (int i = 0; i < kLaneValues; ++i)
-        if (v[i] > top) { top = v[i]; at = i; }
-      mine = order_of(top);
-    };
-    look();
-    for (;;) {
-      uint32_t top, low;
-      int who;
-      if (!best_head(mine, (uint32_t)token_of(base, at), &top, &low, &who) || top <= least) break;
-      const int place = __popc(__ballot_sync(0xffffffffu, list_order >= top));
-      const uint32_t up_order = __shfl_up_sync(0xffffffffu, list_order, 1), up_token = __shfl_up_sync(0xffffffffu, list_token, 1);
-      if (lane > place) { list_order = up_order; list_token = up_token; }
-      if (lane == place) { list_order = top; list_token = low; }
-      least = __shfl_sync(0xffffffffu, list_order, p.W - 1);
-      if (lane == who) {
-#pragma unroll
-        for (int i = 0; i < kLaneValues; ++i)
-          if (i == at) v[i] = -INFINITY;
-        look();
-      }
-      __syncwarp();
+        if (!(v[i] < INFINITY)) v[i] = -INFINITY;
+      add_up();
     }
+    const float to = fmaxf(m, most);
+    sum = sum * (m == -INFINITY ? 0.0f : exp2_fast((m - to) * kLog2e)) + part;
+    m = to;
+
+    uint32_t top = order_of(m + 0.0f);
+    for (int r = kScanWarps; r < p.W; r += kScanWarps) {               // without the largest, as often as it takes
+      const uint32_t most = __reduce_max_sync(0xffffffffu, top);
+      if (lane == __ffs(__ballot_sync(0xffffffffu, top == most)) - 1) top = 0;
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) reached[warp] = top;
+    if (base == t0) __syncthreads();                   // later, what another warp has not written yet is lower than it might be, no more
+    else __syncwarp();
+    const uint32_t floor = max(least_order, __reduce_min_sync(0xffffffffu, reached[lane % kScanWarps]));     // logits of a lower order are no candidates
+    const float low = of_order(floor);                 // -infinity: everything above it
+    if (!__any_sync(0xffffffffu, most >= low && most > -INFINITY)) continue;
+    unsigned hits = 0;                                 // of this lane's logits
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) hits |= (v[i] >= low && v[i] > -INFINITY ? 1u : 0u) << i;
+    int n = __popc(hits);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, n, d);
+      if (lane >= d) n += up;
+    }
+    const int all = __shfl_sync(0xffffffffu, n, 31);
+    for (n -= __popc(hits); hits; hits &= hits - 1, ++n) {
+      const int i = __ffs(hits) - 1;
+      float value = v[0];
+#pragma unroll
+      for (int e = 1; e < kLaneValues; ++e) value = i == e ? v[e] : value;
+      found[warp][n] = make_uint2(order_of(value + 0.0f), (uint32_t)token_of(base, i));          // -0 and +0 are one value
+    }
+    __syncwarp();
+    for (int c0 = 0; c0 < all; c0 += 32) {
+      const uint2 mine = c0 + lane < all ? found[warp][c0 + lane] : make_uint2(0u, 0u);
+      auto passes = [&]() { return mine.x > least_order || (mine.x == least_order && mine.y < least_token); };
+      for (unsigned left = __ballot_sync(0xffffffffu, passes() && mine.x > kNone); left;) {
+        const int who = __ffs(left) - 1;
+        const uint32_t o = __shfl_sync(0xffffffffu, mine.x, who), t = __shfl_sync(0xffffffffu, mine.y, who);
+        const int place = __popc(__ballot_sync(0xffffffffu, list_order > o || (list_order == o && list_token < t)));
+        const uint32_t up_order = __shfl_up_sync(0xffffffffu, list_order, 1), up_token = __shfl_up_sync(0xffffffffu, list_token, 1);
+        if (lane > place) { list_order = up_order; list_token = up_token; }
+        if (lane == place) { list_order = o; list_token = t; }
+        least_order = __shfl_sync(0xffffffffu, list_order, p.W - 1);
+        least_token = __shfl_sync(0xffffffffu, list_token, p.W - 1);
+        left &= ~(1u << who) & __ballot_sync(0xffffffffu, passes());
+      }
+    }
+    __syncwarp();
   }
   serving_next();
   if (__any_sync(0xffffffffu, bad) && lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
@@ -222,41 +264,46 @@ beam_pick_kernel(BeamParams p) {
   __shared__ int counts[32], lengths[32];
   serving_begin();
   serving_next();
+  // what a beam that goes on has in the workspace is on its way before it is known whether this one does (it is not used otherwise)
+  uint2* const mine = lists + w * p.chunks * W;
+  const uint2* from = p.best + (size_t)beam * p.chunks * W;
+  for (int i = lane; i < p.chunks * W; i += 32) mine[i] = from[i];
+  const float2 ms = lane < p.chunks ? p.sums[(size_t)beam * p.chunks + lane] : make_float2(-INFINITY, 0.0f);
   int row, n = 0;
   const BeamKind kind = beam_kind(p, beam, &row, false);
   const int length = p.lengths ? p.lengths[beam] : 0;
   const double score = p.scores[beam];
-  const double later = (double)length + (kind == kBeamGoesOn ? 1 : 0);
-  const double divisor = p.power == 0.0f ? 1.0 : pow(fmax(later, 1.0), (double)p.power);
+  const double later = fmax((double)length + (kind == kBeamGoesOn ? 1 : 0), 1.0);
+  const double divisor = p.power == 0.0f ? 1.0 : p.power == 1.0f ? later : pow(later, (double)p.power);
   if (kind == kBeamEnded) {
     n = 1;
     if (lane == 0) { value[w * W] = score; rank[w * W] = score / divisor; token[w * W] = p.end_token; }
   } else if (kind == kBeamGoesOn) {
-    uint2* const mine = lists + w * p.chunks * W;
-    const uint2* from = p.best + (size_t)beam * p.chunks * W;
-    for (int i = lane; i < p.chunks * W; i += 32) mine[i] = from[i];
-    const float2 ms = lane < p.chunks ? p.sums[(size_t)beam * p.chunks + lane] : make_float2(-INFINITY, 0.0f);
     float top = ms.x;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
     double sum = ms.x == -INFINITY ? 0.0 : (double)ms.y * exp2_fast((ms.x - top) * kLog2e);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    const double norm = (double)finite_max(top) + log(sum);
+    // log2 of the sum: its exponent, and the fp32 logarithm of the rest in [1, 2), off by 2^-24 of at most 1
+    const long long bits = __double_as_longlong(sum);
+    const double norm = (double)finite_max(top) + ((double)((int)(bits >> 52) - 1023) +
+                        (double)log2f((float)__longlong_as_double((bits & 0xfffffffffffffll) | 0x3ff0000000000000ll))) / kLog2e;
     __syncwarp();
     int next = 0;
-    uint2 head = lane < p.chunks ? mine[lane * W] : make_uint2(0u, 0u);
+    uint2 head = lane < p.chunks ? mine[lane * W] : make_uint2(0u, 0u), best = make_uint2(0u, 0u);
     for (; n < W; ++n) {
       uint32_t order, low;
       int who;
       if (!best_head(head.x, head.y, &order, &low, &who)) break;
-      if (lane == who) {
-        const double v = score + ((double)of_order(order) - norm);
-        value[w * W + n] = v;
-        rank[w * W + n] = v / divisor;
-        token[w * W + n] = (int)low;
-        head = ++next < W ? mine[lane * W + next] : make_uint2(0u, 0u);
-      }
+      if (lane == n) best = make_uint2(order, low);
+      if (lane == who) head = ++next < W ? mine[lane * W + next] : make_uint2(0u, 0u);
+    }
+    if (lane < n) {
+      const double v = score + ((double)of_order(best.x) - norm);
+      value[w * W + lane] = v;
+      rank[w * W + lane] = v / divisor;
+      token[w * W + lane] = (int)best.y;
     }
   }
   if (lane == 0) { counts[w] = n; lengths[w] = kind == kBeamGoesOn ? length + 1 : length; }
@@ -278,18 +325,18 @@ beam_pick_kernel(BeamParams p) {
   }
   if (lane >= W) return;
   const size_t out = (size_t)blockIdx.x * W + lane;
-  const int from = max(parent, 0) * W + take;
+  const int pick = max(parent, 0) * W + take;
   p.parents[out] = parent < 0 ? -1 : (int)blockIdx.x * W + parent;
-  p.tokens[out] = parent < 0 ? -1 : token[from];
-  p.scores_out[out] = parent < 0 ? -INFINITY : (float)value[from];
+  p.tokens[out] = parent < 0 ? -1 : token[pick];
+  p.scores_out[out] = parent < 0 ? -INFINITY : (float)value[pick];
   if (p.lengths_out) p.lengths_out[out] = parent < 0 ? 0 : lengths[parent];
 }
 
-// How many chunks a row is cut into: enough CTAs to fill the SMs, none with less than a thousand tokens, and no more lists than
-// the second kernel has room and lanes for.
+// How many chunks a row is cut into: enough CTAs to fill the SMs, of at least a thousand tokens; for many rows of about five tiles, so that
+// the last of them end together; no more lists than the second kernel has room and lanes for.
 int beam_chunks(int64_t beams, int W, int V) {
   const int64_t fill = (kSMs * 4 + beams - 1) / beams;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({fill, 32, 256 / W, V / 1024}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({std::max<int64_t>(V / (5 * kTileValues), std::min<int64_t>(fill, V / 1024)), 32, 256 / W}));
 }
 
 size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
@@ -323,7 +370,9 @@ int qzo_beam_select(const float* d_logits, int64_t ldl, int n_rows, const int32_
   const int64_t beams = (int64_t)B * W;
   BeamParams p{d_logits, ldl, n_rows, d_rows, d_scores, d_last_tokens, end_token, d_lengths, length_power, B, W, V, beam_chunks(beams, W, V), 0,
                nullptr, nullptr, d_parents, d_tokens, d_scores_out, d_lengths_out, d_status};
-  p.per = ceil_div(ceil_div(V, p.chunks), 4) * 4;
+  p.per = ceil_div(V, p.chunks);
+  const int step = p.per > kTileValues ? kTileValues : 4;              // whole tiles, so that none is left nearly empty
+  p.per = ceil_div(p.per, step) * step;
   p.chunks = ceil_div(V, p.per);                       // rounding may have left the last one empty
   p.sums = (float2*)d_workspace;
   p.best = (uint2*)((uint8_t*)d_workspace + align_up(beams * p.chunks * sizeof(float2)));
