@@ -198,6 +198,10 @@ qk_norm_rope_cache_kernel(RopeCacheParams p) {
 // Attention of one new token per row
 // =========================================================================================
 
+// How the prefixes of groups are taken: by the rows, through their own tables; by units of few queries; by units of many, in prefix.cu
+enum PrefixPath { kByRule, kOwnTables, kFewPath, kManyPath };
+constexpr int kFewQueries = 32;                        // of a group and key head
+constexpr int64_t kLeastAskedMany = 270000000, kLeastAskedFew = 135000000;       // bytes, see prefix_plan
 constexpr int kStageBytes = 8192;                      // of a warp's ring: 4 KB of keys and 4 KB of values
 constexpr int kSub = 16;                               // keys of one matrix tile; a block of the cache holds whole ones
 
@@ -322,8 +326,11 @@ __host__ __device__ constexpr int ring_stages(int NT) { return NT == 1 ? 2 : 3; 
 // key heads: 44.7 us, 6.3 TB/s; e4m3 1 row of 131071 45.9 us, 5.8 TB/s), by what a CTA needs before its first keys and after
 // its last where they run short (1 row of 4096 keys, 32 key heads: 16.5 us, 4.1 TB/s).  The rings (64 KB a CTA) keep
 // 190 KB in flight or in use on an SM; with the next tile in registers instead, 8 rows of 2048 keys took 51.5 us, now 42.1.
-// GROUPS: rows of a group start behind the prefix that the group's rows share, and leave their part to the join.
-template <int DH, int NT, bool F8, int W, bool GROUPS>
+// What of the keys a launch is for: all that a row sees; what a row of a group has behind the prefix that the group's rows share; that prefix,
+// for up to 8 NT of the group's queries of a key head, which take the place of a row's heads.  The last two leave their results to a join.
+enum class Keys { kAll, kOwn, kPrefix };
+
+template <int DH, int NT, bool F8, int W, Keys KEYS>
 __global__ void __launch_bounds__(W * 32, 4 * resident_ctas(NT) / W)
 paged_attention_kernel(PagedParams p) {
   using Lay = Layout<DH, F8>;
@@ -334,18 +341,28 @@ paged_attention_kernel(PagedParams p) {
   __shared__ int sm_n[W][kStages][Lay::kSubs];         // keys of the tiles in the rings
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int per_row = p.Hkv * p.chunks;
-  const int row = blockIdx.x / per_row, hk = blockIdx.x % per_row / p.chunks, chunk = blockIdx.x % p.chunks;
-  const int head0 = hk * p.G + chunk * 8 * NT;                       // first query head of the CTA
-  const int n_heads = min(8 * NT, p.G - chunk * 8 * NT);
   const int split = blockIdx.y;
   serving_begin();
-  const int shared = GROUPS ? group_prefix(p, row) : 0;
+  PrefixGroup group = {};
+  int unit = 0;
+  if (KEYS == Keys::kPrefix && !find_unit(p, blockIdx.x, blockIdx.x == 0 && split == 0 && warp == 0, &group, &unit)) return;
+  const int row = KEYS == Keys::kPrefix ? 0 : blockIdx.x / per_row, hk = KEYS == Keys::kPrefix ? unit / group.tiles : blockIdx.x % per_row / p.chunks;
+  const int chunk = KEYS == Keys::kPrefix ? unit % group.tiles : blockIdx.x % p.chunks;
+  const int head0 = hk * p.G + chunk * 8 * NT;                       // first query head of the CTA
+  const int n_heads = min(8 * NT, (KEYS == Keys::kPrefix ? group.rows * p.G : p.G) - chunk * 8 * NT);
+  const int shared = KEYS == Keys::kOwn ? group_prefix(p, row) : 0;
   // Query fragments: the same chunks of dimensions as a key's lane t.
   uint32_t qf[NT][Lay::kKeyWords];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const bool have = nt * 8 + g < n_heads;
+    bool have = nt * 8 + g < n_heads;
     const __nv_bfloat16* qr = p.q + (size_t)row * p.ldq + (size_t)(head0 + (have ? nt * 8 + g : 0)) * DH;
+    if (KEYS == Keys::kPrefix) {                       // rows that do not see the whole prefix take it with their own keys
+      const int item = chunk * 8 * NT + (have ? nt * 8 + g : 0), t = group.row0 + item / p.G;
+      int seq;
+      have = have && row_keys(p, t, &seq, false) >= group.prefix;
+      qr = p.q + (size_t)t * p.ldq + (size_t)(hk * p.G + item % p.G) * DH;
+    }
 #pragma unroll
     for (int j = 0; j < Lay::kKeyLoads; ++j)
 #pragma unroll
@@ -356,13 +373,13 @@ paged_attention_kernel(PagedParams p) {
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
       }
   }
-  int seq = 0;
-  const int len = row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
-  const int first = GROUPS && len >= shared ? shared : 0;
-  const int per = split_keys(p, len - first);
+  int seq = group.seq;
+  const int len = KEYS == Keys::kPrefix ? group.prefix : row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
+  const int first = KEYS == Keys::kOwn && len >= shared ? shared : 0;
+  const int per = KEYS == Keys::kPrefix ? prefix_split_keys(p, len) : split_keys(p, len - first);
   const int k0 = first + split * per, k1 = min(len, k0 + per);
   if (k0 >= k1) {
-    if (len == 0 && split == 0)
+    if (KEYS != Keys::kPrefix && len == 0 && split == 0)
       for (int i = threadIdx.x; i < n_heads * DH / 8; i += W * 32)
         *reinterpret_cast<uint4*>(p.out + (size_t)row * p.ldo + (size_t)head0 * DH + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
     return;
@@ -663,7 +680,11 @@ paged_attention_kernel(PagedParams p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) val[e] = fmaf(c, sm_o[w][h][d + e], val[e]);
     }
-    if (len <= per && first == 0) {                    // one split: nothing to join
+    if (KEYS == Keys::kPrefix) {
+      const size_t at = ((size_t)blockIdx.x * p.prefix_splits + split) * p.unit_items + h;
+      *reinterpret_cast<float4*>(p.prefix_o + at * DH + d) = make_float4(val[0], val[1], val[2], val[3]);
+      if (d == 0) *reinterpret_cast<float2*>(p.prefix_ml + 2 * at) = make_float2(mx, sum);
+    } else if (len <= per && first == 0) {             // one split: nothing to join
       const float f = inverse_sum(p, sum);
 #pragma unroll
       for (int e = 0; e < 4; ++e) val[e] *= f;
@@ -761,15 +782,15 @@ Plan attention_plan(int64_t R, int Hkv, int G, int subs, int64_t max_len) {
   const int64_t even = R > 1 ? std::min<int64_t>(max_len / (2048 * subs), 8 * slots / ctas) : 1;
   return {(int)std::max<int64_t>(1, std::max(fill, even)), 0, (even > fill ? 2048 : 128) * subs};
 }
-template <int DH, int NT, bool F8, int W, bool GROUPS>
-int run_attention_w(const PagedParams& p, cudaStream_t st) {
-  const dim3 grid((unsigned)((int64_t)p.R * p.Hkv * p.chunks), p.splits);
+template <int DH, int NT, bool F8, int W, Keys KEYS>
+int run_attention_w(const PagedParams& p, int64_t ctas, int splits, cudaStream_t st) {
+  const dim3 grid((unsigned)ctas, splits);
   constexpr int smem = std::max(W * ring_stages(NT) * kStageBytes, W * 8 * NT * (DH + 1) * (int)sizeof(float));
   {
     static std::atomic<unsigned long long> allowed{0};
-    QZO_CUDA_TRY(allow_dynamic_smem(paged_attention_kernel<DH, NT, F8, W, GROUPS>, smem, allowed));
+    QZO_CUDA_TRY(allow_dynamic_smem(paged_attention_kernel<DH, NT, F8, W, KEYS>, smem, allowed));
   }
-  return launch_serving(paged_attention_kernel<DH, NT, F8, W, GROUPS>, grid, dim3(W * 32), smem, 1, st, p);
+  return launch_serving(paged_attention_kernel<DH, NT, F8, W, KEYS>, grid, dim3(W * 32), smem, 1, st, p);
 }
 
 template <int DH, int COLS, int ROWS>
@@ -778,22 +799,29 @@ int run_join(const PagedParams& p, cudaStream_t st) {
                                      dim3(COLS * ROWS), p.splits * sizeof(float), 1, st, p);
 }
 
-template <int DH, bool F8, bool GROUPS>
+template <int DH, bool F8, Keys KEYS>
 int run_attention(const PagedParams& p, bool wide, cudaStream_t st) {
-  if (p.G <= 8) QZO_TRY(wide ? (run_attention_w<DH, 1, F8, 8, GROUPS>(p, st)) : (run_attention_w<DH, 1, F8, 4, GROUPS>(p, st)));
-  else QZO_TRY(wide ? (run_attention_w<DH, 2, F8, 8, GROUPS>(p, st)) : (run_attention_w<DH, 2, F8, 4, GROUPS>(p, st)));
-  if (GROUPS) return launch_prefix_join(p, DH, st);
+  const int64_t ctas = (int64_t)p.R * p.Hkv * p.chunks;
+  if (p.G <= 8) return wide ? run_attention_w<DH, 1, F8, 8, KEYS>(p, ctas, p.splits, st) : run_attention_w<DH, 1, F8, 4, KEYS>(p, ctas, p.splits, st);
+  return wide ? run_attention_w<DH, 2, F8, 8, KEYS>(p, ctas, p.splits, st) : run_attention_w<DH, 2, F8, 4, KEYS>(p, ctas, p.splits, st);
+}
+template <int DH, bool F8>
+int run_rows(const PagedParams& p, bool wide, cudaStream_t st) {
+  QZO_TRY((run_attention<DH, F8, Keys::kAll>(p, wide, st)));
   if (p.splits <= 1) return QZO_OK;
   // many splits of few heads: a head's dimensions go to several CTAs, so that a thread adds up fewer of them
   return p.splits > 16 ? run_join<DH, 8, 32>(p, st) : run_join<DH, DH / 4, 4>(p, st);
 }
-
-template <bool GROUPS>
-int run_attention_of(const PagedParams& p, const qzo_kv_cache& c, bool wide, cudaStream_t st) {
-  const bool f8 = c.dtype == QZO_DTYPE_E4M3;
-  if (c.head_dim == 128) return f8 ? run_attention<128, true, GROUPS>(p, wide, st) : run_attention<128, false, GROUPS>(p, wide, st);
-  return f8 ? run_attention<64, true, GROUPS>(p, wide, st) : run_attention<64, false, GROUPS>(p, wide, st);
+template <int DH, bool F8>
+int run_groups(const PagedParams& p, const qzo_kv_cache& c, int64_t units, bool wide, cudaStream_t st) {
+  if (!p.prefix_splits) QZO_TRY(launch_prefix_attention(p, c, st));
+  else if (p.unit_items == 8) QZO_TRY((run_attention_w<DH, 1, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
+  else QZO_TRY((run_attention_w<DH, 2, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
+  QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
+  return launch_prefix_join(p, DH, st);
 }
+
+std::atomic<int> forced_path{kByRule};
 
 }  // namespace
 
@@ -834,26 +862,55 @@ size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
   return splits > 1 ? (size_t)R * H * splits * (dh + 2) * sizeof(float) : 0;
 }
 
-// Room for the results of prefixes: parts, queries of a part, and bytes.  0 parts: too many tiles to count in 32 bits.
-struct PrefixRoom {
-  int64_t parts;
-  int rows;
-  size_t bytes;
+// How the prefixes of a call are taken.
+struct PrefixPlan {
+  PrefixPath path;
+  int items, splits, least;                            // queries of a unit; small units: splits, keys of one
+  int64_t units, parts;
+  size_t bytes;                                        // of the parts
 };
-PrefixRoom prefix_room(int R, int n_groups, int G, int Hkv, int dh, int max_len) {
-  const int64_t units = prefix_units(R, n_groups, G, Hkv);
-  if (units * (ceil_div64(max_len, kPrefixTile) + 1) > INT32_MAX) return {0, 0, 0};
-  const int rows = (int)std::min<int64_t>(kPrefixQueries, (int64_t)R * G);
-  return {units + 2 * kSMs, rows, (size_t)(units + 2 * kSMs) * rows * (dh + 2) * sizeof(float)};
+
+PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int64_t max_len) {
+  PrefixPlan plan{kOwnTables, 0, 0, 0, 0, 0, 0};
+  const int subs = 256 / (dh * (f8 ? 1 : 2)), forced = forced_path.load();
+  // With groups of few rows a call without groups reads the shared blocks from L2, so that sharing pays only where that is a lot: at 270 MB of
+  // keys and values asked for the two took equally long, whatever the rows, heads and lengths (tensor-core units; 4 to 64 rows over 8 and
+  // 32 key heads, bf16 and e4m3).  All of this goes by the table's width, as lengths are known on the device only.
+  const int64_t asked = (int64_t)R * Hkv * max_len * dh * (f8 ? 2 : 4), queries = (int64_t)R * G / std::max(1, std::min(R, n_groups));
+  plan.path = forced != kByRule ? (PrefixPath)forced : asked < (queries <= kFewQueries ? kLeastAskedFew : kLeastAskedMany) ? kOwnTables
+              : queries <= kFewQueries ? kFewPath : kManyPath;
+  if (plan.path == kOwnTables) return plan;
+  plan.items = plan.path == kManyPath ? kPrefixQueries : queries <= 8 ? 8 : 16;
+  plan.units = prefix_units(R, n_groups, G, Hkv, plan.items);
+  if (plan.path == kManyPath) {
+    plan.parts = plan.units + 2 * kSMs;
+    if (plan.units * (max_len / kPrefixTile + 2) > INT32_MAX) plan.path = kOwnTables;          // places of the line are counted in 32 bits
+  } else {
+    // as attention_plan
+    const int64_t slots = kSMs * resident_ctas(plan.items / 8);
+    const int64_t fill = std::min<int64_t>(slots / plan.units, max_len / (128 * subs)), even = std::min<int64_t>(max_len / (2048 * subs), 8 * slots / plan.units);
+    plan.splits = (int)std::max<int64_t>(1, std::max(fill, even));
+    plan.least = (even > fill ? 2048 : 128) * subs;
+    plan.parts = plan.units * plan.splits;
+    if (plan.units > INT32_MAX) plan.path = kOwnTables;
+  }
+  plan.bytes = (size_t)plan.parts * plan.items * (dh + 2) * sizeof(float);
+  return plan;
 }
 
 // Splits of rows whose prefix is taken elsewhere: what the table has room for is mostly prefix, so long rows are not cut into as many
 // pieces (most of those CTAs would find nothing: 128 rows with 16384 of 16500 tokens in common, 6 splits 20 us, 2 splits 9 us).
 int own_splits(const Plan& plan) { return std::min(plan.splits, 2); }
 
+// For either type of cache
 size_t shared_prefix_bytes(int R, int n_groups, int H, int Hkv, int dh, int max_len) {
-  const int splits = own_splits(attention_plan(R, Hkv, H / Hkv, 128 / dh, max_len));
-  return (size_t)R * H * splits * (dh + 2) * sizeof(float) + prefix_room(R, n_groups, H / Hkv, Hkv, dh, max_len).bytes;
+  size_t most = paged_attention_bytes(R, H, Hkv, dh, max_len);
+  for (bool f8 : {false, true}) {
+    const PrefixPlan plan = prefix_plan(R, n_groups, H / Hkv, Hkv, dh, f8, max_len);
+    const int splits = own_splits(attention_plan(R, Hkv, H / Hkv, 256 / (dh * (f8 ? 1 : 2)), max_len));
+    if (plan.path != kOwnTables) most = std::max(most, plan.bytes + (size_t)R * H * splits * (dh + 2) * sizeof(float));
+  }
+  return most;
 }
 
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
@@ -864,40 +921,50 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
   if ((int64_t)R * c.n_kv_heads * chunks > INT32_MAX) return QZO_ERR_BAD_ARG;
   const int subs = 256 / (c.head_dim * (c.dtype == QZO_DTYPE_E4M3 ? 1 : 2));
   const Plan plan = attention_plan(R, c.n_kv_heads, G, subs, max_len);
-  int splits = groups ? own_splits(plan) : plan.splits;
+  const bool f8 = c.dtype == QZO_DTYPE_E4M3;
   const size_t per_split = (size_t)R * H * (c.head_dim + 2) * sizeof(float);
+  PagedParams p{};
+  p.q = q; p.ldq = ldq; p.ck = c.k; p.cv = c.v; p.table = table; p.n_seqs = n_seqs; p.width = width;
+  p.row_seq = row_seq; p.positions = positions; p.slots = slots;
+  p.scale_log2e = scale * kLog2e * c.k_scale; p.v_scale = c.v_scale;
+  p.out = out; p.ldo = ldo; p.R = R; p.H = H; p.Hkv = c.n_kv_heads; p.G = G; p.chunks = chunks;
+  p.min_keys = plan.min_keys; p.round_keys = 64 * subs; p.n_blocks = c.n_blocks; p.log2_block = log2_of(c.block_size);
+  p.status = status;
   if (groups) {
-    const PrefixRoom room = prefix_room(R, groups->n, G, c.n_kv_heads, c.head_dim, max_len);
-    // rows that a tensor map can name
-    if ((int64_t)c.n_blocks * c.block_size * c.n_kv_heads > INT32_MAX) return QZO_ERR_BAD_ARG;
-    if (!fewer_splits && (!ws || ws_bytes < shared_prefix_bytes(R, groups->n, H, c.n_kv_heads, c.head_dim, max_len) || ((uintptr_t)ws & 255))) return QZO_ERR_WORKSPACE;
-    if (fewer_splits && ws_bytes >= room.bytes + per_split) splits = (int)std::min<size_t>(splits, (ws_bytes - room.bytes) / per_split);
-    if (room.parts > 0 && ws_bytes >= room.bytes + splits * per_split) {
-      PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, slots, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
-                    R, H, c.n_kv_heads, G, chunks, splits, plan.min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status,
-                    *groups, 2 * kSMs, room.rows, nullptr, nullptr};
+    if ((int64_t)c.n_blocks * c.block_size * c.n_kv_heads > INT32_MAX) return QZO_ERR_BAD_ARG;               // rows that a tensor map can name
+    if (!fewer_splits)
+      if (const size_t need = shared_prefix_bytes(R, groups->n, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
+        if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
+    const PrefixPlan prefix = prefix_plan(R, groups->n, G, c.n_kv_heads, c.head_dim, f8, max_len);
+    int splits = own_splits(plan);
+    if (fewer_splits && ws_bytes >= prefix.bytes + per_split) splits = (int)std::min<size_t>(splits, (ws_bytes - prefix.bytes) / per_split);
+    if (prefix.path != kOwnTables && ws_bytes >= prefix.bytes + splits * per_split) {
+      p.groups = *groups;
+      p.unit_items = prefix.items;
+      p.prefix_ctas = 2 * kSMs;
+      p.prefix_splits = prefix.splits;
+      p.prefix_least = prefix.least;
+      p.splits = splits;
       p.prefix_o = (float*)ws;
-      p.part_o = p.prefix_o + (size_t)room.parts * room.rows * c.head_dim;
+      p.part_o = p.prefix_o + (size_t)prefix.parts * prefix.items * c.head_dim;
       p.prefix_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
-      p.part_ml = p.prefix_ml + 2 * (size_t)room.parts * room.rows;
-      QZO_TRY(launch_prefix_attention(p, c, st));
-      return run_attention_of<true>(p, c, plan.wide, st);
+      p.part_ml = p.prefix_ml + 2 * (size_t)prefix.parts * prefix.items;
+      if (c.head_dim == 128) return f8 ? run_groups<128, true>(p, c, prefix.units, plan.wide, st) : run_groups<128, false>(p, c, prefix.units, plan.wide, st);
+      return f8 ? run_groups<64, true>(p, c, prefix.units, plan.wide, st) : run_groups<64, false>(p, c, prefix.units, plan.wide, st);
     }
-    // no room for what prefixes leave: every row reads its own table
+    // every row reads all of its keys through its own table
   }
-  splits = plan.splits;
+  p.splits = plan.splits;
   if (fewer_splits)
-    splits = (int)std::max<size_t>(1, std::min<size_t>(splits, ws_bytes / per_split));
+    p.splits = (int)std::max<size_t>(1, std::min<size_t>(p.splits, ws_bytes / per_split));
   else if (const size_t need = paged_attention_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
     if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
-  PagedParams p{q, ldq, c.k, c.v, table, n_seqs, width, row_seq, positions, slots, scale * kLog2e * c.k_scale, c.v_scale, out, ldo,
-                R, H, c.n_kv_heads, G, chunks, splits, plan.min_keys, 64 * subs, c.n_blocks, log2_of(c.block_size), nullptr, nullptr, status,
-                {nullptr, nullptr, nullptr, 0}, 0, 0, nullptr, nullptr};
-  if (splits > 1) {
+  if (p.splits > 1) {
     p.part_o = (float*)ws;
-    p.part_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
+    p.part_ml = p.part_o + (size_t)R * H * p.splits * c.head_dim;
   }
-  return run_attention_of<false>(p, c, plan.wide, st);
+  if (c.head_dim == 128) return f8 ? run_rows<128, true>(p, plan.wide, st) : run_rows<128, false>(p, plan.wide, st);
+  return f8 ? run_rows<64, true>(p, plan.wide, st) : run_rows<64, false>(p, plan.wide, st);
 }
 
 }  // namespace qzo
@@ -961,6 +1028,12 @@ int qzo_paged_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache
   return launch_paged_attention((const __nv_bfloat16*)d_q_bf16, ldq, *cache, d_block_table, n_seqs, table_width, d_row_seq, d_positions,
                                 nullptr, scale, (__nv_bfloat16*)d_out_bf16, ldo, R, n_heads, d_workspace, workspace_bytes, false,
                                 d_status, (cudaStream_t)stream);
+}
+
+int qzo_debug_prefix_path(int path) {
+  if (path < kByRule || path > kManyPath) return QZO_ERR_BAD_ARG;
+  forced_path.store(path);
+  return QZO_OK;
 }
 
 int qzo_shared_prefix_attention_workspace_bytes(int R, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes) {

@@ -27,8 +27,10 @@ struct PagedParams {
   float *part_o, *part_ml;                             // [R][H][splits][DH], [R][H][splits][2]
   int* status;
   PrefixGroups groups;                                 // of the rows that share the beginning of their cache; none: n = 0
-  int prefix_ctas, prefix_rows;                        // CTAs of the prefix kernel; queries that a part of its results has room for
-  float *prefix_o, *prefix_ml;                         // [parts][prefix_rows][DH], [parts][prefix_rows][2]
+  int unit_items;                                      // queries of a unit of work on prefixes
+  int prefix_ctas;                                     // units of 128: CTAs of the kernel on the tensor cores' line
+  int prefix_splits, prefix_least;                     // smaller units: splits of each (0 where units have 128), keys of one, at least
+  float *prefix_o, *prefix_ml;                         // results: [parts][unit_items][DH], [parts][unit_items][2]
 };
 
 // Keys of split s of a row that sees len keys: [s * per, min(len, (s + 1) * per)), per at least the launch's minimum.
@@ -62,10 +64,12 @@ __device__ __forceinline__ float upper_half(uint32_t bits) { return __uint_as_fl
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
 
 // ----------------------------------------------------------------------------- shared beginnings
-// The work on prefixes: a unit is 128 queries (the rows of a group times the query heads of a key head, in that order) over
-// the whole prefix of their group, tiles of 64 keys and one place more for what a change of units costs.  All units, group by group,
-// key head by key head, stand in one line, of which every CTA takes an equal stretch.  What a CTA finds of unit u is part (CTA + u) of
-// the results: from one stretch or unit to the next, one of the two grows.
+// The work on prefixes: a unit is some queries (the rows of a group times the query heads of a key head, in that order) over the
+// whole prefix of their group; units are numbered group by group, key head by key head.
+// Many queries to a group: units of 128 for the tensor cores' larger instructions (prefix.cu), in tiles of 64 keys and one place more for
+// what a change of units costs.  All units stand in one line, of which every CTA takes an equal stretch.  What a CTA finds of unit u is
+// part (CTA + u) of the results: from one stretch or unit to the next, one of the two grows.
+// Few: units of 8 or 16, which are to paged_attention_kernel what the heads of a row are; split s of unit u is part (u * splits + s).
 constexpr int kPrefixQueries = 128, kPrefixTile = 64;
 constexpr int kPrefixStep = 16;                        // tokens that a prefix counts in: what the rows' own kernel starts at
 constexpr int kPrefixLeast = 4;                        // places of a CTA's stretch, at least
@@ -82,8 +86,46 @@ __device__ __forceinline__ PrefixGroup prefix_group(const PagedParams& p, int i,
   const bool bad = len < 0 || len > (p.width << p.log2_block) || (unsigned)seq >= (unsigned)p.n_seqs;
   if (bad && report && p.status) atomicOr(p.status, kStatusBadToken);
   const int prefix = bad ? 0 : len / kPrefixStep * kPrefixStep;
-  return {row0, rows, prefix, seq, (rows * p.G + kPrefixQueries - 1) / kPrefixQueries, rows > 0 ? (prefix + kPrefixTile - 1) / kPrefixTile : 0};
+  return {row0, rows, prefix, seq, (rows * p.G + p.unit_items - 1) / p.unit_items, rows > 0 ? (prefix + kPrefixTile - 1) / kPrefixTile : 0};
 }
+// Keys of a split of a small unit
+__device__ __forceinline__ int prefix_split_keys(const PagedParams& p, int prefix) {
+  return max(p.prefix_least, ((prefix + p.prefix_splits - 1) / p.prefix_splits + p.round_keys - 1) / p.round_keys * p.round_keys);
+}
+// The unit of this number: its group, and its number within it; false where there is none, or where the groups' bounds do not ascend within the
+// rows (which is reported).  Whole warps.
+__device__ __forceinline__ bool find_unit(const PagedParams& p, int number, bool report, PrefixGroup* group, int* unit) {
+  const int lane = threadIdx.x & 31;
+  int before = 0;
+  bool bad = false, found = false;
+  for (int i0 = 0; i0 < p.groups.n; i0 += 32) {
+    PrefixGroup g = {};
+    if (i0 + lane < p.groups.n) {
+      g = prefix_group(p, i0 + lane, report);
+      bad = bad || g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R;
+    }
+    const int units = g.units(p.Hkv);
+    int sum = units;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, sum, d);
+      if (lane >= d) sum += up;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, before + sum > number);
+    if (!found && past) {
+      found = true;
+      const int who = __ffs(past) - 1;
+      *group = {__shfl_sync(0xffffffffu, g.row0, who), __shfl_sync(0xffffffffu, g.rows, who), __shfl_sync(0xffffffffu, g.prefix, who),
+                __shfl_sync(0xffffffffu, g.seq, who), __shfl_sync(0xffffffffu, g.tiles, who), __shfl_sync(0xffffffffu, g.key_tiles, who)};
+      *unit = number - before - __shfl_sync(0xffffffffu, sum - units, who);
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  bad = __any_sync(0xffffffffu, bad);
+  if (bad && report && lane == 0 && p.status) atomicOr(p.status, kStatusBadToken);
+  return found && !bad;
+}
+
 // Places of a CTA's stretch, of `places` in all
 __device__ __forceinline__ int prefix_stretch(const PagedParams& p, int places) { return max(kPrefixLeast, (places + p.prefix_ctas - 1) / p.prefix_ctas); }
 
@@ -103,6 +145,6 @@ __device__ __forceinline__ int group_prefix(const PagedParams& p, int row) {
 // prefix.cu: the results of every group's prefix, for the rows that see all of it, and their join with those of the rows' own keys
 int launch_prefix_attention(const PagedParams& p, const qzo_kv_cache& c, cudaStream_t st);
 int launch_prefix_join(const PagedParams& p, int dh, cudaStream_t st);
-int64_t prefix_units(int R, int n_groups, int G, int Hkv);      // at most
+int64_t prefix_units(int R, int n_groups, int G, int Hkv, int items);      // at most
 
 }  // namespace qzo

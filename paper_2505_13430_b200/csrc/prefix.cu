@@ -488,7 +488,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       }
       // the unit's sums leave tensor memory
       wait(bar_values, j - 1);
-      const size_t part = (size_t)(blockIdx.x + number) * p.prefix_rows + mine;
+      const size_t part = (size_t)(blockIdx.x + number) * p.unit_items + mine;
       if (active) {
 #pragma unroll 1
         for (int c = 0; c < DH; c += 32) {
@@ -610,12 +610,18 @@ prefix_join_kernel(PagedParams p) {
       const PrefixGroup g = prefix_group(p, group);
       if (g.key_tiles && len >= g.prefix) {
         prefix = g.prefix;
-        const int in_unit = (row - g.row0) * p.G + head % p.G, unit = head / p.G * g.tiles + in_unit / kPrefixQueries;
-        const int stretch = prefix_stretch(p, places), t0 = places_before + unit * g.places();
-        const int c0 = t0 / stretch, c1 = (t0 + g.key_tiles - 1) / stretch;
-        n_first = c1 - c0 + 1;
-        first_part = (size_t)(c0 + units_before + unit) * p.prefix_rows + in_unit % kPrefixQueries;
-        part_step = p.prefix_rows;
+        const int in_unit = (row - g.row0) * p.G + head % p.G, unit = head / p.G * g.tiles + in_unit / p.unit_items;
+        part_step = p.unit_items;
+        if (p.prefix_splits) {
+          const int per = prefix_split_keys(p, prefix);
+          n_first = (prefix + per - 1) / per;
+          first_part = (size_t)(units_before + unit) * p.prefix_splits * p.unit_items + in_unit % p.unit_items;
+        } else {
+          const int stretch = prefix_stretch(p, places), t0 = places_before + unit * g.places();
+          const int c0 = t0 / stretch, c1 = (t0 + g.key_tiles - 1) / stretch;
+          n_first = c1 - c0 + 1;
+          first_part = (size_t)(c0 + units_before + unit) * p.unit_items + in_unit % p.unit_items;
+        }
       }
     }
   }
@@ -718,9 +724,9 @@ int run_prefix_join(const PagedParams& p, cudaStream_t st) {
 }  // namespace
 
 // Every group may leave one unfinished tile of queries.
-int64_t prefix_units(int R, int n_groups, int G, int Hkv) {
+int64_t prefix_units(int R, int n_groups, int G, int Hkv, int items) {
   const int64_t k = std::min(R, n_groups);
-  return (k + ((int64_t)R * G - k) / kM) * Hkv;
+  return (k + ((int64_t)R * G - k) / items) * Hkv;
 }
 
 int launch_prefix_attention(const PagedParams& p, const qzo_kv_cache& c, cudaStream_t st) {

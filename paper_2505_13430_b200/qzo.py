@@ -32,7 +32,7 @@ EXPORTS = (
     "qzo_gemv_int4", "qzo_rope_table", "qzo_qk_norm_rope_cache", "qzo_paged_attention_workspace_bytes", "qzo_paged_attention",
     "qzo_assign_slots", "qzo_decode", "qzo_decode_requests",
     "qzo_beam_select_workspace_bytes", "qzo_beam_select", "qzo_fork_requests", "qzo_compact_blocks", "qzo_copy_blocks",
-    "qzo_shared_prefix_attention_workspace_bytes", "qzo_shared_prefix_attention",
+    "qzo_shared_prefix_attention_workspace_bytes", "qzo_shared_prefix_attention", "qzo_debug_prefix_path",
 )
 
 
@@ -123,6 +123,7 @@ def _load():
         "qzo_fork_requests": (ci, [vp, vp, ci, vp, ci, ci, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp, vp]),
         "qzo_compact_blocks": (ci, [vp, ci, vp, ci, ci, ci, ci, vp, vp, ci, vp, vp, ci, vp, vp, vp]),
         "qzo_shared_prefix_attention_workspace_bytes": (ci, [ci, ci, ci, ci, ci, ci, P(sz)]),
+        "qzo_debug_prefix_path": (ci, [ci]),
         "qzo_shared_prefix_attention": (ci, [vp, ci, P(KvCacheDesc), vp, ci, ci, vp, vp, vp, vp, vp, ci, cf, vp, ci, ci, ci, vp, sz, vp, vp]),
         "qzo_copy_blocks": (ci, [P(KvCacheDesc), ci, vp, vp, ci, vp, vp]),
         "qzo_profile_gemms": (ci, [vp, ci]),
@@ -504,6 +505,11 @@ def qzo_shared_prefix_attention_workspace_bytes(R, n_groups, n_heads, n_kv_heads
     return out.value
 
 
+def qzo_debug_prefix_path(path):
+    """For tests: 0 = as measured best, 1 = own tables, 2 = units of few queries, 3 = units of 128; see include/qzo.h."""
+    _check(_lib.qzo_debug_prefix_path(path), "qzo_debug_prefix_path")
+
+
 def qzo_shared_prefix_attention(q, cache, block_table, positions, group_rows, prefix_seq, prefix_len, row_seq=None, scale=None, out=None,
                                 workspace=None, status=None):
     """qzo_paged_attention for groups of rows that share the beginning of their cache (int32): rows group_rows[i] .. group_rows[i + 1] - 1
@@ -529,12 +535,15 @@ def qzo_shared_prefix_attention(q, cache, block_table, positions, group_rows, pr
         _ints(dev, R, row_seq)
         seqs = row_seq.data_ptr()
     if workspace is None:
-        workspace = q.new_empty(qzo_shared_prefix_attention_workspace_bytes(R, n, H, cache.n_kv_heads, dh, width * cache.block_size), dtype=_U8)
-    assert workspace.is_contiguous() and workspace.get_device() == dev, "workspace: contiguous, on the current device"
+        need = qzo_shared_prefix_attention_workspace_bytes(R, n, H, cache.n_kv_heads, dh, width * cache.block_size)
+        workspace = q.new_empty(need, dtype=_U8) if need else None
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        assert workspace.is_contiguous() and (workspace.get_device() == dev or workspace.numel() == 0), "workspace: contiguous, on the current device"
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     rc = _lib.qzo_shared_prefix_attention(q.data_ptr(), ldq, cache._ref, block_table.data_ptr(), n_seqs, width, seqs, positions.data_ptr(),
                                           group_rows.data_ptr(), prefix_seq.data_ptr(), prefix_len.data_ptr(), n, dh ** -0.5 if scale is None else scale,
-                                          out.data_ptr(), ldo, R, H, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                          None if status is None else _status(dev, status), _raw_stream(dev))
+                                          out.data_ptr(), ldo, R, H, ws, ws_bytes, None if status is None else _status(dev, status), _raw_stream(dev))
     if rc:
         _check(rc, "qzo_shared_prefix_attention")
     return out

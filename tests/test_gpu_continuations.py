@@ -298,6 +298,21 @@ def test_copies_beyond_32_bit_offsets(lib):
 
 # ------------------------------------------------------------------ attention over shared beginnings
 
+# how prefixes are taken: by the rows through their own tables, in units of few queries, in units of 128
+@pytest.fixture(params=[1, 2, 3], ids=["own-tables", "few", "many"])
+def path(request, lib):
+    lib.qzo_debug_prefix_path(request.param)
+    yield request.param
+    lib.qzo_debug_prefix_path(0)
+
+
+@pytest.fixture(params=[2, 3], ids=["few", "many"])
+def units(request, lib):
+    lib.qzo_debug_prefix_path(request.param)
+    yield request.param
+    lib.qzo_debug_prefix_path(0)
+
+
 CACHES = {"bf16": (torch.bfloat16, 1.0, 1.0), "e4m3": (torch.float8_e4m3fn, 0.25, 0.5)}
 
 
@@ -401,7 +416,7 @@ SHARED_CASES = [
 
 
 @pytest.mark.parametrize("groups,H,Hkv,dh,block,kind,loose", SHARED_CASES)
-def test_shared_prefix_attention_matches_oracle(lib, groups, H, Hkv, dh, block, kind, loose):
+def test_shared_prefix_attention_matches_oracle(lib, path, groups, H, Hkv, dh, block, kind, loose):
     case = Shared(groups, H, Hkv, dh, block, kind, 300 + H + dh, loose=loose)
     out = case.run(lib)
     case.check(out)
@@ -410,7 +425,7 @@ def test_shared_prefix_attention_matches_oracle(lib, groups, H, Hkv, dh, block, 
 
 @pytest.mark.parametrize("kind,dh", [("bf16", 64), ("bf16", 128), ("e4m3", 64), ("e4m3", 128)])
 @pytest.mark.parametrize("rising", [False, True])
-def test_long_runs_of_tiles(lib, kind, dh, rising):
+def test_long_runs_of_tiles(lib, units, kind, dh, rising):
     # so many groups that a prefix is not split: dozens of tiles one after the other, two CTAs on an SM.  Rising: scores that pass the
     # running maximum again and again, so that the sums are rescaled between products; some rows fall instead
     case = Shared([(2, 450 + 13 * i, 1 + 3 * i) for i in range(40)], 8, 8, dh, 32, kind, 900 + dh)
@@ -426,7 +441,7 @@ def test_long_runs_of_tiles(lib, kind, dh, rising):
         assert torch.equal(out.view(torch.int16), case.run(lib).view(torch.int16))
 
 
-def test_peaked_scores_over_a_shared_prefix(lib):
+def test_peaked_scores_over_a_shared_prefix(lib, units):
     case = Shared([(5, 1500, 100), (4, 300, 3)], 8, 2, 128, 16, "bf16", 31, q_std=12.0)
     case.check(case.run(lib))
     case.scale = 0.7
@@ -434,7 +449,7 @@ def test_peaked_scores_over_a_shared_prefix(lib):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
-def test_leading_keys_of_no_value_in_a_prefix(lib, kind):
+def test_leading_keys_of_no_value_in_a_prefix(lib, units, kind):
     # keys that lead and whose values are zero leave the row to the others, whose weights are 2^-10 to 2^-40 of theirs
     case = Shared([(4, 900, 60)], 8, 2, 64, 16, kind, 32)
     case.ck[..., 0] = 0.0
@@ -447,7 +462,7 @@ def test_leading_keys_of_no_value_in_a_prefix(lib, kind):
     case.check(case.run(lib))
 
 
-def test_infinite_values_and_scores_in_a_prefix(lib):
+def test_infinite_values_and_scores_in_a_prefix(lib, units):
     case = Shared([(3, 500, [1, 64, 300])], 4, 2, 64, 16, "bf16", 33)
     for j, dim, v in ((0, 3, "inf"), (200, 17, "-inf"), (447, 63, "inf"), (0, 40, "inf"), (300, 40, "-inf"), (100, 5, "nan")):
         case.cv[int(case.table[0, j // 16]), :, j % 16, dim] = float(v)
@@ -467,7 +482,7 @@ def test_infinite_values_and_scores_in_a_prefix(lib):
     case.check(out, only=[0, 1])
 
 
-def test_what_is_out_of_range_in_groups_is_reported(lib):
+def test_what_is_out_of_range_in_groups_is_reported(lib, units):
     groups = [(3, 500, [1, 64, 300]), (2, 200, 30), (2, 300, 5)]
     case = Shared(groups, 8, 2, 64, 16, "bf16", 35)
     plain = case.run(lib)
@@ -498,7 +513,7 @@ def test_what_is_out_of_range_in_groups_is_reported(lib):
                 assert np.abs(f64(out[t, h]) - want).max() <= BF16_STEP * np.abs(want).max() + 1e-3
 
 
-def test_several_rows_of_a_request_and_strided_rows(lib):
+def test_several_rows_of_a_request_and_strided_rows(lib, units):
     # the options of a question: every request has several new rows, which see the shared prefix and their own tokens up to themselves
     case = Shared([(4, 333, [40, 41, 42, 43])], 8, 4, 128, 16, "bf16", 36)
     take = [(t, p) for t in range(4) for p in range(330 + 20 * t, case.lens[t], 3)]
@@ -515,7 +530,7 @@ def test_several_rows_of_a_request_and_strided_rows(lib):
     case.check(out[:, :8])
 
 
-def test_a_prefix_of_a_cache_beyond_32_bit_offsets(lib):
+def test_a_prefix_of_a_cache_beyond_32_bit_offsets(lib, units):
     Hkv, block, dh = 8, 64, 128
     n_blocks = (1 << 32) // (Hkv * block * dh * 2) + 6            # 4 GB and a little of keys, as many of values
     small = Shared([(3, 640, [5, 70, 1])], 16, Hkv, dh, block, "bf16", 37)
