@@ -327,7 +327,7 @@ __host__ __device__ constexpr int ring_stages(int NT) { return NT == 1 ? 2 : 3; 
 // its last where they run short (1 row of 4096 keys, 32 key heads: 16.5 us, 4.1 TB/s).  The rings (64 KB a CTA) keep
 // 190 KB in flight or in use on an SM; with the next tile in registers instead, 8 rows of 2048 keys took 51.5 us, now 42.1.
 // What of the keys a launch is for: all that a row sees; what a row of a group has behind the prefix that the group's rows share; that prefix,
-// for up to 8 NT of the group's queries of a key head, which take the place of a row's heads.  The last two leave their results to a join.
+// for up to 8 NT of the group's queries of a key head, which take the place of a row's heads, and whose results the second joins (a kernel of its own does where own keys are split).
 enum class Keys { kAll, kOwn, kPrefix };
 
 template <int DH, int NT, bool F8, int W, Keys KEYS>
@@ -350,7 +350,8 @@ paged_attention_kernel(PagedParams p) {
   const int chunk = KEYS == Keys::kPrefix ? unit % group.tiles : blockIdx.x % p.chunks;
   const int head0 = hk * p.G + chunk * 8 * NT;                       // first query head of the CTA
   const int n_heads = min(8 * NT, (KEYS == Keys::kPrefix ? group.rows * p.G : p.G) - chunk * 8 * NT);
-  const int shared = KEYS == Keys::kOwn ? group_prefix(p, row) : 0;
+  RowPrefix shared = {};
+  if (KEYS == Keys::kOwn) shared = row_prefix(p, row);
   // Query fragments: the same chunks of dimensions as a key's lane t.
   uint32_t qf[NT][Lay::kKeyWords];
 #pragma unroll
@@ -375,10 +376,11 @@ paged_attention_kernel(PagedParams p) {
   }
   int seq = group.seq;
   const int len = KEYS == Keys::kPrefix ? group.prefix : row_keys(p, row, &seq, threadIdx.x == 0 && split == 0 && blockIdx.x % per_row == 0);
-  const int first = KEYS == Keys::kOwn && len >= shared ? shared : 0;
+  const int first = KEYS == Keys::kOwn && len >= shared.prefix ? shared.prefix : 0;
   const int per = KEYS == Keys::kPrefix ? prefix_split_keys(p, len) : split_keys(p, len - first);
   const int k0 = first + split * per, k1 = min(len, k0 + per);
-  if (k0 >= k1) {
+  const bool joins = KEYS == Keys::kOwn && first > 0 && p.splits == 1;         // this CTA joins what the prefix left with what it finds
+  if (k0 >= k1 && !joins) {
     if (KEYS != Keys::kPrefix && len == 0 && split == 0)
       for (int i = threadIdx.x; i < n_heads * DH / 8; i += W * 32)
         *reinterpret_cast<uint4*>(p.out + (size_t)row * p.ldo + (size_t)head0 * DH + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
@@ -684,6 +686,43 @@ paged_attention_kernel(PagedParams p) {
       const size_t at = ((size_t)blockIdx.x * p.prefix_splits + split) * p.unit_items + h;
       *reinterpret_cast<float4*>(p.prefix_o + at * DH + d) = make_float4(val[0], val[1], val[2], val[3]);
       if (d == 0) *reinterpret_cast<float2*>(p.prefix_ml + 2 * at) = make_float2(mx, sum);
+    } else if (joins) {
+      size_t part;
+      int step;
+      const int n = shared.parts(p, hk, (row - shared.row0) * p.G + chunk * 8 * NT + h, &part, &step);
+      constexpr int kAhead = 4;                        // parts whose loads are in flight
+      for (int s0 = 0; s0 < n; s0 += kAhead) {
+        float2 ml[kAhead];
+        float4 x[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          ml[e] = make_float2(-INFINITY, 0.0f);
+          x[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (s0 + e >= n) continue;
+          const size_t at = part + (size_t)(s0 + e) * step;
+          ml[e] = *reinterpret_cast<const float2*>(p.prefix_ml + 2 * at);
+          x[e] = *reinterpret_cast<const float4*>(p.prefix_o + at * DH + d);
+        }
+        float top = mx;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) top = fmaxf(top, ml[e].x);
+        const float to = finite_max(top), by = fast_exp2(mx - to);
+        sum *= by;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) val[e] *= by;
+        mx = top;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const float w = fast_exp2(ml[e].x - to);
+          sum = fmaf(w, ml[e].y, sum);
+          val[0] = fmaf(w, x[e].x, val[0]); val[1] = fmaf(w, x[e].y, val[1]);
+          val[2] = fmaf(w, x[e].z, val[2]); val[3] = fmaf(w, x[e].w, val[3]);
+        }
+      }
+      const float f = inverse_sum(p, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) val[e] *= f;
+      *reinterpret_cast<uint2*>(p.out + (size_t)row * p.ldo + (size_t)(head0 + h) * DH + d) = pack4_bf16(val);
     } else if (len <= per && first == 0) {             // one split: nothing to join
       const float f = inverse_sum(p, sum);
 #pragma unroll
@@ -817,8 +856,13 @@ int run_groups(const PagedParams& p, const qzo_kv_cache& c, int64_t units, bool 
   if (!p.prefix_splits) QZO_TRY(launch_prefix_attention(p, c, st));
   else if (p.unit_items == 8) QZO_TRY((run_attention_w<DH, 1, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
   else QZO_TRY((run_attention_w<DH, 2, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
-  QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
-  return launch_prefix_join(p, DH, st);
+  // Own keys are few as a rule: CTAs of one warp, twelve on an SM, where there are enough rows and key heads (64 rows on 16 prefixes, 32 key
+  // heads, 1 to 64 own keys: 72.0 us in all, 78.7 with four warps; 1 to 400 own keys: 124.6 and 120.0).
+  const int64_t ctas = (int64_t)p.R * p.Hkv * p.chunks;
+  if (ctas < 3 * kSMs) QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
+  else if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 1, Keys::kOwn>(p, ctas, p.splits, st)));
+  else QZO_TRY((run_attention_w<DH, 2, F8, 1, Keys::kOwn>(p, ctas, p.splits, st)));
+  return p.splits > 1 ? launch_prefix_join(p, DH, st) : QZO_OK;
 }
 
 std::atomic<int> forced_path{kByRule};
@@ -898,16 +942,17 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
   return plan;
 }
 
-// Splits of rows whose prefix is taken elsewhere: what the table has room for is mostly prefix, so long rows are not cut into as many
-// pieces (most of those CTAs would find nothing: 128 rows with 16384 of 16500 tokens in common, 6 splits 20 us, 2 splits 9 us).
-int own_splits(const Plan& plan) { return std::min(plan.splits, 2); }
+// Splits of rows whose prefix is taken elsewhere: what the table has room for is mostly prefix, so they have few keys of their own, and with
+// one split they join the prefix's results themselves (128 rows with 16384 of 16500 tokens in common, splits and a join: 20 + 11 us of
+// 6 and 14 + 12 us of 2; 9 us of one).
+int own_splits(const Plan& plan, int64_t ctas) { return ctas >= kSMs ? 1 : std::min(plan.splits, 4); }
 
 // For either type of cache
 size_t shared_prefix_bytes(int R, int n_groups, int H, int Hkv, int dh, int max_len) {
   size_t most = paged_attention_bytes(R, H, Hkv, dh, max_len);
   for (bool f8 : {false, true}) {
     const PrefixPlan plan = prefix_plan(R, n_groups, H / Hkv, Hkv, dh, f8, max_len);
-    const int splits = own_splits(attention_plan(R, Hkv, H / Hkv, 256 / (dh * (f8 ? 1 : 2)), max_len));
+    const int splits = own_splits(attention_plan(R, Hkv, H / Hkv, 256 / (dh * (f8 ? 1 : 2)), max_len), (int64_t)R * Hkv * head_chunks(H / Hkv));
     if (plan.path != kOwnTables) most = std::max(most, plan.bytes + (size_t)R * H * splits * (dh + 2) * sizeof(float));
   }
   return most;
@@ -936,7 +981,7 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
       if (const size_t need = shared_prefix_bytes(R, groups->n, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
         if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
     const PrefixPlan prefix = prefix_plan(R, groups->n, G, c.n_kv_heads, c.head_dim, f8, max_len);
-    int splits = own_splits(plan);
+    int splits = own_splits(plan, (int64_t)R * c.n_kv_heads * chunks);
     if (fewer_splits && ws_bytes >= prefix.bytes + per_split) splits = (int)std::min<size_t>(splits, (ws_bytes - prefix.bytes) / per_split);
     if (prefix.path != kOwnTables && ws_bytes >= prefix.bytes + splits * per_split) {
       p.groups = *groups;

@@ -129,17 +129,60 @@ __device__ __forceinline__ bool find_unit(const PagedParams& p, int number, bool
 // Places of a CTA's stretch, of `places` in all
 __device__ __forceinline__ int prefix_stretch(const PagedParams& p, int places) { return max(kPrefixLeast, (places + p.prefix_ctas - 1) / p.prefix_ctas); }
 
-// How many of the keys that a row sees (len) the prefix kernel takes: those its group shares, or none where it does not see all of
-// them, or where the groups' bounds do not ascend within the rows.  Called by whole warps, `row` the same in all lanes.
-__device__ __forceinline__ int group_prefix(const PagedParams& p, int row) {
-  int prefix = 0;
+// Where the results of a row's prefix are.
+struct RowPrefix {
+  int prefix;                                          // keys that the row's group shares; 0: no group
+  int row0, tiles, key_tiles, places;                  // of its group
+  int places_before, units_before, stretch;
+
+  // The parts of query `in_group` of the group (rows times heads of a key head) at key head hk: how many, the first one's place, and from one
+  // to the next, in queries
+  __device__ __forceinline__ int parts(const PagedParams& p, int hk, int in_group, size_t* first, int* step) const {
+    const int unit = hk * tiles + in_group / p.unit_items, number = units_before + unit, in_unit = in_group % p.unit_items;
+    *step = p.unit_items;
+    if (p.prefix_splits) {
+      const int per = prefix_split_keys(p, prefix);
+      *first = (size_t)number * p.prefix_splits * p.unit_items + in_unit;
+      return (prefix + per - 1) / per;
+    }
+    const int t0 = places_before + unit * places, c0 = t0 / stretch;
+    *first = (size_t)(c0 + number) * p.unit_items + in_unit;
+    return (t0 + key_tiles - 1) / stretch - c0 + 1;
+  }
+};
+
+// Whole warps, `row` the same in all lanes.  Bounds that do not ascend within the rows make no groups.
+__device__ __forceinline__ RowPrefix row_prefix(const PagedParams& p, int row) {
+  int places = 0, before = 0, units_before = 0, prefix = 0, row0 = 0, tiles = 0, key_tiles = 0;
+  bool bad = false, mine = false;
   for (int i = threadIdx.x & 31; i < p.groups.n; i += 32) {
     const PrefixGroup g = prefix_group(p, i);
-    if (g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R) prefix = INT32_MAX;
-    else if (g.row0 <= row && row < g.row0 + g.rows && prefix < INT32_MAX) prefix = g.prefix;
+    bad = bad || g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R;
+    const int units = g.units(p.Hkv), all = units * g.places();
+    places += all;
+    if (g.row0 + g.rows <= row) {
+      before += all;
+      units_before += units;
+    } else if (g.row0 <= row) {
+      mine = true;
+      prefix = g.prefix; row0 = g.row0; tiles = g.tiles; key_tiles = g.key_tiles;
+    }
   }
-  prefix = __reduce_max_sync(0xffffffffu, prefix);
-  return prefix == INT32_MAX ? 0 : prefix;
+  RowPrefix r = {};
+  const unsigned who = __ballot_sync(0xffffffffu, mine);
+  bad = __any_sync(0xffffffffu, bad);
+  places = __reduce_add_sync(0xffffffffu, places);
+  r.places_before = __reduce_add_sync(0xffffffffu, before);
+  r.units_before = __reduce_add_sync(0xffffffffu, units_before);
+  if (bad || !who) return r;
+  const int lane = __ffs(who) - 1;
+  r.prefix = __shfl_sync(0xffffffffu, prefix, lane);
+  r.row0 = __shfl_sync(0xffffffffu, row0, lane);
+  r.tiles = __shfl_sync(0xffffffffu, tiles, lane);
+  r.key_tiles = __shfl_sync(0xffffffffu, key_tiles, lane);
+  r.places = r.key_tiles + 1;
+  r.stretch = prefix_stretch(p, places);
+  return r;
 }
 
 // prefix.cu: the results of every group's prefix, for the rows that see all of it, and their join with those of the rows' own keys

@@ -570,7 +570,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
   }
 }
 
-// Joins the parts of a row's head: those of the prefix, where the row has them, and those of its own keys.  A head takes WARPS warps of the
+// Joins the parts of a row's head where its own keys are in several: those of the prefix, if the row has them, and its own.  A head takes WARPS warps of the
 // CTA, which go over the parts in turn and are added up in their order; a lane has DH / 32 dimensions.
 constexpr int kJoinWarps = 8;
 
@@ -587,43 +587,13 @@ prefix_join_kernel(PagedParams p) {
   serving_next();
   const bool there = item < (int64_t)p.R * p.H;        // the same for a head's warps
   const int row = there ? (int)(item / p.H) : 0, head = (int)(item % p.H);
-  int seq = 0, prefix = 0, n_first = 0;
-  size_t first_part = 0, part_step = 0;
+  int seq = 0, prefix = 0, n_first = 0, part_step = 0;
+  size_t first_part = 0;
+  const RowPrefix shared = row_prefix(p, row);
   const int len = there ? row_keys(p, row, &seq, false) : 0;
-  if (len > 0) {
-    // this row's group, and how many places and units stand before it in the line
-    int places = 0, places_before = 0, units_before = 0, group = -1;
-    bool bad = false;
-    for (int i = lane; i < p.groups.n; i += 32) {
-      const PrefixGroup g = prefix_group(p, i);
-      bad = bad || g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R;
-      const int units = g.units(p.Hkv), all = units * g.places();
-      places += all;
-      if (g.row0 + g.rows <= row) { places_before += all; units_before += units; }
-      else if (g.row0 <= row) group = i;
-    }
-    places = __reduce_add_sync(0xffffffffu, places);
-    places_before = __reduce_add_sync(0xffffffffu, places_before);
-    units_before = __reduce_add_sync(0xffffffffu, units_before);
-    group = __any_sync(0xffffffffu, bad) ? -1 : __reduce_max_sync(0xffffffffu, group);
-    if (group >= 0) {
-      const PrefixGroup g = prefix_group(p, group);
-      if (g.key_tiles && len >= g.prefix) {
-        prefix = g.prefix;
-        const int in_unit = (row - g.row0) * p.G + head % p.G, unit = head / p.G * g.tiles + in_unit / p.unit_items;
-        part_step = p.unit_items;
-        if (p.prefix_splits) {
-          const int per = prefix_split_keys(p, prefix);
-          n_first = (prefix + per - 1) / per;
-          first_part = (size_t)(units_before + unit) * p.prefix_splits * p.unit_items + in_unit % p.unit_items;
-        } else {
-          const int stretch = prefix_stretch(p, places), t0 = places_before + unit * g.places();
-          const int c0 = t0 / stretch, c1 = (t0 + g.key_tiles - 1) / stretch;
-          n_first = c1 - c0 + 1;
-          first_part = (size_t)(c0 + units_before + unit) * p.unit_items + in_unit % p.unit_items;
-        }
-      }
-    }
+  if (shared.prefix > 0 && len >= shared.prefix) {
+    prefix = shared.prefix;
+    n_first = shared.parts(p, head / p.G, (row - shared.row0) * p.G + head % p.G, &first_part, &part_step);
   }
   const int own = len - prefix, per = split_keys(p, own), n_own = own > 0 ? (own + per - 1) / per : 0;
   const bool work = there && (prefix > 0 || n_own > 1);      // other rows are written already
@@ -642,7 +612,7 @@ prefix_join_kernel(PagedParams p) {
       x[e] = {};
       if (s >= n) continue;
       const bool own_keys = s >= n_first;
-      const size_t at = own_keys ? own_part + (s - n_first) : first_part + s * part_step;
+      const size_t at = own_keys ? own_part + (s - n_first) : first_part + (size_t)s * part_step;
       ml[e] = *reinterpret_cast<const float2*>((own_keys ? p.part_ml : p.prefix_ml) + 2 * at);
       const float* from = (own_keys ? p.part_o : p.prefix_o) + at * DH + kDims * lane;
       if constexpr (kDims == 4) {
