@@ -481,6 +481,13 @@ int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_toke
                const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
                int table_width, float* d_logits);
 
+/* qzo_decode for rows that share the beginning of their caches: the groups are those of qzo_shared_prefix_attention, which takes the place
+ * of the attention in every layer (as long as the model's workspace has room for what prefixes leave; without it every row reads its own table). */
+int qzo_decode_groups(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
+                      const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
+                      int table_width, const int32_t* d_group_rows, const int32_t* d_prefix_seq, const int32_t* d_prefix_len, int n_groups,
+                      float* d_logits);
+
 /* The same step from the requests' side: qzo_assign_slots on (d_lens, d_new, ...), in place and for R rows, then qzo_decode of the
  * rows it numbers.  d_tokens int32 [R]: the new tokens, request by request, anything behind the last row; d_maps int32 [3][R]
  * receives row_seq, positions and slots.  The block size is the caches', d_block_table int32 [B][table_width], the other

@@ -4,6 +4,7 @@
 #include "qzo_common.cuh"
 #include "launch.cuh"
 #include "layers.cuh"
+#include "paged.cuh"
 
 #include <atomic>
 #include <cmath>
@@ -351,7 +352,7 @@ static int decode_linears(qzo_model* m, const Linear* const* Ls, __nv_bfloat16* 
 
 // One step of answering: R rows through the unperturbed model over the paged caches of its layers.
 int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, const int32_t* row_seq, const int32_t* positions,
-           const int32_t* slots, int R, const int32_t* table, int n_seqs, int width, float* d_logits) {
+           const int32_t* slots, int R, const int32_t* table, int n_seqs, int width, float* d_logits, const PrefixGroups* groups = nullptr) {
   const qzo_model_desc& d = m->desc;
   const int dm = d.d_model, H = d.n_heads, dh = dm / H, F = d.d_ffn;
   const bool llama = d.arch == QZO_ARCH_LLAMA;
@@ -373,7 +374,7 @@ int decode(qzo_model* m, const qzo_kv_cache* caches, const int32_t* tokens, cons
                                       llama ? m->rope_cs : nullptr, d.max_seq, positions, slots, m->qkv, 3 * dm, caches[li], R, H,
                                       m->answer_status, st));
     QZO_TRY(launch_paged_attention(m->qkv, 3 * dm, caches[li], table, n_seqs, width, row_seq, positions, slots, scale, m->att, dm, R, H,
-                                   m->logits, ws_bytes, true, m->answer_status, st));
+                                   m->logits, ws_bytes, true, m->answer_status, st, groups));
     const Linear* o_l[1] = {&L.lin[3]};
     __nv_bfloat16* xn_o[1] = {m->xn};
     QZO_TRY(decode_linears(m, o_l, xn_o, 1, dm, m->att, R));
@@ -908,6 +909,20 @@ int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_toke
   if (!words_aligned(d_tokens, d_row_seq, d_positions, d_slots, d_block_table)) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_decode(m, h_caches, R, n_seqs, table_width, d_logits));
   return decode(m, h_caches, d_tokens, d_row_seq, d_positions, d_slots, R, d_block_table, n_seqs, table_width, d_logits);
+}
+
+int qzo_decode_groups(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
+                      const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
+                      int table_width, const int32_t* d_group_rows, const int32_t* d_prefix_seq, const int32_t* d_prefix_len, int n_groups,
+                      float* d_logits) {
+  if (!d_tokens || !d_row_seq || !d_positions || !d_slots || !d_block_table) return QZO_ERR_BAD_ARG;
+  if (!d_group_rows || !d_prefix_seq || !d_prefix_len || n_groups <= 0) return QZO_ERR_BAD_ARG;
+  if (!words_aligned(d_tokens, d_row_seq, d_positions, d_slots, d_block_table, d_group_rows, d_prefix_seq, d_prefix_len)) return QZO_ERR_BAD_ARG;
+  QZO_TRY(check_decode(m, h_caches, R, n_seqs, table_width, d_logits));
+  for (int li = 0; li < m->desc.n_layers; ++li)      // rows that a tensor map can name
+    if ((int64_t)h_caches[li].n_blocks * h_caches[li].block_size * h_caches[li].n_kv_heads > INT32_MAX) return QZO_ERR_BAD_ARG;
+  const PrefixGroups groups{d_group_rows, d_prefix_seq, d_prefix_len, n_groups};
+  return decode(m, h_caches, d_tokens, d_row_seq, d_positions, d_slots, R, d_block_table, n_seqs, table_width, d_logits, &groups);
 }
 
 int qzo_decode_requests(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, int32_t* d_lens, const int32_t* d_new,

@@ -859,7 +859,7 @@ int run_groups(const PagedParams& p, const qzo_kv_cache& c, int64_t units, bool 
   // Own keys are few as a rule: CTAs of one warp, twelve on an SM, where there are enough rows and key heads (64 rows on 16 prefixes, 32 key
   // heads, 1 to 64 own keys: 72.0 us in all, 78.7 with four warps; 1 to 400 own keys: 124.6 and 120.0).
   const int64_t ctas = (int64_t)p.R * p.Hkv * p.chunks;
-  if (ctas < 3 * kSMs) QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
+  if (ctas < 3 * kSMs || !p.prefix_splits) QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
   else if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 1, Keys::kOwn>(p, ctas, p.splits, st)));
   else QZO_TRY((run_attention_w<DH, 2, F8, 1, Keys::kOwn>(p, ctas, p.splits, st)));
   return p.splits > 1 ? launch_prefix_join(p, DH, st) : QZO_OK;

@@ -32,7 +32,7 @@ EXPORTS = (
     "qzo_gemv_int4", "qzo_rope_table", "qzo_qk_norm_rope_cache", "qzo_paged_attention_workspace_bytes", "qzo_paged_attention",
     "qzo_assign_slots", "qzo_decode", "qzo_decode_requests",
     "qzo_beam_select_workspace_bytes", "qzo_beam_select", "qzo_fork_requests", "qzo_compact_blocks", "qzo_copy_blocks",
-    "qzo_shared_prefix_attention_workspace_bytes", "qzo_shared_prefix_attention", "qzo_debug_prefix_path",
+    "qzo_shared_prefix_attention_workspace_bytes", "qzo_shared_prefix_attention", "qzo_debug_prefix_path", "qzo_decode_groups",
 )
 
 
@@ -126,6 +126,7 @@ def _load():
         "qzo_debug_prefix_path": (ci, [ci]),
         "qzo_shared_prefix_attention": (ci, [vp, ci, P(KvCacheDesc), vp, ci, ci, vp, vp, vp, vp, vp, ci, cf, vp, ci, ci, ci, vp, sz, vp, vp]),
         "qzo_copy_blocks": (ci, [P(KvCacheDesc), ci, vp, vp, ci, vp, vp]),
+        "qzo_decode_groups": (ci, [vp, P(KvCacheDesc), vp, vp, vp, vp, ci, vp, ci, ci, vp, vp, vp, ci, vp]),
         "qzo_profile_gemms": (ci, [vp, ci]),
         "qzo_profile_read": (ci, [vp, P(i64), P(ctypes.c_double), P(ctypes.c_double)]),
     }
@@ -760,6 +761,21 @@ class Model:
         _ints(dev, 1, block_table)
         _check(_lib.qzo_decode(self.handle, descs, tokens.data_ptr(), row_seq.data_ptr(), positions.data_ptr(), slots.data_ptr(), R,
                                block_table.data_ptr(), n_seqs, width, logits.data_ptr()), "qzo_decode")
+        return logits
+
+    def qzo_decode_groups(self, caches, tokens, row_seq, positions, slots, block_table, group_rows, prefix_seq, prefix_len, logits=None):
+        """qzo_decode for rows that share the beginning of their caches (int32): rows group_rows[i] .. group_rows[i + 1] - 1 ([n + 1]) have the
+        first prefix_len[i] tokens of request prefix_seq[i] ([n] each) as the first tokens of their own requests."""
+        R, n = tokens.numel(), prefix_seq.numel()
+        dev, descs, logits = self._decode_args(caches, R, logits)
+        _ints(dev, R, tokens, row_seq, positions, slots)
+        _ints(dev, n, prefix_seq, prefix_len)
+        _ints(dev, n + 1, group_rows)
+        n_seqs, width = block_table.shape
+        _ints(dev, 1, block_table)
+        _check(_lib.qzo_decode_groups(self.handle, descs, tokens.data_ptr(), row_seq.data_ptr(), positions.data_ptr(), slots.data_ptr(), R,
+                                      block_table.data_ptr(), n_seqs, width, group_rows.data_ptr(), prefix_seq.data_ptr(), prefix_len.data_ptr(), n,
+                                      logits.data_ptr()), "qzo_decode_groups")
         return logits
 
     def qzo_decode_requests(self, caches, tokens, lens, new, block_table, free, free_count, logits=None, status=None):

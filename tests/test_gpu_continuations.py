@@ -545,3 +545,211 @@ def test_a_prefix_of_a_cache_beyond_32_bit_offsets(lib, units):
     small.table, small.ck, small.cv = far, k, v
     assert torch.equal(near, small.run(lib))
     del k, v
+
+
+# ------------------------------------------------------------------ together
+
+def _model(lib, name, max_tokens):
+    from tests.helpers import build_oracle_model
+    cfg = inputs.model_cfg(name)
+    raw = inputs.raw_model_tensors(cfg, seed=1000)
+    return cfg, build_oracle_model(raw), lib.build_model_from_raw(raw, max_tokens)
+
+
+def _oracle_logits(om, tokens):
+    from oracle import model as omodel
+    cap, tok = {}, np.asarray(tokens)[None]
+    omodel.forward_loss(om, tok, np.full_like(tok, -100), 0, 0, 1e-3, capture=cap)
+    return cap["logits"]
+
+
+@pytest.mark.parametrize("name,block,dtype", [("tiny_dh128", 16, torch.bfloat16), ("tiny", 16, torch.bfloat16), ("tiny_opt", 32, torch.bfloat16)])
+def test_beam_search_with_a_model(lib, path, name, block, dtype):
+    # two prompts, four beams each, over one pool: prompts by the first beam, then select, fork, copy, decode, step by step, with a
+    # compaction on the way; every live row's logits are those of the oracle's forward of that beam's whole text
+    cfg, om, gm = _model(lib, name, 4096)
+    B, W, n_blocks, steps, power = 2, 4, 90, 9, 0.6
+    H, dh = cfg["n_heads"], cfg["d_model"] // cfg["n_heads"]
+    pages = lambda: torch.full((n_blocks, H, block, dh), float("nan"), dtype=dtype, device="cuda")  # noqa: E731
+    caches = [lib.KvCache(pages(), pages()) for _ in range(cfg["n_layers"])]
+    rng = _gen(7)
+    longest = cfg["max_seq"] - steps - 1
+    prompts = [rng.integers(0, cfg["vocab"], n).tolist() for n in (longest, longest // 2 + 3)]
+    width = -(-cfg["max_seq"] // block)
+    lens, count, table = ints([0] * (B * W)), ints([n_blocks]), torch.full((B * W, width), -1, dtype=torch.int32, device="cuda")
+    free = torch.from_numpy(rng.permutation(n_blocks).astype(np.int32)).cuda()
+    status = ints([0])
+    end = 3
+    # the prompts: rows of the first beam of each request
+    new = [len(prompts[r // W]) if r % W == 0 else 0 for r in range(B * W)]
+    logits, maps = gm.qzo_decode_requests(caches, ints(sum(prompts, [])), lens, ints(new), table, free, count, status=status)
+    rows = np.full((B, W), -1, np.int32)
+    rows[:, 0] = np.cumsum([len(p) for p in prompts]) - 1
+    text = [list(prompts[r // W]) if r % W == 0 else None for r in range(B * W)]
+    scores = torch.full((B, W), -INF, device="cuda")
+    scores[:, 0] = 0.0
+    last, lengths = ints([[0] * W] * B), ints([[0] * W] * B)
+    groups = dict(group_rows=ints([0, W, 2 * W]), prefix_seq=ints([0, W]), prefix_len=ints([len(p) for p in prompts]))
+    for step in range(steps):
+        host = logits.cpu().numpy()
+        for b in range(B):
+            for w in range(W):
+                r = int(rows[b, w])
+                if r >= 0 and text[b * W + w] is not None:
+                    want = _oracle_logits(om, text[b * W + w])[-1]
+                    assert np.abs(host[r] - want).max() <= 2e-2 * np.abs(want).max(), (step, b, w)
+        want = oracle.beam_select(host, scores.cpu().numpy(), rows, last.cpu().numpy(), end, lengths.cpu().numpy(), power)
+        parents, tokens, scores, lengths = lib.qzo_beam_select(logits, scores, rows=torch.from_numpy(rows).cuda(), last_tokens=last, end_token=end,
+                                                               lengths=lengths, length_power=power, status=status)
+        assert parents.tolist() == [[f[0] for f in best] for best in want] and tokens.tolist() == [[f[1] for f in best] for best in want]
+        table, lens, count, copies, n_copies = lib.qzo_fork_requests(lens, parents, table, free, count, block, n_blocks, status=status)
+        lib.qzo_copy_blocks(caches, copies, n_copies, status=status)
+        if step == 4:
+            table, count, copies, n_copies = lib.qzo_compact_blocks(lens, table, free, block, n_blocks, 60, free_count=count, status=status)
+            lib.qzo_copy_blocks(caches, copies, n_copies, status=status)
+            assert int(table.max()) < 60 and int(count) == 60 - len(set(table[table >= 0].tolist()))
+        was_end = [bool(v) for v in (last.view(-1) == end).tolist()]
+        text = [None if p < 0 else text[p] + ([] if was_end[p] else [t]) for p, t in zip(parents.view(-1).tolist(), tokens.view(-1).tolist())]
+        last = tokens
+        # every beam that goes on adds its token; the others have no row of their own, and padding stands in its place
+        goes = (tokens != end) & (parents >= 0)
+        seq, pos, slots = lib.qzo_assign_slots(lens, goes.to(torch.int32).view(-1).contiguous(), table, free, count, block, B * W, status=status)
+        step_tokens = torch.where(seq >= 0, tokens.view(-1)[seq.clamp(min=0).long()], 0).to(torch.int32)
+        n_rows = [int(goes[:b].sum()) for b in range(B + 1)]
+        groups["group_rows"] = ints(n_rows)
+        # the request that holds the prefix: any of its beams that is still there
+        groups["prefix_seq"] = ints([b * W + int((parents[b] >= 0).int().argmax()) for b in range(B)])
+        logits = gm.qzo_decode_groups(caches, step_tokens, seq, pos, slots, table, **groups)
+        assert int(status) == 0 and gm.qzo_device_status() == 0
+        rows = np.full(B * W, -1, np.int32)
+        live = [r for r in seq.tolist() if r >= 0]
+        rows[live] = np.arange(len(live))
+        rows = rows.reshape(B, W)
+        assert lens.tolist() == [0 if t is None else len(t) for t in text]
+    gm.close()
+
+
+def test_decode_of_groups_refuses_and_reports(lib):
+    cfg, _, gm = _model(lib, "tiny", 64)
+    cache = [lib.KvCache(*(torch.zeros((8, 4, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))) for _ in range(2)]
+    table, z, one = ints([[0, 1, 2, 3], [4, 5, 6, 7]]), ints([0, 0]), ints([0, 1])
+    a = dict(tokens=z, row_seq=one, positions=z, slots=ints([0, 64]), block_table=table)
+    for rows, seq, length, ok in ((ints([0, 2]), ints([0]), ints([1]), True), (ints([0]), ints([0]), ints([1]), False), (ints([0, 2]), ints([0]).float(), ints([1]), False),
+                                  (torch.tensor([0, 2], dtype=torch.int32), ints([0]), ints([1]), False)):
+        if ok:
+            assert gm.qzo_decode_groups(cache, group_rows=rows, prefix_seq=seq, prefix_len=length, **a).shape == (2, cfg["vocab"])
+        else:
+            with pytest.raises(AssertionError):
+                gm.qzo_decode_groups(cache, group_rows=rows, prefix_seq=seq, prefix_len=length, **a)
+    lib.qzo_debug_prefix_path(2)
+    try:                                                # a workspace that holds no prefix: own tables; and none is touched beyond its end
+        plain = gm.qzo_decode(cache, **a)
+        assert torch.equal(plain, gm.qzo_decode_groups(cache, group_rows=ints([0, 2]), prefix_seq=z[:1], prefix_len=ints([1]), **a))
+    finally:
+        lib.qzo_debug_prefix_path(0)
+    for bad in (-1, 4):
+        with pytest.raises(lib.QzoError):
+            lib.qzo_debug_prefix_path(bad)
+    gm.close()
+
+
+def test_a_search_step_in_a_replayed_graph_and_on_two_streams(lib, path):
+    # select, fork, copy and attend, captured behind a side stream's work, replayed with new inputs; then two streams at once with a workspace each
+    case = Shared([(4, 500, [9, 20, 33, 70]), (4, 300, [1, 2, 3, 4])], 8, 2, 128, 16, "bf16", 51)
+    R, V, block, n_blocks = case.R, 3000, 16, case.ck.shape[0]
+    rng = _gen(52)
+    side = torch.cuda.Stream()
+
+    def state(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        s = dict(logits=torch.randn(R, V, generator=g, device="cuda"), scores=-torch.rand(2, 4, generator=g, device="cuda"), q=torch.randn(R, 8, 128, generator=g, device="cuda").bfloat16(),
+                 k=case.ck.clone(), v=case.cv.clone(), table=torch.from_numpy(case.table[2:]).cuda(), lens=ints(case.lens), count=ints([60]))
+        s["free"] = torch.full((n_blocks + 70,), -1, dtype=torch.int32, device="cuda")
+        s["free"][:60] = torch.arange(n_blocks, n_blocks + 60)
+        s["k"] = torch.cat((s["k"], torch.zeros_like(s["k"][:60].repeat(60 // s["k"].shape[0] + 1, 1, 1, 1)[:60])))
+        s["v"] = torch.cat((s["v"], torch.zeros_like(s["v"][:60].repeat(60 // s["v"].shape[0] + 1, 1, 1, 1)[:60])))
+        return s
+
+    def step(s, ws):
+        cache = lib.KvCache(s["k"], s["v"])
+        parents, tokens, scores, _ = lib.qzo_beam_select(s["logits"], s["scores"], workspace=ws[0])
+        table, lens, count, copies, n = lib.qzo_fork_requests(s["lens"], parents, s["table"], s["free"], s["count"], block, n_blocks + 60)
+        lib.qzo_copy_blocks([cache], copies, n)
+        positions = lens - 1
+        out = lib.qzo_shared_prefix_attention(s["q"], cache, table, positions, s["rows"], s["seq"], s["prefix"], workspace=ws[1])
+        return parents, tokens, scores, table, lens, count, copies, n, out
+
+    def workspaces():
+        return (torch.empty(lib.qzo_beam_select_workspace_bytes(2, 4, V), dtype=torch.uint8, device="cuda"),
+                torch.empty(max(1, lib.qzo_shared_prefix_attention_workspace_bytes(R, 2, 8, 2, 128, case.table.shape[1] * block)), dtype=torch.uint8, device="cuda"))
+    states = [state(i) for i in range(4)]
+    for s in states:
+        s["rows"], s["seq"], s["prefix"] = ints([0, 4, 8]), ints([0, 4]), ints([500, 300])
+    ws = workspaces()
+    # what each state gives by itself, on copies (a step changes pages and stack)
+    want = [[t.clone() for t in step({k: v.clone() for k, v in s.items()}, ws)] for s in states]
+    for w in want:
+        assert not torch.isnan(w[-1].float()).any()
+    live = {k: v.clone() for k, v in states[0].items()}
+    fresh = {k: v.clone() for k, v in states[0].items()}
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step({k: v.clone() for k, v in states[0].items()}, ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            for k in live:
+                live[k].copy_(fresh[k])
+            got = step(live, ws)
+        for i in (1, 0, 2, 3, 1):
+            for k in fresh:
+                fresh[k].copy_(states[i][k])
+            graph.replay()
+            side.synchronize()
+            for a, b in zip(got, want[i]):
+                assert torch.equal(a, b)
+    # two streams at once
+    other = torch.cuda.Stream()
+    mine = [{k: v.clone() for k, v in s.items()} for s in states[:2]]
+    both = [workspaces(), workspaces()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for turn in range(10):
+        for i, st in enumerate((side, other)):
+            with torch.cuda.stream(st):
+                got[i].append(step({k: v.clone() for k, v in mine[i].items()}, both[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            for a, b in zip(g, want[i]):
+                assert torch.equal(a, b)
+    del graph
+
+
+def test_tensors_off_the_device_or_of_another_shape_are_refused(lib):
+    case = Shared([(2, 100, 5)], 2, 2, 64, 16, "bf16", 61)
+    cache, table, pos = lib.KvCache(case.ck, case.cv), torch.from_numpy(case.table).cuda(), ints(case.positions)
+    good = dict(q=case.q.cuda(), cache=cache, block_table=table, positions=pos, group_rows=ints([0, 2]), prefix_seq=ints([0]), prefix_len=ints([100]), row_seq=ints([1, 2]))
+    lib.qzo_shared_prefix_attention(**good)
+    for change in (dict(q=case.q), dict(positions=pos.cpu()), dict(group_rows=ints([0])), dict(prefix_len=ints([])), dict(prefix_seq=ints([0]).long()), dict(row_seq=ints([1])),
+                   dict(out=torch.empty(2, 2, 32, dtype=torch.bfloat16, device="cuda")), dict(q=case.q.cuda().float())):
+        with pytest.raises(AssertionError):
+            lib.qzo_shared_prefix_attention(**{**good, **change})
+    lib.qzo_debug_prefix_path(3)
+    with pytest.raises(lib.QzoError):
+        lib.qzo_shared_prefix_attention(**good, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    lib.qzo_debug_prefix_path(0)
+    x, scores = torch.randn(4, 50, device="cuda"), torch.zeros(2, 2, device="cuda")
+    lib.qzo_beam_select(x, scores)
+    for change in (dict(logits=x.cpu()), dict(logits=x.half()), dict(scores=scores.cpu()), dict(scores=scores.double()), dict(last_tokens=ints([1])), dict(logits=x.t()),
+                   dict(rows=ints([[0, 1]])), dict(scores_out=torch.zeros(1, device="cuda"))):
+        with pytest.raises(AssertionError):
+            lib.qzo_beam_select(**{**dict(logits=x, scores=scores), **change})
+    lens, tab, free, n = ints([5, 20]), ints([[0, 1], [2, 3]]), ints([4, 5, -1, -1, -1, -1]), ints([2])
+    for change in (dict(parents=ints([0])), dict(lens=lens.cpu()), dict(block_table=tab.long()), dict(table_out=ints([[0, 1]])), dict(copies=ints([0, 0, 0]))):
+        with pytest.raises(AssertionError):
+            lib.qzo_fork_requests(**{**dict(lens=lens, parents=ints([0, 1]), block_table=tab, free=free, free_count=n, block_size=16, n_blocks=6), **change})
+    with pytest.raises(lib.QzoError):                   # never in place
+        lib.qzo_fork_requests(lens, ints([0, 1]), tab, free, n, 16, 6, table_out=tab)
+    with pytest.raises(AssertionError):
+        lib.qzo_copy_blocks([], ints([[0, 1, 2]]), ints([1]))

@@ -168,14 +168,22 @@ def test_fork_compact_and_copy_refusals():
 @made_up
 def test_shared_prefix_attention_refusals():
     qzo = _lib()
-    need = qzo.qzo_shared_prefix_attention_workspace_bytes(3, 2, 4, 2, 64, 64)
-    assert need > 0
+    sizes = {}
+    for path in (0, 1, 2, 3):
+        qzo.qzo_debug_prefix_path(path)
+        sizes[path] = qzo.qzo_shared_prefix_attention_workspace_bytes(3, 2, 4, 2, 64, 64)
+    qzo.qzo_debug_prefix_path(0)
+    assert sizes[0] == sizes[1] == 0 < sizes[2] < sizes[3]              # by rule, little that is shared stays with the rows
+    assert qzo.qzo_shared_prefix_attention_workspace_bytes(64, 1, 32, 32, 128, 4096) > 0
+    for path in (-1, 4):
+        with pytest.raises(qzo.QzoError):
+            qzo.qzo_debug_prefix_path(path)
     for args in ((0, 1, 4, 2, 64, 64), (1, 0, 4, 2, 64, 64), (1, 1, 3, 2, 64, 64), (1, 1, 4, 0, 64, 64), (1, 1, 4, 2, 80, 64), (1, 1, 4, 2, 64, 0),
                  (1, 1, 4, 2, 64, (1 << 30) + 1)):
         with pytest.raises(qzo.QzoError):
             qzo.qzo_shared_prefix_attention_workspace_bytes(*args)
 
-    def call(q, ldq, cache, tab, n, w, seq, pos, rows, pseq, plen, g, scale, out, ldo, R, H, ws=P, b=need, status=NONE):
+    def call(q, ldq, cache, tab, n, w, seq, pos, rows, pseq, plen, g, scale, out, ldo, R, H, ws=NONE, b=0, status=NONE):
         return qzo._lib.qzo_shared_prefix_attention(q, ldq, None if cache is None else ctypes.byref(cache), tab, n, w, seq, pos, rows, pseq, plen, g, scale, out,
                                                     ldo, R, H, ws, b, status, None)
     good = dict(q=P, ldq=256, cache=_cache(), tab=P, n=3, w=4, seq=NONE, pos=P, rows=P, pseq=P, plen=P, g=2, scale=0.125, out=Q, ldo=256, R=3, H=4)
@@ -186,6 +194,15 @@ def test_shared_prefix_attention_refusals():
     assert call(**good) in (qzo.QZO_OK, qzo.ERR_UNSUPPORTED_DEVICE)
     for change in bad + [dict(cache=_cache(**c)) for c in caches]:
         assert call(**{**good, **change}) == qzo.ERR_BAD_ARG, change
+
+
+@made_up
+def test_decode_of_groups_refuses_before_the_model_is_looked_at():
+    lib, qzo = _lib()._lib, _lib()
+    def call(m=NONE, tok=P, seq=P, pos=P, slots=P, tab=P, rows=P, pseq=P, plen=P, n=2, out=P):
+        return lib.qzo_decode_groups(m, ctypes.byref(_cache()), tok, seq, pos, slots, 2, tab, 2, 4, rows, pseq, plen, n, out)
+    for change in [{n: v} for n in ("tok", "seq", "pos", "slots", "tab", "rows", "pseq", "plen") for v in (NONE, ODD)] + [dict(n=0), dict(out=NONE), dict(m=NONE)]:
+        assert call(**change) == qzo.ERR_BAD_ARG, change
 
 
 def test_the_binding_names_the_limits_of_the_header():
