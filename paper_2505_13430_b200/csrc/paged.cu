@@ -200,8 +200,6 @@ qk_norm_rope_cache_kernel(RopeCacheParams p) {
 
 // How the prefixes of groups are taken: by the rows, through their own tables; by units of few queries; by units of many, in prefix.cu
 enum PrefixPath { kByRule, kOwnTables, kFewPath, kManyPath };
-constexpr int kFewQueries = 32;                        // of a group and key head
-constexpr int64_t kLeastAskedMany = 270000000, kLeastAskedFew = 135000000;       // bytes, see prefix_plan
 constexpr int kStageBytes = 8192;                      // of a warp's ring: 4 KB of keys and 4 KB of values
 constexpr int kSub = 16;                               // keys of one matrix tile; a block of the cache holds whole ones
 
@@ -857,9 +855,10 @@ int run_groups(const PagedParams& p, const qzo_kv_cache& c, int64_t units, bool 
   else if (p.unit_items == 8) QZO_TRY((run_attention_w<DH, 1, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
   else QZO_TRY((run_attention_w<DH, 2, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
   // Own keys are few as a rule: CTAs of one warp, twelve on an SM, where there are enough rows and key heads (64 rows on 16 prefixes, 32 key
-  // heads, 1 to 64 own keys: 72.0 us in all, 78.7 with four warps; 1 to 400 own keys: 124.6 and 120.0).
-  const int64_t ctas = (int64_t)p.R * p.Hkv * p.chunks;
-  if (ctas < 3 * kSMs || !p.prefix_splits) QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
+  // heads, 1 to 64 own keys: 72.0 us in all, 78.7 with four warps; 1 to 400 own keys: 124.6 and 120.0), but not where several heads have
+  // many parts to join (128 rows of 8 heads, ten parts: 83.9 us and 73.7).
+  const int64_t ctas = (int64_t)p.R * p.Hkv * p.chunks, parts = p.prefix_splits ? p.prefix_splits : p.prefix_ctas / units + 1;
+  if (ctas < 3 * kSMs || parts * std::min(p.G, 16) >= 32) QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
   else if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 1, Keys::kOwn>(p, ctas, p.splits, st)));
   else QZO_TRY((run_attention_w<DH, 2, F8, 1, Keys::kOwn>(p, ctas, p.splits, st)));
   return p.splits > 1 ? launch_prefix_join(p, DH, st) : QZO_OK;
@@ -917,14 +916,22 @@ struct PrefixPlan {
 PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int64_t max_len) {
   PrefixPlan plan{kOwnTables, 0, 0, 0, 0, 0, 0};
   const int subs = 256 / (dh * (f8 ? 1 : 2)), forced = forced_path.load();
-  // With groups of few rows a call without groups reads the shared blocks from L2, so that sharing pays only where that is a lot: at 270 MB of
-  // keys and values asked for the two took equally long, whatever the rows, heads and lengths (tensor-core units; 4 to 64 rows over 8 and
-  // 32 key heads, bf16 and e4m3).  All of this goes by the table's width, as lengths are known on the device only.
-  const int64_t asked = (int64_t)R * Hkv * max_len * dh * (f8 ? 2 : 4), queries = (int64_t)R * G / std::max(1, std::min(R, n_groups));
-  plan.path = forced != kByRule ? (PrefixPath)forced : asked < (queries <= kFewQueries ? kLeastAskedFew : kLeastAskedMany) ? kOwnTables
-              : queries <= kFewQueries ? kFewPath : kManyPath;
+  const int64_t queries = (int64_t)R * G / std::max(1, std::min(R, n_groups));   // of a group and key head, on average
+  const int few_items = queries <= 8 ? 8 : 16;
+  // The way whose time is estimated as the shortest, in us: what it takes beside the keys and values, and the bytes of those that its CTAs
+  // ask for.  The rates are those of measurements with 4 to 128 rows in 1 to 16 groups over 4 to 32 key heads of 128 and 256 to 16384 shared
+  // tokens, bf16 (e4m3); most of the rows' own requests are met by L2, and e4m3 tiles are held up by their conversion in the kernel for many
+  // queries.  Examples, us through own tables, few, many: 64 rows of 64 queries on 2048 138, 30, 42, on 16384 1045, 143, 84; 128 rows of 1024 queries
+  // on 16384 275, 238, 72 (203, 159, 103); 32 rows of 128 queries on 8192 95, 45, 39 (68, 34, 42); 64 rows on 16 prefixes of 256 33, 22, 49.
+  // Lengths are known on the device only: all of this goes by the table's width.
+  const double bytes = (double)max_len * dh * (f8 ? 2 : 4);           // of a key head
+  const double own = 4 + (double)R * Hkv * bytes / (f8 ? 11e6 : 14.5e6);
+  const double rows = R * (double)Hkv / 400;           // the rows' own keys: a CTA for each row and key head
+  const double few = 9 + rows + (double)prefix_units(R, n_groups, G, Hkv, few_items) * bytes / (f8 ? 6.5e6 : 7.6e6);
+  const double many = (f8 ? 37 : 25) + rows + (double)prefix_units(R, n_groups, G, Hkv, kPrefixQueries) * bytes / (f8 ? 2e6 : 6.3e6);
+  plan.path = forced != kByRule ? (PrefixPath)forced : own <= std::min(few, many) ? kOwnTables : few <= many ? kFewPath : kManyPath;
   if (plan.path == kOwnTables) return plan;
-  plan.items = plan.path == kManyPath ? kPrefixQueries : queries <= 8 ? 8 : 16;
+  plan.items = plan.path == kManyPath ? kPrefixQueries : few_items;
   plan.units = prefix_units(R, n_groups, G, Hkv, plan.items);
   if (plan.path == kManyPath) {
     plan.parts = plan.units + 2 * kSMs;

@@ -383,8 +383,9 @@ bool tables_ok(const void* lens, const void* table, const void* table_out, const
   return block_size_ok(block_size) && (int64_t)width * block_size <= kMostKeys && (int64_t)n_blocks * block_size <= INT32_MAX;
 }
 
-// CTAs of the cluster that goes over B tables
+// CTAs of the cluster that goes over B tables, and their threads: small tables and pools do with fewer, which meet sooner
 int table_ctas(int B, int width) { return (int64_t)B * width > 4096 ? kMostCtas : 1; }
+int table_threads(int B, int width, int words) { return (int64_t)B * width <= 1024 && words <= 1024 ? 256 : kPageThreads; }
 
 }  // namespace
 }  // namespace qzo
@@ -411,7 +412,7 @@ int qzo_fork_requests(const int32_t* d_lens, const int32_t* d_parents, int B, co
     QZO_CUDA_TRY(allow_dynamic_smem(fork_requests_kernel, kMost, allowed));
   }
   const int ctas = table_ctas(B, table_width);
-  return launch_serving(fork_requests_kernel, dim3(ctas), dim3(kPageThreads), (3 * B + 2 * words) * sizeof(int), ctas, (cudaStream_t)stream, p);
+  return launch_serving(fork_requests_kernel, dim3(ctas), dim3(table_threads(B, table_width, words)), (3 * B + 2 * words) * sizeof(int), ctas, (cudaStream_t)stream, p);
 }
 
 int qzo_compact_blocks(const int32_t* d_lens, int B, const int32_t* d_block_table, int table_width, int block_size, int n_blocks, int keep,
@@ -430,7 +431,7 @@ int qzo_compact_blocks(const int32_t* d_lens, int B, const int32_t* d_block_tabl
     constexpr int kMost = 2 * (QZO_MAX_POOL_BLOCKS / 32) * (int)sizeof(int);
     QZO_CUDA_TRY(allow_dynamic_smem(compact_blocks_kernel, kMost, allowed));
   }
-  return launch_serving(compact_blocks_kernel, dim3(ctas), dim3(kPageThreads), 2 * words * sizeof(int), ctas, (cudaStream_t)stream, p);
+  return launch_serving(compact_blocks_kernel, dim3(ctas), dim3(table_threads(B, table_width, words)), 2 * words * sizeof(int), ctas, (cudaStream_t)stream, p);
 }
 
 int qzo_copy_blocks(const qzo_kv_cache* h_caches, int n_caches, const int32_t* d_copies, const int32_t* d_copy_count, int max_copies,

@@ -566,27 +566,46 @@ def qzo_beam_select(logits, scores, rows=None, last_tokens=None, end_token=-1, l
     B, W = scores.shape
     n_rows, V = logits.shape
     ldl, one = logits.stride()
+    n = B * W
     assert logits.dtype is _F32 and (one == 1 or V == 1) and logits.get_device() == dev, "logits: expects float32 [rows][V] on the current device"
-    _floats(dev, B * W, scores, "scores")
-    _ints(dev, B * W, *(t for t in (rows, last_tokens, lengths, parents, tokens, lengths_out) if t is not None))
-    if parents is None:
-        parents = scores.new_empty(B, W, dtype=_I32)
-    if tokens is None:
-        tokens = scores.new_empty(B, W, dtype=_I32)
+    scores_at = _floats(dev, n, scores, "scores")
+    rows_at = last_at = lengths_at = lengths_out_at = None
+    if rows is not None:
+        _ints(dev, n, rows)
+        rows_at = rows.data_ptr()
+    if last_tokens is not None:
+        _ints(dev, n, last_tokens)
+        last_at = last_tokens.data_ptr()
+    if lengths is not None:
+        _ints(dev, n, lengths)
+        lengths_at = lengths.data_ptr()
+    if parents is None and tokens is None and lengths_out is None:       # one allocation for what is int32
+        made = scores.new_empty(2 if lengths is None else 3, B, W, dtype=_I32)
+        parents, tokens, *rest = made.unbind()
+        at = made.data_ptr()
+        parents_at, tokens_at = at, at + 4 * n
+        if rest:
+            lengths_out, lengths_out_at = rest[0], at + 8 * n
+    else:
+        parents = scores.new_empty(B, W, dtype=_I32) if parents is None else parents
+        tokens = scores.new_empty(B, W, dtype=_I32) if tokens is None else tokens
+        _ints(dev, n, parents, tokens)
+        parents_at, tokens_at = parents.data_ptr(), tokens.data_ptr()
+        if lengths is not None or lengths_out is not None:
+            lengths_out = scores.new_empty(B, W, dtype=_I32) if lengths_out is None else lengths_out
+            _ints(dev, n, lengths_out)
+            lengths_out_at = lengths_out.data_ptr()
     if scores_out is None:
         scores_out = scores.new_empty(B, W)
+        scores_out_at = scores_out.data_ptr()
     else:
-        _floats(dev, B * W, scores_out, "scores_out")
-    if lengths is not None and lengths_out is None:
-        lengths_out = scores.new_empty(B, W, dtype=_I32)
+        scores_out_at = _floats(dev, n, scores_out, "scores_out")
     if workspace is None:
         workspace = scores.new_empty(qzo_beam_select_workspace_bytes(B, W, V), dtype=_U8)
     assert workspace.is_contiguous() and workspace.get_device() == dev, "workspace: contiguous, on the current device"
-    opt = lambda t: None if t is None else t.data_ptr()
-    rc = _lib.qzo_beam_select(logits.data_ptr(), ldl if n_rows > 1 else V, n_rows, opt(rows), scores.data_ptr(), opt(last_tokens), end_token, opt(lengths),
-                              length_power, B, W, V, parents.data_ptr(), tokens.data_ptr(), scores_out.data_ptr(), opt(lengths_out),
-                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), None if status is None else _status(dev, status),
-                              _raw_stream(dev))
+    rc = _lib.qzo_beam_select(logits.data_ptr(), ldl if n_rows > 1 else V, n_rows, rows_at, scores_at, last_at, end_token, lengths_at, length_power, B, W, V,
+                              parents_at, tokens_at, scores_out_at, lengths_out_at, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                              None if status is None else _status(dev, status), _raw_stream(dev))
     if rc:
         _check(rc, "qzo_beam_select")
     return parents, tokens, scores_out, lengths_out
@@ -607,20 +626,24 @@ def qzo_fork_requests(lens, parents, block_table, free, free_count, block_size, 
     else:
         assert table_out.shape == block_table.shape, "table_out: as block_table"
         _ints(dev, 1, table_out)
-    if lens_out is None:
-        lens_out = lens.new_empty(B)
-    if free_count_out is None:
-        free_count_out = lens.new_empty(1)
-    if copies is None:
-        copies = lens.new_empty(B, 3)
-    if copy_count is None:
-        copy_count = lens.new_empty(1)
-    _ints(dev, B, lens_out)
-    _ints(dev, 1, free_count_out, copy_count)
-    _ints(dev, 3 * B, copies)
+    if lens_out is None and free_count_out is None and copies is None and copy_count is None:       # one allocation for all of them
+        made = lens.new_empty(4 * B + 2)
+        lens_out, copies, free_count_out, copy_count = made.split((B, 3 * B, 1, 1))
+        copies = copies.view(B, 3)
+        at = made.data_ptr()
+        lens_at, copies_at, free_count_at, count_at = at, at + 4 * B, at + 16 * B, at + 16 * B + 4
+    else:
+        lens_out = lens.new_empty(B) if lens_out is None else lens_out
+        free_count_out = lens.new_empty(1) if free_count_out is None else free_count_out
+        copies = lens.new_empty(B, 3) if copies is None else copies
+        copy_count = lens.new_empty(1) if copy_count is None else copy_count
+        _ints(dev, B, lens_out)
+        _ints(dev, 1, free_count_out, copy_count)
+        _ints(dev, 3 * B, copies)
+        lens_at, copies_at, free_count_at, count_at = lens_out.data_ptr(), copies.data_ptr(), free_count_out.data_ptr(), copy_count.data_ptr()
     rc = _lib.qzo_fork_requests(lens.data_ptr(), parents.data_ptr(), B, block_table.data_ptr(), width, block_size, n_blocks, free.data_ptr(), free.numel(),
-                                free_count.data_ptr(), lens_out.data_ptr(), table_out.data_ptr(), free_count_out.data_ptr(), copies.data_ptr(),
-                                copy_count.data_ptr(), None if status is None else _status(dev, status), _raw_stream(dev))
+                                free_count.data_ptr(), lens_at, table_out.data_ptr(), free_count_at, copies_at, count_at,
+                                None if status is None else _status(dev, status), _raw_stream(dev))
     if rc:
         _check(rc, "qzo_fork_requests")
     return table_out, lens_out, free_count_out, copies, copy_count
@@ -655,7 +678,9 @@ def qzo_copy_blocks(caches, copies, copy_count, status=None):
     """The listed copies of pages (int32 [n][3]: from, to, tokens; copy_count int32 [1]: how many) in every one of the caches (list of KvCache of
     one shape and type, as the layers of a model)."""
     dev = _device_now()
-    assert len(caches) > 0 and all(c.device == dev for c in caches), "caches: expects KvCache on the current device"
+    assert len(caches) > 0, "caches: expects at least one"
+    for c in caches:
+        assert c.device == dev, "caches: expects KvCache on the current device"
     _ints(dev, 1, copies, copy_count)
     rc = _lib.qzo_copy_blocks((KvCacheDesc * len(caches))(*[c.desc for c in caches]), len(caches), copies.data_ptr(), copy_count.data_ptr(),
                               copies.numel() // 3, None if status is None else _status(dev, status), _raw_stream(dev))
