@@ -275,7 +275,7 @@ int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int B, int32_t
  *   d_scores_out float [B][W] (-inf),  d_lengths_out int32 [B][W] (0; may be NULL, has to be where d_lengths is).
  * Tokens that are not allowed have logits of -inf.  NaN and +inf logits count as -inf, and a beam with such a score or with a row from
  * n_rows on has no candidates; each sets bit 1 of the status word.  Sums of exponentials are fp32 per thread and fp64 from there, values and ranks fp64.
- * d_logits float [n_rows][ldl], ldl >= V (16-byte rows are read fastest); length_power from 0 to 8; W up to QZO_MAX_BEAMS.
+ * d_logits float [n_rows][ldl], ldl >= V (16-byte rows are read fastest); length_power from 0 to 8; W up to QZO_MAX_BEAMS, V up to 2^30.
  * The outputs may be the inputs of the same kind (tokens for last tokens); nothing else overlaps.
  * d_workspace: qzo_beam_select_workspace_bytes, 256-aligned; calls that may run at the same time need one each. */
 #define QZO_MAX_BEAMS 32
@@ -298,7 +298,7 @@ int qzo_beam_select(const float* d_logits, int64_t ldl, int n_rows, const int32_
  * d_free, d_free_count as for qzo_assign_slots; n_blocks: blocks of the pool, up to QZO_MAX_POOL_BLOCKS.  d_lens_out may be d_lens and
  * d_free_count_out may be d_free_count; no other arguments overlap (d_block_table_out is a table of its own).
  * When it cannot be served (too few free blocks, a stack beyond its capacity, a negative length or one beyond the table, a block
- * id outside the pool, a parent >= B), nothing is changed: tables, lengths and count are handed on as they are, no copies are listed, and bit 2 of
+ * id outside the pool among those that requests hold, a parent >= B), nothing is changed: tables, lengths and count are handed on as they are, no copies are listed, and bit 2 of
  * the status word is set.  B up to QZO_MAX_REQUESTS, table_width * block_size up to 2^30. */
 #define QZO_MAX_POOL_BLOCKS 524288
 int qzo_fork_requests(const int32_t* d_lens, const int32_t* d_parents, int B, const int32_t* d_block_table, int table_width, int block_size,
@@ -328,7 +328,7 @@ int qzo_copy_blocks(const qzo_kv_cache* h_caches, int n_caches, const int32_t* d
  * (int32 [n_groups + 1], ascending, from 0 to R at most; rows outside of all groups and groups without rows are allowed), have the
  * first d_prefix_len[i] tokens of request d_prefix_seq[i] (int32 [n_groups] each) as the first tokens of their own requests, which
  * may name the same blocks for them or hold copies.  Those keys and values are read once for a group and key head, not once for every row:
- * through the table of request d_prefix_seq[i], in whole runs of 64 tokens; what remains of them, and the rows' own tokens, through the
+ * through the table of request d_prefix_seq[i], in whole runs of 16 tokens; what remains of them, and the rows' own tokens, through the
  * rows' own tables.  A row that does not see the whole prefix reads everything through its own table, as does every row of a group whose
  * request or length is out of range (bit 1 of the status word).  Bounds that do not ascend within 0 .. R make no groups (bit 1 too).
  * Everything else as in qzo_paged_attention, the meaning of every output among it: the sums are those, taken in another order.  Bit 0 of the

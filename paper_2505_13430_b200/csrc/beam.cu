@@ -277,7 +277,7 @@ beam_pick_kernel(BeamParams p) {
   const double divisor = p.power == 0.0f ? 1.0 : p.power == 1.0f ? later : pow(later, (double)p.power);
   if (kind == kBeamEnded) {
     n = 1;
-    if (lane == 0) { value[w * W] = score; rank[w * W] = score / divisor; token[w * W] = p.end_token; }
+    if (lane == 0) { value[w * W] = score; rank[w * W] = score / divisor + 0.0; token[w * W] = p.end_token; }
   } else if (kind == kBeamGoesOn) {
     float top = ms.x;
 #pragma unroll
@@ -349,7 +349,7 @@ using namespace qzo;
 extern "C" {
 
 int qzo_beam_select_workspace_bytes(int B, int W, int V, size_t* bytes) {
-  if (!bytes || B <= 0 || W <= 0 || W > QZO_MAX_BEAMS || V <= 0 || (int64_t)B * W > INT32_MAX / 32) return QZO_ERR_BAD_ARG;
+  if (!bytes || B <= 0 || W <= 0 || W > QZO_MAX_BEAMS || V <= 0 || V > (1 << 30) || (int64_t)B * W > INT32_MAX / 32) return QZO_ERR_BAD_ARG;
   const int64_t lists = (int64_t)B * W * beam_chunks((int64_t)B * W, W, V);
   *bytes = align_up(lists * sizeof(float2)) + align_up(lists * W * sizeof(uint2));
   return QZO_OK;

@@ -125,7 +125,7 @@ def test_beam_select_refusals():
     qzo = _lib()
     need = qzo.qzo_beam_select_workspace_bytes(3, 4, 1000)
     assert 0 < need < qzo.qzo_beam_select_workspace_bytes(3, 4, 32000)
-    for args in ((0, 4, 10), (1, 0, 10), (1, 33, 10), (1, 4, 0), (1 << 24, 32, 10)):
+    for args in ((0, 4, 10), (1, 0, 10), (1, 33, 10), (1, 4, 0), (1 << 24, 32, 10), (1, 4, (1 << 30) + 1)):
         with pytest.raises(qzo.QzoError):
             qzo.qzo_beam_select_workspace_bytes(*args)
 
