@@ -935,7 +935,7 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
   plan.units = prefix_units(R, n_groups, G, Hkv, plan.items);
   if (plan.path == kManyPath) {
     plan.parts = plan.units + 2 * kSMs;
-    if (plan.units * (max_len / kPrefixTile + 2) > INT32_MAX) plan.path = kOwnTables;          // places of the line are counted in 32 bits
+    if (plan.units * (max_len / kPrefixTile + 2) > INT32_MAX / 2) plan.path = kOwnTables;      // places of the line are counted in 32 bits
   } else {
     // as attention_plan
     const int64_t slots = kSMs * resident_ctas(plan.items / 8);

@@ -82,7 +82,8 @@ struct PrefixGroup {
 
 // A group; without keys where its request or its length is out of range
 __device__ __forceinline__ PrefixGroup prefix_group(const PagedParams& p, int i, bool report = false) {
-  const int row0 = p.groups.rows[i], rows = p.groups.rows[i + 1] - row0, len = p.groups.len[i], seq = p.groups.seq[i];
+  const int row0 = p.groups.rows[i], end = p.groups.rows[i + 1], len = p.groups.len[i], seq = p.groups.seq[i];
+  const int rows = end < row0 ? -1 : end - row0;       // negative, as row0 < 0: no bounds (differences may wrap then)
   const bool bad = len < 0 || len > (p.width << p.log2_block) || (unsigned)seq >= (unsigned)p.n_seqs;
   if (bad && report && p.status) atomicOr(p.status, kStatusBadToken);
   const int prefix = bad ? 0 : len / kPrefixStep * kPrefixStep;

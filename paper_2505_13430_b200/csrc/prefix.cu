@@ -363,6 +363,9 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
   } else if (warp < kSoftmaxWarps) {
     const uint32_t my_lane = (uint32_t)(warp * 32) << 16;
     const float2 factor = make_float2(p.scale_log2e, p.scale_log2e);
+    // A zero that the compiler does not know: a packed product without it and the sum behind would become one operation that rounds once.
+    const float zero1 = __uint_as_float(__float_as_uint(p.scale_log2e) & 0x80000000u);
+    const float2 zero = make_float2(zero1, zero1);
     // The walk of a warp is in shared memory: inside a unit its registers are needed for the scores.
     Walk* const place = reinterpret_cast<Walk*>(smem + Plan::kOffWalks + 64 * warp);
     static_assert(sizeof(Walk) <= 64, "");
@@ -462,7 +465,8 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
 #pragma unroll
             for (int c = 0; c < 16; c += 2) {
               const uint32_t* const from = s + (kKeep ? c0 : c0 % 32) + c;
-              const float2 x = fma2(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), factor, less);
+              // Scores are rounded before the reference is taken off, as they are for the rows' own keys: what is equal there is equal here
+              const float2 x = add2(fma2(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), factor, zero), less);
               const float2 v = make_float2(fast_exp2(x.x), fast_exp2(x.y));
               sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], v);
               // the first term is the weight cut to bf16, the second what is left and 2^-20 of the weight: above zero, as the first is, for a

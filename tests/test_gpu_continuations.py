@@ -131,6 +131,11 @@ def test_large_and_small_logits(lib):
     _check_beams(lib, x, np.array([[0.0], [-1.0], [-2.0], [-3.0]], np.float32))
 
 
+def test_zeros_of_either_sign_are_one_rank(lib):
+    scores = np.array([[-0.0, 0.0, -1.0], [0.0, -0.0, -0.0]], np.float32)
+    _check_beams(lib, torch.zeros((6, 8), device="cuda"), scores, last=np.full((2, 3), 5, np.int32), end_token=5)
+
+
 def test_beams_in_place(lib):
     rng = _gen(5)
     B, W, V = 3, 4, 2000
@@ -449,6 +454,22 @@ def test_peaked_scores_over_a_shared_prefix(lib, units):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_large_scores_that_are_equal_in_a_prefix_and_behind_it(lib, units, kind):
+    # every key has the same score, which fp32 holds in steps of 2 and more: what is rounded of it has to be the same on either side
+    case = Shared([(4, 900, [60, 500, 1, 300]), (3, 200, 200)], 8, 2, 128, 16, kind, 38)
+    case.ck.zero_()
+    case.ck[..., 0] = 128.0
+    case.q[:] = 0.0
+    case.q[..., 0] = 2.0 ** 18 * 1.375
+    case.scale = 0.3
+    out = f64(case.run(lib))
+    want, spread = serving.paged_attention(f64(case.q), f64(case.ck) * case.ks, f64(case.cv) * case.vs, case.table, case.seqs, case.positions, case.scale)
+    # weights of one, which 16 bits hold; sums: two additions for every 16 keys, a join of up to 30 parts
+    allowed = BF16_STEP * np.abs(want) + ((2.0 ** -15 if kind == "bf16" else F16_STEP) + (64 + max(case.lens) / 4) * F32_STEP) * spread * (1 + BF16_STEP)
+    assert (np.abs(out - want) <= allowed).all(), (np.abs(out - want) / allowed).max()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 def test_leading_keys_of_no_value_in_a_prefix(lib, units, kind):
     # keys that lead and whose values are zero leave the row to the others, whose weights are 2^-10 to 2^-40 of theirs
     case = Shared([(4, 900, 60)], 8, 2, 64, 16, kind, 32)
@@ -491,7 +512,8 @@ def test_what_is_out_of_range_in_groups_is_reported(lib, units):
     n, width = case.table.shape
     for change in (dict(seq=[0, n, 2]), dict(seq=[-1, 1, 2]), dict(prefix=[500, -1, 300]), dict(prefix=[500, 200, width * 16 + 1])):
         case.check(case.run(lib, reported=2, **change))
-    for rows in ([0, 5, 3, 7], [-1, 3, 5, 7], [0, 3, 5, 8], [7, 5, 3, 0]):
+    low, high = -2 ** 31, 2 ** 31 - 1
+    for rows in ([0, 5, 3, 7], [-1, 3, 5, 7], [0, 3, 5, 8], [7, 5, 3, 0], [0, 3, low, 7], [high, low, 5, 7], [0, high, low, 7], [low, 3, 5, high]):
         case.check(case.run(lib, reported=2, rows=rows))
     # bounds that leave rows out, and groups that are smaller than what shares the prefix
     for rows, prefix in (([1, 3, 5, 7], case.prefix), ([0, 2, 2, 2], [500, 1, 1]), ([0, 3, 5, 5], [400, 200, 0]), ([3, 3, 5, 7], [0, 128, 300])):
