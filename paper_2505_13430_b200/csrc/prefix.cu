@@ -50,6 +50,11 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
+// 32 bytes, a whole sector
+__device__ __forceinline__ void store32(float* to, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" :: "l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+               "r"(v[6]), "r"(v[7]) : "memory");
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -88,8 +93,10 @@ __device__ __forceinline__ int find_stretch(const PagedParams& p, int cta, bool 
   const int lane = threadIdx.x & 31;
   int all = 0;
   bool bad = false;
+  PrefixGroup first = {};                              // of the first 32 groups this lane's
   for (int i = lane; i < p.groups.n; i += 32) {
     const PrefixGroup g = prefix_group(p, i, report);
+    if (i == lane) first = g;
     bad = bad || g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R;
     all += g.units(p.Hkv) * g.places();
   }
@@ -104,8 +111,8 @@ __device__ __forceinline__ int find_stretch(const PagedParams& p, int cta, bool 
   int places_before = 0, units_before = 0, tiles = 0;
   bool found = false;
   for (int i0 = 0; i0 < p.groups.n && places_before < to; i0 += 32) {
-    PrefixGroup g = {};
-    if (i0 + lane < p.groups.n) g = prefix_group(p, i0 + lane);
+    PrefixGroup g = first;
+    if (i0) g = i0 + lane < p.groups.n ? prefix_group(p, i0 + lane) : PrefixGroup{};
     const int units = g.units(p.Hkv), places = units * g.places();
     int sum = places, unit_sum = units;
 #pragma unroll
@@ -183,6 +190,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncwarp();
+  if (warp == kLoadWarp && lane < 4) prefetch_tmap(lane < 2 ? &maps.whole[lane] : &maps.step[lane - 2]);
   serving_begin();
   Walk start;
   const int n_tiles = find_stretch(p, blockIdx.x, blockIdx.x == 0 && warp == 0, &start);
@@ -254,11 +262,10 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       ++loaded;
     }
   };
-  if (warp == kLoadWarp) {                             // the first loads, ahead of everything else
+  if (warp == kLoadWarp) {                             // the first load, ahead of everything else
     box[0] = look_up(0);
     box[1] = look_up(1);
     load(box[0], &maps.whole[0], &maps.step[0], 0);
-    load_until(kRing);
   }
   const int mine = tid & (kM - 1);                     // a softmax thread's query of a tile
   // Rows that do not see the whole prefix take it with their own keys: -1
@@ -499,9 +506,8 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
           uint32_t o[32];
           tmem_ld32(tmem_o + my_lane + c, o);
           if (row >= 0) {
-            uint4* out = reinterpret_cast<uint4*>(p.prefix_o + part * DH + c);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) out[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            for (int e = 0; e < 32; e += 8) store32(p.prefix_o + part * DH + c + e, o + e);
           }
         }
         if (row >= 0) *reinterpret_cast<float2*>(p.prefix_ml + 2 * part) = make_float2(m == -INFINITY ? -INFINITY : ref, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
