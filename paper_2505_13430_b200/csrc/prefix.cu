@@ -29,12 +29,12 @@ struct PrefixPlan {
   static constexpr int kQueryBytes = kM * DH * 2, kSlotBytes = kTile * DH * 2, kRawBytes = kTile * DH;
   static constexpr int kSlots = (F8 ? 3 : 4) * 128 / DH, kRawSlots = F8 ? 3 * 128 / DH : 0;
   static constexpr int kOffSlots = kQueryBytes, kOffRaw = kOffSlots + kSlots * kSlotBytes, kOffBars = kOffRaw + kRawSlots * kRawBytes;
-  static constexpr int kBars = 2 * kSlots + 2 * kRawSlots + 8;
+  static constexpr int kBars = 2 * kSlots + 2 * kRawSlots + 10;
   static constexpr int kOffWalks = kOffBars + 8 * kBars, kOffThere = kOffWalks + kSoftmaxWarps * 64, kOffMisc = kOffThere + 4 * kThereRing;
   static constexpr int kDynamicBytes = kOffMisc + 16 + 1024;         // slack for the 1024-byte alignment
   static_assert(2 * (kDynamicBytes + 1024) <= 228 * 1024, "two CTAs to an SM");
-  static constexpr int kColSums = 0, kColScores = DH, kColWeights = DH + kTile;
-  static_assert(kColWeights + kTile <= kTmemCols, "tensor memory budget");
+  static constexpr int kColSums = 0, kColScores = DH;  // two tiles' scores
+  static_assert(kColScores + 2 * kTile <= kTmemCols, "tensor memory budget");
 };
 
 // Two fp32 operations in one instruction
@@ -145,11 +145,18 @@ __device__ __forceinline__ int find_stretch(const PagedParams& p, int cta, bool 
   return tiles;
 }
 
-// Two CTAs on every SM, each with its stretch of the line of tiles, unit after unit.  S = Q K^T goes to tensor memory; a thread of
-// the softmax warps takes a query's 64 scores into registers, upon which the next tile's product may overwrite them, and
-// writes their weights beside them, as the sum of two bf16 (2^-15 of a weight; one alone would leave 2^-8, as much as the output's
-// rounding), from where they enter O += P V as the A operand.  O stays in tensor memory; it is rescaled only when a maximum
-// passes the reference by 2^8.
+// Where the weights of a tile's keys c .. c + 15 are, their first or second terms: in the place of the scores of the 32 that they belong to
+__device__ __forceinline__ uint32_t weights_at(uint32_t scores, int j, int c, int part) {
+  return scores + kTile * (j & 1) + c / 32 * 32 + 16 * part + c % 32 / 2;
+}
+
+// Two CTAs on every SM, each with its stretch of the line of tiles, unit after unit.  S = Q K^T goes to tensor memory, to one of two places
+// in turn; a thread of the softmax warps takes a query's 64 scores into registers and writes their weights in their place, as the sum of two
+// bf16 (2^-15 of a weight; one alone would leave 2^-8, as much as the output's rounding), from where they enter O += P V as the A
+// operand; then the place is free for the scores of the tile after the next.  O stays in tensor memory; it is rescaled only when a maximum passes
+// the reference by 2^8.
+// A wait goes by the parity of a phase, so that a barrier must not be two phases ahead of whoever waits: scores j + 2 come after values j,
+// those after weights j, those after scores j have been read, and tiles in turn have barriers of their own.
 template <int DH, bool F8>
 __global__ void __launch_bounds__((PrefixPlan<DH, F8>::kThreads), 2)
 prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_constant__ PagedParams p, int64_t cache_rows, int box_rows) {
@@ -164,10 +171,12 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
   auto bar_raw_full = [&](int s) { return bar0 + 8u * (2 * kSlots + s); };       // the same of the tiles as they are stored
   auto bar_raw_empty = [&](int s) { return bar0 + 8u * (2 * kSlots + kRawSlots + s); };
   constexpr int kRest = 2 * kSlots + 2 * kRawSlots;
-  // of a tile, one phase each: its scores are there, have been taken into registers, its weights are there, are in the sums; of a unit: its
-  // queries are there, its sums have been read; the end after a failed wait
-  const uint32_t bar_scores = bar0 + 8u * kRest, bar_taken = bar_scores + 8u, bar_weights = bar_scores + 16u, bar_values = bar_scores + 24u;
-  const uint32_t bar_queries = bar_scores + 32u, bar_read = bar_scores + 40u, bar_drain = bar_scores + 48u;   // (two)
+  // of a tile, by its place's parity: its scores are there, its weights are there, are in the sums; of a unit: its queries are there, its
+  // sums have been read; the end after a failed wait
+  auto bar_scores = [&](int j) { return bar0 + 8u * (kRest + (j & 1)); };
+  auto bar_weights = [&](int j) { return bar0 + 8u * (kRest + 2 + (j & 1)); };
+  auto bar_values = [&](int j) { return bar0 + 8u * (kRest + 4 + (j & 1)); };
+  const uint32_t bar_queries = bar0 + 8u * (kRest + 6), bar_read = bar_queries + 8u, bar_drain = bar_queries + 16u;   // (two)
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + Plan::kOffMisc);
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(smem + Plan::kOffMisc + 4);
   volatile int* const never_set = reinterpret_cast<volatile int*>(smem + Plan::kOffMisc + 8);
@@ -179,10 +188,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
     *never_set = 0;
     for (int s = 0; s < kSlots; ++s) { mbar_init(bar_full(s), F8 ? kConvertWarps : 1); mbar_init(bar_empty(s), 1); }
     for (int s = 0; s < kRawSlots; ++s) { mbar_init(bar_raw_full(s), 1); mbar_init(bar_raw_empty(s), kConvertWarps); }
-    mbar_init(bar_scores, 2);
-    mbar_init(bar_taken, kSoftmaxWarps);
-    mbar_init(bar_weights, kSoftmaxWarps);
-    mbar_init(bar_values, 1);
+    for (int j = 0; j < 2; ++j) { mbar_init(bar_scores(j), 2); mbar_init(bar_weights(j), kSoftmaxWarps); mbar_init(bar_values(j), 1); }
     mbar_init(bar_queries, kSoftmaxWarps);
     mbar_init(bar_read, kSoftmaxWarps);
     mbar_init(bar_drain, 1);
@@ -302,7 +308,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
   tcgen05_fence_before();
   __syncthreads();
   tcgen05_fence_after();
-  const uint32_t tmem = *tmem_slot, tmem_s = tmem + Plan::kColScores, tmem_w = tmem + Plan::kColWeights, tmem_o = tmem + Plan::kColSums;
+  const uint32_t tmem = *tmem_slot, tmem_s = tmem + Plan::kColScores, tmem_o = tmem + Plan::kColSums;
 
   if (warp == kLoadWarp) {
     load_until(INT32_MAX);
@@ -318,7 +324,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
     if (warp == kScoreWarp) {
       for (int j = 0; j < n_tiles; ++j) {
         const int load = j < 2 ? j : 2 * j - 1, slot = load % kSlots;            // the tile's place among the loads
-        ok = wait(bar_full(slot), load / kSlots) && (j == 0 || wait(bar_taken, j - 1)) && (!first || wait(bar_queries, unit));
+        ok = wait(bar_full(slot), load / kSlots) && (j < 2 || wait(bar_values(j), (j - 2) >> 1)) && (!first || wait(bar_queries, unit));
         if (!ok) break;
         tcgen05_fence_after();
         const uint64_t q = umma_desc_k_major_sw128(base), k = umma_desc_k_major_sw128(slots + slot * Plan::kSlotBytes);
@@ -327,10 +333,10 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
           for (int h = 0; h < kHalves; ++h)
 #pragma unroll
             for (int e = 0; e < 4; ++e)                // a descriptor's address counts in 16 bytes
-              umma_bf16(tmem_s, q + h * (kM * 128 / 16) + 2 * e, k + h * (kTile * 128 / 16) + 2 * e, kIdescS, h + e > 0);
+              umma_bf16(tmem_s + kTile * (j & 1), q + h * (kM * 128 / 16) + 2 * e, k + h * (kTile * 128 / 16) + 2 * e, kIdescS, h + e > 0);
           umma_commit(bar_empty(slot));
-          umma_commit(bar_scores);
-          mbar_arrive(bar_scores);                     // hands on what the load warp wrote of the tile
+          umma_commit(bar_scores(j));
+          mbar_arrive(bar_scores(j));                     // hands on what the load warp wrote of the tile
         }
         __syncwarp();
         first = w.at_end();
@@ -340,7 +346,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
     } else {
       for (int j = 0; j < n_tiles; ++j) {
         const int load = j + 1 < n_tiles ? 2 * j + 2 : 2 * n_tiles - 1, slot = load % kSlots;
-        ok = wait(bar_full(slot), load / kSlots) && wait(bar_weights, j) && (!first || unit == 0 || wait(bar_read, unit - 1));
+        ok = wait(bar_full(slot), load / kSlots) && wait(bar_weights(j), j >> 1) && (!first || unit == 0 || wait(bar_read, unit - 1));
         if (!ok) break;
         tcgen05_fence_after();
         const uint64_t v = umma_desc_mn_major_sw128(slots + slot * Plan::kSlotBytes, kTile * 128);
@@ -349,9 +355,9 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
 #pragma unroll
           for (int part = 0; part < 2; ++part)
 #pragma unroll
-            for (int e = 0; e < kTile / 16; ++e) umma_bf16_tmem_a(tmem_o, tmem_w + kTile / 2 * part + 8 * e, v + e * (2048 / 16), kIdescO, part + e > 0 ? 1 : add);
+            for (int e = 0; e < kTile / 16; ++e) umma_bf16_tmem_a(tmem_o, weights_at(tmem_s, j, 16 * e, part), v + e * (2048 / 16), kIdescO, part + e > 0 ? 1 : add);
           umma_commit(bar_empty(slot));
-          umma_commit(bar_values);
+          umma_commit(bar_values(j));
         }
         __syncwarp();
         first = w.at_end();
@@ -403,7 +409,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       float m = -INFINITY, ref = 0.0f;
       float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
       for (int i = 0; i < count; ++i, ++j) {
-        wait(bar_scores, j);
+        wait(bar_scores(j), j >> 1);
         const bool ask = i + 1 == count && more;
         const uint32_t there = there_ring[j % kThereRing];
         constexpr uint32_t kAll = (1u << kTile / kPrefixStep) - 1;
@@ -412,7 +418,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
         uint32_t s[kKeep ? kTile : kTile / 2];
         auto fetch = [&](int half) {
           uint32_t* const to = s + (kKeep ? 32 * half : 0);
-          tmem_ld32(tmem_s + my_lane + 32 * half, to);
+          tmem_ld32(tmem_s + kTile * (j & 1) + my_lane + 32 * half, to);
           if (there != kAll) {                         // keys behind the prefix and of blocks out of range: nothing
 #pragma unroll
             for (int c = 0; c < 32; ++c)
@@ -431,10 +437,6 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
               most[1] = max3(most[1], __uint_as_float(from[c + 2]), __uint_as_float(from[c + 3]));
             }
           }
-          if (kKeep) {
-            tcgen05_fence_before();
-            hand_over(bar_taken);
-          }
           if (ask) ask_queries(unit_after(), next_row);
           const float top = fmaxf(most[0], most[1]) * p.scale_log2e;
           const bool raise = m == -INFINITY ? top > -INFINITY : top > ref + kSlack;
@@ -447,7 +449,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
               for (int e = 0; e < 2; ++e) sum[e] = make_float2(sum[e].x * by, sum[e].y * by);
             }
             if (i > 0) {                               // O holds the unit's tiles before this one, once their product is done
-              wait(bar_values, j - 1);
+              wait(bar_values(j - 1), (j - 1) >> 1);
 #pragma unroll 1
               for (int c = 0; c < DH; c += 16) {
                 uint32_t o[16];
@@ -461,13 +463,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
           const float2 less = make_float2(-ref, -ref), up = make_float2(1.0f + 0x1p-20f, 1.0f + 0x1p-20f);
 #pragma unroll
           for (int c0 = 0; c0 < kTile; c0 += 16) {
-            if (!kKeep && c0 % 32 == 0) {
-              fetch(c0 / 32);
-              if (c0 > 0) {
-                tcgen05_fence_before();
-                hand_over(bar_taken);
-              }
-            }
+            if (!kKeep && c0 % 32 == 0) fetch(c0 / 32);
             uint32_t hi[8], lo[8];
 #pragma unroll
             for (int c = 0; c < 16; c += 2) {
@@ -483,22 +479,19 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
               const float2 rest = fma2(v, up, make_float2(__uint_as_float((a & 0xffff0000u) ^ 0x80000000u), __uint_as_float((b & 0xffff0000u) ^ 0x80000000u)));
               lo[c / 2] = pack_bf16x2(rest.x, rest.y);
             }
-            if (c0 == 0 && j > 0) wait(bar_values, j - 1);       // the weights before these have been used
-            tmem_st8(tmem_w + my_lane + c0 / 2, hi);
-            tmem_st8(tmem_w + my_lane + kTile / 2 + c0 / 2, lo);
+            tmem_st8(weights_at(tmem_s + my_lane, j, c0, 0), hi);
+            tmem_st8(weights_at(tmem_s + my_lane, j, c0, 1), lo);
           }
           tmem_wait_st();
-        } else {
-          hand_over(bar_taken);
-          if (ask) ask_queries(unit_after(), next_row);
-          if (j > 0) wait(bar_values, j - 1);
+        } else if (ask) {
+          ask_queries(unit_after(), next_row);
         }
         tcgen05_fence_before();
-        hand_over(bar_weights);
+        hand_over(bar_weights(j));
         if (ask) queries_there();
       }
       // the unit's sums leave tensor memory
-      wait(bar_values, j - 1);
+      wait(bar_values(j - 1), (j - 1) >> 1);
       const size_t part = (size_t)(blockIdx.x + number) * p.unit_items + mine;
       if (active) {
 #pragma unroll 1
