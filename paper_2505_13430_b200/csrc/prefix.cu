@@ -198,6 +198,7 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
   __syncwarp();
   if (warp == kLoadWarp && lane < 4) prefetch_tmap(lane < 2 ? &maps.whole[lane] : &maps.step[lane - 2]);
   serving_begin();
+  serving_next();                                      // for the rows' own keys
   Walk start;
   const int n_tiles = find_stretch(p, blockIdx.x, blockIdx.x == 0 && warp == 0, &start);
   if (n_tiles == 0) return;
@@ -558,7 +559,6 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
     if (!ok) *abort_flag = 1;
   }
 
-  serving_next();
   if (!ok && p.status) atomicOr(p.status, kStatusTimeout);
   tcgen05_fence_before();
   __syncthreads();

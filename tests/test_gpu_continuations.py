@@ -446,6 +446,19 @@ def test_long_runs_of_tiles(lib, units, kind, dh, rising):
         assert torch.equal(out.view(torch.int16), case.run(lib).view(torch.int16))
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+def test_every_code_of_8_bit_pages(lib, units, dh):
+    # a dimension has one code in all keys, so that a row's result is that code's value: the weights' roundings leave less than half a bf16 step of it
+    for first in range(0, 256, dh):
+        case = Shared([(5, 200, [1, 3, 60, 7, 1])], 8, 4, dh, 16, "e4m3", 39)
+        codes = torch.arange(first, first + dh, dtype=torch.uint8)
+        case.cv.view(torch.uint8)[:] = codes.cuda()
+        out = case.run(lib)
+        want = codes.view(torch.float8_e4m3fn).float() * case.vs
+        assert torch.equal(torch.isnan(out.cpu()), torch.isnan(want).expand(out.shape))
+        assert torch.equal(torch.nan_to_num(out.cpu().float()), torch.nan_to_num(want).expand(out.shape))
+
+
 def test_peaked_scores_over_a_shared_prefix(lib, units):
     case = Shared([(5, 1500, 100), (4, 300, 3)], 8, 2, 128, 16, "bf16", 31, q_std=12.0)
     case.check(case.run(lib))
