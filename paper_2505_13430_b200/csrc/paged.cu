@@ -926,15 +926,16 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
   const int few_items = queries <= 8 ? 8 : 16;
   // The way whose time is estimated as the shortest, in us: what it takes beside the keys and values, and the bytes of those that its CTAs
   // ask for.  The rates are those of measurements with 4 to 128 rows in 1 to 16 groups over 4 to 32 key heads of 128 and 256 to 16384 shared
-  // tokens, bf16 (e4m3); most of the rows' own requests are met by L2, and e4m3 tiles are held up by their conversion in the kernel for many
-  // queries.  Examples, us through own tables, few, many: 64 rows of 64 queries on 2048 138, 30, 42, on 16384 1045, 143, 84; 128 rows of 1024 queries
-  // on 16384 275, 238, 72 (203, 159, 103); 32 rows of 128 queries on 8192 95, 45, 39 (68, 34, 42); 64 rows on 16 prefixes of 256 33, 22, 49.
+  // tokens, bf16 (e4m3); most of the rows' own requests are met by L2 where there are many, and e4m3 tiles are held up by their conversion in
+  // the kernel for many queries.  Examples, us through own tables, few, many: 64 rows of 64 queries on 2048 139, 28, 26, on 16384 1033, 139, 62;
+  // 128 rows of 1024 queries on 16384 275, 231, 67 (203, 156, 104); 32 rows of 128 queries on 8192 90, 46, 31 (67, 31, 33).
   // Lengths are known on the device only: all of this goes by the table's width.
   const double bytes = (double)max_len * dh * (f8 ? 2 : 4);           // of a key head
-  const double own = 4 + (double)R * Hkv * bytes / (f8 ? 11e6 : 14.5e6);
+  const double asked = (double)R * Hkv * bytes;
+  const double own = std::min(3 + asked / (f8 ? 7e6 : 10.5e6), 12 + asked / (f8 ? 11.3e6 : 15.7e6));
   const double rows = R * (double)Hkv / 400;           // the rows' own keys: a CTA for each row and key head
-  const double few = 9 + rows + (double)prefix_units(R, n_groups, G, Hkv, few_items) * bytes / (f8 ? 6.5e6 : 7.6e6);
-  const double many = (f8 ? 37 : 25) + rows + (double)prefix_units(R, n_groups, G, Hkv, kPrefixQueries) * bytes / (f8 ? 2e6 : 6.3e6);
+  const double few = 8 + rows + (double)prefix_units(R, n_groups, G, Hkv, few_items) * bytes / (f8 ? 7e6 : 8.3e6);
+  const double many = (f8 ? 23 : 21) + rows + (double)prefix_units(R, n_groups, G, Hkv, kPrefixQueries) * bytes / (f8 ? 1.8e6 : 6.2e6);
   plan.path = forced != kByRule ? (PrefixPath)forced : own <= std::min(few, many) ? kOwnTables : few <= many ? kFewPath : kManyPath;
   if (plan.path == kOwnTables) return plan;
   plan.items = plan.path == kManyPath ? kPrefixQueries : few_items;
