@@ -3,6 +3,7 @@
 #include "qzo_common.cuh"
 #include "launch.cuh"
 
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -93,7 +94,8 @@ __global__ void __launch_bounds__(kScanThreads)
 beam_scan_kernel(BeamParams p) {
   __shared__ uint2 lists[kScanWarps][32];
   __shared__ float2 warp_sums[kScanWarps];
-  __shared__ uint2 found[kScanWarps][32 * kLaneValues];              // candidates of a tile
+  __shared__ float4 values[kScanWarps][kLaneValues / 4][32];         // a tile's logits, where there are candidates among them
+  __shared__ uint16_t found[kScanWarps][32 * kLaneValues];           // the candidates: number of the thread's logit, lane
   __shared__ volatile uint32_t reached[kScanWarps];    // order of a logit that ceil(W / 8) of a warp's lanes have reached
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int beam = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
@@ -176,11 +178,13 @@ beam_scan_kernel(BeamParams p) {
     if (base == t0) __syncthreads();                   // later, what another warp has not written yet is lower than it might be, no more
     else __syncwarp();
     const uint32_t floor = max(least_order, __reduce_min_sync(0xffffffffu, reached[lane % kScanWarps]));     // logits of a lower order are no candidates
-    const float low = of_order(floor);                 // -infinity: everything above it
-    if (!__any_sync(0xffffffffu, most >= low && most > -INFINITY)) continue;
+    const float low = fmaxf(of_order(floor), -FLT_MAX);
+    if (!__any_sync(0xffffffffu, most >= low)) continue;
     unsigned hits = 0;                                 // of this lane's logits
 #pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) hits |= (v[i] >= low && v[i] > -INFINITY ? 1u : 0u) << i;
+    for (int i = 0; i < kLaneValues; ++i) hits |= v[i] >= low ? 1u << i : 0u;
+#pragma unroll
+    for (int i = 0; i < kLaneValues; i += 4) values[warp][i / 4][lane] = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
     int n = __popc(hits);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -188,16 +192,15 @@ beam_scan_kernel(BeamParams p) {
       if (lane >= d) n += up;
     }
     const int all = __shfl_sync(0xffffffffu, n, 31);
-    for (n -= __popc(hits); hits; hits &= hits - 1, ++n) {
-      const int i = __ffs(hits) - 1;
-      float value = v[0];
-#pragma unroll
-      for (int e = 1; e < kLaneValues; ++e) value = i == e ? v[e] : value;
-      found[warp][n] = make_uint2(order_of(value + 0.0f), (uint32_t)token_of(base, i));          // -0 and +0 are one value
-    }
+    for (n -= __popc(hits); hits; hits &= hits - 1, ++n) found[warp][n] = (uint16_t)((__ffs(hits) - 1) * 32 + lane);
     __syncwarp();
     for (int c0 = 0; c0 < all; c0 += 32) {
-      const uint2 mine = c0 + lane < all ? found[warp][c0 + lane] : make_uint2(0u, 0u);
+      uint2 mine = make_uint2(0u, 0u);
+      if (c0 + lane < all) {
+        const int at = found[warp][c0 + lane], i = at / 32, who = at % 32;
+        const float value = reinterpret_cast<const float*>(&values[warp][i / 4][who])[i % 4];
+        mine = make_uint2(order_of(value + 0.0f), (uint32_t)(token_of(base, i) + (who - lane) * (VEC ? 4 : 1)));       // -0 and +0 are one value
+      }
       auto passes = [&]() { return mine.x > least_order || (mine.x == least_order && mine.y < least_token); };
       for (unsigned left = __ballot_sync(0xffffffffu, passes() && mine.x > kNone); left;) {
         const int who = __ffs(left) - 1;
