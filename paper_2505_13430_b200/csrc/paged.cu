@@ -860,9 +860,9 @@ int run_groups(const PagedParams& p, const qzo_kv_cache& c, int64_t units, bool 
   if (!p.prefix_splits) QZO_TRY(launch_prefix_attention(p, c, st));
   else if (p.unit_items == 8) QZO_TRY((run_attention_w<DH, 1, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
   else QZO_TRY((run_attention_w<DH, 2, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
-  // Own keys are few as a rule: CTAs of one warp, twelve on an SM, where there are enough rows and key heads (64 rows on 16 prefixes, 32 key
-  // heads, 1 to 64 own keys: 72.0 us in all, 78.7 with four warps; 1 to 400 own keys: 124.6 and 120.0), but not where several heads have
-  // many parts to join (128 rows of 8 heads, ten parts: 83.9 us and 73.7).
+  // Own keys are few as a rule: CTAs of one warp, twelve on an SM, where there are enough rows and key heads (64 rows on one prefix of 4096, 32
+  // key heads, 1 to 32 own keys: 42.1 us in all, 53.9 with four warps), but not where several heads have many parts to join (128 rows of
+  // 8 heads to a key head on 16384, ten parts: 71.8 us and 66.6).
   const int64_t ctas = (int64_t)p.R * p.Hkv * p.chunks, parts = p.prefix_splits ? p.prefix_splits : p.prefix_ctas / units + 1;
   if (ctas < 3 * kSMs || parts * std::min(p.G, 16) >= 32) QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
   else if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 1, Keys::kOwn>(p, ctas, p.splits, st)));
