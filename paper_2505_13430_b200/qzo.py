@@ -628,7 +628,7 @@ def qzo_fork_requests(lens, parents, block_table, free, free_count, block_size, 
         _ints(dev, 1, table_out)
     if lens_out is None and free_count_out is None and copies is None and copy_count is None:       # one allocation for all of them
         made = lens.new_empty(4 * B + 2)
-        lens_out, copies, free_count_out, copy_count = made.split((B, 3 * B, 1, 1))
+        lens_out, copies, free_count_out, copy_count = made.split_with_sizes((B, 3 * B, 1, 1))
         copies = copies.view(B, 3)
         at = made.data_ptr()
         lens_at, copies_at, free_count_at, count_at = at, at + 4 * B, at + 16 * B, at + 16 * B + 4
