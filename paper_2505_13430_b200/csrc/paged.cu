@@ -928,14 +928,16 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
   // ask for.  The rates are those of measurements with 4 to 128 rows in 1 to 16 groups over 4 to 32 key heads of 128 and 256 to 16384 shared
   // tokens, bf16 (e4m3); most of the rows' own requests are met by L2 where there are many, and e4m3 tiles are held up by their conversion in
   // the kernel for many queries.  Examples, us through own tables, few, many: 64 rows of 64 queries on 2048 139, 28, 26, on 16384 1033, 139, 62;
-  // 128 rows of 1024 queries on 16384 275, 231, 67 (203, 156, 104); 32 rows of 128 queries on 8192 90, 46, 31 (67, 31, 33).
+  // 128 rows of 1024 queries on 16384 275, 231, 67 (203, 156, 89); 32 rows of 128 queries on 8192 90, 46, 31 (67, 31, 33).
   // Lengths are known on the device only: all of this goes by the table's width.
   const double bytes = (double)max_len * dh * (f8 ? 2 : 4);           // of a key head
   const double asked = (double)R * Hkv * bytes;
   const double own = std::min(3 + asked / (f8 ? 7e6 : 10.5e6), 12 + asked / (f8 ? 11.3e6 : 15.7e6));
   const double rows = R * (double)Hkv / 400;           // the rows' own keys: a CTA for each row and key head
-  const double few = 8 + rows + (double)prefix_units(R, n_groups, G, Hkv, few_items) * bytes / (f8 ? 7e6 : 8.3e6);
-  const double many = (f8 ? 23 : 21) + rows + (double)prefix_units(R, n_groups, G, Hkv, kPrefixQueries) * bytes / (f8 ? 1.8e6 : 6.2e6);
+  const double asked_few = (double)prefix_units(R, n_groups, G, Hkv, few_items) * bytes;
+  const double asked_many = std::min(R, n_groups) * std::max(1.0, (double)queries / kPrefixQueries) * Hkv * bytes;   // a unit that is not full costs less
+  const double few = rows + (f8 ? std::min(9.5 + asked_few / 5.7e6, 25 + asked_few / 8.1e6) : 8 + asked_few / 8.3e6);
+  const double many = rows + (f8 ? std::min(20 + asked_many / 1.25e6, 27 + asked_many / 2.4e6) : 21 + asked_many / 6.2e6);
   plan.path = forced != kByRule ? (PrefixPath)forced : own <= std::min(few, many) ? kOwnTables : few <= many ? kFewPath : kManyPath;
   if (plan.path == kOwnTables) return plan;
   plan.items = plan.path == kManyPath ? kPrefixQueries : few_items;

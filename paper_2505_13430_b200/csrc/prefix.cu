@@ -16,7 +16,7 @@ namespace qzo {
 namespace {
 
 constexpr int kM = kPrefixQueries, kTile = kPrefixTile;
-constexpr int kSoftmaxWarps = 4, kLoadWarp = 4, kScoreWarp = 5, kValueWarp = 6, kFirstConvertWarp = 7, kConvertWarps = 4;
+constexpr int kSoftmaxWarps = 4, kLoadWarp = 4, kScoreWarp = 5, kValueWarp = 6, kFirstConvertWarp = 7, kConvertWarps = 4, kTileWarps = 2;       // of the converters, for a tile
 constexpr int kTmemCols = 256;                         // two CTAs to an SM
 constexpr int kThereRing = 8;                          // tiles whose masks are kept: more than the rings hold
 constexpr float kSlack = 8.0f;                         // by which scores may pass the reference before it is raised
@@ -158,7 +158,7 @@ __device__ __forceinline__ uint32_t weights_at(uint32_t scores, int j, int c, in
 // Bound by the chain of a tile: 2350 cycles for the two tiles of an SM's CTAs, of which the tensor pipe is busy 1790 (8 x 48 for Q K^T, 8 x 64 for
 // P V with its two terms, for each) and the exponentials' pipe 1024; with start (5 us) and end 128 rows of 8 heads to each of 4 key heads on
 // 2 prefixes of 16384 take 58 us of the call's 68.  One place for the scores and another for the weights took 0.9 us more, tiles of 128 keys with
-// one CTA on an SM 30 us more, eight softmax warps 8 us more.  e4m3 pages are bound by issue slots: 3900 cycles.
+// one CTA on an SM 30 us more, eight softmax warps 8 us more.  e4m3 pages are bound by their conversion, 3300 cycles.
 // A wait goes by the parity of a phase, so that a barrier must not be two phases ahead of whoever waits: scores j + 2 come after values j,
 // those after weights j, those after scores j have been read, and tiles in turn have barriers of their own.
 template <int DH, bool F8>
@@ -190,8 +190,8 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
   if (tid == kLoadWarp * 32) {
     *abort_flag = 0;
     *never_set = 0;
-    for (int s = 0; s < kSlots; ++s) { mbar_init(bar_full(s), F8 ? kConvertWarps : 1); mbar_init(bar_empty(s), 1); }
-    for (int s = 0; s < kRawSlots; ++s) { mbar_init(bar_raw_full(s), 1); mbar_init(bar_raw_empty(s), kConvertWarps); }
+    for (int s = 0; s < kSlots; ++s) { mbar_init(bar_full(s), F8 ? kTileWarps : 1); mbar_init(bar_empty(s), 1); }
+    for (int s = 0; s < kRawSlots; ++s) { mbar_init(bar_raw_full(s), 1); mbar_init(bar_raw_empty(s), kTileWarps); }
     for (int j = 0; j < 2; ++j) { mbar_init(bar_scores(j), 2); mbar_init(bar_weights(j), kSoftmaxWarps); mbar_init(bar_values(j), 1); }
     mbar_init(bar_queries, kSoftmaxWarps);
     mbar_init(bar_read, kSoftmaxWarps);
@@ -351,7 +351,8 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
     } else {
       for (int j = 0; j < n_tiles; ++j) {
         const int load = j + 1 < n_tiles ? 2 * j + 2 : 2 * n_tiles - 1, slot = load % kSlots;
-        ok = wait(bar_full(slot), load / kSlots) && wait(bar_weights(j), j >> 1) && (!first || unit == 0 || wait(bar_read, unit - 1));
+        // the weights first: with three slots the load before this one in its slot is this tile's keys, which have been used then
+        ok = wait(bar_weights(j), j >> 1) && wait(bar_full(slot), load / kSlots) && (!first || unit == 0 || wait(bar_read, unit - 1));
         if (!ok) break;
         tcgen05_fence_after();
         const uint64_t v = umma_desc_mn_major_sw128(slots + slot * Plan::kSlotBytes, kTile * 128);
@@ -519,19 +520,27 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       row = next_row;
     }
   } else if (F8 && warp >= kFirstConvertWarp) {
-    // converters: a tile's codes to bf16 (exact), into the swizzled layout of the products
-    const int c0 = tid - kFirstConvertWarp * 32;
-    Ring raw;
-    for (int i = 0; i < 2 * n_tiles; ++i) {
-      if (!__all_sync(0xffffffffu, mbar_wait_likely(bar_raw_full(raw.s), raw.ph, abort_flag, limit) && mbar_wait(bar_empty(ring.s), ring.ph ^ 1u, abort_flag, limit))) {
-        ok = false;
-        break;
+    // Converters: a tile's codes to bf16 (exact), into the swizzled layout of the products.  Two warps have the even loads and two the odd
+    // ones: a tile is mostly waiting and latency (128 rows on 16384 tokens, 4 key heads: 104 us when all four had every tile, now 89).  They
+    // meet behind every two loads: by then the slots in front of these two have been found free, so that no phase that is waited for
+    // next is two ahead, and none behind it can be complete before its load has been converted.  That the load before in a slot has landed
+    // follows from its being free.  After a failed wait a warp goes on through the loop, so that the others are not left alone.
+    static_assert(!F8 || (kRawSlots == kSlots && kConvertWarps == 2 * kTileWarps), "");
+    const int number = warp - kFirstConvertWarp, c0 = number % kTileWarps * 32 + lane;
+    for (int i = number / kTileWarps; i < 2 * n_tiles; i += 2) {
+      const int slot = i % kSlots;
+      const uint32_t phase = (uint32_t)(i / kSlots) & 1u;
+      if (i > 1) named_bar_sync(1, kConvertWarps * 32);
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_likely(bar_empty(slot), phase ^ 1u, abort_flag, limit) && mbar_wait_likely(bar_raw_full(slot), phase, abort_flag, limit));
+      if (!ok) {
+        *abort_flag = 1;
+        continue;
       }
-      const uint32_t src = raws + raw.s * Plan::kRawBytes;
-      uint8_t* const dst = smem + Plan::kOffSlots + ring.s * Plan::kSlotBytes;
+      const uint32_t src = raws + slot * Plan::kRawBytes;
+      uint8_t* const dst = smem + Plan::kOffSlots + slot * Plan::kSlotBytes;
       constexpr int kUnits = kTile * DH / 16, kRowUnits = DH / 16;
 #pragma unroll 4
-      for (int u = c0; u < kUnits; u += kConvertWarps * 32) {
+      for (int u = c0; u < kUnits; u += kTileWarps * 32) {
         const int r = u / kRowUnits, c = u % kRowUnits, h = c >> 2;
         const uint4 raw16 = lds16(src + 16 * u);
         const uint32_t codes[4] = {raw16.x, raw16.y, raw16.z, raw16.w};
@@ -554,13 +563,10 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(bar_full(ring.s));
-        mbar_arrive(bar_raw_empty(raw.s));
+        mbar_arrive(bar_full(slot));
+        mbar_arrive(bar_raw_empty(slot));
       }
-      raw.next(kRing);
-      ring.next(kSlots);
     }
-    if (!ok) *abort_flag = 1;
   }
 
   if (!ok && p.status) atomicOr(p.status, kStatusTimeout);
