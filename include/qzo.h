@@ -333,16 +333,16 @@ int qzo_copy_blocks(const qzo_kv_cache* h_caches, int n_caches, const int32_t* d
  * request or length is out of range (bit 1 of the status word).  Bounds that do not ascend within 0 .. R make no groups (bit 1 too).
  * Everything else as in qzo_paged_attention, the meaning of every output among it: the sums are those, taken in another order.  Bit 0 of the
  * status word: a bounded wait inside a kernel ran out, and the output means nothing.
- * n_blocks * block_size * n_kv_heads < 2^31.  d_workspace: qzo_shared_prefix_attention_workspace_bytes, 256-aligned.
+ * n_blocks * block_size * n_kv_heads < 2^31, n_groups up to 2^20.  d_workspace: qzo_shared_prefix_attention_workspace_bytes, 256-aligned.
  * Where little is shared, every row reads all of its keys through its own table, as in qzo_paged_attention (indices of groups are not looked at then). */
-/* For tests: how later calls of this process take prefixes, whatever their sizes.  0: as measured best (the default), 1: every row through its
- * own table, 2: in units of few queries, 3: in units of 128.  The workspace's size goes by it too. */
-int qzo_debug_prefix_path(int path);
 int qzo_shared_prefix_attention_workspace_bytes(int R, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes);
 int qzo_shared_prefix_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache, const int32_t* d_block_table, int n_seqs, int table_width,
                                 const int32_t* d_row_seq, const int32_t* d_positions, const int32_t* d_group_rows, const int32_t* d_prefix_seq,
                                 const int32_t* d_prefix_len, int n_groups, float scale, void* d_out_bf16, int ldo, int R, int n_heads,
                                 void* d_workspace, size_t workspace_bytes, int* d_status, void* stream);
+/* For tests: how later calls of this process take prefixes, whatever their sizes.  0: as measured best (the default), 1: every row through its
+ * own table, 2: in units of few queries, 3: in units of 128.  The workspace's size goes by it too. */
+int qzo_debug_prefix_path(int path);
 
 /* ------------------------------------------------------------------------------------
  * Model-level entry points

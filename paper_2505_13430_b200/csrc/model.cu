@@ -916,7 +916,7 @@ int qzo_decode_groups(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t*
                       int table_width, const int32_t* d_group_rows, const int32_t* d_prefix_seq, const int32_t* d_prefix_len, int n_groups,
                       float* d_logits) {
   if (!d_tokens || !d_row_seq || !d_positions || !d_slots || !d_block_table) return QZO_ERR_BAD_ARG;
-  if (!d_group_rows || !d_prefix_seq || !d_prefix_len || n_groups <= 0) return QZO_ERR_BAD_ARG;
+  if (!d_group_rows || !d_prefix_seq || !d_prefix_len || n_groups <= 0 || n_groups > kMostGroups) return QZO_ERR_BAD_ARG;
   if (!words_aligned(d_tokens, d_row_seq, d_positions, d_slots, d_block_table, d_group_rows, d_prefix_seq, d_prefix_len)) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_decode(m, h_caches, R, n_seqs, table_width, d_logits));
   for (int li = 0; li < m->desc.n_layers; ++li)      // rows that a tensor map can name

@@ -1098,7 +1098,7 @@ int qzo_debug_prefix_path(int path) {
 }
 
 int qzo_shared_prefix_attention_workspace_bytes(int R, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes) {
-  if (!bytes || R <= 0 || n_groups <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || max_len > kMostKeys) return QZO_ERR_BAD_ARG;
+  if (!bytes || R <= 0 || n_groups <= 0 || n_groups > kMostGroups || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || max_len > kMostKeys) return QZO_ERR_BAD_ARG;
   if (head_dim != 64 && head_dim != 128) return QZO_ERR_BAD_ARG;
   *bytes = shared_prefix_bytes(R, n_groups, n_heads, n_kv_heads, head_dim, max_len);
   return QZO_OK;
@@ -1108,7 +1108,7 @@ int qzo_shared_prefix_attention(const void* d_q_bf16, int ldq, const qzo_kv_cach
                                 const int32_t* d_row_seq, const int32_t* d_positions, const int32_t* d_group_rows, const int32_t* d_prefix_seq,
                                 const int32_t* d_prefix_len, int n_groups, float scale, void* d_out_bf16, int ldo, int R, int n_heads,
                                 void* d_workspace, size_t workspace_bytes, int* d_status, void* stream) {
-  if (!d_q_bf16 || !d_block_table || !d_positions || !d_out_bf16 || !d_group_rows || !d_prefix_seq || !d_prefix_len || n_groups <= 0) return QZO_ERR_BAD_ARG;
+  if (!d_q_bf16 || !d_block_table || !d_positions || !d_out_bf16 || !d_group_rows || !d_prefix_seq || !d_prefix_len || n_groups <= 0 || n_groups > kMostGroups) return QZO_ERR_BAD_ARG;
   if (!words_aligned(d_block_table, d_row_seq, d_positions, d_group_rows, d_prefix_seq, d_prefix_len, d_status)) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_attention(d_q_bf16, ldq, cache, n_seqs, table_width, d_row_seq, scale, d_out_bf16, ldo, R, n_heads));
   QZO_TRY(check_device());

@@ -73,6 +73,7 @@ __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0
 constexpr int kPrefixQueries = 128, kPrefixTile = 64;
 constexpr int kPrefixStep = 16;                        // tokens that a prefix counts in: what the rows' own kernel starts at
 constexpr int kPrefixLeast = 4;                        // places of a CTA's stretch, at least
+constexpr int kMostGroups = 1 << 20;                   // every row goes over all of them
 
 struct PrefixGroup {
   int row0, rows, prefix, seq, tiles, key_tiles;       // tiles of queries of a key head, tiles of keys

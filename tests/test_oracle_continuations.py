@@ -179,7 +179,7 @@ def test_shared_prefix_attention_refusals():
         with pytest.raises(qzo.QzoError):
             qzo.qzo_debug_prefix_path(path)
     for args in ((0, 1, 4, 2, 64, 64), (1, 0, 4, 2, 64, 64), (1, 1, 3, 2, 64, 64), (1, 1, 4, 0, 64, 64), (1, 1, 4, 2, 80, 64), (1, 1, 4, 2, 64, 0),
-                 (1, 1, 4, 2, 64, (1 << 30) + 1)):
+                 (1, 1, 4, 2, 64, (1 << 30) + 1), (1, (1 << 20) + 1, 4, 2, 64, 64)):
         with pytest.raises(qzo.QzoError):
             qzo.qzo_shared_prefix_attention_workspace_bytes(*args)
 
@@ -188,7 +188,7 @@ def test_shared_prefix_attention_refusals():
                                                     ldo, R, H, ws, b, status, None)
     good = dict(q=P, ldq=256, cache=_cache(), tab=P, n=3, w=4, seq=NONE, pos=P, rows=P, pseq=P, plen=P, g=2, scale=0.125, out=Q, ldo=256, R=3, H=4)
     bad = [{n: v} for n in ("q", "tab", "pos", "rows", "pseq", "plen", "out") for v in (NONE, ODD)] + [dict(seq=ODD), dict(status=ODD)]
-    bad += [dict(ldq=248), dict(ldq=260), dict(ldo=64), dict(n=0), dict(w=0), dict(w=(1 << 26) + 1), dict(R=0), dict(R=4), dict(H=3), dict(H=0), dict(g=0),
+    bad += [dict(ldq=248), dict(ldq=260), dict(ldo=64), dict(n=0), dict(w=0), dict(w=(1 << 26) + 1), dict(R=0), dict(R=4), dict(H=3), dict(H=0), dict(g=0), dict(g=(1 << 20) + 1),
             dict(scale=0.0), dict(scale=float("nan")), dict(cache=None)]
     caches = (dict(k=0), dict(v=0x20008), dict(dtype=1), dict(block_size=8), dict(head_dim=96), dict(k_scale=2.0), dict(dtype=4, v_scale=0.0), dict(n_blocks=1 << 27))
     assert call(**good) in (qzo.QZO_OK, qzo.ERR_UNSUPPORTED_DEVICE)
@@ -201,7 +201,7 @@ def test_decode_of_groups_refuses_before_the_model_is_looked_at():
     lib, qzo = _lib()._lib, _lib()
     def call(m=NONE, tok=P, seq=P, pos=P, slots=P, tab=P, rows=P, pseq=P, plen=P, n=2, out=P):
         return lib.qzo_decode_groups(m, ctypes.byref(_cache()), tok, seq, pos, slots, 2, tab, 2, 4, rows, pseq, plen, n, out)
-    for change in [{n: v} for n in ("tok", "seq", "pos", "slots", "tab", "rows", "pseq", "plen") for v in (NONE, ODD)] + [dict(n=0), dict(out=NONE), dict(m=NONE)]:
+    for change in [{n: v} for n in ("tok", "seq", "pos", "slots", "tab", "rows", "pseq", "plen") for v in (NONE, ODD)] + [dict(n=0), dict(n=(1 << 20) + 1), dict(out=NONE), dict(m=NONE)]:
         assert call(**change) == qzo.ERR_BAD_ARG, change
 
 
