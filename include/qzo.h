@@ -274,7 +274,7 @@ int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int B, int32_t
  *   d_parents int32 [B][W]: number of the beam it continues (-1 where there are no more candidates),  d_tokens int32 [B][W] (-1),
  *   d_scores_out float [B][W] (-inf),  d_lengths_out int32 [B][W] (0; may be NULL, has to be where d_lengths is).
  * Tokens that are not allowed have logits of -inf.  NaN and +inf logits count as -inf, and a beam with such a score or with a row from
- * n_rows on has no candidates; each sets bit 1 of the status word.  Sums of exponentials are fp32 per thread and fp64 from there, values and ranks fp64.
+ * n_rows on has no candidates; each sets bit 1 of the status word.  Sums of exponentials are fp32 within a CTA and fp64 from there, values and ranks fp64.
  * d_logits float [n_rows][ldl], ldl >= V (16-byte rows are read fastest); length_power from 0 to 8; W up to QZO_MAX_BEAMS, V up to 2^30.
  * The outputs may be the inputs of the same kind (tokens for last tokens); nothing else overlaps.
  * d_workspace: qzo_beam_select_workspace_bytes, 256-aligned; calls that may run at the same time need one each. */
