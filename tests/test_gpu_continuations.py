@@ -565,6 +565,49 @@ def test_several_rows_of_a_request_and_strided_rows(lib, units):
     case.check(out[:, :8])
 
 
+def test_calls_one_behind_the_other_see_what_was_written_before_them(lib, units):
+    # the rows' own keys are read while the kernel in front runs: queries and positions that are written just before a call, and queries that are
+    # the call before's output, in a stream and in a replayed graph
+    case = Shared([(3, 500, [64, 300, 90]), (3, 200, [400, 17, 20])], 8, 4, 128, 16, "bf16", 40)
+    cache, table, rows, seq, prefix, of = lib.KvCache(case.ck, case.cv), torch.from_numpy(case.table).cuda(), ints(case.rows), ints([0, 1]), ints(case.prefix), ints(case.seqs.tolist())
+    R, n = case.R, 4
+    queries = [inputs.normal_fp32((R, 8, 128), 1.0, 60 + i).bfloat16().cuda() for i in range(n)]
+    places = [ints([p - 5 * i for p in case.positions]) for i in range(n)]
+    q, positions = torch.empty_like(queries[0]), torch.empty_like(places[0])
+    ws = torch.empty(lib.qzo_shared_prefix_attention_workspace_bytes(R, 2, 8, 4, 128, case.table.shape[1] * 16), dtype=torch.uint8, device="cuda")
+
+    def call(q, out):
+        return lib.qzo_shared_prefix_attention(q, cache, table, positions, rows, seq, prefix, row_seq=of, workspace=ws, out=out)
+
+    def steps(outs, wait=lambda: None):
+        for i in range(n):
+            q.copy_(queries[i])
+            positions.copy_(places[i])
+            wait()
+            call(q, outs[i][0])
+            wait()
+            call(outs[i][0], outs[i][1])
+            wait()
+    outs, want = ([[torch.empty_like(q) for _ in range(2)] for _ in range(n)] for _ in range(2))
+    steps(want, torch.cuda.synchronize)
+    same = lambda: all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for pair in zip(outs, want) for a, b in zip(*pair))  # noqa: E731
+    for _ in range(10):
+        steps(outs)
+        assert same()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        steps(outs)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            steps(outs)
+    for _ in range(10):
+        for pair in outs:
+            for t in pair:
+                t.zero_()
+        graph.replay()
+        assert same()
+
+
 def test_a_prefix_of_a_cache_beyond_32_bit_offsets(lib, units):
     Hkv, block, dh = 8, 64, 128
     n_blocks = (1 << 32) // (Hkv * block * dh * 2) + 6            # 4 GB and a little of keys, as many of values
