@@ -340,10 +340,7 @@ paged_attention_kernel(PagedParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int per_row = p.Hkv * p.chunks;
   const int split = blockIdx.y;
-  // Own keys are read while the kernel of the prefixes, which is in front, still runs (64 rows on 16 prefixes 64.0 -> 59.7 us): it has waited
-  // for what was before it, and only then let this one start.  Its results are for the join: every CTA waits there, so that this
-  // kernel does not end before that one.
-  if (KEYS != Keys::kOwn) serving_begin();
+  serving_begin();
   if (KEYS == Keys::kPrefix) serving_next();
   PrefixGroup group = {};
   int unit = 0;
@@ -386,7 +383,6 @@ paged_attention_kernel(PagedParams p) {
     if (KEYS != Keys::kPrefix && len == 0 && split == 0)
       for (int i = threadIdx.x; i < n_heads * DH / 8; i += W * 32)
         *reinterpret_cast<uint4*>(p.out + (size_t)row * p.ldo + (size_t)head0 * DH + 8 * i) = make_uint4(0u, 0u, 0u, 0u);
-    if (KEYS == Keys::kOwn) serving_begin();
     return;
   }
 
@@ -648,7 +644,6 @@ paged_attention_kernel(PagedParams p) {
     free_stage = free_stage + 1 == kStages ? 0 : free_stage + 1;
   }
 
-  if (KEYS == Keys::kOwn) serving_begin();
   if (KEYS != Keys::kPrefix) serving_next();      // not earlier: CTAs that wait take room from those that load (83.6 us, 86.1 us if at the start)
   __syncthreads();                     // the rings are free: the warps' results go there
   // join the warps

@@ -831,3 +831,44 @@ def test_tensors_off_the_device_or_of_another_shape_are_refused(lib):
         lib.qzo_fork_requests(lens, ints([0, 1]), tab, free, n, 16, 6, table_out=tab)
     with pytest.raises(AssertionError):
         lib.qzo_copy_blocks([], ints([[0, 1, 2]]), ints([1]))
+
+
+def test_a_chain_of_serving_calls_sees_what_the_calls_before_wrote(lib, units):
+    # slots, head norms, cache write and attention right behind one another, step after step in the same buffers, with no other kernel between them: each
+    # may start while the one before it ends.  What a step gives is what it gives when every call is waited for
+    case = Shared([(4, 500, [9, 20, 33, 60]), (4, 200, [1, 30, 5, 100])], 8, 4, 128, 16, "bf16", 41)
+    R, n, steps, spare = case.R, len(case.prefix), 6, 2 * case.R
+    n_blocks = case.ck.shape[0]
+    more = torch.full((spare, 4, 16, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    first = dict(k=torch.cat((case.ck, more)), v=torch.cat((case.cv, more)), lens=ints(case.prefix + case.lens), count=ints([spare]),
+                 free=torch.arange(n_blocks, n_blocks + spare, dtype=torch.int32, device="cuda"),
+                 table=torch.nn.functional.pad(torch.from_numpy(case.table).cuda(), (0, 2), value=-1))
+    live = {name: t.clone() for name, t in first.items()}
+    cache, new = lib.KvCache(live["k"], live["v"]), ints([0] * n + [1] * R)
+    given = [[inputs.normal_fp32((R, h, 128), 1.0, 70 + 3 * i + j).bfloat16().cuda() for j, h in enumerate((8, 4, 4))] for i in range(steps)]
+    gain, angles = torch.linspace(0.5, 1.5, 128, device="cuda"), lib.qzo_rope_table(4096, 128)
+    seq, pos, slots = (ints([0] * R) for _ in range(3))
+    q, status, rows, prefix, of = torch.empty_like(given[0][0]), ints([0]), ints(case.rows), ints(case.prefix), ints(list(range(n)))
+    ws = torch.empty(lib.qzo_shared_prefix_attention_workspace_bytes(R, n, 8, 4, 128, live["table"].shape[1] * 16), dtype=torch.uint8, device="cuda")
+
+    def run(outs, wait):
+        for name, t in first.items():
+            live[name].copy_(t)
+        torch.cuda.synchronize()
+        for i in range(steps):
+            lib.qzo_assign_slots(live["lens"], new, live["table"], live["free"], live["count"], 16, R, row_seq=seq, positions=pos, slots=slots, status=status)
+            wait()
+            lib.qzo_qk_norm_rope_cache(*given[i], pos, slots, cache, q_gain=gain, k_gain=gain, table=angles, q_out=q, status=status)
+            wait()
+            lib.qzo_shared_prefix_attention(q, cache, live["table"], pos, rows, of, prefix, row_seq=seq, out=outs[i], workspace=ws, status=status)
+            wait()
+    want, outs = ([torch.empty_like(q) for _ in range(steps)] for _ in range(2))
+    run(want, torch.cuda.synchronize)
+    assert int(status) == 0 and live["lens"].tolist() == case.prefix + [v + steps for v in case.lens]
+    for _ in range(20):
+        run(outs, lambda: None)
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(outs, want))
+    case.q, case.ck, case.cv, case.table = q, live["k"], live["v"], live["table"].cpu().numpy()
+    case.lens = [v + steps for v in case.lens]
+    case.positions = [v - 1 for v in case.lens]
+    case.check(outs[-1])
