@@ -270,7 +270,8 @@ int qzo_assign_slots(const int32_t* d_lens, const int32_t* d_new, int B, int32_t
  *   score + x_t - log sum_u exp x_u,   t = 0 .. V - 1,   length + 1,
  * x = row d_rows[b W + w] of d_logits (d_rows int32 [B][W]; NULL: row b W + w; a negative row: no candidates).
  * Of all candidates of a request the W largest by score / length^length_power (a length below 1 counts as 1) come out, largest
- * first, equal ones by beam, then by token:
+ * first, equal ones by beam, then by token.  That quotient is formed in fp64; candidates of one beam go by their logits, also where a score of
+ * large magnitude (-1e9 for a beam that is out) or logits next to zero leave them the same quotient:
  *   d_parents int32 [B][W]: number of the beam it continues (-1 where there are no more candidates),  d_tokens int32 [B][W] (-1),
  *   d_scores_out float [B][W] (-inf),  d_lengths_out int32 [B][W] (0; may be NULL, has to be where d_lengths is).
  * Tokens that are not allowed have logits of -inf.  NaN and +inf logits count as -inf, and a beam with such a score or with a row from

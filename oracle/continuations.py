@@ -10,7 +10,8 @@ import numpy as np
 
 
 def beam_select(logits, scores, rows=None, last=None, end_token=-1, lengths=None, power=0.0):
-    """-> lists [B][W] of (parent, token, score, length, rank); (-1, -1, -inf, 0, -inf) where there are no more candidates."""
+    """-> lists [B][W] of (parent, token, score, length, rank); (-1, -1, -inf, 0, -inf) where there are no more candidates.  Candidates of a beam
+    whose ranks round to one number stay in the order of their logits."""
     B, W = scores.shape
     out = []
     for b in range(B):
@@ -21,7 +22,7 @@ def beam_select(logits, scores, rows=None, last=None, end_token=-1, lengths=None
             if not -math.inf < score < math.inf:
                 continue
             if last is not None and int(last[b, w]) == end_token:
-                found.append((score / max(length, 1) ** power, beam, end_token, score, length))
+                found.append((score / max(length, 1) ** power, beam, 0.0, end_token, score, length))
                 continue
             row = beam if rows is None else int(rows[b, w])
             if not 0 <= row < len(logits):
@@ -34,9 +35,9 @@ def beam_select(logits, scores, rows=None, last=None, end_token=-1, lengths=None
             for t in np.argsort(-x, kind="stable")[:W]:
                 if x[t] > -np.inf:
                     value = score + (x[t] - norm)
-                    found.append((value / max(length + 1, 1) ** power, beam, int(t), value, length + 1))
-        found.sort(key=lambda f: (-f[0], f[1], f[2]))
-        best = [(beam, t, value, length, rank) for rank, beam, t, value, length in found[:W]]
+                    found.append((value / max(length + 1, 1) ** power, beam, float(x[t]), int(t), value, length + 1))
+        found.sort(key=lambda f: (-f[0], f[1], -f[2], f[3]))
+        best = [(beam, t, value, length, rank) for rank, beam, _, t, value, length in found[:W]]
         out.append(best + [(-1, -1, -math.inf, 0, -math.inf)] * (W - len(best)))
     return out
 

@@ -258,7 +258,8 @@ struct BeamDynamic {                                   // of the second kernel's
 };
 
 // A CTA = a request, a warp = one of its beams: it joins its chunks' sums and lists, then the first warp joins the beams.  Values
-// and ranks are formed in 64 bits, where different logits of a beam give different ranks.  Bound by latency: W steps of joining one after
+// and ranks are formed in 64 bits.  A beam's list stays in the order of its logits, which is that of the ranks before they were rounded: next to
+// a score of -1e9 logits that differ by less than 2^-23 have one rank.  Bound by latency: W steps of joining one after
 // the other, twice (about 5 us, whatever the vocabulary).
 __global__ void __launch_bounds__(1024)
 beam_pick_kernel(BeamParams p) {

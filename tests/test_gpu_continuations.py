@@ -136,6 +136,22 @@ def test_zeros_of_either_sign_are_one_rank(lib):
     _check_beams(lib, torch.zeros((6, 8), device="cuda"), scores, last=np.full((2, 3), 5, np.int32), end_token=5)
 
 
+@pytest.mark.parametrize("size", [0.0, 1e9, 1e15])
+@pytest.mark.parametrize("power", [0.0, 0.7])
+def test_candidates_whose_ranks_round_to_one(lib, size, power):
+    # logits next to zero, and scores so low that logits vanish beside them: a beam's candidates go by their logits all the same, beams of one rank by their number
+    W, V = 4, 5000
+    x = torch.full((2 * W, V), -1.0, device="cuda")
+    x[:, [10, 20, 30, 40, 4900]] = torch.tensor([0.0, 1e-18, 2e-18, 2e-18, 4e-18], device="cuda")
+    x[W:, [7, 4000, 3000]] = torch.tensor([0.01, 0.02, 0.03], device="cuda")
+    scores = np.full((2, W), -INF, np.float32)
+    scores[0, 1] = scores[1, 2] = scores[1, 3] = -size
+    lengths = np.full((2, W), 5, np.int32)
+    _check_beams(lib, x, scores, lengths=lengths, power=power)
+    rows = np.zeros((2, W), np.int32)                    # beams of one row and one score: the first has all places
+    _check_beams(lib, x, np.full((2, W), -size, np.float32), rows=rows, lengths=lengths, power=power)
+
+
 def test_beams_in_place(lib):
     rng = _gen(5)
     B, W, V = 3, 4, 2000

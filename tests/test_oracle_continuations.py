@@ -210,3 +210,13 @@ def test_the_binding_names_the_limits_of_the_header():
     header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "qzo.h")).read()
     for name in ("MAX_BEAMS", "MAX_POOL_BLOCKS"):
         assert getattr(qzo, name) == int(re.search(rf"#define QZO_{name} (\d+)", header).group(1))
+
+
+def test_candidates_of_a_beam_whose_ranks_round_to_one_stay_in_the_order_of_their_logits():
+    x = np.full((3, 50), -1.0)
+    x[:, [10, 20, 30, 40]] = 0.0, 1e-18, 2e-18, 2e-18
+    picked = lambda *scores: [(p, t) for p, t, *_ in oracle.beam_select(x, np.array([scores]))[0]]  # noqa: E731
+    assert picked(-1.0, -math.inf, -math.inf) == [(0, 30), (0, 40), (0, 20)]      # equal logits: by token
+    x[:, [30, 20]] = 0.01, 0.02
+    assert picked(-1e15, -math.inf, -math.inf) == [(0, 20), (0, 30), (0, 40)]
+    assert picked(-math.inf, -1e18, -1e18) == [(1, 20), (1, 30), (1, 40)]         # equal ranks of several beams: by beam
