@@ -335,7 +335,9 @@ int qzo_copy_blocks(const qzo_kv_cache* h_caches, int n_caches, const int32_t* d
  * Everything else as in qzo_paged_attention, the meaning of every output among it: the sums are those, taken in another order.  Bit 0 of the
  * status word: a bounded wait inside a kernel ran out, and the output means nothing.
  * n_blocks * block_size * n_kv_heads < 2^31, n_groups up to 2^20.  d_workspace: qzo_shared_prefix_attention_workspace_bytes, 256-aligned.
- * Where little is shared, every row reads all of its keys through its own table, as in qzo_paged_attention (indices of groups are not looked at then). */
+ * Where little is shared, every row reads all of its keys through its own table, as in qzo_paged_attention (indices of groups are not looked at then).
+ * The workspace's size is that for every call of up to R rows, n_groups groups and tables of max_len tokens: one for the largest serves as
+ * requests end. */
 int qzo_shared_prefix_attention_workspace_bytes(int R, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes);
 int qzo_shared_prefix_attention(const void* d_q_bf16, int ldq, const qzo_kv_cache* cache, const int32_t* d_block_table, int n_seqs, int table_width,
                                 const int32_t* d_row_seq, const int32_t* d_positions, const int32_t* d_group_rows, const int32_t* d_prefix_seq,

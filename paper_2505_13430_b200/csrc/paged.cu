@@ -682,7 +682,7 @@ paged_attention_kernel(PagedParams p) {
       for (int e = 0; e < 4; ++e) val[e] = fmaf(c, sm_o[w][h][d + e], val[e]);
     }
     if (KEYS == Keys::kPrefix) {
-      const size_t at = ((size_t)blockIdx.x * p.prefix_splits + split) * p.unit_items + h;
+      const size_t at = prefix_query(p, group.row0, group.rows, hk, chunk * 8 * NT + h) * p.prefix_splits + split;
       *reinterpret_cast<float4*>(p.prefix_o + at * DH + d) = make_float4(val[0], val[1], val[2], val[3]);
       if (d == 0) *reinterpret_cast<float2*>(p.prefix_ml + 2 * at) = make_float2(mx, sum);
     } else if (joins) {
@@ -910,9 +910,19 @@ size_t paged_attention_bytes(int R, int H, int Hkv, int dh, int max_len) {
 struct PrefixPlan {
   PrefixPath path;
   int items, splits, least;                            // queries of a unit; small units: splits, keys of one
-  int64_t units, parts;
-  size_t bytes;                                        // of the parts
+  int64_t units, results;
+  size_t bytes;                                        // of the results
 };
+
+// Estimated time, in us, of R rows that read `bytes` of each key head through their own tables; prefix_plan says where the rates are from
+double own_tables_us(int64_t R, int Hkv, double bytes, bool f8) {
+  const double asked = (double)R * Hkv * bytes;
+  return std::min(3 + asked / (f8 ? 7e6 : 10.5e6), 12 + asked / (f8 ? 11.3e6 : 15.7e6));
+}
+double key_head_bytes(int64_t max_len, int dh, bool f8) { return (double)max_len * dh * (f8 ? 2 : 4); }
+// The least that either way of taking prefixes is estimated at
+constexpr double few_least_us(bool f8) { return f8 ? 9.5 : 8; }
+constexpr double many_least_us(bool f8) { return f8 ? 20 : 21; }
 
 PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int64_t max_len) {
   PrefixPlan plan{kOwnTables, 0, 0, 0, 0, 0, 0};
@@ -925,20 +935,18 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
   // the kernel for many queries.  Examples, us through own tables, few, many: 64 rows of 64 queries on 2048 139, 28, 26, on 16384 1033, 139, 62;
   // 128 rows of 1024 queries on 16384 275, 231, 67 (203, 156, 89); 32 rows of 128 queries on 8192 90, 46, 31 (67, 31, 33).
   // Lengths are known on the device only: all of this goes by the table's width.
-  const double bytes = (double)max_len * dh * (f8 ? 2 : 4);           // of a key head
-  const double asked = (double)R * Hkv * bytes;
-  const double own = std::min(3 + asked / (f8 ? 7e6 : 10.5e6), 12 + asked / (f8 ? 11.3e6 : 15.7e6));
+  const double bytes = key_head_bytes(max_len, dh, f8), own = own_tables_us(R, Hkv, bytes, f8);
   const double rows = R * (double)Hkv / 400;           // the rows' own keys: a CTA for each row and key head
   const double asked_few = (double)prefix_units(R, n_groups, G, Hkv, few_items) * bytes;
   const double asked_many = std::min(R, n_groups) * std::max(1.0, (double)queries / kPrefixQueries) * Hkv * bytes;   // a unit that is not full costs less
-  const double few = rows + (f8 ? std::min(9.5 + asked_few / 5.7e6, 25 + asked_few / 8.1e6) : 8 + asked_few / 8.3e6);
-  const double many = rows + (f8 ? std::min(20 + asked_many / 1.25e6, 27 + asked_many / 2.4e6) : 21 + asked_many / 6.2e6);
+  const double few = rows + (f8 ? std::min(few_least_us(f8) + asked_few / 5.7e6, 25 + asked_few / 8.1e6) : few_least_us(f8) + asked_few / 8.3e6);
+  const double many = rows + (f8 ? std::min(many_least_us(f8) + asked_many / 1.25e6, 27 + asked_many / 2.4e6) : many_least_us(f8) + asked_many / 6.2e6);
   plan.path = forced != kByRule ? (PrefixPath)forced : own <= std::min(few, many) ? kOwnTables : few <= many ? kFewPath : kManyPath;
   if (plan.path == kOwnTables) return plan;
   plan.items = plan.path == kManyPath ? kPrefixQueries : few_items;
   plan.units = prefix_units(R, n_groups, G, Hkv, plan.items);
   if (plan.path == kManyPath) {
-    plan.parts = plan.units + 2 * kSMs;
+    plan.results = (int64_t)R * G * Hkv + 2 * kSMs * kPrefixQueries;
     if (plan.units * (max_len / kPrefixTile + 2) > INT32_MAX / 2) plan.path = kOwnTables;      // places of the line are counted in 32 bits
   } else {
     // as attention_plan
@@ -946,10 +954,10 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
     const int64_t fill = std::min<int64_t>(slots / plan.units, max_len / (128 * subs)), even = std::min<int64_t>(max_len / (2048 * subs), 8 * slots / plan.units);
     plan.splits = (int)std::max<int64_t>(1, std::max(fill, even));
     plan.least = (even > fill ? 2048 : 128) * subs;
-    plan.parts = plan.units * plan.splits;
+    plan.results = (int64_t)R * G * Hkv * plan.splits;
     if (plan.units > INT32_MAX) plan.path = kOwnTables;
   }
-  plan.bytes = (size_t)plan.parts * plan.items * (dh + 2) * sizeof(float);
+  plan.bytes = (size_t)plan.results * (dh + 2) * sizeof(float);
   return plan;
 }
 
@@ -958,15 +966,30 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
 // 6 and 14 + 12 us of 2; 9 us of one).
 int own_splits(const Plan& plan, int64_t ctas) { return ctas >= kSMs ? 1 : std::min(plan.splits, 4); }
 
-// For either type of cache
-size_t shared_prefix_bytes(int R, int n_groups, int H, int Hkv, int dh, int max_len) {
-  size_t most = paged_attention_bytes(R, H, Hkv, dh, max_len);
+// For either type of cache, and a bound over all calls of up to R rows and max_len tokens, however many groups there are: what one call needs does
+// not grow with each of these (fewer rows are cut into more splits, fewer groups may be taken another way), and a program sizes its workspace once.
+size_t shared_prefix_bytes(int R, int H, int Hkv, int dh, int max_len) {
+  const int64_t G = H / Hkv, row_ctas = Hkv * (int64_t)head_chunks((int)G), rows = R, forced = forced_path.load();
+  // r of `many` rows or queries in s splits, as attention_plan and prefix_plan choose them, are r s results: at most what the SMs hold at once, or
+  // eight times that, and at most the pieces of 128 or 2048 keys of them all
+  auto in_splits = [&](int64_t once, int64_t eight_times, int64_t many, int subs) {
+    const int64_t fill = max_len / (128 * subs), even = max_len / (2048 * subs);
+    return std::max<int64_t>(fill > 1 ? std::min(once, many * fill) : 0, even > 1 ? std::min(eight_times, many * even) : 0);
+  };
+  const int64_t slots = kSMs * resident_ctas(G <= 8 ? 1 : 2);
+  int64_t most = in_splits(slots / row_ctas, 8 * slots / row_ctas, rows, 128 / dh) * H;               // own tables
+  const int64_t own_keys = std::max(rows, 4 * std::min(rows, (kSMs - 1) / row_ctas)) * H;             // as own_splits
   for (bool f8 : {false, true}) {
-    const PrefixPlan plan = prefix_plan(R, n_groups, H / Hkv, Hkv, dh, f8, max_len);
-    const int splits = own_splits(attention_plan(R, Hkv, H / Hkv, 256 / (dh * (f8 ? 1 : 2)), max_len), (int64_t)R * Hkv * head_chunks(H / Hkv));
-    if (plan.path != kOwnTables) most = std::max(most, plan.bytes + (size_t)R * H * splits * (dh + 2) * sizeof(float));
+    const int subs = 256 / (dh * (f8 ? 1 : 2));
+    const double own = own_tables_us(rows, Hkv, key_head_bytes(max_len, dh, f8), f8);
+    if (forced == kFewPath || (forced == kByRule && own > few_least_us(f8)))
+      for (int items : {8, 16}) {
+        const int64_t queries = (int64_t)kSMs * resident_ctas(items / 8) * items;
+        most = std::max(most, std::max(rows * H, in_splits(queries, 8 * queries, rows * H, subs)) + own_keys);
+      }
+    if (forced == kManyPath || (forced == kByRule && own > many_least_us(f8))) most = std::max(most, rows * H + 2 * kSMs * kPrefixQueries + own_keys);
   }
-  return most;
+  return (size_t)most * (dh + 2) * sizeof(float);
 }
 
 int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& c, const int32_t* table, int n_seqs, int width,
@@ -989,7 +1012,7 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
   if (groups) {
     if ((int64_t)c.n_blocks * c.block_size * c.n_kv_heads > INT32_MAX) return QZO_ERR_BAD_ARG;               // rows that a tensor map can name
     if (!fewer_splits)
-      if (const size_t need = shared_prefix_bytes(R, groups->n, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
+      if (const size_t need = shared_prefix_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
         if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
     const PrefixPlan prefix = prefix_plan(R, groups->n, G, c.n_kv_heads, c.head_dim, f8, max_len);
     int splits = own_splits(plan, (int64_t)R * c.n_kv_heads * chunks);
@@ -1002,9 +1025,9 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
       p.prefix_least = prefix.least;
       p.splits = splits;
       p.prefix_o = (float*)ws;
-      p.part_o = p.prefix_o + (size_t)prefix.parts * prefix.items * c.head_dim;
+      p.part_o = p.prefix_o + (size_t)prefix.results * c.head_dim;
       p.prefix_ml = p.part_o + (size_t)R * H * splits * c.head_dim;
-      p.part_ml = p.prefix_ml + 2 * (size_t)prefix.parts * prefix.items;
+      p.part_ml = p.prefix_ml + 2 * (size_t)prefix.results;
       if (c.head_dim == 128) return f8 ? run_groups<128, true>(p, c, prefix.units, plan.wide, st) : run_groups<128, false>(p, c, prefix.units, plan.wide, st);
       return f8 ? run_groups<64, true>(p, c, prefix.units, plan.wide, st) : run_groups<64, false>(p, c, prefix.units, plan.wide, st);
     }
@@ -1095,7 +1118,7 @@ int qzo_debug_prefix_path(int path) {
 int qzo_shared_prefix_attention_workspace_bytes(int R, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes) {
   if (!bytes || R <= 0 || n_groups <= 0 || n_groups > kMostGroups || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || max_len <= 0 || max_len > kMostKeys) return QZO_ERR_BAD_ARG;
   if (head_dim != 64 && head_dim != 128) return QZO_ERR_BAD_ARG;
-  *bytes = shared_prefix_bytes(R, n_groups, n_heads, n_kv_heads, head_dim, max_len);
+  *bytes = shared_prefix_bytes(R, n_heads, n_kv_heads, head_dim, max_len);
   return QZO_OK;
 }
 

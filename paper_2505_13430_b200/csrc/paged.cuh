@@ -30,7 +30,7 @@ struct PagedParams {
   int unit_items;                                      // queries of a unit of work on prefixes
   int prefix_ctas;                                     // units of 128: CTAs of the kernel on the tensor cores' line
   int prefix_splits, prefix_least;                     // smaller units: splits of each (0 where units have 128), keys of one, at least
-  float *prefix_o, *prefix_ml;                         // results: [parts][unit_items][DH], [parts][unit_items][2]
+  float *prefix_o, *prefix_ml;                         // results: [..][DH], [..][2], in the order told below
 };
 
 // Keys of split s of a row that sees len keys: [s * per, min(len, (s + 1) * per)), per at least the launch's minimum.
@@ -67,9 +67,10 @@ __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0
 // The work on prefixes: a unit is some queries (the rows of a group times the query heads of a key head, in that order) over the
 // whole prefix of their group; units are numbered group by group, key head by key head.
 // Many queries to a group: units of 128 for the tensor cores' larger instructions (prefix.cu), in tiles of 64 keys and one place more for
-// what a change of units costs.  All units stand in one line, of which every CTA takes an equal stretch.  What a CTA finds of unit u is
-// part (CTA + u) of the results: from one stretch or unit to the next, one of the two grows.
-// Few: units of 8 or 16, which are to paged_attention_kernel what the heads of a row are; split s of unit u is part (u * splits + s).
+// what a change of units costs.  All units stand in one line, of which every CTA takes an equal stretch.
+// Few: units of 8 or 16, which are to paged_attention_kernel what the heads of a row are, in splits of their keys.
+// Results are as many as there are queries, whatever the units' number: query q of the line leaves what CTA c finds of it at 128 c + q (from one
+// stretch to the next a unit's results move by 128, from one unit to the next by the unit's queries), or what split s does at q * splits + s.
 constexpr int kPrefixQueries = 128, kPrefixTile = 64;
 constexpr int kPrefixStep = 16;                        // tokens that a prefix counts in: what the rows' own kernel starts at
 constexpr int kPrefixLeast = 4;                        // places of a CTA's stretch, at least
@@ -81,6 +82,10 @@ struct PrefixGroup {
   __device__ __forceinline__ int places() const { return key_tiles + 1; }        // of a unit
 };
 
+// Place in the line of query `item` of a group's rows `row0 ..` at key head hk
+__device__ __forceinline__ size_t prefix_query(const PagedParams& p, int row0, int rows, int hk, int item) {
+  return (size_t)row0 * p.H + (size_t)hk * rows * p.G + item;
+}
 // A group; without keys where its request or its length is out of range
 __device__ __forceinline__ PrefixGroup prefix_group(const PagedParams& p, int i, bool report = false) {
   const int row0 = p.groups.rows[i], end = p.groups.rows[i + 1], len = p.groups.len[i], seq = p.groups.seq[i];
@@ -134,40 +139,40 @@ __device__ __forceinline__ int prefix_stretch(const PagedParams& p, int places) 
 // Where the results of a row's prefix are.
 struct RowPrefix {
   int prefix;                                          // keys that the row's group shares; 0: no group
-  int row0, tiles, key_tiles, places;                  // of its group
-  int places_before, units_before, stretch;
+  int row0, rows, tiles, key_tiles, places;            // of its group
+  int places_before, stretch;
 
-  // The parts of query `in_group` of the group (rows times heads of a key head) at key head hk: how many, the first one's place, and from one
-  // to the next, in queries
+  // The results of query `in_group` of the group (rows times heads of a key head) at key head hk: how many, the first one's place, and from one
+  // to the next
   __device__ __forceinline__ int parts(const PagedParams& p, int hk, int in_group, size_t* first, int* step) const {
-    const int unit = hk * tiles + in_group / p.unit_items, number = units_before + unit, in_unit = in_group % p.unit_items;
-    *step = p.unit_items;
+    const size_t query = prefix_query(p, row0, rows, hk, in_group);
     if (p.prefix_splits) {
       const int per = prefix_split_keys(p, prefix);
-      *first = (size_t)number * p.prefix_splits * p.unit_items + in_unit;
+      *first = query * p.prefix_splits;
+      *step = 1;
       return (prefix + per - 1) / per;
     }
-    const int t0 = places_before + unit * places, c0 = t0 / stretch;
-    *first = (size_t)(c0 + number) * p.unit_items + in_unit;
+    const int t0 = places_before + (hk * tiles + in_group / kPrefixQueries) * places, c0 = t0 / stretch;
+    *first = query + (size_t)kPrefixQueries * c0;
+    *step = kPrefixQueries;
     return (t0 + key_tiles - 1) / stretch - c0 + 1;
   }
 };
 
 // Whole warps, `row` the same in all lanes.  Bounds that do not ascend within the rows make no groups.
 __device__ __forceinline__ RowPrefix row_prefix(const PagedParams& p, int row) {
-  int places = 0, before = 0, units_before = 0, prefix = 0, row0 = 0, tiles = 0, key_tiles = 0;
+  int places = 0, before = 0, prefix = 0, row0 = 0, rows = 0, tiles = 0, key_tiles = 0;
   bool bad = false, mine = false;
   for (int i = threadIdx.x & 31; i < p.groups.n; i += 32) {
     const PrefixGroup g = prefix_group(p, i);
     bad = bad || g.row0 < 0 || g.rows < 0 || g.row0 + g.rows > p.R;
-    const int units = g.units(p.Hkv), all = units * g.places();
+    const int all = g.units(p.Hkv) * g.places();
     places += all;
     if (g.row0 + g.rows <= row) {
       before += all;
-      units_before += units;
     } else if (g.row0 <= row) {
       mine = true;
-      prefix = g.prefix; row0 = g.row0; tiles = g.tiles; key_tiles = g.key_tiles;
+      prefix = g.prefix; row0 = g.row0; rows = g.rows; tiles = g.tiles; key_tiles = g.key_tiles;
     }
   }
   RowPrefix r = {};
@@ -175,11 +180,11 @@ __device__ __forceinline__ RowPrefix row_prefix(const PagedParams& p, int row) {
   bad = __any_sync(0xffffffffu, bad);
   places = __reduce_add_sync(0xffffffffu, places);
   r.places_before = __reduce_add_sync(0xffffffffu, before);
-  r.units_before = __reduce_add_sync(0xffffffffu, units_before);
   if (bad || !who) return r;
   const int lane = __ffs(who) - 1;
   r.prefix = __shfl_sync(0xffffffffu, prefix, lane);
   r.row0 = __shfl_sync(0xffffffffu, row0, lane);
+  r.rows = __shfl_sync(0xffffffffu, rows, lane);
   r.tiles = __shfl_sync(0xffffffffu, tiles, lane);
   r.key_tiles = __shfl_sync(0xffffffffu, key_tiles, lane);
   r.places = r.key_tiles + 1;

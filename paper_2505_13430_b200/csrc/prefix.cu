@@ -67,11 +67,9 @@ struct PrefixMaps { CUtensorMap whole[2], step[2]; };
 struct Walk {
   PrefixGroup group;
   int index, unit, key_tile;                           // group, unit within it, tile of keys
-  int number;                                          // of the unit among all
 
   __device__ __forceinline__ void next_unit(const PagedParams& p) {
     key_tile = 0;
-    ++number;
     if (++unit < group.units(p.Hkv)) return;
     unit = 0;
     while (++index < p.groups.n) {                     // to the next group with units
@@ -108,17 +106,17 @@ __device__ __forceinline__ int find_stretch(const PagedParams& p, int cta, bool 
   const int stretch = prefix_stretch(p, all), from = min(all, cta * stretch), to = min(all, from + stretch);
   if (from >= to) return 0;
   // the group that `from` is in, and the tiles between `from` and `to`: places less the one at the end of each unit
-  int places_before = 0, units_before = 0, tiles = 0;
+  int places_before = 0, tiles = 0;
   bool found = false;
   for (int i0 = 0; i0 < p.groups.n && places_before < to; i0 += 32) {
     PrefixGroup g = first;
     if (i0) g = i0 + lane < p.groups.n ? prefix_group(p, i0 + lane) : PrefixGroup{};
     const int units = g.units(p.Hkv), places = units * g.places();
-    int sum = places, unit_sum = units;
+    int sum = places;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, sum, d), unit_up = __shfl_up_sync(0xffffffffu, unit_sum, d);
-      if (lane >= d) { sum += up; unit_sum += unit_up; }
+      const int up = __shfl_up_sync(0xffffffffu, sum, d);
+      if (lane >= d) sum += up;
     }
     const int begin = places_before + sum - places;
     if (units) {                                       // tiles in front of place x of the group
@@ -135,10 +133,8 @@ __device__ __forceinline__ int find_stretch(const PagedParams& p, int cta, bool 
       const int in_group = from - __shfl_sync(0xffffffffu, begin, who);
       w->unit = in_group / w->group.places();
       w->key_tile = in_group % w->group.places();
-      w->number = units_before + __shfl_sync(0xffffffffu, unit_sum - units, who) + w->unit;
     }
     places_before += __shfl_sync(0xffffffffu, sum, 31);
-    units_before += __shfl_sync(0xffffffffu, unit_sum, 31);
   }
   tiles = __reduce_add_sync(0xffffffffu, tiles);
   if (tiles && w->key_tile == w->group.key_tiles) w->next_unit(p);
@@ -402,12 +398,11 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       tcgen05_fence_after();
     };
     for (int j = 0; j < n_tiles;) {
-      int count, number, next_row = -1;                // tiles of this unit that are this CTA's; the unit's number
+      int count, next_row = -1;                        // tiles of this unit that are this CTA's
       bool active;                                     // any query for this warp
       {
         const Walk w = *place;
         count = min(n_tiles - j, w.group.key_tiles - w.key_tile);
-        number = w.number;
         active = w.first_item() + warp * 32 < w.group.rows * p.G;
       }
       const bool more = j + count < n_tiles;
@@ -498,8 +493,8 @@ prefix_attention_kernel(const __grid_constant__ PrefixMaps maps, const __grid_co
       }
       // the unit's sums leave tensor memory
       wait(bar_values(j - 1), (j - 1) >> 1);
-      const size_t part = (size_t)(blockIdx.x + number) * p.unit_items + mine;
       if (active) {
+        const size_t part = prefix_query(p, place->group.row0, place->group.rows, place->head(), place->first_item() + mine) + (size_t)kM * blockIdx.x;
 #pragma unroll 1
         for (int c = 0; c < DH; c += 32) {
           uint32_t o[32];

@@ -624,6 +624,32 @@ def test_calls_one_behind_the_other_see_what_was_written_before_them(lib, units)
         assert same()
 
 
+def test_one_workspace_as_requests_end_and_groups_become_fewer(lib):
+    # sized once for 64 rows in 64 groups; then fewer rows in fewer groups, which take other ways; none writes behind the workspace's end
+    H = Hkv = 8
+    case = Shared([(64, 1500, 40)], H, Hkv, 128, 16, "bf16", 42)
+    cache, table, q, pos, of = lib.KvCache(case.ck, case.cv), torch.from_numpy(case.table).cuda(), case.q.cuda(), ints(case.positions), ints(case.seqs.tolist())
+    need = lib.qzo_shared_prefix_attention_workspace_bytes(64, 64, H, Hkv, 128, case.table.shape[1] * 16)
+    buffer = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+    want = case.run(lib)
+    case.check(want)
+    lens = np.array(case.lens)
+    for path in (0, 2, 3):
+        lib.qzo_debug_prefix_path(path)
+        assert path == 0 or lib.qzo_shared_prefix_attention_workspace_bytes(64, 64, H, Hkv, 128, case.table.shape[1] * 16) <= need
+        try:
+            for R, n in ((64, 64), (64, 16), (64, 2), (64, 1), (37, 37), (37, 5), (32, 2), (18, 18), (18, 1), (5, 2), (1, 1)):
+                status = ints([0])
+                out = lib.qzo_shared_prefix_attention(q[:R], cache, table, pos[:R].contiguous(), ints([R * i // n for i in range(n + 1)]), ints([0] * n), ints([1500] * n),
+                                                      row_seq=of, workspace=buffer[:need], status=status)
+                assert int(status) == 0 and (buffer[need:] == 77).all(), (path, R, n)
+                few = Shared.__new__(Shared)
+                few.__dict__.update(case.__dict__, R=R, q=case.q[:R], seqs=case.seqs[:R], positions=case.positions[:R], lens=lens[:R].tolist())
+                few.check(out)
+        finally:
+            lib.qzo_debug_prefix_path(0)
+
+
 def test_a_prefix_of_a_cache_beyond_32_bit_offsets(lib, units):
     Hkv, block, dh = 8, 64, 128
     n_blocks = (1 << 32) // (Hkv * block * dh * 2) + 6            # 4 GB and a little of keys, as many of values

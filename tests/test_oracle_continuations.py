@@ -220,3 +220,16 @@ def test_candidates_of_a_beam_whose_ranks_round_to_one_stay_in_the_order_of_thei
     x[:, [30, 20]] = 0.01, 0.02
     assert picked(-1e15, -math.inf, -math.inf) == [(0, 20), (0, 30), (0, 40)]
     assert picked(-math.inf, -1e18, -1e18) == [(1, 20), (1, 30), (1, 40)]         # equal ranks of several beams: by beam
+
+
+def test_a_workspace_for_the_largest_call_is_one_for_smaller_calls():
+    qzo = _lib()
+    size = qzo.qzo_shared_prefix_attention_workspace_bytes
+    rng = np.random.default_rng(3)
+    shapes = [(64, 64, 32, 32, 128, 2048), (64, 8, 32, 32, 128, 2048), (64, 2, 32, 32, 128, 2048), (128, 16, 32, 4, 128, 16384), (9, 1, 64, 1, 64, 70000)]
+    for R, n, H, Hkv, dh, longest in shapes + [(int(rng.integers(1, 300)), int(rng.integers(1, 300)), 8 * g, 8, 128, int(rng.integers(1, 30000))) for g in (1, 2, 5, 12) for _ in range(5)]:
+        most = size(R, n, H, Hkv, dh, longest)
+        for _ in range(200):
+            fewer = int(rng.integers(1, R + 1)), int(rng.integers(1, n + 1)), H, Hkv, dh, int(rng.integers(1, longest + 1))
+            assert size(*fewer) <= most, (R, n, H, Hkv, dh, longest, fewer)
+        assert most <= 4 * (dh + 2) * (5 * R * H + 8 * 296 * 16)     # results of every query, own keys in four splits, what the SMs hold eight times
