@@ -485,7 +485,8 @@ int qzo_decode(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_toke
                int table_width, float* d_logits);
 
 /* qzo_decode for rows that share the beginning of their caches: the groups are those of qzo_shared_prefix_attention, which takes the place
- * of the attention in every layer (as long as the model's workspace has room for what prefixes leave; without it every row reads its own table). */
+ * of the attention in every layer, by the fastest way whose results the model's workspace holds (2 max_tokens vocab floats; where it holds none,
+ * every row reads its own table). */
 int qzo_decode_groups(qzo_model* m, const qzo_kv_cache* h_caches, const int32_t* d_tokens, const int32_t* d_row_seq,
                       const int32_t* d_positions, const int32_t* d_slots, int R, const int32_t* d_block_table, int n_seqs,
                       int table_width, const int32_t* d_group_rows, const int32_t* d_prefix_seq, const int32_t* d_prefix_len, int n_groups,

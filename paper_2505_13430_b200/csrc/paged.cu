@@ -924,7 +924,8 @@ double key_head_bytes(int64_t max_len, int dh, bool f8) { return (double)max_len
 constexpr double few_least_us(bool f8) { return f8 ? 9.5 : 8; }
 constexpr double many_least_us(bool f8) { return f8 ? 20 : 21; }
 
-PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int64_t max_len) {
+// room: bytes for the results of prefixes and of the rows' own keys; only ways that it holds are taken
+PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int64_t max_len, size_t room = SIZE_MAX) {
   PrefixPlan plan{kOwnTables, 0, 0, 0, 0, 0, 0};
   const int subs = 256 / (dh * (f8 ? 1 : 2)), forced = forced_path.load();
   const int64_t queries = (int64_t)R * G / std::max(1, std::min(R, n_groups));   // of a group and key head, on average
@@ -941,20 +942,25 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
   const double asked_many = std::min(R, n_groups) * std::max(1.0, (double)queries / kPrefixQueries) * Hkv * bytes;   // a unit that is not full costs less
   const double few = rows + (f8 ? std::min(few_least_us(f8) + asked_few / 5.7e6, 25 + asked_few / 8.1e6) : few_least_us(f8) + asked_few / 8.3e6);
   const double many = rows + (f8 ? std::min(many_least_us(f8) + asked_many / 1.25e6, 27 + asked_many / 2.4e6) : many_least_us(f8) + asked_many / 6.2e6);
-  plan.path = forced != kByRule ? (PrefixPath)forced : own <= std::min(few, many) ? kOwnTables : few <= many ? kFewPath : kManyPath;
+  const int64_t all = (int64_t)R * G * Hkv, per_result = (dh + 2) * sizeof(float);     // own keys: a result for every query at least
+  const int64_t fits = (int64_t)std::min<size_t>(room, INT64_MAX) / per_result - all, line = all + 2 * kSMs * kPrefixQueries;
+  const bool few_fits = fits >= all, many_fits = fits >= line;
+  if (forced != kByRule) plan.path = (forced == kFewPath && !few_fits) || (forced == kManyPath && !many_fits) ? kOwnTables : (PrefixPath)forced;
+  else if (many_fits && many < std::min(own, few)) plan.path = kManyPath;
+  else if (few_fits && few < own) plan.path = kFewPath;
   if (plan.path == kOwnTables) return plan;
   plan.items = plan.path == kManyPath ? kPrefixQueries : few_items;
   plan.units = prefix_units(R, n_groups, G, Hkv, plan.items);
   if (plan.path == kManyPath) {
-    plan.results = (int64_t)R * G * Hkv + 2 * kSMs * kPrefixQueries;
+    plan.results = line;
     if (plan.units * (max_len / kPrefixTile + 2) > INT32_MAX / 2) plan.path = kOwnTables;      // places of the line are counted in 32 bits
   } else {
     // as attention_plan
     const int64_t slots = kSMs * resident_ctas(plan.items / 8);
     const int64_t fill = std::min<int64_t>(slots / plan.units, max_len / (128 * subs)), even = std::min<int64_t>(max_len / (2048 * subs), 8 * slots / plan.units);
-    plan.splits = (int)std::max<int64_t>(1, std::max(fill, even));
+    plan.splits = (int)std::max<int64_t>(1, std::min(std::max(fill, even), fits / all));
     plan.least = (even > fill ? 2048 : 128) * subs;
-    plan.results = (int64_t)R * G * Hkv * plan.splits;
+    plan.results = all * plan.splits;
     if (plan.units > INT32_MAX) plan.path = kOwnTables;
   }
   plan.bytes = (size_t)plan.results * (dh + 2) * sizeof(float);
@@ -1014,10 +1020,9 @@ int launch_paged_attention(const __nv_bfloat16* q, int ldq, const qzo_kv_cache& 
     if (!fewer_splits)
       if (const size_t need = shared_prefix_bytes(R, H, c.n_kv_heads, c.head_dim, max_len); need > 0)
         if (!ws || ws_bytes < need || ((uintptr_t)ws & 255)) return QZO_ERR_WORKSPACE;
-    const PrefixPlan prefix = prefix_plan(R, groups->n, G, c.n_kv_heads, c.head_dim, f8, max_len);
-    int splits = own_splits(plan, (int64_t)R * c.n_kv_heads * chunks);
-    if (fewer_splits && ws_bytes >= prefix.bytes + per_split) splits = (int)std::min<size_t>(splits, (ws_bytes - prefix.bytes) / per_split);
-    if (prefix.path != kOwnTables && ws_bytes >= prefix.bytes + splits * per_split) {
+    const PrefixPlan prefix = prefix_plan(R, groups->n, G, c.n_kv_heads, c.head_dim, f8, max_len, ws_bytes);
+    if (prefix.path != kOwnTables) {
+      const int splits = (int)std::min<size_t>(own_splits(plan, (int64_t)R * c.n_kv_heads * chunks), (ws_bytes - prefix.bytes) / per_split);
       p.groups = *groups;
       p.unit_items = prefix.items;
       p.prefix_ctas = 2 * kSMs;

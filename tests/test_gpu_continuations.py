@@ -914,3 +914,77 @@ def test_a_chain_of_serving_calls_sees_what_the_calls_before_wrote(lib, units):
     case.lens = [v + steps for v in case.lens]
     case.positions = [v - 1 for v in case.lens]
     case.check(outs[-1])
+
+
+# ------------------------------------------------------------------ a decode step over shared prefixes
+
+class Step:
+    """One decode step of R rows of a model whose caches hold `prefix` random tokens that all rows share and some of their own."""
+
+    def __init__(self, lib, name, R, prefix, max_tokens, kind="bf16", width=None, **override):
+        cfg = inputs.model_cfg(name, **override)
+        self.gm = lib.build_model_from_raw(inputs.raw_model_tensors(cfg, seed=1000), max_tokens)
+        H, dh, block = cfg["n_heads"], cfg["d_model"] // cfg["n_heads"], 16
+        dt, ks, vs = CACHES[kind]
+        own = [prefix + 1 + 7 * (r % 5) for r in range(R)]                      # tokens of a row behind this step
+        common, most = prefix // block, -(-max(own) // block)
+        n_blocks = common + R * (most - common)
+        self.caches = [lib.KvCache(*((inputs.normal_fp32((n_blocks, H, block, dh), 1.0, 80 + 2 * i + j) / s).to(dt).cuda() for j, s in enumerate((ks, vs))), ks, vs)
+                       for i in range(cfg["n_layers"])]
+        table = np.full((R, width or most), -1, np.int32)
+        table[:, :common] = np.arange(common)
+        table[:, common:most] = common + np.arange(R * (most - common)).reshape(R, -1)
+        for c in self.caches:                                                   # the rest of the prefix stands in every row's own block
+            for pages in (c.k.view(torch.uint8), c.v.view(torch.uint8)):
+                pages[table[1:, common].tolist(), :, :prefix % block] = pages[int(table[0, common]), :, :prefix % block].clone()
+        pos = np.array(own) - 1
+        slots = table[np.arange(R), pos // block] * block + pos % block
+        self.args = [ints(a.tolist()) for a in (_gen(81).integers(0, cfg["vocab"], R), np.arange(R), pos, slots)] + [torch.from_numpy(table).cuda()]
+        self.groups = dict(group_rows=ints([0, R]), prefix_seq=ints([0]), prefix_len=ints([prefix]))
+
+    def plain(self):
+        return self.gm.qzo_decode(self.caches, *self.args)
+
+    def shared(self):
+        out = self.gm.qzo_decode_groups(self.caches, *self.args, **self.groups)
+        assert self.gm.qzo_device_status() == 0
+        return out
+
+
+    def reads_once(self):
+        """Whether the prefix is read through the first row's table alone: without the other rows' entries for it nothing is missed, while a row that reads
+        its own table meets blocks that no cache has.  The last thing a step is used for (the status stays)."""
+        want = self.shared()
+        self.args[4][1:, :int(self.groups["prefix_len"]) // 16] = -1
+        got = self.gm.qzo_decode_groups(self.caches, *self.args, **self.groups)
+        missed = self.gm.qzo_device_status() != 0
+        assert missed or torch.equal(got, want)
+        return not missed
+
+
+def _close(a, b):
+    return ((a - b).abs().max() <= 2e-2 * b.abs().max()).item()
+
+
+def test_decode_of_groups_takes_the_next_way_where_the_first_does_not_fit(lib):
+    # a table so wide that units of 128 are the choice, and a buffer of 1008 results that holds units of 16 only
+    step = Step(lib, "tiny_dh128", 64, 150, 64, width=3000)
+    plain, rule = step.plain(), step.shared()
+    lib.qzo_debug_prefix_path(2)
+    try:
+        few = step.shared()
+    finally:
+        lib.qzo_debug_prefix_path(0)
+    assert torch.equal(rule, few) and _close(rule, plain) and step.reads_once()
+    step.gm.close()
+
+
+@pytest.mark.parametrize("max_tokens", [2, 3, 4, 5, 6, 9, 40])
+def test_decode_of_groups_in_buffers_of_any_size(lib, path, max_tokens):
+    # 62 results of a query and upwards: the smallest has room for the few-query way without splits at most, none for units of 128: own tables then
+    step = Step(lib, "tiny", 2, 1000, max_tokens, width=256, max_seq=2048)
+    plain, shared = step.plain(), step.shared()
+    assert _close(shared, plain)
+    assert path == 2 or torch.equal(shared, plain)
+    assert step.reads_once() == (path == 2), "only units of few queries fit"
+    step.gm.close()
