@@ -988,3 +988,11 @@ def test_decode_of_groups_in_buffers_of_any_size(lib, path, max_tokens):
     assert path == 2 or torch.equal(shared, plain)
     assert step.reads_once() == (path == 2), "only units of few queries fit"
     step.gm.close()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("name,R,prefix", [("tiny", 3, 40), ("tiny_dh128", 21, 150), ("tiny_opt", 9, 33)])
+def test_decode_of_groups_over_either_cache(lib, units, name, R, prefix, kind):
+    step = Step(lib, name, R, prefix, 4096, kind)         # units of 128 leave 37888 results of 520 bytes at least: 20 MB of the 32
+    assert _close(step.shared(), step.plain()) and step.reads_once()
+    step.gm.close()
