@@ -387,8 +387,11 @@ bool tables_ok(const void* lens, const void* table, const void* table_out, const
   return block_size_ok(block_size) && (int64_t)width * block_size <= kMostKeys && (int64_t)n_blocks * block_size <= INT32_MAX;
 }
 
-// CTAs of the cluster that goes over B tables, and their threads: small tables and pools do with fewer, which meet sooner
-int table_ctas(int B, int width) { return (int64_t)B * width > 4096 ? kMostCtas : 1; }
+// CTAs of the cluster that goes over B tables and a pool, and their threads: small ones do with fewer, which meet sooner.  A compaction goes over every
+// block of the pool and its whole stack, a fork over its bit maps (4 requests of 32 blocks, one CTA against eight, us: compaction in a pool of
+// 4096 blocks 9.0 and 10.2, of 16384 12.6 and 9.8, of 524288 102 and 30; fork of 65536 6.1 and 7.7, of 524288 22.0 and 15.5).
+constexpr int kCompactPool = 16384, kForkPool = 131072;              // blocks from which on eight take the call
+int table_ctas(int B, int width, int n_blocks, int most_blocks) { return (int64_t)B * width > 4096 || n_blocks >= most_blocks ? kMostCtas : 1; }
 int table_threads(int B, int width, int words) { return (int64_t)B * width <= 1024 && words <= 1024 ? 256 : kPageThreads; }
 
 }  // namespace
@@ -415,7 +418,7 @@ int qzo_fork_requests(const int32_t* d_lens, const int32_t* d_parents, int B, co
     constexpr int kMost = (3 * QZO_MAX_REQUESTS + 2 * (QZO_MAX_POOL_BLOCKS / 32)) * (int)sizeof(int);
     QZO_CUDA_TRY(allow_dynamic_smem(fork_requests_kernel, kMost, allowed));
   }
-  const int ctas = table_ctas(B, table_width);
+  const int ctas = table_ctas(B, table_width, n_blocks, kForkPool);
   return launch_serving(fork_requests_kernel, dim3(ctas), dim3(table_threads(B, table_width, words)), (3 * B + 2 * words) * sizeof(int), ctas, (cudaStream_t)stream, p);
 }
 
@@ -427,7 +430,7 @@ int qzo_compact_blocks(const int32_t* d_lens, int B, const int32_t* d_block_tabl
   if (keep <= 0 || keep > n_blocks || max_copies <= 0 || max_copies > QZO_MAX_POOL_BLOCKS) return QZO_ERR_BAD_ARG;
   if (!words_aligned(d_lens, d_block_table, d_block_table_out, d_free, d_free_count_out, d_copies, d_copy_count, d_status)) return QZO_ERR_BAD_ARG;
   QZO_TRY(check_device());
-  const int words = ceil_div(n_blocks, 32), ctas = table_ctas(B, table_width);
+  const int words = ceil_div(n_blocks, 32), ctas = table_ctas(B, table_width, n_blocks, kCompactPool);
   CompactParams p{{d_lens, d_block_table, B, table_width, log2_up(block_size), n_blocks, words, d_block_table_out, d_free, free_capacity, d_free_count_out,
                    d_copies, d_copy_count, max_copies, d_status}, keep, log2_up(ceil_div(words, ctas))};
   {

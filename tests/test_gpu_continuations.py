@@ -261,6 +261,13 @@ def test_compaction_follows_the_oracle(lib, B, block, longest, n_blocks):
             assert [tuple(c) for c in copies[:int(n)].tolist()] == want[2] and (copies[int(n):] == -1).all()
 
 
+@pytest.mark.parametrize("B,block,longest,n_blocks", [(1, 16, 40, 16383), (2, 16, 100, 16384), (5, 32, 200, 131072), (3, 16, 300, 524288), (1, 16, 1, 524288)])
+def test_few_requests_in_a_large_pool(lib, B, block, longest, n_blocks):
+    # how many CTAs take a call goes by the pool too
+    test_compaction_follows_the_oracle(lib, B, block, longest, n_blocks)
+    test_forks_follow_the_oracle_step_after_step(lib, B, block, longest, n_blocks, False)
+
+
 def test_compactions_that_cannot_be_done(lib):
     lens, table = np.array([20, 16, 5], np.int32), np.array([[13, 1], [0, -1], [9, -1]], np.int32)
     good = dict(lens=lens, table=table, keep=5, room=5, most=20)
