@@ -856,8 +856,8 @@ int run_groups(const PagedParams& p, const qzo_kv_cache& c, int64_t units, bool 
   else if (p.unit_items == 8) QZO_TRY((run_attention_w<DH, 1, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
   else QZO_TRY((run_attention_w<DH, 2, F8, 4, Keys::kPrefix>(p, units, p.prefix_splits, st)));
   // Own keys are few as a rule: CTAs of one warp, twelve on an SM, where there are enough rows and key heads (64 rows on one prefix of 4096, 32
-  // key heads, 1 to 32 own keys: 42.1 us in all, 53.9 with four warps), but not where several heads have many parts to join (128 rows of
-  // 8 heads to a key head on 16384, ten parts: 71.8 us and 66.6).
+  // key heads, 1 to 32 own keys: 33.9 us in all, 46.3 with four warps), but not where several heads have many parts to join (128 rows of
+  // 8 heads to a key head on 16384, ten parts: 73.8 us and 68.2).
   const int64_t ctas = (int64_t)p.R * p.Hkv * p.chunks, parts = p.prefix_splits ? p.prefix_splits : p.prefix_ctas / units + 1;
   if (ctas < 3 * kSMs || parts * std::min(p.G, 16) >= 32) QZO_TRY((run_attention<DH, F8, Keys::kOwn>(p, wide, st)));
   else if (p.G <= 8) QZO_TRY((run_attention_w<DH, 1, F8, 1, Keys::kOwn>(p, ctas, p.splits, st)));
@@ -922,7 +922,7 @@ double own_tables_us(int64_t R, int Hkv, double bytes, bool f8) {
 double key_head_bytes(int64_t max_len, int dh, bool f8) { return (double)max_len * dh * (f8 ? 2 : 4); }
 // The least that either way of taking prefixes is estimated at
 constexpr double few_least_us(bool f8) { return f8 ? 9.5 : 8; }
-constexpr double many_least_us(bool f8) { return f8 ? 20 : 21; }
+constexpr double many_least_us(bool f8) { return f8 ? 24 : 15; }
 
 // room: bytes for the results of prefixes and of the rows' own keys; only ways that it holds are taken
 PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int64_t max_len, size_t room = SIZE_MAX) {
@@ -931,17 +931,18 @@ PrefixPlan prefix_plan(int R, int n_groups, int G, int Hkv, int dh, bool f8, int
   const int64_t queries = (int64_t)R * G / std::max(1, std::min(R, n_groups));   // of a group and key head, on average
   const int few_items = queries <= 8 ? 8 : 16;
   // The way whose time is estimated as the shortest, in us: what it takes beside the keys and values, and the bytes of those that its CTAs
-  // ask for.  The rates are those of measurements with 4 to 128 rows in 1 to 16 groups over 4 to 32 key heads of 128 and 256 to 16384 shared
-  // tokens, bf16 (e4m3); most of the rows' own requests are met by L2 where there are many, and e4m3 tiles are held up by their conversion in
-  // the kernel for many queries.  Examples, us through own tables, few, many: 64 rows of 64 queries on 2048 139, 28, 26, on 16384 1033, 139, 62;
-  // 128 rows of 1024 queries on 16384 275, 231, 67 (203, 156, 89); 32 rows of 128 queries on 8192 90, 46, 31 (67, 31, 33).
+  // ask for.  The rates are those of measurements with 4 to 128 rows in 1 to 16 groups over 1 to 32 key heads of 128 and 256 to 16384 shared
+  // tokens, bf16 (e4m3): the way taken was the fastest or within 5 % of it in 140 of 147 calls (144 of 147), off by 24 % at most.  Most of the rows' own
+  // requests are met by L2 where there are many, and e4m3 tiles are held up by their conversion in the kernel for many queries.  Examples, us through
+  // own tables, few, many: 64 rows of 64 queries on 2048 139, 30, 28, on 16384 1032, 156, 68; 128 rows of 1024 queries on 16384 274, 233, 68 (203, 157,
+  // 91); 32 rows of 128 queries on 8192 81, 40, 31 (65, 31, 35).
   // Lengths are known on the device only: all of this goes by the table's width.
   const double bytes = key_head_bytes(max_len, dh, f8), own = own_tables_us(R, Hkv, bytes, f8);
   const double rows = R * (double)Hkv / 400;           // the rows' own keys: a CTA for each row and key head
   const double asked_few = (double)prefix_units(R, n_groups, G, Hkv, few_items) * bytes;
   const double asked_many = std::min(R, n_groups) * std::max(1.0, (double)queries / kPrefixQueries) * Hkv * bytes;   // a unit that is not full costs less
-  const double few = rows + (f8 ? std::min(few_least_us(f8) + asked_few / 5.7e6, 25 + asked_few / 8.1e6) : few_least_us(f8) + asked_few / 8.3e6);
-  const double many = rows + (f8 ? std::min(many_least_us(f8) + asked_many / 1.25e6, 27 + asked_many / 2.4e6) : many_least_us(f8) + asked_many / 6.2e6);
+  const double few = rows + (f8 ? std::min(few_least_us(f8) + asked_few / 5.3e6, 26 + asked_few / 7.7e6) : few_least_us(f8) + asked_few / 8.3e6);
+  const double many = rows + (f8 ? std::min(many_least_us(f8) + asked_many / 1.25e6, 30 + asked_many / 2.15e6) : many_least_us(f8) + asked_many / 6e6);
   const int64_t all = (int64_t)R * G * Hkv, per_result = (dh + 2) * sizeof(float);     // own keys: a result for every query at least
   const int64_t fits = (int64_t)std::min<size_t>(room, INT64_MAX) / per_result - all, line = all + 2 * kSMs * kPrefixQueries;
   const bool few_fits = fits >= all, many_fits = fits >= line;
