@@ -631,6 +631,19 @@ def test_calls_one_behind_the_other_see_what_was_written_before_them(lib, units)
         assert same()
 
 
+@pytest.mark.parametrize("H,Hkv,dh,block,kind", [(8, 8, 64, 16, "bf16"), (32, 8, 128, 32, "bf16"), (96, 8, 64, 16, "bf16"), (80, 4, 64, 16, "bf16"), (8, 8, 128, 16, "e4m3"), (32, 8, 64, 64, "e4m3")])
+def test_rows_with_many_tokens_of_their_own_among_rows_with_few(lib, units, H, Hkv, dh, block, kind):
+    # many rows and key heads, each of which has one CTA for its own keys, whatever their number: from none to thousands, with a prefix, without one and in
+    # front of its end
+    owns = [[3, 700, None, 2100], [513, 512, 514, 1], [5, -20, 40, 1500], [1200, 1030, 1025, 2049], [0, 0, 1, 0], [2048, 1024, 17, 16], [1, 2, 3, 4], [9, 9, 600, 9]]
+    groups = [(4, 130 + 41 * i, owns[i % len(owns)]) for i in range(14)] + [(5, 0, [3000, 5, 513, 4000, 1])]
+    case = Shared(groups, H, Hkv, dh, block, kind, 43)
+    out = case.run(lib)
+    case.check(out)
+    for _ in range(5):
+        assert torch.equal(out.view(torch.int16), case.run(lib).view(torch.int16))
+
+
 def test_one_workspace_as_requests_end_and_groups_become_fewer(lib):
     # sized once for 64 rows in 64 groups; then fewer rows in fewer groups, which take other ways; none writes behind the workspace's end
     H = Hkv = 8
