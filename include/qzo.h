@@ -336,6 +336,9 @@ int qzo_copy_blocks(const qzo_kv_cache* h_caches, int n_caches, const int32_t* d
  * status word: a bounded wait inside a kernel ran out, and the output means nothing.
  * n_blocks * block_size * n_kv_heads < 2^31, n_groups up to 2^20.  d_workspace: qzo_shared_prefix_attention_workspace_bytes, 256-aligned.
  * Where little is shared, every row reads all of its keys through its own table, as in qzo_paged_attention (indices of groups are not looked at then).
+ * Lengths are known on the device only: the way is chosen by the table's width, as if most of it were prefix, and tokens outside of prefixes count as few.
+ * Meant for rows with up to some hundred of these: where there are many rows and key heads, one CTA reads all of a row's own tokens for a key head, while
+ * qzo_paged_attention cuts them into pieces.  A row with thousands of its own among shorter ones is faster in a call of qzo_paged_attention.
  * The workspace's size is that for every call of up to R rows, n_groups groups and tables of max_len tokens: one for the largest serves as
  * requests end. */
 int qzo_shared_prefix_attention_workspace_bytes(int R, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_len, size_t* bytes);

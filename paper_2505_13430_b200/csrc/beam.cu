@@ -87,8 +87,9 @@ __device__ __forceinline__ bool best_head(uint32_t order, uint32_t token, uint32
 // it has met, one to a lane in order.  A logit is a candidate only if it reaches what W others are known to reach: the last of the
 // warp's list, or the least, over the eight warps, of the (W / 8)-th largest of a warp's lanes' maxima, which leaves about twenty of
 // the first tile's 4096 for W = 8; a candidate is put in its place by the whole warp.
-// Bound by instructions: 512 beams of 50272 logits, a fifth of them ended, go by in 24.3 us (29.4 us with the second kernel), 3.4 TB/s.  Without the
-// search for candidates behind the first tile it would be 5.6 us less, without the exponentials 1.8 us.  Copies two tiles ahead into shared
+// 512 beams of 50272 logits, a fifth of them ended, go by in 24.3 us (29.4 us with the second kernel), 3.4 TB/s, bound by loads that no work hides:
+// warps wait for them most, the issue slots are 55 % busy with 20 instructions to a logit, as most tiles have candidates and take the whole search.  Without
+// the search behind the first tile it would be 5.6 us less, without the exponentials 1.8 us.  Copies two tiles ahead into shared
 // memory took 2.6 us more (three CTAs to an SM instead of five); chunks of 12, 4, 3, 2 tiles for many rows 0.0, 0.5, 1.6, 3.0 us.
 // Exponentials are 2^(x c), c = log2 e in fp32: the sums' logarithm is divided by that c in the end, so that its rounding (2^-26) counts
 // for a distribution's entropy only.

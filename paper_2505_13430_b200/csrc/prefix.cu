@@ -153,8 +153,9 @@ __device__ __forceinline__ uint32_t weights_at(uint32_t scores, int j, int c, in
 // the reference by 2^8.
 // Bound by the chain of a tile: 2350 cycles for the two tiles of an SM's CTAs, of which the tensor pipe is busy 1790 (8 x 48 for Q K^T, 8 x 64 for
 // P V with its two terms, for each) and the exponentials' pipe 1024; with start (5 us) and end 128 rows of 8 heads to each of 4 key heads on
-// 2 prefixes of 16384 take 58 us of the call's 68.  One place for the scores and another for the weights took 0.9 us more, tiles of 128 keys with
-// one CTA on an SM 30 us more, eight softmax warps 8 us more.  e4m3 pages are bound by their conversion, 3300 cycles.
+// 2 prefixes of 16384 take 58 us of the call's 71.  One place for the scores and another for the weights took 0.9 us more, tiles of 128 keys with
+// one CTA on an SM 30 us more, eight softmax warps 8 us more.  Over e4m3 pages
+// two tiles take 3300 cycles with no pipe above 31 % and issue at 37 %: the conversion's latency, not its instructions, is in the chain there.
 // A wait goes by the parity of a phase, so that a barrier must not be two phases ahead of whoever waits: scores j + 2 come after values j,
 // those after weights j, those after scores j have been read, and tiles in turn have barriers of their own.
 template <int DH, bool F8>
