@@ -1006,6 +1006,7 @@ def test_decode_of_groups_in_buffers_of_any_size(lib, path, max_tokens):
     plain, shared = step.plain(), step.shared()
     assert _close(shared, plain)
     assert path == 2 or torch.equal(shared, plain)
+    assert torch.equal(step.plain(), plain), "what stands behind the buffer, the table of rotations among it, is as it was"
     assert step.reads_once() == (path == 2), "only units of few queries fit"
     step.gm.close()
 
